@@ -70,6 +70,23 @@ extern "C" {
 /* ---- formats -------------------------------------------------------- */
 #define JF_FMT_AFFINE4_G64 0      /* affine 4-bit, 64-element groups (above) */
 #define JF_FMT_TQ4         1      /* TQ4 (Sec. 3.1 Eq. 4), see below         */
+#define JF_FMT_E4M3_B32    8      /* 8-bit e4m3, one scale per 32 positions
+                                     and KV head, see below                 */
+
+/*
+ * 8-bit block format (no paper counterpart: a cache with twice the bytes of
+ * the 4-bit formats and a relative error of at most 2^-4 per element).  The
+ * codes are e4m3 values (1 sign, 4 exponent, 3 mantissa bits; bias 7; largest
+ * 448); positions 32 j .. 32 j + 31 of a KV head share a scale 2^e for K and
+ * one for V:  x_hat = code * 2^e.  e is the smallest exponent with
+ * max|x| <= 448 * 2^e over the block's finite values, limited to [-40, 40]
+ * (so magnitudes past 448 * 2^40 saturate, infinities too; NaN stays NaN).
+ *   page record = [K codes: Hkv x P x D bytes][V codes: same]
+ *                 [K scales: Hkv x P/32 x fp32][V scales: same]
+ * page_bytes = 2*Hkv*(P*D + P/8), 2,049 bytes per position and layer at
+ * Hkv 4, D 256.  A reader takes a scale word's exponent bits alone and limits
+ * them to [-40, 40].
+ */
 
 /*
  * TQ4 format (Sec. 3.1 Eq. 4; App. A.1 Table 3).  A vector x of D elements is
@@ -103,8 +120,9 @@ typedef struct jf_kv_pool {
   int32_t page_size;     /* P: 64, 128 or 256 positions                    */
   int32_t num_kv_heads;  /* Hkv >= 1                                       */
   int32_t head_dim;      /* D: 128 or 256                                  */
-  int32_t group_size;    /* 64 (affine format; ignored for TQ4)            */
-  int32_t format;        /* JF_FMT_AFFINE4_G64 or JF_FMT_TQ4               */
+  int32_t group_size;    /* 64 (affine format; ignored for the others)     */
+  int32_t format;        /* JF_FMT_AFFINE4_G64, JF_FMT_TQ4 or
+                            JF_FMT_E4M3_B32                                */
   const jf_tq4_codec* tq4;  /* host pointer, read during each call;
                                required for JF_FMT_TQ4, else ignored       */
 } jf_kv_pool;
@@ -212,6 +230,11 @@ int jf_kv_quantize_append(const jf_kv_pool* pool, const int32_t* page_table, int
  * pools the same way (the fused step encodes the new rows exactly as
  * jf_kv_quantize_append does); the no-workspace variant returns
  * JF_ERR_UNSUPPORTED for them.
+ * E4M3 pools: codes enter fp16 products exactly and q after a power-of-two
+ * scale per head; block scales are applied to the fp32 scores and, as
+ * exponents, to the probabilities before they enter fp16 (rounded relative to
+ * the largest of 2^score * V scale met so far, so blocks of very different
+ * scales keep their precision); no V scale is out of range.
  */
 int jf_paged_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
                          const int32_t* context_lens, int32_t batch, const void* q,
@@ -279,7 +302,7 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * already hold the chunk's own rows (append, then attend).
  *   page_table_row  int32 [>= ceil((q_start + chunk_len) / P)]
  *   q, out          bf16 [chunk_len, Hq, D]
- *   workspace       affine pool: >= jf_prefill_workspace_bytes() (an int32
+ *   workspace       affine or E4M3 pool: >= jf_prefill_workspace_bytes() (an int32
  *                   status word); TQ4 pool: >= jf_prefill_batch_workspace_bytes(
  *                   JF_FMT_TQ4, chunk_len, Hq, D, 1), 256-byte aligned.
  * Wave balance: the kernel runs one CTA per SM, two per pair.  A chunk over
@@ -304,6 +327,9 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * workspace), K and V tiles are built in shared memory as norm * centroid
  * (fp16) in the rotated basis, and each output row is rotated back
  * (S_V H / sqrt(D)) as the partials are merged.
+ * E4M3 pools: workspaces as for affine pools; the tiles hold the codes as fp16
+ * (exact) and the block scales are applied as in the decode; no scale is out
+ * of range.
  */
 int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
                           const void* q, int32_t q_start, int32_t chunk_len, int32_t num_q_heads,
@@ -341,12 +367,12 @@ size_t jf_prefill_chunk_workspace_bytes(const jf_kv_pool* pool, int32_t q_start,
  *   workspace    >= jf_prefill_batch_workspace_bytes(pool->format,
  *                sum_b chunk_len[b], Hq, D, num_splits) bytes, 256-byte
  *                aligned; its first int32 is the device status word.
- * The longest request's query tiles are scheduled first.  Either format.
+ * The longest request's query tiles are scheduled first.  Any format.
  */
 #define JF_PREFILL_MAX_BATCH 64
 
 /* Workspace of a prefill launch over a pool of `format`: 256 bytes for an
- * affine pool with num_splits == 1; else 256 + roundup(8 R S, 256) + 4 R S D,
+ * affine or E4M3 pool with num_splits == 1; else 256 + roundup(8 R S, 256) + 4 R S D,
  * R = total_rows * Hq (the split partials), plus 4 R D for a TQ4 pool (its
  * rotated queries).  0 for invalid arguments. */
 size_t jf_prefill_batch_workspace_bytes(int32_t format, int64_t total_rows, int32_t num_q_heads,
@@ -370,7 +396,7 @@ int64_t jf_reservation_pages(int64_t prompt_len, int64_t output_len, int64_t g_o
 
 /*
  * Page-gather checkpoint (Sec. 3.4: read the request's page runs in place and
- * emit one packed stream).  Either format.  dst[k * page_bytes .. (k+1) * page_bytes) =
+ * emit one packed stream).  Any format.  dst[k * page_bytes .. (k+1) * page_bytes) =
  * page record page_table_row[k] for k < num_pages, tail bytes included.
  *   dst        device buffer, >= num_pages * page_bytes bytes, 16-byte aligned
  *   err_flag   device int32 or NULL (JF_DEV_ERR_PAGE_ID for bad ids; the
@@ -382,7 +408,7 @@ int jf_kv_checkpoint(const jf_kv_pool* pool, const int32_t* page_table_row, int3
 /*
  * Restore (Sec. 3.4: restoration writes packed runs into the existing pool):
  * the inverse of jf_kv_checkpoint.  Page record page_table_row[k] of the pool
- * = src[k * page_bytes ..).  Page ids must be distinct.  Either format.
+ * = src[k * page_bytes ..).  Page ids must be distinct.  Any format.
  */
 int jf_kv_restore(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t num_pages,
                   const void* src, size_t src_bytes, int32_t* err_flag, void* stream);
@@ -432,6 +458,155 @@ int jf_paged_decode_attn_noalloc(const jf_kv_pool* pool, const int32_t* page_tab
                                  int32_t pt_stride, const int32_t* context_lens, int32_t batch,
                                  const void* q, int32_t num_q_heads, float softmax_scale,
                                  void* out, int32_t num_splits, int32_t* err_flag, void* stream);
+
+/* ======================================================================
+ * Rotary positions with several axes
+ * ====================================================================== */
+#define JF_ROPE_PAIR_HALF     0   /* pair i is channels (i, i + R/2)         */
+#define JF_ROPE_PAIR_ADJACENT 1   /* pair i is channels (2 i, 2 i + 1)       */
+#define JF_ROPE_MAX_AXES      3
+#define JF_DTYPE_BF16 0
+#define JF_DTYPE_F16  1
+#define JF_DTYPE_F32  2
+
+typedef struct jf_rope {          /* host, read during each call             */
+  int32_t rotary_dim;             /* R: channels turned, a multiple of 16,
+                                     16 <= R <= 256; the rest pass through   */
+  int32_t pairing;                /* JF_ROPE_PAIR_*                          */
+  int32_t num_axes;               /* 1 .. JF_ROPE_MAX_AXES                   */
+  float   inv_freq[128];          /* radians per position of pair i < R/2,
+                                     finite, |inv_freq| < 2^32               */
+  uint8_t axis[128];              /* axis of pair i, < num_axes              */
+} jf_rope;
+
+typedef struct jf_rope_rows {     /* the queries' or the keys' rows          */
+  const void* in;                 /* device, 16-byte aligned                 */
+  void*       out;                /* device, 16-byte aligned; `in` itself is
+                                     allowed, other overlaps are not         */
+  int64_t in_token_stride, in_head_stride;    /* in elements, each a multiple  */
+  int64_t out_token_stride, out_head_stride;  /* of 16 bytes; channels adjoin  */
+  int32_t num_heads;              /* 0: none (the pointers are not used)     */
+} jf_rope_rows;
+
+/*
+ * Turn the first R channels of every query and key head: pair i of token t's
+ * heads, (x, y), becomes (x cos p - y sin p, x sin p + y cos p) with
+ * p = positions[axis_i, t] * inv_freq_i; inverse != 0 turns by -p, which is
+ * the gradient of the forward call (dL/d in from dL/d out).
+ *   positions   int32 [num_axes, n_tokens] on the device, axis rows
+ *               pos_stride elements apart; any int32 value
+ *   q, k        host structs; head_dim channels a head (a multiple of 16,
+ *               R <= head_dim <= 512), elements of type `dtype`
+ * Numerics: angles are exact to 2^-32 of a turn at any position; products in
+ * fp32, one rounding to the element type.  n_tokens == 0 is a no-op.
+ */
+int jf_rope_axes(const jf_rope* rope, const int32_t* positions, int64_t pos_stride,
+                 int32_t n_tokens, int32_t head_dim, const jf_rope_rows* q, const jf_rope_rows* k,
+                 int32_t dtype, int32_t inverse, void* stream);
+
+/* ======================================================================
+ * The 8-bit block-scaled cache (pools of format JF_FMT_E4M3_B32)
+ *
+ * Attention reads such pools through jf_paged_decode_attn (one query token),
+ * jf_paged_decode_weights_attn below, jf_prefill_chunk_attn and
+ * jf_prefill_batch_attn; jf_kv_checkpoint and jf_kv_restore copy their pages.
+ * jf_kv_quantize_append, jf_paged_decode_append_attn, jf_paged_verify_attn and
+ * the no-workspace decode return JF_ERR_UNSUPPORTED for them.
+ * ====================================================================== */
+
+/*
+ * Append runs of rows.  Rows row_offsets[b] .. row_offsets[b + 1] - 1 of k and
+ * v go to positions start_pos[b], start_pos[b] + 1, ... of request b.  A block
+ * of 32 positions whose first one is written starts afresh; a block that
+ * already holds positions (below start_pos[b]) keeps the larger of its scale
+ * and the new rows', and when that grows its earlier codes are rounded again
+ * under it (exactly, but for what falls below the smallest code).
+ *   page_table   int32 [num_requests, pt_stride]
+ *   start_pos    int32 [num_requests] on the device
+ *   row_offsets  int32 [num_requests + 1] on the device, from 0 up, <= n_rows
+ *   k, v         bf16, row i at k + i * k_stride elements, its Hkv x D
+ *                elements adjoining; 16-byte aligned, strides multiples of 8
+ *   n_rows       rows of k and v, >= row_offsets[num_requests]; 0: a no-op
+ *   err_flag     device int32 or NULL: JF_DEV_ERR_POSITION for a request whose
+ *                offsets or positions do not fit (it is skipped),
+ *                JF_DEV_ERR_PAGE_ID for a page outside the pool (its block is)
+ * No two requests may append to the same block in one call.
+ */
+int jf_kv8_append(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                  int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                  const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  int32_t n_rows, int32_t* err_flag, void* stream);
+
+/*
+ * Read runs of positions back as bf16 values code * 2^e (exact): the inverse
+ * addressing of jf_kv8_append, into k and v.  Rows of no request, and those of
+ * a request or page that err_flag reports, are left as they are.
+ */
+int jf_kv8_read(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t n_rows,
+                int32_t* err_flag, void* stream);
+
+/* Workspace bytes of jf_paged_decode_weights_attn: that of
+ * jf_paged_decode_attn (rounded up to 256) and 4 * batch * Hq * weight_stride
+ * for the scores.  0 for invalid arguments. */
+size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                         int32_t head_dim, int32_t num_splits,
+                                         int64_t weight_stride);
+
+/*
+ * jf_paged_decode_attn on an 8-bit pool that also adds up what each position
+ * is attended with:
+ *   weights_out[b, h, t] = weights_in[b, h, t] + sum over the Hq / Hkv query
+ *   heads of KV head h of softmax_t, for t < context_lens[b];
+ * elements past the context are not written.
+ *   weights_in   fp32 [batch, Hkv, weight_stride] or NULL (zeros)
+ *   weights_out  fp32, same layout; weights_in itself is allowed
+ *   weight_stride >= every context length (JF_DEV_ERR_POSITION in the status
+ *                word otherwise: positions past it are then not attended)
+ *   workspace    >= jf_decode_weights_workspace_bytes(...), 256-byte aligned
+ * Other arguments, limits and errors as for jf_paged_decode_attn.
+ */
+int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_table,
+                                 int32_t pt_stride, const int32_t* context_lens, int32_t batch,
+                                 const void* q, int32_t num_q_heads, float softmax_scale,
+                                 void* out, const float* weights_in, float* weights_out,
+                                 int64_t weight_stride, void* workspace, size_t workspace_bytes,
+                                 int32_t num_splits, void* stream);
+
+/*
+ * Eviction by accumulated attention weight.  Each (request, KV head) keeps
+ * min(context, budget) positions: the first `sinks`, the last `recent`, and of
+ * the others those with the largest weights (equal weights: the lower
+ * position; NaN counts least).  Kept positions move, in order, to positions
+ * 0, 1, ... of dst_page_table's pages -- each KV head its own -- where every
+ * block of 32 takes the scale its rows call for (jf_kv8_append's rule).  The
+ * source pages are left as they are, so they may be shared with other
+ * requests.
+ *   page_table      int32 [batch, pt_stride]
+ *   context_lens    int32 [batch]
+ *   weights         fp32 [batch, Hkv, weight_stride], weight_stride >= every
+ *                   context length
+ *   budget          >= 1;  sinks, recent >= 0, sinks + recent <= budget
+ *   dst_page_table  int32 [batch, dst_stride]: pages of the same pool for
+ *                   ceil(min(context, budget) / P) positions a request, none of
+ *                   them among any request's source pages
+ *   dst_context_lens int32 [batch], written
+ *   dst_weights     fp32 [batch, Hkv, budget] or NULL: the kept weights, zeros
+ *                   past them; may not overlap weights
+ *   kept            int32 [batch, Hkv, budget]: the kept positions in rising
+ *                   order, -1 past them
+ *   err_flag        device int32 or NULL: JF_DEV_ERR_POSITION for a context
+ *                   that does not fit its table or weights (kept as empty) or
+ *                   a destination row too short, JF_DEV_ERR_PAGE_ID for a page
+ *                   outside the pool (a source row then reads as zeros, a
+ *                   destination block is not written)
+ */
+int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                 const int32_t* context_lens, int32_t batch, const float* weights,
+                 int64_t weight_stride, int32_t budget, int32_t sinks, int32_t recent,
+                 const int32_t* dst_page_table, int32_t dst_stride, int32_t* dst_context_lens,
+                 float* dst_weights, int32_t* kept, int32_t* err_flag, void* stream);
 
 /* Human-readable name of a JF_* status code. */
 const char* jf_status_string(int status);

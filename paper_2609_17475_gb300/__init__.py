@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     JF_FMT_AFFINE4_G64, JF_FMT_TQ4, Tq4Codec, jf_kv_page_bytes_fmt, jf_tq4_codebook,
     jf_prefill_batch_attn, jf_reservation_pages, prefill_batch_workspace, default_prefill_splits,
     jf_prefill_chunk_workspace_bytes, prefill_chunk_workspace,
+    JF_FMT_E4M3_B32, JF_KV8_BLOCK, Rope, jf_rope_axes, jf_kv8_append, jf_kv8_read,
+    jf_paged_decode_weights_attn, decode_weights_workspace, jf_kv8_evict,
 )

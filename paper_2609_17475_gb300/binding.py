@@ -28,6 +28,11 @@ JF_DEV_ERR_LAYOUT = 8
 JF_DEV_ERR_RANGE = 16
 JF_FMT_AFFINE4_G64 = 0
 JF_FMT_TQ4 = 1
+JF_FMT_E4M3_B32 = 8
+JF_KV8_BLOCK = 32           # positions that share a scale in an E4M3 pool
+JF_ROPE_PAIR_HALF = 0
+JF_ROPE_PAIR_ADJACENT = 1
+JF_ROPE_MAX_AXES = 3
 
 EXPORTS = [
     "jf_kv_page_bytes", "jf_attn_workspace_bytes", "jf_prefill_workspace_bytes",
@@ -36,7 +41,8 @@ EXPORTS = [
     "jf_paged_decode_attn_noalloc", "jf_paged_decode_append_attn", "jf_paged_verify_attn",
     "jf_kv_page_bytes_fmt", "jf_tq4_codebook", "jf_prefill_batch_attn", "jf_reservation_pages",
     "jf_prefill_batch_workspace_bytes", "jf_prefill_chunk_workspace_bytes",
-    "jf_selftest_bounded_wait",
+    "jf_selftest_bounded_wait", "jf_rope_axes", "jf_kv8_append", "jf_kv8_read",
+    "jf_decode_weights_workspace_bytes", "jf_paged_decode_weights_attn", "jf_kv8_evict",
 ]
 JF_STATIC_WORKSPACE_BYTES = 8 << 20
 
@@ -57,6 +63,19 @@ class _Pool(ctypes.Structure):
                 ("page_size", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("group_size", ctypes.c_int32),
                 ("format", ctypes.c_int32), ("tq4", ctypes.POINTER(_Tq4Codec))]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("pairing", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32), ("inv_freq", ctypes.c_float * 128),
+                ("axis", ctypes.c_uint8 * 128)]
+
+
+class _RopeRows(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("in_token_stride", ctypes.c_int64), ("in_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("num_heads", ctypes.c_int32)]
 
 
 _lib = None
@@ -97,6 +116,16 @@ def lib() -> ctypes.CDLL:
             "jf_prefill_chunk_workspace_bytes": (SZ, [PP, I32, I32, I32, I32]),
             "jf_reservation_pages": (I64, [I64, I64, I64, I32]),
             "jf_selftest_bounded_wait": (ctypes.c_int, [P, I32, P]),
+            "jf_rope_axes": (ctypes.c_int, [ctypes.POINTER(_Rope), P, I64, I32, I32,
+                                            ctypes.POINTER(_RopeRows), ctypes.POINTER(_RopeRows),
+                                            I32, I32, P]),
+            "jf_kv8_append": (ctypes.c_int, [PP, P, I32, I32, P, P, P, I64, P, I64, I32, P, P]),
+            "jf_kv8_read": (ctypes.c_int, [PP, P, I32, I32, P, P, P, I64, P, I64, I32, P, P]),
+            "jf_decode_weights_workspace_bytes": (SZ, [I32, I32, I32, I32, I32, I64]),
+            "jf_paged_decode_weights_attn": (ctypes.c_int, [PP, P, I32, P, I32, P, I32, F32, P, P,
+                                                            P, I64, P, SZ, I32, P]),
+            "jf_kv8_evict": (ctypes.c_int, [PP, P, I32, P, I32, P, I64, I32, I32, I32, P, I32, P,
+                                            P, P, P, P]),
             "jf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "jf_version": (ctypes.c_char_p, []),
         }
@@ -200,8 +229,8 @@ class Tq4Codec:
 
 @dataclasses.dataclass
 class KVPool:
-    """A paged 4-bit KV pool: ``data`` is a CUDA uint8 tensor [num_pages, page_bytes].
-    ``codec`` is required for the TQ4 format."""
+    """A paged KV pool (4-bit, or 8-bit with JF_FMT_E4M3_B32): ``data`` is a CUDA uint8
+    tensor [num_pages, page_bytes].  ``codec`` is required for the TQ4 format."""
     data: torch.Tensor
     page_size: int
     num_kv_heads: int
@@ -587,10 +616,237 @@ def default_num_splits(batch: int, num_kv_heads: int, device=None,
                        format: int = JF_FMT_AFFINE4_G64, num_sms: Optional[int] = None) -> int:
     """Split cap per (request, KV head) so the split grid fills every SM slot
     once (two split CTAs per SM for the affine format, one for TQ4, whose
-    centroid table takes a CTA's spare shared memory).  A batch plans its
+    centroid table takes a CTA's spare shared memory, and for E4M3).  A batch plans its
     splits over all requests together, and its workspace then needs room for
     about two more splits per request than an even share (rounding up per
     request)."""
-    target = (1 if format == JF_FMT_TQ4 else 2) * _num_sms(device, num_sms)
+    one = format in (JF_FMT_TQ4, JF_FMT_E4M3_B32)
+    target = (1 if one else 2) * _num_sms(device, num_sms)
     per = -(-target // (batch * num_kv_heads))
     return max(1, per if batch == 1 else per + 2)
+
+
+# ---------------------------------------------------------------------------
+# rotary positions with several axes
+# ---------------------------------------------------------------------------
+_ROPE_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+class Rope:
+    """Rotary embedding of the first ``rotary_dim`` channels of each head over one
+    to three position axes (say time, height, width).
+
+    ``sections`` counts the pairs of each axis (their sum is rotary_dim / 2).
+    ``layout`` "sectioned": the first sections[0] pairs turn with axis 0, the
+    next with axis 1, ...; "interleaved": pair i turns with axis i % n while
+    i < n * sections[i % n] (n axes), else with axis 0.  ``axis`` (one axis
+    index per pair) replaces both.  ``pairing`` "half": pair i is channels
+    (i, i + rotary_dim / 2); "adjacent": channels (2 i, 2 i + 1).  Frequencies
+    are base ** (-2 i / rotary_dim), or ``inv_freq`` when given."""
+
+    def __init__(self, rotary_dim: int, sections=None, base: float = 1e4,
+                 layout: str = "sectioned", pairing: str = "half", inv_freq=None, axis=None):
+        import numpy as np
+        if rotary_dim < 16 or rotary_dim % 16 or rotary_dim > 256:
+            raise ValueError("rotary_dim must be a multiple of 16 from 16 to 256")
+        half = rotary_dim // 2
+        if layout not in ("sectioned", "interleaved"):
+            raise ValueError("layout must be 'sectioned' or 'interleaved'")
+        if pairing not in ("half", "adjacent"):
+            raise ValueError("pairing must be 'half' or 'adjacent'")
+        sections = [half] if sections is None else [int(n) for n in sections]
+        if not 1 <= len(sections) <= JF_ROPE_MAX_AXES or min(sections) < 0 or sum(sections) != half:
+            raise ValueError("sections must be one to three counts that add up to rotary_dim / 2")
+        n = len(sections)
+        if axis is None:
+            if layout == "sectioned":
+                axis = [a for a, m in enumerate(sections) for _ in range(m)]
+            else:
+                axis = [i % n if i < n * sections[i % n] else 0 for i in range(half)]
+        axis = np.asarray(axis, dtype=np.int64)
+        if inv_freq is None:
+            inv_freq = float(base) ** (-np.arange(half, dtype=np.float64) / half)
+        f = np.asarray(inv_freq, dtype=np.float64).astype(np.float32)
+        if axis.shape != (half,) or f.shape != (half,):
+            raise ValueError("one axis and one frequency per pair")
+        if axis.min() < 0 or axis.max() >= n:
+            raise ValueError("axis out of range")
+        self.rotary_dim, self.num_axes, self.pairing = int(rotary_dim), n, pairing
+        self.inv_freq, self.axis = f, axis
+        c = self._c = _Rope()
+        c.rotary_dim = rotary_dim
+        c.pairing = JF_ROPE_PAIR_HALF if pairing == "half" else JF_ROPE_PAIR_ADJACENT
+        c.num_axes = n
+        for i in range(half):
+            c.inv_freq[i] = float(f[i])
+            c.axis[i] = int(axis[i])
+        self._ref = ctypes.byref(c)
+
+
+def _rope_rows(x: Optional[torch.Tensor], out: Optional[torch.Tensor], n: int, name: str):
+    if x is None:
+        return _RopeRows(), None, 0
+    o = x if out is None else out
+    if x.dim() != 3 or o.shape != x.shape or x.shape[0] != n:
+        raise ValueError(f"{name} must be [tokens, heads, head_dim], its output the same")
+    if x.dtype not in _ROPE_DTYPES or o.dtype != x.dtype or not x.is_cuda or not o.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor of bf16, fp16 or fp32, its output the same")
+    xs, os_ = x.stride(), o.stride()
+    if xs[2] != 1 or os_[2] != 1:
+        raise ValueError(f"{name}: the channels of a head must adjoin")
+    return (_RopeRows(x.data_ptr(), o.data_ptr(), xs[0], xs[1], os_[0], os_[1], x.shape[1]),
+            x.dtype, x.shape[2])
+
+
+@_traced
+def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
+                 q_out: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> None:
+    """Turn query and key rows [tokens, heads, head_dim] (either may be None) by
+    their positions, int32 [axes, tokens]; outputs default to in place.  With
+    ``inverse`` the gradient of that: q, k are then the outputs' gradients."""
+    if not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or not positions.is_cuda:
+        raise TypeError("positions must be a CUDA tensor of dtype torch.int32")
+    if positions.dim() != 2 or positions.shape[0] != rope.num_axes or (
+            positions.shape[1] > 1 and positions.stride(1) != 1):
+        raise ValueError("positions must be [axes, tokens], the tokens of an axis adjoining")
+    n = positions.shape[1]
+    qr, qt, qd = _rope_rows(q, q_out, n, "q")
+    kr, kt, kd = _rope_rows(k, k_out, n, "k")
+    if qt is None and kt is None:
+        raise ValueError("q or k is needed")
+    if qt is not None and kt is not None and (qt != kt or qd != kd):
+        raise ValueError("q and k must have one dtype and head_dim")
+    _check("jf_rope_axes",
+           lib().jf_rope_axes(rope._ref, positions.data_ptr(), positions.stride(0), n, qd or kd,
+                              ctypes.byref(qr), ctypes.byref(kr), _ROPE_DTYPES[qt or kt],
+                              int(bool(inverse)), _stream(stream)))
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit block-scaled cache
+# ---------------------------------------------------------------------------
+def _kv8_rows(fn: str, pool: KVPool, page_table, start_pos, row_offsets, k, v, err_flag, stream):
+    _need(page_table, torch.int32, "page_table")
+    _need(start_pos, torch.int32, "start_pos")
+    _need(row_offsets, torch.int32, "row_offsets")
+    n = k.shape[0]
+    for name, x in (("k", k), ("v", v)):
+        if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or not x.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
+        if tuple(x.shape) != (n, pool.num_kv_heads, pool.head_dim):
+            raise ValueError(f"{name} must be [rows, Hkv, D]")
+        if n and (x.stride(2) != 1 or (pool.num_kv_heads > 1 and x.stride(1) != pool.head_dim)):
+            raise ValueError(f"{name}: the elements of a row must adjoin")
+    pt = page_table if page_table.dim() == 2 else page_table.view(1, -1)
+    B = pt.shape[0]
+    if start_pos.numel() != B or row_offsets.numel() != B + 1:
+        raise ValueError("one start_pos per page-table row, and one row offset more")
+    if err_flag is not None:
+        _need(err_flag, torch.int32, "err_flag")
+    row = pool.num_kv_heads * pool.head_dim
+    # the row stride of a single row is whatever a slicing left: it is not used
+    ks, vs = (k.stride(0), v.stride(0)) if n > 1 else (row, row)
+    st = getattr(lib(), fn)(ctypes.byref(pool.c_struct()), pt.data_ptr(), pt.shape[1], B,
+                            start_pos.data_ptr(), row_offsets.data_ptr(), k.data_ptr(), ks,
+                            v.data_ptr(), vs, n, None if err_flag is None else err_flag.data_ptr(),
+                            _stream(stream))
+    _check(fn, st)
+
+
+@_traced
+def jf_kv8_append(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
+                  row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                  err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Append rows row_offsets[b] .. row_offsets[b + 1] - 1 of k and v (bf16 [rows,
+    Hkv, D], rows any stride apart) at positions start_pos[b] .. of request b."""
+    _kv8_rows("jf_kv8_append", pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+
+
+@_traced
+def jf_kv8_read(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
+                row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Read runs of positions back into k and v as bf16 values (exact)."""
+    _kv8_rows("jf_kv8_read", pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+
+
+def decode_weights_workspace(batch, num_q_heads, num_kv_heads, head_dim, num_splits,
+                             weight_stride, device="cuda"):
+    n = int(lib().jf_decode_weights_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim,
+                                                    num_splits, weight_stride))
+    if n == 0:
+        raise ValueError("invalid workspace geometry")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+@_traced
+def jf_paged_decode_weights_attn(pool: KVPool, page_table: torch.Tensor,
+                                 context_lens: torch.Tensor, q: torch.Tensor,
+                                 softmax_scale: float, out: torch.Tensor,
+                                 weights_in: Optional[torch.Tensor], weights_out: torch.Tensor,
+                                 workspace: torch.Tensor, num_splits: int, stream=None) -> None:
+    """jf_paged_decode_attn on an 8-bit pool that also adds what each position is
+    attended with, summed over a KV head's query heads, to weights_in (fp32
+    [batch, Hkv, stride], None: zeros); weights_out may be weights_in."""
+    _need(page_table, torch.int32, "page_table")
+    _need(context_lens, torch.int32, "context_lens")
+    _need(q, torch.bfloat16, "q")
+    _need(out, torch.bfloat16, "out")
+    _need(weights_out, torch.float32, "weights_out")
+    _need(workspace, torch.uint8, "workspace")
+    B, Hq, D = q.shape
+    if out.shape != q.shape or D != pool.head_dim or page_table.shape[0] != B or context_lens.numel() != B:
+        raise ValueError("shape mismatch")
+    if weights_out.dim() != 3 or tuple(weights_out.shape[:2]) != (B, pool.num_kv_heads):
+        raise ValueError("weights must be [batch, Hkv, stride]")
+    if weights_in is not None:
+        _need(weights_in, torch.float32, "weights_in")
+        if weights_in.shape != weights_out.shape:
+            raise ValueError("weights_in and weights_out must have one shape")
+    st = lib().jf_paged_decode_weights_attn(
+        ctypes.byref(pool.c_struct()), page_table.data_ptr(), page_table.shape[1],
+        context_lens.data_ptr(), B, q.data_ptr(), Hq, float(softmax_scale), out.data_ptr(),
+        None if weights_in is None else weights_in.data_ptr(), weights_out.data_ptr(),
+        weights_out.shape[2], workspace.data_ptr(), workspace.numel(), int(num_splits),
+        _stream(stream))
+    _check("jf_paged_decode_weights_attn", st)
+
+
+@_traced
+def jf_kv8_evict(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Tensor,
+                 weights: torch.Tensor, budget: int, sinks: int, recent: int,
+                 dst_page_table: torch.Tensor, dst_context_lens: torch.Tensor,
+                 dst_weights: Optional[torch.Tensor], kept: torch.Tensor,
+                 err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Keep min(context, budget) positions of every request and KV head -- the first
+    ``sinks``, the last ``recent`` and the heaviest of the others -- and move them, in
+    order, to the pages of dst_page_table.  kept and dst_weights are [batch, Hkv, budget]."""
+    _need(page_table, torch.int32, "page_table")
+    _need(context_lens, torch.int32, "context_lens")
+    _need(weights, torch.float32, "weights")
+    _need(dst_page_table, torch.int32, "dst_page_table")
+    _need(dst_context_lens, torch.int32, "dst_context_lens")
+    _need(kept, torch.int32, "kept")
+    B, H = page_table.shape[0], pool.num_kv_heads
+    if context_lens.numel() != B or dst_context_lens.numel() != B or dst_page_table.dim() != 2 or dst_page_table.shape[0] != B:
+        raise ValueError("one row per request")
+    if weights.dim() != 3 or tuple(weights.shape[:2]) != (B, H):
+        raise ValueError("weights must be [batch, Hkv, stride]")
+    if tuple(kept.shape) != (B, H, int(budget)):
+        raise ValueError("kept must be [batch, Hkv, budget]")
+    if dst_weights is not None:
+        _need(dst_weights, torch.float32, "dst_weights")
+        if dst_weights.shape != kept.shape:
+            raise ValueError("dst_weights must be [batch, Hkv, budget]")
+    if err_flag is not None:
+        _need(err_flag, torch.int32, "err_flag")
+    st = lib().jf_kv8_evict(
+        ctypes.byref(pool.c_struct()), page_table.data_ptr(), page_table.shape[1],
+        context_lens.data_ptr(), B, weights.data_ptr(), weights.shape[2], int(budget), int(sinks),
+        int(recent), dst_page_table.data_ptr(), dst_page_table.shape[1],
+        dst_context_lens.data_ptr(), None if dst_weights is None else dst_weights.data_ptr(),
+        kept.data_ptr(), None if err_flag is None else err_flag.data_ptr(), _stream(stream))
+    _check("jf_kv8_evict", st)

@@ -36,6 +36,18 @@ int launch_prefill_batch(const Geom&, const jf_kv_pool&, const int32_t* const*, 
                          int32_t, void*, void*, cudaStream_t, int32_t, int64_t,
                          const Tq4Params*);
 size_t prefill_workspace_bytes(int64_t rows, int64_t Hq, int64_t D, int64_t S, int fmt);
+int launch_rope(const jf_rope&, const int32_t*, int64_t, int32_t, int32_t, const jf_rope_rows&,
+                const jf_rope_rows&, int32_t, int32_t, cudaStream_t);
+int launch_kv8_rows(const Geom&, const jf_kv_pool&, const int32_t*, int32_t, int32_t,
+                    const int32_t*, const int32_t*, void*, int64_t, void*, int64_t, int32_t,
+                    int32_t*, bool, cudaStream_t);
+int kv8_box_rows();
+int launch_kv8_decode(const Geom&, const jf_kv_pool&, const CUtensorMap&, const int32_t*, int32_t,
+                      const int32_t*, int32_t, const void*, int32_t, float, void*, void*, int32_t,
+                      float*, const float*, float*, int64_t, cudaStream_t);
+int launch_kv8_evict(const Geom&, const jf_kv_pool&, const int32_t*, int32_t, const int32_t*,
+                     int32_t, const float*, int64_t, int32_t, int32_t, int32_t, const int32_t*,
+                     int32_t, int32_t*, float*, int32_t*, int32_t*, cudaStream_t);
 int sm_count();
 }  // namespace jfkv
 
@@ -74,6 +86,25 @@ int check_pool_any(const jf_kv_pool* pool) {
   return JF_OK;
 }
 
+// Pools of the 8-bit block format.
+int check_pool8(const jf_kv_pool* pool) {
+  if (!pool || !pool->base || !aligned(pool->base, 16)) return JF_ERR_INVALID_ARG;
+  if (pool->num_pages < 1 || pool->num_kv_heads < 1) return JF_ERR_INVALID_ARG;
+  if (pool->format != JF_FMT_E4M3_B32) return JF_ERR_UNSUPPORTED;
+  if (pool->head_dim != 128 && pool->head_dim != 256) return JF_ERR_UNSUPPORTED;
+  if (pool->page_size != 64 && pool->page_size != 128 && pool->page_size != 256)
+    return JF_ERR_UNSUPPORTED;
+  if (pool->num_kv_heads > 65535) return JF_ERR_UNSUPPORTED;
+  if (pool->num_pages > 0x7FFFFFFFLL) return JF_ERR_UNSUPPORTED;
+  return JF_OK;
+}
+
+// Pools of any format, for the entry points that read or copy all of them
+// (single-query decode, prefill, checkpoint, restore).
+int check_pool_read(const jf_kv_pool* pool) {
+  return pool && pool->format == JF_FMT_E4M3_B32 ? check_pool8(pool) : check_pool_any(pool);
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                   const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -110,6 +141,25 @@ int make_codes_map(const Geom& g, void* base, int rows_per_box, CUtensorMap* map
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
+// 5-D map over the code rows of an 8-bit pool: (byte of a 128-byte half, half,
+// row of K or V over all KV heads, K|V, page), box = (128, D / 128,
+// rows_per_box, 2, 1), 128B swizzle: one copy brings K and V of rows_per_box
+// positions of a KV head.
+int make_kv8_map(const Geom& g, void* base, int rows_per_box, CUtensorMap* map) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return JF_ERR_CUDA;
+  cuuint64_t dims[5] = {128, (cuuint64_t)g.D / 128, (cuuint64_t)g.Hkv * g.P, 2,
+                        (cuuint64_t)g.num_pages};
+  cuuint64_t strides[4] = {128, (cuuint64_t)g.D, (cuuint64_t)g.codes_region,
+                           (cuuint64_t)g.page_bytes};
+  cuuint32_t box[5] = {128, (cuuint32_t)g.D / 128, (cuuint32_t)rows_per_box, 2, 1};
+  cuuint32_t estr[5] = {1, 1, 1, 1, 1};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, dims, strides, box, estr,
+                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
+}
+
 }  // namespace
 
 extern "C" {
@@ -126,7 +176,8 @@ size_t jf_kv_page_bytes(int32_t num_kv_heads, int32_t page_size, int32_t head_di
 
 size_t jf_kv_page_bytes_fmt(int32_t format, int32_t num_kv_heads, int32_t page_size,
                             int32_t head_dim) {
-  if (format != JF_FMT_AFFINE4_G64 && format != JF_FMT_TQ4) return 0;
+  if (format != JF_FMT_AFFINE4_G64 && format != JF_FMT_TQ4 && format != JF_FMT_E4M3_B32) return 0;
+  if (format == JF_FMT_E4M3_B32 && page_size % 32) return 0;
   if (num_kv_heads < 1 || page_size < 1 || (head_dim != 128 && head_dim != 256)) return 0;
   jf_kv_pool p{};
   p.num_pages = 1;
@@ -179,7 +230,9 @@ static int decode_common(const jf_kv_pool* pool, const int32_t* page_table, int3
                          const void* v_new, const void* q, int32_t num_q_heads,
                          float softmax_scale, void* out, void* workspace, size_t workspace_bytes,
                          int32_t num_splits, void* stream, int32_t q_len = 1) {
-  int st = check_pool_any(pool);
+  const bool kv8 = pool && pool->format == JF_FMT_E4M3_B32;
+  if (kv8 && (q_len != 1 || k_new)) return JF_ERR_UNSUPPORTED;   // single-query decode only
+  int st = check_pool_read(pool);
   if (st) return st;
   if (!page_table || !context_lens || !q || !out || !workspace) return JF_ERR_INVALID_ARG;
   if (batch < 1 || batch > 65535 || pt_stride < 1 || num_q_heads < 1) return JF_ERR_INVALID_ARG;
@@ -194,6 +247,14 @@ static int decode_common(const jf_kv_pool* pool, const int32_t* page_table, int3
                                               pool->head_dim, num_splits);
   if (workspace_bytes < need) return JF_ERR_WORKSPACE_TOO_SMALL;
   const Geom g = make_geom(*pool);
+  if (kv8) {
+    CUtensorMap tmap8;
+    st = make_kv8_map(g, pool->base, kv8_box_rows(), &tmap8);
+    if (st) return st;
+    return launch_kv8_decode(g, *pool, tmap8, page_table, pt_stride, context_lens, batch, q,
+                             num_q_heads, softmax_scale, out, workspace, num_splits, nullptr,
+                             nullptr, nullptr, 0, static_cast<cudaStream_t>(stream));
+  }
   Tq4Params prm;
   if (pool->format == JF_FMT_TQ4) {
     st = tq4_make_params(pool->tq4, g.D, &prm);
@@ -227,6 +288,7 @@ int jf_paged_verify_attn(const jf_kv_pool* pool, const int32_t* page_table, int3
                          void* workspace, size_t workspace_bytes, int32_t num_splits,
                          void* stream) {
   if (q_len < 1 || q_len > 4) return JF_ERR_INVALID_ARG;
+  if (pool && pool->format == JF_FMT_E4M3_B32) return JF_ERR_UNSUPPORTED;
   return decode_common(pool, page_table, pt_stride, context_lens, batch, nullptr, nullptr, q,
                        num_q_heads, softmax_scale, out, workspace, workspace_bytes, num_splits,
                        stream, q_len);
@@ -310,7 +372,7 @@ extern "C" {
 
 size_t jf_prefill_chunk_workspace_bytes(const jf_kv_pool* pool, int32_t q_start,
                                         int32_t chunk_len, int32_t num_q_heads, int32_t num_sms) {
-  if (check_pool_any(pool)) return 0;
+  if (check_pool_read(pool)) return 0;
   if (q_start < 0 || chunk_len < 0 || num_q_heads < 1 || num_sms < 0) return 0;
   if (num_q_heads % pool->num_kv_heads) return 0;
   const bool tq = pool->format == JF_FMT_TQ4;
@@ -329,7 +391,7 @@ int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
                           int32_t q_start, int32_t chunk_len, int32_t num_q_heads,
                           float softmax_scale, int32_t causal, void* out, void* workspace,
                           size_t workspace_bytes, void* stream) {
-  int st = check_pool_any(pool);
+  int st = check_pool_read(pool);
   if (st) return st;
   if (!page_table_row || !q || !out || !workspace) return JF_ERR_INVALID_ARG;
   if (q_start < 0 || chunk_len < 0 || num_q_heads < 1) return JF_ERR_INVALID_ARG;
@@ -381,7 +443,7 @@ int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
 
 size_t jf_prefill_batch_workspace_bytes(int32_t format, int64_t total_rows, int32_t num_q_heads,
                                         int32_t head_dim, int32_t num_splits) {
-  if (format != JF_FMT_AFFINE4_G64 && format != JF_FMT_TQ4) return 0;
+  if (format != JF_FMT_AFFINE4_G64 && format != JF_FMT_TQ4 && format != JF_FMT_E4M3_B32) return 0;
   if (total_rows < 0 || num_q_heads < 1 || num_splits < 1 || num_splits > 65535) return 0;
   if (head_dim != 128 && head_dim != 256) return 0;
   return prefill_workspace_bytes(total_rows, num_q_heads, head_dim, num_splits, format);
@@ -392,7 +454,7 @@ int jf_prefill_batch_attn(const jf_kv_pool* pool, const int32_t* page_table, int
                           const void* q, int32_t num_q_heads, float softmax_scale, int32_t causal,
                           int32_t num_splits, void* out, void* workspace, size_t workspace_bytes,
                           void* stream) {
-  int st = check_pool_any(pool);
+  int st = check_pool_read(pool);
   if (st) return st;
   if (batch < 1 || pt_stride < 1 || num_q_heads < 1) return JF_ERR_INVALID_ARG;
   if (batch > JF_PREFILL_MAX_BATCH) return JF_ERR_UNSUPPORTED;
@@ -440,7 +502,7 @@ int64_t jf_reservation_pages(int64_t prompt_len, int64_t output_len, int64_t g_o
 
 int jf_kv_checkpoint(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t num_pages,
                      void* dst, size_t dst_bytes, int32_t* err_flag, void* stream) {
-  int st = check_pool_any(pool);
+  int st = check_pool_read(pool);
   if (st) return st;
   if (num_pages < 0) return JF_ERR_INVALID_ARG;
   if (num_pages == 0) return JF_OK;
@@ -453,7 +515,7 @@ int jf_kv_checkpoint(const jf_kv_pool* pool, const int32_t* page_table_row, int3
 
 int jf_kv_restore(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t num_pages,
                   const void* src, size_t src_bytes, int32_t* err_flag, void* stream) {
-  int st = check_pool_any(pool);
+  int st = check_pool_read(pool);
   if (st) return st;
   if (num_pages < 0) return JF_ERR_INVALID_ARG;
   if (num_pages == 0) return JF_OK;
@@ -462,6 +524,148 @@ int jf_kv_restore(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t
   if (src_bytes < (size_t)num_pages * (size_t)g.page_bytes) return JF_ERR_INVALID_ARG;
   return launch_page_copy(g, *pool, page_table_row, num_pages, const_cast<void*>(src), err_flag,
                           false, static_cast<cudaStream_t>(stream));
+}
+
+// ---------------------------------------------------------------------------
+// Rotary axes and the 8-bit block-scaled cache
+// ---------------------------------------------------------------------------
+int jf_rope_axes(const jf_rope* rope, const int32_t* positions, int64_t pos_stride,
+                 int32_t n_tokens, int32_t head_dim, const jf_rope_rows* q, const jf_rope_rows* k,
+                 int32_t dtype, int32_t inverse, void* stream) {
+  if (!rope || !q || !k) return JF_ERR_INVALID_ARG;
+  if (dtype != JF_DTYPE_BF16 && dtype != JF_DTYPE_F16 && dtype != JF_DTYPE_F32)
+    return JF_ERR_UNSUPPORTED;
+  if (rope->pairing != JF_ROPE_PAIR_HALF && rope->pairing != JF_ROPE_PAIR_ADJACENT)
+    return JF_ERR_INVALID_ARG;
+  if (rope->num_axes < 1 || rope->num_axes > JF_ROPE_MAX_AXES) return JF_ERR_INVALID_ARG;
+  if (rope->rotary_dim < 16 || rope->rotary_dim % 16 || rope->rotary_dim > 256)
+    return JF_ERR_UNSUPPORTED;
+  if (head_dim < rope->rotary_dim || head_dim % 16 || head_dim > 512) return JF_ERR_UNSUPPORTED;
+  for (int i = 0; i < rope->rotary_dim / 2; ++i) {
+    if (!(rope->inv_freq[i] > -4294967296.f && rope->inv_freq[i] < 4294967296.f))
+      return JF_ERR_INVALID_ARG;
+    if (rope->axis[i] >= rope->num_axes) return JF_ERR_INVALID_ARG;
+  }
+  if (n_tokens < 0 || pos_stride < 0) return JF_ERR_INVALID_ARG;
+  const int64_t vec = dtype == JF_DTYPE_F32 ? 4 : 8;   // elements of 16 bytes
+  const jf_rope_rows* rows[2] = {q, k};
+  for (const jf_rope_rows* r : rows) {
+    if (r->num_heads < 0 || r->num_heads > 65535) return JF_ERR_INVALID_ARG;
+    if (r->num_heads == 0 || n_tokens == 0) continue;
+    if (!r->in || !r->out || !aligned(r->in, 16) || !aligned(r->out, 16)) return JF_ERR_INVALID_ARG;
+    if (r->in_token_stride % vec || r->in_head_stride % vec || r->out_token_stride % vec ||
+        r->out_head_stride % vec)
+      return JF_ERR_INVALID_ARG;
+    if (r->in == r->out && (r->in_token_stride != r->out_token_stride ||
+                            r->in_head_stride != r->out_head_stride))
+      return JF_ERR_INVALID_ARG;   // in place, but to other rows
+  }
+  if (n_tokens == 0 || q->num_heads + k->num_heads == 0) return JF_OK;
+  if (!positions) return JF_ERR_INVALID_ARG;
+  return launch_rope(*rope, positions, pos_stride, n_tokens, head_dim, *q, *k, dtype, inverse,
+                     static_cast<cudaStream_t>(stream));
+}
+
+static int kv8_rows(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                    int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                    void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t n_rows,
+                    int32_t* err_flag, bool read, void* stream) {
+  int st = check_pool8(pool);
+  if (st) return st;
+  if (n_rows < 0 || pt_stride < 1 || num_requests < 1) return JF_ERR_INVALID_ARG;
+  if (n_rows == 0) return JF_OK;
+  if (!page_table || !start_pos || !row_offsets || !k || !v) return JF_ERR_INVALID_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16)) return JF_ERR_INVALID_ARG;
+  const int64_t row = (int64_t)pool->num_kv_heads * pool->head_dim;
+  if (k_stride % 8 || v_stride % 8 || k_stride < row || v_stride < row) return JF_ERR_INVALID_ARG;
+  const Geom g = make_geom(*pool);
+  return launch_kv8_rows(g, *pool, page_table, pt_stride, num_requests, start_pos, row_offsets, k,
+                         k_stride, v, v_stride, n_rows, err_flag, read,
+                         static_cast<cudaStream_t>(stream));
+}
+
+int jf_kv8_append(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                  int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                  const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                  int32_t n_rows, int32_t* err_flag, void* stream) {
+  return kv8_rows(pool, page_table, pt_stride, num_requests, start_pos, row_offsets,
+                  const_cast<void*>(k), k_stride, const_cast<void*>(v), v_stride, n_rows, err_flag,
+                  false, stream);
+}
+
+int jf_kv8_read(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                void* k, int64_t k_stride, void* v, int64_t v_stride, int32_t n_rows,
+                int32_t* err_flag, void* stream) {
+  return kv8_rows(pool, page_table, pt_stride, num_requests, start_pos, row_offsets, k, k_stride,
+                  v, v_stride, n_rows, err_flag, true, stream);
+}
+
+size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
+                                         int32_t head_dim, int32_t num_splits,
+                                         int64_t weight_stride) {
+  if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return 0;
+  const size_t n = jf_attn_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_splits);
+  if (n == 0) return 0;
+  return (n + 255) / 256 * 256 + (size_t)batch * num_q_heads * (size_t)weight_stride * 4;
+}
+
+int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_table,
+                                 int32_t pt_stride, const int32_t* context_lens, int32_t batch,
+                                 const void* q, int32_t num_q_heads, float softmax_scale,
+                                 void* out, const float* weights_in, float* weights_out,
+                                 int64_t weight_stride, void* workspace, size_t workspace_bytes,
+                                 int32_t num_splits, void* stream) {
+  int st = check_pool8(pool);
+  if (st) return st;
+  if (!page_table || !context_lens || !q || !out || !weights_out || !workspace)
+    return JF_ERR_INVALID_ARG;
+  if (batch < 1 || batch > 65535 || pt_stride < 1 || num_q_heads < 1) return JF_ERR_INVALID_ARG;
+  if (num_q_heads % pool->num_kv_heads) return JF_ERR_INVALID_ARG;
+  if (num_q_heads / pool->num_kv_heads > 8) return JF_ERR_UNSUPPORTED;
+  if (num_splits < 1 || num_splits > 65535) return JF_ERR_INVALID_ARG;
+  if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return JF_ERR_INVALID_ARG;
+  if (!(softmax_scale == softmax_scale)) return JF_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256) ||
+      !aligned(weights_in, 4) || !aligned(weights_out, 4))
+    return JF_ERR_INVALID_ARG;
+  const size_t base = (jf_attn_workspace_bytes(batch, num_q_heads, pool->num_kv_heads,
+                                               pool->head_dim, num_splits) + 255) / 256 * 256;
+  if (workspace_bytes < jf_decode_weights_workspace_bytes(batch, num_q_heads, pool->num_kv_heads,
+                                                          pool->head_dim, num_splits,
+                                                          weight_stride))
+    return JF_ERR_WORKSPACE_TOO_SMALL;
+  const Geom g = make_geom(*pool);
+  CUtensorMap tmap;
+  st = make_kv8_map(g, pool->base, kv8_box_rows(), &tmap);
+  if (st) return st;
+  return launch_kv8_decode(g, *pool, tmap, page_table, pt_stride, context_lens, batch, q,
+                           num_q_heads, softmax_scale, out, workspace, num_splits,
+                           reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + base),
+                           weights_in, weights_out, weight_stride,
+                           static_cast<cudaStream_t>(stream));
+}
+
+int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                 const int32_t* context_lens, int32_t batch, const float* weights,
+                 int64_t weight_stride, int32_t budget, int32_t sinks, int32_t recent,
+                 const int32_t* dst_page_table, int32_t dst_stride, int32_t* dst_context_lens,
+                 float* dst_weights, int32_t* kept, int32_t* err_flag, void* stream) {
+  const int st = check_pool8(pool);
+  if (st) return st;
+  if (!page_table || !context_lens || !weights || !dst_page_table || !dst_context_lens || !kept)
+    return JF_ERR_INVALID_ARG;
+  if (batch < 1 || batch > 65535 || pt_stride < 1 || dst_stride < 1) return JF_ERR_INVALID_ARG;
+  if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return JF_ERR_INVALID_ARG;
+  if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return JF_ERR_INVALID_ARG;
+  if (2 * (int64_t)pool->num_kv_heads > 65535) return JF_ERR_UNSUPPORTED;   // launch grid
+  if (!aligned(weights, 4) || !aligned(dst_weights, 4)) return JF_ERR_INVALID_ARG;
+  const Geom g = make_geom(*pool);
+  return launch_kv8_evict(g, *pool, page_table, pt_stride, context_lens, batch, weights,
+                          weight_stride, budget, sinks, recent, dst_page_table, dst_stride,
+                          dst_context_lens, dst_weights, kept, err_flag,
+                          static_cast<cudaStream_t>(stream));
 }
 
 // ---------------------------------------------------------------------------

@@ -20,7 +20,7 @@ struct Geom {
   int32_t Hkv;
   int32_t D;
   // derived
-  int32_t CB;     // code bytes per vector  = D/2
+  int32_t CB;     // code bytes per vector  = D/2 (4-bit formats), D (E4M3)
   int32_t NG;     // groups per vector      = D/64
   int32_t SBB;    // side bytes per vector: 4*NG scale/bias (affine), 2 norm (TQ4)
   int64_t codes_region;  // Hkv*P*CB
@@ -34,12 +34,16 @@ inline Geom make_geom(const jf_kv_pool& p) {
   g.P = p.page_size;
   g.Hkv = p.num_kv_heads;
   g.D = p.head_dim;
-  g.CB = g.D / 2;
+  g.CB = p.format == JF_FMT_E4M3_B32 ? g.D : g.D / 2;
   g.NG = g.D / 64;
   // side data per vector: affine scale/bias words, or the TQ4 fp16 norm
   g.SBB = (p.format == JF_FMT_TQ4) ? 2 : 4 * g.NG;
   g.codes_region = (int64_t)g.Hkv * g.P * g.CB;
   g.sb_region = (int64_t)g.Hkv * g.P * g.SBB;
+  if (p.format == JF_FMT_E4M3_B32) {   // one fp32 scale per 32 positions
+    g.SBB = 0;
+    g.sb_region = (int64_t)g.Hkv * (g.P / 32) * 4;
+  }
   g.page_bytes = 2 * g.codes_region + 2 * g.sb_region;
   return g;
 }

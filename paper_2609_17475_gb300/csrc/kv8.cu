@@ -1,0 +1,264 @@
+// Append to and read back from the 8-bit block-scaled cache.
+//
+// Append.  The rows of request b (row_offsets[b] .. row_offsets[b + 1]) go to
+// consecutive positions from start_pos[b].  A CTA takes one block of 32
+// positions of one KV head, K or V: it holds the block's new rows in
+// registers (32 rows x D bf16 over 256 threads), takes their largest
+// magnitude, settles the block's exponent and writes the codes.  A block
+// that already holds positions keeps the larger of its exponent and the new
+// rows'; when it grows, the CTA rounds the earlier codes again under the new
+// scale.  Scales are powers of two so that growing loses only what falls
+// below the smallest code (a shift of an e4m3 exponent is exact), and
+// appending a run row by row gives the scale that appending it at once does.
+//
+// Read.  The inverse on runs of positions: bf16 values code * 2^e (exact: a
+// code has 4 significant bits).
+#include "kv8.cuh"
+
+namespace jfkv {
+
+struct Kv8Args {
+  uint8_t* pool;
+  int64_t num_pages;
+  int64_t page_bytes;
+  int64_t codes_region;
+  int64_t sb_region;
+  int32_t P;
+  int32_t Hkv;
+  const int32_t* page_table;
+  int32_t pt_stride;
+  int32_t num_requests;
+  const int32_t* start_pos;
+  const int32_t* row_offsets;
+  uint16_t* k;               // append: read; read back: written
+  uint16_t* v;
+  int64_t k_stride, v_stride;  // elements between rows
+  int32_t n_rows;
+  int32_t* err;
+};
+
+// Rows [r0, r1) of request b and its first position; false where they do not
+// fit the row list or the request's page-table row.
+__device__ __forceinline__ bool kv8_run(const Kv8Args& a, int b, int& r0, int& r1, int& pos0) {
+  r0 = a.row_offsets[b];
+  r1 = a.row_offsets[b + 1];
+  pos0 = a.start_pos[b];
+  return r0 >= 0 && r0 <= r1 && r1 <= a.n_rows && pos0 >= 0 &&
+         (int64_t)pos0 + (r1 - r0) <= (int64_t)a.pt_stride * a.P;
+}
+
+template <int D>
+__global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Args a) {
+  constexpr int LPR = D / 8;               // lanes per row, 8 elements each
+  constexpr int RPP = 256 / LPR;           // rows per pass
+  constexpr int NP = KV8_BLOCK / RPP;      // passes over the block's 32 rows
+  __shared__ uint32_t warp_max[8];
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int head = blockIdx.y, kind = blockIdx.z;
+
+  // the request and block this CTA takes: requests' block counts laid end to
+  // end, 32 requests at a time (every warp works it out itself)
+  int b = -1, r0 = 0, r1 = 0, pos0 = 0, blk = 0;
+  for (int b0 = 0, base = 0; b0 < a.num_requests; b0 += 32) {
+    const int bb = b0 + lane;
+    int q0 = 0, q1 = 0, p0 = 0, n = 0;
+    if (bb < a.num_requests) {
+      if (kv8_run(a, bb, q0, q1, p0)) {
+        if (q1 > q0) n = (p0 + (q1 - q0) - 1) / KV8_BLOCK - p0 / KV8_BLOCK + 1;
+      } else if (blockIdx.x == 0 && head == 0 && kind == 0 && warp == 0) {
+        flag_error(a.err, JF_DEV_ERR_POSITION);
+      }
+    }
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    const int excl = base + incl - n;
+    const unsigned m = __ballot_sync(0xffffffffu, n > 0 && (int)blockIdx.x >= excl &&
+                                                      (int)blockIdx.x < excl + n);
+    if (m && b < 0) {
+      const int src = __ffs(m) - 1;
+      b = b0 + src;
+      r0 = __shfl_sync(0xffffffffu, q0, src);
+      r1 = __shfl_sync(0xffffffffu, q1, src);
+      pos0 = __shfl_sync(0xffffffffu, p0, src);
+      blk = pos0 / KV8_BLOCK + (int)blockIdx.x - __shfl_sync(0xffffffffu, excl, src);
+      if (blockIdx.x != 0) break;   // CTA 0 goes on to check every request
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (b < 0) return;
+
+  const int block_pos = blk * KV8_BLOCK;
+  const int first = max(pos0 - block_pos, 0);                          // new rows of the block:
+  const int last = min(pos0 + (r1 - r0) - block_pos, KV8_BLOCK);       // [first, last)
+  const int32_t page = a.page_table[(int64_t)b * a.pt_stride + block_pos / a.P];
+  if (page < 0 || page >= a.num_pages) {
+    if (threadIdx.x == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
+    return;
+  }
+  const int slot = block_pos % a.P;
+  uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
+  uint8_t* const codes = rec + kind * a.codes_region + ((int64_t)head * a.P + slot) * D;
+  float* const scale = reinterpret_cast<float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
+                       head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK;
+
+  const uint16_t* const src = kind ? a.v : a.k;
+  const int64_t stride = kind ? a.v_stride : a.k_stride;
+  const int li = threadIdx.x % LPR, rr = threadIdx.x / LPR;
+  uint4 x[NP];
+  uint32_t mx = 0;   // largest magnitude's bf16 bits (finite values only)
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int row = p * RPP + rr;
+    x[p] = make_uint4(0u, 0u, 0u, 0u);
+    if (row >= first && row < last)
+      x[p] = *reinterpret_cast<const uint4*>(src + (int64_t)(r0 + block_pos + row - pos0) * stride +
+                                             head * D + li * 8);
+    const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t lo = w[i] & 0x7FFFu, hi = (w[i] >> 16) & 0x7FFFu;
+      if (lo < 0x7F80u) mx = max(mx, lo);
+      if (hi < 0x7F80u) mx = max(mx, hi);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  if (lane == 0) warp_max[warp] = mx;
+  const int e_old = first > 0 ? exp8_of_scale(*scale) : KV8_EMIN;
+  __syncthreads();   // every thread has read the old scale
+#pragma unroll
+  for (int i = 0; i < 8; ++i) mx = max(mx, warp_max[i]);
+  const int e = max(e_old, exp8_of(__uint_as_float(mx << 16)));
+  if (threadIdx.x == 0) *scale = two8(e);
+
+  const float inv = two8(-e);
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int row = p * RPP + rr;
+    if (row >= first && row < last) {
+      uint2 c;
+      c.x = e4m3x2(bf16lo_to_f32(x[p].x) * inv, bf16hi_to_f32(x[p].x) * inv) |
+            (e4m3x2(bf16lo_to_f32(x[p].y) * inv, bf16hi_to_f32(x[p].y) * inv) << 16);
+      c.y = e4m3x2(bf16lo_to_f32(x[p].z) * inv, bf16hi_to_f32(x[p].z) * inv) |
+            (e4m3x2(bf16lo_to_f32(x[p].w) * inv, bf16hi_to_f32(x[p].w) * inv) << 16);
+      *reinterpret_cast<uint2*>(codes + row * D + li * 8) = c;
+    } else if (row < first && e > e_old) {   // the block grew: its earlier rows again
+      uint2* const at = reinterpret_cast<uint2*>(codes + row * D + li * 8);
+      const float s = two8(e_old - e);
+      uint2 c = *at;
+      c.x = rescale_e4m3x4(c.x, s);
+      c.y = rescale_e4m3x4(c.y, s);
+      *at = c;
+    }
+  }
+}
+
+// Read back: a group of D/8 lanes takes the K (or V) vector of one row and
+// KV head, 8 codes a lane.
+template <int D>
+__global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
+  constexpr int LPR = D / 8;
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int64_t u = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+  const int li = threadIdx.x % LPR;
+  const int kind = blockIdx.z;
+  const int64_t row = u / a.Hkv;
+  const int head = (int)(u % a.Hkv);
+  if (row >= a.n_rows) return;
+  // the request of this row: the last b with row_offsets[b] <= row
+  int lo = 0, hi = a.num_requests - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a.row_offsets[mid] <= row) lo = mid; else hi = mid - 1;
+  }
+  int r0, r1, pos0;
+  const bool ok = kv8_run(a, lo, r0, r1, pos0);
+  if (!ok || row < r0 || row >= r1) {
+    if (!ok && li == 0) flag_error(a.err, JF_DEV_ERR_POSITION);
+    return;   // a row of no request is left as it is
+  }
+  const int pos = pos0 + (int)(row - r0);
+  const int32_t page = a.page_table[(int64_t)lo * a.pt_stride + pos / a.P];
+  if (page < 0 || page >= a.num_pages) {
+    if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
+    return;
+  }
+  const int slot = pos % a.P;
+  const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
+  const uint2 c = *reinterpret_cast<const uint2*>(rec + kind * a.codes_region +
+                                                  ((int64_t)head * a.P + slot) * D + li * 8);
+  const float s = two8(exp8_of_scale(
+      *(reinterpret_cast<const float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
+        head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK)));
+  uint32_t h[4];
+  f16x4_of_e4m3(c.x, h[0], h[1]);
+  f16x4_of_e4m3(c.y, h[2], h[3]);
+  uint32_t o[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = f32x2_of_f16x2(h[i]);
+    o[i] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f.x * s)) |
+           ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f.y * s)) << 16);
+  }
+  uint16_t* const dst = (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D;
+  *reinterpret_cast<uint4*>(dst + li * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_table,
+                    int32_t pt_stride, int32_t num_requests, const int32_t* start_pos,
+                    const int32_t* row_offsets, void* k, int64_t k_stride, void* v,
+                    int64_t v_stride, int32_t n_rows, int32_t* err, bool read,
+                    cudaStream_t stream) {
+  Kv8Args a;
+  a.pool = static_cast<uint8_t*>(pool.base);
+  a.num_pages = g.num_pages;
+  a.page_bytes = g.page_bytes;
+  a.codes_region = g.codes_region;
+  a.sb_region = g.sb_region;
+  a.P = g.P;
+  a.Hkv = g.Hkv;
+  a.page_table = page_table;
+  a.pt_stride = pt_stride;
+  a.num_requests = num_requests;
+  a.start_pos = start_pos;
+  a.row_offsets = row_offsets;
+  a.k = static_cast<uint16_t*>(k);
+  a.v = static_cast<uint16_t*>(v);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.n_rows = n_rows;
+  a.err = err;
+  // append: a request's r >= 1 rows touch at most (r - 1) / 32 + 2 blocks and
+  // at most r; read: one group of D / 8 lanes per (row, KV head)
+  const int64_t by_block = (int64_t)n_rows / KV8_BLOCK + 2 * (int64_t)num_requests;
+  const int64_t blocks = read ? ((int64_t)n_rows * g.Hkv * (g.D / 8) + 255) / 256
+                              : (by_block < n_rows ? by_block : n_rows);
+  if (blocks > 0x7FFFFFFF) return JF_ERR_UNSUPPORTED;
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = read ? dim3((unsigned)blocks, 1u, 2u)
+                     : dim3((unsigned)blocks, (unsigned)g.Hkv, 2u);
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cfg.attrs = pdl;
+  cfg.numAttrs = 1;
+  cudaError_t e;
+  if (read)
+    e = g.D == 256 ? cudaLaunchKernelEx(&cfg, kv8_read_kernel<256>, a)
+                   : cudaLaunchKernelEx(&cfg, kv8_read_kernel<128>, a);
+  else
+    e = g.D == 256 ? cudaLaunchKernelEx(&cfg, kv8_append_kernel<256>, a)
+                   : cudaLaunchKernelEx(&cfg, kv8_append_kernel<128>, a);
+  return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+}
+
+}  // namespace jfkv

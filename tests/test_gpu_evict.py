@@ -1,0 +1,120 @@
+"""Eviction by accumulated weight on the GPU: kept positions, weights and the compacted pages, bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_17475_gb300 as jf
+from oracle import kv8 as O
+from tests import kv8_cases as C
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def evict(L, pool, table, ctx, w, budget, sinks, recent, dst, with_weights=True):
+    g = C.gpu_pool(L, pool.copy())
+    B = len(ctx)
+    kept = torch.full((B, L.Hkv, budget), -7, dtype=torch.int32, device=DEV)
+    wout = torch.full((B, L.Hkv, budget), -7.0, device=DEV) if with_weights else None
+    n, err = torch.full((B,), -7, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    jf.jf_kv8_evict(g, C.ints(table), C.ints(ctx), torch.from_numpy(w).to(DEV), budget, sinks, recent, C.ints(dst), n,
+                    wout, kept, err)
+    return g, kept, wout, n, int(err)
+
+
+def check(hkv, d, p, ctx, budget, sinks, recent, make, seed=0, spread=6):
+    rng = np.random.default_rng(seed + sum(ctx) + budget)
+    extra = [-(-min(n, budget) // p) for n in ctx]
+    L, table, pool = C.filled(rng, hkv, p, d, ctx, fill=0xFF, spread=spread, extra=extra)
+    own = [-(-n // p) for n in ctx]
+    dst = np.full((len(ctx), max(max(extra), 1)), -1, dtype=np.int32)
+    src = np.full((len(ctx), max(max(own), 1)), -1, dtype=np.int32)
+    for b in range(len(ctx)):
+        src[b, :own[b]] = table[b, :own[b]]
+        dst[b, :extra[b]] = table[b, own[b]:own[b] + extra[b]]
+    w = make(rng, (len(ctx), hkv, max(max(ctx), 1) + 5)).astype(np.float32)
+    g, kept, wout, n, err = evict(L, pool, src, ctx, w, budget, sinks, recent, dst)
+    want_kept, want_w = O.evict(pool, L, src, ctx, w, budget, sinks, recent, dst)
+    assert err == 0
+    assert np.array_equal(kept.cpu().numpy(), want_kept)
+    assert np.array_equal(wout.cpu().numpy().view(np.int32), want_w.view(np.int32))
+    assert n.tolist() == [min(c, budget) for c in ctx]
+    assert np.array_equal(g.data.cpu().numpy(), pool)       # the compacted pages, and nothing else
+
+
+def uneven(rng, shape):
+    return np.exp(2 * rng.standard_normal(shape)) * (rng.random(shape) < 0.7)
+
+
+def ties(rng, shape):
+    return rng.integers(0, 4, shape) / 4
+
+
+def odd(rng, shape):
+    """NaN, infinities, signed zeros, negative and subnormal weights."""
+    pick = np.array([np.nan, np.inf, -np.inf, 0.0, -0.0, -1.5, 1e-40, -1e-40, 2.0, 3e38])
+    return pick[rng.integers(0, len(pick), shape)]
+
+
+@pytest.mark.parametrize("make", [uneven, ties, odd])
+@pytest.mark.parametrize("hkv,d,p,ctx,budget,sinks,recent", [
+    (2, 128, 64, [300], 100, 4, 32),
+    (1, 256, 128, [1, 0, 33, 500, 129], 33, 0, 0),
+    (3, 128, 256, [700, 64], 64, 0, 64),
+    (4, 256, 64, [65], 64, 1, 0),
+    (1, 128, 128, [2000, 31], 1, 0, 0),
+    (2, 128, 64, [1025, 1024], 1024, 1000, 24),
+])
+def test_evict(make, hkv, d, p, ctx, budget, sinks, recent):
+    check(hkv, d, p, ctx, budget, sinks, recent, make)
+
+
+def test_evict_long_rows():
+    """Rows of tens of thousands of positions (odd lengths), keys that share long prefixes."""
+    check(1, 128, 256, [40003, 16385], 5001, 4, 77, lambda r, s: 1 + r.integers(0, 1 << 12, s) * 2.0 ** -23, spread=0)
+
+
+def test_evict_then_decode_sees_the_kept_positions():
+    rng = np.random.default_rng(5)
+    L, table, pool = C.filled(rng, 2, 64, 128, [500, 90], extra=[2, 2])
+    src, dst = table[:, :8].copy(), np.stack([table[0, 8:10], table[1, 2:4]])
+    w = uneven(rng, (2, 2, 500)).astype(np.float32)
+    g, kept, _, n, err = evict(L, pool, src, [500, 90], w, 100, 4, 16, dst, with_weights=False)
+    assert err == 0 and n.tolist() == [100, 90]
+    q = torch.randn(2, 8, 128, device=DEV).bfloat16()
+    out, ws = torch.empty_like(q), jf.decode_workspace(2, 8, 2, 128, 3)
+    jf.jf_paged_decode_attn(g, C.ints(dst), n, q, 0.1, out, ws, 3)
+    assert jf.workspace_status(ws) == 0
+    after = g.data.cpu().numpy()
+    for b in range(2):
+        k, v = O.read(after, L, dst[b], int(n[b]))
+        ref, p, mass = O.attend(k, v, q[b:b + 1].double().cpu().numpy(), float(np.float32(0.1)))
+        e = np.abs(out[b].double().cpu().numpy() - ref[0])
+        assert (e <= C.out_bound(ref[0], mass[0], 100, np.abs(v).max())).all()
+
+
+def test_evict_reports_and_refuses():
+    rng = np.random.default_rng(6)
+    L, table, pool = C.filled(rng, 1, 64, 128, [200, 130])
+    w = uneven(rng, (2, 1, 200)).astype(np.float32)
+    P, G = jf.binding.JF_DEV_ERR_POSITION, jf.binding.JF_DEV_ERR_PAGE_ID
+    spare = sorted(set(range(len(pool))) - set(table[0, :4]) - set(table[1, :3]))
+    dst = np.array([[spare[0]], [spare[1]]], dtype=np.int32)
+    # a context past its weights or its table: kept as empty, the other request done
+    for ctx in ([201, 130], [-1, 130], [64 * 4 + 1, 130]):
+        g, kept, _, n, err = evict(L, pool, table, ctx, w, 40, 2, 2, dst)
+        assert err == P and n.tolist() == [0, 40] and (kept[0] == -1).all()
+        want = pool.copy()
+        wk, _ = O.evict(want, L, table[1:], [130], w[1:], 40, 2, 2, dst[1:])
+        assert np.array_equal(kept[1:].cpu().numpy(), wk) and np.array_equal(g.data.cpu().numpy(), want)
+    # a source page outside the pool reads as zeros; a destination one is not written
+    bad = table.copy()
+    bad[0, 0] = -1
+    assert evict(L, pool, bad, [200, 130], w, 40, 2, 2, dst)[4] == G
+    assert evict(L, pool, table, [200, 130], w, 40, 2, 2, np.array([[-1], [spare[1]]]))[4] == G
+    # a destination row too short for the budget
+    assert evict(L, pool, table, [200, 130], w, 65, 2, 2, dst)[4] == P
+    for budget, sinks, recent in ((0, 0, 0), (4, 3, 2), (4, -1, 0), (4, 0, -1)):
+        with pytest.raises((jf.JfError, RuntimeError)) as e:
+            evict(L, pool, table, [200, 130], w, budget, sinks, recent, dst)
+        assert isinstance(e.value, jf.JfError) and e.value.status == jf.binding.JF_ERR_INVALID_ARG
