@@ -23,7 +23,7 @@ struct Kv8Args {
   int64_t page_bytes;
   int64_t codes_region;
   int64_t sb_region;
-  int32_t P;
+  int32_t P, log2P;
   int32_t Hkv;
   const int32_t* page_table;
   int32_t pt_stride;
@@ -96,14 +96,14 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Args a) {
   const int block_pos = blk * KV8_BLOCK;
   const int first = max(pos0 - block_pos, 0);                          // new rows of the block:
   const int last = min(pos0 + (r1 - r0) - block_pos, KV8_BLOCK);       // [first, last)
-  const int32_t page = a.page_table[(int64_t)b * a.pt_stride + block_pos / a.P];
+  const int32_t page = a.page_table[(int64_t)b * a.pt_stride + (block_pos >> a.log2P)];
   if (page < 0 || page >= a.num_pages) {
     if (threadIdx.x == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
     return;
   }
-  const int slot = block_pos % a.P;
+  const int slot = block_pos & (a.P - 1);
   uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  uint8_t* const codes = rec + kind * a.codes_region + ((int64_t)head * a.P + slot) * D;
+  uint8_t* const codes = rec + kind * a.codes_region + (int64_t)(head * a.P + slot) * D;
   float* const scale = reinterpret_cast<float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
                        head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK;
 
@@ -159,18 +159,16 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Args a) {
   }
 }
 
-// Read back: a group of D/8 lanes takes the K (or V) vector of one row and
-// KV head, 8 codes a lane.
+// Read back: a group of D/16 lanes takes the K (or V) vector of one row and
+// KV head, 16 codes a lane.
 template <int D>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
-  constexpr int LPR = D / 8;
+  constexpr int LPR = D / 16;
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int64_t u = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LPR;
+  const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int li = threadIdx.x % LPR;
-  const int kind = blockIdx.z;
-  const int64_t row = u / a.Hkv;
-  const int head = (int)(u % a.Hkv);
+  const int head = blockIdx.y, kind = blockIdx.z;
   if (row >= a.n_rows) return;
   // the request of this row: the last b with row_offsets[b] <= row
   int lo = 0, hi = a.num_requests - 1;
@@ -184,31 +182,33 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
     if (!ok && li == 0) flag_error(a.err, JF_DEV_ERR_POSITION);
     return;   // a row of no request is left as it is
   }
-  const int pos = pos0 + (int)(row - r0);
-  const int32_t page = a.page_table[(int64_t)lo * a.pt_stride + pos / a.P];
+  const int pos = pos0 + (row - r0);
+  const int32_t page = a.page_table[(int64_t)lo * a.pt_stride + (pos >> a.log2P)];
   if (page < 0 || page >= a.num_pages) {
     if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
     return;
   }
-  const int slot = pos % a.P;
+  const int slot = pos & (a.P - 1);
   const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  const uint2 c = *reinterpret_cast<const uint2*>(rec + kind * a.codes_region +
-                                                  ((int64_t)head * a.P + slot) * D + li * 8);
+  const uint4 c = *reinterpret_cast<const uint4*>(rec + kind * a.codes_region +
+                                                  (int64_t)(head * a.P + slot) * D + li * 16);
   const float s = two8(exp8_of_scale(
       *(reinterpret_cast<const float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
         head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK)));
-  uint32_t h[4];
-  f16x4_of_e4m3(c.x, h[0], h[1]);
-  f16x4_of_e4m3(c.y, h[2], h[3]);
-  uint32_t o[4];
+  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+  uint32_t o[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const float2 f = f32x2_of_f16x2(h[i]);
-    o[i] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f.x * s)) |
-           ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(f.y * s)) << 16);
+    uint32_t h0, h1;
+    f16x4_of_e4m3(w[i], h0, h1);
+    const float2 f0 = f32x2_of_f16x2(h0), f1 = f32x2_of_f16x2(h1);
+    o[2 * i] = pack_bf16x2_rn(f0.x * s, f0.y * s);
+    o[2 * i + 1] = pack_bf16x2_rn(f1.x * s, f1.y * s);
   }
-  uint16_t* const dst = (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D;
-  *reinterpret_cast<uint4*>(dst + li * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+  uint4* const dst = reinterpret_cast<uint4*>(
+      (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D + li * 16);
+  dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+  dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
 }
 
 int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_table,
@@ -223,6 +223,7 @@ int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_t
   a.codes_region = g.codes_region;
   a.sb_region = g.sb_region;
   a.P = g.P;
+  a.log2P = __builtin_ctz((unsigned)g.P);
   a.Hkv = g.Hkv;
   a.page_table = page_table;
   a.pt_stride = pt_stride;
@@ -236,17 +237,16 @@ int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_t
   a.n_rows = n_rows;
   a.err = err;
   // append: a request's r >= 1 rows touch at most (r - 1) / 32 + 2 blocks and
-  // at most r; read: one group of D / 8 lanes per (row, KV head)
+  // at most r; read: one group of D / 16 lanes per row
   const int64_t by_block = (int64_t)n_rows / KV8_BLOCK + 2 * (int64_t)num_requests;
-  const int64_t blocks = read ? ((int64_t)n_rows * g.Hkv * (g.D / 8) + 255) / 256
+  const int64_t blocks = read ? ((int64_t)n_rows * (g.D / 16) + 255) / 256
                               : (by_block < n_rows ? by_block : n_rows);
   if (blocks > 0x7FFFFFFF) return JF_ERR_UNSUPPORTED;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = read ? dim3((unsigned)blocks, 1u, 2u)
-                     : dim3((unsigned)blocks, (unsigned)g.Hkv, 2u);
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)g.Hkv, 2u);
   cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cfg.attrs = pdl;

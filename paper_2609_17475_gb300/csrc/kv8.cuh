@@ -49,6 +49,12 @@ __device__ __forceinline__ float2 f32x2_of_f16x2(uint32_t h) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+__device__ __forceinline__ uint32_t pack_bf16x2_rn(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // the four codes of a word rounded again for a scale 2^s times smaller
 // (value = code * 2^s under the new scale)
 __device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float two_s) {

@@ -549,19 +549,31 @@ __device__ K8Rows k8_rows(const Kv8DecodeArgs& a, int b, int lane) {
 
 constexpr int K8F_THREADS = 256;
 constexpr int K8F_COLS = 64;                       // columns of an output row per merging CTA
-constexpr int K8F_TILE = 2048;                     // positions per weighing CTA
+constexpr int K8F_TILE = 1024;                     // positions per weighing CTA
 
 // Merging CTA: 64 columns of one query row; warp w sums the partials w, w + 8,
-// ... of two columns a lane.  Weighing CTA: 2,048 positions of one KV head.
+// ... of two columns a lane.  Weighing CTA: 1,024 positions of one KV head.
 template <int D>
 __global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8DecodeArgs a) {
   constexpr float NEG = -INFINITY;
   __shared__ float2 red[8][32];
   __shared__ float2 gml[8];
+  __shared__ int plan[2];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
+  auto plan_of = [&](int b) {   // one warp works it out
+    if (warp == 0) {
+      const K8Rows rows = k8_rows(a, b, lane);
+      if (lane == 0) {
+        plan[0] = rows.row;
+        plan[1] = rows.n;
+      }
+    }
+    __syncthreads();
+    return K8Rows{plan[0], plan[1]};
+  };
   if ((int)blockIdx.x < a.merge_blocks) {
     constexpr int SL = D / K8F_COLS;
     const int sl = blockIdx.x % SL;
@@ -572,7 +584,7 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8Decode
       if (ctx < 0 || ctx > (int64_t)a.pt_stride * a.P || (a.w_out && ctx > a.wstride))
         flag_error(a.status, JF_DEV_ERR_POSITION);
     }
-    const K8Rows rows = k8_rows(a, b, lane);
+    const K8Rows rows = plan_of(b);
     float M = NEG;
     for (int s = lane; s < rows.n; s += 32) M = fmaxf(M, ml[(int64_t)(rows.row + s) * a.Hq + hq].x);
 #pragma unroll
@@ -617,7 +629,7 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8Decode
   const int n = (int)min((int64_t)k8_ctx(a, b), a.wstride);
   const int t0 = tile * K8F_TILE;
   if (t0 >= n) return;
-  const K8Rows rows = k8_rows(a, b, lane);
+  const K8Rows rows = plan_of(b);
   if (warp < a.G) {   // warp g: the reference and 1 / l of head g
     const int hq = kvh * a.G + warp;
     float M = NEG, l = 0.f;
@@ -635,16 +647,29 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8Decode
   __syncthreads();
   const float* const sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.wstride;
   const int64_t wrow = ((int64_t)b * a.Hkv + kvh) * a.wstride;
+  constexpr int NT = K8F_TILE / K8F_THREADS;   // positions per thread
+  float add[NT], w[NT];
 #pragma unroll
-  for (int i = 0; i < K8F_TILE / K8F_THREADS; ++i) {
+  for (int i = 0; i < NT; ++i) {
     const int t = t0 + i * K8F_THREADS + threadIdx.x;
-    if (t < n) {
-      float w = a.w_in ? a.w_in[wrow + t] : 0.f;
-      float add = 0.f;
-      for (int g = 0; g < a.G; ++g)
-        add = fmaf(fast_exp2(sc[(int64_t)g * a.wstride + t] - gml[g].x), gml[g].y, add);
-      a.w_out[wrow + t] = w + add;
+    add[i] = 0.f;
+    w[i] = a.w_in && t < n ? a.w_in[wrow + t] : 0.f;
+  }
+  for (int g = 0; g < a.G; ++g) {
+    const float2 m = gml[g];
+    float x[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+      const int t = t0 + i * K8F_THREADS + threadIdx.x;
+      x[i] = t < n ? sc[(int64_t)g * a.wstride + t] : NEG;
     }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) add[i] = fmaf(fast_exp2(x[i] - m.x), m.y, add[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < NT; ++i) {
+    const int t = t0 + i * K8F_THREADS + threadIdx.x;
+    if (t < n) a.w_out[wrow + t] = w[i] + add[i];
   }
 }
 

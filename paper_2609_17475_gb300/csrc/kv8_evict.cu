@@ -4,9 +4,12 @@
 // `sinks` and the last `recent` positions always do; of the others those with
 // the largest weights, equal weights in order of position.  Weights map to
 // 32-bit keys whose unsigned order is theirs (a protected position takes the
-// largest key, NaN the smallest); a radix select finds the budget-th largest
-// key 8 bits at a time, and the kept positions are then written in rising
-// order: all above that key, and the first of those that equal it.
+// largest key, NaN the smallest).  A cluster of CTAs shares a row: each keeps
+// the keys of its range of positions in shared memory, read from memory once,
+// and a radix select over the cluster's histograms (11, 11 and 10 bits,
+// combined through distributed shared memory) finds the budget-th largest
+// key.  The kept positions are then written in rising order: all above that
+// key, and the first of those that equal it.
 //
 // Compact kernel: a CTA gathers 32 kept positions of one KV head, K or V, and
 // writes them as one block of the destination pages.  The block gets the
@@ -18,6 +21,10 @@ namespace jfkv {
 
 constexpr int EV_THREADS = 1024;
 constexpr int EV_WARPS = EV_THREADS / 32;
+constexpr int EV_BINS = 2048;
+constexpr int EV_SLICE = 8192;              // keys a CTA should have before a row takes more CTAs
+constexpr int EV_MAX_CLUSTER = 8;
+constexpr int EV_MAX_KEYS = 48 * 1024;      // keys that fit a CTA's shared memory
 
 struct EvictArgs {
   uint8_t* pool;
@@ -25,7 +32,7 @@ struct EvictArgs {
   int64_t page_bytes;
   int64_t codes_region;
   int64_t sb_region;
-  int32_t P, Hkv, B;
+  int32_t P, log2P, Hkv, B;
   const int32_t* page_table;
   int32_t pt_stride;
   const int32_t* ctx;
@@ -38,6 +45,7 @@ struct EvictArgs {
   float* dst_weights;          // [B, Hkv, budget] or null
   int32_t* kept;               // [B, Hkv, budget]
   int32_t* err;
+  int32_t key_cap;             // keys that the select kernel's shared memory holds
 };
 
 // Context of request b; 0 (and flagged by the select kernel) where it does not
@@ -54,16 +62,55 @@ __device__ __forceinline__ uint32_t ev_key(float w) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
+__device__ __forceinline__ uint32_t ev_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ uint32_t ev_ranks() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void ev_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n"
+               "barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+// the int at this CTA's shared address `addr`, in CTA `rank` of the cluster
+__device__ __forceinline__ int ev_remote(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  int v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+
+// One count per key with `in` set: the lanes that share the first such lane's
+// bin add once (weights crowd into few bins: exact zeros, one exponent), the
+// others each.
+__device__ __forceinline__ void ev_count(int* hist, uint32_t bin, bool in, int lane) {
+  const unsigned all = __ballot_sync(0xffffffffu, in);
+  if (!all) return;
+  const int lead = __ffs(all) - 1;
+  const uint32_t top = __shfl_sync(0xffffffffu, bin, lead);
+  const unsigned same = __ballot_sync(0xffffffffu, in && bin == top);
+  if (lane == lead) atomicAdd(&hist[bin], __popc(same));
+  if (in && bin != top) atomicAdd(&hist[bin], 1);
+}
+
 __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictArgs a) {
-  __shared__ int hist[256];
+  extern __shared__ float slice_w[];        // this CTA's weights, or unused where they do not fit
+  __shared__ int hist[3][EV_BINS];          // one a pass: the cluster may still read the last one
   __shared__ int sums[2][EV_WARPS];
   __shared__ int pick[2];
+  __shared__ int mine[2];                   // keys above, and equal to, the last one kept
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int h = blockIdx.x, b = blockIdx.y;
+  const uint32_t rank = ev_rank(), ranks = ev_ranks();
+  const int h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int n = ev_ctx(a, b);
-  if (h == 0 && tid == 0) {
+  if (h == 0 && rank == 0 && tid == 0) {
     if (n != a.ctx[b]) flag_error(a.err, JF_DEV_ERR_POSITION);
     a.dst_ctx[b] = min(n, a.budget);
   }
@@ -71,58 +118,92 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
   const float* const w = a.weights + row * a.wstride;
   int32_t* const kept = a.kept + row * a.budget;
   float* const wout = a.dst_weights ? a.dst_weights + row * a.budget : nullptr;
-  if (n <= a.budget) {   // everything stays
-    for (int j = tid; j < a.budget; j += EV_THREADS) {
+  if (n <= a.budget) {   // everything stays (the whole cluster takes this way)
+    for (int j = rank * EV_THREADS + tid; j < a.budget; j += ranks * EV_THREADS) {
       kept[j] = j < n ? j : -1;
       if (wout) wout[j] = j < n ? w[j] : 0.f;
     }
     return;
   }
+  // this CTA's positions [p0, p1), a multiple of 32 but for the row's end
+  const int slice = (int)(((int64_t)n + 32 * (int64_t)ranks - 1) / (32 * (int64_t)ranks)) * 32;
+  const int p0 = (int)min((int64_t)rank * slice, (int64_t)n);
+  const int p1 = (int)min((int64_t)p0 + slice, (int64_t)n);
+  const bool cached = slice <= a.key_cap;
+  auto weight_of = [&](int t) -> float { return cached ? slice_w[t - p0] : w[t]; };
   auto key_of = [&](int t) -> uint32_t {
-    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(w[t]);
+    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(weight_of(t));
   };
-  // the budget-th largest key, a byte at a time from the top
+  for (int i = tid; i < 3 * EV_BINS; i += EV_THREADS) hist[0][i] = 0;
+  if (cached) {   // 8 loads in flight a thread
+    for (int tb = p0 + tid; tb < p1; tb += 8 * EV_THREADS) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (tb + u * EV_THREADS < p1) x[u] = w[tb + u * EV_THREADS];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (tb + u * EV_THREADS < p1) slice_w[tb + u * EV_THREADS - p0] = x[u];
+    }
+  }
+  __syncthreads();
+  // the budget-th largest key, digit by digit from the top
   uint32_t prefix = 0;
   int need = a.budget;   // how many of the keys with this prefix stay
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int t = tid; t < n; t += EV_THREADS) {
-      const uint32_t k = key_of(t);
-      if (shift == 24 || (k >> (shift + 8)) == prefix) atomicAdd(&hist[(k >> shift) & 255u], 1);
-    }
-    __syncthreads();
-    if (warp == 0) {   // the largest digit with at least `need` keys at or above it
-      int s = 0;       // keys of this lane's 8 digits, from the top down
-      for (int i = 0; i < 8; ++i) s += hist[255 - (8 * lane + i)];
-      int incl = s;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-      }
-      int above = incl - s;
-      if (above < need && need <= incl) {
-        for (int i = 0; i < 8; ++i) {
-          const int d = 255 - (8 * lane + i);
-          if (need <= above + hist[d]) {
-            pick[0] = d;
-            pick[1] = need - above;
-            break;
-          }
-          above += hist[d];
-        }
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const int bits = pass == 2 ? 10 : 11;
+    int* const hs = hist[pass];
+#pragma unroll 4
+    for (int tb = p0; tb < p1; tb += EV_THREADS) {
+      const int t = tb + tid;
+      const uint32_t k = t < p1 ? key_of(t) : 0u;
+      // whole warps take part
+      ev_count(hs, (k >> shift) & ((1u << bits) - 1u),
+               t < p1 && (pass == 0 || (k >> (shift + bits)) == prefix), lane);
+    }
+    ev_cluster_sync();
+    // thread i sums bins top - 2i and top - 2i - 1 over the cluster; the
+    // largest digit with at least `need` keys at or above it is picked
+    const int top = (1 << bits) - 1;
+    int c0 = 0, c1 = 0;
+    if (2 * tid <= top) {
+      const uint32_t at = smem_u32(hs + top - 2 * tid);
+#pragma unroll 4
+      for (uint32_t r = 0; r < ranks; ++r) {
+        c0 += ev_remote(at, r);
+        c1 += ev_remote(at - 4, r);
       }
     }
+    int incl = c0 + c1;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 31) sums[0][warp] = incl;
     __syncthreads();
-    prefix = (prefix << 8) | (uint32_t)pick[0];
+    int before = 0;
+    for (int i = 0; i < warp; ++i) before += sums[0][i];
+    const int above = before + incl - c0 - c1;
+    if (above < need && need <= above + c0) {
+      pick[0] = top - 2 * tid;
+      pick[1] = need - above;
+    } else if (above + c0 < need && need <= above + c0 + c1) {
+      pick[0] = top - 2 * tid - 1;
+      pick[1] = need - above - c0;
+    }
+    __syncthreads();
+    prefix = (prefix << bits) | (uint32_t)pick[0];
     need = pick[1];
     __syncthreads();
   }
-  // ordered compaction: each warp a contiguous range of positions
-  const int per = ((n + EV_WARPS - 1) / EV_WARPS + 31) & ~31;
-  const int t0 = min(warp * per, n), t1 = min(t0 + per, n);
+  // ordered compaction: each warp a contiguous range of the CTA's positions
+  const int per = ((p1 - p0 + EV_WARPS - 1) / EV_WARPS + 31) & ~31;
+  const int t0 = min(p0 + warp * per, p1), t1 = min(t0 + per, p1);
   int above = 0, equal = 0;
+#pragma unroll 4
   for (int t = t0 + lane; t < t1; t += 32) {
     const uint32_t k = key_of(t);
     above += k > prefix;
@@ -138,27 +219,45 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     sums[1][warp] = equal;
   }
   __syncthreads();
-  int eq = 0, at = 0;   // equal keys, and kept positions, before this warp's range
+  if (warp == 0) {
+    int x = sums[0][lane], y = sums[1][lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      x += __shfl_xor_sync(0xffffffffu, x, o);
+      y += __shfl_xor_sync(0xffffffffu, y, o);
+    }
+    if (lane == 0) {
+      mine[0] = x;
+      mine[1] = y;
+    }
+  }
+  ev_cluster_sync();
+  int at = 0, eq = 0;   // keys above, and equal, before this warp's range
+  for (uint32_t r = 0; r < rank; ++r) {
+    at += ev_remote(smem_u32(&mine[0]), r);
+    eq += ev_remote(smem_u32(&mine[1]), r);
+  }
   for (int i = 0; i < warp; ++i) {
     at += sums[0][i];
     eq += sums[1][i];
   }
-  at += min(eq, need);
+  at += min(eq, need);   // kept positions before it
   for (int tb = t0; tb < t1; tb += 32) {
     const int t = tb + lane;
     const uint32_t k = t < t1 ? key_of(t) : 0u;
-    const unsigned mine = (1u << lane) - 1u;
+    const unsigned lower = (1u << lane) - 1u;
     const unsigned me = __ballot_sync(0xffffffffu, t < t1 && k == prefix);
-    const bool keep = t < t1 && (k > prefix || (k == prefix && eq + __popc(me & mine) < need));
+    const bool keep = t < t1 && (k > prefix || (k == prefix && eq + __popc(me & lower) < need));
     const unsigned mk = __ballot_sync(0xffffffffu, keep);
     if (keep) {
-      const int j = at + __popc(mk & mine);
+      const int j = at + __popc(mk & lower);
       kept[j] = t;
-      if (wout) wout[j] = w[t];
+      if (wout) wout[j] = weight_of(t);
     }
     at += __popc(mk);
     eq += __popc(me);
   }
+  ev_cluster_sync();   // no CTA leaves while another may read its counts
 }
 
 template <int D>
@@ -186,28 +285,30 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
     e_old[p] = KV8_EMIN;
     if (j < m) {
       const int t = kept[j];
-      const int32_t page = a.page_table[(int64_t)b * a.pt_stride + t / a.P];
+      const int32_t page = a.page_table[(int64_t)b * a.pt_stride + (t >> a.log2P)];
       if (page < 0 || page >= a.num_pages) {
         if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);   // the row becomes zeros
       } else {
-        const int slot = t % a.P;
+        const int slot = t & (a.P - 1);
         const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
         x[p] = *reinterpret_cast<const uint4*>(rec + kind * a.codes_region +
-                                               ((int64_t)h * a.P + slot) * D + li * 16);
+                                               (int64_t)(h * a.P + slot) * D + li * 16);
         e_old[p] = exp8_of_scale(
             *(reinterpret_cast<const float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
               h * (a.P / KV8_BLOCK) + slot / KV8_BLOCK));
       }
     }
     const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-    uint32_t top = 0;   // largest finite magnitude code (its order is that of the values)
+    // largest finite magnitude code (the codes' order is that of the values)
+    uint32_t m4 = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t c = (w[i] >> (8 * k)) & 0x7Fu;
-        if (c != 0x7Fu) top = max(top, c);
-      }
+    for (int i = 0; i < 4; ++i) {
+      uint32_t c = w[i] & 0x7F7F7F7Fu;
+      c &= ~__vcmpeq4(c, 0x7F7F7F7Fu);
+      m4 = __vmaxu2(m4, c & 0x00FF00FFu);
+      m4 = __vmaxu2(m4, (c >> 8) & 0x00FF00FFu);
+    }
+    const uint32_t top = max(m4 & 0xFFFFu, m4 >> 16);
     uint32_t lo, hi;
     f16x4_of_e4m3(top, lo, hi);
     amax = fmaxf(amax, f32x2_of_f16x2(lo).x * two8(e_old[p]));
@@ -219,17 +320,18 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) amax = fmaxf(amax, warp_max[i]);
   const int e = exp8_of(amax);
-  const int32_t page = j0 / a.P < a.dst_stride ? a.dst_table[(int64_t)b * a.dst_stride + j0 / a.P] : -1;
+  const int pd = j0 >> a.log2P, slot0 = j0 & (a.P - 1);
+  const int32_t page = pd < a.dst_stride ? a.dst_table[(int64_t)b * a.dst_stride + pd] : -1;
   if (page < 0 || page >= a.num_pages) {
     if (threadIdx.x == 0)
-      flag_error(a.err, j0 / a.P < a.dst_stride ? JF_DEV_ERR_PAGE_ID : JF_DEV_ERR_POSITION);
+      flag_error(a.err, pd < a.dst_stride ? JF_DEV_ERR_PAGE_ID : JF_DEV_ERR_POSITION);
     return;
   }
   uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  uint8_t* const codes = rec + kind * a.codes_region + ((int64_t)h * a.P + j0 % a.P) * D;
+  uint8_t* const codes = rec + kind * a.codes_region + (int64_t)(h * a.P + slot0) * D;
   if (threadIdx.x == 0)
     *(reinterpret_cast<float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
-      h * (a.P / KV8_BLOCK) + (j0 % a.P) / KV8_BLOCK) = two8(e);
+      h * (a.P / KV8_BLOCK) + slot0 / KV8_BLOCK) = two8(e);
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int row = p * RPP + rr;
@@ -259,6 +361,7 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   a.codes_region = g.codes_region;
   a.sb_region = g.sb_region;
   a.P = g.P;
+  a.log2P = __builtin_ctz((unsigned)g.P);
   a.Hkv = g.Hkv;
   a.B = batch;
   a.page_table = page_table;
@@ -279,12 +382,30 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)g.Hkv, (unsigned)batch);
+  // CTAs per row: one for each EV_SLICE keys of the longest row there may be, in
+  // powers of two (262,144 keys of 4 rows: one CTA a row took 430 us of four
+  // byte-wise passes over memory)
+  int cl = 1;
+  while (cl < EV_MAX_CLUSTER && wstride > (int64_t)cl * EV_SLICE) cl *= 2;
+  const int64_t cap = (wstride + 32 * cl - 1) / (32 * cl) * 32;
+  a.key_cap = (int32_t)(cap <= EV_MAX_KEYS ? cap : 0);
+  if (smem_optin((const void*)kv8_select_kernel, EV_MAX_KEYS * 4) != JF_OK) return JF_ERR_CUDA;
+  cudaLaunchAttribute attrs[2];
+  attrs[0] = pdl[0];
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = (unsigned)cl;
+  attrs[1].val.clusterDim.y = 1;
+  attrs[1].val.clusterDim.z = 1;
+  cfg.gridDim = dim3((unsigned)cl, (unsigned)g.Hkv, (unsigned)batch);
   cfg.blockDim = dim3(EV_THREADS);
+  cfg.dynamicSmemBytes = (size_t)a.key_cap * 4;
   cfg.stream = stream;
+  cfg.attrs = attrs;
+  cfg.numAttrs = 2;
+  if (cudaLaunchKernelEx(&cfg, kv8_select_kernel, a) != cudaSuccess) return JF_ERR_CUDA;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, kv8_select_kernel, a) != cudaSuccess) return JF_ERR_CUDA;
+  cfg.dynamicSmemBytes = 0;
   cfg.gridDim = dim3((unsigned)((budget + KV8_BLOCK - 1) / KV8_BLOCK), (unsigned)(2 * g.Hkv),
                      (unsigned)batch);
   cfg.blockDim = dim3(256);

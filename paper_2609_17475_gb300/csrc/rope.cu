@@ -4,8 +4,9 @@
 // Pair i of a head's first R channels is a point (x, y) turned by the angle
 // pos[axis_i, t] * f_i:  (x cos - y sin, x sin + y cos); channels past R pass
 // through.  The angle depends on the token alone, so a CTA works out the R/2
-// cosines and sines of its token once in shared memory and turns every query
-// and key head with them, 16 bytes of a row per thread and step.
+// cosines and sines of its tokens once in shared memory and turns every query
+// and key head with them, 16 bytes of a row (two pieces with half pairing) per
+// thread and step.
 //
 // The angle is kept as a fraction of a turn in 64-bit fixed point: the host
 // rounds f_i / (2 pi) to a multiple of 2^-64 and pos * that, modulo 2^64, is
@@ -17,8 +18,11 @@
 
 namespace jfkv {
 
+int sm_count();
+
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_MAX_PAIRS = 128;
+constexpr int ROPE_MAX_TPB = 4;     // tokens per CTA
 
 struct RopeSide {
   const uint8_t* in;
@@ -32,6 +36,7 @@ struct RopeArgs {
   const int32_t* pos;
   int64_t pos_stride;            // elements between the axes' rows
   int32_t n_tokens;
+  int32_t tpb;                   // tokens per CTA
   int32_t D;                     // channels per head
   int32_t R;                     // rotated channels
   int32_t adjacent;              // pairs (2i, 2i+1) instead of (i, i + R/2)
@@ -41,85 +46,143 @@ struct RopeArgs {
   uint8_t axis[ROPE_MAX_PAIRS];
 };
 
-template <typename T> struct Elem;
-template <> struct Elem<__nv_bfloat16> {
-  static __device__ __forceinline__ float get(__nv_bfloat16 x) { return __bfloat162float(x); }
-  static __device__ __forceinline__ __nv_bfloat16 put(float x) { return __float2bfloat16_rn(x); }
+// 16 bytes of elements <-> fp32, two elements an instruction where there is one
+template <typename T> struct Pack;
+template <> struct Pack<__nv_bfloat16> {
+  static __device__ __forceinline__ void get(uint32_t w, float* x) {
+    x[0] = bf16lo_to_f32(w);
+    x[1] = bf16hi_to_f32(w);
+  }
+  static __device__ __forceinline__ uint32_t put(const float* x) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(x[1]), "f"(x[0]));
+    return r;
+  }
 };
-template <> struct Elem<__half> {
-  static __device__ __forceinline__ float get(__half x) { return __half2float(x); }
-  static __device__ __forceinline__ __half put(float x) { return __float2half_rn(x); }
+template <> struct Pack<__half> {
+  static __device__ __forceinline__ void get(uint32_t w, float* x) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    x[0] = f.x;
+    x[1] = f.y;
+  }
+  static __device__ __forceinline__ uint32_t put(const float* x) { return pack_f16x2(x[0], x[1]); }
 };
-template <> struct Elem<float> {
-  static __device__ __forceinline__ float get(float x) { return x; }
-  static __device__ __forceinline__ float put(float x) { return x; }
+template <> struct Pack<float> {
+  static __device__ __forceinline__ void get(uint32_t w, float* x) { x[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ uint32_t put(const float* x) { return __float_as_uint(x[0]); }
 };
-
 template <typename T>
-union Vec16 {
-  uint4 w;
-  T e[16 / sizeof(T)];
-  __device__ Vec16() : w(make_uint4(0u, 0u, 0u, 0u)) {}
-};
-
+__device__ __forceinline__ void unpack16(const uint4& v, float (&x)[16 / sizeof(T)]) {
+  constexpr int E = 4 / sizeof(T);   // elements of a word
+  Pack<T>::get(v.x, x);
+  Pack<T>::get(v.y, x + E);
+  Pack<T>::get(v.z, x + 2 * E);
+  Pack<T>::get(v.w, x + 3 * E);
+}
 template <typename T>
+__device__ __forceinline__ uint4 pack16(const float (&x)[16 / sizeof(T)]) {
+  constexpr int E = 4 / sizeof(T);
+  return make_uint4(Pack<T>::put(x), Pack<T>::put(x + E), Pack<T>::put(x + 2 * E),
+                    Pack<T>::put(x + 3 * E));
+}
+
+// `tpb` tokens a CTA.  Threads 0 .. per * steps - 1 work: thread u has place
+// u % steps of every per-th of the CTA's (token, head) pairs, the next pair's
+// loads issued before the current one is turned.
+template <typename T, bool ADJ>
 __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int V = 16 / sizeof(T);
-  __shared__ float2 cs[ROPE_MAX_PAIRS];
+  constexpr int NC = ADJ ? V / 2 : V;      // pairs of a place
+  __shared__ __align__(16) float2 cs[ROPE_MAX_TPB * ROPE_MAX_PAIRS];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int64_t t = blockIdx.x;
   const int half = a.R / 2;
-  for (int i = threadIdx.x; i < half; i += ROPE_THREADS) {
-    const int32_t p = a.pos[a.axis[i] * a.pos_stride + t];
+  const int64_t t0 = (int64_t)blockIdx.x * a.tpb;
+  const int nt = (int)min((int64_t)a.tpb, a.n_tokens - t0);
+  // places of a head: those turned, then the channels that pass through
+  const int turned = ADJ ? a.R / V : half / V;
+  const int steps = turned + (a.D - a.R) / V;
+  const int per = ROPE_THREADS / steps;    // pairs side by side (D <= 512: at least two)
+  const int h0 = threadIdx.x / steps, k = threadIdx.x - h0 * steps;
+  const int hq = a.side[0].heads, heads = hq + a.side[1].heads;
+  const bool turn = k < turned;
+  const int d = turn ? k * V : a.R + (k - turned) * V;
+  const bool second = !ADJ && turn;
+  // (token j, head h) -> its input and output places
+  auto place = [&](int j, int h, const T*& in, T*& out) {
+    const RopeSide& sd = a.side[h >= hq];
+    const int hh = h >= hq ? h - hq : h;
+    in = reinterpret_cast<const T*>(sd.in) + (t0 + j) * sd.in_token + hh * sd.in_head + d;
+    out = reinterpret_cast<T*>(sd.out) + (t0 + j) * sd.out_token + hh * sd.out_head + d;
+  };
+  int j = 0, h = h0;
+  auto settle = [&]() {
+    while (h >= heads) {
+      h -= heads;
+      ++j;
+    }
+  };
+  settle();
+  bool live = h0 < per && j < nt;
+  const T* in = nullptr;
+  T* out = nullptr;
+  uint4 v0 = make_uint4(0u, 0u, 0u, 0u), v1 = v0;
+  if (live) {
+    place(j, h, in, out);
+    v0 = *reinterpret_cast<const uint4*>(in);
+    if (second) v1 = *reinterpret_cast<const uint4*>(in + half);
+  }
+  for (int u = threadIdx.x; u < nt * half; u += ROPE_THREADS) {
+    const int jj = u / half, i = u - jj * half;
+    const int32_t p = a.pos[a.axis[i] * a.pos_stride + t0 + jj];
     const uint64_t turns = (uint64_t)(int64_t)p * a.turn[i];
     // the nearest signed fraction of a turn, in half turns
     const float x = (float)(int32_t)(turns >> 32) * 4.656612873077393e-10f;   // 2^-31
     float s, c;
     sincospif(x, &s, &c);
-    cs[i] = make_float2(c, a.inverse ? -s : s);
+    cs[u] = make_float2(c, a.inverse ? -s : s);
   }
   __syncthreads();
-  // steps of a head: half pairing turns two vectors at once; then the
-  // channels that pass through
-  const int turn_steps = a.adjacent ? a.R / V : half / V;
-  const int steps = turn_steps + (a.D - a.R) / V;
-  const int heads = a.side[0].heads + a.side[1].heads;
-  for (int u = threadIdx.x; u < heads * steps; u += ROPE_THREADS) {
-    const int h = u / steps, k = u % steps;
-    const bool key = h >= a.side[0].heads;
-    const RopeSide& sd = a.side[key];
-    const int hh = key ? h - a.side[0].heads : h;
-    const T* in = reinterpret_cast<const T*>(sd.in) + t * sd.in_token + hh * sd.in_head;
-    T* out = reinterpret_cast<T*>(sd.out) + t * sd.out_token + hh * sd.out_head;
-    if (k >= turn_steps) {
-      const int d = a.R + (k - turn_steps) * V;
-      if (in != out)
-        *reinterpret_cast<uint4*>(out + d) = *reinterpret_cast<const uint4*>(in + d);
-    } else if (a.adjacent) {
-      Vec16<T> x, y;
-      x.w = *reinterpret_cast<const uint4*>(in + k * V);
+  while (live) {
+    const uint4 x0 = v0, x1 = v1;
+    T* const to = out;
+    const bool same = in == out;
+    const int jc = j;
+    h += per;
+    settle();
+    live = j < nt;
+    if (live) {
+      place(j, h, in, out);
+      v0 = *reinterpret_cast<const uint4*>(in);
+      if (second) v1 = *reinterpret_cast<const uint4*>(in + half);
+    }
+    if (turn) {
+      const float4* const w = reinterpret_cast<const float4*>(cs + jc * half + k * NC);
+      float p0[V], p1[V], y0[V], y1[V];
+      unpack16<T>(x0, p0);
+      if (!ADJ) unpack16<T>(x1, p1);
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
-        const float2 w = cs[k * (V / 2) + i];
-        const float p = Elem<T>::get(x.e[2 * i]), q = Elem<T>::get(x.e[2 * i + 1]);
-        y.e[2 * i] = Elem<T>::put(p * w.x - q * w.y);
-        y.e[2 * i + 1] = Elem<T>::put(p * w.y + q * w.x);
-      }
-      *reinterpret_cast<uint4*>(out + k * V) = y.w;
-    } else {
-      Vec16<T> x0, x1, y0, y1;
-      x0.w = *reinterpret_cast<const uint4*>(in + k * V);
-      x1.w = *reinterpret_cast<const uint4*>(in + half + k * V);
+      for (int i = 0; i < NC; i += 2) {
+        const float4 f = w[i / 2];   // cosine and sine of pairs i and i + 1
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float2 w = cs[k * V + i];
-        const float p = Elem<T>::get(x0.e[i]), q = Elem<T>::get(x1.e[i]);
-        y0.e[i] = Elem<T>::put(p * w.x - q * w.y);
-        y1.e[i] = Elem<T>::put(p * w.y + q * w.x);
+        for (int e = 0; e < 2; ++e) {
+          const float c = e ? f.z : f.x, s = e ? f.w : f.y;
+          const float p = ADJ ? p0[2 * (i + e)] : p0[i + e];
+          const float q = ADJ ? p0[2 * (i + e) + 1] : p1[i + e];
+          const float r0 = p * c - q * s, r1 = p * s + q * c;
+          if (ADJ) {
+            y0[2 * (i + e)] = r0;
+            y0[2 * (i + e) + 1] = r1;
+          } else {
+            y0[i + e] = r0;
+            y1[i + e] = r1;
+          }
+        }
       }
-      *reinterpret_cast<uint4*>(out + k * V) = y0.w;
-      *reinterpret_cast<uint4*>(out + half + k * V) = y1.w;
+      *reinterpret_cast<uint4*>(to) = pack16<T>(y0);
+      if (!ADJ) *reinterpret_cast<uint4*>(to + half) = pack16<T>(y1);
+    } else if (!same) {
+      *reinterpret_cast<uint4*>(to) = x0;
     }
   }
 }
@@ -168,16 +231,29 @@ int launch_rope(const jf_rope& rope, const int32_t* positions, int64_t pos_strid
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)n_tokens);
+  // a token a CTA while that fills the GPU no more than a few times over, more
+  // for long runs, where the cosines and the launch of a CTA weigh more
+  a.tpb = n_tokens >= 16 * sm_count() ? 4 : 1;
+  cfg.gridDim = dim3((unsigned)((n_tokens + a.tpb - 1) / a.tpb));
   cfg.blockDim = dim3(ROPE_THREADS);
   cfg.stream = stream;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   cudaError_t e;
+  const bool adj = a.adjacent != 0;
   switch (dtype) {
-    case JF_DTYPE_BF16: e = cudaLaunchKernelEx(&cfg, rope_kernel<__nv_bfloat16>, a); break;
-    case JF_DTYPE_F16: e = cudaLaunchKernelEx(&cfg, rope_kernel<__half>, a); break;
-    default: e = cudaLaunchKernelEx(&cfg, rope_kernel<float>, a); break;
+    case JF_DTYPE_BF16:
+      e = adj ? cudaLaunchKernelEx(&cfg, rope_kernel<__nv_bfloat16, true>, a)
+              : cudaLaunchKernelEx(&cfg, rope_kernel<__nv_bfloat16, false>, a);
+      break;
+    case JF_DTYPE_F16:
+      e = adj ? cudaLaunchKernelEx(&cfg, rope_kernel<__half, true>, a)
+              : cudaLaunchKernelEx(&cfg, rope_kernel<__half, false>, a);
+      break;
+    default:
+      e = adj ? cudaLaunchKernelEx(&cfg, rope_kernel<float, true>, a)
+              : cudaLaunchKernelEx(&cfg, rope_kernel<float, false>, a);
+      break;
   }
   return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
