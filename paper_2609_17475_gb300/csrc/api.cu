@@ -607,7 +607,7 @@ size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int
   if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return 0;
   const size_t n = jf_attn_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_splits);
   if (n == 0) return 0;
-  return (n + 255) / 256 * 256 + (size_t)batch * num_q_heads * (size_t)weight_stride * 4;
+  return (n + 255) / 256 * 256 + (size_t)batch * num_q_heads * (((size_t)weight_stride + 3) / 4 * 16 + 8);
 }
 
 int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_table,

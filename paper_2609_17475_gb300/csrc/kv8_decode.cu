@@ -29,8 +29,10 @@
 // its largest element in [2^13, 2^14) (exact for elements within 2^27 of it);
 // probabilities enter P V as fp16 (11 bits); sums are fp32.
 //
-// Finish kernel.  Merges the pieces' partials, and where weights are asked
-// for turns the scores the split kernel left in the workspace into
+// Merge kernel.  Joins the pieces' partials of each query row:
+//   o = sum_s 2^(m_s - m) O_s / l,  l = sum_s 2^(m_s - m) l_s.
+// Weigh kernel.  Where weights are asked for, the split kernel leaves the
+// scores x in the workspace (they mostly stay in L2) and the merge m and 1/l;
 //   weights_out[b, h, t] = weights_in[b, h, t] + sum_g 2^(x_gt - m_g) / l_g.
 #include <cmath>
 
@@ -42,7 +44,8 @@ int sm_count();
 
 constexpr int K8_CH = 32;       // positions per plan chunk
 constexpr int K8_SUB = 16;      // positions per pipeline stage
-constexpr int K8_NW = 12;       // warps per CTA
+constexpr int K8_NW = 12;       // warps per CTA, one CTA per SM (two of 6 warps share the SM
+                                // unevenly: one request of 262,144 positions 103 us, not 88)
 constexpr int K8_HDR = 8;       // plan places standing for a segment's start
 constexpr int K8_MIN_W = 6;     // least places per piece (one stage for each warp)
 constexpr float K8_TOP = 14.f;  // 2^(y - m) stays below 2^14
@@ -65,11 +68,13 @@ struct Kv8DecodeArgs {
   int32_t* status;
   int32_t budget;           // pieces per KV head
   float scale_log2;
-  float* scores;            // [B, Hq, wstride] or null
+  float* scores;            // [B, Hq, sstride] or null
+  int64_t sstride;          // wstride rounded up to 4: 16-byte rows
+  float2* row_ml;           // [B, Hq] (m, 1 / l) for the weigh kernel
   const float* w_in;        // [B, Hkv, wstride] or null (zeros)
   float* w_out;
   int64_t wstride;
-  int32_t merge_blocks;     // finish kernel: CTAs that merge, then those that weigh
+  int32_t slices;           // merging CTAs per query row
 };
 
 // ---- plan: the requests' 32-position chunks laid end to end, each request's
@@ -417,9 +422,9 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
     }
     float *sc0 = nullptr, *sc1 = nullptr;
     if constexpr (WEIGH) {
-      float* const base = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.wstride;
-      if (2 * c < a.G) sc0 = base + (int64_t)(2 * c) * a.wstride;
-      if (2 * c + 1 < a.G) sc1 = base + (int64_t)(2 * c + 1) * a.wstride;
+      float* const base = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.sstride;
+      if (2 * c < a.G) sc0 = base + (int64_t)(2 * c) * a.sstride;
+      if (2 * c + 1 < a.G) sc1 = base + (int64_t)(2 * c + 1) * a.sstride;
     }
 
     K8State<D> st;
@@ -548,61 +553,58 @@ __device__ K8Rows k8_rows(const Kv8DecodeArgs& a, int b, int lane) {
 }
 
 constexpr int K8F_THREADS = 256;
-constexpr int K8F_COLS = 64;                       // columns of an output row per merging CTA
-constexpr int K8F_TILE = 1024;                     // positions per weighing CTA
+constexpr int K8F_COLS = 64;                       // columns of an output row per merging step
 
-// Merging CTA: 64 columns of one query row; warp w sums the partials w, w + 8,
-// ... of two columns a lane.  Weighing CTA: 1,024 positions of one KV head.
+// A CTA takes one query row, every `slices`-th run of 64 columns of it; warp w
+// sums the partials w, w + 8, ... of two columns a lane.
 template <int D>
-__global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8DecodeArgs a) {
+__global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeArgs a) {
   constexpr float NEG = -INFINITY;
   __shared__ float2 red[8][32];
-  __shared__ float2 gml[8];
+  __shared__ float red_l[8];
   __shared__ int plan[2];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
-  auto plan_of = [&](int b) {   // one warp works it out
-    if (warp == 0) {
-      const K8Rows rows = k8_rows(a, b, lane);
-      if (lane == 0) {
-        plan[0] = rows.row;
-        plan[1] = rows.n;
-      }
+  const int sl0 = blockIdx.x % a.slices;
+  const int hq = (blockIdx.x / a.slices) % a.Hq;
+  const int b = blockIdx.x / (a.slices * a.Hq);
+  if (sl0 == 0 && hq == 0 && threadIdx.x == 0) {
+    const int64_t ctx = a.ctx[b];
+    if (ctx < 0 || ctx > (int64_t)a.pt_stride * a.P || (a.w_out && ctx > a.wstride))
+      flag_error(a.status, JF_DEV_ERR_POSITION);
+  }
+  if (warp == 0) {   // one warp works the plan out
+    const K8Rows r = k8_rows(a, b, lane);
+    if (lane == 0) {
+      plan[0] = r.row;
+      plan[1] = r.n;
     }
-    __syncthreads();
-    return K8Rows{plan[0], plan[1]};
-  };
-  if ((int)blockIdx.x < a.merge_blocks) {
-    constexpr int SL = D / K8F_COLS;
-    const int sl = blockIdx.x % SL;
-    const int hq = (blockIdx.x / SL) % a.Hq;
-    const int b = blockIdx.x / (SL * a.Hq);
-    if (sl == 0 && hq == 0 && threadIdx.x == 0) {
-      const int64_t ctx = a.ctx[b];
-      if (ctx < 0 || ctx > (int64_t)a.pt_stride * a.P || (a.w_out && ctx > a.wstride))
-        flag_error(a.status, JF_DEV_ERR_POSITION);
-    }
-    const K8Rows rows = plan_of(b);
-    float M = NEG;
-    for (int s = lane; s < rows.n; s += 32) M = fmaxf(M, ml[(int64_t)(rows.row + s) * a.Hq + hq].x);
+  }
+  __syncthreads();
+  const K8Rows rows{plan[0], plan[1]};
+  float M = NEG;
+  for (int s = lane; s < rows.n; s += 32) M = fmaxf(M, ml[(int64_t)(rows.row + s) * a.Hq + hq].x);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  for (int sl = sl0; sl < D / K8F_COLS; sl += a.slices) {
     float l = 0.f;
     float2 acc = make_float2(0.f, 0.f);
-#pragma unroll 4
+#pragma unroll 5
     for (int s = warp; s < rows.n; s += 8) {
       const int64_t row = (int64_t)(rows.row + s) * a.Hq + hq;
       const float2 v = ml[row];
-      const float2 o = *reinterpret_cast<const float2*>(a.part_o + row * D + sl * K8F_COLS + 2 * lane);
+      const float2 o =
+          *reinterpret_cast<const float2*>(a.part_o + row * D + sl * K8F_COLS + 2 * lane);
       const float f = v.x == NEG ? 0.f : fast_exp2(v.x - M);
       l = fmaf(f, v.y, l);
       acc.x = fmaf(f, o.x, acc.x);
       acc.y = fmaf(f, o.y, acc.y);
     }
+    __syncthreads();   // red is free again
     red[warp][lane] = acc;
-    if (lane == 0) gml[warp].x = l;
+    if (lane == 0) red_l[warp] = l;
     __syncthreads();
     if (warp == 0) {
       acc = make_float2(0.f, 0.f);
@@ -611,65 +613,55 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_finish_kernel(const Kv8Decode
       for (int w = 0; w < 8; ++w) {
         acc.x += red[w][lane].x;
         acc.y += red[w][lane].y;
-        l += gml[w].x;
+        l += red_l[w];
       }
       const float inv = l != 0.f ? 1.f / l : 0.f;   // nothing attended: zeros
-      const uint32_t o = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.x * inv)) |
-                         ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.y * inv)) << 16);
-      reinterpret_cast<uint32_t*>(a.out + ((int64_t)b * a.Hq + hq) * D + sl * K8F_COLS)[lane] = o;
+      reinterpret_cast<uint32_t*>(a.out + ((int64_t)b * a.Hq + hq) * D + sl * K8F_COLS)[lane] =
+          pack_bf16x2_rn(acc.x * inv, acc.y * inv);
+      if (a.row_ml && sl == 0 && lane == 0) a.row_ml[(int64_t)b * a.Hq + hq] = make_float2(M, inv);
     }
-    return;
   }
-  // ---- weights -----------------------------------------------------------------
-  const int tiles = (int)((a.wstride + K8F_TILE - 1) / K8F_TILE);
-  const int u = (int)blockIdx.x - a.merge_blocks;
-  const int tile = u % tiles;
-  const int kvh = (u / tiles) % a.Hkv;
-  const int b = u / (tiles * a.Hkv);
+}
+
+constexpr int K8W_TILE = 8 * K8F_THREADS;   // positions per weighing CTA: two steps of 4 a thread
+
+__global__ void __launch_bounds__(K8F_THREADS) kv8_weigh_kernel(const Kv8DecodeArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int kvh = blockIdx.y, b = blockIdx.z;
   const int n = (int)min((int64_t)k8_ctx(a, b), a.wstride);
-  const int t0 = tile * K8F_TILE;
+  const int64_t t0 = (int64_t)blockIdx.x * K8W_TILE;
   if (t0 >= n) return;
-  const K8Rows rows = plan_of(b);
-  if (warp < a.G) {   // warp g: the reference and 1 / l of head g
-    const int hq = kvh * a.G + warp;
-    float M = NEG, l = 0.f;
-    for (int s = lane; s < rows.n; s += 32) M = fmaxf(M, ml[(int64_t)(rows.row + s) * a.Hq + hq].x);
+  float2 m[8];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    for (int s = lane; s < rows.n; s += 32) {
-      const float2 v = ml[(int64_t)(rows.row + s) * a.Hq + hq];
-      if (v.x != NEG) l = fmaf(fast_exp2(v.x - M), v.y, l);
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) gml[warp] = make_float2(M, l != 0.f ? 1.f / l : 0.f);
-  }
-  __syncthreads();
-  const float* const sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.wstride;
+  for (int g = 0; g < 8; ++g)
+    if (g < a.G) m[g] = a.row_ml[(int64_t)b * a.Hq + kvh * a.G + g];
+  // a thread takes four adjacent positions a step; the heads' scores are all
+  // loaded before any is used
+  const float* const sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.sstride;
   const int64_t wrow = ((int64_t)b * a.Hkv + kvh) * a.wstride;
-  constexpr int NT = K8F_TILE / K8F_THREADS;   // positions per thread
-  float add[NT], w[NT];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int t = t0 + i * K8F_THREADS + threadIdx.x;
-    add[i] = 0.f;
-    w[i] = a.w_in && t < n ? a.w_in[wrow + t] : 0.f;
-  }
-  for (int g = 0; g < a.G; ++g) {
-    const float2 m = gml[g];
-    float x[NT];
+  for (int step = 0; step < K8W_TILE / (4 * K8F_THREADS); ++step) {
+    const int t = (int)t0 + (step * K8F_THREADS + threadIdx.x) * 4;
+    if (t >= n) return;
+    float4 x[8];
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-      const int t = t0 + i * K8F_THREADS + threadIdx.x;
-      x[i] = t < n ? sc[(int64_t)g * a.wstride + t] : NEG;
-    }
+    for (int g = 0; g < 8; ++g)
+      if (g < a.G) x[g] = __ldcs(reinterpret_cast<const float4*>(sc + (int64_t)g * a.sstride + t));
+    float w[4], add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < NT; ++i) add[i] = fmaf(fast_exp2(x[i] - m.x), m.y, add[i]);
-  }
+    for (int i = 0; i < 4; ++i) w[i] = a.w_in && t + i < n ? a.w_in[wrow + t + i] : 0.f;
 #pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    const int t = t0 + i * K8F_THREADS + threadIdx.x;
-    if (t < n) a.w_out[wrow + t] = w[i] + add[i];
+    for (int g = 0; g < 8; ++g)
+      if (g < a.G) {
+        add[0] = fmaf(fast_exp2(x[g].x - m[g].x), m[g].y, add[0]);
+        add[1] = fmaf(fast_exp2(x[g].y - m[g].x), m[g].y, add[1]);
+        add[2] = fmaf(fast_exp2(x[g].z - m[g].x), m[g].y, add[2]);
+        add[3] = fmaf(fast_exp2(x[g].w - m[g].x), m[g].y, add[3]);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i < n) a.w_out[wrow + t + i] = w[i] + add[i];
   }
 }
 
@@ -692,20 +684,23 @@ static int launch_t(const CUtensorMap& tmap, const Kv8DecodeArgs& a, cudaStream_
   cfg.stream = stream;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  cudaError_t e = weigh ? cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, true>, tmap, a)
-                        : cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, false>, tmap, a);
+  const cudaError_t e = weigh ? cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, true>, tmap, a)
+                              : cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, false>, tmap, a);
   if (e != cudaSuccess) return JF_ERR_CUDA;
-  int64_t blocks = a.merge_blocks;
-  if (weigh) blocks += (a.wstride + K8F_TILE - 1) / K8F_TILE * a.Hkv * a.B;
-  if (blocks > 0x7FFFFFFF) return JF_ERR_UNSUPPORTED;
-  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.gridDim = dim3((unsigned)(a.slices * a.Hq * a.B));
   cfg.blockDim = dim3(K8F_THREADS);
   cfg.dynamicSmemBytes = 0;
-  e = cudaLaunchKernelEx(&cfg, kv8_finish_kernel<D>, a);
-  return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, kv8_merge_kernel<D>, a) != cudaSuccess) return JF_ERR_CUDA;
+  if (weigh) {
+    cfg.gridDim = dim3((unsigned)((a.wstride + K8W_TILE - 1) / K8W_TILE), (unsigned)a.Hkv,
+                       (unsigned)a.B);
+    if (cudaLaunchKernelEx(&cfg, kv8_weigh_kernel, a) != cudaSuccess) return JF_ERR_CUDA;
+  }
+  return JF_OK;
 }
 
-// weights (w_out non-null): `scores` holds B * Hq * wstride floats
+// weights (w_out non-null): `scores`, 16-byte aligned, holds B * Hq * sstride
+// floats and then B * Hq pairs
 int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& tmap,
                       const int32_t* page_table, int32_t pt_stride, const int32_t* context_lens,
                       int32_t batch, const void* q, int32_t Hq, float softmax_scale, void* out,
@@ -743,9 +738,12 @@ int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& 
   a.w_in = w_in;
   a.w_out = w_out;
   a.wstride = wstride;
-  const int64_t mb = (int64_t)batch * Hq * (g.D / K8F_COLS);
-  if (mb > 0x7FFFFFFF || g.Hkv > 65535) return JF_ERR_UNSUPPORTED;
-  a.merge_blocks = (int32_t)mb;
+  a.sstride = (wstride + 3) / 4 * 4;
+  // few query rows: a CTA for each 64 columns; many: one for the row
+  const int64_t qrows = (int64_t)batch * Hq;
+  a.slices = qrows * (g.D / K8F_COLS) <= 4 * sm_count() ? g.D / K8F_COLS : 1;
+  if (qrows * a.slices > 0x7FFFFFFF || g.Hkv > 65535) return JF_ERR_UNSUPPORTED;
+  a.row_ml = w_out ? reinterpret_cast<float2*>(scores + qrows * a.sstride) : nullptr;
   return g.D == 256 ? launch_t<256>(tmap, a, stream) : launch_t<128>(tmap, a, stream);
 }
 
