@@ -42,6 +42,7 @@ int launch_kv8_rows(const Geom&, const jf_kv_pool&, const int32_t*, int32_t, int
                     const int32_t*, const int32_t*, void*, int64_t, void*, int64_t, int32_t,
                     int32_t*, bool, cudaStream_t);
 int kv8_box_rows();
+int64_t kv8_score_floats(int64_t G, int64_t wstride);
 int launch_kv8_decode(const Geom&, const jf_kv_pool&, const CUtensorMap&, const int32_t*, int32_t,
                       const int32_t*, int32_t, const void*, int32_t, float, void*, void*, int32_t,
                       float*, const float*, float*, int64_t, cudaStream_t);
@@ -607,7 +608,10 @@ size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int
   if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return 0;
   const size_t n = jf_attn_workspace_bytes(batch, num_q_heads, num_kv_heads, head_dim, num_splits);
   if (n == 0) return 0;
-  return (n + 255) / 256 * 256 + (size_t)batch * num_q_heads * (((size_t)weight_stride + 3) / 4 * 16 + 8);
+  return (n + 255) / 256 * 256 +
+         (size_t)batch * num_kv_heads *
+             (size_t)kv8_score_floats(num_q_heads / num_kv_heads, weight_stride) * 4 +
+         (size_t)batch * num_q_heads * 8;
 }
 
 int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_table,

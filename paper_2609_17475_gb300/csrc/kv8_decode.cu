@@ -34,6 +34,9 @@
 // Weigh kernel.  Where weights are asked for, the split kernel leaves the
 // scores x in the workspace (they mostly stay in L2) and the merge m and 1/l;
 //   weights_out[b, h, t] = weights_in[b, h, t] + sum_g 2^(x_gt - m_g) / l_g.
+// Scores lie as [chunk of 16 positions][8 positions of it][odd heads or even]
+// [pair of heads][8 positions], as the MMA leaves them, so that each store of
+// the split kernel is one run of 32 bytes a pair of heads.
 #include <cmath>
 
 #include "kv8.cuh"
@@ -68,8 +71,9 @@ struct Kv8DecodeArgs {
   int32_t* status;
   int32_t budget;           // pieces per KV head
   float scale_log2;
-  float* scores;            // [B, Hq, sstride] or null
-  int64_t sstride;          // wstride rounded up to 4: 16-byte rows
+  float* scores;            // [B, Hkv] blocks of sstride floats (above), or null
+  int64_t sstride;          // chunks of 16 positions x 32 x pairs
+  int32_t pairs;            // pairs of a KV head's query heads: ceil(G / 2)
   float2* row_ml;           // [B, Hq] (m, 1 / l) for the weigh kernel
   const float* w_in;        // [B, Hkv, wstride] or null (zeros)
   float* w_out;
@@ -185,8 +189,8 @@ struct K8State {
 template <int D, bool FULL>
 __device__ __forceinline__ void k8_chunk(K8State<D>& st, const uint32_t (&qf)[D / 16][2],
                                          uint32_t kb, int r, int c, float cA0, float cA1,
-                                         float ks, float ve, float vinv, int nv, float* sc0,
-                                         float* sc1) {
+                                         float ks, float ve, float vinv, int nv, float* sc,
+                                         int pairs, bool h0, bool h1) {
   constexpr int HV = D / 128;
   constexpr float NEG = -INFINITY;
   const int pr = k8_pos<D>(r);       // position of MMA row r; row r + 8: pr + 8
@@ -215,13 +219,12 @@ __device__ __forceinline__ void k8_chunk(K8State<D>& st, const uint32_t (&qf)[D 
   x[2] = (s[2] + s2[2]) * f0;
   x[3] = (s[3] + s2[3]) * f1;
   const bool va = FULL || pr < nv, vb = FULL || pr + 8 < nv;
-  if (sc0) {   // scores of this stage's positions (log2 domain)
-    if (va) sc0[pr] = x[0];
-    if (vb) sc0[pr + 8] = x[2];
-  }
-  if (sc1) {
-    if (va) sc1[pr] = x[1];
-    if (vb) sc1[pr + 8] = x[3];
+  if (sc) {   // this stage's scores (log2 domain) of this thread's heads, if they exist
+    sc += pr;
+    if (h0 && va) sc[0] = x[0];
+    if (h1 && va) sc[8 * pairs] = x[1];
+    if (h0 && vb) sc[16 * pairs] = x[2];
+    if (h1 && vb) sc[24 * pairs] = x[3];
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? va : vb) ? x[i] + ve : NEG;
@@ -420,12 +423,8 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
       cA0 = __shfl_sync(0xffffffffu, mine, 8 * c);       // lane of head 2c: r = 2c, c = 0
       cA1 = __shfl_sync(0xffffffffu, mine, 8 * c + 4);
     }
-    float *sc0 = nullptr, *sc1 = nullptr;
-    if constexpr (WEIGH) {
-      float* const base = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.sstride;
-      if (2 * c < a.G) sc0 = base + (int64_t)(2 * c) * a.sstride;
-      if (2 * c + 1 < a.G) sc1 = base + (int64_t)(2 * c + 1) * a.sstride;
-    }
+    float* scb = nullptr;   // this thread's pair of heads in the segment's scores
+    if constexpr (WEIGH) scb = a.scores + ((int64_t)b * a.Hkv + kvh) * a.sstride + 8 * c;
 
     K8State<D> st;
     st.m0 = st.m1 = NEG;
@@ -455,14 +454,14 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
             const int nv = ((valid >> s) & 1u) ? lim - p0 : 0;
             const int ek = exp8_of_scale(ksc[s]), ev = exp8_of_scale(vsc[s]);
             const uint32_t kb = ring + rs * L::STAGE;
+            float* sc = nullptr;
+            if constexpr (WEIGH) sc = scb + (int64_t)(p0 / K8_SUB) * (32 * a.pairs);
             if (nv >= K8_SUB)
-              k8_chunk<D, true>(st, qf, kb, r, c, cA0, cA1, two8(ek), (float)ev, two8(-ev), 0,
-                                WEIGH && sc0 ? sc0 + p0 : nullptr,
-                                WEIGH && sc1 ? sc1 + p0 : nullptr);
+              k8_chunk<D, true>(st, qf, kb, r, c, cA0, cA1, two8(ek), (float)ev, two8(-ev), 0, sc,
+                                a.pairs, 2 * c < a.G, 2 * c + 1 < a.G);
             else
-              k8_chunk<D, false>(st, qf, kb, r, c, cA0, cA1, two8(ek), (float)ev, two8(-ev), nv,
-                                 WEIGH && sc0 ? sc0 + p0 : nullptr,
-                                 WEIGH && sc1 ? sc1 + p0 : nullptr);
+              k8_chunk<D, false>(st, qf, kb, r, c, cA0, cA1, two8(ek), (float)ev, two8(-ev), nv, sc,
+                                 a.pairs, 2 * c < a.G, 2 * c + 1 < a.G);
             __syncwarp();
             if (it + ST < my_n) {
               fence_proxy_async_smem();
@@ -638,16 +637,19 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_weigh_kernel(const Kv8DecodeA
     if (g < a.G) m[g] = a.row_ml[(int64_t)b * a.Hq + kvh * a.G + g];
   // a thread takes four adjacent positions a step; the heads' scores are all
   // loaded before any is used
-  const float* const sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.sstride;
+  const float* const sc = a.scores + ((int64_t)b * a.Hkv + kvh) * a.sstride;
   const int64_t wrow = ((int64_t)b * a.Hkv + kvh) * a.wstride;
 #pragma unroll
   for (int step = 0; step < K8W_TILE / (4 * K8F_THREADS); ++step) {
     const int t = (int)t0 + (step * K8F_THREADS + threadIdx.x) * 4;
     if (t >= n) return;
+    const float* const sx = sc + (int64_t)(t / K8_SUB) * (32 * a.pairs) +
+                            ((t >> 3) & 1) * (16 * a.pairs) + (t & 7);
     float4 x[8];
 #pragma unroll
     for (int g = 0; g < 8; ++g)
-      if (g < a.G) x[g] = __ldcs(reinterpret_cast<const float4*>(sc + (int64_t)g * a.sstride + t));
+      if (g < a.G)
+        x[g] = __ldcs(reinterpret_cast<const float4*>(sx + ((g & 1) * a.pairs + (g >> 1)) * 8));
     float w[4], add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = a.w_in && t + i < n ? a.w_in[wrow + t + i] : 0.f;
@@ -699,8 +701,13 @@ static int launch_t(const CUtensorMap& tmap, const Kv8DecodeArgs& a, cudaStream_
   return JF_OK;
 }
 
-// weights (w_out non-null): `scores`, 16-byte aligned, holds B * Hq * sstride
-// floats and then B * Hq pairs
+// floats of the scores of one (request, KV head)
+int64_t kv8_score_floats(int64_t G, int64_t wstride) {
+  return (wstride + K8_SUB - 1) / K8_SUB * 32 * ((G + 1) / 2);
+}
+
+// weights (w_out non-null): `scores`, 16-byte aligned, holds the scores of the
+// B * Hkv (request, KV head) pairs and then B * Hq float2
 int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& tmap,
                       const int32_t* page_table, int32_t pt_stride, const int32_t* context_lens,
                       int32_t batch, const void* q, int32_t Hq, float softmax_scale, void* out,
@@ -738,12 +745,14 @@ int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& 
   a.w_in = w_in;
   a.w_out = w_out;
   a.wstride = wstride;
-  a.sstride = (wstride + 3) / 4 * 4;
+  a.pairs = (a.G + 1) / 2;
+  a.sstride = kv8_score_floats(a.G, wstride);
   // few query rows: a CTA for each 64 columns; many: one for the row
   const int64_t qrows = (int64_t)batch * Hq;
   a.slices = qrows * (g.D / K8F_COLS) <= 4 * sm_count() ? g.D / K8F_COLS : 1;
   if (qrows * a.slices > 0x7FFFFFFF || g.Hkv > 65535) return JF_ERR_UNSUPPORTED;
-  a.row_ml = w_out ? reinterpret_cast<float2*>(scores + qrows * a.sstride) : nullptr;
+  a.row_ml = w_out ? reinterpret_cast<float2*>(scores + (int64_t)batch * g.Hkv * a.sstride)
+                   : nullptr;
   return g.D == 256 ? launch_t<256>(tmap, a, stream) : launch_t<128>(tmap, a, stream);
 }
 
