@@ -663,7 +663,6 @@ int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_s
   if (weight_stride < 1 || weight_stride > 0x7FFFFFFF) return JF_ERR_INVALID_ARG;
   if (budget < 1 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
     return JF_ERR_INVALID_ARG;
-  if (2 * (int64_t)pool->num_kv_heads > 65535) return JF_ERR_UNSUPPORTED;   // launch grid
   if (!aligned(weights, 4) || !aligned(dst_weights, 4)) return JF_ERR_INVALID_ARG;
   const Geom g = make_geom(*pool);
   return launch_kv8_evict(g, *pool, page_table, pt_stride, context_lens, batch, weights,

@@ -150,17 +150,16 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Args a) {
       *reinterpret_cast<uint2*>(codes + row * D + li * 8) = c;
     } else if (row < first && e > e_old) {   // the block grew: its earlier rows again
       uint2* const at = reinterpret_cast<uint2*>(codes + row * D + li * 8);
-      const float s = two8(e_old - e);
       uint2 c = *at;
-      c.x = rescale_e4m3x4(c.x, s);
-      c.y = rescale_e4m3x4(c.y, s);
+      c.x = rescale_e4m3x4(c.x, e_old - e);
+      c.y = rescale_e4m3x4(c.y, e_old - e);
       *at = c;
     }
   }
 }
 
-// Read back: a group of D/16 lanes takes the K (or V) vector of one row and
-// KV head, 16 codes a lane.
+// Read back: a group of D/16 lanes takes the K and V vectors of one row and
+// KV head, 16 codes of each a lane.
 template <int D>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
   constexpr int LPR = D / 16;
@@ -168,7 +167,7 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int li = threadIdx.x % LPR;
-  const int head = blockIdx.y, kind = blockIdx.z;
+  const int head = blockIdx.y;
   if (row >= a.n_rows) return;
   // the request of this row: the last b with row_offsets[b] <= row
   int lo = 0, hi = a.num_requests - 1;
@@ -190,25 +189,34 @@ __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
   }
   const int slot = pos & (a.P - 1);
   const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  const uint4 c = *reinterpret_cast<const uint4*>(rec + kind * a.codes_region +
-                                                  (int64_t)(head * a.P + slot) * D + li * 16);
-  const float s = two8(exp8_of_scale(
-      *(reinterpret_cast<const float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
-        head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK)));
-  const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-  uint32_t o[8];
+  const uint8_t* const code = rec + (int64_t)(head * a.P + slot) * D + li * 16;
+  const uint8_t* const scale =
+      rec + 2 * a.codes_region + (head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK) * 4;
+  uint4 c[2];
+  float s[2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t h0, h1;
-    f16x4_of_e4m3(w[i], h0, h1);
-    const float2 f0 = f32x2_of_f16x2(h0), f1 = f32x2_of_f16x2(h1);
-    o[2 * i] = pack_bf16x2_rn(f0.x * s, f0.y * s);
-    o[2 * i + 1] = pack_bf16x2_rn(f1.x * s, f1.y * s);
+  for (int kind = 0; kind < 2; ++kind) {
+    c[kind] = *reinterpret_cast<const uint4*>(code + kind * a.codes_region);
+    s[kind] = *reinterpret_cast<const float*>(scale + kind * a.sb_region);
   }
-  uint4* const dst = reinterpret_cast<uint4*>(
-      (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D + li * 16);
-  dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-  dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    const float two = two8(exp8_of_scale(s[kind]));
+    const uint32_t w[4] = {c[kind].x, c[kind].y, c[kind].z, c[kind].w};
+    uint32_t o[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t h0, h1;
+      f16x4_of_e4m3(w[i], h0, h1);
+      const float2 f0 = f32x2_of_f16x2(h0), f1 = f32x2_of_f16x2(h1);
+      o[2 * i] = pack_bf16x2_rn(f0.x * two, f0.y * two);
+      o[2 * i + 1] = pack_bf16x2_rn(f1.x * two, f1.y * two);
+    }
+    uint4* const dst = reinterpret_cast<uint4*>(
+        (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D + li * 16);
+    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  }
 }
 
 int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_table,
@@ -246,7 +254,7 @@ int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_t
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks, (unsigned)g.Hkv, 2u);
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)g.Hkv, read ? 1u : 2u);
   cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cfg.attrs = pdl;

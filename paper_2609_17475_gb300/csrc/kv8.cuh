@@ -55,13 +55,37 @@ __device__ __forceinline__ uint32_t pack_bf16x2_rn(float lo, float hi) {
   return r;
 }
 
-// the four codes of a word rounded again for a scale 2^s times smaller
-// (value = code * 2^s under the new scale)
-__device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, float two_s) {
+// The four codes of a word rounded again for a scale 2^-s times as large
+// (value = code * 2^s under the new scale, at most 448).  In fp16: products of
+// at least 2^-10, half the smallest code, are exact, and smaller ones become
+// zero either way; s < -24 leaves only those.
+__device__ __forceinline__ uint32_t f16x2_two(int s) {
+  const __half2 h = __float2half2_rn(s < -24 ? 0.f : two8(s));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t e4m3x4_of_f16x2(uint32_t lo, uint32_t hi) {
+  uint32_t r;
+  asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n"
+      "cvt.rn.satfinite.e4m3x2.f16x2 b, %2;\nmov.b32 %0, {a, b};\n}\n"
+      : "=r"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, int s) {
   uint32_t lo, hi;
   f16x4_of_e4m3(w, lo, hi);
-  const float2 a = f32x2_of_f16x2(lo), b = f32x2_of_f16x2(hi);
-  return e4m3x2(a.x * two_s, a.y * two_s) | (e4m3x2(b.x * two_s, b.y * two_s) << 16);
+  if (s > 15) {   // past fp16's powers of two: only subnormal codes get here
+    const uint32_t p = f16x2_two(15);
+    lo = mul_f16x2(lo, p);
+    hi = mul_f16x2(hi, p);
+    s -= 15;
+  }
+  const uint32_t p = f16x2_two(s);
+  return e4m3x4_of_f16x2(mul_f16x2(lo, p), mul_f16x2(hi, p));
 }
 
 }  // namespace jfkv

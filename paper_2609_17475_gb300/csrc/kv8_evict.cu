@@ -11,8 +11,8 @@
 // key.  The kept positions are then written in rising order: all above that
 // key, and the first of those that equal it.
 //
-// Compact kernel: a CTA gathers 32 kept positions of one KV head, K or V, and
-// writes them as one block of the destination pages.  The block gets the
+// Compact kernel: a CTA gathers 32 kept positions of one KV head and writes them
+// as one block, K and V, of the destination pages.  The block gets the
 // scale its own rows call for; a row whose old scale differs is rounded again
 // under it (an exact shift but for what falls below the smallest code).
 #include "kv8.cuh"
@@ -76,18 +76,20 @@ __device__ __forceinline__ void ev_cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n"
                "barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
-// the int at this CTA's shared address `addr`, in CTA `rank` of the cluster
-__device__ __forceinline__ int ev_remote(uint32_t addr, uint32_t rank) {
+// the ints at this CTA's shared address `addr` (8-byte aligned), in CTA `rank`
+// of the cluster
+__device__ __forceinline__ int2 ev_remote2(uint32_t addr, uint32_t rank) {
   uint32_t a;
-  int v;
+  int2 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.s32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];\n"
+               : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
   return v;
 }
 
 // One count per key with `in` set: the lanes that share the first such lane's
 // bin add once (weights crowd into few bins: exact zeros, one exponent), the
-// others each.
+// others each.  Whole warps.
 __device__ __forceinline__ void ev_count(int* hist, uint32_t bin, bool in, int lane) {
   const unsigned all = __ballot_sync(0xffffffffu, in);
   if (!all) return;
@@ -99,11 +101,12 @@ __device__ __forceinline__ void ev_count(int* hist, uint32_t bin, bool in, int l
 }
 
 __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictArgs a) {
-  extern __shared__ float slice_w[];        // this CTA's weights, or unused where they do not fit
-  __shared__ int hist[3][EV_BINS];          // one a pass: the cluster may still read the last one
+  extern __shared__ __align__(16) uint32_t keys[];   // this CTA's slice, or unused where it
+                                                     // does not fit
+  __shared__ __align__(8) int hist[3][EV_BINS];      // one a pass: the cluster may still read the last one
   __shared__ int sums[2][EV_WARPS];
   __shared__ int pick[2];
-  __shared__ int mine[2];                   // keys above, and equal to, the last one kept
+  __shared__ __align__(8) int mine[2];      // keys above, and equal to, the last one kept
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const uint32_t rank = ev_rank(), ranks = ev_ranks();
@@ -125,25 +128,38 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     }
     return;
   }
-  // this CTA's positions [p0, p1), a multiple of 32 but for the row's end
-  const int slice = (int)(((int64_t)n + 32 * (int64_t)ranks - 1) / (32 * (int64_t)ranks)) * 32;
+  // this CTA's positions [p0, p1), a multiple of 128 but for the row's end
+  const int slice = (int)(((int64_t)n + 128 * (int64_t)ranks - 1) / (128 * (int64_t)ranks)) * 128;
   const int p0 = (int)min((int64_t)rank * slice, (int64_t)n);
   const int p1 = (int)min((int64_t)p0 + slice, (int64_t)n);
   const bool cached = slice <= a.key_cap;
-  auto weight_of = [&](int t) -> float { return cached ? slice_w[t - p0] : w[t]; };
-  auto key_of = [&](int t) -> uint32_t {
-    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(weight_of(t));
+  auto make_key = [&](int t) -> uint32_t {
+    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(w[t]);
+  };
+  // the keys of positions t .. t + 3 (t - p0 a multiple of 4); those at or past
+  // p1 are not keys
+  auto load4 = [&](int t) -> uint4 {
+    if (cached) return *reinterpret_cast<const uint4*>(keys + (t - p0));
+    uint4 k;
+    k.x = make_key(t);
+    k.y = t + 1 < p1 ? make_key(t + 1) : 0u;
+    k.z = t + 2 < p1 ? make_key(t + 2) : 0u;
+    k.w = t + 3 < p1 ? make_key(t + 3) : 0u;
+    return k;
   };
   for (int i = tid; i < 3 * EV_BINS; i += EV_THREADS) hist[0][i] = 0;
-  if (cached) {   // 8 loads in flight a thread
-    for (int tb = p0 + tid; tb < p1; tb += 8 * EV_THREADS) {
-      float x[8];
+  if (cached) {   // 16 loads in flight a thread
+    constexpr int U = 16;
+    for (int tb = p0 + tid; tb < p1; tb += U * EV_THREADS) {
+      float x[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < U; ++u)
         if (tb + u * EV_THREADS < p1) x[u] = w[tb + u * EV_THREADS];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (tb + u * EV_THREADS < p1) slice_w[tb + u * EV_THREADS - p0] = x[u];
+      for (int u = 0; u < U; ++u) {
+        const int t = tb + u * EV_THREADS;
+        if (t < p1) keys[t - p0] = t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(x[u]);
+      }
     }
   }
   __syncthreads();
@@ -155,13 +171,20 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const int bits = pass == 2 ? 10 : 11;
     int* const hs = hist[pass];
-#pragma unroll 4
-    for (int tb = p0; tb < p1; tb += EV_THREADS) {
-      const int t = tb + tid;
-      const uint32_t k = t < p1 ? key_of(t) : 0u;
-      // whole warps take part
-      ev_count(hs, (k >> shift) & ((1u << bits) - 1u),
-               t < p1 && (pass == 0 || (k >> (shift + bits)) == prefix), lane);
+    const uint32_t mask = (1u << bits) - 1u;
+#pragma unroll 2
+    for (int tb = p0 + 128 * warp; tb < p1; tb += 128 * EV_WARPS) {   // whole warps take part
+      const int t = tb + 4 * lane;
+      const uint4 k4 = t < p1 ? load4(t) : make_uint4(0u, 0u, 0u, 0u);
+      const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+      bool in[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        in[i] = t + i < p1 && (pass == 0 || (k[i] >> (shift + bits)) == prefix);
+      // after the first digit few keys are left
+      if (pass > 0 && !__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ev_count(hs, (k[i] >> shift) & mask, in[i], lane);
     }
     ev_cluster_sync();
     // thread i sums bins top - 2i and top - 2i - 1 over the cluster; the
@@ -169,12 +192,17 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     const int top = (1 << bits) - 1;
     int c0 = 0, c1 = 0;
     if (2 * tid <= top) {
-      const uint32_t at = smem_u32(hs + top - 2 * tid);
-#pragma unroll 4
-      for (uint32_t r = 0; r < ranks; ++r) {
-        c0 += ev_remote(at, r);
-        c1 += ev_remote(at - 4, r);
-      }
+      const uint32_t at = smem_u32(hs + top - 2 * tid - 1);
+      int2 v[EV_MAX_CLUSTER];
+#pragma unroll
+      for (uint32_t r = 0; r < EV_MAX_CLUSTER; ++r)
+        if (r < ranks) v[r] = ev_remote2(at, r);
+#pragma unroll
+      for (uint32_t r = 0; r < EV_MAX_CLUSTER; ++r)
+        if (r < ranks) {
+          c0 += v[r].y;
+          c1 += v[r].x;
+        }
     }
     int incl = c0 + c1;
 #pragma unroll
@@ -184,8 +212,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     }
     if (lane == 31) sums[0][warp] = incl;
     __syncthreads();
-    int before = 0;
-    for (int i = 0; i < warp; ++i) before += sums[0][i];
+    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[0][lane] : 0);
     const int above = before + incl - c0 - c1;
     if (above < need && need <= above + c0) {
       pick[0] = top - 2 * tid;
@@ -200,14 +227,18 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     __syncthreads();
   }
   // ordered compaction: each warp a contiguous range of the CTA's positions
-  const int per = ((p1 - p0 + EV_WARPS - 1) / EV_WARPS + 31) & ~31;
+  const int per = ((p1 - p0 + EV_WARPS - 1) / EV_WARPS + 127) & ~127;
   const int t0 = min(p0 + warp * per, p1), t1 = min(t0 + per, p1);
   int above = 0, equal = 0;
-#pragma unroll 4
-  for (int t = t0 + lane; t < t1; t += 32) {
-    const uint32_t k = key_of(t);
-    above += k > prefix;
-    equal += k == prefix;
+#pragma unroll 2
+  for (int t = t0 + 4 * lane; t < t1; t += 128) {
+    const uint4 k4 = load4(t);
+    const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      above += t + i < t1 && k[i] > prefix;
+      equal += t + i < t1 && k[i] == prefix;
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -219,43 +250,66 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     sums[1][warp] = equal;
   }
   __syncthreads();
-  if (warp == 0) {
+  int at = 0, eq = 0;   // keys above, and equal, before this warp's range
+  {
     int x = sums[0][lane], y = sums[1][lane];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      x += __shfl_xor_sync(0xffffffffu, x, o);
-      y += __shfl_xor_sync(0xffffffffu, y, o);
-    }
-    if (lane == 0) {
+    const int x0 = lane < warp ? x : 0, y0 = lane < warp ? y : 0;
+    at = __reduce_add_sync(0xffffffffu, x0);
+    eq = __reduce_add_sync(0xffffffffu, y0);
+    x = __reduce_add_sync(0xffffffffu, x);
+    y = __reduce_add_sync(0xffffffffu, y);
+    if (tid == 0) {
       mine[0] = x;
       mine[1] = y;
     }
   }
   ev_cluster_sync();
-  int at = 0, eq = 0;   // keys above, and equal, before this warp's range
-  for (uint32_t r = 0; r < rank; ++r) {
-    at += ev_remote(smem_u32(&mine[0]), r);
-    eq += ev_remote(smem_u32(&mine[1]), r);
-  }
-  for (int i = 0; i < warp; ++i) {
-    at += sums[0][i];
-    eq += sums[1][i];
-  }
-  at += min(eq, need);   // kept positions before it
-  for (int tb = t0; tb < t1; tb += 32) {
-    const int t = tb + lane;
-    const uint32_t k = t < t1 ? key_of(t) : 0u;
-    const unsigned lower = (1u << lane) - 1u;
-    const unsigned me = __ballot_sync(0xffffffffu, t < t1 && k == prefix);
-    const bool keep = t < t1 && (k > prefix || (k == prefix && eq + __popc(me & lower) < need));
-    const unsigned mk = __ballot_sync(0xffffffffu, keep);
-    if (keep) {
-      const int j = at + __popc(mk & lower);
-      kept[j] = t;
-      if (wout) wout[j] = weight_of(t);
+  int cta_at = 0, cta_eq = 0;   // and before this CTA's
+#pragma unroll
+  for (uint32_t r = 0; r + 1 < EV_MAX_CLUSTER; ++r)
+    if (r < rank) {
+      const int2 v = ev_remote2(smem_u32(mine), r);
+      cta_at += v.x;
+      cta_eq += v.y;
     }
-    at += __popc(mk);
-    eq += __popc(me);
+  at += cta_at;
+  eq += cta_eq;
+  const unsigned lower = (1u << lane) - 1u;
+  for (int tb = t0; tb < t1; tb += 128) {
+    uint32_t k[4];
+    bool same = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = tb + 32 * i + lane;
+      k[i] = t < t1 ? (cached ? keys[t - p0] : make_key(t)) : 0u;
+      same |= t < t1 && k[i] == prefix;
+    }
+    // equal keys are rare, but for weights that are all alike
+    const bool any = __any_sync(0xffffffffu, same) && eq < need;
+    int j = at + min(eq, need);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = tb + 32 * i + lane;
+      bool keep = t < t1 && k[i] > prefix;
+      const unsigned mh = __ballot_sync(0xffffffffu, keep);
+      at += __popc(mh);
+      if (any) {
+        const bool e = t < t1 && k[i] == prefix;
+        const unsigned me = __ballot_sync(0xffffffffu, e);
+        keep = keep || (e && eq + __popc(me & lower) < need);
+        eq += __popc(me);
+      }
+      const unsigned mk = __ballot_sync(0xffffffffu, keep);
+      if (keep) kept[j + __popc(mk & lower)] = t;
+      j += __popc(mk);
+    }
+  }
+  if (wout) {   // the weights of what this CTA kept
+    __syncthreads();
+    const int j0 = cta_at + min(cta_eq, need);
+    const int j1 = cta_at + mine[0] + min(cta_eq + mine[1], need);
+#pragma unroll 4
+    for (int j = j0 + tid; j < j1; j += EV_THREADS) wout[j] = w[kept[j]];
   }
   ev_cluster_sync();   // no CTA leaves while another may read its counts
 }
@@ -265,24 +319,25 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
   constexpr int LPR = D / 16;              // lanes per row, 16 codes each
   constexpr int RPP = 256 / LPR;           // rows per pass
   constexpr int NP = KV8_BLOCK / RPP;
-  __shared__ float warp_max[8];
+  __shared__ float warp_max[2][8];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int h = blockIdx.y % a.Hkv, kind = blockIdx.y / a.Hkv, b = blockIdx.z;
+  const int h = blockIdx.y, b = blockIdx.z;
   const int m = min(ev_ctx(a, b), a.budget);
   const int j0 = blockIdx.x * KV8_BLOCK;
   if (j0 >= m) return;
   const int li = threadIdx.x % LPR, rr = threadIdx.x / LPR;
   const int32_t* const kept = a.kept + ((int64_t)b * a.Hkv + h) * a.budget;
-  uint4 x[NP];
-  int e_old[NP];
-  float amax = 0.f;
+  const int pd = j0 >> a.log2P, slot0 = j0 & (a.P - 1);
+  const int32_t dst = pd < a.dst_stride ? a.dst_table[(int64_t)b * a.dst_stride + pd] : -1;
+  uint4 x[NP][2];
+  float s_old[NP][2];
 #pragma unroll
   for (int p = 0; p < NP; ++p) {
     const int j = j0 + p * RPP + rr;
-    x[p] = make_uint4(0u, 0u, 0u, 0u);
-    e_old[p] = KV8_EMIN;
+    x[p][0] = x[p][1] = make_uint4(0u, 0u, 0u, 0u);
+    s_old[p][0] = s_old[p][1] = 0.f;
     if (j < m) {
       const int t = kept[j];
       const int32_t page = a.page_table[(int64_t)b * a.pt_stride + (t >> a.log2P)];
@@ -291,60 +346,75 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
       } else {
         const int slot = t & (a.P - 1);
         const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-        x[p] = *reinterpret_cast<const uint4*>(rec + kind * a.codes_region +
-                                               (int64_t)(h * a.P + slot) * D + li * 16);
-        e_old[p] = exp8_of_scale(
-            *(reinterpret_cast<const float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
-              h * (a.P / KV8_BLOCK) + slot / KV8_BLOCK));
+        const uint8_t* const code = rec + (int64_t)(h * a.P + slot) * D + li * 16;
+        const uint8_t* const scale =
+            rec + 2 * a.codes_region + (h * (a.P / KV8_BLOCK) + slot / KV8_BLOCK) * 4;
+#pragma unroll
+        for (int kind = 0; kind < 2; ++kind) {
+          x[p][kind] = *reinterpret_cast<const uint4*>(code + kind * a.codes_region);
+          s_old[p][kind] = *reinterpret_cast<const float*>(scale + kind * a.sb_region);
+        }
       }
     }
-    const uint32_t w[4] = {x[p].x, x[p].y, x[p].z, x[p].w};
-    // largest finite magnitude code (the codes' order is that of the values)
-    uint32_t m4 = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t c = w[i] & 0x7F7F7F7Fu;
-      c &= ~__vcmpeq4(c, 0x7F7F7F7Fu);
-      m4 = __vmaxu2(m4, c & 0x00FF00FFu);
-      m4 = __vmaxu2(m4, (c >> 8) & 0x00FF00FFu);
-    }
-    const uint32_t top = max(m4 & 0xFFFFu, m4 >> 16);
-    uint32_t lo, hi;
-    f16x4_of_e4m3(top, lo, hi);
-    amax = fmaxf(amax, f32x2_of_f16x2(lo).x * two8(e_old[p]));
   }
+  float amax[2] = {0.f, 0.f};
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-  if (lane == 0) warp_max[warp] = amax;
+  for (int kind = 0; kind < 2; ++kind) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      // largest finite magnitude code (the codes' order is that of the values)
+      const uint32_t w[4] = {x[p][kind].x, x[p][kind].y, x[p][kind].z, x[p][kind].w};
+      uint32_t m4 = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t c = w[i] & 0x7F7F7F7Fu;
+        // 0x7F, NaN, is the only magnitude whose increment reaches bit 7
+        const uint32_t nan = ((c + 0x01010101u) & 0x80808080u) >> 7;
+        if (nan) c &= ~(nan * 0x7Fu);
+        m4 = __vmaxu2(m4, c & 0x00FF00FFu);
+        m4 = __vmaxu2(m4, (c >> 8) & 0x00FF00FFu);
+      }
+      uint32_t lo, hi;
+      f16x4_of_e4m3(max(m4 & 0xFFFFu, m4 >> 16), lo, hi);
+      amax[kind] = fmaxf(amax[kind], f32x2_of_f16x2(lo).x * two8(exp8_of_scale(s_old[p][kind])));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+      amax[kind] = fmaxf(amax[kind], __shfl_xor_sync(0xffffffffu, amax[kind], o));
+    if (lane == 0) warp_max[kind][warp] = amax[kind];
+  }
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) amax = fmaxf(amax, warp_max[i]);
-  const int e = exp8_of(amax);
-  const int pd = j0 >> a.log2P, slot0 = j0 & (a.P - 1);
-  const int32_t page = pd < a.dst_stride ? a.dst_table[(int64_t)b * a.dst_stride + pd] : -1;
-  if (page < 0 || page >= a.num_pages) {
+  if (dst < 0 || dst >= a.num_pages) {
     if (threadIdx.x == 0)
       flag_error(a.err, pd < a.dst_stride ? JF_DEV_ERR_PAGE_ID : JF_DEV_ERR_POSITION);
     return;
   }
-  uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  uint8_t* const codes = rec + kind * a.codes_region + (int64_t)(h * a.P + slot0) * D;
-  if (threadIdx.x == 0)
-    *(reinterpret_cast<float*>(rec + 2 * a.codes_region + kind * a.sb_region) +
-      h * (a.P / KV8_BLOCK) + slot0 / KV8_BLOCK) = two8(e);
+  uint8_t* const rec = a.pool + (int64_t)dst * a.page_bytes;
 #pragma unroll
-  for (int p = 0; p < NP; ++p) {
-    const int row = p * RPP + rr;
-    if (j0 + row < m) {
-      uint4 c = x[p];
-      if (e_old[p] != e) {
-        const float s = two8(e_old[p] - e);
-        c.x = rescale_e4m3x4(c.x, s);
-        c.y = rescale_e4m3x4(c.y, s);
-        c.z = rescale_e4m3x4(c.z, s);
-        c.w = rescale_e4m3x4(c.w, s);
+  for (int kind = 0; kind < 2; ++kind) {
+    float top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, warp_max[kind][i]);
+    const int e = exp8_of(top);
+    if (threadIdx.x == 0)
+      *reinterpret_cast<float*>(rec + 2 * a.codes_region + kind * a.sb_region +
+                                (h * (a.P / KV8_BLOCK) + slot0 / KV8_BLOCK) * 4) = two8(e);
+    uint8_t* const codes =
+        rec + kind * a.codes_region + (int64_t)(h * a.P + slot0) * D + li * 16;
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int row = p * RPP + rr;
+      if (j0 + row < m) {
+        uint4 c = x[p][kind];
+        const int s = exp8_of_scale(s_old[p][kind]) - e;
+        if (s != 0) {
+          c.x = rescale_e4m3x4(c.x, s);
+          c.y = rescale_e4m3x4(c.y, s);
+          c.z = rescale_e4m3x4(c.z, s);
+          c.w = rescale_e4m3x4(c.w, s);
+        }
+        *reinterpret_cast<uint4*>(codes + row * D) = c;
       }
-      *reinterpret_cast<uint4*>(codes + row * D + li * 16) = c;
     }
   }
 }
@@ -383,11 +453,10 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   // CTAs per row: one for each EV_SLICE keys of the longest row there may be, in
-  // powers of two (262,144 keys of 4 rows: one CTA a row took 430 us of four
-  // byte-wise passes over memory)
+  // powers of two
   int cl = 1;
   while (cl < EV_MAX_CLUSTER && wstride > (int64_t)cl * EV_SLICE) cl *= 2;
-  const int64_t cap = (wstride + 32 * cl - 1) / (32 * cl) * 32;
+  const int64_t cap = (wstride + 128 * cl - 1) / (128 * cl) * 128;
   a.key_cap = (int32_t)(cap <= EV_MAX_KEYS ? cap : 0);
   if (smem_optin((const void*)kv8_select_kernel, EV_MAX_KEYS * 4) != JF_OK) return JF_ERR_CUDA;
   cudaLaunchAttribute attrs[2];
@@ -406,7 +475,7 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   cfg.dynamicSmemBytes = 0;
-  cfg.gridDim = dim3((unsigned)((budget + KV8_BLOCK - 1) / KV8_BLOCK), (unsigned)(2 * g.Hkv),
+  cfg.gridDim = dim3((unsigned)((budget + KV8_BLOCK - 1) / KV8_BLOCK), (unsigned)g.Hkv,
                      (unsigned)batch);
   cfg.blockDim = dim3(256);
   const cudaError_t e = g.D == 256 ? cudaLaunchKernelEx(&cfg, kv8_compact_kernel<256>, a)
