@@ -158,64 +158,75 @@ __global__ void __launch_bounds__(256) kv8_append_kernel(const Kv8Args a) {
   }
 }
 
-// Read back: a group of D/16 lanes takes the K and V vectors of one row and
-// KV head, 16 codes of each a lane.
+// Read back: a group of D/8 lanes takes the K and V vectors of KV8_RR rows and a
+// KV head, 8 codes of each a lane, all rows' loads before their use.
+constexpr int KV8_RR = 2;
+
 template <int D>
 __global__ void __launch_bounds__(256) kv8_read_kernel(const Kv8Args a) {
-  constexpr int LPR = D / 16;
+  constexpr int LPR = D / 8;
+  constexpr int RPP = 256 / LPR;   // rows side by side
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int row = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int li = threadIdx.x % LPR;
   const int head = blockIdx.y;
-  if (row >= a.n_rows) return;
-  // the request of this row: the last b with row_offsets[b] <= row
-  int lo = 0, hi = a.num_requests - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (a.row_offsets[mid] <= row) lo = mid; else hi = mid - 1;
-  }
-  int r0, r1, pos0;
-  const bool ok = kv8_run(a, lo, r0, r1, pos0);
-  if (!ok || row < r0 || row >= r1) {
-    if (!ok && li == 0) flag_error(a.err, JF_DEV_ERR_POSITION);
-    return;   // a row of no request is left as it is
-  }
-  const int pos = pos0 + (row - r0);
-  const int32_t page = a.page_table[(int64_t)lo * a.pt_stride + (pos >> a.log2P)];
-  if (page < 0 || page >= a.num_pages) {
-    if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
-    return;
-  }
-  const int slot = pos & (a.P - 1);
-  const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
-  const uint8_t* const code = rec + (int64_t)(head * a.P + slot) * D + li * 16;
-  const uint8_t* const scale =
-      rec + 2 * a.codes_region + (head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK) * 4;
-  uint4 c[2];
-  float s[2];
+  const int row0 = blockIdx.x * (RPP * KV8_RR) + threadIdx.x / LPR;
+  uint2 c[KV8_RR][2];
+  float s[KV8_RR][2];
+  bool live[KV8_RR];
 #pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    c[kind] = *reinterpret_cast<const uint4*>(code + kind * a.codes_region);
-    s[kind] = *reinterpret_cast<const float*>(scale + kind * a.sb_region);
-  }
-#pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    const float two = two8(exp8_of_scale(s[kind]));
-    const uint32_t w[4] = {c[kind].x, c[kind].y, c[kind].z, c[kind].w};
-    uint32_t o[8];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t h0, h1;
-      f16x4_of_e4m3(w[i], h0, h1);
-      const float2 f0 = f32x2_of_f16x2(h0), f1 = f32x2_of_f16x2(h1);
-      o[2 * i] = pack_bf16x2_rn(f0.x * two, f0.y * two);
-      o[2 * i + 1] = pack_bf16x2_rn(f1.x * two, f1.y * two);
+  for (int u = 0; u < KV8_RR; ++u) {
+    const int row = row0 + u * RPP;
+    live[u] = false;
+    if (row >= a.n_rows) continue;
+    // the request of this row: the last b with row_offsets[b] <= row
+    int lo = 0, hi = a.num_requests - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (a.row_offsets[mid] <= row) lo = mid; else hi = mid - 1;
     }
-    uint4* const dst = reinterpret_cast<uint4*>(
-        (kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) + head * D + li * 16);
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    int r0, r1, pos0;
+    const bool ok = kv8_run(a, lo, r0, r1, pos0);
+    if (!ok || row < r0 || row >= r1) {
+      if (!ok && li == 0) flag_error(a.err, JF_DEV_ERR_POSITION);
+      continue;   // a row of no request is left as it is
+    }
+    const int pos = pos0 + (row - r0);
+    const int32_t page = a.page_table[(int64_t)lo * a.pt_stride + (pos >> a.log2P)];
+    if (page < 0 || page >= a.num_pages) {
+      if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);
+      continue;
+    }
+    live[u] = true;
+    const int slot = pos & (a.P - 1);
+    const uint8_t* const rec = a.pool + (int64_t)page * a.page_bytes;
+    const uint8_t* const code = rec + (int64_t)(head * a.P + slot) * D + li * 8;
+    const uint8_t* const scale =
+        rec + 2 * a.codes_region + (head * (a.P / KV8_BLOCK) + slot / KV8_BLOCK) * 4;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      c[u][kind] = *reinterpret_cast<const uint2*>(code + kind * a.codes_region);
+      s[u][kind] = *reinterpret_cast<const float*>(scale + kind * a.sb_region);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < KV8_RR; ++u) {
+    if (!live[u]) continue;
+    const int64_t row = row0 + u * RPP;
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      const float two = two8(exp8_of_scale(s[u][kind]));
+      uint32_t h[4], o[4];
+      f16x4_of_e4m3(c[u][kind].x, h[0], h[1]);
+      f16x4_of_e4m3(c[u][kind].y, h[2], h[3]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 f = f32x2_of_f16x2(h[i]);
+        o[i] = pack_bf16x2_rn(f.x * two, f.y * two);
+      }
+      *reinterpret_cast<uint4*>((kind ? a.v : a.k) + row * (kind ? a.v_stride : a.k_stride) +
+                                head * D + li * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
   }
 }
 
@@ -245,9 +256,10 @@ int launch_kv8_rows(const Geom& g, const jf_kv_pool& pool, const int32_t* page_t
   a.n_rows = n_rows;
   a.err = err;
   // append: a request's r >= 1 rows touch at most (r - 1) / 32 + 2 blocks and
-  // at most r; read: one group of D / 16 lanes per row
+  // at most r; read: groups of D / 8 lanes, KV8_RR rows each
   const int64_t by_block = (int64_t)n_rows / KV8_BLOCK + 2 * (int64_t)num_requests;
-  const int64_t blocks = read ? ((int64_t)n_rows * (g.D / 16) + 255) / 256
+  const int64_t per = KV8_RR * 256 / (g.D / 8);
+  const int64_t blocks = read ? (n_rows + per - 1) / per
                               : (by_block < n_rows ? by_block : n_rows);
   if (blocks > 0x7FFFFFFF) return JF_ERR_UNSUPPORTED;
   cudaLaunchAttribute pdl[1];

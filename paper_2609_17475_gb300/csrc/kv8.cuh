@@ -55,10 +55,10 @@ __device__ __forceinline__ uint32_t pack_bf16x2_rn(float lo, float hi) {
   return r;
 }
 
-// The four codes of a word rounded again for a scale 2^-s times as large
-// (value = code * 2^s under the new scale, at most 448).  In fp16: products of
-// at least 2^-10, half the smallest code, are exact, and smaller ones become
-// zero either way; s < -24 leaves only those.
+// Codes rounded again for a scale 2^-s times as large (value = code * 2^s under
+// the new scale, at most 448).  In fp16: products of at least 2^-10, half the
+// smallest code, are exact, and smaller ones become zero either way; s < -24
+// leaves only those.
 __device__ __forceinline__ uint32_t f16x2_two(int s) {
   const __half2 h = __float2half2_rn(s < -24 ? 0.f : two8(s));
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -75,17 +75,28 @@ __device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, int s) {
-  uint32_t lo, hi;
-  f16x4_of_e4m3(w, lo, hi);
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void rescale_f16(uint32_t (&v)[N], int s) {
   if (s > 15) {   // past fp16's powers of two: only subnormal codes get here
     const uint32_t p = f16x2_two(15);
-    lo = mul_f16x2(lo, p);
-    hi = mul_f16x2(hi, p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = mul_f16x2(v[i], p);
     s -= 15;
   }
   const uint32_t p = f16x2_two(s);
-  return e4m3x4_of_f16x2(mul_f16x2(lo, p), mul_f16x2(hi, p));
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = mul_f16x2(v[i], p);
+}
+__device__ __forceinline__ uint32_t rescale_e4m3x4(uint32_t w, int s) {
+  uint32_t v[2];
+  f16x4_of_e4m3(w, v[0], v[1]);
+  rescale_f16(v, s);
+  return e4m3x4_of_f16x2(v[0], v[1]);
 }
 
 }  // namespace jfkv

@@ -357,31 +357,28 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
       }
     }
   }
-  float amax[2] = {0.f, 0.f};
+  // the rows' values under their own scales as fp16 (exact), and the block's
+  // largest finite magnitude (the maximum passes over NaN)
+  uint32_t f[NP][2][8];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
+    float amax = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      // largest finite magnitude code (the codes' order is that of the values)
-      const uint32_t w[4] = {x[p][kind].x, x[p][kind].y, x[p][kind].z, x[p][kind].w};
-      uint32_t m4 = 0;
+      uint32_t* const v = f[p][kind];
+      f16x4_of_e4m3(x[p][kind].x, v[0], v[1]);
+      f16x4_of_e4m3(x[p][kind].y, v[2], v[3]);
+      f16x4_of_e4m3(x[p][kind].z, v[4], v[5]);
+      f16x4_of_e4m3(x[p][kind].w, v[6], v[7]);
+      uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t c = w[i] & 0x7F7F7F7Fu;
-        // 0x7F, NaN, is the only magnitude whose increment reaches bit 7
-        const uint32_t nan = ((c + 0x01010101u) & 0x80808080u) >> 7;
-        if (nan) c &= ~(nan * 0x7Fu);
-        m4 = __vmaxu2(m4, c & 0x00FF00FFu);
-        m4 = __vmaxu2(m4, (c >> 8) & 0x00FF00FFu);
-      }
-      uint32_t lo, hi;
-      f16x4_of_e4m3(max(m4 & 0xFFFFu, m4 >> 16), lo, hi);
-      amax[kind] = fmaxf(amax[kind], f32x2_of_f16x2(lo).x * two8(exp8_of_scale(s_old[p][kind])));
+      for (int i = 0; i < 8; ++i) top = max_f16x2(top, v[i] & 0x7FFF7FFFu);
+      const float2 t2 = f32x2_of_f16x2(top);
+      amax = fmaxf(amax, fmaxf(t2.x, t2.y) * two8(exp8_of_scale(s_old[p][kind])));
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-      amax[kind] = fmaxf(amax[kind], __shfl_xor_sync(0xffffffffu, amax[kind], o));
-    if (lane == 0) warp_max[kind][warp] = amax[kind];
+    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+    if (lane == 0) warp_max[kind][warp] = amax;
   }
   __syncthreads();
   if (dst < 0 || dst >= a.num_pages) {
@@ -405,15 +402,11 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
     for (int p = 0; p < NP; ++p) {
       const int row = p * RPP + rr;
       if (j0 + row < m) {
-        uint4 c = x[p][kind];
-        const int s = exp8_of_scale(s_old[p][kind]) - e;
-        if (s != 0) {
-          c.x = rescale_e4m3x4(c.x, s);
-          c.y = rescale_e4m3x4(c.y, s);
-          c.z = rescale_e4m3x4(c.z, s);
-          c.w = rescale_e4m3x4(c.w, s);
-        }
-        *reinterpret_cast<uint4*>(codes + row * D) = c;
+        uint32_t (&v)[8] = f[p][kind];
+        rescale_f16(v, exp8_of_scale(s_old[p][kind]) - e);
+        *reinterpret_cast<uint4*>(codes + row * D) =
+            make_uint4(e4m3x4_of_f16x2(v[0], v[1]), e4m3x4_of_f16x2(v[2], v[3]),
+                       e4m3x4_of_f16x2(v[4], v[5]), e4m3x4_of_f16x2(v[6], v[7]));
       }
     }
   }
