@@ -173,25 +173,30 @@ def _check(fn: str, status: int) -> None:
 
 
 def _ptr(t: Optional[torch.Tensor]):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 # The current stream's handle without building a torch.cuda.Stream (3 us a call on a Grace core, a fifth
-# of a small call's host time; this takes 0.3 us)
+# of a small call's host time; this takes 0.2 us)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream) -> ctypes.c_void_p:
+def _stream(stream) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
+            return _raw_stream(_get_device())
         stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> None:
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise TypeError(f"{name} must be a contiguous CUDA tensor of dtype {dtype}")
+    try:
+        if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+            return
+    except AttributeError:   # not a tensor
+        pass
+    raise TypeError(f"{name} must be a contiguous CUDA tensor of dtype {dtype}")
 
 
 def jf_tq4_codebook(head_dim: int):
@@ -269,15 +274,16 @@ class KVPool:
     def page_bytes(self) -> int:
         return self.data.shape[1]
 
+    def __setattr__(self, name, value):
+        # the struct below is built again once a field has changed
+        self.__dict__.pop("_c", None)
+        self.__dict__[name] = value
+
     def c_struct(self) -> _Pool:
-        # built again whenever a field that it holds has changed
-        key = (self.data.data_ptr(), self.data.shape, self.page_size, self.num_kv_heads,
-               self.head_dim, self.group_size, self.format, self.codec)
-        if getattr(self, "_key", None) == key:
-            return self._c
-        self._c = self._struct()
-        self._key = key
-        return self._c
+        c = self.__dict__.get("_c")
+        if c is None or c.base != self.data.data_ptr() or c.num_pages != self.data.shape[0]:
+            c = self.__dict__["_c"] = self._struct()
+        return c
 
     def _struct(self) -> _Pool:
         p = _Pool(self.data.data_ptr(), self.num_pages, self.page_size, self.num_kv_heads,
@@ -732,53 +738,64 @@ def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
     """Turn query and key rows [tokens, heads, head_dim] (either may be None) by
     their positions, int32 [axes, tokens]; outputs default to in place.  With
     ``inverse`` the gradient of that: q, k are then the outputs' gradients."""
-    if not isinstance(positions, torch.Tensor) or positions.dtype != torch.int32 or not positions.is_cuda:
+    if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or not positions.is_cuda:
         raise TypeError("positions must be a CUDA tensor of dtype torch.int32")
-    if positions.dim() != 2 or positions.shape[0] != rope.num_axes or (
-            positions.shape[1] > 1 and positions.stride(1) != 1):
+    shape, strides = positions.shape, positions.stride()
+    if len(shape) != 2 or shape[0] != rope.num_axes or (shape[1] > 1 and strides[1] != 1):
         raise ValueError("positions must be [axes, tokens], the tokens of an axis adjoining")
-    n = positions.shape[1]
+    n = shape[1]
     qr, qt, qd = _rope_rows(q, q_out, n, "q")
     kr, kt, kd = _rope_rows(k, k_out, n, "k")
     if qt is None and kt is None:
         raise ValueError("q or k is needed")
     if qt is not None and kt is not None and (qt != kt or qd != kd):
         raise ValueError("q and k must have one dtype and head_dim")
-    _check("jf_rope_axes",
-           lib().jf_rope_axes(rope._ref, positions.data_ptr(), positions.stride(0), n, qd or kd,
-                              ctypes.byref(qr), ctypes.byref(kr), _ROPE_DTYPES[qt or kt],
-                              int(bool(inverse)), _stream(stream)))
+    st = lib().jf_rope_axes(rope._ref, positions.data_ptr(), strides[0], n, qd or kd,
+                            ctypes.byref(qr), ctypes.byref(kr), _ROPE_DTYPES[qt or kt],
+                            1 if inverse else 0, _stream(stream))
+    if st:
+        raise JfError("jf_rope_axes", st)
 
 
 # ---------------------------------------------------------------------------
 # the 8-bit block-scaled cache
 # ---------------------------------------------------------------------------
-def _kv8_rows(fn: str, pool: KVPool, page_table, start_pos, row_offsets, k, v, err_flag, stream):
+def _kv_rows_arg(x: torch.Tensor, name: str, hkv: int, d: int):
+    """(rows, elements between rows) of a [rows, Hkv, D] tensor whose rows may lie apart."""
+    try:
+        if x.dtype is not torch.bfloat16 or not x.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
+        shape, stride = x.shape, x.stride()
+    except AttributeError:
+        raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16") from None
+    if len(shape) != 3 or shape[1] != hkv or shape[2] != d:
+        raise ValueError(f"{name} must be [rows, Hkv, D]")
+    n = shape[0]
+    if n and (stride[2] != 1 or (hkv > 1 and stride[1] != d)):
+        raise ValueError(f"{name}: the elements of a row must adjoin")
+    # the row stride of a single row is whatever a slicing left: it is not used
+    return n, stride[0] if n > 1 else hkv * d
+
+
+def _kv8_rows(name: str, fn, pool: KVPool, page_table, start_pos, row_offsets, k, v, err_flag, stream):
     _need(page_table, torch.int32, "page_table")
     _need(start_pos, torch.int32, "start_pos")
     _need(row_offsets, torch.int32, "row_offsets")
-    n = k.shape[0]
-    for name, x in (("k", k), ("v", v)):
-        if not isinstance(x, torch.Tensor) or x.dtype != torch.bfloat16 or not x.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
-        if tuple(x.shape) != (n, pool.num_kv_heads, pool.head_dim):
-            raise ValueError(f"{name} must be [rows, Hkv, D]")
-        if n and (x.stride(2) != 1 or (pool.num_kv_heads > 1 and x.stride(1) != pool.head_dim)):
-            raise ValueError(f"{name}: the elements of a row must adjoin")
-    pt = page_table if page_table.dim() == 2 else page_table.view(1, -1)
-    B = pt.shape[0]
+    n, ks = _kv_rows_arg(k, "k", pool.num_kv_heads, pool.head_dim)
+    nv, vs = _kv_rows_arg(v, "v", pool.num_kv_heads, pool.head_dim)
+    shape = page_table.shape
+    B, stride = shape if len(shape) == 2 else (1, page_table.numel())
+    if n != nv:
+        raise ValueError("k and v must have the same rows")
     if start_pos.numel() != B or row_offsets.numel() != B + 1:
         raise ValueError("one start_pos per page-table row, and one row offset more")
     if err_flag is not None:
         _need(err_flag, torch.int32, "err_flag")
-    row = pool.num_kv_heads * pool.head_dim
-    # the row stride of a single row is whatever a slicing left: it is not used
-    ks, vs = (k.stride(0), v.stride(0)) if n > 1 else (row, row)
-    st = getattr(lib(), fn)(ctypes.byref(pool.c_struct()), pt.data_ptr(), pt.shape[1], B,
-                            start_pos.data_ptr(), row_offsets.data_ptr(), k.data_ptr(), ks,
-                            v.data_ptr(), vs, n, None if err_flag is None else err_flag.data_ptr(),
-                            _stream(stream))
-    _check(fn, st)
+        err_flag = err_flag.data_ptr()
+    st = fn(ctypes.byref(pool.c_struct()), page_table.data_ptr(), stride, B, start_pos.data_ptr(),
+            row_offsets.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, n, err_flag, _stream(stream))
+    if st:
+        raise JfError(name, st)
 
 
 @_traced
@@ -787,7 +804,7 @@ def jf_kv8_append(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tenso
                   err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Append rows row_offsets[b] .. row_offsets[b + 1] - 1 of k and v (bf16 [rows,
     Hkv, D], rows any stride apart) at positions start_pos[b] .. of request b."""
-    _kv8_rows("jf_kv8_append", pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    _kv8_rows("jf_kv8_append", lib().jf_kv8_append, pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
 
 
 @_traced
@@ -795,7 +812,7 @@ def jf_kv8_read(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
                 row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                 err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Read runs of positions back into k and v as bf16 values (exact)."""
-    _kv8_rows("jf_kv8_read", pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    _kv8_rows("jf_kv8_read", lib().jf_kv8_read, pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
 
 
 def decode_weights_workspace(batch, num_q_heads, num_kv_heads, head_dim, num_splits,

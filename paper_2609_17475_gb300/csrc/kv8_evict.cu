@@ -4,10 +4,10 @@
 // `sinks` and the last `recent` positions always do; of the others those with
 // the largest weights, equal weights in order of position.  Weights map to
 // 32-bit keys whose unsigned order is theirs (a protected position takes the
-// largest key, NaN the smallest).  A cluster of CTAs shares a row: each keeps
-// the keys of its range of positions in shared memory, read from memory once,
-// and a radix select over the cluster's histograms (11, 11 and 10 bits,
-// combined through distributed shared memory) finds the budget-th largest
+// largest key, NaN the smallest).  A cluster of up to 16 CTAs shares a row: each
+// keeps the keys of its range of positions in shared memory, read from memory
+// once, and a radix select over the cluster's histograms (11, 11 and 10 bits,
+// added up through distributed shared memory) finds the budget-th largest
 // key.  The kept positions are then written in rising order: all above that
 // key, and the first of those that equal it.
 //
@@ -22,8 +22,8 @@ namespace jfkv {
 constexpr int EV_THREADS = 1024;
 constexpr int EV_WARPS = EV_THREADS / 32;
 constexpr int EV_BINS = 2048;
-constexpr int EV_SLICE = 8192;              // keys a CTA should have before a row takes more CTAs
-constexpr int EV_MAX_CLUSTER = 8;
+constexpr int EV_SLICE = 4096;              // keys a CTA should have before a row takes more CTAs
+constexpr int EV_MAX_CLUSTER = 16;
 constexpr int EV_MAX_KEYS = 48 * 1024;      // keys that fit a CTA's shared memory
 
 struct EvictArgs {
@@ -45,7 +45,6 @@ struct EvictArgs {
   float* dst_weights;          // [B, Hkv, budget] or null
   int32_t* kept;               // [B, Hkv, budget]
   int32_t* err;
-  int32_t key_cap;             // keys that the select kernel's shared memory holds
 };
 
 // Context of request b; 0 (and flagged by the select kernel) where it does not
@@ -55,10 +54,11 @@ __device__ __forceinline__ int ev_ctx(const EvictArgs& a, int b) {
   return c < 0 || c > (int64_t)a.pt_stride * a.P || c > a.wstride ? 0 : (int)c;
 }
 
-// unsigned order = order of the weights; NaN below all, -0 as +0
+// unsigned order = order of the weights; NaN, 1, below all of them, -0 as +0.
+// 0 stands for no position: it is never kept.
 __device__ __forceinline__ uint32_t ev_key(float w) {
   const uint32_t b = __float_as_uint(w + 0.f);
-  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return 0u;
+  if ((b & 0x7FFFFFFFu) > 0x7F800000u) return 1u;
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 
@@ -76,34 +76,40 @@ __device__ __forceinline__ void ev_cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n"
                "barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
-// the ints at this CTA's shared address `addr` (8-byte aligned), in CTA `rank`
-// of the cluster
-__device__ __forceinline__ int2 ev_remote2(uint32_t addr, uint32_t rank) {
+// this CTA's shared address `addr` in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t ev_map(uint32_t addr, uint32_t rank) {
   uint32_t a;
-  int2 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ int2 ev_remote2(uint32_t addr, uint32_t rank) {
+  int2 v;
   asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];\n"
-               : "=r"(v.x), "=r"(v.y) : "r"(a) : "memory");
+               : "=r"(v.x), "=r"(v.y) : "r"(ev_map(addr, rank)) : "memory");
   return v;
 }
-
-// One count per key with `in` set: the lanes that share the first such lane's
-// bin add once (weights crowd into few bins: exact zeros, one exponent), the
-// others each.  Whole warps.
-__device__ __forceinline__ void ev_count(int* hist, uint32_t bin, bool in, int lane) {
-  const unsigned all = __ballot_sync(0xffffffffu, in);
-  if (!all) return;
-  const int lead = __ffs(all) - 1;
-  const uint32_t top = __shfl_sync(0xffffffffu, bin, lead);
-  const unsigned same = __ballot_sync(0xffffffffu, in && bin == top);
-  if (lane == lead) atomicAdd(&hist[bin], __popc(same));
-  if (in && bin != top) atomicAdd(&hist[bin], 1);
+__device__ __forceinline__ void ev_remote_add(uint32_t addr, uint32_t rank, int v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;\n"
+               ::"r"(ev_map(addr, rank)), "r"(v) : "memory");
 }
 
+// One count per key with `in` set, at once for a warp whose keys share a bin
+// (weights that are all alike).  Whole warps.
+__device__ __forceinline__ void ev_count(int* hist, uint32_t bin, bool in, int lane) {
+  const uint32_t lead = __shfl_sync(0xffffffffu, bin, 0);
+  if (__all_sync(0xffffffffu, in && bin == lead)) {
+    if (lane == 0) atomicAdd(&hist[bin], 32);
+  } else if (in) {
+    atomicAdd(&hist[bin], 1);
+  }
+}
+
+// CACHED: a CTA's keys fit its shared memory (rows up to 16 x 48 Ki positions);
+// otherwise they are made again from the weights wherever they are needed.
+template <bool CACHED>
 __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictArgs a) {
-  extern __shared__ __align__(16) uint32_t keys[];   // this CTA's slice, or unused where it
-                                                     // does not fit
-  __shared__ __align__(8) int hist[3][EV_BINS];      // one a pass: the cluster may still read the last one
+  extern __shared__ __align__(16) uint32_t keys[];   // this CTA's slice
+  __shared__ __align__(8) int hist[3][EV_BINS];      // one a digit
   __shared__ int sums[2][EV_WARPS];
   __shared__ int pick[2];
   __shared__ __align__(8) int mine[2];      // keys above, and equal to, the last one kept
@@ -128,37 +134,39 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     }
     return;
   }
-  // this CTA's positions [p0, p1), a multiple of 128 but for the row's end
+  // this CTA's positions [p0, p0 + len), len a multiple of 128; those at or past
+  // n are none
   const int slice = (int)(((int64_t)n + 128 * (int64_t)ranks - 1) / (128 * (int64_t)ranks)) * 128;
-  const int p0 = (int)min((int64_t)rank * slice, (int64_t)n);
-  const int p1 = (int)min((int64_t)p0 + slice, (int64_t)n);
-  const bool cached = slice <= a.key_cap;
-  auto make_key = [&](int t) -> uint32_t {
-    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(w[t]);
+  const int64_t first = (int64_t)rank * slice;
+  const int p0 = (int)min(first, (int64_t)n);
+  const int len = (int)min((int64_t)slice, ((int64_t)n - p0 + 127) / 128 * 128);
+  auto key_at = [&](int i, float x) -> uint32_t {   // of position p0 + i with weight x
+    const int t = p0 + i;
+    return t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(x);
   };
-  // the keys of positions t .. t + 3 (t - p0 a multiple of 4); those at or past
-  // p1 are not keys
-  auto load4 = [&](int t) -> uint4 {
-    if (cached) return *reinterpret_cast<const uint4*>(keys + (t - p0));
-    uint4 k;
-    k.x = make_key(t);
-    k.y = t + 1 < p1 ? make_key(t + 1) : 0u;
-    k.z = t + 2 < p1 ? make_key(t + 2) : 0u;
-    k.w = t + 3 < p1 ? make_key(t + 3) : 0u;
-    return k;
+  auto key1 = [&](int i) -> uint32_t {
+    if (CACHED) return keys[i];
+    return p0 + i < n ? key_at(i, w[p0 + i]) : 0u;
+  };
+  auto key4 = [&](int i) -> uint4 {
+    if (CACHED) return *reinterpret_cast<const uint4*>(keys + i);
+    return make_uint4(key1(i), key1(i + 1), key1(i + 2), key1(i + 3));
   };
   for (int i = tid; i < 3 * EV_BINS; i += EV_THREADS) hist[0][i] = 0;
-  if (cached) {   // 16 loads in flight a thread
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // zeroed
+  if (CACHED) {   // 16 loads in flight a thread
     constexpr int U = 16;
-    for (int tb = p0 + tid; tb < p1; tb += U * EV_THREADS) {
+    for (int ib = tid; ib < len; ib += U * EV_THREADS) {
       float x[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (tb + u * EV_THREADS < p1) x[u] = w[tb + u * EV_THREADS];
+      for (int u = 0; u < U; ++u) {
+        const int i = ib + u * EV_THREADS;
+        x[u] = i < len && p0 + i < n ? w[p0 + i] : 0.f;
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int t = tb + u * EV_THREADS;
-        if (t < p1) keys[t - p0] = t < a.sinks || t >= n - a.recent ? 0xFFFFFFFFu : ev_key(x[u]);
+        const int i = ib + u * EV_THREADS;
+        if (i < len) keys[i] = p0 + i < n ? key_at(i, x[u]) : 0u;
       }
     }
   }
@@ -170,39 +178,47 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
   for (int pass = 0; pass < 3; ++pass) {
     const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
     const int bits = pass == 2 ? 10 : 11;
-    int* const hs = hist[pass];
     const uint32_t mask = (1u << bits) - 1u;
+    int* const hs = hist[pass];
 #pragma unroll 2
-    for (int tb = p0 + 128 * warp; tb < p1; tb += 128 * EV_WARPS) {   // whole warps take part
-      const int t = tb + 4 * lane;
-      const uint4 k4 = t < p1 ? load4(t) : make_uint4(0u, 0u, 0u, 0u);
+    for (int ib = 128 * warp; ib < len; ib += 128 * EV_WARPS) {   // whole warps take part
+      const uint4 k4 = key4(ib + 4 * lane);
       const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
       bool in[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        in[i] = t + i < p1 && (pass == 0 || (k[i] >> (shift + bits)) == prefix);
+      for (int i = 0; i < 4; ++i) in[i] = pass == 0 || (k[i] >> (shift + bits)) == prefix;
       // after the first digit few keys are left
       if (pass > 0 && !__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i) ev_count(hs, (k[i] >> shift) & mask, in[i], lane);
     }
-    ev_cluster_sync();
-    // thread i sums bins top - 2i and top - 2i - 1 over the cluster; the
-    // largest digit with at least `need` keys at or above it is picked
-    const int top = (1 << bits) - 1;
+    __syncthreads();
+    if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+    // Each CTA gathers the cluster's counts of its share of the bins: the others
+    // add theirs to it, most bins being empty (reading all of every CTA's
+    // histogram took 12,000 cycles of a 16-CTA cluster, this takes 3,000).
+    const int share = (1 << bits) / (int)ranks;   // bins per CTA, even
+    if (ranks > 1) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int bin = tid + u * EV_THREADS;
+        if (bin <= (int)mask && bin / share != (int)rank) {
+          const int c = hs[bin];
+          if (c) ev_remote_add(smem_u32(hs + bin), bin / share, c);
+        }
+      }
+      ev_cluster_sync();
+    }
+    // thread i looks at bins top - 2i and top - 2i - 1; the largest digit with
+    // at least `need` keys at or above it is picked
+    const int top = (int)mask;
     int c0 = 0, c1 = 0;
     if (2 * tid <= top) {
-      const uint32_t at = smem_u32(hs + top - 2 * tid - 1);
-      int2 v[EV_MAX_CLUSTER];
-#pragma unroll
-      for (uint32_t r = 0; r < EV_MAX_CLUSTER; ++r)
-        if (r < ranks) v[r] = ev_remote2(at, r);
-#pragma unroll
-      for (uint32_t r = 0; r < EV_MAX_CLUSTER; ++r)
-        if (r < ranks) {
-          c0 += v[r].y;
-          c1 += v[r].x;
-        }
+      const int bin = top - 2 * tid - 1;
+      const int2 v = ranks > 1 ? ev_remote2(smem_u32(hs + bin), bin / share)
+                               : *reinterpret_cast<const int2*>(hs + bin);
+      c0 = v.y;
+      c1 = v.x;
     }
     int incl = c0 + c1;
 #pragma unroll
@@ -212,8 +228,8 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     }
     if (lane == 31) sums[0][warp] = incl;
     __syncthreads();
-    const int before = __reduce_add_sync(0xffffffffu, lane < warp ? sums[0][lane] : 0);
-    const int above = before + incl - c0 - c1;
+    const int above =
+        __reduce_add_sync(0xffffffffu, lane < warp ? sums[0][lane] : 0) + incl - c0 - c1;
     if (above < need && need <= above + c0) {
       pick[0] = top - 2 * tid;
       pick[1] = need - above;
@@ -226,90 +242,83 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     need = pick[1];
     __syncthreads();
   }
-  // ordered compaction: each warp a contiguous range of the CTA's positions
-  const int per = ((p1 - p0 + EV_WARPS - 1) / EV_WARPS + 127) & ~127;
-  const int t0 = min(p0 + warp * per, p1), t1 = min(t0 + per, p1);
+  // ordered compaction: each warp a contiguous range [i0, i1) of the CTA's keys
+  const int per = ((len + EV_WARPS - 1) / EV_WARPS + 127) & ~127;
+  const int i0 = min(warp * per, len), i1 = min(i0 + per, len);
   int above = 0, equal = 0;
 #pragma unroll 2
-  for (int t = t0 + 4 * lane; t < t1; t += 128) {
-    const uint4 k4 = load4(t);
-    const uint32_t k[4] = {k4.x, k4.y, k4.z, k4.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      above += t + i < t1 && k[i] > prefix;
-      equal += t + i < t1 && k[i] == prefix;
-    }
+  for (int i = i0 + 4 * lane; i < i1; i += 128) {
+    const uint4 k = key4(i);
+    above += (k.x > prefix) + (k.y > prefix) + (k.z > prefix) + (k.w > prefix);
+    equal += (k.x == prefix) + (k.y == prefix) + (k.z == prefix) + (k.w == prefix);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    above += __shfl_xor_sync(0xffffffffu, above, o);
-    equal += __shfl_xor_sync(0xffffffffu, equal, o);
-  }
+  above = __reduce_add_sync(0xffffffffu, above);
+  equal = __reduce_add_sync(0xffffffffu, equal);
   if (lane == 0) {
     sums[0][warp] = above;
     sums[1][warp] = equal;
   }
   __syncthreads();
-  int at = 0, eq = 0;   // keys above, and equal, before this warp's range
+  int at, eq;   // keys above, and equal, before this warp's range
   {
-    int x = sums[0][lane], y = sums[1][lane];
-    const int x0 = lane < warp ? x : 0, y0 = lane < warp ? y : 0;
-    at = __reduce_add_sync(0xffffffffu, x0);
-    eq = __reduce_add_sync(0xffffffffu, y0);
-    x = __reduce_add_sync(0xffffffffu, x);
-    y = __reduce_add_sync(0xffffffffu, y);
-    if (tid == 0) {
-      mine[0] = x;
-      mine[1] = y;
+    const int x = sums[0][lane], y = sums[1][lane];
+    at = __reduce_add_sync(0xffffffffu, lane < warp ? x : 0);
+    eq = __reduce_add_sync(0xffffffffu, lane < warp ? y : 0);
+    if (warp == 0) {
+      const int xs = __reduce_add_sync(0xffffffffu, x), ys = __reduce_add_sync(0xffffffffu, y);
+      if (lane == 0) {
+        mine[0] = xs;
+        mine[1] = ys;
+      }
     }
   }
   ev_cluster_sync();
-  int cta_at = 0, cta_eq = 0;   // and before this CTA's
-#pragma unroll
-  for (uint32_t r = 0; r + 1 < EV_MAX_CLUSTER; ++r)
-    if (r < rank) {
-      const int2 v = ev_remote2(smem_u32(mine), r);
-      cta_at += v.x;
-      cta_eq += v.y;
-    }
-  at += cta_at;
-  eq += cta_eq;
+  if (rank > 0) {
+    const int2 v = lane < (int)rank ? ev_remote2(smem_u32(mine), lane) : make_int2(0, 0);
+    at += __reduce_add_sync(0xffffffffu, v.x);
+    eq += __reduce_add_sync(0xffffffffu, v.y);
+  }
+  // A warp first packs its kept positions over its own range of the keys (no
+  // more are kept than have been read), then writes them out in whole lines.
   const unsigned lower = (1u << lane) - 1u;
-  for (int tb = t0; tb < t1; tb += 128) {
+  const int jw = at + min(eq, need);   // this warp's first place
+  int j = jw;
+  auto put = [&](int to, int t) {
+    if (CACHED) keys[i0 + to - jw] = (uint32_t)t;
+    else kept[to] = t;
+  };
+  for (int ib = i0; ib < i1; ib += 128) {
     uint32_t k[4];
-    bool same = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = tb + 32 * i + lane;
-      k[i] = t < t1 ? (cached ? keys[t - p0] : make_key(t)) : 0u;
-      same |= t < t1 && k[i] == prefix;
-    }
-    // equal keys are rare, but for weights that are all alike
-    const bool any = __any_sync(0xffffffffu, same) && eq < need;
-    int j = at + min(eq, need);
+    for (int i = 0; i < 4; ++i) k[i] = key1(ib + 32 * i + lane);
+    const bool same = k[0] == prefix || k[1] == prefix || k[2] == prefix || k[3] == prefix;
+    if (__any_sync(0xffffffffu, same)) {   // rare, but for weights that are all alike
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = tb + 32 * i + lane;
-      bool keep = t < t1 && k[i] > prefix;
-      const unsigned mh = __ballot_sync(0xffffffffu, keep);
-      at += __popc(mh);
-      if (any) {
-        const bool e = t < t1 && k[i] == prefix;
-        const unsigned me = __ballot_sync(0xffffffffu, e);
-        keep = keep || (e && eq + __popc(me & lower) < need);
+      for (int i = 0; i < 4; ++i) {
+        const unsigned me = __ballot_sync(0xffffffffu, k[i] == prefix);
+        const bool keep = k[i] > prefix || (k[i] == prefix && eq + __popc(me & lower) < need);
+        const unsigned mk = __ballot_sync(0xffffffffu, keep);
+        if (keep) put(j + __popc(mk & lower), p0 + ib + 32 * i + lane);
+        j += __popc(mk);
         eq += __popc(me);
       }
-      const unsigned mk = __ballot_sync(0xffffffffu, keep);
-      if (keep) kept[j + __popc(mk & lower)] = t;
-      j += __popc(mk);
+    } else {
+      unsigned mk[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mk[i] = __ballot_sync(0xffffffffu, k[i] > prefix);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (k[i] > prefix) put(j + __popc(mk[i] & lower), p0 + ib + 32 * i + lane);
+        j += __popc(mk[i]);
+      }
     }
   }
-  if (wout) {   // the weights of what this CTA kept
-    __syncthreads();
-    const int j0 = cta_at + min(cta_eq, need);
-    const int j1 = cta_at + mine[0] + min(cta_eq + mine[1], need);
+  __syncwarp();
 #pragma unroll 4
-    for (int j = j0 + tid; j < j1; j += EV_THREADS) wout[j] = w[kept[j]];
+  for (int jj = jw + lane; jj < j; jj += 32) {
+    const int t = CACHED ? (int)keys[i0 + jj - jw] : kept[jj];
+    if (CACHED) kept[jj] = t;
+    if (wout) wout[jj] = w[t];
   }
   ev_cluster_sync();   // no CTA leaves while another may read its counts
 }
@@ -449,9 +458,16 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   // powers of two
   int cl = 1;
   while (cl < EV_MAX_CLUSTER && wstride > (int64_t)cl * EV_SLICE) cl *= 2;
-  const int64_t cap = (wstride + 128 * cl - 1) / (128 * cl) * 128;
-  a.key_cap = (int32_t)(cap <= EV_MAX_KEYS ? cap : 0);
-  if (smem_optin((const void*)kv8_select_kernel, EV_MAX_KEYS * 4) != JF_OK) return JF_ERR_CUDA;
+  const int64_t keys = (wstride + 128 * cl - 1) / (128 * cl) * 128;
+  const bool cached = keys <= EV_MAX_KEYS;
+  const void* const select = cached ? (const void*)kv8_select_kernel<true>
+                                    : (const void*)kv8_select_kernel<false>;
+  if (cached && smem_optin(select, EV_MAX_KEYS * 4) != JF_OK) return JF_ERR_CUDA;
+  // clusters past 8 CTAs are opted into (a flag of the function: setting it again
+  // changes nothing)
+  if (cl > 8 &&
+      cudaFuncSetAttribute(select, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+    return JF_ERR_CUDA;
   cudaLaunchAttribute attrs[2];
   attrs[0] = pdl[0];
   attrs[1].id = cudaLaunchAttributeClusterDimension;
@@ -460,11 +476,13 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   attrs[1].val.clusterDim.z = 1;
   cfg.gridDim = dim3((unsigned)cl, (unsigned)g.Hkv, (unsigned)batch);
   cfg.blockDim = dim3(EV_THREADS);
-  cfg.dynamicSmemBytes = (size_t)a.key_cap * 4;
+  cfg.dynamicSmemBytes = cached ? (size_t)keys * 4 : 0;
   cfg.stream = stream;
   cfg.attrs = attrs;
   cfg.numAttrs = 2;
-  if (cudaLaunchKernelEx(&cfg, kv8_select_kernel, a) != cudaSuccess) return JF_ERR_CUDA;
+  const cudaError_t es = cached ? cudaLaunchKernelEx(&cfg, kv8_select_kernel<true>, a)
+                                : cudaLaunchKernelEx(&cfg, kv8_select_kernel<false>, a);
+  if (es != cudaSuccess) return JF_ERR_CUDA;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   cfg.dynamicSmemBytes = 0;
