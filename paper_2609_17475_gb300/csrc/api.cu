@@ -142,18 +142,21 @@ int make_codes_map(const Geom& g, void* base, int rows_per_box, CUtensorMap* map
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
+}  // namespace
+
+namespace jfkv {
+
 // 5-D map over the code rows of an 8-bit pool: (byte of a 128-byte half, half,
-// row of K or V over all KV heads, K|V, page), box = (128, D / 128,
-// rows_per_box, 2, 1), 128B swizzle: one copy brings K and V of rows_per_box
-// positions of a KV head.
-int make_kv8_map(const Geom& g, void* base, int rows_per_box, CUtensorMap* map) {
+// row of K or V over all KV heads, K|V, page), box = (128, halves, rows, kv, 1),
+// 128B swizzle.
+int kv8_tensor_map(const Geom& g, void* base, int halves, int rows, int kv, CUtensorMap* map) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return JF_ERR_CUDA;
   cuuint64_t dims[5] = {128, (cuuint64_t)g.D / 128, (cuuint64_t)g.Hkv * g.P, 2,
                         (cuuint64_t)g.num_pages};
   cuuint64_t strides[4] = {128, (cuuint64_t)g.D, (cuuint64_t)g.codes_region,
                            (cuuint64_t)g.page_bytes};
-  cuuint32_t box[5] = {128, (cuuint32_t)g.D / 128, (cuuint32_t)rows_per_box, 2, 1};
+  cuuint32_t box[5] = {128, (cuuint32_t)halves, (cuuint32_t)rows, (cuuint32_t)kv, 1};
   cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 5, base, dims, strides, box, estr,
                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
@@ -161,7 +164,7 @@ int make_kv8_map(const Geom& g, void* base, int rows_per_box, CUtensorMap* map) 
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
-}  // namespace
+}  // namespace jfkv
 
 extern "C" {
 
@@ -250,7 +253,7 @@ static int decode_common(const jf_kv_pool* pool, const int32_t* page_table, int3
   const Geom g = make_geom(*pool);
   if (kv8) {
     CUtensorMap tmap8;
-    st = make_kv8_map(g, pool->base, kv8_box_rows(), &tmap8);
+    st = kv8_tensor_map(g, pool->base, g.D / 128, kv8_box_rows(), 2, &tmap8);
     if (st) return st;
     return launch_kv8_decode(g, *pool, tmap8, page_table, pt_stride, context_lens, batch, q,
                              num_q_heads, softmax_scale, out, workspace, num_splits, nullptr,
@@ -641,7 +644,7 @@ int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_tab
     return JF_ERR_WORKSPACE_TOO_SMALL;
   const Geom g = make_geom(*pool);
   CUtensorMap tmap;
-  st = make_kv8_map(g, pool->base, kv8_box_rows(), &tmap);
+  st = kv8_tensor_map(g, pool->base, g.D / 128, kv8_box_rows(), 2, &tmap);
   if (st) return st;
   return launch_kv8_decode(g, *pool, tmap, page_table, pt_stride, context_lens, batch, q,
                            num_q_heads, softmax_scale, out, workspace, num_splits,

@@ -1,0 +1,567 @@
+// Prefill-chunk attention over the 8-bit block-scaled cache on the 5th-generation
+// tensor cores.
+//
+// The tiling is prefill.cu's: a CTA holds 128 (query, head) rows of one KV head,
+// two CTAs form a pair whose M = 256 MMAs share every 64-position K/V tile, S is
+// taken over pairs of tiles (N = 128) into two TMEM buffers, P (fp16) replaces
+// S columns already read, O stays in TMEM.  What the 8-bit codes change:
+//  * S = Q K^T multiplies the codes as they lie in the pool (kind::f8f6f4): TMA
+//    brings K rows straight into the MMA's swizzled layout and nothing is
+//    dequantized.  Q, which needs more than e4m3's 4 bits, enters as a sum of two
+//    e4m3 terms, hi + lo, of the row scaled so that its largest element lies in
+//    [2^7, 2^8): bf16's 8 bits exactly for elements within 2^9 of the largest,
+//    and at most 2^-17 of it off below.  Two 8-bit products take the time of one
+//    16-bit product.
+//  * P V stays fp16 -- P has to keep small weights, which e4m3 cannot -- with V's
+//    codes widened to fp16 (exact) by four warps.
+//  * The block scales are powers of two and a half tile is a block: K's multiplies
+//    the fp32 score, V's exponent is added to it, so that P carries it, and l
+//    takes it out again (kv8_decode.cu has the identity).
+//  * With half of the dequantization gone, eight warps do the softmax: two groups
+//    of four take the even and the odd tiles, so that a pair's two tiles are
+//    worked on side by side while the tensor core runs the next pair's S and the
+//    last pair's P V.  The groups agree on each row's reference maximum tile by
+//    tile through shared memory; it moves only when a score exceeds it by 2^14.
+// Warp roles (each CTA):
+//   warp 0       TMEM; CTA 0's lane 0 issues every MMA of the pair, CTA 1's lane 0
+//                passes its K arrivals on to CTA 0
+//   warp 1       lane 0 loads this CTA's K halves (32 positions of each tile) by
+//                TMA into four pair buffers
+//   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers
+//   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
+#include <cmath>
+
+#include "kv8.cuh"
+#include "prefill.cuh"
+
+namespace jfkv {
+
+int kv8_tensor_map(const Geom& g, void* base, int halves, int rows, int kv, CUtensorMap* map);
+
+constexpr int P8_KBUF = 4;                 // K pair buffers
+constexpr int P8_VBUF = 4;                 // V tile buffers
+constexpr int P8_V_WARP0 = 2, P8_SM_WARP0 = 6;
+constexpr int P8_THREADS = 32 * 14;
+constexpr float P8_TOP = 14.f;             // P stays below 2^14
+constexpr float P8_SET = 6.f;              // a new reference puts the largest P at 2^6
+
+template <int D>
+struct P8Smem {
+  static constexpr int NB = D / 128;                     // 128-byte blocks of a row
+  static constexpr int Q_BYTES = PF_BM * D;              // one term: [D/128][128 rows][128 B]
+  static constexpr int KP_BYTES = PF_BN * D;             // [D/128][64 rows][128 B]
+  static constexpr int VT_BYTES = PF_BN * (D / 2) * 2;   // [D/128][64 rows][128 B]
+  static constexpr int OFF_Q = 0;                        // hi, then lo
+  static constexpr int OFF_K = 2 * Q_BYTES;
+  static constexpr int OFF_V = OFF_K + P8_KBUF * KP_BYTES;
+  static constexpr int OFF_BAR = OFF_V + P8_VBUF * VT_BYTES;
+  static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
+  static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
+  static constexpr int TOTAL = 1024 + OFF_L + 2 * PF_BM * 8;
+  static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
+};
+
+template <int D>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
+kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ PrefillArgs a) {
+  using L = P8Smem<D>;
+  constexpr uint32_t IDQK = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
+  constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
+
+  extern __shared__ uint8_t smraw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) &
+                                           ~static_cast<uintptr_t>(1023));
+  uint8_t* const sQ = sm + L::OFF_Q;
+  uint8_t* const sK = sm + L::OFF_K;
+  uint8_t* const sV = sm + L::OFF_V;
+  float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
+  float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
+  uint64_t* const k_land = bars + 0;     // [4] this CTA's K halves of a pair have landed
+  uint64_t* const k_peer = bars + 4;     // [4] on CTA 0: CTA 1's have
+  uint64_t* const k_free = bars + 8;     // [4] both CTAs: S of the pair in this buffer is done
+  uint64_t* const v_full = bars + 12;    // [4] on CTA 0: both CTAs' V halves stored (tile j % 4)
+  uint64_t* const pv_done = bars + 16;   // [4] both CTAs: P V of tile j done (j % 4)
+  uint64_t* const s_full = bars + 20;    // [2] both CTAs: S of pair i done (i & 1)
+  uint64_t* const p_full = bars + 22;    // [4] on CTA 0: both CTAs' P stored (tile j % 4)
+  uint64_t* const m_bar = bars + 26;     // [2 groups][4 quarters] the group's reference is set
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  // CTA pairs in launch order, as in prefill.cu: the KV heads of a pair of query
+  // tiles are consecutive, latest (longest) tiles first
+  const int pair = (int)(blockIdx.x >> 1);
+  const int kvh = pair % a.Hkv;
+  const int tile = (pair / a.Hkv) * 2 + (int)(blockIdx.x & 1);
+  int ri = 0;
+  for (int i = 1; i < a.nreq; ++i)
+    if (tile >= a.req[i].tile0) ri = i;
+  const PfReq& rq = a.req[ri];
+  const int32_t* const pt = rq.pt;
+  const int q_start = rq.q_start, C = rq.C;
+  const int bx = tile - rq.tile0;
+  const int qt = rq.n_tiles2 - 1 - bx;
+  const int qt_partner = rq.n_tiles2 - 1 - (bx ^ 1);
+  const int q0 = qt * a.QPC;
+  const int nq = max(0, min(a.QPC, C - q0));
+  const int rows = nq * a.G;
+  const int total = q_start + C;
+  auto kmax_of = [&](int t) {   // positions a query tile attends (0 for a padding tile)
+    const int first = t * a.QPC;
+    const int n = max(0, min(a.QPC, C - first));
+    return n == 0 ? 0 : (a.causal ? q_start + first + n : total);
+  };
+  const int kmax_pair = max(kmax_of(qt), kmax_of(qt_partner));
+  const int ntiles_all = (kmax_pair + PF_BN - 1) / PF_BN;
+  const int jb = (int)(((int64_t)ntiles_all * blockIdx.z) / a.num_splits);
+  const int je = (int)(((int64_t)ntiles_all * (blockIdx.z + 1)) / a.num_splits);
+  const int ntiles = je - jb;
+  const int npairs = (ntiles + 1) >> 1;
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&kmap);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&k_land[i], 1);
+      mbar_init(&k_peer[i], 1);
+      mbar_init(&k_free[i], 1);
+      mbar_init(&v_full[i], 8);   // the 4 V warps of each CTA
+      mbar_init(&pv_done[i], 1);
+      mbar_init(&p_full[i], 2 * PF_SM_WARPS);
+      mbar_init(&m_bar[i], 1);
+      mbar_init(&m_bar[4 + i], 1);
+    }
+    for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) tc::alloc2(tmem_slot, 512);
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+  tc::fence_after();
+  const uint32_t tbase = *tmem_slot;
+  const uint32_t tO = tbase;
+  const uint32_t tS = tbase + D;               // two S/P buffers of 2 PF_BN columns
+
+  auto page_of = [&](int j) -> int {           // of tile j (P >= 64: a tile lies in one page)
+    return j < ntiles ? __ldg(pt + ((jb + j) * PF_BN) / a.P) : -1;
+  };
+
+  // ---- softmax warps: their half of a Q row as two e4m3 terms (K-major, 128-byte
+  // swizzle: 16-byte piece m of row r at block m / 8, piece (m % 8) ^ (r % 8)) -------
+  const int quarter = warp & 3;                // TMEM lanes this warp may access
+  const int group = warp >= P8_SM_WARP0 + 4 ? 1 : 0;
+  const int r = quarter * 32 + lane;
+  const bool row_ok = r < rows;
+  const int qi = row_ok ? r / a.G : 0;
+  const int64_t qrow_at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
+  const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+  float smul = 0.f;                            // score = smul * S
+  if (warp >= P8_SM_WARP0) {
+    const uint16_t* const qrow = rq.q + qrow_at * D;
+    uint32_t mx = 0;                           // largest finite magnitude's bf16 bits
+    if (row_ok) {
+      for (int c = 0; c < D / 8; ++c) {
+        const uint4 w = *reinterpret_cast<const uint4*>(qrow + 8 * c);
+        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
+          if (lo < 0x7F80u) mx = max(mx, lo);
+          if (hi < 0x7F80u) mx = max(mx, hi);
+        }
+      }
+    }
+    const int qe = mx >= 0x80u ? max((int)(mx >> 7) - 127 - 7, -100) : -100;
+    smul = fabsf(a.scale_log2) * two8(qe);     // the scale's sign goes to Q
+    const float qs = a.scale_log2 < 0.f ? -two8(-qe) : two8(-qe);
+    if (smul == 0.f) smul = 1.f;               // a zero scale: zero scores
+    const bool zero = a.scale_log2 == 0.f;
+#pragma unroll 2
+    for (int mm = 0; mm < D / 32; ++mm) {
+      const int m = group * (D / 32) + mm;     // this group's half of the row
+      uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
+      if (row_ok && !zero) {
+        const uint4 w0 = *reinterpret_cast<const uint4*>(qrow + 16 * m);
+        const uint4 w1 = *reinterpret_cast<const uint4*>(qrow + 16 * m + 8);
+        const uint32_t ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const float x0 = bf16lo_to_f32(ws[k]) * qs, x1 = bf16hi_to_f32(ws[k]) * qs;
+          const uint32_t h = e4m3x2(x0, x1);
+          uint32_t f, unused;
+          f16x4_of_e4m3(h, f, unused);
+          const float2 hf = f32x2_of_f16x2(f);
+          const uint32_t l = e4m3x2(x0 - hf.x, x1 - hf.y);
+          hi[k >> 1] |= h << (16 * (k & 1));
+          lo[k >> 1] |= l << (16 * (k & 1));
+        }
+      }
+      uint8_t* const at = sQ + (m >> 3) * (PF_BM * 128) + r * 128 + (((m & 7) ^ (r & 7)) << 4);
+      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4*>(at + L::Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+    fence_proxy_async_smem();
+  }
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs' Q rows are in shared memory before the first MMA
+  tc::fence_after();
+
+  float m_own = -INFINITY, l = 0.f;   // softmax: the reference at this group's last tile
+  bool ok = true;
+  if (warp == 0) {
+    if (rank == 0 && lane == 0) {
+      // ================= MMA issuer =================
+      const uint32_t qaddr = smem_u32(sQ), kaddr = smem_u32(sK), vaddr = smem_u32(sV);
+      auto pv = [&](int j) {   // j: local tile index within this split
+        const int vb = j % P8_VBUF;
+        if (!tc::wait_cluster(&v_full[vb], (j / P8_VBUF) & 1) ||
+            !tc::wait_cluster(&p_full[j & 3], (j >> 2) & 1)) { ok = false; return; }
+        tc::fence_after();
+        const uint32_t tp = tS + ((j >> 1) & 1) * (2 * PF_BN) + (j & 1) * 32;
+#pragma unroll
+        for (int k = 0; k < PF_BN / 16; ++k)
+          tc::mma2_ts(tO, tp + 8 * k,
+                      tc::sdesc_sw128(vaddr + vb * L::VT_BYTES + k * 2048, PF_BN * 128, 1024),
+                      IDPV, (j > 0 || k > 0) ? 1u : 0u);
+        tc::commit2_both(&pv_done[j & 3]);
+      };
+      // S of pair i (column n = K row n of CTA 0 for n < 64, row n - 64 of CTA 1
+      // otherwise: position 32 rank + n % 32 of tile 2i + (n % 64) / 32), then P V of
+      // the previous pair's tiles
+      int jn = 0;   // next tile whose P V is due
+      for (int i = 0; i <= npairs && ok; ++i) {
+        if (i < npairs) {
+          const int kb = i % P8_KBUF;
+          if (!tc::wait_cluster(&k_land[kb], (i / P8_KBUF) & 1) ||
+              !tc::wait_cluster(&k_peer[kb], (i / P8_KBUF) & 1)) { ok = false; break; }
+          tc::fence_after();
+#pragma unroll
+          for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // hi's steps, then lo's
+            const int k = ks % (D / 32);
+            tc::mma2_ss_f8(tS + (i & 1) * (2 * PF_BN),
+                           tc::sdesc_sw128(qaddr + (ks / (D / 32)) * L::Q_BYTES +
+                                               (k >> 2) * (PF_BM * 128) + (k & 3) * 32, 16, 1024),
+                           tc::sdesc_sw128(kaddr + kb * L::KP_BYTES + (k >> 2) * (PF_BN * 128) +
+                                               (k & 3) * 32, 16, 1024),
+                           IDQK, ks ? 1u : 0u);
+          }
+          tc::commit2_both(&s_full[i & 1]);
+          tc::commit2_both(&k_free[kb]);
+        }
+        for (const int upto = i < npairs ? 2 * i : ntiles; jn < upto && ok; ++jn) pv(jn);
+      }
+    } else if (rank == 1 && lane == 0) {
+      // ================= CTA 1's K arrivals =================
+      for (int i = 0; i < npairs && ok; ++i) {
+        const int kb = i % P8_KBUF;
+        if (!tc::wait_cluster(&k_land[kb], (i / P8_KBUF) & 1)) { ok = false; break; }
+        tc::arrive_cluster(&k_peer[kb], 0);
+      }
+    }
+    if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    __syncwarp();
+  } else if (warp == 1) {
+    // ================= K halves by TMA =================
+    if (lane == 0) {
+      for (int i = 0; i < npairs; ++i) {
+        const int kb = i % P8_KBUF;
+        if (i >= P8_KBUF && !tc::wait_cluster(&k_free[kb], ((i / P8_KBUF) - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        const int tiles = min(2, ntiles - 2 * i);
+        mbar_arrive_expect_tx(&k_land[kb], (uint32_t)tiles * L::NB * 4096);
+        for (int u = 0; u < tiles; ++u) {
+          const int j = 2 * i + u;
+          int page = page_of(j);
+          if (page < 0 || page >= a.num_pages) {   // past the map's end: zeros
+            flag_error(a.status, JF_DEV_ERR_PAGE_ID);
+            page = (int)min(a.num_pages, (int64_t)0x7FFFFFFF);
+          }
+          const int row = kvh * a.P + ((jb + j) * PF_BN) % a.P + 32 * (int)rank;
+          for (int b = 0; b < L::NB; ++b)
+            tma_load_5d(sK + kb * L::KP_BYTES + b * (PF_BN * 128) + u * (32 * 128), &kmap, 0, b, row,
+                        0, page, &k_land[kb]);
+        }
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp < P8_SM_WARP0) {
+    // ================= V halves -> fp16 =================
+    // thread t: position t % 64, and of this CTA's D/2 columns the 64 (D = 256) or
+    // 32 (D = 128) that t / 64 names
+    const int e = (int)threadIdx.x - 32 * P8_V_WARP0;
+    const int t = e % PF_BN, part = e / PF_BN;
+    constexpr int NLD = D / 64;                      // 16-byte loads per item
+    const int64_t off = a.codes_region + (int)rank * (D / 2) + part * (D / 4);
+    // its 16-byte pieces (8 fp16) in the tile [D/128][64 rows][128 B]
+    uint8_t* const dst = sV + (D == 256 ? part : 0) * (PF_BN * 128) + t * 128;
+    const int piece0 = D == 256 ? 0 : 4 * part;
+    struct Tile {
+      uint4 c[NLD];
+      bool valid;
+    };
+    auto load_tile = [&](int j, int page, Tile& x) {
+      const int key0 = (jb + j) * PF_BN;
+      x.valid = page >= 0 && page < a.num_pages && key0 + t < kmax_pair;
+      if (x.valid) {
+        const uint8_t* const p = a.pool + (int64_t)page * a.page_bytes + off +
+                                 (int64_t)(kvh * a.P + key0 % a.P + t) * D;
+#pragma unroll
+        for (int u = 0; u < NLD; ++u) x.c[u] = __ldg(reinterpret_cast<const uint4*>(p + 16 * u));
+      }
+    };
+    auto step = [&](int j, const Tile& cur, Tile& nxt, int& page_next) {
+      const int vb = j % P8_VBUF;
+      if (j >= P8_VBUF && !tc::wait_cluster(&pv_done[vb], ((j / P8_VBUF) - 1) & 1)) {
+        ok = false;
+        return;
+      }
+#pragma unroll
+      for (int u = 0; u < NLD; ++u) {
+        const uint32_t w[4] = {cur.c[u].x, cur.c[u].y, cur.c[u].z, cur.c[u].w};
+        uint32_t f[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f16x4_of_e4m3(cur.valid ? w[k] : 0u, f[2 * k], f[2 * k + 1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int piece = piece0 + 2 * u + h;
+          *reinterpret_cast<uint4*>(dst + vb * L::VT_BYTES + ((piece ^ (t & 7)) << 4)) =
+              make_uint4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
+        }
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::arrive_cluster(&v_full[vb], 0);
+      // the next loads only now: the arrive's release would wait for them
+      if (j + 2 < ntiles) load_tile(j + 2, page_next, nxt);
+      page_next = page_of(j + 3);
+    };
+    Tile ta, tb, tcur;
+    int page_next = page_of(2);
+    if (ntiles > 0) load_tile(0, page_of(0), ta);
+    if (ntiles > 1) load_tile(1, page_of(1), tb);
+    for (int j = 0; j < ntiles && ok; j += 3) {
+      step(j, ta, tcur, page_next);
+      if (j + 1 < ntiles && ok) step(j + 1, tb, ta, page_next);
+      if (j + 2 < ntiles && ok) step(j + 2, tcur, tb, page_next);
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+  } else {
+    // ================= softmax: the tiles j = group, group + 2, ... =================
+    // padding rows see every position: their Q rows are zero and their outputs
+    // are not stored
+    const int limit = (row_ok && a.causal) ? q_start + q0 + qi : kmax_pair - 1;
+    // the two K and two V scales of a tile, loaded a tile of the group ahead (the
+    // page id two)
+    float2 ks, vs, ks_next = make_float2(1.f, 1.f), vs_next = ks_next;
+    auto load_scales = [&](int j, int page) {
+      ks_next = vs_next = make_float2(1.f, 1.f);
+      if (page >= 0 && page < a.num_pages) {
+        const uint8_t* p = a.pool + (int64_t)page * a.page_bytes + a.sb_base +
+                           (kvh * (a.P / KV8_BLOCK) + ((jb + j) * PF_BN) % a.P / KV8_BLOCK) * 4;
+        ks_next = __ldg(reinterpret_cast<const float2*>(p));
+        vs_next = __ldg(reinterpret_cast<const float2*>(p + a.sb_region));
+      }
+    };
+    load_scales(group, page_of(group));
+    int page_next = page_of(group + 2);
+    for (int j = group; j < ntiles; j += 2) {
+      ks = ks_next;
+      vs = vs_next;
+      load_scales(j + 2, page_next);
+      page_next = page_of(j + 4);
+      const int pi = j >> 1;
+      if (!tc::wait_cluster(&s_full[pi & 1], (pi >> 1) & 1)) { ok = false; break; }
+      tc::fence_after();
+      // tile j's S: positions 0..31 in columns 32 (j & 1) .., 32..63 in columns
+      // 64 + 32 (j & 1) .. of its pair's buffer; P_j goes to columns 32 (j & 1) ..
+      const uint32_t tb = tS + (pi & 1) * (2 * PF_BN) + group * 32 + lane_off;
+      uint32_t s0[32], s1[32];
+      tc::ld32(tb, s0);
+      tc::ld32(tb + 64, s1);
+      tc::wait_ld();
+      const int key0 = (jb + j) * PF_BN;
+      if (key0 + PF_BN - 1 > limit) {
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          if (key0 + c > limit) s0[c] = 0xFF800000u;
+          if (key0 + c + 32 > limit) s1[c] = 0xFF800000u;
+        }
+      }
+      // the largest score of each block, then of the tile (the factors are positive)
+      float x0[2] = {-INFINITY, -INFINITY}, x1[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int c = 0; c < 32; ++c) {
+        x0[c & 1] = fmaxf(x0[c & 1], __uint_as_float(s0[c]));
+        x1[c & 1] = fmaxf(x1[c & 1], __uint_as_float(s1[c]));
+      }
+      const int ev0 = exp8_of_scale(vs.x), ev1 = exp8_of_scale(vs.y);
+      const float k0 = smul * two8(exp8_of_scale(ks.x)), k1 = smul * two8(exp8_of_scale(ks.y));
+      const float mt = fmaxf(fmaf(fmaxf(x0[0], x0[1]), k0, (float)ev0),
+                             fmaf(fmaxf(x1[0], x1[1]), k1, (float)ev1));
+      // the reference after tile j - 1, the other group's
+      float m_ref = -INFINITY;
+      if (j > 0) {
+        const int jp = j - 1;
+        if (!mbar_wait_bounded(&m_bar[(jp & 1) * 4 + quarter], (jp >> 1) & 1)) { ok = false; break; }
+        m_ref = s_m[r];
+      }
+      const bool need = mt > m_ref + P8_TOP;
+      const float m_new = need ? mt - P8_SET : m_ref;
+      s_m[r] = m_new;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&m_bar[group * 4 + quarter]);
+      if (__any_sync(0xffffffffu, need) && j > 0) {   // O's rows to the new reference
+        const float f = (need && m_ref != -INFINITY) ? fast_exp2(m_ref - m_new) : 1.f;
+        if (!tc::wait_cluster(&pv_done[(j - 1) % PF_KVBUF], ((j - 1) / PF_KVBUF) & 1)) {
+          ok = false;
+          break;
+        }
+        tc::fence_after();
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          uint32_t o[32];
+          tc::ld32(tO + c0 + lane_off, o);
+          tc::wait_ld();
+#pragma unroll
+          for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+          tc::st32(tO + c0 + lane_off, o);
+        }
+      }
+      if (m_new != m_own) {
+        l = m_own == -INFINITY ? 0.f : l * fast_exp2(m_own - m_new);
+        m_own = m_new;
+      }
+      uint32_t p[32];
+      if (m_new == -INFINITY) {   // nothing visible yet on this row
+#pragma unroll
+        for (int c = 0; c < 32; ++c) p[c] = 0u;
+      } else {
+        const float c0 = (float)ev0 - m_new, c1 = (float)ev1 - m_new;
+        const uint64_t kk0 = f32x2(k0, k0), kk1 = f32x2(k1, k1);
+        const uint64_t cc0 = f32x2(c0, c0), cc1 = f32x2(c1, c1);
+        uint64_t l0 = f32x2(0.f, 0.f), l1 = l0;
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          float d0, d1;
+          unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s0[2 * c]), __uint_as_float(s0[2 * c + 1])),
+                                 kk0, cc0), d0, d1);
+          const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
+          l0 = add_f32x2(l0, f32x2(p0, p1));
+          p[c] = pack_f16x2(p0, p1);
+        }
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+          float d0, d1;
+          unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s1[2 * c]), __uint_as_float(s1[2 * c + 1])),
+                                 kk1, cc1), d0, d1);
+          const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
+          l1 = add_f32x2(l1, f32x2(p0, p1));
+          p[16 + c] = pack_f16x2(p0, p1);
+        }
+        float a0, a1, b0, b1;
+        unpack_f32x2(l0, a0, a1);
+        unpack_f32x2(l1, b0, b1);
+        l = fmaf(a0 + a1, two8(-ev0), fmaf(b0 + b1, two8(-ev1), l));
+      }
+      tc::st32(tb, p);
+      tc::wait_st();
+      tc::fence_before();
+      __syncwarp();
+      if (lane == 0) tc::arrive_cluster(&p_full[j & 3], 0);
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    s_ml[group * PF_BM + r] = make_float2(m_own, l);
+  }
+
+  // ---- O / l -> bf16 (one split) or the unnormalized partial (m, l, O); each
+  // softmax group half of the columns -------------------------------------------------
+  const bool all_ok = !__syncthreads_or(!ok);
+  if (warp >= P8_SM_WARP0) {
+    const bool split = a.num_splits > 1;
+    const int64_t prow = ((int64_t)rq.row0 * a.Hq + qrow_at) * a.num_splits + blockIdx.z;
+    float* const po = a.part_o + prow * D + group * (D / 2);
+    if (ntiles == 0) {   // an empty history range: a neutral partial
+      if (split && row_ok) {
+        if (group == 0) {
+          a.part_ml[prow * 2 + 0] = -INFINITY;
+          a.part_ml[prow * 2 + 1] = 0.f;
+        }
+        for (int c = 0; c < D / 8; ++c)
+          reinterpret_cast<float4*>(po)[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    } else if (all_ok && tc::wait_cluster(&pv_done[(ntiles - 1) % PF_KVBUF],
+                                          ((ntiles - 1) / PF_KVBUF) & 1)) {
+      tc::fence_after();
+      const float m = s_m[r];   // after the last tile
+      float lsum = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float2 v = s_ml[g * PF_BM + r];
+        if (v.x != -INFINITY) lsum = fmaf(v.y, fast_exp2(v.x - m), lsum);
+      }
+      if (split && row_ok && group == 0) {
+        a.part_ml[prow * 2 + 0] = m;
+        a.part_ml[prow * 2 + 1] = lsum;
+      }
+      const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
+      uint16_t* const orow = rq.out + qrow_at * D + group * (D / 2);
+#pragma unroll 1
+      for (int c0 = 0; c0 < D / 2; c0 += 32) {
+        uint32_t o[32];
+        tc::ld32(tO + group * (D / 2) + c0 + lane_off, o);
+        tc::wait_ld();
+        if (row_ok && split) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            reinterpret_cast<uint4*>(po + c0)[k] =
+                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
+        } else if (row_ok) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              w[i] = pack_bf16x2_rn(__uint_as_float(o[8 * k + 2 * i]) * inv,
+                                    __uint_as_float(o[8 * k + 2 * i + 1]) * inv);
+            *reinterpret_cast<uint4*>(orow + c0 + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    } else if (all_ok && lane == 0) {
+      flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+  }
+
+  // neither CTA may release TMEM or exit while its partner can still reach it
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  if (warp == 0) {
+    tc::fence_after();
+    tc::dealloc2(tbase, 512);
+  }
+}
+
+template <int D>
+static int launch_t(const CUtensorMap& kmap, const PrefillArgs& a, const dim3& grid,
+                    cudaStream_t stream) {
+  if (smem_optin((const void*)kv8_prefill_kernel<D>, P8Smem<D>::TOTAL) != JF_OK) return JF_ERR_CUDA;
+  kv8_prefill_kernel<D><<<grid, P8_THREADS, P8Smem<D>::TOTAL, stream>>>(kmap, a);
+  return cudaGetLastError() == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+}
+
+int launch_kv8_prefill(const Geom& g, const jf_kv_pool& pool, const PrefillArgs& a, unsigned ctas,
+                       unsigned splits, cudaStream_t stream) {
+  CUtensorMap kmap;
+  const int st = kv8_tensor_map(g, pool.base, 1, 32, 1, &kmap);
+  if (st) return st;
+  const dim3 grid(ctas, 1u, splits);
+  return g.D == 256 ? launch_t<256>(kmap, a, grid, stream) : launch_t<128>(kmap, a, grid, stream);
+}
+
+}  // namespace jfkv

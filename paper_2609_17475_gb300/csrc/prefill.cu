@@ -50,62 +50,15 @@
 // order, so Q K^T is unchanged, and the epilogue undoes it for O.  Q is
 // stored pre-multiplied by softmax_scale * log2(e), so S arrives in the log2
 // domain.
-//
-// 8-bit block pools (JF_FMT_E4M3_B32): the tiles hold the codes themselves as
-// fp16 (exact, natural d order), and no dequantizing thread multiplies.  The
-// block scales, powers of two, meet the softmax warps instead: a 64-position
-// tile has two of each, K's multiplies the fp32 score, and V's exponent is
-// added to it, so that P carries it (kv8_decode.cu has the identity); l takes
-// it back out.
 #include <cmath>
 
-#include "kv8.cuh"
-#include "tc.cuh"
+#include "prefill.cuh"
 #include "tq4.cuh"
 
 namespace jfkv {
 
-constexpr int PF_BM = 128;   // MMA rows per CTA (256 per CTA pair)
-constexpr int PF_BN = 64;    // positions per K/V tile
 constexpr int PF_DQ_WARPS = 8;
-constexpr int PF_SM_WARPS = 4;   // one per TMEM lane quarter, one row per thread
 constexpr int PF_THREADS = 32 * (1 + PF_DQ_WARPS + PF_SM_WARPS);
-constexpr int PF_KVBUF = 4;     // P V completion barriers, by tile index mod 4
-constexpr float PF_TAU = 8.f;   // log2 headroom before the running max moves
-constexpr float PF_SET8 = 6.f;  // E4M3: a new reference puts the largest P at 2^6, so that
-                                // small ones stay above fp16's subnormals for longer
-
-// One request's chunk in a launch: its query tiles are CTAs tile0 ..
-// tile0 + n_tiles2 - 1 (n_tiles2 even, so a CTA pair never spans requests).
-struct PfReq {
-  const int32_t* pt;    // its page-table row
-  const uint16_t* q;    // its chunk's queries [C, Hq, D]
-  uint16_t* out;        // [C, Hq, D]
-  int32_t q_start, C, tile0, n_tiles2;
-  int32_t row0;         // its first query's row in the launch (split partials)
-};
-
-constexpr int PF_MAX_REQ = 64;   // requests per launch
-
-struct PrefillArgs {
-  const uint8_t* pool;
-  int64_t num_pages;
-  int64_t page_bytes;
-  int64_t codes_region;
-  int64_t sb_base;
-  int64_t sb_region;
-  int32_t P, Hkv, Hq, G, QPC;
-  int32_t causal;
-  float scale_log2;
-  int32_t* status;
-  int32_t num_splits;   // > 1: history ranges per query tile, partials + merge
-  float* part_ml;       // [rows * Hq][num_splits][2] (m, l)
-  float* part_o;        // [rows * Hq][num_splits][D], unnormalized
-  const float* qrot;     // TQ4: rotated queries H S_K q / sqrt(D), fp32 [rows * Hq][D]
-  float cent[16];        // TQ4: centroids
-  int32_t nreq;
-  PfReq req[PF_MAX_REQ];
-};
 
 // Each CTA of a pair holds its 128 query rows (fp16, K-major) and half of
 // every K/V tile: K positions 32 r .. 32 r + 31 (all of head_dim, K-major)
@@ -126,26 +79,6 @@ struct PfSmem {
   static constexpr int TOTAL = 1024 + OFF_LUT + (FMT == JF_FMT_TQ4 ? 256 * 32 * 4 : 0);
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
-
-// packed fp32 pairs (Blackwell f32x2 arithmetic)
-__device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};\n" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack_f32x2(uint64_t v, float& lo, float& hi) {
-  asm("mov.b64 {%0, %1}, %2;\n" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ uint64_t sub_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("sub.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
 
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -192,21 +125,16 @@ __device__ __forceinline__ void sb_to_h2(uint32_t w, uint32_t& s2, uint32_t& b2)
 }
 
 // FMT: JF_FMT_AFFINE4_G64, or JF_FMT_TQ4 (centroid table, rotated queries,
-// natural d order, partial outputs rotated back by the merge kernel), or
-// JF_FMT_E4M3_B32 (8-bit codes, natural d order, scales in the softmax)
+// natural d order, partial outputs rotated back by the merge kernel)
 template <int D, int FMT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PF_THREADS, 1)
 prefill_kernel(const __grid_constant__ PrefillArgs a) {
   using L = PfSmem<D, FMT>;
   constexpr bool TQ = FMT == JF_FMT_TQ4;
-  constexpr bool E8 = FMT == JF_FMT_E4M3_B32;
-  constexpr bool NAT = TQ || E8;        // natural d order in the tiles
   constexpr int NKB = D / 64;           // 64-wide d blocks
-  constexpr int UPI = (D == 256) ? 2 : 1;   // units of 32 codes per dequant item
-  constexpr int UB = E8 ? 32 : 16;          // bytes of a unit
-  constexpr int NLD = UPI * UB / 16;        // 16-byte loads per item
+  constexpr int UPI = (D == 256) ? 2 : 1;   // 16-byte code units per dequant item
   constexpr int SBB = D / 16;
-  constexpr int CB = E8 ? D : D / 2;
+  constexpr int CB = D / 2;
   // 128 K items (32 positions x NKB blocks x 2/UPI units) + 128 V items
   // (64 positions x NKB/2 blocks x 2/UPI units): one per dequant thread
   static_assert((PF_BN / 2) * NKB * 2 / UPI == 128 && PF_BN * (NKB / 2) * 2 / UPI == 128,
@@ -345,13 +273,8 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
           qmax = fmaxf(qmax, fmaxf(fabsf(bf16lo_to_f32(ws[k])), fabsf(bf16hi_to_f32(ws[k]))));
       }
     }
-    if constexpr (E8) {   // always: the scores are rescaled by the block scales anyway
-      qmax *= fabsf(a.scale_log2);
-      qe = (qmax > 0.f && qmax < INFINITY) ? max(ilogbf(qmax) - 13, -100) : 0;
-    } else {
-      qmax *= a.scale_log2;
-      qe = (qmax >= 16384.f) ? (ilogbf(qmax) - 13) : 0;
-    }
+    qmax *= a.scale_log2;
+    qe = (qmax >= 16384.f) ? (ilogbf(qmax) - 13) : 0;
     const float qs = ldexpf(a.scale_log2, -qe);
 #pragma unroll 4
     for (int m = 0; m < D / 8; ++m) {
@@ -361,12 +284,8 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
       const float e2 = bf16lo_to_f32(w.y) * qs, e3 = bf16hi_to_f32(w.y) * qs;
       const float e4 = bf16lo_to_f32(w.z) * qs, e5 = bf16hi_to_f32(w.z) * qs;
       const float e6 = bf16lo_to_f32(w.w) * qs, e7 = bf16hi_to_f32(w.w) * qs;
-      if constexpr (E8)
-        *q_chunk(m) = make_uint4(pack_f16x2(e0, e1), pack_f16x2(e2, e3), pack_f16x2(e4, e5),
-                                 pack_f16x2(e6, e7));
-      else
-        *q_chunk(m) = make_uint4(pack_f16x2(e0, e4), pack_f16x2(e1, e5), pack_f16x2(e2, e6),
-                                 pack_f16x2(e3, e7));
+      *q_chunk(m) = make_uint4(pack_f16x2(e0, e4), pack_f16x2(e1, e5), pack_f16x2(e2, e6),
+                               pack_f16x2(e3, e7));
     }
     fence_proxy_async_smem();
   }
@@ -436,12 +355,12 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
     const int tpos = is_v ? t : (PF_BN / 2) * (int)rank + t;   // position within the tile
     // V tile buffers [D/128][64 rows][128 B]; K pair buffers [D/64][64 rows][128 B]
     uint8_t* dst_base = (is_v ? sV : sK) + kbl * (PF_BN * 128) + t * 128;
-    const int64_t code_off = (is_v ? a.codes_region : 0) + kb * (2 * UB) + u0 * UB;
+    const int64_t code_off = (is_v ? a.codes_region : 0) + kb * 32 + u0 * 16;
     // affine: the block's scale/bias word; TQ4: the vector's fp16 norm
     const int64_t sb_off = a.sb_base + (is_v ? a.sb_region : 0) + (TQ ? 0 : kb * 4);
     const uint32_t lut_lane = smem_u32(sm + L::OFF_LUT) + 4u * (uint32_t)lane;
     struct Tile {
-      uint4 c[NLD];
+      uint4 c[UPI];
       uint32_t sbw;
       bool valid;
     };
@@ -461,10 +380,8 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
         const int64_t row = (int64_t)kvh * a.P + key0 % a.P + tpos;
         const uint8_t* cp = base + code_off + row * CB;
 #pragma unroll
-        for (int u = 0; u < NLD; ++u) x.c[u] = __ldg(reinterpret_cast<const uint4*>(cp + 16 * u));
-        if constexpr (E8)
-          x.sbw = 0u;   // the softmax warps read the block scales
-        else if constexpr (TQ)
+        for (int u = 0; u < UPI; ++u) x.c[u] = __ldg(reinterpret_cast<const uint4*>(cp + 16 * u));
+        if constexpr (TQ)
           x.sbw = __ldg(reinterpret_cast<const uint16_t*>(base + sb_off + row * 2));
         else
           x.sbw = __ldg(reinterpret_cast<const uint32_t*>(base + sb_off + row * SBB));
@@ -472,18 +389,7 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
     };
     auto store = [&](uint8_t* tile, const Tile& x) {
       uint4 o[UPI][4];
-      if constexpr (E8) {
-#pragma unroll
-        for (int u = 0; u < NLD; ++u) {   // 16 codes: two chunks of 8 fp16
-          uint32_t f[8];
-          f16x4_of_e4m3(x.c[u].x, f[0], f[1]);
-          f16x4_of_e4m3(x.c[u].y, f[2], f[3]);
-          f16x4_of_e4m3(x.c[u].z, f[4], f[5]);
-          f16x4_of_e4m3(x.c[u].w, f[6], f[7]);
-          o[u >> 1][2 * (u & 1)] = make_uint4(f[0], f[1], f[2], f[3]);
-          o[u >> 1][2 * (u & 1) + 1] = make_uint4(f[4], f[5], f[6], f[7]);
-        }
-      } else if constexpr (TQ) {
+      if constexpr (TQ) {
         // TQ4: norm * centroid of each index, natural d order (byte i gives
         // d 2i, 2i+1); |c| < 1/4 and norm <= 65504 keep it in fp16 range
         const uint32_t n2 = (x.sbw & 0xFFFFu) | (x.sbw << 16);
@@ -572,33 +478,7 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
     const float smul = ldexpf(1.f, qe);   // S = (scaled Q) K^T * 2^qe
     float m_ref = -INFINITY, l = 0.f;
     bool ok = true;
-    // E4M3: the two K and two V scales of a tile (positions 0..31 and 32..63),
-    // loaded a tile ahead, the page id two
-    float2 ks = make_float2(1.f, 1.f), vs = ks, ks_next = ks, vs_next = ks;
-    int pg_next = -1;
-    auto page8_of = [&](int j) -> int {
-      return j < ntiles ? __ldg(pt + ((jb + j) * PF_BN) / a.P) : -1;
-    };
-    auto load_scales = [&](int j, int page) {
-      ks_next = vs_next = make_float2(1.f, 1.f);
-      if (page >= 0 && page < a.num_pages) {
-        const uint8_t* p = a.pool + (int64_t)page * a.page_bytes + a.sb_base +
-                           (kvh * (a.P / KV8_BLOCK) + ((jb + j) * PF_BN) % a.P / KV8_BLOCK) * 4;
-        ks_next = __ldg(reinterpret_cast<const float2*>(p));
-        vs_next = __ldg(reinterpret_cast<const float2*>(p + a.sb_region));
-      }
-    };
-    if constexpr (E8) {
-      load_scales(0, page8_of(0));
-      pg_next = page8_of(1);
-    }
     for (int j = 0; j < ntiles; ++j) {
-      if constexpr (E8) {
-        ks = ks_next;
-        vs = vs_next;
-        load_scales(j + 1, pg_next);
-        pg_next = page8_of(j + 2);
-      }
       // tile j's S: positions 0..31 in columns 32 (j & 1) .., 32..63 in
       // columns 64 + 32 (j & 1) .. of its pair's S/P buffer; P_j (fp16)
       // goes to columns 32 (j & 1) .. once both are read
@@ -615,23 +495,7 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
       float mt;
       {
         float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-        if constexpr (E8) {   // score times K scale, plus the V scale's exponent
-          const float k0 = smul * two8(exp8_of_scale(ks.x)), k1 = smul * two8(exp8_of_scale(ks.y));
-          const float v0 = (float)exp8_of_scale(vs.x), v1 = (float)exp8_of_scale(vs.y);
-          const bool full = key0 + PF_BN - 1 <= limit;
-#pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            x[c] = fmaf(__uint_as_float(s0[c]), k0, v0);
-            x[c + 32] = fmaf(__uint_as_float(s1[c]), k1, v1);
-          }
-          if (!full) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) {
-              if (key0 + c > limit) x[c] = -INFINITY;
-              if (key0 + c + 32 > limit) x[c + 32] = -INFINITY;
-            }
-          }
-        } else if (key0 + PF_BN - 1 <= limit) {
+        if (key0 + PF_BN - 1 <= limit) {
 #pragma unroll
           for (int c = 0; c < 32; ++c) { x[c] = __uint_as_float(s0[c]); x[c + 32] = __uint_as_float(s1[c]); }
         } else {
@@ -641,7 +505,7 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
             x[c + 32] = (key0 + c + 32 <= limit) ? __uint_as_float(s1[c]) : -INFINITY;
           }
         }
-        if (!E8 && qe != 0) {
+        if (qe != 0) {
 #pragma unroll
           for (int c = 0; c < PF_BN; ++c) x[c] *= smul;
         }
@@ -649,9 +513,9 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
         for (int c = 0; c < PF_BN; ++c) m4[c & 3] = fmaxf(m4[c & 3], x[c]);
         mt = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
       }
-      const bool need = mt > m_ref + (E8 ? PF_TAU + PF_SET8 : PF_TAU);
+      const bool need = mt > m_ref + PF_TAU;
       if (__any_sync(0xffffffffu, need)) {
-        const float nref = need ? (E8 ? mt - PF_SET8 : mt) : m_ref;
+        const float nref = need ? mt : m_ref;
         const float f = (need && m_ref != -INFINITY) ? fast_exp2(m_ref - nref) : 1.f;
         if (j > 0) {
           if (!tc::wait_cluster(&pv_done[(j - 1) % PF_KVBUF], ((j - 1) / PF_KVBUF) & 1)) { ok = false; break; }
@@ -683,17 +547,13 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
           float d0, d1;
           unpack_f32x2(sub_f32x2(f32x2(x[2 * c], x[2 * c + 1]), mm), d0, d1);
           const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
-          // E4M3: a sum for each block, whose V scales differ
-          l2[E8 ? c >> 4 : c & 1] = add_f32x2(l2[E8 ? c >> 4 : c & 1], f32x2(p0, p1));
+          l2[c & 1] = add_f32x2(l2[c & 1], f32x2(p0, p1));
           p[c] = pack_f16x2(p0, p1);
         }
         float a0, a1, b0, b1;
         unpack_f32x2(l2[0], a0, a1);
         unpack_f32x2(l2[1], b0, b1);
-        if constexpr (E8)
-          l = fmaf(a0 + a1, two8(-exp8_of_scale(vs.x)), fmaf(b0 + b1, two8(-exp8_of_scale(vs.y)), l));
-        else
-          l += (a0 + a1) + (b0 + b1);
+        l += (a0 + a1) + (b0 + b1);
       }
       tc::st32(tb + (j & 1) * 32 + lane_off, p);
       tc::wait_st();
@@ -733,7 +593,7 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
           for (int k = 0; k < 4; ++k) {
             const float* v = reinterpret_cast<const float*>(o + 8 * k);
             float4* dst = reinterpret_cast<float4*>(prow_o + c0 + 8 * k);
-            if constexpr (NAT) {
+            if constexpr (TQ) {
               dst[0] = make_float4(v[0], v[1], v[2], v[3]);
               dst[1] = make_float4(v[4], v[5], v[6], v[7]);
             } else {
@@ -745,17 +605,14 @@ prefill_kernel(const __grid_constant__ PrefillArgs a) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const float* v = reinterpret_cast<const float*>(o + 8 * k);
-            // the places of elements 0..7 in the tile's order
-            constexpr int e1 = NAT ? 1 : 2, e2 = NAT ? 2 : 4, e3 = NAT ? 3 : 6;
-            constexpr int e4 = NAT ? 4 : 1, e5 = NAT ? 5 : 3, e6 = NAT ? 6 : 5;
             uint4 w;
             w.x = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[0] * inv)) |
-                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e1] * inv)) << 16);
-            w.y = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e2] * inv)) |
-                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e3] * inv)) << 16);
-            w.z = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e4] * inv)) |
-                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e5] * inv)) << 16);
-            w.w = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[e6] * inv)) |
+                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[2] * inv)) << 16);
+            w.y = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[4] * inv)) |
+                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[6] * inv)) << 16);
+            w.z = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[1] * inv)) |
+                  ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[3] * inv)) << 16);
+            w.w = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[5] * inv)) |
                   ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v[7] * inv)) << 16);
             *reinterpret_cast<uint4*>(orow + c0 + 8 * k) = w;
           }
@@ -981,8 +838,7 @@ int launch_prefill_batch(const Geom& g, const jf_kv_pool& pool, const int32_t* c
   }
   int st;
   if (pool.format == JF_FMT_E4M3_B32)
-    st = g.D == 256 ? launch_pf<256, JF_FMT_E4M3_B32>(grid, a, stream)
-                    : launch_pf<128, JF_FMT_E4M3_B32>(grid, a, stream);
+    st = launch_kv8_prefill(g, pool, a, grid.x, grid.z, stream);
   else if (g.D == 256)
     st = tq ? launch_pf<256, JF_FMT_TQ4>(grid, a, stream)
             : launch_pf<256, JF_FMT_AFFINE4_G64>(grid, a, stream);

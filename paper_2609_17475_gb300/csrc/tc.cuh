@@ -67,6 +67,21 @@ __device__ __forceinline__ void mma2_ss(uint32_t d_tmem, uint64_t a_desc, uint64
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// Instruction descriptor, kind::f8f6f4 with e4m3 A/B (both K-major) and f32
+// accumulation.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+
+// As mma2_ss for 8-bit operands: 32 elements of K an instruction.
+__device__ __forceinline__ void mma2_ss_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+
 // The barrier at this shared offset in both CTAs arrives once the pair's
 // tcgen05 ops issued so far by this thread are done.
 __device__ __forceinline__ void commit2_both(uint64_t* bar) {
