@@ -20,8 +20,10 @@
 //  * With half of the dequantization gone, eight warps do the softmax: two groups
 //    of four take the even and the odd tiles, so that a pair's two tiles are
 //    worked on side by side while the tensor core runs the next pair's S and the
-//    last pair's P V.  The groups agree on each row's reference maximum tile by
-//    tile through shared memory; it moves only when a score exceeds it by 2^14.
+//    last pair's P V.  A row's reference maximum moves only when a score exceeds
+//    it by 2^14; the groups agree on it tile by tile through shared memory, but
+//    only after a tile's exponentials, which are worked out with the last known
+//    reference and again where it turns out to have moved.
 // Warp roles (each CTA):
 //   warp 0       TMEM; CTA 0's lane 0 issues every MMA of the pair, CTA 1's lane 0
 //                passes its K arrivals on to CTA 0
@@ -44,6 +46,12 @@ constexpr int P8_V_WARP0 = 2, P8_SM_WARP0 = 6;
 constexpr int P8_THREADS = 32 * 14;
 constexpr float P8_TOP = 14.f;             // P stays below 2^14
 constexpr float P8_SET = 6.f;              // a new reference puts the largest P at 2^6
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 
 template <int D>
 struct P8Smem {
@@ -143,8 +151,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const uint32_t tO = tbase;
   const uint32_t tS = tbase + D;               // two S/P buffers of 2 PF_BN columns
 
+  const int log2P = 31 - __clz(a.P);           // P is a power of two
   auto page_of = [&](int j) -> int {           // of tile j (P >= 64: a tile lies in one page)
-    return j < ntiles ? __ldg(pt + ((jb + j) * PF_BN) / a.P) : -1;
+    return j < ntiles ? __ldg(pt + (((jb + j) * PF_BN) >> log2P)) : -1;
   };
 
   // ---- softmax warps: their half of a Q row as two e4m3 terms (K-major, 128-byte
@@ -280,7 +289,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             flag_error(a.status, JF_DEV_ERR_PAGE_ID);
             page = (int)min(a.num_pages, (int64_t)0x7FFFFFFF);
           }
-          const int row = kvh * a.P + ((jb + j) * PF_BN) % a.P + 32 * (int)rank;
+          const int row = kvh * a.P + (((jb + j) * PF_BN) & (a.P - 1)) + 32 * (int)rank;
           for (int b = 0; b < L::NB; ++b)
             tma_load_5d(sK + kb * L::KP_BYTES + b * (PF_BN * 128) + u * (32 * 128), &kmap, 0, b, row,
                         0, page, &k_land[kb]);
@@ -309,7 +318,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       x.valid = page >= 0 && page < a.num_pages && key0 + t < kmax_pair;
       if (x.valid) {
         const uint8_t* const p = a.pool + (int64_t)page * a.page_bytes + off +
-                                 (int64_t)(kvh * a.P + key0 % a.P + t) * D;
+                                 (int64_t)(kvh * a.P + (key0 & (a.P - 1)) + t) * D;
 #pragma unroll
         for (int u = 0; u < NLD; ++u) x.c[u] = __ldg(reinterpret_cast<const uint4*>(p + 16 * u));
       }
@@ -362,7 +371,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       ks_next = vs_next = make_float2(1.f, 1.f);
       if (page >= 0 && page < a.num_pages) {
         const uint8_t* p = a.pool + (int64_t)page * a.page_bytes + a.sb_base +
-                           (kvh * (a.P / KV8_BLOCK) + ((jb + j) * PF_BN) % a.P / KV8_BLOCK) * 4;
+                           (kvh * (a.P / KV8_BLOCK) + (((jb + j) * PF_BN) & (a.P - 1)) / KV8_BLOCK) * 4;
         ks_next = __ldg(reinterpret_cast<const float2*>(p));
         vs_next = __ldg(reinterpret_cast<const float2*>(p + a.sb_region));
       }
@@ -375,99 +384,109 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       load_scales(j + 2, page_next);
       page_next = page_of(j + 4);
       const int pi = j >> 1;
-      if (!tc::wait_cluster(&s_full[pi & 1], (pi >> 1) & 1)) { ok = false; break; }
-      tc::fence_after();
+      const int ev0 = exp8_of_scale(vs.x), ev1 = exp8_of_scale(vs.y);
+      const float k0 = smul * two8(exp8_of_scale(ks.x)), k1 = smul * two8(exp8_of_scale(ks.y));
+      const int key0 = (jb + j) * PF_BN;
       // tile j's S: positions 0..31 in columns 32 (j & 1) .., 32..63 in columns
       // 64 + 32 (j & 1) .. of its pair's buffer; P_j goes to columns 32 (j & 1) ..
       const uint32_t tb = tS + (pi & 1) * (2 * PF_BN) + group * 32 + lane_off;
-      uint32_t s0[32], s1[32];
-      tc::ld32(tb, s0);
-      tc::ld32(tb + 64, s1);
-      tc::wait_ld();
-      const int key0 = (jb + j) * PF_BN;
-      if (key0 + PF_BN - 1 > limit) {
+      if (!tc::wait_cluster(&s_full[pi & 1], (pi >> 1) & 1)) { ok = false; break; }
+      tc::fence_after();
+      uint32_t p[32];
+      float m_use = m_own, l_new = 0.f;
+      bool agreed = false;
+#pragma unroll 1
+      for (;;) {
+        uint32_t s0[32], s1[32];
+        tc::ld32(tb, s0);
+        tc::ld32(tb + 64, s1);
+        tc::wait_ld();
+        if (key0 + PF_BN - 1 > limit) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          if (key0 + c > limit) s0[c] = 0xFF800000u;
-          if (key0 + c + 32 > limit) s1[c] = 0xFF800000u;
+          for (int c = 0; c < 32; ++c) {
+            if (key0 + c > limit) s0[c] = 0xFF800000u;
+            if (key0 + c + 32 > limit) s1[c] = 0xFF800000u;
+          }
         }
-      }
-      // the largest score of each block, then of the tile (the factors are positive)
-      float x0[2] = {-INFINITY, -INFINITY}, x1[2] = {-INFINITY, -INFINITY};
+        // the largest score of each block, then of the tile (the factors are positive)
+        float x0[2] = {-INFINITY, -INFINITY}, x1[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-      for (int c = 0; c < 32; ++c) {
-        x0[c & 1] = fmaxf(x0[c & 1], __uint_as_float(s0[c]));
-        x1[c & 1] = fmaxf(x1[c & 1], __uint_as_float(s1[c]));
+        for (int c = 0; c < 32; c += 2) {
+          x0[(c >> 1) & 1] = max3(x0[(c >> 1) & 1], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
+          x1[(c >> 1) & 1] = max3(x1[(c >> 1) & 1], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
+        }
+        const float mt = fmaxf(fmaf(fmaxf(x0[0], x0[1]), k0, (float)ev0),
+                               fmaf(fmaxf(x1[0], x1[1]), k1, (float)ev1));
+        const bool over = __any_sync(0xffffffffu, mt > m_use + P8_TOP);
+        if (!over) {
+          const float mm = m_use == -INFINITY ? 0.f : m_use;   // -inf: nothing visible yet, p = 0
+          const float c0 = (float)ev0 - mm, c1 = (float)ev1 - mm;
+          const uint64_t kk0 = f32x2(k0, k0), kk1 = f32x2(k1, k1);
+          const uint64_t cc0 = f32x2(c0, c0), cc1 = f32x2(c1, c1);
+          uint64_t l0 = f32x2(0.f, 0.f), l1 = l0;
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            float d0, d1;
+            unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s0[2 * c]),
+                                         __uint_as_float(s0[2 * c + 1])), kk0, cc0), d0, d1);
+            const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
+            l0 = add_f32x2(l0, f32x2(p0, p1));
+            p[c] = pack_f16x2(p0, p1);
+          }
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            float d0, d1;
+            unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s1[2 * c]),
+                                         __uint_as_float(s1[2 * c + 1])), kk1, cc1), d0, d1);
+            const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
+            l1 = add_f32x2(l1, f32x2(p0, p1));
+            p[16 + c] = pack_f16x2(p0, p1);
+          }
+          float a0, a1, b0, b1;
+          unpack_f32x2(l0, a0, a1);
+          unpack_f32x2(l1, b0, b1);
+          l_new = fmaf(a0 + a1, two8(-ev0), (b0 + b1) * two8(-ev1));
+        }
+        if (agreed) break;
+        // the reference after tile j - 1, the other group's
+        float m_ref = -INFINITY;
+        if (j > 0) {
+          const int jp = j - 1;
+          if (!mbar_wait_bounded(&m_bar[(jp & 1) * 4 + quarter], (jp >> 1) & 1)) { ok = false; break; }
+          m_ref = s_m[r];
+        }
+        if (!over && !__any_sync(0xffffffffu, m_ref != m_use)) break;
+        // it has moved, or moves now (O's rows with it): once more
+        const bool need = mt > m_ref + P8_TOP;
+        m_use = need ? mt - P8_SET : m_ref;
+        if (__any_sync(0xffffffffu, need) && j > 0) {
+          const float f = (need && m_ref != -INFINITY) ? fast_exp2(m_ref - m_use) : 1.f;
+          if (!tc::wait_cluster(&pv_done[(j - 1) % PF_KVBUF], ((j - 1) / PF_KVBUF) & 1)) {
+            ok = false;
+            break;
+          }
+          tc::fence_after();
+#pragma unroll 1
+          for (int c0 = 0; c0 < D; c0 += 32) {
+            uint32_t o[32];
+            tc::ld32(tO + c0 + lane_off, o);
+            tc::wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+            tc::st32(tO + c0 + lane_off, o);
+          }
+        }
+        agreed = true;
       }
-      const int ev0 = exp8_of_scale(vs.x), ev1 = exp8_of_scale(vs.y);
-      const float k0 = smul * two8(exp8_of_scale(ks.x)), k1 = smul * two8(exp8_of_scale(ks.y));
-      const float mt = fmaxf(fmaf(fmaxf(x0[0], x0[1]), k0, (float)ev0),
-                             fmaf(fmaxf(x1[0], x1[1]), k1, (float)ev1));
-      // the reference after tile j - 1, the other group's
-      float m_ref = -INFINITY;
-      if (j > 0) {
-        const int jp = j - 1;
-        if (!mbar_wait_bounded(&m_bar[(jp & 1) * 4 + quarter], (jp >> 1) & 1)) { ok = false; break; }
-        m_ref = s_m[r];
-      }
-      const bool need = mt > m_ref + P8_TOP;
-      const float m_new = need ? mt - P8_SET : m_ref;
-      s_m[r] = m_new;
+      if (!ok) break;
+      s_m[r] = m_use;
       __syncwarp();
       if (lane == 0) mbar_arrive(&m_bar[group * 4 + quarter]);
-      if (__any_sync(0xffffffffu, need) && j > 0) {   // O's rows to the new reference
-        const float f = (need && m_ref != -INFINITY) ? fast_exp2(m_ref - m_new) : 1.f;
-        if (!tc::wait_cluster(&pv_done[(j - 1) % PF_KVBUF], ((j - 1) / PF_KVBUF) & 1)) {
-          ok = false;
-          break;
-        }
-        tc::fence_after();
-#pragma unroll 1
-        for (int c0 = 0; c0 < D; c0 += 32) {
-          uint32_t o[32];
-          tc::ld32(tO + c0 + lane_off, o);
-          tc::wait_ld();
-#pragma unroll
-          for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-          tc::st32(tO + c0 + lane_off, o);
-        }
+      if (m_use != m_own) {
+        l = m_own == -INFINITY ? 0.f : l * fast_exp2(m_own - m_use);
+        m_own = m_use;
       }
-      if (m_new != m_own) {
-        l = m_own == -INFINITY ? 0.f : l * fast_exp2(m_own - m_new);
-        m_own = m_new;
-      }
-      uint32_t p[32];
-      if (m_new == -INFINITY) {   // nothing visible yet on this row
-#pragma unroll
-        for (int c = 0; c < 32; ++c) p[c] = 0u;
-      } else {
-        const float c0 = (float)ev0 - m_new, c1 = (float)ev1 - m_new;
-        const uint64_t kk0 = f32x2(k0, k0), kk1 = f32x2(k1, k1);
-        const uint64_t cc0 = f32x2(c0, c0), cc1 = f32x2(c1, c1);
-        uint64_t l0 = f32x2(0.f, 0.f), l1 = l0;
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          float d0, d1;
-          unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s0[2 * c]), __uint_as_float(s0[2 * c + 1])),
-                                 kk0, cc0), d0, d1);
-          const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
-          l0 = add_f32x2(l0, f32x2(p0, p1));
-          p[c] = pack_f16x2(p0, p1);
-        }
-#pragma unroll
-        for (int c = 0; c < 16; ++c) {
-          float d0, d1;
-          unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s1[2 * c]), __uint_as_float(s1[2 * c + 1])),
-                                 kk1, cc1), d0, d1);
-          const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
-          l1 = add_f32x2(l1, f32x2(p0, p1));
-          p[16 + c] = pack_f16x2(p0, p1);
-        }
-        float a0, a1, b0, b1;
-        unpack_f32x2(l0, a0, a1);
-        unpack_f32x2(l1, b0, b1);
-        l = fmaf(a0 + a1, two8(-ev0), fmaf(b0 + b1, two8(-ev1), l));
-      }
+      l += l_new;
       tc::st32(tb, p);
       tc::wait_st();
       tc::fence_before();
