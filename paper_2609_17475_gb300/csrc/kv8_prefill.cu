@@ -28,7 +28,8 @@
 //   warp 0       TMEM; CTA 0's lane 0 issues every MMA of the pair, CTA 1's lane 0
 //                passes its K arrivals on to CTA 0
 //   warp 1       lane 0 loads this CTA's K halves (32 positions of each tile) by
-//                TMA into four pair buffers
+//                TMA into three pair buffers, and the 128 bytes of each V row that
+//                hold its half into four staging tiles
 //   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers
 //   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
@@ -43,7 +44,8 @@ namespace jfkv {
 
 int kv8_tensor_map(const Geom& g, void* base, int halves, int rows, int kv, CUtensorMap* map);
 
-constexpr int P8_KBUF = 4;                 // K pair buffers
+constexpr int P8_KBUF = 3;                 // K pair buffers
+constexpr int P8_SBUF = 4;                 // V staging tiles
 constexpr int P8_VBUF = 4;                 // V tile buffers
 constexpr int P8_V_WARP0 = 2, P8_SM_WARP0 = 6;
 constexpr int P8_THREADS = 32 * 14;
@@ -65,7 +67,9 @@ struct P8Smem {
   static constexpr int OFF_Q = 0;                        // hi, then lo
   static constexpr int OFF_K = 2 * Q_BYTES;
   static constexpr int OFF_V = OFF_K + P8_KBUF * KP_BYTES;
-  static constexpr int OFF_BAR = OFF_V + P8_VBUF * VT_BYTES;
+  static constexpr int VS_BYTES = PF_BN * 128;           // staged codes: [64 rows][128 B]
+  static constexpr int OFF_S = OFF_V + P8_VBUF * VT_BYTES;
+  static constexpr int OFF_BAR = OFF_S + P8_SBUF * VS_BYTES;
   static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
   static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
   static constexpr int TOTAL = 1024 + OFF_L + 2 * PF_BM * 8;
@@ -85,20 +89,24 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   uint8_t* const sQ = sm + L::OFF_Q;
   uint8_t* const sK = sm + L::OFF_K;
   uint8_t* const sV = sm + L::OFF_V;
+  uint8_t* const sS = sm + L::OFF_S;
   float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
   float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
-  uint64_t* const k_land = bars + 0;     // [4] this CTA's K halves of a pair have landed
-  uint64_t* const k_peer = bars + 4;     // [4] on CTA 0: CTA 1's have
-  uint64_t* const k_free = bars + 8;     // [4] both CTAs: S of the pair in this buffer is done
+  uint64_t* const k_land = bars + 0;     // [3] this CTA's K halves of a pair have landed
+  uint64_t* const k_peer = bars + 4;     // [3] on CTA 0: CTA 1's have
+  uint64_t* const k_free = bars + 8;     // [3] both CTAs: S of the pair in this buffer is done
   uint64_t* const v_full = bars + 12;    // [4] on CTA 0: both CTAs' V halves stored (tile j % 4)
   uint64_t* const pv_done = bars + 16;   // [4] both CTAs: P V of tile j done (j % 4)
   uint64_t* const s_full = bars + 20;    // [2] both CTAs: S of pair i done (i & 1)
   uint64_t* const p_full = bars + 22;    // [4] on CTA 0: both CTAs' P stored (tile j % 4)
   uint64_t* const m_bar = bars + 26;     // [2 groups][4 quarters] the group's reference is set
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
+  uint64_t* const s_land = bars + 34;    // [4] staged V codes have landed
+  uint64_t* const s_free = bars + 38;    // [4] and been read by the 4 V warps
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 42);
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
+  const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
   // CTA pairs in launch order, as in prefill.cu: the KV heads of a pair of query
   // tiles are consecutive, latest (longest) tiles first
@@ -141,6 +149,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       mbar_init(&p_full[i], 2 * PF_SM_WARPS);
       mbar_init(&m_bar[i], 1);
       mbar_init(&m_bar[4 + i], 1);
+      mbar_init(&s_land[i], 1);
+      mbar_init(&s_free[i], 4);
     }
     for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1);
     fence_barrier_init();
@@ -223,21 +233,18 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   float m_own = -INFINITY, l = 0.f;   // softmax: the reference at this group's last tile
   bool ok = true;
   if (warp == 0) {
-    if (rank == 0 && lane == 0) {
+    if (rank == 0) {
       // ================= MMA issuer =================
-      const uint32_t qaddr = smem_u32(sQ), kaddr = smem_u32(sK), vaddr = smem_u32(sV);
-      auto pv = [&](int j) {   // j: local tile index within this split
-        const int vb = j % P8_VBUF;
-        if (!mbar_wait_bounded(&v_full[vb], (j / P8_VBUF) & 1) ||
-            !mbar_wait_bounded(&p_full[j & 3], (j >> 2) & 1)) { ok = false; return; }
-        tc::fence_after();
-        const uint32_t tp = tS + ((j >> 1) & 1) * (2 * PF_BN) + (j & 1) * 32;
-#pragma unroll
-        for (int k = 0; k < PF_BN / 16; ++k)
-          tc::mma2_ts(tO, tp + 8 * k,
-                      tc::sdesc_sw128(vaddr + vb * L::VT_BYTES + k * 2048, PF_BN * 128, 1024),
-                      IDPV, (j > 0 || k > 0) ? 1u : 0u);
-        tc::commit2_both(&pv_done[j & 3]);
+      // The whole warp runs this loop, so that its control flow and the operands'
+      // descriptors are uniform values; lane 0 alone issues (the loop run by lane 0
+      // alone moved every descriptor to uniform registers first, which took longer
+      // than the products: TIMES).
+      const uint64_t qd = tc::sdesc_sw128(smem_u32(sQ), 16, 1024);
+      const uint64_t kd = tc::sdesc_sw128(smem_u32(sK), 16, 1024);
+      const uint64_t vd = tc::sdesc_sw128(smem_u32(sV), PF_BN * 128, 1024);
+      const uint32_t leader = lane == 0;
+      auto wait = [&](uint64_t* bar, int phase) {
+        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
       // S of pair i (column n = K row n of CTA 0 for n < 64, row n - 64 of CTA 1
       // otherwise: position 32 rank + n % 32 of tile 2i + (n % 64) / 32), then P V of
@@ -246,23 +253,36 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       for (int i = 0; i <= npairs && ok; ++i) {
         if (i < npairs) {
           const int kb = i % P8_KBUF;
-          if (!mbar_wait_bounded(&k_land[kb], (i / P8_KBUF) & 1) ||
-              !mbar_wait_bounded(&k_peer[kb], (i / P8_KBUF) & 1)) { ok = false; break; }
+          ok = wait(&k_land[kb], i / P8_KBUF) && wait(&k_peer[kb], i / P8_KBUF);
+          if (!ok) break;
           tc::fence_after();
+          const uint64_t kd_i = kd + (uint64_t)(kb * (L::KP_BYTES >> 4));
+          const uint32_t d = tS + (i & 1) * (2 * PF_BN);
 #pragma unroll
           for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // hi's steps, then lo's
             const int k = ks % (D / 32);
-            tc::mma2_ss_f8(tS + (i & 1) * (2 * PF_BN),
-                           tc::sdesc_sw128(qaddr + (ks / (D / 32)) * L::Q_BYTES +
-                                               (k >> 2) * (PF_BM * 128) + (k & 3) * 32, 16, 1024),
-                           tc::sdesc_sw128(kaddr + kb * L::KP_BYTES + (k >> 2) * (PF_BN * 128) +
-                                               (k & 3) * 32, 16, 1024),
-                           IDQK, ks ? 1u : 0u);
+            tc::mma2_ss_f8_if(leader, d,
+                              qd + (((ks / (D / 32)) * L::Q_BYTES + (k >> 2) * (PF_BM * 128) +
+                                     (k & 3) * 32) >> 4),
+                              kd_i + (((k >> 2) * (PF_BN * 128) + (k & 3) * 32) >> 4), IDQK,
+                              ks ? 1u : 0u);
           }
-          tc::commit2_both(&s_full[i & 1]);
-          tc::commit2_both(&k_free[kb]);
+          tc::commit2_both_if(leader, &s_full[i & 1]);
+          tc::commit2_both_if(leader, &k_free[kb]);
         }
-        for (const int upto = i < npairs ? 2 * i : ntiles; jn < upto && ok; ++jn) pv(jn);
+        for (const int upto = i < npairs ? 2 * i : ntiles; jn < upto; ++jn) {
+          const int vb = jn % P8_VBUF;
+          ok = wait(&v_full[vb], jn / P8_VBUF) && wait(&p_full[jn & 3], jn >> 2);
+          if (!ok) break;
+          tc::fence_after();
+          const uint64_t vd_j = vd + (uint64_t)(vb * (L::VT_BYTES >> 4));
+          const uint32_t tp = tS + ((jn >> 1) & 1) * (2 * PF_BN) + (jn & 1) * 32;
+#pragma unroll
+          for (int k = 0; k < PF_BN / 16; ++k)
+            tc::mma2_ts_if(leader, tO, tp + 8 * k, vd_j + ((k * 2048) >> 4), IDPV,
+                           (jn > 0 || k > 0) ? 1u : 0u);
+          tc::commit2_both_if(leader, &pv_done[jn & 3]);
+        }
       }
     } else if (rank == 1 && lane == 0) {
       // ================= CTA 1's K arrivals =================
@@ -272,30 +292,45 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         tc::arrive_cluster(&k_peer[kb], 0);
       }
     }
-    if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     __syncwarp();
   } else if (warp == 1) {
-    // ================= K halves by TMA =================
+    // ================= K halves and V codes by TMA =================
     if (lane == 0) {
-      for (int i = 0; i < npairs; ++i) {
+      int pg[2] = {page_of(0), page_of(1)};
+      for (int i = 0; i < npairs && ok; ++i) {
+        const int tiles = min(2, ntiles - 2 * i);
+        int page[2] = {pg[0], pg[1]};
+        pg[0] = page_of(2 * i + 2);   // a pair ahead
+        pg[1] = page_of(2 * i + 3);
+        for (int u = 0; u < tiles; ++u)
+          if (page[u] < 0 || page[u] >= a.num_pages) {   // past the map's end: zeros
+            flag_error(a.status, JF_DEV_ERR_PAGE_ID);
+            page[u] = (int)min(a.num_pages, (int64_t)0x7FFFFFFF);
+          }
         const int kb = i % P8_KBUF;
         if (i >= P8_KBUF && !mbar_wait_bounded(&k_free[kb], ((i / P8_KBUF) - 1) & 1)) {
           ok = false;
           break;
         }
-        const int tiles = min(2, ntiles - 2 * i);
         mbar_arrive_expect_tx(&k_land[kb], (uint32_t)tiles * L::NB * 4096);
         for (int u = 0; u < tiles; ++u) {
-          const int j = 2 * i + u;
-          int page = page_of(j);
-          if (page < 0 || page >= a.num_pages) {   // past the map's end: zeros
-            flag_error(a.status, JF_DEV_ERR_PAGE_ID);
-            page = (int)min(a.num_pages, (int64_t)0x7FFFFFFF);
-          }
-          const int row = kvh * a.P + (((jb + j) * PF_BN) & (a.P - 1)) + 32 * (int)rank;
+          const int row = kvh * a.P + (((jb + 2 * i + u) * PF_BN) & (a.P - 1));
           for (int b = 0; b < L::NB; ++b)
-            tma_load_5d(sK + kb * L::KP_BYTES + b * (PF_BN * 128) + u * (32 * 128), &kmap, 0, b, row,
-                        0, page, &k_land[kb]);
+            tma_load_5d(sK + kb * L::KP_BYTES + b * (PF_BN * 128) + u * (32 * 128), &kmap, 0, b,
+                        row + 32 * (int)rank, 0, page[u], &k_land[kb]);
+        }
+        for (int u = 0; u < tiles; ++u) {
+          const int j = 2 * i + u, sb = j % P8_SBUF;
+          if (j >= P8_SBUF && !mbar_wait_bounded(&s_free[sb], ((j / P8_SBUF) - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          mbar_arrive_expect_tx(&s_land[sb], L::VS_BYTES);
+          const int row = kvh * a.P + (((jb + j) * PF_BN) & (a.P - 1));
+          for (int h = 0; h < 2; ++h)
+            tma_load_5d(sS + sb * L::VS_BYTES + h * (32 * 128), &kmap, 0, D == 256 ? (int)rank : 0,
+                        row + 32 * h, 1, page[u], &s_land[sb]);
         }
       }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -307,59 +342,49 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // 32 (D = 128) that t / 64 names
     const int e = (int)threadIdx.x - 32 * P8_V_WARP0;
     const int t = e % PF_BN, part = e / PF_BN;
-    constexpr int NLD = D / 64;                      // 16-byte loads per item
-    const int64_t off = a.codes_region + (int)rank * (D / 2) + part * (D / 4);
+    constexpr int NLD = D / 64;                      // 16-byte pieces of codes
+    const int code0 = D == 256 ? 4 * part : 4 * (int)rank + 2 * part;
+    const uint32_t src = smem_u32(sS) + t * 128;
     // its 16-byte pieces (8 fp16) in the tile [D/128][64 rows][128 B]
     uint8_t* const dst = sV + (D == 256 ? part : 0) * (PF_BN * 128) + t * 128;
     const int piece0 = D == 256 ? 0 : 4 * part;
-    struct Tile {
+    for (int j = 0; j < ntiles; ++j) {
+      const int sb = j % P8_SBUF, vb = j % P8_VBUF;
+      if (!mbar_wait_bounded(&s_land[sb], (j / P8_SBUF) & 1)) { ok = false; break; }
       uint4 c[NLD];
-      bool valid;
-    };
-    auto load_tile = [&](int j, int page, Tile& x) {
-      const int key0 = (jb + j) * PF_BN;
-      x.valid = page >= 0 && page < a.num_pages && key0 + t < kmax_pair;
-      if (x.valid) {
-        const uint8_t* const p = a.pool + (int64_t)page * a.page_bytes + off +
-                                 (int64_t)(kvh * a.P + (key0 & (a.P - 1)) + t) * D;
 #pragma unroll
-        for (int u = 0; u < NLD; ++u) x.c[u] = __ldg(reinterpret_cast<const uint4*>(p + 16 * u));
+      for (int u = 0; u < NLD; ++u)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+                     : "=r"(c[u].x), "=r"(c[u].y), "=r"(c[u].z), "=r"(c[u].w)
+                     : "r"(src + sb * L::VS_BYTES + (((code0 + u) ^ (t & 7)) << 4)));
+      if ((jb + j) * PF_BN + t >= kmax_pair) {   // a slot no query sees: whatever it holds
+#pragma unroll
+        for (int u = 0; u < NLD; ++u) c[u] = make_uint4(0u, 0u, 0u, 0u);
       }
-    };
-    auto step = [&](int j, const Tile& cur, Tile& nxt, int& page_next) {
-      const int vb = j % P8_VBUF;
-      if (j >= P8_VBUF && !mbar_wait_bounded(&pv_done[vb], ((j / P8_VBUF) - 1) & 1)) {
-        ok = false;
-        return;
-      }
+      uint32_t f[NLD][8];
 #pragma unroll
       for (int u = 0; u < NLD; ++u) {
-        const uint32_t w[4] = {cur.c[u].x, cur.c[u].y, cur.c[u].z, cur.c[u].w};
-        uint32_t f[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f16x4_of_e4m3(cur.valid ? w[k] : 0u, f[2 * k], f[2 * k + 1]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int piece = piece0 + 2 * u + h;
-          *reinterpret_cast<uint4*>(dst + vb * L::VT_BYTES + ((piece ^ (t & 7)) << 4)) =
-              make_uint4(f[4 * h], f[4 * h + 1], f[4 * h + 2], f[4 * h + 3]);
-        }
+        f16x4_of_e4m3(c[u].x, f[u][0], f[u][1]);
+        f16x4_of_e4m3(c[u].y, f[u][2], f[u][3]);
+        f16x4_of_e4m3(c[u].z, f[u][4], f[u][5]);
+        f16x4_of_e4m3(c[u].w, f[u][6], f[u][7]);
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_free[sb]);
+      if (j >= P8_VBUF && !mbar_wait_bounded(&pv_done[vb], ((j / P8_VBUF) - 1) & 1)) {
+        ok = false;
+        break;
+      }
+#pragma unroll
+      for (int u = 0; u < NLD; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<uint4*>(dst + vb * L::VT_BYTES +
+                                    (((piece0 + 2 * u + h) ^ (t & 7)) << 4)) =
+              make_uint4(f[u][4 * h], f[u][4 * h + 1], f[u][4 * h + 2], f[u][4 * h + 3]);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) tc::arrive_cluster(&v_full[vb], 0);
-      // the next loads only now: the arrive's release would wait for them
-      if (j + 2 < ntiles) load_tile(j + 2, page_next, nxt);
-      page_next = page_of(j + 3);
-    };
-    Tile ta, tb, tcur;
-    int page_next = page_of(2);
-    if (ntiles > 0) load_tile(0, page_of(0), ta);
-    if (ntiles > 1) load_tile(1, page_of(1), tb);
-    for (int j = 0; j < ntiles && ok; j += 3) {
-      step(j, ta, tcur, page_next);
-      if (j + 1 < ntiles && ok) step(j + 1, tb, ta, page_next);
-      if (j + 2 < ntiles && ok) step(j + 2, tcur, tb, page_next);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   } else {
@@ -396,60 +421,52 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       if (!mbar_wait_bounded(&s_full[pi & 1], (pi >> 1) & 1)) { ok = false; break; }
       tc::fence_after();
       uint32_t p[32];
+#pragma unroll
+      for (int c = 0; c < 16; ++c) p[16 + c] = 0u;
       float m_use = m_own, l_new = 0.f;
       bool agreed = false;
 #pragma unroll 1
       for (;;) {
-        uint32_t s0[32], s1[32];
-        tc::ld32(tb, s0);
-        tc::ld32(tb + 64, s1);
-        tc::wait_ld();
-        if (key0 + PF_BN - 1 > limit) {
+        // Block by block (one copy of the code: the roles share the instruction
+        // caches): P under the reference m_use, its sum, and the largest score -- one
+        // past the reference's reach is found only afterwards.
+        const float mm = m_use == -INFINITY ? 0.f : m_use;   // -inf: nothing visible so far
+        float mt = -INFINITY;
+        l_new = 0.f;
+#pragma unroll 1
+        for (int h = 0; h < 2; ++h) {
+          uint32_t s[32];
+          tc::ld32(tb + 64 * h, s);
+          tc::wait_ld();
+          const int first = key0 + 32 * h;
+          if (first + 31 > limit) {
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if (key0 + c > limit) s0[c] = 0xFF800000u;
-            if (key0 + c + 32 > limit) s1[c] = 0xFF800000u;
+            for (int c = 0; c < 32; ++c)
+              if (first + c > limit) s[c] = 0xFF800000u;
           }
-        }
-        // the largest score of each block, then of the tile (the factors are positive)
-        float x0[2] = {-INFINITY, -INFINITY}, x1[2] = {-INFINITY, -INFINITY};
+          const float k = h ? k1 : k0;
+          const float ev = (float)(h ? ev1 : ev0);
+          const uint64_t kk = f32x2(k, k), cc = f32x2(ev - mm, ev - mm);
+          uint64_t sum = f32x2(0.f, 0.f);
+          float x[2] = {-INFINITY, -INFINITY};
 #pragma unroll
-        for (int c = 0; c < 32; c += 2) {
-          x0[(c >> 1) & 1] = max3(x0[(c >> 1) & 1], __uint_as_float(s0[c]), __uint_as_float(s0[c + 1]));
-          x1[(c >> 1) & 1] = max3(x1[(c >> 1) & 1], __uint_as_float(s1[c]), __uint_as_float(s1[c + 1]));
-        }
-        const float mt = fmaxf(fmaf(fmaxf(x0[0], x0[1]), k0, (float)ev0),
-                               fmaf(fmaxf(x1[0], x1[1]), k1, (float)ev1));
-        const bool over = __any_sync(0xffffffffu, mt > m_use + P8_TOP);
-        if (!over) {
-          const float mm = m_use == -INFINITY ? 0.f : m_use;   // -inf: nothing visible yet, p = 0
-          const float c0 = (float)ev0 - mm, c1 = (float)ev1 - mm;
-          const uint64_t kk0 = f32x2(k0, k0), kk1 = f32x2(k1, k1);
-          const uint64_t cc0 = f32x2(c0, c0), cc1 = f32x2(c1, c1);
-          uint64_t l0 = f32x2(0.f, 0.f), l1 = l0;
+          for (int c = 0; c < 16; ++c) p[c] = p[16 + c];
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
+            const float a0 = __uint_as_float(s[2 * c]), a1 = __uint_as_float(s[2 * c + 1]);
+            x[c & 1] = max3(x[c & 1], a0, a1);
             float d0, d1;
-            unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s0[2 * c]),
-                                         __uint_as_float(s0[2 * c + 1])), kk0, cc0), d0, d1);
+            unpack_f32x2(fma_f32x2(f32x2(a0, a1), kk, cc), d0, d1);
             const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
-            l0 = add_f32x2(l0, f32x2(p0, p1));
-            p[c] = pack_f16x2(p0, p1);
-          }
-#pragma unroll
-          for (int c = 0; c < 16; ++c) {
-            float d0, d1;
-            unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s1[2 * c]),
-                                         __uint_as_float(s1[2 * c + 1])), kk1, cc1), d0, d1);
-            const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
-            l1 = add_f32x2(l1, f32x2(p0, p1));
+            sum = add_f32x2(sum, f32x2(p0, p1));
             p[16 + c] = pack_f16x2(p0, p1);
           }
-          float a0, a1, b0, b1;
-          unpack_f32x2(l0, a0, a1);
-          unpack_f32x2(l1, b0, b1);
-          l_new = fmaf(a0 + a1, two8(-ev0), (b0 + b1) * two8(-ev1));
+          mt = fmaxf(mt, fmaf(fmaxf(x[0], x[1]), k, ev));   // k is positive
+          float u, v;
+          unpack_f32x2(sum, u, v);
+          l_new = fmaf(u + v, two8(-(h ? ev1 : ev0)), l_new);
         }
+        const bool over = __any_sync(0xffffffffu, mt > m_use + P8_TOP);
         if (agreed) break;
         // the reference after tile j - 1, the other group's
         float m_ref = -INFINITY;
