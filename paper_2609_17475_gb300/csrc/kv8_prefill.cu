@@ -93,17 +93,17 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
   float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
-  uint64_t* const k_land = bars + 0;     // [3] this CTA's K halves of a pair have landed
-  uint64_t* const k_peer = bars + 4;     // [3] on CTA 0: CTA 1's have
-  uint64_t* const k_free = bars + 8;     // [3] both CTAs: S of the pair in this buffer is done
-  uint64_t* const v_full = bars + 12;    // [4] on CTA 0: both CTAs' V halves stored (tile j % 4)
-  uint64_t* const pv_done = bars + 16;   // [4] both CTAs: P V of tile j done (j % 4)
-  uint64_t* const s_full = bars + 20;    // [2] both CTAs: S of pair i done (i & 1)
-  uint64_t* const p_full = bars + 22;    // [4] on CTA 0: both CTAs' P stored (tile j % 4)
-  uint64_t* const m_bar = bars + 26;     // [2 groups][4 quarters] the group's reference is set
-  uint64_t* const s_land = bars + 34;    // [4] staged V codes have landed
-  uint64_t* const s_free = bars + 38;    // [4] and been read by the 4 V warps
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 42);
+  // On CTA 0, where the pair's MMAs are issued:
+  uint64_t* const k_full = bars + 0;     // [3] both CTAs' K halves of a pair have landed
+  uint64_t* const pv_ready = bars + 3;   // [4] both CTAs' V halves and P of tile j % 4 stored
+  // on each CTA:
+  uint64_t* const k_land = bars + 7;     // [3] CTA 1: its K halves have landed
+  uint64_t* const s_full = bars + 10;    // [3] S of pair i % 3 done (its K buffer is free)
+  uint64_t* const pv_done = bars + 13;   // [4] P V of tile j % 4 done
+  uint64_t* const m_bar = bars + 17;     // [2 groups][4 quarters] the group's reference is set
+  uint64_t* const s_land = bars + 25;    // [4] staged V codes have landed
+  uint64_t* const s_free = bars + 29;    // [4] and been read by the 4 V warps
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 33);
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
@@ -141,18 +141,18 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&k_land[i], 1);
-      mbar_init(&k_peer[i], 1);
-      mbar_init(&k_free[i], 1);
-      mbar_init(&v_full[i], 8);   // the 4 V warps of each CTA
+      mbar_init(&pv_ready[i], 2 * (4 + PF_SM_WARPS));   // 4 V and 4 softmax warps of each CTA
       mbar_init(&pv_done[i], 1);
-      mbar_init(&p_full[i], 2 * PF_SM_WARPS);
       mbar_init(&m_bar[i], 1);
       mbar_init(&m_bar[4 + i], 1);
       mbar_init(&s_land[i], 1);
       mbar_init(&s_free[i], 4);
     }
-    for (int i = 0; i < 2; ++i) mbar_init(&s_full[i], 1);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&k_full[i], 2);   // CTA 0's own copies, CTA 1's arrival
+      mbar_init(&k_land[i], 1);
+      mbar_init(&s_full[i], 1);
+    }
     fence_barrier_init();
   }
   if (warp == 0) tc::alloc2(tmem_slot, 512);
@@ -253,7 +253,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       for (int i = 0; i <= npairs && ok; ++i) {
         if (i < npairs) {
           const int kb = i % P8_KBUF;
-          ok = wait(&k_land[kb], i / P8_KBUF) && wait(&k_peer[kb], i / P8_KBUF);
+          ok = wait(&k_full[kb], i / P8_KBUF);
           if (!ok) break;
           tc::fence_after();
           const uint64_t kd_i = kd + (uint64_t)(kb * (L::KP_BYTES >> 4));
@@ -267,12 +267,11 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
                               kd_i + (((k >> 2) * (PF_BN * 128) + (k & 3) * 32) >> 4), IDQK,
                               ks ? 1u : 0u);
           }
-          tc::commit2_both_if(leader, &s_full[i & 1]);
-          tc::commit2_both_if(leader, &k_free[kb]);
+          tc::commit2_both_if(leader, &s_full[kb]);
         }
         for (const int upto = i < npairs ? 2 * i : ntiles; jn < upto; ++jn) {
           const int vb = jn % P8_VBUF;
-          ok = wait(&v_full[vb], jn / P8_VBUF) && wait(&p_full[jn & 3], jn >> 2);
+          ok = wait(&pv_ready[vb], jn / P8_VBUF);
           if (!ok) break;
           tc::fence_after();
           const uint64_t vd_j = vd + (uint64_t)(vb * (L::VT_BYTES >> 4));
@@ -281,7 +280,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           for (int k = 0; k < PF_BN / 16; ++k)
             tc::mma2_ts_if(leader, tO, tp + 8 * k, vd_j + ((k * 2048) >> 4), IDPV,
                            (jn > 0 || k > 0) ? 1u : 0u);
-          tc::commit2_both_if(leader, &pv_done[jn & 3]);
+          tc::commit2_both_if(leader, &pv_done[vb]);
         }
       }
     } else if (rank == 1 && lane == 0) {
@@ -289,7 +288,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       for (int i = 0; i < npairs && ok; ++i) {
         const int kb = i % P8_KBUF;
         if (!mbar_wait_bounded(&k_land[kb], (i / P8_KBUF) & 1)) { ok = false; break; }
-        tc::arrive_cluster(&k_peer[kb], 0);
+        tc::arrive_cluster(&k_full[kb], 0);
       }
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -309,16 +308,17 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             page[u] = (int)min(a.num_pages, (int64_t)0x7FFFFFFF);
           }
         const int kb = i % P8_KBUF;
-        if (i >= P8_KBUF && !mbar_wait_bounded(&k_free[kb], ((i / P8_KBUF) - 1) & 1)) {
+        uint64_t* const land = rank == 0 ? &k_full[kb] : &k_land[kb];
+        if (i >= P8_KBUF && !mbar_wait_bounded(&s_full[kb], ((i / P8_KBUF) - 1) & 1)) {
           ok = false;
           break;
         }
-        mbar_arrive_expect_tx(&k_land[kb], (uint32_t)tiles * L::NB * 4096);
+        mbar_arrive_expect_tx(land, (uint32_t)tiles * L::NB * 4096);
         for (int u = 0; u < tiles; ++u) {
           const int row = kvh * a.P + (((jb + 2 * i + u) * PF_BN) & (a.P - 1));
           for (int b = 0; b < L::NB; ++b)
             tma_load_5d(sK + kb * L::KP_BYTES + b * (PF_BN * 128) + u * (32 * 128), &kmap, 0, b,
-                        row + 32 * (int)rank, 0, page[u], &k_land[kb]);
+                        row + 32 * (int)rank, 0, page[u], land);
         }
         for (int u = 0; u < tiles; ++u) {
           const int j = 2 * i + u, sb = j % P8_SBUF;
@@ -384,7 +384,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
               make_uint4(f[u][4 * h], f[u][4 * h + 1], f[u][4 * h + 2], f[u][4 * h + 3]);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) tc::arrive_cluster(&v_full[vb], 0);
+      if (lane == 0) tc::arrive_cluster(&pv_ready[vb], 0);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   } else {
@@ -418,7 +418,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // tile j's S: positions 0..31 in columns 32 (j & 1) .., 32..63 in columns
       // 64 + 32 (j & 1) .. of its pair's buffer; P_j goes to columns 32 (j & 1) ..
       const uint32_t tb = tS + (pi & 1) * (2 * PF_BN) + group * 32 + lane_off;
-      if (!mbar_wait_bounded(&s_full[pi & 1], (pi >> 1) & 1)) { ok = false; break; }
+      if (!mbar_wait_bounded(&s_full[pi % P8_KBUF], (pi / P8_KBUF) & 1)) { ok = false; break; }
       tc::fence_after();
       uint32_t p[32];
 #pragma unroll
@@ -511,7 +511,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       tc::wait_st();
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) tc::arrive_cluster(&p_full[j & 3], 0);
+      if (lane == 0) tc::arrive_cluster(&pv_ready[j % P8_VBUF], 0);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     s_ml[group * PF_BM + r] = make_float2(m_own, l);
