@@ -333,11 +333,18 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int h = blockIdx.y, b = blockIdx.z;
-  const int m = min(ev_ctx(a, b), a.budget);
   const int j0 = blockIdx.x * KV8_BLOCK;
-  if (j0 >= m) return;
   const int li = threadIdx.x % LPR, rr = threadIdx.x / LPR;
   const int32_t* const kept = a.kept + ((int64_t)b * a.Hkv + h) * a.budget;
+  // the kept positions, -1 past them, are loaded beside the context they depend on
+  int kept_t[NP];
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    const int j = j0 + p * RPP + rr;
+    kept_t[p] = j < a.budget ? kept[j] : -1;
+  }
+  const int m = min(ev_ctx(a, b), a.budget);
+  if (j0 >= m) return;
   const int pd = j0 >> a.log2P, slot0 = j0 & (a.P - 1);
   const int32_t dst = pd < a.dst_stride ? a.dst_table[(int64_t)b * a.dst_stride + pd] : -1;
   uint4 x[NP][2];
@@ -348,7 +355,7 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
     x[p][0] = x[p][1] = make_uint4(0u, 0u, 0u, 0u);
     s_old[p][0] = s_old[p][1] = 0.f;
     if (j < m) {
-      const int t = kept[j];
+      const int t = kept_t[p];
       const int32_t page = a.page_table[(int64_t)b * a.pt_stride + (t >> a.log2P)];
       if (page < 0 || page >= a.num_pages) {
         if (li == 0) flag_error(a.err, JF_DEV_ERR_PAGE_ID);   // the row becomes zeros

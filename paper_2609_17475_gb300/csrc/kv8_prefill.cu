@@ -520,6 +520,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   // ---- O / l -> bf16 (one split) or the unnormalized partial (m, l, O); each
   // softmax group half of the columns -------------------------------------------------
   const bool all_ok = !__syncthreads_or(!ok);
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");   // the merge waits for the rest
   if (warp >= P8_SM_WARP0) {
     const bool split = a.num_splits > 1;
     const int64_t prow = ((int64_t)rq.row0 * a.Hq + qrow_at) * a.num_splits + blockIdx.z;

@@ -678,6 +678,7 @@ prefill_merge_kernel(const float* part_ml, const float* part_o, uint16_t* out, i
   constexpr int E = D / 32;
   const int64_t row = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5;
   const int lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the partials are complete
   if (row >= rows) return;   // whole warps
   const float2* ml = reinterpret_cast<const float2*>(part_ml) + row * S;
   float M = -INFINITY;
@@ -847,23 +848,26 @@ int launch_prefill_batch(const Geom& g, const jf_kv_pool& pool, const int32_t* c
             : launch_pf<128, JF_FMT_AFFINE4_G64>(grid, a, stream);
   if (st) return st;
   if (num_splits > 1 || tq) {
+    // programmatic dependent launch: scheduled while the prefill kernel drains
+    cudaLaunchAttribute pdl[1];
+    pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    pdl[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)rblocks);
+    cfg.blockDim = dim3(256);
+    cfg.stream = stream;
+    cfg.attrs = pdl;
+    cfg.numAttrs = 1;
     uint16_t* o = static_cast<uint16_t*>(out);
-    if (g.D == 256) {
-      if (tq)
-        prefill_merge_kernel<256, true><<<(unsigned)rblocks, 256, 0, stream>>>(
-            a.part_ml, a.part_o, o, rows, num_splits, sv);
-      else
-        prefill_merge_kernel<256, false><<<(unsigned)rblocks, 256, 0, stream>>>(
-            a.part_ml, a.part_o, o, rows, num_splits, sv);
-    } else {
-      if (tq)
-        prefill_merge_kernel<128, true><<<(unsigned)rblocks, 256, 0, stream>>>(
-            a.part_ml, a.part_o, o, rows, num_splits, sv);
-      else
-        prefill_merge_kernel<128, false><<<(unsigned)rblocks, 256, 0, stream>>>(
-            a.part_ml, a.part_o, o, rows, num_splits, sv);
-    }
-    if (cudaGetLastError() != cudaSuccess) return JF_ERR_CUDA;
+    const float *ml = a.part_ml, *po = a.part_o;
+    cudaError_t e;
+    if (g.D == 256)
+      e = tq ? cudaLaunchKernelEx(&cfg, prefill_merge_kernel<256, true>, ml, po, o, rows, num_splits, sv)
+             : cudaLaunchKernelEx(&cfg, prefill_merge_kernel<256, false>, ml, po, o, rows, num_splits, sv);
+    else
+      e = tq ? cudaLaunchKernelEx(&cfg, prefill_merge_kernel<128, true>, ml, po, o, rows, num_splits, sv)
+             : cudaLaunchKernelEx(&cfg, prefill_merge_kernel<128, false>, ml, po, o, rows, num_splits, sv);
+    if (e != cudaSuccess) return JF_ERR_CUDA;
   }
   return JF_OK;
 }

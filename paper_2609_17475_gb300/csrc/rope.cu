@@ -20,9 +20,9 @@ namespace jfkv {
 
 int sm_count();
 
-constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_THREADS = 128;
 constexpr int ROPE_MAX_PAIRS = 128;
-constexpr int ROPE_MAX_TPB = 4;     // tokens per CTA
+constexpr int ROPE_MAX_TPB = 2;     // tokens per CTA
 
 struct RopeSide {
   const uint8_t* in;
@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   // places of a head: those turned, then the channels that pass through
   const int turned = ADJ ? a.R / V : half / V;
   const int steps = turned + (a.D - a.R) / V;
-  const int per = ROPE_THREADS / steps;    // pairs side by side (D <= 512: at least two)
+  const int per = ROPE_THREADS / steps;    // pairs side by side (D <= 512: at least one)
   const int h0 = threadIdx.x / steps, k = threadIdx.x - h0 * steps;
   const int hq = a.side[0].heads, heads = hq + a.side[1].heads;
   const bool turn = k < turned;
@@ -231,9 +231,10 @@ int launch_rope(const jf_rope& rope, const int32_t* positions, int64_t pos_strid
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
-  // a token a CTA while that fills the GPU no more than a few times over, more
-  // for long runs, where the cosines and the launch of a CTA weigh more
-  a.tpb = n_tokens >= 16 * sm_count() ? 4 : 1;
+  // One token a CTA, or two in long runs, where the start of a CTA weighs more
+  // (16,391 tokens of 20 heads x 128: 36.7 us with one, 33.6 with two; 2,048
+  // tokens of 28 x 256: 13.9 us with one, 17.9 with two).
+  a.tpb = n_tokens >= 16 * sm_count() ? 2 : 1;
   cfg.gridDim = dim3((unsigned)((n_tokens + a.tpb - 1) / a.tpb));
   cfg.blockDim = dim3(ROPE_THREADS);
   cfg.stream = stream;
