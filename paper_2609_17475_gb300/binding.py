@@ -137,6 +137,28 @@ def lib() -> ctypes.CDLL:
     return _lib
 
 
+_fast = None
+
+
+def _calls():
+    """The C marshalling of the calls of a step (csrc/pycall.c), set up with the library's entry points."""
+    global _fast
+    if _fast is None:
+        L = lib()
+        try:
+            from . import _jfcall
+        except ImportError as e:
+            raise RuntimeError("the binding's C part is missing: build it with __graft_entry__.build()") from e
+        at = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
+        _jfcall.setup((at(L.jf_kv8_append), at(L.jf_kv8_read), at(L.jf_rope_axes),
+                       at(L.jf_paged_decode_attn), at(L.jf_paged_decode_weights_attn),
+                       at(L.jf_kv8_evict)),
+                      (torch.int32, torch.uint8, torch.float32, torch.bfloat16, torch.float16),
+                      _raw_stream, _get_device, torch.cuda.current_stream)
+        _fast = _jfcall
+    return _fast
+
+
 def status_string(status: int) -> str:
     return lib().jf_status_string(int(status)).decode()
 
@@ -348,6 +370,12 @@ def jf_kv_quantize_append(pool: KVPool, page_table: torch.Tensor, row_req: torch
 def jf_paged_decode_attn(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Tensor,
                          q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
                          workspace: torch.Tensor, num_splits: int, stream=None) -> None:
+    if pool.codec is None:
+        st = (_fast or _calls()).decode(pool, page_table, context_lens, q, softmax_scale, out, workspace,
+                                        num_splits, stream)
+        if st:
+            raise JfError("jf_paged_decode_attn", st)
+        return
     _need(page_table, torch.int32, "page_table")
     _need(context_lens, torch.int32, "context_lens")
     _need(q, torch.bfloat16, "q")
@@ -652,9 +680,6 @@ def default_num_splits(batch: int, num_kv_heads: int, device=None,
 # ---------------------------------------------------------------------------
 # rotary positions with several axes
 # ---------------------------------------------------------------------------
-_ROPE_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
-
-
 class Rope:
     """Rotary embedding of the first ``rotary_dim`` channels of each head over one
     to three position axes (say time, height, width).
@@ -703,32 +728,7 @@ class Rope:
         for i in range(half):
             c.inv_freq[i] = float(f[i])
             c.axis[i] = int(axis[i])
-        self._ref = ctypes.byref(c)
-
-
-_NO_ROWS = _RopeRows()
-
-
-def _rope_rows(x: Optional[torch.Tensor], out: Optional[torch.Tensor], n: int, name: str):
-    if x is None:
-        return _NO_ROWS, None, 0
-    shape, xs, dtype = x.shape, x.stride(), x.dtype
-    if len(shape) != 3 or shape[0] != n:
-        raise ValueError(f"{name} must be [tokens, heads, head_dim]")
-    if dtype not in _ROPE_DTYPES or not x.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor of bf16, fp16 or fp32")
-    if out is None:
-        out, os_ = x, xs
-    else:
-        os_ = out.stride()
-        if out.shape != shape:
-            raise ValueError(f"{name}'s output must have its shape")
-        if out.dtype != dtype or not out.is_cuda:
-            raise TypeError(f"{name}'s output must be a CUDA tensor of its dtype")
-    if xs[2] != 1 or os_[2] != 1:
-        raise ValueError(f"{name}: the channels of a head must adjoin")
-    return (_RopeRows(x.data_ptr(), out.data_ptr(), xs[0], xs[1], os_[0], os_[1], shape[1]),
-            dtype, shape[2])
+        self._addr = ctypes.addressof(c)
 
 
 @_traced
@@ -738,21 +738,7 @@ def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
     """Turn query and key rows [tokens, heads, head_dim] (either may be None) by
     their positions, int32 [axes, tokens]; outputs default to in place.  With
     ``inverse`` the gradient of that: q, k are then the outputs' gradients."""
-    if not isinstance(positions, torch.Tensor) or positions.dtype is not torch.int32 or not positions.is_cuda:
-        raise TypeError("positions must be a CUDA tensor of dtype torch.int32")
-    shape, strides = positions.shape, positions.stride()
-    if len(shape) != 2 or shape[0] != rope.num_axes or (shape[1] > 1 and strides[1] != 1):
-        raise ValueError("positions must be [axes, tokens], the tokens of an axis adjoining")
-    n = shape[1]
-    qr, qt, qd = _rope_rows(q, q_out, n, "q")
-    kr, kt, kd = _rope_rows(k, k_out, n, "k")
-    if qt is None and kt is None:
-        raise ValueError("q or k is needed")
-    if qt is not None and kt is not None and (qt != kt or qd != kd):
-        raise ValueError("q and k must have one dtype and head_dim")
-    st = lib().jf_rope_axes(rope._ref, positions.data_ptr(), strides[0], n, qd or kd,
-                            ctypes.byref(qr), ctypes.byref(kr), _ROPE_DTYPES[qt or kt],
-                            1 if inverse else 0, _stream(stream))
+    st = (_fast or _calls()).rope_axes(rope._addr, positions, q, q_out, k, k_out, inverse, stream)
     if st:
         raise JfError("jf_rope_axes", st)
 
@@ -760,51 +746,15 @@ def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
 # ---------------------------------------------------------------------------
 # the 8-bit block-scaled cache
 # ---------------------------------------------------------------------------
-def _kv_rows_arg(x: torch.Tensor, name: str, hkv: int, d: int):
-    """(rows, elements between rows) of a [rows, Hkv, D] tensor whose rows may lie apart."""
-    try:
-        if x.dtype is not torch.bfloat16 or not x.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
-        shape, stride = x.shape, x.stride()
-    except AttributeError:
-        raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16") from None
-    if len(shape) != 3 or shape[1] != hkv or shape[2] != d:
-        raise ValueError(f"{name} must be [rows, Hkv, D]")
-    n = shape[0]
-    if n and (stride[2] != 1 or (hkv > 1 and stride[1] != d)):
-        raise ValueError(f"{name}: the elements of a row must adjoin")
-    # the row stride of a single row is whatever a slicing left: it is not used
-    return n, stride[0] if n > 1 else hkv * d
-
-
-def _kv8_rows(name: str, fn, pool: KVPool, page_table, start_pos, row_offsets, k, v, err_flag, stream):
-    _need(page_table, torch.int32, "page_table")
-    _need(start_pos, torch.int32, "start_pos")
-    _need(row_offsets, torch.int32, "row_offsets")
-    n, ks = _kv_rows_arg(k, "k", pool.num_kv_heads, pool.head_dim)
-    nv, vs = _kv_rows_arg(v, "v", pool.num_kv_heads, pool.head_dim)
-    shape = page_table.shape
-    B, stride = shape if len(shape) == 2 else (1, page_table.numel())
-    if n != nv:
-        raise ValueError("k and v must have the same rows")
-    if start_pos.numel() != B or row_offsets.numel() != B + 1:
-        raise ValueError("one start_pos per page-table row, and one row offset more")
-    if err_flag is not None:
-        _need(err_flag, torch.int32, "err_flag")
-        err_flag = err_flag.data_ptr()
-    st = fn(ctypes.byref(pool.c_struct()), page_table.data_ptr(), stride, B, start_pos.data_ptr(),
-            row_offsets.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, n, err_flag, _stream(stream))
-    if st:
-        raise JfError(name, st)
-
-
 @_traced
 def jf_kv8_append(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
                   row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                   err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Append rows row_offsets[b] .. row_offsets[b + 1] - 1 of k and v (bf16 [rows,
     Hkv, D], rows any stride apart) at positions start_pos[b] .. of request b."""
-    _kv8_rows("jf_kv8_append", lib().jf_kv8_append, pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    st = (_fast or _calls()).kv8_append(pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    if st:
+        raise JfError("jf_kv8_append", st)
 
 
 @_traced
@@ -812,7 +762,9 @@ def jf_kv8_read(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
                 row_offsets: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                 err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Read runs of positions back into k and v as bf16 values (exact)."""
-    _kv8_rows("jf_kv8_read", lib().jf_kv8_read, pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    st = (_fast or _calls()).kv8_read(pool, page_table, start_pos, row_offsets, k, v, err_flag, stream)
+    if st:
+        raise JfError("jf_kv8_read", st)
 
 
 def decode_weights_workspace(batch, num_q_heads, num_kv_heads, head_dim, num_splits,
@@ -835,28 +787,10 @@ def jf_paged_decode_weights_attn(pool: KVPool, page_table: torch.Tensor,
     """jf_paged_decode_attn on an 8-bit pool that also adds what each position is
     attended with, summed over a KV head's query heads, to weights_in (fp32
     [batch, Hkv, stride], None: zeros); weights_out may be weights_in."""
-    _need(page_table, torch.int32, "page_table")
-    _need(context_lens, torch.int32, "context_lens")
-    _need(q, torch.bfloat16, "q")
-    _need(out, torch.bfloat16, "out")
-    _need(weights_out, torch.float32, "weights_out")
-    _need(workspace, torch.uint8, "workspace")
-    B, Hq, D = q.shape
-    if out.shape != q.shape or D != pool.head_dim or page_table.shape[0] != B or context_lens.numel() != B:
-        raise ValueError("shape mismatch")
-    if weights_out.dim() != 3 or tuple(weights_out.shape[:2]) != (B, pool.num_kv_heads):
-        raise ValueError("weights must be [batch, Hkv, stride]")
-    if weights_in is not None:
-        _need(weights_in, torch.float32, "weights_in")
-        if weights_in.shape != weights_out.shape:
-            raise ValueError("weights_in and weights_out must have one shape")
-    st = lib().jf_paged_decode_weights_attn(
-        ctypes.byref(pool.c_struct()), page_table.data_ptr(), page_table.shape[1],
-        context_lens.data_ptr(), B, q.data_ptr(), Hq, float(softmax_scale), out.data_ptr(),
-        None if weights_in is None else weights_in.data_ptr(), weights_out.data_ptr(),
-        weights_out.shape[2], workspace.data_ptr(), workspace.numel(), int(num_splits),
-        _stream(stream))
-    _check("jf_paged_decode_weights_attn", st)
+    st = (_fast or _calls()).decode_weights(pool, page_table, context_lens, q, softmax_scale, out, weights_in,
+                                            weights_out, workspace, num_splits, stream)
+    if st:
+        raise JfError("jf_paged_decode_weights_attn", st)
 
 
 @_traced
@@ -868,29 +802,7 @@ def jf_kv8_evict(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Ten
     """Keep min(context, budget) positions of every request and KV head -- the first
     ``sinks``, the last ``recent`` and the heaviest of the others -- and move them, in
     order, to the pages of dst_page_table.  kept and dst_weights are [batch, Hkv, budget]."""
-    _need(page_table, torch.int32, "page_table")
-    _need(context_lens, torch.int32, "context_lens")
-    _need(weights, torch.float32, "weights")
-    _need(dst_page_table, torch.int32, "dst_page_table")
-    _need(dst_context_lens, torch.int32, "dst_context_lens")
-    _need(kept, torch.int32, "kept")
-    B, H = page_table.shape[0], pool.num_kv_heads
-    if context_lens.numel() != B or dst_context_lens.numel() != B or dst_page_table.dim() != 2 or dst_page_table.shape[0] != B:
-        raise ValueError("one row per request")
-    if weights.dim() != 3 or tuple(weights.shape[:2]) != (B, H):
-        raise ValueError("weights must be [batch, Hkv, stride]")
-    if tuple(kept.shape) != (B, H, int(budget)):
-        raise ValueError("kept must be [batch, Hkv, budget]")
-    if dst_weights is not None:
-        _need(dst_weights, torch.float32, "dst_weights")
-        if dst_weights.shape != kept.shape:
-            raise ValueError("dst_weights must be [batch, Hkv, budget]")
-    if err_flag is not None:
-        _need(err_flag, torch.int32, "err_flag")
-    st = lib().jf_kv8_evict(
-        ctypes.byref(pool.c_struct()), page_table.data_ptr(), page_table.shape[1],
-        context_lens.data_ptr(), B, weights.data_ptr(), weights.shape[2], int(budget), int(sinks),
-        int(recent), dst_page_table.data_ptr(), dst_page_table.shape[1],
-        dst_context_lens.data_ptr(), None if dst_weights is None else dst_weights.data_ptr(),
-        kept.data_ptr(), None if err_flag is None else err_flag.data_ptr(), _stream(stream))
-    _check("jf_kv8_evict", st)
+    st = (_fast or _calls()).kv8_evict(pool, page_table, context_lens, weights, budget, sinks, recent,
+                                       dst_page_table, dst_context_lens, dst_weights, kept, err_flag, stream)
+    if st:
+        raise JfError("jf_kv8_evict", st)

@@ -2,7 +2,9 @@
 
 Each CUDA translation unit is compiled in parallel, then linked into one
 shared library next to this file.  No CMake, no torch extension machinery:
-the library exposes a plain C ABI (include/jfkv.h).
+the library exposes a plain C ABI (include/jfkv.h).  The binding's argument
+marshalling for the calls of a step (csrc/pycall.c) is a small C extension of
+Python beside it.
 """
 from __future__ import annotations
 
@@ -10,6 +12,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -18,8 +21,10 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libjfkv.so")
+CALL = os.path.join(HERE, "_jfcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["api.cu", "append.cu", "checkpoint.cu", "decode.cu", "kv8.cu", "kv8_decode.cu",
-           "kv8_evict.cu", "kv8_prefill.cu", "prefill.cu", "rope.cu", "selftest.cu", "tq4.cu", "tq4_verify.cu", "verify.cu"]
+           "kv8_evict.cu", "kv8_prefill.cu", "prefill.cu", "rope.cu", "selftest.cu", "tq4.cu",
+           "tq4_verify.cu", "verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -40,8 +45,19 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def _compile_call() -> None:
+    cmd = [shutil.which("gcc") or shutil.which("cc") or "cc", "-O2", "-Wall", "-shared", "-fPIC",
+           "-I", sysconfig.get_paths()["include"], "-I", INCLUDE, os.path.join(CSRC, "pycall.c"),
+           "-o", CALL + ".tmp"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError(f"the C compiler failed for pycall.c:\n{p.stdout}\n{p.stderr}")
+    os.replace(CALL + ".tmp", CALL)
+
+
 def build(verbose: bool = False, extra=()) -> str:
     os.makedirs(BUILD, exist_ok=True)
+    _compile_call()
     with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
         objs = list(ex.map(lambda s: _compile(s, list(extra)), SOURCES))
     tmp = LIB + ".tmp"
