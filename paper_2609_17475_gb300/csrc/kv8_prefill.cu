@@ -72,7 +72,8 @@ struct P8Smem {
   static constexpr int OFF_BAR = OFF_S + P8_SBUF * VS_BYTES;
   static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
   static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
-  static constexpr int TOTAL = 1024 + OFF_L + 2 * PF_BM * 8;
+  static constexpr int OFF_X = OFF_L + 2 * PF_BM * 8;    // [2 groups][128] largest of half a row
+  static constexpr int TOTAL = 1024 + OFF_X + 2 * PF_BM * 4;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -92,6 +93,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   uint8_t* const sS = sm + L::OFF_S;
   float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
   float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
+  uint32_t* const s_x = reinterpret_cast<uint32_t*>(sm + L::OFF_X);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // On CTA 0, where the pair's MMAs are issued:
   uint64_t* const k_full = bars + 0;     // [3] both CTAs' K halves of a pair have landed
@@ -103,7 +105,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   uint64_t* const m_bar = bars + 17;     // [2 groups][4 quarters] the group's reference is set
   uint64_t* const s_land = bars + 25;    // [4] staged V codes have landed
   uint64_t* const s_free = bars + 29;    // [4] and been read by the 4 V warps
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 33);
+  uint64_t* const q_ready = bars + 33;   // on CTA 0: both CTAs' Q rows stored
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
@@ -138,8 +141,24 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const int ntiles = je - jb;
   const int npairs = (ntiles + 1) >> 1;
 
+  const int quarter = warp & 3;                // TMEM lanes a softmax warp may access
+  const int group = warp >= P8_SM_WARP0 + 4 ? 1 : 0;
+  const int r = quarter * 32 + lane;
+  const bool row_ok = r < rows;
+  const int qi = row_ok ? r / a.G : 0;
+  const int64_t qrow_at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
+  const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+  // each softmax group's half of a Q row, under way while the barriers are set up
+  constexpr int NQ = D / 16;
+  uint4 qv[NQ];
+  if (warp >= P8_SM_WARP0) {
+    const uint4* const src = reinterpret_cast<const uint4*>(rq.q + qrow_at * D) + group * NQ;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) qv[c] = row_ok ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+  }
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
+    mbar_init(q_ready, 2 * 2 * PF_SM_WARPS);
     for (int i = 0; i < 4; ++i) {
       mbar_init(&pv_ready[i], 2 * (4 + PF_SM_WARPS));   // 4 V and 4 softmax warps of each CTA
       mbar_init(&pv_done[i], 1);
@@ -171,41 +190,33 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 
   // ---- softmax warps: their half of a Q row as two e4m3 terms (K-major, 128-byte
   // swizzle: 16-byte piece m of row r at block m / 8, piece (m % 8) ^ (r % 8)) -------
-  const int quarter = warp & 3;                // TMEM lanes this warp may access
-  const int group = warp >= P8_SM_WARP0 + 4 ? 1 : 0;
-  const int r = quarter * 32 + lane;
-  const bool row_ok = r < rows;
-  const int qi = row_ok ? r / a.G : 0;
-  const int64_t qrow_at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
-  const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
   float smul = 0.f;                            // score = smul * S
   if (warp >= P8_SM_WARP0) {
-    const uint16_t* const qrow = rq.q + qrow_at * D;
     uint32_t mx = 0;                           // largest finite magnitude's bf16 bits
-    if (row_ok) {
-      for (int c = 0; c < D / 8; ++c) {
-        const uint4 w = *reinterpret_cast<const uint4*>(qrow + 8 * c);
-        const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
-          if (lo < 0x7F80u) mx = max(mx, lo);
-          if (hi < 0x7F80u) mx = max(mx, hi);
-        }
+    for (int c = 0; c < NQ; ++c) {
+      const uint32_t ws[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
+        if (lo < 0x7F80u) mx = max(mx, lo);
+        if (hi < 0x7F80u) mx = max(mx, hi);
       }
     }
+    s_x[group * PF_BM + r] = mx;
+    asm volatile("bar.sync 1, %0;\n" ::"n"(2 * PF_SM_WARPS * 32) : "memory");   // the two groups
+    mx = max(mx, s_x[(group ^ 1) * PF_BM + r]);
     const int qe = mx >= 0x80u ? max((int)(mx >> 7) - 127 - 7, -100) : -100;
     smul = fabsf(a.scale_log2) * two8(qe);     // the scale's sign goes to Q
     const float qs = a.scale_log2 < 0.f ? -two8(-qe) : two8(-qe);
     if (smul == 0.f) smul = 1.f;               // a zero scale: zero scores
     const bool zero = a.scale_log2 == 0.f;
-#pragma unroll 2
+#pragma unroll
     for (int mm = 0; mm < D / 32; ++mm) {
       const int m = group * (D / 32) + mm;     // this group's half of the row
       uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
-      if (row_ok && !zero) {
-        const uint4 w0 = *reinterpret_cast<const uint4*>(qrow + 16 * m);
-        const uint4 w1 = *reinterpret_cast<const uint4*>(qrow + 16 * m + 8);
+      if (!zero) {
+        const uint4 w0 = qv[2 * mm], w1 = qv[2 * mm + 1];
         const uint32_t ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
@@ -224,11 +235,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       *reinterpret_cast<uint4*>(at + L::Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
     fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) tc::arrive_cluster(q_ready, 0);
   }
-  tc::fence_before();
-  __syncthreads();
-  tc::cluster_sync();   // both CTAs' Q rows are in shared memory before the first MMA
-  tc::fence_after();
 
   float m_own = -INFINITY, l = 0.f;   // softmax: the reference at this group's last tile
   bool ok = true;
@@ -250,6 +259,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // otherwise: position 32 rank + n % 32 of tile 2i + (n % 64) / 32), then P V of
       // the previous pair's tiles
       int jn = 0;   // next tile whose P V is due
+      ok = wait(q_ready, 0);
       for (int i = 0; i <= npairs && ok; ++i) {
         if (i < npairs) {
           const int kb = i % P8_KBUF;
