@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "prefill.cuh"
 #include "tq4.cuh"
 
 namespace jfkv {
@@ -34,7 +35,7 @@ int launch_prefill(const Geom&, const jf_kv_pool&, const CUtensorMap&, const int
 int launch_prefill_batch(const Geom&, const jf_kv_pool&, const int32_t* const*, const int32_t*,
                          const int32_t*, const void*, const int64_t*, int32_t, int32_t, float,
                          int32_t, void*, void*, cudaStream_t, int32_t, int64_t,
-                         const Tq4Params*);
+                         const Tq4Params*, const P8Plan* plan = nullptr);
 size_t prefill_workspace_bytes(int64_t rows, int64_t Hq, int64_t D, int64_t S, int fmt);
 int launch_rope(const jf_rope&, const int32_t*, int64_t, int32_t, int32_t, const jf_rope_rows&,
                 const jf_rope_rows&, int32_t, int32_t, cudaStream_t);
@@ -383,6 +384,18 @@ size_t jf_prefill_chunk_workspace_bytes(const jf_kv_pool* pool, int32_t q_start,
   const size_t one = tq ? prefill_workspace_bytes(chunk_len, num_q_heads, pool->head_dim, 1,
                                                   JF_FMT_TQ4)
                         : jf_prefill_workspace_bytes();
+  if (pool->format == JF_FMT_E4M3_B32) {
+    size_t bytes = one;
+    for (int causal = 0; causal < 2; ++causal) {
+      P8Plan plan;
+      kv8_prefill_plan(num_q_heads / pool->num_kv_heads, pool->num_kv_heads, q_start, chunk_len,
+                       causal != 0, num_sms ? num_sms : sm_count(), &plan);
+      const size_t n = prefill_workspace_bytes(plan.rows, num_q_heads, pool->head_dim, plan.k,
+                                               pool->format);
+      if (plan.n && n > bytes) bytes = n;
+    }
+    return bytes;
+  }
   const PfTailPlan p = prefill_tail_plan(num_q_heads / pool->num_kv_heads, pool->num_kv_heads,
                                          q_start, chunk_len, num_sms ? num_sms : sm_count());
   if (p.k == 1) return one;
@@ -419,6 +432,18 @@ int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
   }
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   const int64_t row0 = 0;
+  if (pool->format == JF_FMT_E4M3_B32) {
+    P8Plan plan;
+    kv8_prefill_plan(num_q_heads / pool->num_kv_heads, pool->num_kv_heads, q_start, chunk_len,
+                     causal != 0, sm_count(), &plan);
+    const bool planned =
+        plan.n > 0 && aligned(workspace, 256) &&
+        workspace_bytes >= prefill_workspace_bytes(plan.rows, num_q_heads, g.D, plan.k, pool->format);
+    return launch_prefill_batch(g, *pool, &page_table_row, &q_start, &chunk_len, q, &row0, 1,
+                                num_q_heads, softmax_scale, causal, out, workspace, s,
+                                planned ? plan.k : 1, planned ? plan.rows : chunk_len, nullptr,
+                                planned ? &plan : nullptr);
+  }
   const PfTailPlan p = prefill_tail_plan(num_q_heads / pool->num_kv_heads, pool->num_kv_heads,
                                          q_start, chunk_len, sm_count());
   if (p.k > 1 && aligned(workspace, 256) &&

@@ -77,9 +77,15 @@ struct P8Smem {
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
-template <int D>
+struct P8NoPlan {};
+template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
+template <> struct P8PlanArg<false> { using type = P8NoPlan; };
+
+// PLAN: whole pairs, then the plan's parts; otherwise gridDim.z ranges of every pair.
+template <int D, bool PLAN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
-kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ PrefillArgs a) {
+kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ PrefillArgs a,
+                   const __grid_constant__ typename P8PlanArg<PLAN>::type plan) {
   using L = P8Smem<D>;
   constexpr uint32_t IDQK = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
   constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
@@ -113,7 +119,20 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const uint32_t rank = tc::cluster_rank();
   // CTA pairs in launch order, as in prefill.cu: the KV heads of a pair of query
   // tiles are consecutive, latest (longest) tiles first
-  const int pair = (int)(blockIdx.x >> 1);
+  int pair = (int)(blockIdx.x >> 1), z = (int)blockIdx.z;
+  bool split = a.num_splits > 1;
+  int f0 = 0, f1 = 0, last = 0;
+  if constexpr (PLAN) {
+    split = pair >= plan.whole;
+    if (split) {
+      const P8Seg& sg = plan.seg[pair - plan.whole];
+      pair = sg.pair;
+      z = sg.z;
+      f0 = sg.f0;
+      f1 = sg.f1;
+      last = sg.last;
+    }
+  }
   const int kvh = pair % a.Hkv;
   const int tile = (pair / a.Hkv) * 2 + (int)(blockIdx.x & 1);
   int ri = 0;
@@ -136,8 +155,14 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   };
   const int kmax_pair = max(kmax_of(qt), kmax_of(qt_partner));
   const int ntiles_all = (kmax_pair + PF_BN - 1) / PF_BN;
-  const int jb = (int)(((int64_t)ntiles_all * blockIdx.z) / a.num_splits);
-  const int je = (int)(((int64_t)ntiles_all * (blockIdx.z + 1)) / a.num_splits);
+  int jb = 0, je = ntiles_all;
+  if (PLAN && split) {
+    jb = (int)(((int64_t)ntiles_all * f0) >> 15);
+    je = (int)(((int64_t)ntiles_all * f1) >> 15);
+  } else if (split) {
+    jb = (int)(((int64_t)ntiles_all * z) / a.num_splits);
+    je = (int)(((int64_t)ntiles_all * (z + 1)) / a.num_splits);
+  }
   const int ntiles = je - jb;
   const int npairs = (ntiles + 1) >> 1;
 
@@ -148,14 +173,6 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const int qi = row_ok ? r / a.G : 0;
   const int64_t qrow_at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
   const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-  // each softmax group's half of a Q row, under way while the barriers are set up
-  constexpr int NQ = D / 16;
-  uint4 qv[NQ];
-  if (warp >= P8_SM_WARP0) {
-    const uint4* const src = reinterpret_cast<const uint4*>(rq.q + qrow_at * D) + group * NQ;
-#pragma unroll
-    for (int c = 0; c < NQ; ++c) qv[c] = row_ok ? src[c] : make_uint4(0u, 0u, 0u, 0u);
-  }
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
     mbar_init(q_ready, 2 * 2 * PF_SM_WARPS);
@@ -175,6 +192,15 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     fence_barrier_init();
   }
   if (warp == 0) tc::alloc2(tmem_slot, 512);
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
+  // each softmax group's half of a Q row, under way while the CTAs meet
+  constexpr int NQ = D / 16;
+  uint4 qv[NQ];
+  if (warp >= P8_SM_WARP0) {
+    const uint4* const src = reinterpret_cast<const uint4*>(rq.q + qrow_at * D) + group * NQ;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) qv[c] = row_ok ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+  }
   tc::fence_before();
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
@@ -532,8 +558,12 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const bool all_ok = !__syncthreads_or(!ok);
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");   // the merge waits for the rest
   if (warp >= P8_SM_WARP0) {
-    const bool split = a.num_splits > 1;
-    const int64_t prow = ((int64_t)rq.row0 * a.Hq + qrow_at) * a.num_splits + blockIdx.z;
+    const int64_t prow = ((int64_t)rq.row0 * a.Hq + qrow_at) * a.num_splits + z;
+    if (PLAN && last && row_ok && group == 0)   // the pair's unused partials: neutral
+      for (int u = 1; z + u < a.num_splits; ++u) {
+        a.part_ml[(prow + u) * 2 + 0] = -INFINITY;
+        a.part_ml[(prow + u) * 2 + 1] = 0.f;
+      }
     float* const po = a.part_o + prow * D + group * (D / 2);
     if (ntiles == 0) {   // an empty history range: a neutral partial
       if (split && row_ok) {
@@ -597,21 +627,104 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   }
 }
 
-template <int D>
-static int launch_t(const CUtensorMap& kmap, const PrefillArgs& a, const dim3& grid,
-                    cudaStream_t stream) {
-  if (smem_optin((const void*)kv8_prefill_kernel<D>, P8Smem<D>::TOTAL) != JF_OK) return JF_ERR_CUDA;
-  kv8_prefill_kernel<D><<<grid, P8_THREADS, P8Smem<D>::TOTAL, stream>>>(kmap, a);
-  return cudaGetLastError() == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+// The plan's estimate, in history tiles (0.8 us each at D = 256): a part beyond a
+// place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
+// merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
+// queries after 30,720 positions (44 of 196 pairs left over): one launch more with three
+// even splits 1,163 us, the plan TIMES.
+constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
+
+void kv8_prefill_plan(int64_t G, int64_t Hkv, int64_t q_start, int64_t chunk_len, bool causal,
+                      int64_t num_sms, P8Plan* plan) {
+  plan->whole = plan->n = plan->rows = 0;
+  plan->k = 1;
+  if (G < 1 || G > PF_BM || Hkv < 1 || num_sms < 2 || chunk_len < 1 || q_start < 4 * chunk_len)
+    return;   // pairs of unlike lengths already end one after the other
+  const int64_t slots = num_sms / 2 < P8_MAX_SEG / 2 ? num_sms / 2 : P8_MAX_SEG / 2;
+  const int64_t qpp = 2 * (PF_BM / G);                  // queries per CTA pair
+  const int64_t pph = (chunk_len + qpp - 1) / qpp;      // pairs per KV head
+  const int64_t pairs = pph * Hkv, rem = pairs % slots;
+  if (pairs <= slots || rem == 0 || pairs > 0xFFFF) return;
+  const int64_t t_tail = (rem + Hkv - 1) / Hkv, tail = t_tail * Hkv;
+  if (t_tail >= pph || tail > slots) return;
+  // pair p of the launch order holds query tiles pph - 1 - p / Hkv of its head
+  auto tiles_of = [&](int64_t p) {
+    const int64_t q = (pph - p / Hkv) * qpp;
+    const int64_t seen = causal ? q_start + (q < chunk_len ? q : chunk_len) : q_start + chunk_len;
+    return (seen + PF_BN - 1) / PF_BN;
+  };
+  const int64_t first = pairs - tail;
+  int64_t total = 0;
+  for (int64_t p = first; p < pairs; ++p) total += tiles_of(p) + P8_HDR;
+  int64_t width = (total + slots - 1) / slots;
+  if (width < P8_MIN_PIECE + P8_HDR) width = P8_MIN_PIECE + P8_HDR;
+  if (width + P8_MERGE >= tiles_of(first)) return;
+  int n = 0, k = 1;
+  int64_t len[P8_MAX_SEG];
+  int64_t at = 0;   // where the pair's run (header, then tiles) begins
+  for (int64_t p = first; p < pairs; ++p) {
+    const int64_t nt = tiles_of(p), end = at + P8_HDR + nt;
+    int64_t t0 = 0;
+    int z = 0;
+    while (t0 < nt) {
+      // up to the next cut; what is shorter than a header is not worth a part
+      const int64_t here = at + P8_HDR + t0;
+      int64_t cut = (here / width + 1) * width;
+      if (cut - here < P8_HDR) cut += width;
+      const int64_t t1 = end - cut < P8_HDR ? nt : cut - at - P8_HDR;
+      if (n == P8_MAX_SEG || z == 255) return;
+      int i = n++;
+      for (; i > 0 && len[i - 1] < t1 - t0; --i) {   // longest first
+        len[i] = len[i - 1];
+        plan->seg[i] = plan->seg[i - 1];
+      }
+      len[i] = t1 - t0;
+      plan->seg[i] = P8Seg{(uint16_t)p, (uint8_t)z, (uint8_t)(t1 == nt),
+                           (uint16_t)((t0 * 32768 + nt - 1) / nt),
+                           (uint16_t)(t1 == nt ? 32768 : (t1 * 32768 + nt - 1) / nt)};
+      ++z;
+      t0 = t1;
+    }
+    if (z > k) k = z;
+    at = end;
+  }
+  plan->whole = (int32_t)first;
+  plan->rows = (int32_t)(t_tail * qpp);
+  plan->k = k;
+  plan->n = n;
 }
 
-int launch_kv8_prefill(const Geom& g, const jf_kv_pool& pool, const PrefillArgs& a, unsigned ctas,
-                       unsigned splits, cudaStream_t stream) {
+template <int D, bool PLAN>
+static int launch_t(const CUtensorMap& kmap, const PrefillArgs& a,
+                    const typename P8PlanArg<PLAN>::type& plan, const dim3& grid,
+                    cudaStream_t stream) {
+  const auto kernel = kv8_prefill_kernel<D, PLAN>;
+  if (smem_optin((const void*)kernel, P8Smem<D>::TOTAL) != JF_OK) return JF_ERR_CUDA;
+  // programmatic dependent launch: barriers and TMEM are set up while the kernel before drains
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(P8_THREADS);
+  cfg.dynamicSmemBytes = P8Smem<D>::TOTAL;
+  cfg.stream = stream;
+  cfg.attrs = pdl;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, kmap, a, plan) == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+}
+
+int launch_kv8_prefill(const Geom& g, const jf_kv_pool& pool, const PrefillArgs& a,
+                       const P8Plan* plan, unsigned ctas, unsigned splits, cudaStream_t stream) {
   CUtensorMap kmap;
   const int st = kv8_tensor_map(g, pool.base, 1, 32, 1, &kmap);
   if (st) return st;
   const dim3 grid(ctas, 1u, splits);
-  return g.D == 256 ? launch_t<256>(kmap, a, grid, stream) : launch_t<128>(kmap, a, grid, stream);
+  if (plan)
+    return g.D == 256 ? launch_t<256, true>(kmap, a, *plan, grid, stream)
+                      : launch_t<128, true>(kmap, a, *plan, grid, stream);
+  return g.D == 256 ? launch_t<256, false>(kmap, a, P8NoPlan{}, grid, stream)
+                    : launch_t<128, false>(kmap, a, P8NoPlan{}, grid, stream);
 }
 
 }  // namespace jfkv

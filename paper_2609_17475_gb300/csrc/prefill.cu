@@ -753,12 +753,14 @@ static int launch_pf(const dim3& grid, const PrefillArgs& a, cudaStream_t stream
 
 // One launch over the chunks of `nreq` requests (nreq <= PF_MAX_REQ); requests
 // with an empty chunk get no CTAs.  The request with the most attended
-// positions goes first, so the longest CTA pairs start earliest.
+// positions goes first, so the longest CTA pairs start earliest.  plan (one
+// request over an 8-bit pool): its partials are total_rows rows, the chunk's first.
 int launch_prefill_batch(const Geom& g, const jf_kv_pool& pool, const int32_t* const* pt_rows,
                          const int32_t* q_start, const int32_t* chunk_len, const void* q,
                          const int64_t* q_row0, int32_t nreq, int32_t Hq, float softmax_scale,
                          int32_t causal, void* out, void* workspace, cudaStream_t stream,
-                         int32_t num_splits, int64_t total_rows, const Tq4Params* tq4) {
+                         int32_t num_splits, int64_t total_rows, const Tq4Params* tq4,
+                         const P8Plan* plan) {
   if (nreq < 1 || nreq > PF_MAX_REQ) return JF_ERR_UNSUPPORTED;
   const bool tq = tq4 != nullptr;
   if (num_splits < 1 || num_splits > 65535) return JF_ERR_INVALID_ARG;
@@ -839,7 +841,8 @@ int launch_prefill_batch(const Geom& g, const jf_kv_pool& pool, const int32_t* c
   }
   int st;
   if (pool.format == JF_FMT_E4M3_B32)
-    st = launch_kv8_prefill(g, pool, a, grid.x, grid.z, stream);
+    st = launch_kv8_prefill(g, pool, a, plan, plan ? 2u * (plan->whole + plan->n) : grid.x,
+                            plan ? 1u : grid.z, stream);
   else if (g.D == 256)
     st = tq ? launch_pf<256, JF_FMT_TQ4>(grid, a, stream)
             : launch_pf<256, JF_FMT_AFFINE4_G64>(grid, a, stream);
@@ -879,7 +882,7 @@ int launch_prefill(const Geom& g, const jf_kv_pool& pool, const CUtensorMap&,
   const int64_t row0 = 0;
   return launch_prefill_batch(g, pool, &page_table_row, &q_start, &chunk_len, q, &row0, 1, Hq,
                               softmax_scale, causal, out, workspace, stream, 1, chunk_len,
-                              nullptr);
+                              nullptr, nullptr);
 }
 
 }  // namespace jfkv

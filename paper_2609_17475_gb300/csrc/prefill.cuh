@@ -43,9 +43,32 @@ struct PrefillArgs {
   PfReq req[PF_MAX_REQ];
 };
 
-// One launch over an 8-bit pool (kv8_prefill.cu): ctas CTAs, splits history ranges.
-int launch_kv8_prefill(const Geom& g, const jf_kv_pool& pool, const PrefillArgs& a, unsigned ctas,
-                       unsigned splits, cudaStream_t stream);
+// Wave balance of one chunk over an 8-bit pool (kv8_prefill.cu).  CTA pairs run
+// num_sms / 2 at a time; the pairs that fill whole waves run as they are, and the
+// histories of the `tail` pairs left over, laid end to end, are cut into one piece
+// per place, so that the last wave ends everywhere at once.  seg: the pieces' parts
+// that belong to one pair, longest first (a place that gets a short part is free
+// early and takes the rest of another).
+constexpr int P8_MAX_SEG = 192;
+struct P8Seg {
+  uint16_t pair;        // in launch order
+  uint8_t z, last;      // its partial row; whether the pair's later ones are unused
+  uint16_t f0, f1;      // history range, in units of 1 / 32768 of the pair's tiles
+};
+struct P8Plan {
+  int32_t whole;        // pairs run whole
+  int32_t n;            // parts of the others (0: no plan)
+  int32_t rows;         // queries of the others: the first of the chunk
+  int32_t k;            // partial rows per query and head
+  P8Seg seg[P8_MAX_SEG];
+};
+void kv8_prefill_plan(int64_t G, int64_t Hkv, int64_t q_start, int64_t chunk_len, bool causal,
+                      int64_t num_sms, P8Plan* plan);
+
+// One launch over an 8-bit pool (kv8_prefill.cu): ctas CTAs, splits history ranges,
+// or those of a plan.
+int launch_kv8_prefill(const Geom& g, const jf_kv_pool& pool, const PrefillArgs& a,
+                       const P8Plan* plan, unsigned ctas, unsigned splits, cudaStream_t stream);
 
 // packed fp32 pairs (Blackwell f32x2 arithmetic)
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
