@@ -72,10 +72,29 @@ struct P8Smem {
   static constexpr int OFF_BAR = OFF_S + P8_SBUF * VS_BYTES;
   static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
   static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
-  static constexpr int OFF_X = OFF_L + 2 * PF_BM * 8;    // [2 groups][128] largest of half a row
-  static constexpr int TOTAL = 1024 + OFF_X + 2 * PF_BM * 4;
+  static constexpr int OFF_X = OFF_L + 2 * PF_BM * 8;    // [128] largest magnitude of a Q row
+  static constexpr int TOTAL = 1024 + OFF_X + PF_BM * 4;
+  // at the end O's rows pass through what held Q, K and V on their way out
+  static_assert(PF_BM * D * 4 <= OFF_BAR, "O rows");
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
+
+// exponent of a Q row whose largest magnitude has the bf16 bits mx: mx 2^-e in [2^7, 2^8)
+__device__ __forceinline__ int q_exp(uint32_t mx) {
+  return mx >= 0x80u ? max((int)(mx >> 7) - 127 - 7, -100) : -100;
+}
+
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t x, uint32_t y, uint32_t z,
+                                             uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n"
+               ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
 
 struct P8NoPlan {};
 template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
@@ -193,13 +212,24 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   }
   if (warp == 0) tc::alloc2(tmem_slot, 512);
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
-  // each softmax group's half of a Q row, under way while the CTAs meet
-  constexpr int NQ = D / 16;
-  uint4 qv[NQ];
+  // 16 Q rows to a softmax warp, a whole row (two at D = 128) per load, under way while
+  // the CTAs meet
+  constexpr int LPR = D / 8;                   // lanes of a row, 8 elements each
+  constexpr int RPI = 32 / LPR, NI = 16 / RPI;
+  const int qpiece = lane % LPR;
+  const int qr0 = (warp - P8_SM_WARP0) * 16 + lane / LPR;
+  uint4 qv[NI];
   if (warp >= P8_SM_WARP0) {
-    const uint4* const src = reinterpret_cast<const uint4*>(rq.q + qrow_at * D) + group * NQ;
+    const uint32_t inv = (65535u + a.G) / (uint32_t)a.G;   // row / G = row * inv >> 16 below 128
+    const uint16_t* const src = rq.q + ((int64_t)q0 * a.Hq + kvh * a.G) * D + qpiece * 8;
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) qv[c] = row_ok ? src[c] : make_uint4(0u, 0u, 0u, 0u);
+    for (int i = 0; i < NI; ++i) {
+      const int row = qr0 + i * RPI;
+      const int at = (int)((uint32_t)row * inv >> 16);
+      qv[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < rows)
+        qv[i] = *reinterpret_cast<const uint4*>(src + ((int64_t)at * a.Hq + (row - at * a.G)) * D);
+    }
   }
   tc::fence_before();
   __syncthreads();
@@ -214,38 +244,33 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     return j < ntiles ? __ldg(pt + (((jb + j) * PF_BN) >> log2P)) : -1;
   };
 
-  // ---- softmax warps: their half of a Q row as two e4m3 terms (K-major, 128-byte
-  // swizzle: 16-byte piece m of row r at block m / 8, piece (m % 8) ^ (r % 8)) -------
+  // ---- softmax warps: Q rows as two e4m3 terms (K-major, 128-byte swizzle: 16-byte
+  // piece m of row r at block m / 8, piece (m % 8) ^ (r % 8)) -------------------------
   float smul = 0.f;                            // score = smul * S
   if (warp >= P8_SM_WARP0) {
-    uint32_t mx = 0;                           // largest finite magnitude's bf16 bits
+    const bool zero = a.scale_log2 == 0.f;     // zero scores
+    uint8_t* const at = sQ + (qpiece >> 4) * (PF_BM * 128) + (qpiece & 1) * 8;
+    const int m7 = (qpiece >> 1) & 7;
 #pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-      const uint32_t ws[4] = {qv[c].x, qv[c].y, qv[c].z, qv[c].w};
+    for (int i = 0; i < NI; ++i) {
+      const int row = qr0 + i * RPI;
+      const uint32_t ws[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
+      uint32_t mx = 0;                         // largest finite magnitude's bf16 bits
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
         if (lo < 0x7F80u) mx = max(mx, lo);
         if (hi < 0x7F80u) mx = max(mx, hi);
       }
-    }
-    s_x[group * PF_BM + r] = mx;
-    asm volatile("bar.sync 1, %0;\n" ::"n"(2 * PF_SM_WARPS * 32) : "memory");   // the two groups
-    mx = max(mx, s_x[(group ^ 1) * PF_BM + r]);
-    const int qe = mx >= 0x80u ? max((int)(mx >> 7) - 127 - 7, -100) : -100;
-    smul = fabsf(a.scale_log2) * two8(qe);     // the scale's sign goes to Q
-    const float qs = a.scale_log2 < 0.f ? -two8(-qe) : two8(-qe);
-    if (smul == 0.f) smul = 1.f;               // a zero scale: zero scores
-    const bool zero = a.scale_log2 == 0.f;
 #pragma unroll
-    for (int mm = 0; mm < D / 32; ++mm) {
-      const int m = group * (D / 32) + mm;     // this group's half of the row
-      uint32_t hi[4] = {0u, 0u, 0u, 0u}, lo[4] = {0u, 0u, 0u, 0u};
+      for (int o = LPR / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      if (qpiece == 0) s_x[row] = mx;
+      float qs = two8(-q_exp(mx));
+      if (a.scale_log2 < 0.f) qs = -qs;        // the scale's sign goes to Q
+      uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
       if (!zero) {
-        const uint4 w0 = qv[2 * mm], w1 = qv[2 * mm + 1];
-        const uint32_t ws[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < 4; ++k) {
           const float x0 = bf16lo_to_f32(ws[k]) * qs, x1 = bf16hi_to_f32(ws[k]) * qs;
           const uint32_t h = e4m3x2(x0, x1);
           uint32_t f, unused;
@@ -256,13 +281,16 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           lo[k >> 1] |= l << (16 * (k & 1));
         }
       }
-      uint8_t* const at = sQ + (m >> 3) * (PF_BM * 128) + r * 128 + (((m & 7) ^ (r & 7)) << 4);
-      *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      *reinterpret_cast<uint4*>(at + L::Q_BYTES) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      uint8_t* const to = at + row * 128 + ((m7 ^ (row & 7)) << 4);
+      *reinterpret_cast<uint2*>(to) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(to + L::Q_BYTES) = make_uint2(lo[0], lo[1]);
     }
     fence_proxy_async_smem();
     __syncwarp();
     if (lane == 0) tc::arrive_cluster(q_ready, 0);
+    asm volatile("bar.sync 1, %0;\n" ::"n"(2 * PF_SM_WARPS * 32) : "memory");   // s_x
+    smul = fabsf(a.scale_log2) * two8(q_exp(s_x[r]));
+    if (smul == 0.f) smul = 1.f;
   }
 
   float m_own = -INFINITY, l = 0.f;   // softmax: the reference at this group's last tile
@@ -390,9 +418,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       uint4 c[NLD];
 #pragma unroll
       for (int u = 0; u < NLD; ++u)
-        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
-                     : "=r"(c[u].x), "=r"(c[u].y), "=r"(c[u].z), "=r"(c[u].w)
-                     : "r"(src + sb * L::VS_BYTES + (((code0 + u) ^ (t & 7)) << 4)));
+        c[u] = ld_shared_v4(src + sb * L::VS_BYTES + (((code0 + u) ^ (t & 7)) << 4));
       if ((jb + j) * PF_BN + t >= kmax_pair) {   // a slot no query sees: whatever it holds
 #pragma unroll
         for (int u = 0; u < NLD; ++u) c[u] = make_uint4(0u, 0u, 0u, 0u);
@@ -564,18 +590,18 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         a.part_ml[(prow + u) * 2 + 0] = -INFINITY;
         a.part_ml[(prow + u) * 2 + 1] = 0.f;
       }
-    float* const po = a.part_o + prow * D + group * (D / 2);
     if (ntiles == 0) {   // an empty history range: a neutral partial
       if (split && row_ok) {
         if (group == 0) {
           a.part_ml[prow * 2 + 0] = -INFINITY;
           a.part_ml[prow * 2 + 1] = 0.f;
         }
-        for (int c = 0; c < D / 8; ++c)
-          reinterpret_cast<float4*>(po)[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4* const po = reinterpret_cast<float4*>(a.part_o + prow * D + group * (D / 2));
+        for (int c = 0; c < D / 8; ++c) po[c] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
-    } else if (all_ok && mbar_wait_bounded(&pv_done[(ntiles - 1) % PF_KVBUF],
-                                          ((ntiles - 1) / PF_KVBUF) & 1)) {
+    } else if (all_ok &&
+               __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(ntiles - 1) % PF_KVBUF],
+                                                         ((ntiles - 1) / PF_KVBUF) & 1))) {
       tc::fence_after();
       const float m = s_m[r];   // after the last tile
       float lsum = 0.f;
@@ -589,18 +615,22 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         a.part_ml[prow * 2 + 1] = lsum;
       }
       const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
-      uint16_t* const orow = rq.out + qrow_at * D + group * (D / 2);
+      // The warp's 32 half rows go through shared memory (16-byte piece p of row r at
+      // p ^ (r & 7)), so that a store writes whole lines; a row per thread took 3 us.
+      const uint32_t tr = smem_u32(sm) + (warp - P8_SM_WARP0) * (32 * (D / 2) * 4);
+      const int lg = (D == 256 ? 4 : 3) + (split ? 1 : 0);   // 2^lg 16-byte pieces a half row
+      const uint32_t mine = tr + (lane << (lg + 4));
 #pragma unroll 1
       for (int c0 = 0; c0 < D / 2; c0 += 32) {
         uint32_t o[32];
         tc::ld32(tO + group * (D / 2) + c0 + lane_off, o);
         tc::wait_ld();
-        if (row_ok && split) {
+        if (split) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            reinterpret_cast<uint4*>(po + c0)[k] =
-                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
-        } else if (row_ok) {
+            st_shared_v4(mine + (((c0 / 4 + k) ^ (lane & 7)) << 4), o[4 * k], o[4 * k + 1],
+                         o[4 * k + 2], o[4 * k + 3]);
+        } else {
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             uint32_t w[4];
@@ -608,9 +638,22 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             for (int i = 0; i < 4; ++i)
               w[i] = pack_bf16x2_rn(__uint_as_float(o[8 * k + 2 * i]) * inv,
                                     __uint_as_float(o[8 * k + 2 * i + 1]) * inv);
-            *reinterpret_cast<uint4*>(orow + c0 + 8 * k) = make_uint4(w[0], w[1], w[2], w[3]);
+            st_shared_v4(mine + (((c0 / 8 + k) ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
           }
         }
+      }
+      __syncwarp();
+      const int64_t row_at = split ? prow : qrow_at;
+      const int row_bytes = split ? D * 4 : D * 2;
+      uint8_t* const to = (split ? reinterpret_cast<uint8_t*>(a.part_o)
+                                 : reinterpret_cast<uint8_t*>(rq.out)) + group * (row_bytes / 2);
+#pragma unroll 4
+      for (int i = lane; i < 32 << lg; i += 32) {
+        const int row = i >> lg, piece = i & ((1 << lg) - 1);
+        const int64_t dst = __shfl_sync(0xffffffffu, row_at, row);
+        const uint4 v = ld_shared_v4(tr + (row << (lg + 4)) + ((piece ^ (row & 7)) << 4));
+        if (quarter * 32 + row < rows)
+          *reinterpret_cast<uint4*>(to + dst * row_bytes + piece * 16) = v;
       }
     } else if (all_ok && lane == 0) {
       flag_error(a.status, JF_DEV_ERR_TIMEOUT);
