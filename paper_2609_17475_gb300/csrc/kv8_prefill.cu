@@ -96,6 +96,38 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t x, uint32_t
                ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// largest x of the LPR lanes that hold a row
+template <int LPR>
+__device__ __forceinline__ uint32_t row_max(uint32_t x) {
+  if (LPR == 32) return __reduce_max_sync(0xffffffffu, x);
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+// bf16 bits of the largest finite magnitude of a row (rows that hold infinities or NaN)
+template <int LPR>
+__device__ __noinline__ uint32_t finite_max(uint4 w) {
+  uint32_t mx = 0;
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
+    if (lo < 0x7F80u) mx = max(mx, lo);
+    if (hi < 0x7F80u) mx = max(mx, hi);
+  }
+  return row_max<LPR>(mx);
+}
+
 struct P8NoPlan {};
 template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
 template <> struct P8PlanArg<false> { using type = P8NoPlan; };
@@ -255,30 +287,27 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     for (int i = 0; i < NI; ++i) {
       const int row = qr0 + i * RPI;
       const uint32_t ws[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-      uint32_t mx = 0;                         // largest finite magnitude's bf16 bits
+      uint32_t m2 = 0;                         // largest magnitudes, NaN apart
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
-        if (lo < 0x7F80u) mx = max(mx, lo);
-        if (hi < 0x7F80u) mx = max(mx, hi);
-      }
-#pragma unroll
-      for (int o = LPR / 2; o > 0; o >>= 1) mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      for (int k = 0; k < 4; ++k) m2 = max_bf16x2(m2, ws[k] & 0x7FFF7FFFu);
+      uint32_t mx = row_max<LPR>(max(m2 & 0xFFFFu, m2 >> 16));
+      if (__any_sync(0xffffffffu, mx >= 0x7F80u)) mx = finite_max<LPR>(qv[i]);
       if (qpiece == 0) s_x[row] = mx;
       float qs = two8(-q_exp(mx));
       if (a.scale_log2 < 0.f) qs = -qs;        // the scale's sign goes to Q
       uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
       if (!zero) {
+        // by way of fp16, which holds what e4m3 does not round to 0 (2^-10) exactly
+        uint32_t f[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float x0 = bf16lo_to_f32(ws[k]) * qs, x1 = bf16hi_to_f32(ws[k]) * qs;
-          const uint32_t h = e4m3x2(x0, x1);
-          uint32_t f, unused;
-          f16x4_of_e4m3(h, f, unused);
-          const float2 hf = f32x2_of_f16x2(f);
-          const uint32_t l = e4m3x2(x0 - hf.x, x1 - hf.y);
-          hi[k >> 1] |= h << (16 * (k & 1));
-          lo[k >> 1] |= l << (16 * (k & 1));
+        for (int k = 0; k < 4; ++k)
+          f[k] = pack_f16x2(bf16lo_to_f32(ws[k]) * qs, bf16hi_to_f32(ws[k]) * qs);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          hi[k] = e4m3x4_of_f16x2(f[2 * k], f[2 * k + 1]);
+          uint32_t h0, h1;
+          f16x4_of_e4m3(hi[k], h0, h1);
+          lo[k] = e4m3x4_of_f16x2(sub_f16x2(f[2 * k], h0), sub_f16x2(f[2 * k + 1], h1));
         }
       }
       uint8_t* const to = at + row * 128 + ((m7 ^ (row & 7)) << 4);
