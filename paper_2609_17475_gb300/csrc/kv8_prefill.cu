@@ -58,6 +58,15 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
+// Where a CTA's results go, kept in shared memory with the rows' places so that the
+// softmax loop holds none of it in registers (1,596 queries after 30,720 positions
+// 774 us with it there, now 760).
+struct P8Out {
+  uint8_t* to;          // the output, or the partials O
+  int32_t split;
+  int32_t unused;       // partial rows after this one that no part of the plan writes
+};
+
 template <int D>
 struct P8Smem {
   static constexpr int NB = D / 128;                     // 128-byte blocks of a row
@@ -73,7 +82,9 @@ struct P8Smem {
   static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
   static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
   static constexpr int OFF_X = OFF_L + 2 * PF_BM * 8;    // [128] largest magnitude of a Q row
-  static constexpr int TOTAL = 1024 + OFF_X + PF_BM * 4;
+  static constexpr int OFF_R = OFF_X + PF_BM * 4;        // [128] output row, -1: none
+  static constexpr int OFF_OUT = OFF_R + PF_BM * 8;      // P8Out
+  static constexpr int TOTAL = 1024 + OFF_OUT + 16;
   // at the end O's rows pass through what held Q, K and V on their way out
   static_assert(PF_BM * D * 4 <= OFF_BAR, "O rows");
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
@@ -150,6 +161,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   uint8_t* const sS = sm + L::OFF_S;
   float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
   float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
+  int64_t* const s_row = reinterpret_cast<int64_t*>(sm + L::OFF_R);
+  P8Out* const s_out = reinterpret_cast<P8Out*>(sm + L::OFF_OUT);
   uint32_t* const s_x = reinterpret_cast<uint32_t*>(sm + L::OFF_X);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // On CTA 0, where the pair's MMAs are issued:
@@ -222,7 +235,13 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const int r = quarter * 32 + lane;
   const bool row_ok = r < rows;
   const int qi = row_ok ? r / a.G : 0;
-  const int64_t qrow_at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
+  if (warp >= P8_SM_WARP0 && group == 0) {
+    const int64_t at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
+    s_row[r] = !row_ok ? -1 : split ? ((int64_t)rq.row0 * a.Hq + at) * a.num_splits + z : at;
+  }
+  if (threadIdx.x == 0)
+    *s_out = P8Out{split ? reinterpret_cast<uint8_t*>(a.part_o) : reinterpret_cast<uint8_t*>(rq.out),
+                   split ? 1 : 0, last ? a.num_splits - 1 - z : 0};
   const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
@@ -613,19 +632,20 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   const bool all_ok = !__syncthreads_or(!ok);
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");   // the merge waits for the rest
   if (warp >= P8_SM_WARP0) {
-    const int64_t prow = ((int64_t)rq.row0 * a.Hq + qrow_at) * a.num_splits + z;
-    if (PLAN && last && row_ok && group == 0)   // the pair's unused partials: neutral
-      for (int u = 1; z + u < a.num_splits; ++u) {
-        a.part_ml[(prow + u) * 2 + 0] = -INFINITY;
-        a.part_ml[(prow + u) * 2 + 1] = 0.f;
+    const P8Out out = *s_out;
+    const int64_t row_at = s_row[r];
+    if (PLAN && row_at >= 0 && group == 0)   // neutral
+      for (int u = 1; u <= out.unused; ++u) {
+        a.part_ml[(row_at + u) * 2 + 0] = -INFINITY;
+        a.part_ml[(row_at + u) * 2 + 1] = 0.f;
       }
     if (ntiles == 0) {   // an empty history range: a neutral partial
-      if (split && row_ok) {
+      if (out.split && row_at >= 0) {
         if (group == 0) {
-          a.part_ml[prow * 2 + 0] = -INFINITY;
-          a.part_ml[prow * 2 + 1] = 0.f;
+          a.part_ml[row_at * 2 + 0] = -INFINITY;
+          a.part_ml[row_at * 2 + 1] = 0.f;
         }
-        float4* const po = reinterpret_cast<float4*>(a.part_o + prow * D + group * (D / 2));
+        float4* const po = reinterpret_cast<float4*>(a.part_o + row_at * D + group * (D / 2));
         for (int c = 0; c < D / 8; ++c) po[c] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
     } else if (all_ok &&
@@ -639,22 +659,22 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         const float2 v = s_ml[g * PF_BM + r];
         if (v.x != -INFINITY) lsum = fmaf(v.y, fast_exp2(v.x - m), lsum);
       }
-      if (split && row_ok && group == 0) {
-        a.part_ml[prow * 2 + 0] = m;
-        a.part_ml[prow * 2 + 1] = lsum;
+      if (out.split && row_at >= 0 && group == 0) {
+        a.part_ml[row_at * 2 + 0] = m;
+        a.part_ml[row_at * 2 + 1] = lsum;
       }
       const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
       // The warp's 32 half rows go through shared memory (16-byte piece p of row r at
       // p ^ (r & 7)), so that a store writes whole lines; a row per thread took 3 us.
       const uint32_t tr = smem_u32(sm) + (warp - P8_SM_WARP0) * (32 * (D / 2) * 4);
-      const int lg = (D == 256 ? 4 : 3) + (split ? 1 : 0);   // 2^lg 16-byte pieces a half row
+      const int lg = (D == 256 ? 4 : 3) + out.split;   // 2^lg 16-byte pieces a half row
       const uint32_t mine = tr + (lane << (lg + 4));
 #pragma unroll 1
       for (int c0 = 0; c0 < D / 2; c0 += 32) {
         uint32_t o[32];
         tc::ld32(tO + group * (D / 2) + c0 + lane_off, o);
         tc::wait_ld();
-        if (split) {
+        if (out.split) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
             st_shared_v4(mine + (((c0 / 4 + k) ^ (lane & 7)) << 4), o[4 * k], o[4 * k + 1],
@@ -672,16 +692,14 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         }
       }
       __syncwarp();
-      const int64_t row_at = split ? prow : qrow_at;
-      const int row_bytes = split ? D * 4 : D * 2;
-      uint8_t* const to = (split ? reinterpret_cast<uint8_t*>(a.part_o)
-                                 : reinterpret_cast<uint8_t*>(rq.out)) + group * (row_bytes / 2);
+      const int row_bytes = out.split ? D * 4 : D * 2;
+      uint8_t* const to = out.to + group * (row_bytes / 2);
 #pragma unroll 4
       for (int i = lane; i < 32 << lg; i += 32) {
         const int row = i >> lg, piece = i & ((1 << lg) - 1);
-        const int64_t dst = __shfl_sync(0xffffffffu, row_at, row);
+        const int64_t dst = s_row[quarter * 32 + row];
         const uint4 v = ld_shared_v4(tr + (row << (lg + 4)) + ((piece ^ (row & 7)) << 4));
-        if (quarter * 32 + row < rows)
+        if (dst >= 0)
           *reinterpret_cast<uint4*>(to + dst * row_bytes + piece * 16) = v;
       }
     } else if (all_ok && lane == 0) {
@@ -703,7 +721,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
 // queries after 30,720 positions (44 of 196 pairs left over): one launch more with three
-// even splits 1,163 us, the plan TIMES.
+// even splits 1,123 us, the plan 1,013.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 
 void kv8_prefill_plan(int64_t G, int64_t Hkv, int64_t q_start, int64_t chunk_len, bool causal,
