@@ -720,8 +720,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // The plan's estimate, in history tiles (0.8 us each at D = 256): a part beyond a
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
-// queries after 30,720 positions (44 of 196 pairs left over): one launch more with three
-// even splits 1,123 us, the plan 1,013.
+// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,121 us,
+// cut 1,013; before the kernel's later steps, uncut 1,243, the left-over pairs as a
+// second launch of three even splits 1,163, cut so 1,131.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 
 void kv8_prefill_plan(int64_t G, int64_t Hkv, int64_t q_start, int64_t chunk_len, bool causal,
