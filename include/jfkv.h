@@ -1,5 +1,7 @@
 /*
- * jfkv.h -- C ABI of the GB300 paged 4-bit KV library (libjfkv.so).
+ * jfkv.h -- C ABI of the GB300 paged KV library (libjfkv.so): 4-bit pages, and
+ * for long image-and-text sessions 8-bit pages, rotary positions with several
+ * axes and eviction by attention weight.
  *
  * The library implements the data-parallel hot path of KVExec (Sec. 3.1 and
  * Sec. 3.4 of "JustFit: Just-in-Time State Management for Local LLM Serving"):
@@ -311,9 +313,10 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * jf_prefill_chunk_workspace_bytes(...) bytes (256-byte aligned), as two
  * launches: its first query tiles as whole waves, then the rest with their
  * history split across pairs and merged (as jf_prefill_batch_attn with
- * num_splits > 1).  With a smaller workspace it runs as one launch.  Both
- * forms compute the same attention; the summation order, and so the last
- * bits, differ.
+ * num_splits > 1); over an E4M3 pool the two are one launch, the rest's
+ * histories cut into one piece of equal work per pair of SMs.  With a smaller
+ * workspace it runs undivided.  Both forms compute the same attention; the
+ * summation order, and so the last bits, differ.
  * Numerics (affine pools): each 64-position K/V tile is rebuilt in shared
  * memory as fp16 code * scale + bias (one rounding) for the tensor cores, and
  * q * softmax_scale * log2(e) enters as fp16; accumulation and the softmax
@@ -327,9 +330,11 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * workspace), K and V tiles are built in shared memory as norm * centroid
  * (fp16) in the rotated basis, and each output row is rotated back
  * (S_V H / sqrt(D)) as the partials are merged.
- * E4M3 pools: workspaces as for affine pools; the tiles hold the codes as fp16
- * (exact) and the block scales are applied as in the decode; no scale is out
- * of range.
+ * E4M3 pools: workspaces as for affine pools.  K's codes are multiplied as
+ * they are, by q as the sum of two e4m3 terms under a power-of-two scale per
+ * row (bf16's 8 bits exactly for elements within 2^-9 of the row's largest,
+ * at most 2^-17 of the largest off below); V's codes enter as fp16 (exact) and
+ * the block scales are applied as in the decode; no scale is out of range.
  */
 int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
                           const void* q, int32_t q_start, int32_t chunk_len, int32_t num_q_heads,

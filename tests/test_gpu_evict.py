@@ -74,6 +74,30 @@ def test_evict_long_rows():
     check(1, 128, 256, [40003, 16385], 5001, 4, 77, lambda r, s: 1 + r.integers(0, 1 << 12, s) * 2.0 ** -23, spread=0)
 
 
+@pytest.mark.parametrize("skew", [0, 1, 2, 3])
+@pytest.mark.parametrize("n", [101, 130, 4097, 20001])
+def test_evict_weights_at_any_address(skew, n):
+    """Rows of weights that begin and end off a 16-byte boundary, in every way; nothing beside them is read as theirs."""
+    hkv, d, p, budget = 2, 128, 64, 100
+    rng = np.random.default_rng(40 * n + skew)
+    own, extra = -(-n // p), -(-budget // p)
+    L, table, pool = C.filled(rng, hkv, p, d, [n], extra=[extra])
+    src, dst = table[:, :own].copy(), table[:, own:own + extra].copy()
+    w = uneven(rng, (1, hkv, n)).astype(np.float32)      # row 1 begins n weights after row 0
+    wide = torch.full((hkv * n + 8,), 1e30, device=DEV)
+    wide[skew:skew + hkv * n] = torch.from_numpy(w.reshape(-1)).to(DEV)
+    view = wide[skew:skew + hkv * n].view(1, hkv, n)
+    g = C.gpu_pool(L, pool.copy())
+    kept, wout = torch.empty(1, hkv, budget, dtype=torch.int32, device=DEV), torch.empty(1, hkv, budget, device=DEV)
+    m, err = torch.empty(1, dtype=torch.int32, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    jf.jf_kv8_evict(g, C.ints(src), C.ints([n]), view, budget, 3, 8, C.ints(dst), m, wout, kept, err)
+    want_kept, want_w = O.evict(pool, L, src, [n], w, budget, 3, 8, dst)
+    assert int(err) == 0 and int(m) == budget
+    assert np.array_equal(kept.cpu().numpy(), want_kept)
+    assert np.array_equal(wout.cpu().numpy(), want_w)
+    assert np.array_equal(g.data.cpu().numpy(), pool)
+
+
 def test_evict_then_decode_sees_the_kept_positions():
     rng = np.random.default_rng(5)
     L, table, pool = C.filled(rng, 2, 64, 128, [500, 90], extra=[2, 2])

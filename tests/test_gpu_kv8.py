@@ -465,6 +465,67 @@ def test_prefill_wave_balanced_equals_one_launch():
     assert (outs[0] - outs[1]).abs().max() <= 2.0 ** -7 * outs[1].abs().max()
 
 
+@pytest.mark.parametrize("hq,hkv,d,p,start,c,causal", [
+    (24, 4, 256, 256, 3400, 840, True),      # 80 pairs: 4 left over, their histories in many parts
+    (24, 4, 256, 64, 7001, 1700, False),     # 164 pairs: 12 left over
+    (12, 3, 128, 128, 9000, 2005, True),     # odd lengths, 96 pairs: 21 left over
+    (7, 1, 128, 64, 13001, 3001, True),      # 7 query heads: 84 pairs, padding rows
+    (4, 4, 256, 128, 16400, 4100, True),     # one query head a KV head: 68 pairs, one wave
+])
+def test_prefill_divided_last_wave_equals_undivided(hq, hkv, d, p, start, c, causal):
+    """Pairs beyond whole waves with their histories in parts: within rounding of the undivided launch."""
+    rng = np.random.default_rng(c)
+    pages = -(-(start + c) // p)
+    g = jf.KVPool.allocate(pages, p, hkv, d, format=jf.JF_FMT_E4M3_B32)
+    table = C.ints(rng.permutation(pages)[None])
+    torch.manual_seed(c)
+    x = [torch.randn(start + c, hkv, d, device=DEV).bfloat16() for _ in range(2)]
+    err = gpu_append(g, table.cpu().numpy(), [0], [0, start + c], *x)
+    q = torch.randn(c, hq, d, device=DEV).bfloat16()
+    big = jf.prefill_chunk_workspace(g, start, c, hq)
+    big[256:] = 0xFF                         # NaN: what no part writes is not read
+    outs = []
+    for ws in (big, big, torch.zeros(256, dtype=torch.uint8, device=DEV)):
+        out = torch.full_like(q, float("nan"))
+        jf.jf_prefill_chunk_attn(g, table[0], q, start, 1 / math.sqrt(d), causal, out, ws)
+        assert jf.workspace_status(ws) == 0
+        outs.append(out)
+    assert int(err) == 0
+    assert torch.equal(outs[0], outs[1])     # the same bits every time
+    a, b = outs[0].double(), outs[2].double()
+    assert torch.isfinite(a).all()
+    # Each form rounds P to fp16 (2^-11 of it), sums in fp32 and rounds once to bf16 (2^-8):
+    # together they differ by at most 2 (2^-11 max|v| + 2^-8 |out|) and a little for the sums.
+    top = x[1].abs().max().double() * (1 + 2.0 ** -4)
+    assert ((a - b).abs() <= 2 * (2.0 ** -11 + 2.0 ** -16) * top + 2 * 2.0 ** -8 * b.abs()).all()
+
+
+def test_prefill_reports_a_page_outside_the_pool():
+    """One request's bad page id is flagged; the other request's output does not change."""
+    rng = np.random.default_rng(33)
+    hq, hkv, d, p, start, count = 8, 2, 128, 64, [300, 200], [40, 24]
+    ctx = [s + c for s, c in zip(start, count)]
+    L, table, pool = C.filled(rng, hkv, p, d, ctx)
+    g = C.gpu_pool(L, pool)
+    q = torch.randn(sum(count), hq, d, device=DEV).bfloat16()
+
+    def run(tbl, splits):
+        out = torch.full_like(q, float("nan"))
+        ws = jf.prefill_batch_workspace(sum(count), hq, d, splits, format=jf.JF_FMT_E4M3_B32)
+        jf.jf_prefill_batch_attn(g, C.ints(tbl), start, count, q, 0.1, True, out, ws, splits)
+        return out, jf.workspace_status(ws)
+
+    for splits in (1, 3):
+        good, status = run(table, splits)
+        assert status == 0
+        for bad in (-1, len(pool), 1 << 30, -(1 << 31)):
+            t = table.copy()
+            t[0, 2] = bad
+            out, status = run(t, splits)
+            assert status == jf.binding.JF_DEV_ERR_PAGE_ID
+            assert torch.equal(out[count[0]:], good[count[0]:])
+
+
 def test_checkpoint_and_restore_copy_the_pages():
     rng = np.random.default_rng(32)
     L, table, pool = C.filled(rng, 2, 64, 128, [150], fill=0x33)
