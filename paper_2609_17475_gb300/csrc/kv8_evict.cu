@@ -342,6 +342,26 @@ __global__ void __launch_bounds__(EV_THREADS, 1) kv8_select_kernel(const EvictAr
   asm volatile("barrier.cluster.wait.aligned;\n" ::: "memory");
 }
 
+// Largest code of 16, signs apart (0x7F where a NaN is among them).
+__device__ __forceinline__ uint32_t ev_top(uint4 w) {
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    m = __vmaxu2(m, __vmaxu2(ws[i] & 0x7F007F00u, (ws[i] << 8) & 0x7F007F00u));
+  return max(m >> 24, (m >> 8) & 0x7Fu);
+}
+// The same with NaN passed over.
+__device__ __noinline__ uint32_t ev_top_finite(uint4 w) {
+  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+  uint32_t m = 0;
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t c = (ws[i >> 2] >> (8 * (i & 3))) & 0x7Fu;
+    if (c != 0x7Fu) m = max(m, c);
+  }
+  return m;
+}
+
 template <int D>
 __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
   constexpr int LPR = D / 16;              // lanes per row, 16 codes each
@@ -392,28 +412,24 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
       }
     }
   }
-  // the rows' values under their own scales as fp16 (exact), and the block's
-  // largest finite magnitude (the maximum passes over NaN)
-  uint32_t f[NP][2][8];
+  // the block's largest finite magnitude: that of a thread's codes as whole numbers
+  // (their order is the values'), then with the rows' scales
+  uint32_t mag[NP][2];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
     float amax = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      uint32_t* const v = f[p][kind];
-      f16x4_of_e4m3(x[p][kind].x, v[0], v[1]);
-      f16x4_of_e4m3(x[p][kind].y, v[2], v[3]);
-      f16x4_of_e4m3(x[p][kind].z, v[4], v[5]);
-      f16x4_of_e4m3(x[p][kind].w, v[6], v[7]);
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max_f16x2(top, v[i] & 0x7FFF7FFFu);
-      const float2 t2 = f32x2_of_f16x2(top);
-      amax = fmaxf(amax, fmaxf(t2.x, t2.y) * two8(exp8_of_scale(s_old[p][kind])));
+      const uint4 w = x[p][kind];
+      mag[p][kind] = ev_top(w);
+      uint32_t top = mag[p][kind], lo, hi;
+      if (top == 0x7Fu) top = ev_top_finite(w);
+      f16x4_of_e4m3(top, lo, hi);
+      amax = fmaxf(amax, f32x2_of_f16x2(lo).x * two8(exp8_of_scale(s_old[p][kind])));
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-    if (lane == 0) warp_max[kind][warp] = amax;
+    // magnitudes: the order of their bits is theirs
+    const uint32_t all = __reduce_max_sync(0xffffffffu, __float_as_uint(amax));
+    if (lane == 0) warp_max[kind][warp] = __uint_as_float(all);
   }
   __syncthreads();
   if (dst < 0 || dst >= a.num_pages) {
@@ -437,11 +453,13 @@ __global__ void __launch_bounds__(256) kv8_compact_kernel(const EvictArgs a) {
     for (int p = 0; p < NP; ++p) {
       const int row = p * RPP + rr;
       if (j0 + row < m) {
-        uint32_t (&v)[8] = f[p][kind];
-        rescale_f16(v, exp8_of_scale(s_old[p][kind]) - e);
-        *reinterpret_cast<uint4*>(codes + row * D) =
-            make_uint4(e4m3x4_of_f16x2(v[0], v[1]), e4m3x4_of_f16x2(v[2], v[3]),
-                       e4m3x4_of_f16x2(v[4], v[5]), e4m3x4_of_f16x2(v[6], v[7]));
+        // a row under its own scale keeps its codes (NaN apart, which has one code)
+        const int s = exp8_of_scale(s_old[p][kind]) - e;
+        uint4 w = x[p][kind];
+        if (s != 0 || mag[p][kind] == 0x7Fu)
+          w = make_uint4(rescale_e4m3x4(w.x, s), rescale_e4m3x4(w.y, s), rescale_e4m3x4(w.z, s),
+                         rescale_e4m3x4(w.w, s));
+        *reinterpret_cast<uint4*>(codes + row * D) = w;
       }
     }
   }

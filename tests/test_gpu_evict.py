@@ -98,6 +98,25 @@ def test_evict_weights_at_any_address(skew, n):
     assert np.array_equal(g.data.cpu().numpy(), pool)
 
 
+def test_evict_codes_of_nan():
+    """Codes that are NaN (of either sign) stay NaN, in the one code it has, and scale nothing."""
+    hkv, d, p, n, budget = 2, 128, 64, 150, 70
+    rng = np.random.default_rng(77)
+    L, table, pool = C.filled(rng, hkv, p, d, [n], extra=[2], spread=3)
+    src, dst = table[:, :3].copy(), table[:, 3:5].copy()
+    for t in range(0, n, 7):                             # byte t of each position's row, K and V
+        page, slot = pool[table[0, t // p]], t % p
+        for side in range(2):
+            for h in range(hkv):
+                at = (side * hkv + h) * p * d + slot * d + t % d
+                page[at] = (0xFF, 0x7F)[t % 2]
+    w = uneven(rng, (1, hkv, n)).astype(np.float32)
+    g, kept, wout, m, err = evict(L, pool, src, [n], w, budget, 0, 9, dst)
+    want_kept, _ = O.evict(pool, L, src, [n], w, budget, 0, 9, dst)
+    assert err == 0 and np.array_equal(kept.cpu().numpy(), want_kept)
+    assert np.array_equal(g.data.cpu().numpy(), pool)
+
+
 def test_evict_then_decode_sees_the_kept_positions():
     rng = np.random.default_rng(5)
     L, table, pool = C.filled(rng, 2, 64, 128, [500, 90], extra=[2, 2])
