@@ -1,4 +1,5 @@
-"""GB300-native paged 4-bit KV attention (the KVExec hot path of JustFit).
+"""GB300-native paged 4-bit KV attention (the KVExec hot path of JustFit), and an
+8-bit cache with rotary axes and eviction for long image-and-text sessions.
 
 The compute lives in libjfkv.so (hand-written sm_103a CUDA behind a C ABI,
 include/jfkv.h); ``binding`` marshals torch tensors into those calls.

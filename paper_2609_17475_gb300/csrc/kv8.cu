@@ -13,6 +13,12 @@
 //
 // Read.  The inverse on runs of positions: bf16 values code * 2^e (exact: a
 // code has 4 significant bits).
+//
+// Bound: memory for long runs, the launch for a step.  A block to a CTA, since its
+// scale needs all of its rows before the first code is written, and one CTA's registers
+// hold them.  2,048 rows of 4 KV heads x 256 after 30,725 positions: append and read back
+// together 7.4 us (21 MB: 3.1 us at the copy rate); one row to each of 32 requests 6.3 us;
+// 32,768 x 4 rows read back 29 us, 6.9 TB/s with part of the writes left in L2.
 #include "kv8.cuh"
 
 namespace jfkv {

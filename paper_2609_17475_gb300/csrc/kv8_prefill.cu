@@ -32,6 +32,12 @@
 //                hold its half into four staging tiles
 //   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers
 //   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
+// Bound: the tensor core, at the clock its power allows.  1,596 queries after 30,720
+// positions (24 / 4 heads x 256, two full waves) 757 us, 1,630 TFLOP/s: 0.85 of the
+// bf16 burst rate, 0.95 of the sustained one.  At D = 128 a tile has half the products for
+// the same exponentials, and the softmax warps set the pace: 798 queries so, one wave,
+// 930 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
+// ways: 19.5 us of launches, Q's way in, eight tiles one after the other and the merge.
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
 // from TMEM behind a tcgen05 fence, or from this CTA's own shared memory, never by
 // plain loads from the other CTA's (cluster scope cost 4 % at D = 256, 8 % at 128).
@@ -60,7 +66,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // Where a CTA's results go, kept in shared memory with the rows' places so that the
 // softmax loop holds none of it in registers (1,596 queries after 30,720 positions
-// 774 us with it there, now 760).
+// 774 us with it there, 760 without).
 struct P8Out {
   uint8_t* to;          // the output, or the partials O
   int32_t split;
@@ -349,7 +355,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       // The whole warp runs this loop, so that its control flow and the operands'
       // descriptors are uniform values; lane 0 alone issues (the loop run by lane 0
       // alone moved every descriptor to uniform registers first, which took longer
-      // than the products: 1,596 queries after 30,720 positions 982 us, now 924).
+      // than the products: 1,596 queries after 30,720 positions 982 us, 924 after).
       const uint64_t qd = tc::sdesc_sw128(smem_u32(sQ), 16, 1024);
       const uint64_t kd = tc::sdesc_sw128(smem_u32(sK), 16, 1024);
       const uint64_t vd = tc::sdesc_sw128(smem_u32(sV), PF_BN * 128, 1024);
