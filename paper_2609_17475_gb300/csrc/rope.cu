@@ -14,9 +14,9 @@
 // is off by 0.01 rad at position 262,144) and no range reduction is needed.
 //
 // Bound by memory: each element is read and written once.  2,048 tokens of 28 heads x
-// 256 (bf16, all channels turned) 14.0 us, 4.2 TB/s, of which about 4 us are the launch
+// 256 (bf16, all channels turned) 12.6 us, 4.7 TB/s, of which about 4 us are the launch
 // and the first loads (32 tokens: 4.1 us); the gradient of 16,391 tokens of 20 heads x
-// 128 (fp16) 33.2 us, 5.1 TB/s.  One CTA a token (two, where that fills the SMs anyway)
+// 128 (fp16) 33.3 us, 5.0 TB/s.  One CTA a token (two, where that fills the SMs anyway)
 // keeps the cosines beside the heads that use them: 18 KB of rows a CTA, many CTAs an SM.
 #include "common.cuh"
 
@@ -144,7 +144,11 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
     const float x = (float)(int32_t)(turns >> 32) * 4.656612873077393e-10f;   // 2^-31
     float s, c;
     sincospif(x, &s, &c);
-    cs[u] = make_float2(c, a.inverse ? -s : s);
+    // in twos, those of neighbouring places adjoining, so that the loads below meet no
+    // bank twice (a place's pairs in a row: 13.9 us for the 2,048 tokens, not 12.6; kept
+    // in registers across a token's heads: 12.7, and the gradient 36.2, not 33.3)
+    cs[jj * half + 2 * (i % NC / 2 * turned + i / NC) + (i & 1)] =
+        make_float2(c, a.inverse ? -s : s);
   }
   __syncthreads();
   while (live) {
@@ -161,13 +165,13 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
       if (second) v1 = *reinterpret_cast<const uint4*>(in + half);
     }
     if (turn) {
-      const float4* const w = reinterpret_cast<const float4*>(cs + jc * half + k * NC);
+      const float4* const w = reinterpret_cast<const float4*>(cs + jc * half) + k;
       float p0[V], p1[V], y0[V], y1[V];
       unpack16<T>(x0, p0);
       if (!ADJ) unpack16<T>(x1, p1);
 #pragma unroll
       for (int i = 0; i < NC; i += 2) {
-        const float4 f = w[i / 2];   // cosine and sine of pairs i and i + 1
+        const float4 f = w[i / 2 * turned];   // cosine and sine of pairs i and i + 1
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const float c = e ? f.z : f.x, s = e ? f.w : f.y;
@@ -236,8 +240,8 @@ int launch_rope(const jf_rope& rope, const int32_t* positions, int64_t pos_strid
   pdl[0].val.programmaticStreamSerializationAllowed = 1;
   cudaLaunchConfig_t cfg = {};
   // One token a CTA, or two in long runs, where the start of a CTA weighs more
-  // (16,391 tokens of 20 heads x 128: 36.7 us with one, 33.6 with two; 2,048
-  // tokens of 28 x 256: 13.9 us with one, 17.9 with two).
+  // (16,391 tokens of 20 heads x 128: 34.0 us with one, 33.3 with two; 2,048
+  // tokens of 28 x 256: 12.6 us with one, 15.1 with two).
   a.tpb = n_tokens >= 16 * sm_count() ? 2 : 1;
   cfg.gridDim = dim3((unsigned)((n_tokens + a.tpb - 1) / a.tpb));
   cfg.blockDim = dim3(ROPE_THREADS);
