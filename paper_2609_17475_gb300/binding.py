@@ -372,7 +372,7 @@ def jf_paged_decode_attn(pool: KVPool, page_table: torch.Tensor, context_lens: t
                          workspace: torch.Tensor, num_splits: int, stream=None) -> None:
     if pool.codec is None:
         st = (_fast or _calls()).decode(pool, page_table, context_lens, q, softmax_scale, out, workspace,
-                                        num_splits, stream)
+                                        int(num_splits), stream)
         if st:
             raise JfError("jf_paged_decode_attn", st)
         return
