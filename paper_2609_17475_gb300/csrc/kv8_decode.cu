@@ -460,7 +460,14 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
             const int ek = exp8_of_scale(ksc[s]), ev = exp8_of_scale(vsc[s]);
             const uint32_t kb = ring + rs * L::STAGE;
             float* sc = nullptr;
-            if constexpr (WEIGH) sc = scb + (int64_t)(p0 / K8_SUB) * (32 * a.pairs);
+            if constexpr (WEIGH) {
+              sc = scb + (int64_t)(p0 / K8_SUB) * (32 * a.pairs);
+              if (!((valid >> s) & 1u) && p0 < lim) {   // a page outside the pool: no weight
+                const int pr = k8_pos<D>(r);
+                if (2 * c < a.G) sc[pr] = sc[pr + 16 * a.pairs] = NEG;
+                if (2 * c + 1 < a.G) sc[pr + 8 * a.pairs] = sc[pr + 24 * a.pairs] = NEG;
+              }
+            }
             if (nv >= K8_SUB)
               k8_chunk<D, true>(st, qf, kb, r, c, cA0, cA1, two8(ek), (float)ev, two8(-ev), 0, sc,
                                 a.pairs, 2 * c < a.G, 2 * c + 1 < a.G);
@@ -639,7 +646,10 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_weigh_kernel(const Kv8DecodeA
   float2 m[8];
 #pragma unroll
   for (int g = 0; g < 8; ++g)
-    if (g < a.G) m[g] = a.row_ml[(int64_t)b * a.Hq + kvh * a.G + g];
+    if (g < a.G) {
+      m[g] = a.row_ml[(int64_t)b * a.Hq + kvh * a.G + g];
+      if (m[g].x == -INFINITY) m[g].x = 0.f;   // nothing attended: weights of zero
+    }
   // a thread takes four adjacent positions a step; the heads' scores are all
   // loaded before any is used
   const float* const sc = a.scores + ((int64_t)b * a.Hkv + kvh) * a.sstride;

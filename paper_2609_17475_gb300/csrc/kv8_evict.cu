@@ -537,7 +537,7 @@ int launch_kv8_evict(const Geom& g, const jf_kv_pool& pool, const int32_t* page_
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   cfg.dynamicSmemBytes = 0;
-  cfg.gridDim = dim3((unsigned)((budget + KV8_BLOCK - 1) / KV8_BLOCK), (unsigned)g.Hkv,
+  cfg.gridDim = dim3((unsigned)(((int64_t)budget + KV8_BLOCK - 1) / KV8_BLOCK), (unsigned)g.Hkv,
                      (unsigned)batch);
   cfg.blockDim = dim3(256);
   const cudaError_t e = g.D == 256 ? cudaLaunchKernelEx(&cfg, kv8_compact_kernel<256>, a)

@@ -500,6 +500,45 @@ def test_prefill_divided_last_wave_equals_undivided(hq, hkv, d, p, start, c, cau
     assert ((a - b).abs() <= 2 * (2.0 ** -11 + 2.0 ** -16) * top + 2 * 2.0 ** -8 * b.abs()).all()
 
 
+@pytest.mark.parametrize("hq,d", [(8, 128), (6, 256), (2, 128)])
+def test_decode_weights_of_a_page_outside_the_pool(hq, d):
+    """Positions of a bad page draw no weight (whatever the workspace held), and a request of bad pages alone gives
+    zeros; the others' weights and outputs are those of a context without them."""
+    rng = np.random.default_rng(hq)
+    hkv, p, ctx = 2, 64, [200, 130, 64]
+    L, table, pool = C.filled(rng, hkv, p, d, ctx)
+    g = C.gpu_pool(L, pool)
+    q = torch.randn(3, hq, d, device=DEV).bfloat16()
+    bad = table.copy()
+    bad[0, 1], bad[1, :3], bad[2, 0] = len(pool), -1, 1 << 30
+    w_in = torch.rand(3, hkv, 200, device=DEV)
+
+    def run(tbl, splits):
+        out, w = torch.full_like(q, float("nan")), torch.full_like(w_in, float("nan"))
+        ws = jf.decode_weights_workspace(3, hq, hkv, d, splits, 200)
+        ws[256:] = 0xFF                              # NaN partials and scores
+        jf.jf_paged_decode_weights_attn(g, C.ints(tbl), C.ints(ctx), q, 0.1, out, w_in, w, ws, splits)
+        return out, w, jf.workspace_status(ws)
+
+    for splits in (1, 4):
+        out, w, status = run(bad, splits)
+        assert status == jf.binding.JF_DEV_ERR_PAGE_ID
+        assert (out[1:] == 0).all()
+        for b in (1, 2):
+            assert torch.equal(w[b, :, :ctx[b]], w_in[b, :, :ctx[b]])
+        assert torch.equal(w[0, :, 64:128], w_in[0, :, 64:128])
+        # request 0 without its second page: positions 0..63 and 128..199
+        k, v = O.read(pool, L, table[0], 200)
+        seen = np.r_[0:64, 128:200]
+        ref, pr, mass = O.attend(k[seen], v[seen], q[:1].double().cpu().numpy(), float(np.float32(0.1)))
+        e = np.abs(out[0].double().cpu().numpy() - ref[0])
+        assert (e <= C.out_bound(ref[0], mass[0], 200, np.abs(v).max())).all()
+        got = (w[0].double() - w_in[0].double()).cpu().numpy()[:, seen]
+        want = pr[0].reshape(hkv, hq // hkv, len(seen)).sum(1)
+        # sums of up to 4 weights, each good to 2^-10 of itself, added in fp32 to a weight below 1
+        assert (np.abs(got - want) <= 2.0 ** -10 * want + 2.0 ** -21).all()
+
+
 def test_prefill_reports_a_page_outside_the_pool():
     """One request's bad page id is flagged; the other request's output does not change."""
     rng = np.random.default_rng(33)
