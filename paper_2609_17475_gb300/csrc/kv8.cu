@@ -44,13 +44,13 @@ struct Kv8Args {
 };
 
 // Rows [r0, r1) of request b and its first position; false where they do not
-// fit the row list or the request's page-table row.
+// fit the row list, the request's page-table row or 31 bits.
 __device__ __forceinline__ bool kv8_run(const Kv8Args& a, int b, int& r0, int& r1, int& pos0) {
   r0 = a.row_offsets[b];
   r1 = a.row_offsets[b + 1];
   pos0 = a.start_pos[b];
   return r0 >= 0 && r0 <= r1 && r1 <= a.n_rows && pos0 >= 0 &&
-         (int64_t)pos0 + (r1 - r0) <= (int64_t)a.pt_stride * a.P;
+         (int64_t)pos0 + (r1 - r0) <= min((int64_t)a.pt_stride * a.P, (int64_t)0x7FFFFFFF);
 }
 
 template <int D>

@@ -339,7 +339,7 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
     const int ctx = k8_ctx(a, b);
     // this segment's stages [s0, s1) of 16 positions
     const int s0 = max(u0 - K8_HDR, 0) * 2;
-    const int s1 = min(max(u1 - K8_HDR, 0) * 2, (ctx + K8_SUB - 1) / K8_SUB);
+    const int s1 = min(max(u1 - K8_HDR, 0) * 2, (int)((ctx + (int64_t)K8_SUB - 1) / K8_SUB));
     const int n_cta = max(s1 - s0, 0);
     const int my_n = n_cta > warp ? (n_cta - warp + K8_NW - 1) / K8_NW : 0;
     auto pos_of = [&](int it) { return (s0 + warp + it * K8_NW) * K8_SUB; };

@@ -565,6 +565,28 @@ def test_prefill_reports_a_page_outside_the_pool():
             assert torch.equal(out[count[0]:], good[count[0]:])
 
 
+def test_positions_past_31_bits_are_refused():
+    """A run that would end past the last 32-bit position does not fit, however long the page table is; runs that
+    end at it do."""
+    hkv, d, p = 1, 128, 256
+    pages = 2
+    g = jf.KVPool.allocate(pages, p, hkv, d, format=jf.JF_FMT_E4M3_B32)
+    long = torch.zeros(1, (1 << 31) // p + 1, dtype=torch.int32, device=DEV)    # every entry page 0
+    x = torch.randn(20, hkv, d, device=DEV).bfloat16()
+    y, z = torch.full_like(x, -3.0), torch.full_like(x, -3.0)
+    bit = jf.binding.JF_DEV_ERR_POSITION
+    for start, fits in (((1 << 31) - 10, False), ((1 << 31) - 20, False), ((1 << 31) - 21, True)):
+        before, err = g.data.clone(), flag()
+        jf.jf_kv8_append(g, long, C.ints([start]), C.ints([0, 20]), x, x, err)
+        assert int(err) == (0 if fits else bit) and torch.equal(g.data, before) == (not fits)
+        err = flag()
+        jf.jf_kv8_read(g, long, C.ints([start]), C.ints([0, 20]), y, z, err)
+        assert int(err) == (0 if fits else bit)
+        if not fits:
+            assert (y == -3).all() and (z == -3).all()
+    assert torch.equal(y, z) and (y.double() - x.double()).abs().max() <= 2.0 ** -4 * x.abs().max()
+
+
 def test_checkpoint_and_restore_copy_the_pages():
     rng = np.random.default_rng(32)
     L, table, pool = C.filled(rng, 2, 64, 128, [150], fill=0x33)
