@@ -117,6 +117,36 @@ def test_evict_codes_of_nan():
     assert np.array_equal(g.data.cpu().numpy(), pool)
 
 
+@pytest.mark.parametrize("make", [uneven, ties, odd])
+def test_evict_rows_too_long_for_shared_memory(make):
+    """Rows of weights past what a cluster's shared memory holds, whatever the contexts: short contexts in them, pages
+    and all, and one context of the whole row (its pages repeat) by its kept positions and weights."""
+    rng = np.random.default_rng(50)
+    hkv, d, p, budget, stride = 1, 128, 64, 300, 800_003
+    ctx = [9001, 300, 301, 0]
+    own, extra = [-(-n // p) for n in ctx], [-(-min(n, budget) // p) for n in ctx]
+    L, table, pool = C.filled(rng, hkv, p, d, ctx, extra=extra)
+    src, dst = np.full((4, max(own)), -1, np.int32), np.full((4, max(extra)), -1, np.int32)
+    for b in range(4):
+        src[b, :own[b]], dst[b, :extra[b]] = table[b, :own[b]], table[b, own[b]:own[b] + extra[b]]
+    w = np.zeros((4, hkv, stride), np.float32)
+    w[:, :, :9001] = make(rng, (4, hkv, 9001))
+    g, kept, wout, n, err = evict(L, pool, src, ctx, w, budget, 4, 32, dst)
+    want_kept, want_w = O.evict(pool, L, src, ctx, w, budget, 4, 32, dst)
+    assert err == 0 and np.array_equal(kept.cpu().numpy(), want_kept)
+    assert np.array_equal(wout.cpu().numpy().view(np.int32), want_w.view(np.int32))
+    assert np.array_equal(g.data.cpu().numpy(), pool)
+
+    n, budget = stride - 2, 5003
+    w = make(rng, (1, hkv, stride)).astype(np.float32)
+    src = np.zeros((1, -(-n // p)), np.int32) + table[0, 0]
+    dst = np.setdiff1d(np.arange(len(pool)), table[0, :1])[None, :-(-budget // p)].astype(np.int32)
+    _, kept, wout, m, err = evict(L, pool, src, [n], w, budget, 4, 32, dst)
+    at = O.keep(w[0, 0, :n], budget, 4, 32)
+    assert err == 0 and int(m) == budget and np.array_equal(kept[0, 0].cpu().numpy(), at)
+    assert np.array_equal(wout[0, 0].cpu().numpy().view(np.int32), w[0, 0, at].view(np.int32))
+
+
 def test_evict_then_decode_sees_the_kept_positions():
     rng = np.random.default_rng(5)
     L, table, pool = C.filled(rng, 2, 64, 128, [500, 90], extra=[2, 2])
