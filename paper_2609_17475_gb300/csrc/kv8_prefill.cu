@@ -33,10 +33,10 @@
 //   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers
 //   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
 // Bound: the tensor core, at the clock its power allows.  1,596 queries after 30,720
-// positions (24 / 4 heads x 256, two full waves) 757 us, 1,630 TFLOP/s: 0.85 of the
-// bf16 burst rate, 0.95 of the sustained one.  At D = 128 a tile has half the products for
+// positions (24 / 4 heads x 256, two full waves) 725 us, 1,705 TFLOP/s: 0.89 of the
+// bf16 burst rate, 0.99 of the sustained one.  At D = 128 a tile has half the products for
 // the same exponentials, and the softmax warps set the pace: 798 queries so, one wave,
-// 930 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
+// 1,005 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
 // ways: 19.5 us of launches, Q's way in, eight tiles one after the other and the merge.
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
 // from TMEM behind a tcgen05 fence, or from this CTA's own shared memory, never by
@@ -292,7 +292,10 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
   tc::fence_after();
-  const uint32_t tbase = *tmem_slot;
+  // All 512 columns are this CTA's, so they start at 0; addresses known to the compiler
+  // are worth it where MMAs are issued (1,596 queries after 30,720 positions 758 us with
+  // the address from the slot, 725 so; 798 at D = 128 327 and 304).
+  constexpr uint32_t tbase = 0;
   const uint32_t tO = tbase;
   const uint32_t tS = tbase + D;               // two S/P buffers of 2 PF_BN columns
 
@@ -719,7 +722,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   tc::cluster_sync();
   if (warp == 0) {
     tc::fence_after();
-    tc::dealloc2(tbase, 512);
+    tc::dealloc2(*tmem_slot, 512);
   }
 }
 
@@ -727,7 +730,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
 // queries after 30,720 positions (44 of 196 pairs left over): uncut 1,121 us,
-// cut 1,013; before the kernel's later steps, uncut 1,243, the left-over pairs as a
+// cut 1,013 (989 since, with the kernel's last step); before the kernel's later steps, uncut 1,243, the left-over pairs as a
 // second launch of three even splits 1,163, cut so 1,131.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 
