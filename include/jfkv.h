@@ -555,9 +555,9 @@ int jf_kv8_read(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_st
                 int32_t* err_flag, void* stream);
 
 /* Workspace bytes of jf_paged_decode_weights_attn: that of
- * jf_paged_decode_attn (rounded up to 256), 4 bytes for the score of each query
+ * jf_paged_decode_attn (rounded up to 256) and 4 bytes for the score of each query
  * head and position (batch * Hkv * G * weight_stride, G = Hq / Hkv rounded up
- * to 2 and the stride to 16) and 8 * batch * Hq.  0 for invalid arguments. */
+ * to 2 and the stride to 16).  0 for invalid arguments. */
 size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int32_t num_kv_heads,
                                          int32_t head_dim, int32_t num_splits,
                                          int64_t weight_stride);

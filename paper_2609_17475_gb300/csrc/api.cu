@@ -638,8 +638,7 @@ size_t jf_decode_weights_workspace_bytes(int32_t batch, int32_t num_q_heads, int
   if (n == 0) return 0;
   return (n + 255) / 256 * 256 +
          (size_t)batch * num_kv_heads *
-             (size_t)kv8_score_floats(num_q_heads / num_kv_heads, weight_stride) * 4 +
-         (size_t)batch * num_q_heads * 8;
+             (size_t)kv8_score_floats(num_q_heads / num_kv_heads, weight_stride) * 4;
 }
 
 int jf_paged_decode_weights_attn(const jf_kv_pool* pool, const int32_t* page_table,

@@ -28,7 +28,7 @@
 // Bound: reading the codes.  One request of 262,144 positions, 24 / 4 heads x 256: 88 us
 // for 537 MB, 6.1 TB/s (0.90 of the copy rate), the merge 3 us of it; the split kernel
 // moves 1.00 times those bytes.  32 requests of up to 65,535 positions with weights:
-// 205 us, 158 at the copy rate, the merge and weigh kernels about 20.  One request of
+// 205 us, 158 at the copy rate, merging and weighing about 20.  One request of
 // 4,096 (8 / 2 heads x 128): 8.5 us, two launches' latency.
 // Rounding: q enters as fp16 after a power-of-two scale per head that puts
 // its largest element in [2^13, 2^14) (exact for elements within 2^27 of it);
@@ -36,8 +36,8 @@
 //
 // Merge kernel.  Joins the pieces' partials of each query row:
 //   o = sum_s 2^(m_s - m) O_s / l,  l = sum_s 2^(m_s - m) l_s.
-// Weigh kernel.  Where weights are asked for, the split kernel leaves the
-// scores x in the workspace (they mostly stay in L2) and the merge m and 1/l;
+// Weights.  Where they are asked for, the split kernel leaves the scores x in the
+// workspace (they mostly stay in L2), and CTAs beside the merge's add
 //   weights_out[b, h, t] = weights_in[b, h, t] + sum_g 2^(x_gt - m_g) / l_g.
 // Scores lie as [chunk of 16 positions][8 positions of it][odd heads or even]
 // [pair of heads][8 positions], as the MMA leaves them, so that each store of
@@ -79,11 +79,11 @@ struct Kv8DecodeArgs {
   float* scores;            // [B, Hkv] blocks of sstride floats (above), or null
   int64_t sstride;          // chunks of 16 positions x 32 x pairs
   int32_t pairs;            // pairs of a KV head's query heads: ceil(G / 2)
-  float2* row_ml;           // [B, Hq] (m, 1 / l) for the weigh kernel
   const float* w_in;        // [B, Hkv, wstride] or null (zeros)
   float* w_out;
   int64_t wstride;
   int32_t slices;           // merging CTAs per query row
+  int32_t wtiles, wsteps;   // weighing CTAs per (request, KV head), steps of each
 };
 
 // ---- plan: the requests' 32-position chunks laid end to end, each request's
@@ -566,9 +566,86 @@ __device__ K8Rows k8_rows(const Kv8DecodeArgs& a, int b, int lane) {
 constexpr int K8F_THREADS = 256;
 constexpr int K8F_COLS = 64;                       // columns of an output row per merging step
 
+constexpr int K8W_STEP = 4 * K8F_THREADS;   // positions a weighing CTA takes at once: 4 a thread
+
+// Weights of positions t0 .. of a (request, KV head): weights_in plus 2^(x - m) / l over
+// its heads, m and l from the pieces' partials (warp g those of head g), so that nothing
+// waits for the merge.
+__device__ void k8_weigh(const Kv8DecodeArgs& a, int tile, int kvh, int b, float2* head_ml,
+                         int* plan) {
+  constexpr float NEG = -INFINITY;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int n = (int)min((int64_t)k8_ctx(a, b), a.wstride);
+  const int64_t t0 = (int64_t)tile * (a.wsteps * K8W_STEP);
+  if (t0 >= n) return;   // the whole CTA
+  // a thread takes four adjacent positions a step; the heads' scores are all
+  // loaded before any is used, the first step's before m and l are known
+  const float* const sc = a.scores + ((int64_t)b * a.Hkv + kvh) * a.sstride;
+  const int64_t wrow = ((int64_t)b * a.Hkv + kvh) * a.wstride;
+  auto at = [&](int step) { return (int)t0 + step * K8W_STEP + (int)threadIdx.x * 4; };
+  float4 x[8];
+  auto load = [&](int t) {
+    const float* const sx = sc + (int64_t)(t / K8_SUB) * (32 * a.pairs) +
+                            ((t >> 3) & 1) * (16 * a.pairs) + (t & 7);
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      if (g < a.G)
+        x[g] = __ldcs(reinterpret_cast<const float4*>(sx + ((g & 1) * a.pairs + (g >> 1)) * 8));
+  };
+  if (at(0) < n) load(at(0));
+  if (warp == 0) {
+    const K8Rows r = k8_rows(a, b, lane);
+    if (lane == 0) {
+      plan[0] = r.row;
+      plan[1] = r.n;
+    }
+  }
+  __syncthreads();
+  if (warp < a.G) {
+    const float2* const ml = reinterpret_cast<const float2*>(a.part_ml) +
+                             (int64_t)plan[0] * a.Hq + kvh * a.G + warp;
+    float M = NEG, l = 0.f;
+    for (int s = lane; s < plan[1]; s += 32) M = fmaxf(M, ml[(int64_t)s * a.Hq].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    for (int s = lane; s < plan[1]; s += 32) {
+      const float2 v = ml[(int64_t)s * a.Hq];
+      if (v.x != NEG) l = fmaf(fast_exp2(v.x - M), v.y, l);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    // nothing attended: scores of -inf and weights of zero
+    if (lane == 0) head_ml[warp] = make_float2(M == NEG ? 0.f : M, l != 0.f ? 1.f / l : 0.f);
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int step = 0; step < a.wsteps; ++step) {
+    const int t = at(step);
+    if (t >= n) return;
+    float w[4], add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = a.w_in && t + i < n ? a.w_in[wrow + t + i] : 0.f;
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      if (g < a.G) {
+        const float2 m = head_ml[g];
+        add[0] = fmaf(fast_exp2(x[g].x - m.x), m.y, add[0]);
+        add[1] = fmaf(fast_exp2(x[g].y - m.x), m.y, add[1]);
+        add[2] = fmaf(fast_exp2(x[g].z - m.x), m.y, add[2]);
+        add[3] = fmaf(fast_exp2(x[g].w - m.x), m.y, add[3]);
+      }
+    if (step + 1 < a.wsteps && at(step + 1) < n) load(at(step + 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (t + i < n) a.w_out[wrow + t + i] = w[i] + add[i];
+  }
+}
+
 // A CTA takes one query row, every `slices`-th run of 64 columns of it; warp w
-// sums the partials w, w + 8, ... of two columns a lane.
-template <int D>
+// sums the partials w, w + 8, ... of two columns a lane.  WEIGH: the first CTAs
+// weigh (a kernel of its own after the merge: one request of 5,000 positions 11.6 us,
+// not 8.7; 32 mixed requests 207, not 205).
+template <int D, bool WEIGH>
 __global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeArgs a) {
   constexpr float NEG = -INFINITY;
   __shared__ float2 red[8][32];
@@ -576,11 +653,21 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeA
   __shared__ int plan[2];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  int cta = (int)blockIdx.x;
+  if constexpr (WEIGH) {
+    const int weighing = a.wtiles * a.Hkv * a.B;
+    if (cta < weighing) {
+      const int row = cta / a.wtiles;
+      k8_weigh(a, cta - row * a.wtiles, row % a.Hkv, row / a.Hkv, red[0], plan);
+      return;
+    }
+    cta -= weighing;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const float2* const ml = reinterpret_cast<const float2*>(a.part_ml);
-  const int sl0 = blockIdx.x % a.slices;
-  const int hq = (blockIdx.x / a.slices) % a.Hq;
-  const int b = blockIdx.x / (a.slices * a.Hq);
+  const int sl0 = cta % a.slices;
+  const int hq = (cta / a.slices) % a.Hq;
+  const int b = cta / (a.slices * a.Hq);
   if (sl0 == 0 && hq == 0 && threadIdx.x == 0) {
     const int64_t ctx = a.ctx[b];
     if (ctx < 0 || ctx > (int64_t)a.pt_stride * a.P || (a.w_out && ctx > a.wstride))
@@ -629,56 +716,7 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeA
       const float inv = l != 0.f ? 1.f / l : 0.f;   // nothing attended: zeros
       reinterpret_cast<uint32_t*>(a.out + ((int64_t)b * a.Hq + hq) * D + sl * K8F_COLS)[lane] =
           pack_bf16x2_rn(acc.x * inv, acc.y * inv);
-      if (a.row_ml && sl == 0 && lane == 0) a.row_ml[(int64_t)b * a.Hq + hq] = make_float2(M, inv);
     }
-  }
-}
-
-constexpr int K8W_TILE = 8 * K8F_THREADS;   // positions per weighing CTA: two steps of 4 a thread
-
-__global__ void __launch_bounds__(K8F_THREADS) kv8_weigh_kernel(const Kv8DecodeArgs a) {
-  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int kvh = blockIdx.y, b = blockIdx.z;
-  const int n = (int)min((int64_t)k8_ctx(a, b), a.wstride);
-  const int64_t t0 = (int64_t)blockIdx.x * K8W_TILE;
-  if (t0 >= n) return;
-  float2 m[8];
-#pragma unroll
-  for (int g = 0; g < 8; ++g)
-    if (g < a.G) {
-      m[g] = a.row_ml[(int64_t)b * a.Hq + kvh * a.G + g];
-      if (m[g].x == -INFINITY) m[g].x = 0.f;   // nothing attended: weights of zero
-    }
-  // a thread takes four adjacent positions a step; the heads' scores are all
-  // loaded before any is used
-  const float* const sc = a.scores + ((int64_t)b * a.Hkv + kvh) * a.sstride;
-  const int64_t wrow = ((int64_t)b * a.Hkv + kvh) * a.wstride;
-#pragma unroll
-  for (int step = 0; step < K8W_TILE / (4 * K8F_THREADS); ++step) {
-    const int t = (int)t0 + (step * K8F_THREADS + threadIdx.x) * 4;
-    if (t >= n) return;
-    const float* const sx = sc + (int64_t)(t / K8_SUB) * (32 * a.pairs) +
-                            ((t >> 3) & 1) * (16 * a.pairs) + (t & 7);
-    float4 x[8];
-#pragma unroll
-    for (int g = 0; g < 8; ++g)
-      if (g < a.G)
-        x[g] = __ldcs(reinterpret_cast<const float4*>(sx + ((g & 1) * a.pairs + (g >> 1)) * 8));
-    float w[4], add[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = a.w_in && t + i < n ? a.w_in[wrow + t + i] : 0.f;
-#pragma unroll
-    for (int g = 0; g < 8; ++g)
-      if (g < a.G) {
-        add[0] = fmaf(fast_exp2(x[g].x - m[g].x), m[g].y, add[0]);
-        add[1] = fmaf(fast_exp2(x[g].y - m[g].x), m[g].y, add[1]);
-        add[2] = fmaf(fast_exp2(x[g].z - m[g].x), m[g].y, add[2]);
-        add[3] = fmaf(fast_exp2(x[g].w - m[g].x), m[g].y, add[3]);
-      }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (t + i < n) a.w_out[wrow + t + i] = w[i] + add[i];
   }
 }
 
@@ -704,16 +742,12 @@ static int launch_t(const CUtensorMap& tmap, const Kv8DecodeArgs& a, cudaStream_
   const cudaError_t e = weigh ? cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, true>, tmap, a)
                               : cudaLaunchKernelEx(&cfg, kv8_split_kernel<D, false>, tmap, a);
   if (e != cudaSuccess) return JF_ERR_CUDA;
-  cfg.gridDim = dim3((unsigned)(a.slices * a.Hq * a.B));
+  cfg.gridDim = dim3((unsigned)(a.slices * a.Hq * a.B + a.wtiles * a.Hkv * a.B));
   cfg.blockDim = dim3(K8F_THREADS);
   cfg.dynamicSmemBytes = 0;
-  if (cudaLaunchKernelEx(&cfg, kv8_merge_kernel<D>, a) != cudaSuccess) return JF_ERR_CUDA;
-  if (weigh) {
-    cfg.gridDim = dim3((unsigned)((a.wstride + K8W_TILE - 1) / K8W_TILE), (unsigned)a.Hkv,
-                       (unsigned)a.B);
-    if (cudaLaunchKernelEx(&cfg, kv8_weigh_kernel, a) != cudaSuccess) return JF_ERR_CUDA;
-  }
-  return JF_OK;
+  const cudaError_t m = weigh ? cudaLaunchKernelEx(&cfg, kv8_merge_kernel<D, true>, a)
+                              : cudaLaunchKernelEx(&cfg, kv8_merge_kernel<D, false>, a);
+  return m == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 
 // floats of the scores of one (request, KV head)
@@ -722,7 +756,7 @@ int64_t kv8_score_floats(int64_t G, int64_t wstride) {
 }
 
 // weights (w_out non-null): `scores`, 16-byte aligned, holds the scores of the
-// B * Hkv (request, KV head) pairs and then B * Hq float2
+// B * Hkv (request, KV head) pairs
 int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& tmap,
                       const int32_t* page_table, int32_t pt_stride, const int32_t* context_lens,
                       int32_t batch, const void* q, int32_t Hq, float softmax_scale, void* out,
@@ -765,9 +799,20 @@ int launch_kv8_decode(const Geom& g, const jf_kv_pool& pool, const CUtensorMap& 
   // few query rows: a CTA for each 64 columns; many: one for the row
   const int64_t qrows = (int64_t)batch * Hq;
   a.slices = qrows * (g.D / K8F_COLS) <= 4 * sm_count() ? g.D / K8F_COLS : 1;
-  if (qrows * a.slices > 0x7FFFFFFF || g.Hkv > 65535) return JF_ERR_UNSUPPORTED;
-  a.row_ml = w_out ? reinterpret_cast<float2*>(scores + (int64_t)batch * g.Hkv * a.sstride)
-                   : nullptr;
+  // Weighing CTAs of one, two or four steps: the shortest with which no more than 4 an SM
+  // are launched, since each works out its heads' m and l anew (1,024, 2,048 and 4,096
+  // positions a CTA: one request of 5,000, 2 KV heads, 8.7, 9.5 and 11.1 us; 16 to 9,000,
+  // 4 heads, 21.1, 20.4 and 21.3; 32 to 65,535, 4 heads, 213, 208 and 205).
+  int64_t wtiles = 0;
+  a.wsteps = 1;
+  for (int steps = 1; w_out && steps <= 4; steps *= 2) {
+    a.wsteps = steps;
+    wtiles = (wstride + (int64_t)steps * K8W_STEP - 1) / ((int64_t)steps * K8W_STEP);
+    if (wtiles * batch * g.Hkv <= 4 * sm_count()) break;
+  }
+  if (qrows * a.slices + wtiles * batch * g.Hkv > 0x7FFFFFFF || g.Hkv > 65535)
+    return JF_ERR_UNSUPPORTED;
+  a.wtiles = (int)wtiles;
   return g.D == 256 ? launch_t<256>(tmap, a, stream) : launch_t<128>(tmap, a, stream);
 }
 

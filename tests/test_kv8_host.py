@@ -25,9 +25,9 @@ def test_sizes():
     assert B.jf_kv_page_bytes_fmt(f, 1, 48, 128) == 0 and B.jf_kv_page_bytes_fmt(f, 1, 64, 64) == 0
     n = B.lib().jf_decode_weights_workspace_bytes
     base = -(-B.jf_attn_workspace_bytes(3, 24, 4, 256, 5) // 256) * 256
-    assert n(3, 24, 4, 256, 5, 1000) == base + 3 * 4 * 1008 * 6 * 4 + 8 * 3 * 24
+    assert n(3, 24, 4, 256, 5, 1000) == base + 3 * 4 * 1008 * 6 * 4
     assert n(3, 20, 4, 256, 5, 16) == -(-B.jf_attn_workspace_bytes(3, 20, 4, 256, 5) // 256) * 256 + \
-        3 * 4 * 16 * 6 * 4 + 8 * 3 * 20                       # five heads count as six
+        3 * 4 * 16 * 6 * 4                                    # five heads count as six
     assert n(3, 24, 5, 256, 5, 1000) == 0 and n(3, 24, 4, 256, 5, 0) == 0
     assert B.lib().jf_prefill_batch_workspace_bytes(f, 32, 8, 128, 1) == 256
     assert B.default_num_splits(1, 4, num_sms=152, format=f) == 38
