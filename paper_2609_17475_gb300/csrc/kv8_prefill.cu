@@ -126,10 +126,13 @@ __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
 // largest x of the LPR lanes that hold a row
 template <int LPR>
 __device__ __forceinline__ uint32_t row_max(uint32_t x) {
-  if (LPR == 32) return __reduce_max_sync(0xffffffffu, x);
+  if constexpr (LPR == 32) {
+    return __reduce_max_sync(0xffffffffu, x);
+  } else {
 #pragma unroll
-  for (int o = LPR / 2; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
+    for (int o = LPR / 2; o > 0; o >>= 1) x = max(x, __shfl_xor_sync(0xffffffffu, x, o));
+    return x;
+  }
 }
 // bf16 bits of the largest finite magnitude of a row (rows that hold infinities or NaN)
 template <int LPR>
@@ -157,6 +160,12 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   using L = P8Smem<D>;
   constexpr uint32_t IDQK = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
   constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
+  // S/P buffers of 2 PF_BN columns: what O leaves of the 512.  S of pair i is issued before
+  // P V of pair i - AHEAD, so that the softmax of a pair may run while the P V of AHEAD
+  // pairs before it are outstanding: a barrier for each tile of NSB pairs, or an arrival
+  // (pv_ready) or a wait (pv_done) would meet the phase before its own.
+  constexpr int NSB = (512 - D) / (2 * PF_BN), AHEAD = NSB - 1, PVR = 2 * NSB;
+  static_assert(PVR <= 6, "barriers");
 
   extern __shared__ uint8_t smraw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) &
@@ -173,16 +182,16 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // On CTA 0, where the pair's MMAs are issued:
   uint64_t* const k_full = bars + 0;     // [3] both CTAs' K halves of a pair have landed
-  uint64_t* const pv_ready = bars + 3;   // [4] both CTAs' V halves and P of tile j % 4 stored
+  uint64_t* const pv_ready = bars + 3;   // [PVR] both CTAs' V halves and P of tile j % PVR stored
   // on each CTA:
-  uint64_t* const k_land = bars + 7;     // [3] CTA 1: its K halves have landed
-  uint64_t* const s_full = bars + 10;    // [3] S of pair i % 3 done (its K buffer is free)
-  uint64_t* const pv_done = bars + 13;   // [4] P V of tile j % 4 done
-  uint64_t* const m_bar = bars + 17;     // [2 groups][4 quarters] the group's reference is set
-  uint64_t* const s_land = bars + 25;    // [4] staged V codes have landed
-  uint64_t* const s_free = bars + 29;    // [4] and been read by the 4 V warps
-  uint64_t* const q_ready = bars + 33;   // on CTA 0: both CTAs' Q rows stored
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 34);
+  uint64_t* const k_land = bars + 9;     // [3] CTA 1: its K halves have landed
+  uint64_t* const s_full = bars + 12;    // [3] S of pair i % 3 done (its K buffer is free)
+  uint64_t* const pv_done = bars + 15;   // [PVR] P V of tile j % PVR done
+  uint64_t* const m_bar = bars + 21;     // [2 groups][4 quarters] the group's reference is set
+  uint64_t* const s_land = bars + 29;    // [4] staged V codes have landed
+  uint64_t* const s_free = bars + 33;    // [4] and been read by the 4 V warps
+  uint64_t* const q_ready = bars + 37;   // on CTA 0: both CTAs' Q rows stored
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 38);
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
@@ -252,9 +261,11 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
     mbar_init(q_ready, 2 * 2 * PF_SM_WARPS);
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < PVR; ++i) {
       mbar_init(&pv_ready[i], 2 * (4 + PF_SM_WARPS));   // 4 V and 4 softmax warps of each CTA
       mbar_init(&pv_done[i], 1);
+    }
+    for (int i = 0; i < 4; ++i) {
       mbar_init(&m_bar[i], 1);
       mbar_init(&m_bar[4 + i], 1);
       mbar_init(&s_land[i], 1);
@@ -297,7 +308,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   // the address from the slot, 725 so; 798 at D = 128 327 and 304).
   constexpr uint32_t tbase = 0;
   const uint32_t tO = tbase;
-  const uint32_t tS = tbase + D;               // two S/P buffers of 2 PF_BN columns
+  const uint32_t tS = tbase + D;
 
   const int log2P = 31 - __clz(a.P);           // P is a power of two
   auto page_of = [&](int j) -> int {           // of tile j (P >= 64: a tile lies in one page)
@@ -368,17 +379,17 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       };
       // S of pair i (column n = K row n of CTA 0 for n < 64, row n - 64 of CTA 1
       // otherwise: position 32 rank + n % 32 of tile 2i + (n % 64) / 32), then P V of
-      // the previous pair's tiles
+      // the tiles of pair i - AHEAD
       int jn = 0;   // next tile whose P V is due
       ok = wait(q_ready, 0);
-      for (int i = 0; i <= npairs && ok; ++i) {
+      for (int i = 0; i < npairs + AHEAD && ok; ++i) {
         if (i < npairs) {
           const int kb = i % P8_KBUF;
           ok = wait(&k_full[kb], i / P8_KBUF);
           if (!ok) break;
           tc::fence_after();
           const uint64_t kd_i = kd + (uint64_t)(kb * (L::KP_BYTES >> 4));
-          const uint32_t d = tS + (i & 1) * (2 * PF_BN);
+          const uint32_t d = tS + (i % NSB) * (2 * PF_BN);
 #pragma unroll
           for (int ks = 0; ks < 2 * (D / 32); ++ks) {   // hi's steps, then lo's
             const int k = ks % (D / 32);
@@ -390,18 +401,18 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           }
           tc::commit2_both_if(leader, &s_full[kb]);
         }
-        for (const int upto = i < npairs ? 2 * i : ntiles; jn < upto; ++jn) {
+        for (const int upto = min(2 * (i - AHEAD + 1), ntiles); jn < upto; ++jn) {
           const int vb = jn % P8_VBUF;
-          ok = wait(&pv_ready[vb], jn / P8_VBUF);
+          ok = wait(&pv_ready[jn % PVR], jn / PVR);
           if (!ok) break;
           tc::fence_after();
           const uint64_t vd_j = vd + (uint64_t)(vb * (L::VT_BYTES >> 4));
-          const uint32_t tp = tS + ((jn >> 1) & 1) * (2 * PF_BN) + (jn & 1) * 32;
+          const uint32_t tp = tS + ((jn >> 1) % NSB) * (2 * PF_BN) + (jn & 1) * 32;
 #pragma unroll
           for (int k = 0; k < PF_BN / 16; ++k)
             tc::mma2_ts_if(leader, tO, tp + 8 * k, vd_j + ((k * 2048) >> 4), IDPV,
                            (jn > 0 || k > 0) ? 1u : 0u);
-          tc::commit2_both_if(leader, &pv_done[vb]);
+          tc::commit2_both_if(leader, &pv_done[jn % PVR]);
         }
       }
     } else if (rank == 1 && lane == 0) {
@@ -490,7 +501,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_free[sb]);
-      if (j >= P8_VBUF && !mbar_wait_bounded(&pv_done[vb], ((j / P8_VBUF) - 1) & 1)) {
+      if (j >= P8_VBUF && !mbar_wait_bounded(&pv_done[(j - P8_VBUF) % PVR],
+                                             ((j - P8_VBUF) / PVR) & 1)) {
         ok = false;
         break;
       }
@@ -503,7 +515,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
               make_uint4(f[u][4 * h], f[u][4 * h + 1], f[u][4 * h + 2], f[u][4 * h + 3]);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) tc::arrive_cluster(&pv_ready[vb], 0);
+      if (lane == 0) tc::arrive_cluster(&pv_ready[j % PVR], 0);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   } else {
@@ -536,7 +548,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       const int key0 = (jb + j) * PF_BN;
       // tile j's S: positions 0..31 in columns 32 (j & 1) .., 32..63 in columns
       // 64 + 32 (j & 1) .. of its pair's buffer; P_j goes to columns 32 (j & 1) ..
-      const uint32_t tb = tS + (pi & 1) * (2 * PF_BN) + group * 32 + lane_off;
+      const uint32_t tb = tS + (pi % NSB) * (2 * PF_BN) + group * 32 + lane_off;
       if (!mbar_wait_bounded(&s_full[pi % P8_KBUF], (pi / P8_KBUF) & 1)) { ok = false; break; }
       tc::fence_after();
       uint32_t p[32];
@@ -600,7 +612,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         m_use = need ? mt - P8_SET : m_ref;
         if (__any_sync(0xffffffffu, need) && j > 0) {
           const float f = (need && m_ref != -INFINITY) ? fast_exp2(m_ref - m_use) : 1.f;
-          if (!mbar_wait_bounded(&pv_done[(j - 1) % PF_KVBUF], ((j - 1) / PF_KVBUF) & 1)) {
+          if (!mbar_wait_bounded(&pv_done[(j - 1) % PVR], ((j - 1) / PVR) & 1)) {
             ok = false;
             break;
           }
@@ -630,7 +642,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       tc::wait_st();
       tc::fence_before();
       __syncwarp();
-      if (lane == 0) tc::arrive_cluster(&pv_ready[j % P8_VBUF], 0);
+      if (lane == 0) tc::arrive_cluster(&pv_ready[j % PVR], 0);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     s_ml[group * PF_BM + r] = make_float2(m_own, l);
@@ -658,8 +670,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
         for (int c = 0; c < D / 8; ++c) po[c] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
     } else if (all_ok &&
-               __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(ntiles - 1) % PF_KVBUF],
-                                                         ((ntiles - 1) / PF_KVBUF) & 1))) {
+               __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(ntiles - 1) % PVR],
+                                                         ((ntiles - 1) / PVR) & 1))) {
       tc::fence_after();
       const float m = s_m[r];   // after the last tile
       float lsum = 0.f;
