@@ -30,13 +30,14 @@
 //   warp 1       lane 0 loads this CTA's K halves (32 positions of each tile) by
 //                TMA into three pair buffers, and the 128 bytes of each V row that
 //                hold its half into four staging tiles
-//   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers
+//   warps 2-5    V halves (D/2 columns of each tile) -> fp16, four tile buffers (six at
+//                D = 128)
 //   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
 // Bound: the tensor core, at the clock its power allows.  1,596 queries after 30,720
-// positions (24 / 4 heads x 256, two full waves) 725 us, 1,705 TFLOP/s: 0.89 of the
-// bf16 burst rate, 0.99 of the sustained one.  At D = 128 a tile has half the products for
+// positions (24 / 4 heads x 256, two full waves) 711 us, 1,740 TFLOP/s: 0.91 of the
+// bf16 burst rate, 1.01 of the sustained one.  At D = 128 a tile has half the products for
 // the same exponentials, and the softmax warps set the pace: 798 queries so, one wave,
-// 1,005 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
+// 1,030 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
 // ways: 19.5 us of launches, Q's way in, eight tiles one after the other and the merge.
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
 // from TMEM behind a tcgen05 fence, or from this CTA's own shared memory, never by
@@ -52,7 +53,6 @@ int kv8_tensor_map(const Geom& g, void* base, int halves, int rows, int kv, CUte
 
 constexpr int P8_KBUF = 3;                 // K pair buffers
 constexpr int P8_SBUF = 4;                 // V staging tiles
-constexpr int P8_VBUF = 4;                 // V tile buffers
 constexpr int P8_V_WARP0 = 2, P8_SM_WARP0 = 6;
 constexpr int P8_THREADS = 32 * 14;
 constexpr float P8_TOP = 14.f;             // P stays below 2^14
@@ -65,8 +65,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 
 // Where a CTA's results go, kept in shared memory with the rows' places so that the
-// softmax loop holds none of it in registers (1,596 queries after 30,720 positions
-// 774 us with it there, 760 without).
+// softmax loop holds none of it in registers (1,596 queries after 30,720 positions,
+// when it was moved: 774 -> 760 us).
 struct P8Out {
   uint8_t* to;          // the output, or the partials O
   int32_t split;
@@ -83,7 +83,9 @@ struct P8Smem {
   static constexpr int OFF_K = 2 * Q_BYTES;
   static constexpr int OFF_V = OFF_K + P8_KBUF * KP_BYTES;
   static constexpr int VS_BYTES = PF_BN * 128;           // staged codes: [64 rows][128 B]
-  static constexpr int OFF_S = OFF_V + P8_VBUF * VT_BYTES;
+  static constexpr int NSB = (512 - D) / (2 * PF_BN);    // S/P buffers: what O leaves of TMEM
+  static constexpr int VBUF = 2 * NSB;                   // V tile buffers
+  static constexpr int OFF_S = OFF_V + VBUF * VT_BYTES;
   static constexpr int OFF_BAR = OFF_S + P8_SBUF * VS_BYTES;
   static constexpr int OFF_M = OFF_BAR + 512;            // [128] reference maxima
   static constexpr int OFF_L = OFF_M + PF_BM * 4;        // [2 groups][128] (m, l)
@@ -160,11 +162,11 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   using L = P8Smem<D>;
   constexpr uint32_t IDQK = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
   constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
-  // S/P buffers of 2 PF_BN columns: what O leaves of the 512.  S of pair i is issued before
-  // P V of pair i - AHEAD, so that the softmax of a pair may run while the P V of AHEAD
-  // pairs before it are outstanding: a barrier for each tile of NSB pairs, or an arrival
-  // (pv_ready) or a wait (pv_done) would meet the phase before its own.
-  constexpr int NSB = (512 - D) / (2 * PF_BN), AHEAD = NSB - 1, PVR = 2 * NSB;
+  // S of pair i is issued before P V of pair i - AHEAD, so that the softmax of a pair may
+  // run while the P V of AHEAD pairs before it are outstanding: V buffers and barriers for
+  // the tiles of NSB pairs, or an arrival (pv_ready) or a wait (pv_done) would meet the
+  // phase before its own.  798 queries at D = 128, three S/P buffers for two: 304 -> 296 us.
+  constexpr int NSB = L::NSB, AHEAD = NSB - 1, PVR = L::VBUF;
   static_assert(PVR <= 6, "barriers");
 
   extern __shared__ uint8_t smraw[];
@@ -402,8 +404,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           tc::commit2_both_if(leader, &s_full[kb]);
         }
         for (const int upto = min(2 * (i - AHEAD + 1), ntiles); jn < upto; ++jn) {
-          const int vb = jn % P8_VBUF;
-          ok = wait(&pv_ready[jn % PVR], jn / PVR);
+          const int vb = jn % PVR;
+          ok = wait(&pv_ready[vb], jn / PVR);
           if (!ok) break;
           tc::fence_after();
           const uint64_t vd_j = vd + (uint64_t)(vb * (L::VT_BYTES >> 4));
@@ -412,7 +414,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           for (int k = 0; k < PF_BN / 16; ++k)
             tc::mma2_ts_if(leader, tO, tp + 8 * k, vd_j + ((k * 2048) >> 4), IDPV,
                            (jn > 0 || k > 0) ? 1u : 0u);
-          tc::commit2_both_if(leader, &pv_done[jn % PVR]);
+          tc::commit2_both_if(leader, &pv_done[vb]);
         }
       }
     } else if (rank == 1 && lane == 0) {
@@ -481,7 +483,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     uint8_t* const dst = sV + (D == 256 ? part : 0) * (PF_BN * 128) + t * 128;
     const int piece0 = D == 256 ? 0 : 4 * part;
     for (int j = 0; j < ntiles; ++j) {
-      const int sb = j % P8_SBUF, vb = j % P8_VBUF;
+      const int sb = j % P8_SBUF, vb = j % PVR;
       if (!mbar_wait_bounded(&s_land[sb], (j / P8_SBUF) & 1)) { ok = false; break; }
       uint4 c[NLD];
 #pragma unroll
@@ -501,8 +503,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_free[sb]);
-      if (j >= P8_VBUF && !mbar_wait_bounded(&pv_done[(j - P8_VBUF) % PVR],
-                                             ((j - P8_VBUF) / PVR) & 1)) {
+      if (j >= PVR && !mbar_wait_bounded(&pv_done[vb], ((j / PVR) - 1) & 1)) {
         ok = false;
         break;
       }
@@ -515,7 +516,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
               make_uint4(f[u][4 * h], f[u][4 * h + 1], f[u][4 * h + 2], f[u][4 * h + 3]);
       fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) tc::arrive_cluster(&pv_ready[j % PVR], 0);
+      if (lane == 0) tc::arrive_cluster(&pv_ready[vb], 0);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   } else {
@@ -741,9 +742,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // The plan's estimate, in history tiles (0.8 us each at D = 256): a part beyond a
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
-// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,121 us,
-// cut 1,013 (989 since, with the kernel's last step); before the kernel's later steps, uncut 1,243, the left-over pairs as a
-// second launch of three even splits 1,163, cut so 1,131.
+// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,121 us, cut
+// 1,013 (990 with the kernel's later steps); with an earlier kernel uncut 1,243, the
+// left-over pairs as a second launch of three even splits 1,163, cut so 1,131.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 
 void kv8_prefill_plan(int64_t G, int64_t Hkv, int64_t q_start, int64_t chunk_len, bool causal,
