@@ -28,7 +28,7 @@
 // Bound: reading the codes.  One request of 262,144 positions, 24 / 4 heads x 256: 88 us
 // for 537 MB, 6.1 TB/s (0.90 of the copy rate), the merge 3 us of it; the split kernel
 // moves 1.00 times those bytes.  32 requests of up to 65,535 positions with weights:
-// 205 us, 158 at the copy rate, merging and weighing about 20.  One request of
+// 196 us, 158 at the copy rate, merging and weighing about 20.  One request of
 // 4,096 (8 / 2 heads x 128): 8.5 us, two launches' latency.
 // Rounding: q enters as fp16 after a power-of-two scale per head that puts
 // its largest element in [2^13, 2^14) (exact for elements within 2^27 of it);
@@ -54,7 +54,10 @@ constexpr int K8_CH = 32;       // positions per plan chunk
 constexpr int K8_SUB = 16;      // positions per pipeline stage
 constexpr int K8_NW = 12;       // warps per CTA, one CTA per SM (two of 6 warps share the SM
                                 // unevenly: one request of 262,144 positions 103 us, not 88)
-constexpr int K8_HDR = 8;       // plan places standing for a segment's start
+// plan places standing for a segment's start (32 requests to 65,535 with weights, with 8,
+// 16, 24, 32 and 48: 206, 200, 196, 196 and 196 us; 16 to 9,000 positions, 4 heads x 128:
+// 17.1, 17.2, 17.4, 18.9 and 17.9)
+constexpr int K8_HDR = 24;
 constexpr int K8_MIN_W = 6;     // least places per piece (one stage for each warp)
 constexpr float K8_TOP = 14.f;  // 2^(y - m) stays below 2^14
 constexpr float K8_SET = 10.f;  // a new m puts the largest y at 2^10
@@ -644,7 +647,7 @@ __device__ void k8_weigh(const Kv8DecodeArgs& a, int tile, int kvh, int b, float
 // A CTA takes one query row, every `slices`-th run of 64 columns of it; warp w
 // sums the partials w, w + 8, ... of two columns a lane.  WEIGH: the first CTAs
 // weigh (a kernel of its own after the merge: one request of 5,000 positions 11.6 us,
-// not 8.7; 32 mixed requests 207, not 205).
+// not 8.7; 32 mixed requests, then, 207, not 205).
 template <int D, bool WEIGH>
 __global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeArgs a) {
   constexpr float NEG = -INFINITY;
