@@ -742,8 +742,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // The plan's estimate, in history tiles (0.8 us each at D = 256): a part beyond a
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
-// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,121 us, cut
-// 1,013 (990 with the kernel's later steps); with an earlier kernel uncut 1,243, the
+// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,055 us, cut
+// 972 (967 to 974 with headers of 6 to 32); with an earlier kernel uncut 1,243, the
 // left-over pairs as a second launch of three even splits 1,163, cut so 1,131.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 
