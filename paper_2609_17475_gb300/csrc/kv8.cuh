@@ -82,11 +82,13 @@ __device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
 }
 template <int N>
 __device__ __forceinline__ void rescale_f16(uint32_t (&v)[N], int s) {
-  if (s > 15) {   // past fp16's powers of two: only subnormal codes get here
+  if (s > 15) {   // past fp16's powers of two
     const uint32_t p = f16x2_two(15);
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = mul_f16x2(v[i], p);
-    s -= 15;
+    // what is left: a code above zero is at least 2^-9 and its value at most 448, so s <= 17;
+    // zeros come with any s, and have to meet a finite power to stay zeros
+    s = min(s - 15, 15);
   }
   const uint32_t p = f16x2_two(s);
 #pragma unroll
