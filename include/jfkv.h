@@ -337,6 +337,7 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * the block scales are applied as in the decode; no scale is out of range.
  * A position a query does not see has the weight zero: a NaN among its values
  * (not its key) still reaches the queries of the chunk before it, as 0 * NaN.
+ * A query row that holds an infinity or a NaN gives NaN.
  */
 int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,
                           const void* q, int32_t q_start, int32_t chunk_len, int32_t num_q_heads,

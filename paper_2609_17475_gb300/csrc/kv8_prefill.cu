@@ -115,11 +115,6 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t x, uint32_t
                ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.bf16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
@@ -136,20 +131,6 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
     return x;
   }
 }
-// bf16 bits of the largest finite magnitude of a row (rows that hold infinities or NaN)
-template <int LPR>
-__device__ __noinline__ uint32_t finite_max(uint4 w) {
-  uint32_t mx = 0;
-  const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const uint32_t lo = ws[k] & 0x7FFFu, hi = (ws[k] >> 16) & 0x7FFFu;
-    if (lo < 0x7F80u) mx = max(mx, lo);
-    if (hi < 0x7F80u) mx = max(mx, hi);
-  }
-  return row_max<LPR>(mx);
-}
-
 struct P8NoPlan {};
 template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
 template <> struct P8PlanArg<false> { using type = P8NoPlan; };
@@ -328,11 +309,10 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     for (int i = 0; i < NI; ++i) {
       const int row = qr0 + i * RPI;
       const uint32_t ws[4] = {qv[i].x, qv[i].y, qv[i].z, qv[i].w};
-      uint32_t m2 = 0;                         // largest magnitudes, NaN apart
+      uint32_t m2 = 0;                         // largest magnitudes
 #pragma unroll
-      for (int k = 0; k < 4; ++k) m2 = max_bf16x2(m2, ws[k] & 0x7FFF7FFFu);
-      uint32_t mx = row_max<LPR>(max(m2 & 0xFFFFu, m2 >> 16));
-      if (__any_sync(0xffffffffu, mx >= 0x7F80u)) mx = finite_max<LPR>(qv[i]);
+      for (int k = 0; k < 4; ++k) m2 = __vmaxu2(m2, ws[k] & 0x7FFF7FFFu);   // bits in order
+      const uint32_t mx = row_max<LPR>(max(m2 & 0xFFFFu, m2 >> 16));
       if (qpiece == 0) s_x[row] = mx;
       float qs = two8(-q_exp(mx));
       if (a.scale_log2 < 0.f) qs = -qs;        // the scale's sign goes to Q
@@ -359,8 +339,11 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     __syncwarp();
     if (lane == 0) tc::arrive_cluster(q_ready, 0);
     asm volatile("bar.sync 1, %0;\n" ::"n"(2 * PF_SM_WARPS * 32) : "memory");   // s_x
-    smul = fabsf(a.scale_log2) * two8(q_exp(s_x[r]));
+    const uint32_t mx = s_x[r];
+    smul = fabsf(a.scale_log2) * two8(q_exp(mx));
     if (smul == 0.f) smul = 1.f;
+    // e4m3 has no infinity: a row that holds one, or a NaN, is NaN by its factor
+    if (mx >= 0x7F80u) smul = __uint_as_float(0x7FC00000u);
   }
 
   float m_own = -INFINITY, l = 0.f;   // softmax: the reference at this group's last tile
@@ -679,10 +662,11 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         const float2 v = s_ml[g * PF_BM + r];
-        if (v.x != -INFINITY) lsum = fmaf(v.y, fast_exp2(v.x - m), lsum);
+        // no reference: a sum of zero, or NaN where every score was
+        lsum = v.x == -INFINITY ? lsum + v.y : fmaf(v.y, fast_exp2(v.x - m), lsum);
       }
       if (out.split && row_at >= 0 && group == 0) {
-        a.part_ml[row_at * 2 + 0] = m;
+        a.part_ml[row_at * 2 + 0] = lsum == lsum ? m : 0.f;   // NaN: not to be taken for an empty range
         a.part_ml[row_at * 2 + 1] = lsum;
       }
       const float inv = lsum != 0.f ? 1.f / lsum : 0.f;

@@ -1,0 +1,121 @@
+"""Attention over the 8-bit cache for values out of the ordinary: elements that are no numbers, scores that are all
+zero, queries whose elements differ by many powers of two."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_17475_gb300 as jf
+from oracle import kv8 as O
+from tests import kv8_cases as C
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def prefill(L, table, pool, start, q, scale, splits=1, causal=True):
+    """The output [C, Hq, D] of one request's chunk q, through the chunk call or in `splits` history ranges."""
+    g, out = C.gpu_pool(L, pool), torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    if splits == 1:
+        ws = jf.prefill_chunk_workspace(g, start, q.shape[0], q.shape[1])
+        jf.jf_prefill_chunk_attn(g, C.ints(table)[0], C.bf16(q), start, scale, causal, out, ws)
+    else:
+        ws = jf.prefill_batch_workspace(q.shape[0], q.shape[1], L.D, splits, format=jf.JF_FMT_E4M3_B32)
+        ws[256:] = 0xFF
+        jf.jf_prefill_batch_attn(g, C.ints(table), [start], [q.shape[0]], C.bf16(q), scale, causal, out, ws, splits)
+    assert jf.workspace_status(ws) == 0
+    return out.double().cpu().numpy()
+
+
+def decode(L, table, pool, ctx, q, scale, splits, weigh=False):
+    g, B = C.gpu_pool(L, pool), len(ctx)
+    out, w = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device=DEV), None
+    if weigh:
+        w = torch.zeros(B, L.Hkv, max(ctx), device=DEV)
+        ws = jf.decode_weights_workspace(B, q.shape[1], L.Hkv, L.D, splits, max(ctx))
+        ws[256:] = 0
+        jf.jf_paged_decode_weights_attn(g, C.ints(table), C.ints(ctx), C.bf16(q), scale, out, None, w, ws, splits)
+        w = w.double().cpu().numpy()
+    else:
+        ws = jf.decode_workspace(B, q.shape[1], L.Hkv, L.D, splits)
+        jf.jf_paged_decode_attn(g, C.ints(table), C.ints(ctx), C.bf16(q), scale, out, ws, splits)
+    assert jf.workspace_status(ws) == 0
+    return out.double().cpu().numpy(), w
+
+
+def queries(rng, *shape):
+    return torch.from_numpy(rng.standard_normal(shape)).bfloat16().double().numpy()
+
+
+# --------------------------------------------------------------------------
+# elements that are no numbers
+# --------------------------------------------------------------------------
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("hq,hkv,d,start,splits", [(4, 2, 128, 200, 1), (6, 1, 256, 500, 1), (4, 2, 128, 300, 3),
+                                                   (6, 1, 256, 300, 4)])
+def test_prefill_of_a_query_that_is_no_number(bad, hq, hkv, d, start, splits):
+    """A query row with an infinity or a NaN has no softmax: its output is NaN throughout, whatever the split; the
+    other rows' outputs are those of the chunk without it."""
+    rng = np.random.default_rng(d + splits)
+    c = 40
+    L, table, pool = C.filled(rng, hkv, 64, d, [start + c])
+    q = queries(rng, c, hq, d)
+    want = prefill(L, table, pool, start, q, 0.1, splits)
+    assert np.isfinite(want).all()
+    rows = [(0, 0, 0), (7, hq - 1, d - 1), (39, 1, 17)]
+    hit = np.zeros((c, hq), dtype=bool)
+    for i, h, j in rows:
+        q[i, h, j] = bad
+        hit[i, h] = True
+    got = prefill(L, table, pool, start, q, 0.1, splits)
+    assert np.isnan(got[hit]).all()
+    assert np.array_equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("bad", [math.inf, math.nan])
+def test_prefill_of_a_query_that_is_no_number_in_a_divided_wave(bad):
+    """The same where a chunk's last pairs have their histories in parts (80 pairs: 4 left over)."""
+    rng = np.random.default_rng(5)
+    hq, hkv, d, p, start, c = 24, 4, 256, 256, 3400, 840
+    pages = -(-(start + c) // p)
+    g = jf.KVPool.allocate(pages, p, hkv, d, format=jf.JF_FMT_E4M3_B32)
+    table = C.ints(rng.permutation(pages)[None])
+    torch.manual_seed(1)
+    x = [torch.randn(start + c, hkv, d, device=DEV).bfloat16() for _ in range(2)]
+    jf.jf_kv8_append(g, table, C.ints([0]), C.ints([0, start + c]), *x)
+    q = torch.randn(c, hq, d, device=DEV).bfloat16()
+    ws = jf.prefill_chunk_workspace(g, start, c, hq)
+    assert ws.numel() > 256
+    outs = []
+    hit = torch.zeros(c, hq, dtype=torch.bool, device=DEV)
+    for i in (0, 3, 400, 839):       # the parts hold the first rows of the chunk
+        hit[i, i % hq] = True
+    for poison in (False, True):
+        if poison:
+            for i, h in hit.nonzero().tolist():
+                q[i, h, 5] = bad
+        out = torch.full_like(q, 7.0)
+        jf.jf_prefill_chunk_attn(g, table[0], q, start, 1 / 16, True, out, ws)
+        assert jf.workspace_status(ws) == 0
+        outs.append(out)
+    assert torch.isnan(outs[1][hit]).all() and torch.equal(outs[1][~hit], outs[0][~hit])
+
+
+@pytest.mark.parametrize("splits", [1, 3])
+def test_prefill_of_keys_that_are_no_numbers(splits):
+    """Keys that are NaN reach every query that sees one, and no other, also where a whole range of them is."""
+    rng = np.random.default_rng(6)
+    hq, hkv, d, start, c = 4, 2, 128, 250, 40
+    L, table, pool = C.filled(rng, hkv, 64, d, [start + c])
+    q = queries(rng, c, hq, d)
+    want = prefill(L, table, pool, start, q, 0.1, splits)
+    for t0, t1 in ((270, 271), (0, 290)):                  # one key; all of them
+        p = pool.copy()
+        codes, _ = L.views(p)
+        for t in range(t0, t1):
+            p[table[0, t // 64], (t % 64) * d + 3] = 0x7F      # KV head 0's key
+        got = prefill(L, table, p, start, q, 0.1, splits)
+        sees = start + np.arange(c) >= t0
+        assert np.isnan(got[sees][:, :2]).all()
+        assert np.array_equal(got[:, 2:], want[:, 2:]) and np.array_equal(got[~sees], want[~sees])
