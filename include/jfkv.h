@@ -236,7 +236,8 @@ int jf_kv_quantize_append(const jf_kv_pool* pool, const int32_t* page_table, int
  * scale per head; block scales are applied to the fp32 scores and, as
  * exponents, to the probabilities before they enter fp16 (rounded relative to
  * the largest of 2^score * V scale met so far, so blocks of very different
- * scales keep their precision); no V scale is out of range.
+ * scales keep their precision); no V scale is out of range.  A query row that
+ * holds an infinity or a NaN gives NaN, and so do its KV head's weights.
  */
 int jf_paged_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
                          const int32_t* context_lens, int32_t batch, const void* q,

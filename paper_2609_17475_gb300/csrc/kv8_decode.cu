@@ -397,7 +397,7 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
       const bool head_ok = r < a.G;
       const uint16_t* qrow = a.q + ((int64_t)b * a.Hq + kvh * a.G + (head_ok ? r : 0)) * D;
       uint4 qv[D / 64][2];
-      uint32_t mx = 0;
+      uint32_t mx = 0;   // largest magnitude's bf16 bits
 #pragma unroll
       for (int i = 0; i < D / 64; ++i)
 #pragma unroll
@@ -406,11 +406,8 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
                              : make_uint4(0u, 0u, 0u, 0u);
           const uint32_t w[4] = {qv[i][e].x, qv[i][e].y, qv[i][e].z, qv[i][e].w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = w[k] & 0x7FFFu, hi = (w[k] >> 16) & 0x7FFFu;
-            if (lo < 0x7F80u) mx = max(mx, lo);
-            if (hi < 0x7F80u) mx = max(mx, hi);
-          }
+          for (int k = 0; k < 4; ++k)
+            mx = max(mx, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
         }
       mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
       mx = max(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
@@ -427,7 +424,8 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
             qf[4 * i + 2 * e + (k >> 1)][k & 1] =
                 pack_f16x2(bf16lo_to_f32(w[k]) * qs, bf16hi_to_f32(w[k]) * qs);
         }
-      const float mine = a.scale_log2 * two8(qe);
+      // a head with an infinity or a NaN is NaN by its factor, whatever the keys
+      const float mine = mx >= 0x7F80u ? __uint_as_float(0x7FC00000u) : a.scale_log2 * two8(qe);
       cA0 = __shfl_sync(0xffffffffu, mine, 8 * c);       // lane of head 2c: r = 2c, c = 0
       cA1 = __shfl_sync(0xffffffffu, mine, 8 * c + 4);
     }
@@ -532,8 +530,8 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
 #pragma unroll
       for (int w = 0; w < K8_NW; ++w) {
         const float2 ml = sml[w * 8];
-        if (ml.x == NEG) continue;   // this warp saw no position
-        const float f = fast_exp2(ml.x - M);
+        // no reference: this warp saw no position (l and O are zero), or NaN scores alone
+        const float f = ml.x == NEG ? ml.y : fast_exp2(ml.x - M);
         const float4 o = *reinterpret_cast<const float4*>(
             reinterpret_cast<const float*>(smem + w * L::WARP) + g * L::SROW + d);
         lsum = fmaf(f, ml.y, lsum);
@@ -613,7 +611,7 @@ __device__ void k8_weigh(const Kv8DecodeArgs& a, int tile, int kvh, int b, float
     for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
     for (int s = lane; s < plan[1]; s += 32) {
       const float2 v = ml[(int64_t)s * a.Hq];
-      if (v.x != NEG) l = fmaf(fast_exp2(v.x - M), v.y, l);
+      l = fmaf(v.x == NEG ? v.y : fast_exp2(v.x - M), v.y, l);   // v.y is 0 or NaN there
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -698,7 +696,7 @@ __global__ void __launch_bounds__(K8F_THREADS) kv8_merge_kernel(const Kv8DecodeA
       const float2 v = ml[row];
       const float2 o =
           *reinterpret_cast<const float2*>(a.part_o + row * D + sl * K8F_COLS + 2 * lane);
-      const float f = v.x == NEG ? 0.f : fast_exp2(v.x - M);
+      const float f = v.x == NEG ? v.y : fast_exp2(v.x - M);   // v.y is 0 or NaN there
       l = fmaf(f, v.y, l);
       acc.x = fmaf(f, o.x, acc.x);
       acc.y = fmaf(f, o.y, acc.y);

@@ -119,3 +119,41 @@ def test_prefill_of_keys_that_are_no_numbers(splits):
         sees = start + np.arange(c) >= t0
         assert np.isnan(got[sees][:, :2]).all()
         assert np.array_equal(got[:, 2:], want[:, 2:]) and np.array_equal(got[~sees], want[~sees])
+
+
+@pytest.mark.parametrize("weigh", [False, True])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("hq,hkv,d,ctx,splits", [(4, 2, 128, [200, 1, 17], 1), (6, 1, 256, [5000, 64, 3], 9)])
+def test_decode_of_a_query_that_is_no_number(weigh, bad, hq, hkv, d, ctx, splits):
+    """A head with an infinity or a NaN has no softmax: its output and its KV head's weights are NaN; the other heads'
+    are those of the call without it."""
+    rng = np.random.default_rng(d)
+    L, table, pool = C.filled(rng, hkv, 64, d, ctx)
+    q = queries(rng, len(ctx), hq, d)
+    want, w0 = decode(L, table, pool, ctx, q, 0.1, splits, weigh)
+    hit = np.zeros((len(ctx), hq), dtype=bool)
+    for b, h, j in ((0, hq - 1, 5), (1, 0, d - 1), (2, 1, 0)):
+        q[b, h, j] = bad
+        hit[b, h] = True
+    got, w = decode(L, table, pool, ctx, q, 0.1, splits, weigh)
+    assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], want[~hit])
+    if weigh:
+        kv = hit.reshape(len(ctx), hkv, -1).any(-1)
+        for b, n in enumerate(ctx):
+            assert np.isnan(w[b, kv[b], :n]).all() and np.array_equal(w[b, ~kv[b], :n], w0[b, ~kv[b], :n])
+
+
+@pytest.mark.parametrize("ctx,bad", [(1, [0]), (40, range(40)), (3000, [2999]), (3000, range(3000)),
+                                     (3000, range(512, 1024))])
+@pytest.mark.parametrize("splits", [1, 8])
+def test_decode_of_keys_that_are_no_numbers(ctx, bad, splits):
+    """Keys that are NaN make their KV head's outputs NaN, however many of them a warp or a piece holds."""
+    rng = np.random.default_rng(ctx)
+    hq, hkv, d = 4, 2, 128
+    L, table, pool = C.filled(rng, hkv, 64, d, [ctx])
+    q = queries(rng, 1, hq, d)
+    want, _ = decode(L, table, pool, [ctx], q, 0.1, splits)
+    for t in bad:
+        pool[table[0, t // 64], (t % 64) * d + 3] = 0x7F       # KV head 0's key
+    got, _ = decode(L, table, pool, [ctx], q, 0.1, splits)
+    assert np.isnan(got[0, :2]).all() and np.array_equal(got[0, 2:], want[0, 2:])
