@@ -341,7 +341,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     asm volatile("bar.sync 1, %0;\n" ::"n"(2 * PF_SM_WARPS * 32) : "memory");   // s_x
     const uint32_t mx = s_x[r];
     smul = fabsf(a.scale_log2) * two8(q_exp(mx));
-    if (smul == 0.f) smul = 1.f;
+    // the factor stays positive under a block's smallest scale, 2^-40: the -inf of positions
+    // not seen, times zero, would be NaN.  2^-86 moves no score by more than 2^-20.
+    if (smul < 0x1p-86f) smul = 0x1p-86f;
     // e4m3 has no infinity: a row that holds one, or a NaN, is NaN by its factor
     if (mx >= 0x7F80u) smul = __uint_as_float(0x7FC00000u);
   }

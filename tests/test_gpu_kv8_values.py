@@ -157,3 +157,27 @@ def test_decode_of_keys_that_are_no_numbers(ctx, bad, splits):
         pool[table[0, t // 64], (t % 64) * d + 3] = 0x7F       # KV head 0's key
     got, _ = decode(L, table, pool, [ctx], q, 0.1, splits)
     assert np.isnan(got[0, :2]).all() and np.array_equal(got[0, 2:], want[0, 2:])
+
+
+# --------------------------------------------------------------------------
+# scores that are all zero
+# --------------------------------------------------------------------------
+@pytest.mark.parametrize("scale", [2.0 ** -12, 2.0 ** -40, 0.0, 1 / 16])
+@pytest.mark.parametrize("splits", [1, 2])
+def test_prefill_of_zero_queries_over_zero_keys(scale, splits):
+    """Queries of zeros, keys of zeros (whose blocks have the smallest scale), a small softmax scale: each query's
+    output is the mean of the values it sees, and those it does not see stay out."""
+    rng = np.random.default_rng(7)
+    hq, hkv, d, start, c = 2, 1, 128, 70, 50
+    n = start + c
+    L = O.Layout(hkv, 64, d)
+    table, pages = C.tables(rng, [2])
+    pool = O.new_pool(L, pages, 0xFF)
+    v = C.rows(rng, n, hkv, d)
+    O.append(pool, L, table, [0], np.array([0, n]), np.zeros((n, hkv, d)), v)
+    q = np.zeros((c, hq, d))
+    got = prefill(L, table, pool, start, q, scale, splits)
+    kk, vv = O.read(pool, L, table[0], n)
+    ref, _, mass = O.attend(kk, vv, q, scale, start + 1 + np.arange(c))
+    top = np.abs(vv).max() / start
+    assert (np.abs(got - ref) <= C.out_bound(ref, mass, n, top)).all()
