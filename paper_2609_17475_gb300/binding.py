@@ -154,7 +154,8 @@ def _calls():
                        at(L.jf_paged_decode_attn), at(L.jf_paged_decode_weights_attn),
                        at(L.jf_kv8_evict)),
                       (torch.int32, torch.uint8, torch.float32, torch.bfloat16, torch.float16),
-                      _raw_stream, _get_device, torch.cuda.current_stream)
+                      _raw_stream, _get_device, torch.cuda.current_stream, torch.is_grad_enabled,
+                      torch.autograd.graph.increment_version)
         _fast = _jfcall
     return _fast
 
@@ -737,7 +738,11 @@ def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
                  k_out: Optional[torch.Tensor] = None, inverse: bool = False, stream=None) -> None:
     """Turn query and key rows [tokens, heads, head_dim] (either may be None) by
     their positions, int32 [axes, tokens]; outputs default to in place.  With
-    ``inverse`` the gradient of that: q, k are then the outputs' gradients."""
+    ``inverse`` the gradient of that: q, k are then the outputs' gradients.
+
+    Autograd does not record the call (wrap it and its inverse in a torch.autograd.Function for that): rows
+    that need a gradient are not written over while gradients are recorded, and what is written counts as
+    modified in place."""
     st = (_fast or _calls()).rope_axes(rope._addr, positions, q, q_out, k, k_out, inverse, stream)
     if st:
         raise JfError("jf_rope_axes", st)

@@ -32,9 +32,10 @@ static struct {
   PyObject *i32, *u8, *f32, *bf16, *f16;      /* torch dtypes */
   PyObject *raw_stream, *get_device;          /* or raw_stream NULL: current_stream */
   PyObject* current_stream;
+  PyObject *grad_enabled, *written;           /* torch.is_grad_enabled, autograd's increment_version */
 } G;
 
-static PyObject *s_dtype, *s_is_cuda, *s_contig, *s_ptr, *s_shape, *s_stride, *s_numel, *s_stream;
+static PyObject *s_dtype, *s_is_cuda, *s_contig, *s_ptr, *s_shape, *s_stride, *s_numel, *s_stream, *s_grad;
 static PyObject *s_data, *s_page, *s_hkv, *s_dim, *s_group, *s_format;
 
 /* ---- tensors ------------------------------------------------------------- */
@@ -240,6 +241,30 @@ static PyObject* kv8_read(PyObject* m, PyObject* const* a, Py_ssize_t n) {
   return rows_call(G.read, a, n);
 }
 
+/* ---- autograd does not see a call: rows that need a gradient are not written over; those written
+ * get a new version, so that a graph that has saved them notices ---- */
+static int may_write(PyObject* t, const char* name) {
+  const int needs = is_true_attr(t, s_grad);
+  if (needs <= 0) return needs;
+  PyObject* on = PyObject_CallNoArgs(G.grad_enabled);
+  if (!on) return -1;
+  const int recorded = on == Py_True;
+  Py_DECREF(on);
+  if (!recorded) return 0;
+  PyErr_Format(PyExc_ValueError, "%s would be written over, and needs a gradient that this call does not record: "
+               "give an output, or call it under torch.no_grad()", name);
+  return -1;
+}
+static int was_written(PyObject* q, PyObject* k) {
+  PyObject* both = q && k ? PyTuple_Pack(2, q, k) : PyTuple_Pack(1, q ? q : k);
+  if (!both) return -1;
+  PyObject* r = PyObject_CallOneArg(G.written, both);
+  Py_DECREF(both);
+  if (!r) return -1;
+  Py_DECREF(r);
+  return 0;
+}
+
 /* ---- rope: address and axes of the handle, positions, q, q_out, k, k_out, inverse, stream ---- */
 static int rope_rows(PyObject* x, PyObject* out, const char* name, int64_t n, jf_rope_rows* r,
                      int* dtype, int64_t* dim) {
@@ -284,7 +309,7 @@ static int rope_rows(PyObject* x, PyObject* out, const char* name, int64_t n, jf
   r->in_head_stride = st[1];
   r->out_token_stride = os[0];
   r->out_head_stride = os[1];
-  if (fit(sh[1])) return -1;
+  if (fit(sh[1]) || may_write(out != Py_None ? out : x, name)) return -1;
   r->num_heads = (int32_t)sh[1];
   *dim = sh[2];
   return 0;
@@ -313,8 +338,15 @@ static PyObject* rope_axes(PyObject* m, PyObject* const* a, Py_ssize_t na) {
   const int inverse = PyObject_IsTrue(a[6]);
   if (inverse < 0 || stream_of(a[7], &stream)) return NULL;
   if (fit(sh[1]) || fit(qd) || fit(kd)) return NULL;
-  CALL(G.rope(rope, pos, st[0], (int32_t)sh[1], (int32_t)(qt >= 0 ? qd : kd), &q, &k,
-              qt >= 0 ? qt : kt, inverse, stream));
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = G.rope(rope, pos, st[0], (int32_t)sh[1], (int32_t)(qt >= 0 ? qd : kd), &q, &k,
+                  qt >= 0 ? qt : kt, inverse, stream);
+  Py_END_ALLOW_THREADS
+  if (status == JF_OK && was_written(qt < 0 ? NULL : a[3] != Py_None ? a[3] : a[2],
+                                     kt < 0 ? NULL : a[5] != Py_None ? a[5] : a[4]))
+    return NULL;
+  return PyLong_FromLong(status);
 }
 
 /* ---- decode: pool, page_table, context_lens, q, scale, out, workspace, splits, stream;
@@ -418,13 +450,13 @@ static PyObject* kv8_evict(PyObject* m, PyObject* const* a, Py_ssize_t na) {
                (int32_t)ds[1], dctx, dw, kept, err, stream));
 }
 
-/* ---- set-up: the entry points' addresses, torch's dtypes and stream functions ---- */
+/* ---- set-up: the entry points' addresses, torch's dtypes, stream and autograd functions ---- */
 static PyObject* setup(PyObject* m, PyObject* args) {
   (void)m;
   unsigned long long f[6];
-  PyObject *dt[5], *raw, *dev, *cur;
-  if (!PyArg_ParseTuple(args, "(KKKKKK)(OOOOO)OOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, dt,
-                        dt + 1, dt + 2, dt + 3, dt + 4, &raw, &dev, &cur))
+  PyObject *dt[5], *raw, *dev, *cur, *grad, *written;
+  if (!PyArg_ParseTuple(args, "(KKKKKK)(OOOOO)OOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, dt,
+                        dt + 1, dt + 2, dt + 3, dt + 4, &raw, &dev, &cur, &grad, &written))
     return NULL;
   G.append = (rows_fn)(uintptr_t)f[0];
   G.read = (rows_fn)(uintptr_t)f[1];
@@ -440,6 +472,8 @@ static PyObject* setup(PyObject* m, PyObject* args) {
   G.raw_stream = raw == Py_None ? NULL : Py_NewRef(raw);
   G.get_device = Py_NewRef(dev);
   G.current_stream = Py_NewRef(cur);
+  G.grad_enabled = Py_NewRef(grad);
+  G.written = Py_NewRef(written);
   Py_RETURN_NONE;
 }
 
@@ -457,7 +491,8 @@ PyMODINIT_FUNC PyInit__jfcall(void) {
     const char* text;
   } names[] = {{&s_dtype, "dtype"}, {&s_is_cuda, "is_cuda"}, {&s_contig, "is_contiguous"},
                {&s_ptr, "data_ptr"}, {&s_shape, "shape"}, {&s_stride, "stride"},
-               {&s_numel, "numel"}, {&s_stream, "cuda_stream"}, {&s_data, "data"},
+               {&s_numel, "numel"}, {&s_stream, "cuda_stream"},
+               {&s_grad, "requires_grad"}, {&s_data, "data"},
                {&s_page, "page_size"}, {&s_hkv, "num_kv_heads"}, {&s_dim, "head_dim"},
                {&s_group, "group_size"}, {&s_format, "format"}};
   for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i) {
