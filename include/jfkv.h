@@ -506,8 +506,9 @@ typedef struct jf_rope_rows {     /* the queries' or the keys' rows          */
  *               pos_stride elements apart; any int32 value
  *   q, k        host structs; head_dim channels a head (a multiple of 16,
  *               R <= head_dim <= 512), elements of type `dtype`
- * Numerics: angles are exact to 2^-32 of a turn at any position; products in
- * fp32, one rounding to the element type.  n_tokens == 0 is a no-op.
+ * Numerics: angles are worked out to 2^-32 of a turn at any position and
+ * frequency and rounded to fp32 (2^-26 of a turn at most); products in fp32, one
+ * rounding to the element type.  n_tokens == 0 is a no-op.
  */
 int jf_rope_axes(const jf_rope* rope, const int32_t* positions, int64_t pos_stride,
                  int32_t n_tokens, int32_t head_dim, const jf_rope_rows* q, const jf_rope_rows* k,

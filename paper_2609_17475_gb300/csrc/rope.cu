@@ -10,14 +10,18 @@
 //
 // The angle is kept as a fraction of a turn in 64-bit fixed point: the host
 // rounds f_i / (2 pi) to a multiple of 2^-64 and pos * that, modulo 2^64, is
-// exact integer arithmetic, so a far position loses nothing (an fp32 product
-// is off by 0.01 rad at position 262,144) and no range reduction is needed.
+// exact integer arithmetic, so the product is off by at most 2^-34 of a turn at
+// any position (an fp32 product by 0.01 rad at position 262,144) and no range
+// reduction is needed.  Its upper 32 bits become an fp32 in half turns, which
+// rounds to 2^-26 of a turn.
 //
 // Bound by memory: each element is read and written once.  2,048 tokens of 28 heads x
 // 256 (bf16, all channels turned) 12.6 us, 4.7 TB/s, of which about 4 us are the launch
 // and the first loads (32 tokens: 4.1 us); the gradient of 16,391 tokens of 20 heads x
 // 128 (fp16) 33.3 us, 5.0 TB/s.  One CTA a token (two, where that fills the SMs anyway)
 // keeps the cosines beside the heads that use them: 18 KB of rows a CTA, many CTAs an SM.
+#include <cstring>
+
 #include "common.cuh"
 
 namespace jfkv {
@@ -195,17 +199,26 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   }
 }
 
-// f / (2 pi) modulo 1, rounded to a multiple of 2^-64
+// f / (2 pi) modulo 1, rounded to a multiple of 2^-64.  f = m 2^x with a whole m below 2^24, and
+// 1 / (2 pi) to 128 bits, so that the product is good to 2^-104 of a turn times 2^x, x <= 8.
 static uint64_t turns_per_position(float f) {
-  const double t = (double)f * 0.15915494309189533577;   // 1 / (2 pi)
-  double frac = t - (double)(int64_t)t;                  // |t| < 2^62 (checked by the caller)
-  if (frac < 0.0) frac += 1.0;
-  if (frac >= 1.0) return 0;
-  // two 32-bit pieces: 2^64 itself does not fit
-  const double hi = frac * 4294967296.0;
-  const uint64_t h = (uint64_t)hi;
-  const uint64_t l = (uint64_t)((hi - (double)h) * 4294967296.0);
-  return (h << 32) | l;
+  typedef unsigned __int128 u128;
+  const u128 inv = ((u128)0x28BE60DB9391054AULL << 64) | 0x7F09D5F47D4D3770ULL;   // 2^128 / (2 pi)
+  uint32_t b;
+  memcpy(&b, &f, 4);
+  const int e = (int)(b >> 23) & 0xFF, x = (e ? e : 1) - 150;
+  const u128 m = (b & 0x7FFFFFu) | (e ? 0x800000u : 0u);
+  // m inv 2^(x - 64) in units of 2^-64, modulo 2^64: m inv in two parts of 64 bits and what is above
+  const u128 lo = m * (uint64_t)inv, hi = m * (uint64_t)(inv >> 64) + (lo >> 64);   // hi below 2^88
+  const int shift = 64 - x;                                   // 56 (|f| below 2^32) and up
+  uint64_t turns = 0;
+  if (shift <= 64) {
+    const u128 low = (hi << 64) | (uint64_t)lo;               // the product's low 128 bits
+    turns = (uint64_t)(low >> shift) + ((uint64_t)(low >> (shift - 1)) & 1u);
+  } else if (shift - 64 <= 88) {
+    turns = (uint64_t)(hi >> (shift - 64)) + ((uint64_t)(hi >> (shift - 65)) & 1u);
+  }
+  return f < 0.f ? 0 - turns : turns;
 }
 
 int launch_rope(const jf_rope& rope, const int32_t* positions, int64_t pos_stride,

@@ -1,4 +1,6 @@
 """Rotary axes beside autograd, and at the ends of their ranges."""
+from fractions import Fraction
+
 import numpy as np
 import pytest
 import torch
@@ -75,3 +77,47 @@ def test_as_a_function_with_a_gradient():
     u, v = z.double()[..., :8], z.double()[..., 8:16]
     ref = torch.cat([u * c + v * s, -u * s + v * c, z.double()[..., 16:]], -1)
     assert (x.grad.double() - ref).abs().max() <= 2.0 ** -20 * z.abs().max()
+
+
+def two_pi_inverse(bits=256):
+    """1 / (2 pi) to `bits` bits, by Machin's formula in whole numbers."""
+    one = 1 << (bits + 32)
+
+    def arctan_inverse(n):
+        total, term, k = 0, one // n, 0
+        while term:
+            total += (-1) ** k * (term // (2 * k + 1))
+            term //= n * n
+            k += 1
+        return total
+    pi = 4 * (4 * arctan_inverse(5) - arctan_inverse(239))
+    return Fraction(one, 2 * pi)
+
+
+INV = two_pi_inverse()
+
+
+@pytest.mark.parametrize("inverse", [False, True])
+def test_angles_at_far_positions_and_high_frequencies(inverse):
+    """Frequencies from 2^-40 to just below 2^32 at the ends of the positions' range.  The angle's fraction of a turn is
+    worked out exactly here; the kernel's is off by 2^-32 of a turn, and by 2^-26 in fp32 (2^-23.3 radians
+    together), cosine, sine and products by a few 2^-24 more."""
+    f = np.array([2.0 ** -40, 1e-3, 1.0, 3.7, 100.0, 12345.678, 2.0 ** 24 + 2, 2.0 ** 31, 2.0 ** 32 - 512, 0.5, -1.0, -77.7,
+                  -3e9, 2.0 ** -126, 2.0 ** -149, 0.0], dtype=np.float32)
+    pos = np.array([0, 1, -1, 2, 1 << 20, (1 << 31) - 1, -(1 << 31), 2147483001, -2000000011, 1234567891], dtype=np.int32)
+    rope = jf.Rope(32, inv_freq=f)
+    assert np.array_equal(rope.inv_freq, f)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(len(pos), 3, 32, generator=g, device=DEV)
+    y = torch.empty_like(x)
+    jf.jf_rope_axes(rope, torch.from_numpy(pos)[None].to(DEV), x, y, inverse=inverse)
+    x64, got = x.double().cpu().numpy(), y.double().cpu().numpy()
+    for t, p in enumerate(pos.tolist()):
+        turns = [Fraction(float(v)) * p * INV for v in f]
+        a = 2 * np.pi * np.array([float(u - round(u)) for u in turns])
+        c, s = np.cos(a), np.sin(a) * (-1 if inverse else 1)
+        u, v = x64[t, :, :16], x64[t, :, 16:]
+        ref = np.concatenate([u * c - v * s, u * s + v * c], -1)
+        length = np.sqrt(u * u + v * v)
+        bound = np.concatenate([length, length], -1) * 2.0 ** -21 + 2.0 ** -140
+        assert (np.abs(got[t] - ref) <= bound).all(), (p, float((np.abs(got[t] - ref) / bound).max()))
