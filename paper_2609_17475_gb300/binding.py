@@ -302,6 +302,10 @@ class KVPool:
         self.__dict__.pop("_c", None)
         self.__dict__[name] = value
 
+    def __getstate__(self):
+        # a copy or a pickle builds its own struct: this one points into this pool's tensor and codec
+        return {name: value for name, value in self.__dict__.items() if name != "_c"}
+
     def c_struct(self) -> _Pool:
         c = self.__dict__.get("_c")
         if c is None or c.base != self.data.data_ptr() or c.num_pages != self.data.shape[0]:
