@@ -300,7 +300,7 @@ class KVPool:
     def __setattr__(self, name, value):
         # the struct below is built again once a field has changed
         self.__dict__.pop("_c", None)
-        self.__dict__[name] = value
+        object.__setattr__(self, name, value)
 
     def __getstate__(self):
         # a copy or a pickle builds its own struct: this one points into this pool's tensor and codec

@@ -29,3 +29,16 @@ def test_pools_copy_whether_or_not_a_call_has_used_them(dup, used):
         if p.codec is not None:
             assert ctypes.addressof(c.tq4.contents) == ctypes.addressof(q.codec._c)
             assert list(c.tq4.contents.signs_v) [:128] == [-1] * 128
+
+
+def test_pool_fields_and_properties():
+    p = pools()[0]
+    before = p.c_struct()
+    assert p.c_struct() is before
+    p.data = torch.zeros(5, p.page_bytes, dtype=torch.uint8)
+    assert p.num_pages == 5 and p.c_struct().num_pages == 5 and p.c_struct().base == p.data.data_ptr()
+    p.format = jf.JF_FMT_E4M3_B32
+    assert p.c_struct().format == jf.JF_FMT_E4M3_B32
+    for name in ("num_pages", "page_bytes"):        # worked out from data: not to be set
+        with pytest.raises(AttributeError):
+            setattr(p, name, 7)
