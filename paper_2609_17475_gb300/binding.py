@@ -733,7 +733,6 @@ class Rope:
         for i in range(half):
             c.inv_freq[i] = float(f[i])
             c.axis[i] = int(axis[i])
-        self._addr = ctypes.addressof(c)
 
 
 @_traced
@@ -747,7 +746,7 @@ def jf_rope_axes(rope: Rope, positions: torch.Tensor, q: Optional[torch.Tensor],
     Autograd does not record the call (wrap it and its inverse in a torch.autograd.Function for that): rows
     that need a gradient are not written over while gradients are recorded, and what is written counts as
     modified in place."""
-    st = (_fast or _calls()).rope_axes(rope._addr, positions, q, q_out, k, k_out, inverse, stream)
+    st = (_fast or _calls()).rope_axes(ctypes.addressof(rope._c), positions, q, q_out, k, k_out, inverse, stream)
     if st:
         raise JfError("jf_rope_axes", st)
 

@@ -1,6 +1,7 @@
 """The binding's handles as Python objects: copies, pickles, assignments.  No GPU."""
 import copy
 import ctypes
+import gc
 import pickle
 
 import numpy as np
@@ -8,6 +9,7 @@ import pytest
 import torch
 
 import paper_2609_17475_gb300 as jf
+from paper_2609_17475_gb300 import binding as B
 
 
 def pools():
@@ -42,3 +44,27 @@ def test_pool_fields_and_properties():
     for name in ("num_pages", "page_bytes"):        # worked out from data: not to be set
         with pytest.raises(AttributeError):
             setattr(p, name, 7)
+
+
+class _Calls:
+    """Stands for the C part of the binding: keeps what a call passes on."""
+
+    def rope_axes(self, rope, *rest):
+        self.rope = rope
+        return 0
+
+
+@pytest.mark.parametrize("dup", [copy.copy, copy.deepcopy, lambda p: pickle.loads(pickle.dumps(p))])
+def test_rope_handles_copy(dup, monkeypatch):
+    """A copy's calls read the copy's own frequencies, also when the original is gone."""
+    calls = _Calls()
+    monkeypatch.setattr(B, "_fast", calls)
+    r = jf.Rope(32, [6, 5, 5], base=1e4)
+    want, keep = r.inv_freq.copy(), ctypes.addressof(r._c)
+    q = dup(r)
+    del r
+    gc.collect()
+    jf.jf_rope_axes(q, None, None)
+    assert calls.rope == ctypes.addressof(q._c) and (dup is copy.copy or calls.rope != keep)
+    c = B._Rope.from_address(calls.rope)
+    assert (c.rotary_dim, c.num_axes) == (32, 3) and np.array_equal(np.array(c.inv_freq[:16], dtype=np.float32), want)
