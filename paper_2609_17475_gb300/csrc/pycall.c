@@ -124,8 +124,12 @@ static int stream_of(PyObject* stream, void** out) {
     Py_DECREF(s);
   } else if (PyLong_Check(stream)) {
     h = Py_NewRef(stream);
-  } else {
+  } else {   /* an object with a handle, or what int() takes */
     h = PyObject_GetAttr(stream, s_stream);
+    if (!h && PyErr_ExceptionMatches(PyExc_AttributeError)) {
+      PyErr_Clear();
+      h = PyNumber_Long(stream);
+    }
   }
   if (!h) return -1;
   *out = (void*)(uintptr_t)PyLong_AsUnsignedLongLong(h);

@@ -1,4 +1,5 @@
-"""The binding's handles as Python objects: copies, pickles, assignments.  No GPU."""
+"""The binding's handles as Python objects: copies, pickles, assignments; and what its calls take for
+a stream.  No GPU."""
 import copy
 import ctypes
 import gc
@@ -68,3 +69,55 @@ def test_rope_handles_copy(dup, monkeypatch):
     assert calls.rope == ctypes.addressof(q._c) and (dup is copy.copy or calls.rope != keep)
     c = B._Rope.from_address(calls.rope)
     assert (c.rotary_dim, c.num_axes) == (32, 3) and np.array_equal(np.array(c.inv_freq[:16], dtype=np.float32), want)
+
+
+class _Tensor:
+    """What the C part reads of a CUDA tensor; its memory is never touched."""
+
+    def __init__(self, dtype, *shape):
+        self.dtype, self.shape, self.is_cuda, self.requires_grad = dtype, shape, True, False
+
+    def is_contiguous(self):
+        return True
+
+    def data_ptr(self):
+        return 0x20000
+
+    def numel(self):
+        return int(np.prod(self.shape))
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+
+def _decode(stream, table=None):
+    """A decode whose workspace is too small: refused once its arguments have been read."""
+    i32, bf = torch.int32, torch.bfloat16
+    p = B.KVPool(_Tensor(torch.uint8, 8, 64 * 2 * 128), 64, 1, 128, format=jf.JF_FMT_E4M3_B32)
+    q = _Tensor(bf, 1, 4, 128)
+    jf.jf_paged_decode_attn(p, table or _Tensor(i32, 1, 4), _Tensor(i32, 1), q, 0.1, q, _Tensor(torch.uint8, 64), 2, stream)
+
+
+class _Handle:
+    cuda_stream = 5
+
+
+class _Int:
+    def __int__(self):
+        return 5
+
+
+@pytest.mark.parametrize("stream", [0, 5, _Handle(), np.int64(5), np.uint64(5), _Int(), torch.tensor(5)])
+def test_streams(stream):
+    """A stream is an object with a handle, or anything int() takes."""
+    with pytest.raises(jf.JfError) as e:
+        _decode(stream)
+    assert e.value.status == B.JF_ERR_WORKSPACE_TOO_SMALL
+
+
+def test_what_is_no_stream():
+    for stream in ("x", object(), 0.5j):
+        with pytest.raises((TypeError, ValueError)):
+            _decode(stream)
+    with pytest.raises(OverflowError):
+        _decode(-(1 << 70))
