@@ -165,7 +165,7 @@ static int pool_of(PyObject* p, jf_kv_pool* out) {
     out->base = PyLong_AsVoidPtr(at);
     Py_DECREF(at);
   }
-  if (n < 1) return -1;
+  if (n < 1) return n ? -1 : bad("a pool's data must be [pages, bytes]");
   out->num_pages = shape[0];
   out->tq4 = NULL;
   return int_attr(p, s_page, &out->page_size) || int_attr(p, s_hkv, &out->num_kv_heads) ||
@@ -226,7 +226,7 @@ static PyObject* rows_call(rows_fn fn, PyObject* const* a, Py_ssize_t na) {
       (a[6] != Py_None && tensor(a[6], G.i32, "err_flag", 1, I32_T, &err)))
     return NULL;
   const int d = ints_of(a[1], 0, sh);
-  if (d < 1) return NULL;
+  if (d < 0 || (d == 0 && bad("page_table must be [requests, pages]"))) return NULL;
   const int64_t B = d == 2 ? sh[0] : 1, cols = d == 2 ? sh[1] : numel(a[1]);
   if (n != nv && bad("k and v must have the same rows")) return NULL;
   if ((numel(a[2]) != B || numel(a[3]) != B + 1) &&

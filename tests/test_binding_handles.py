@@ -121,3 +121,17 @@ def test_what_is_no_stream():
             _decode(stream)
     with pytest.raises(OverflowError):
         _decode(-(1 << 70))
+
+
+def test_tensors_without_dimensions_are_refused():
+    i32, bf = torch.int32, torch.bfloat16
+    with pytest.raises(ValueError):
+        _decode(0, _Tensor(i32))
+    p = B.KVPool(_Tensor(torch.uint8, 8, 64 * 2 * 128), 64, 1, 128, format=jf.JF_FMT_E4M3_B32)
+    x, one, off = _Tensor(bf, 1, 1, 128), _Tensor(i32, 1), _Tensor(i32, 2)
+    for call in (jf.jf_kv8_append, jf.jf_kv8_read):
+        with pytest.raises(ValueError):
+            call(p, _Tensor(i32), one, off, x, x, None, 0)
+        with pytest.raises(ValueError):
+            call(B.KVPool(_Tensor(torch.uint8), 64, 1, 128, format=jf.JF_FMT_E4M3_B32), _Tensor(i32, 1, 4), one, off, x, x,
+                 None, 0)
