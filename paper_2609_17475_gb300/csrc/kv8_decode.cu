@@ -381,8 +381,8 @@ kv8_split_kernel(const __grid_constant__ CUtensorMap tmap, const Kv8DecodeArgs a
         const float* sc = reinterpret_cast<const float*>(a.pool + (int64_t)page * a.page_bytes +
                                                          2 * a.codes_region) +
                           kvh * (a.P / KV8_BLOCK) + slot / KV8_BLOCK;
-        ksc[s] = __ldg(sc);
-        vsc[s] = __ldg(sc + a.sb_region / 4);
+        ksc[s] = sc[0];   // written by an append that this grid may overlap: no read-only load
+        vsc[s] = sc[a.sb_region / 4];
       }
       valid = (valid & ~(1u << s)) | ((uint32_t)ok << s);
     };

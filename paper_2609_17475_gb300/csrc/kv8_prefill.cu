@@ -517,8 +517,9 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       if (page >= 0 && page < a.num_pages) {
         const uint8_t* p = a.pool + (int64_t)page * a.page_bytes + a.sb_base +
                            (kvh * (a.P / KV8_BLOCK) + (((jb + j) * PF_BN) & (a.P - 1)) / KV8_BLOCK) * 4;
-        ks_next = __ldg(reinterpret_cast<const float2*>(p));
-        vs_next = __ldg(reinterpret_cast<const float2*>(p + a.sb_region));
+        // written by an append that this grid may overlap: no read-only load
+        ks_next = *reinterpret_cast<const float2*>(p);
+        vs_next = *reinterpret_cast<const float2*>(p + a.sb_region);
       }
     };
     load_scales(group, page_of(group));
