@@ -332,9 +332,9 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * (fp16) in the rotated basis, and each output row is rotated back
  * (S_V H / sqrt(D)) as the partials are merged.
  * E4M3 pools: workspaces as for affine pools.  K's codes are multiplied as
- * they are, by q as the sum of two e4m3 terms under a power-of-two scale per
- * row (bf16's 8 bits exactly for elements within 2^-9 of the row's largest,
- * at most 2^-17 of the largest off below); V's codes enter as fp16 (exact) and
+ * they are, by q as the sum of two 8-bit terms under a power-of-two scale per
+ * row (bf16's 8 bits exactly for elements within 2^13 of the row's largest,
+ * at most 2^-21 of the largest off below); V's codes enter as fp16 (exact) and
  * the block scales are applied as in the decode; no scale is out of range.
  * A position a query does not see has the weight zero: a NaN among its values
  * (not its key) still reaches the queries of the chunk before it, as 0 * NaN.

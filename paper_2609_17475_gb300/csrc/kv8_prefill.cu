@@ -8,10 +8,12 @@
 //  * S = Q K^T multiplies the codes as they lie in the pool (kind::f8f6f4): TMA
 //    brings K rows straight into the MMA's swizzled layout and nothing is
 //    dequantized.  Q, which needs more than e4m3's 4 bits, enters as a sum of two
-//    e4m3 terms, hi + lo, of the row scaled so that its largest element lies in
-//    [2^7, 2^8): bf16's 8 bits exactly for elements within 2^9 of the largest,
-//    and at most 2^-17 of it off below.  Two 8-bit products take the time of one
-//    16-bit product.
+//    terms, hi in e4m3 and lo in e5m2, of the row scaled so that its largest element
+//    lies in [2^7, 2^8).  From 2^-6 up hi is off by at most 8 units of bf16's last
+//    place, a whole number that e5m2's 3 bits hold: elements within 2^13 of the largest
+//    enter exactly.  Below, hi is off by at most 2^-10 and lo's rounding of that by
+//    2^-14, 2^-21 of the largest.  (With lo in e4m3, whose least step is 2^-9, the
+//    bounds were 2^9 and 2^-17.)  Two 8-bit products take the time of one 16-bit product.
 //  * P V stays fp16 -- P has to keep small weights, which e4m3 cannot -- with V's
 //    codes widened to fp16 (exact) by four warps.
 //  * The block scales are powers of two and a half tile is a block: K's multiplies
@@ -115,6 +117,13 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t x, uint32_t
                ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
+__device__ __forceinline__ uint32_t e5m2x4_of_f16x2(uint32_t lo, uint32_t hi) {
+  uint32_t r;
+  asm("{\n.reg .b16 a, b;\ncvt.rn.satfinite.e5m2x2.f16x2 a, %1;\n"
+      "cvt.rn.satfinite.e5m2x2.f16x2 b, %2;\nmov.b32 %0, {a, b};\n}\n"
+      : "=r"(r) : "r"(lo), "r"(hi));
+  return r;
+}
 __device__ __forceinline__ uint32_t sub_f16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.rn.f16x2 %0, %1, %2;\n" : "=r"(r) : "r"(a), "r"(b));
@@ -131,6 +140,7 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
     return x;
   }
 }
+
 struct P8NoPlan {};
 template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
 template <> struct P8PlanArg<false> { using type = P8NoPlan; };
@@ -141,7 +151,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
 kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ PrefillArgs a,
                    const __grid_constant__ typename P8PlanArg<PLAN>::type plan) {
   using L = P8Smem<D>;
-  constexpr uint32_t IDQK = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
+  constexpr uint32_t IDHI = tc::idesc_f8_f32(2 * PF_BM, 2 * PF_BN, 0);   // a tile pair
+  constexpr uint32_t IDLO = tc::idesc_f8_f32(2 * PF_BM, 2 * PF_BN, 1);
   constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
   // S of pair i is issued before P V of pair i - AHEAD, so that the softmax of a pair may
   // run while the P V of AHEAD pairs before it are outstanding: V buffers and barriers for
@@ -298,7 +309,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     return j < ntiles ? __ldg(pt + (((jb + j) * PF_BN) >> log2P)) : -1;
   };
 
-  // ---- softmax warps: Q rows as two e4m3 terms (K-major, 128-byte swizzle: 16-byte
+  // ---- softmax warps: Q rows as two 8-bit terms (K-major, 128-byte swizzle: 16-byte
   // piece m of row r at block m / 8, piece (m % 8) ^ (r % 8)) -------------------------
   float smul = 0.f;                            // score = smul * S
   if (warp >= P8_SM_WARP0) {
@@ -318,7 +329,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
       if (a.scale_log2 < 0.f) qs = -qs;        // the scale's sign goes to Q
       uint32_t hi[2] = {0u, 0u}, lo[2] = {0u, 0u};
       if (!zero) {
-        // by way of fp16, which holds what e4m3 does not round to 0 (2^-10) exactly
+        // by way of fp16, which holds what e5m2 does not round to 0 (2^-17) exactly
         uint32_t f[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
@@ -328,7 +339,7 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
           hi[k] = e4m3x4_of_f16x2(f[2 * k], f[2 * k + 1]);
           uint32_t h0, h1;
           f16x4_of_e4m3(hi[k], h0, h1);
-          lo[k] = e4m3x4_of_f16x2(sub_f16x2(f[2 * k], h0), sub_f16x2(f[2 * k + 1], h1));
+          lo[k] = e5m2x4_of_f16x2(sub_f16x2(f[2 * k], h0), sub_f16x2(f[2 * k + 1], h1));
         }
       }
       uint8_t* const to = at + row * 128 + ((m7 ^ (row & 7)) << 4);
@@ -383,8 +394,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
             tc::mma2_ss_f8_if(leader, d,
                               qd + (((ks / (D / 32)) * L::Q_BYTES + (k >> 2) * (PF_BM * 128) +
                                      (k & 3) * 32) >> 4),
-                              kd_i + (((k >> 2) * (PF_BN * 128) + (k & 3) * 32) >> 4), IDQK,
-                              ks ? 1u : 0u);
+                              kd_i + (((k >> 2) * (PF_BN * 128) + (k & 3) * 32) >> 4),
+                              ks < D / 32 ? IDHI : IDLO, ks ? 1u : 0u);
           }
           tc::commit2_both_if(leader, &s_full[kb]);
         }

@@ -181,3 +181,71 @@ def test_prefill_of_zero_queries_over_zero_keys(scale, splits):
     ref, _, mass = O.attend(kk, vv, q, scale, start + 1 + np.arange(c))
     top = np.abs(vv).max() / start
     assert (np.abs(got - ref) <= C.out_bound(ref, mass, n, top)).all()
+
+
+# --------------------------------------------------------------------------
+# queries whose elements differ by many powers of two
+# --------------------------------------------------------------------------
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("far", [8, 10, 12, 13, 15, 17])
+def test_prefill_of_queries_with_an_outlier(d, far):
+    """One channel 2^far times the others, where the keys are zero, so that the others alone make the scores.  Elements
+    within 2^13 of a row's largest enter exactly, smaller ones with an error of at most 2^-21 of it."""
+    rng = np.random.default_rng(far)
+    hq, hkv, start, c = 4, 2, 300, 40
+    n, G = start + c, 2
+    L = O.Layout(hkv, 64, d)
+    table, pages = C.tables(rng, [-(-n // 64)])
+    pool = O.new_pool(L, pages, 0xFF)
+    k, v = rng.standard_normal((n, hkv, d)), C.rows(rng, n, hkv, d)
+    k[:, :, 5] = 0
+    k = torch.from_numpy(k).bfloat16().double().numpy()
+    O.append(pool, L, table, [0], np.array([0, n]), k, v)
+    # magnitudes in [1, 2) and the outlier 2^far: scores of the size that a softmax meets, times 4 so that few
+    # positions carry each row
+    q = (1 + rng.random((c, hq, d))) * rng.choice([-1.0, 1.0], (c, hq, d))
+    q[:, :, 5] = 2.0 ** far
+    q = torch.from_numpy(q).bfloat16().double().numpy()
+    scale = float(np.float32(4 / math.sqrt(d)))
+    got = prefill(L, table, pool, start, q, scale)
+    kk, vv = O.read(pool, L, table[0], n)
+    ref, w, mass = O.attend(kk, vv, q, scale, start + 1 + np.arange(c))
+    rest = np.delete(np.arange(d), 5)
+    for h in range(hq):
+        # a score's error: the elements' own, and 2^-18 of the sum of |q k| for the products' fp32 sums; a weight is
+        # off by its score's error and the largest of its row's
+        off = 0.0 if far <= 13 else 2.0 ** -21 * 2.0 ** far
+        ka = np.abs(kk[:, h // G][:, rest])
+        e = (off * ka.sum(-1)[None] + 2.0 ** -18 * (np.abs(q[:, h][:, rest]) @ ka.T)) * scale
+        # the elements' errors are of either sign and differ from each other: their sum over d of them stays below
+        # 8 sqrt(d) of one's for all of these rows and positions, and max|k|
+        if off:
+            e = np.minimum(e, (off * 8 * math.sqrt(d) * ka.max() + 2.0 ** -18 * 4 * d * ka.max()) * scale)
+        slack = 2 * e.max(-1)[:, None]
+        top = (w[:, h].max(0)[:, None] * np.abs(vv[:, h // G])).max()
+        bound = C.out_bound(ref[:, h], mass[:, h], n, top) + mass[:, h] * slack + n * top * 448 * 2.0 ** -25
+        assert (np.abs(got[:, h] - ref[:, h]) <= bound).all(), float((np.abs(got[:, h] - ref[:, h]) / bound).max())
+
+
+@pytest.mark.parametrize("qscale", [2.0 ** -60, 2.0 ** 20])
+@pytest.mark.parametrize("hq,hkv,d", [(4, 2, 128), (6, 1, 256)])
+def test_prefill_of_scaled_queries(qscale, hq, hkv, d):
+    """Queries far from 8 and 16 bits' ranges, each row by a power of two of its own, under a softmax scale to match."""
+    rng = np.random.default_rng(d)
+    start, c = 300, 40
+    n = start + c
+    L, table, pool = C.filled(rng, hkv, 64, d, [n])
+    q = queries(rng, c, hq, d) * 2.0 ** rng.integers(-6, 3, (c, hq, 1)) * qscale
+    scale = float(np.float32(1 / math.sqrt(d) / qscale))
+    got = prefill(L, table, pool, start, q, scale)
+    kk, vv = O.read(pool, L, table[0], n)
+    ref, w, mass = O.attend(kk, vv, q, scale, start + 1 + np.arange(c))
+    for h in range(hq):
+        # a score's error: 2^-21 of the row's largest for each element that lies below 2^-13 of it, and 2^-18 of the
+        # sum of |q k| for the fp32 sums
+        ka = np.abs(kk[:, h * hkv // hq])
+        e = (2.0 ** -21 * np.abs(q[:, h]).max(-1)[:, None] * ka.sum(-1)[None] + 2.0 ** -18 * np.abs(q[:, h]) @ ka.T) * scale
+        top = (w[:, h].max(0)[:, None] * np.abs(vv[:, h * hkv // hq])).max()
+        bound = (C.out_bound(ref[:, h], mass[:, h], n, top) + mass[:, h] * 2 * e.max(-1)[:, None] +
+                 n * top * 448 * 2.0 ** -25)
+        assert (np.abs(got[:, h] - ref[:, h]) <= bound).all(), float((np.abs(got[:, h] - ref[:, h]) / bound).max())
