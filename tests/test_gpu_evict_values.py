@@ -61,3 +61,45 @@ def test_zero_rows_stay_zero(zero, scale, d, p, budget):
         assert np.isfinite(x).all()
         if zero in (name, "both"):
             assert not x[np.isin(want_kept[0, 0], np.flatnonzero(none))].any()
+
+
+def test_pages_outside_the_pool_by_their_outputs():
+    """A source page outside the pool gives rows of zeros, a destination one and a destination row too short are not
+    written; kept positions, weights and all other bytes are those of the definition."""
+    rng = np.random.default_rng(6)
+    hkv, d, p, n, budget = 2, 128, 64, [200, 130], 70
+    L, table, pool = C.filled(rng, hkv, p, d, n, extra=[2, 2])
+    src = np.stack([table[0, :4], np.append(table[1, :3], -1)])
+    dst = np.stack([table[0, 4:6], table[1, 3:5]])
+    w = rng.random((2, hkv, 200), dtype=np.float32)
+    page_bit, pos_bit = jf.binding.JF_DEV_ERR_PAGE_ID, jf.binding.JF_DEV_ERR_POSITION
+
+    # request 0's second page lies outside: as if its rows had been zeros
+    for outside in (-1, len(pool), 1 << 30):
+        bad = src.copy()
+        bad[0, 1] = outside
+        got, kept, wout, m, err = evict(L, pool, bad, n, w, budget, dst)
+        clean = pool.copy()
+        clean[src[0, 1]] = 0
+        at = 2 * hkv * p * d
+        clean[src[0, 1], at:] = np.full(2 * hkv * (p // 32), 2.0 ** -40, np.float32).view(np.uint8)
+        want_kept, want_w = O.evict(clean, L, src, n, w, budget, 0, 0, dst)
+        want = pool.copy()
+        want[dst.reshape(-1)] = clean[dst.reshape(-1)]
+        assert err == page_bit and m == [budget, budget]
+        assert np.array_equal(kept, want_kept) and np.array_equal(wout, want_w) and np.array_equal(got, want)
+
+    # request 0's destination: its second page outside, or not there
+    want = pool.copy()
+    want_kept, want_w = O.evict(want, L, src, n, w, budget, 0, 0, dst)
+    want[dst[0, 1]] = pool[dst[0, 1]]
+    for outside in (-1, len(pool)):
+        bad = dst.copy()
+        bad[0, 1] = outside
+        got, kept, wout, m, err = evict(L, pool, src, n, w, budget, bad)
+        assert err == page_bit and m == [budget, budget]
+        assert np.array_equal(kept, want_kept) and np.array_equal(wout, want_w) and np.array_equal(got, want)
+    want[dst[1, 1]] = pool[dst[1, 1]]
+    got, kept, wout, m, err = evict(L, pool, src, n, w, budget, dst[:, :1].copy())
+    assert err == pos_bit and m == [budget, budget]
+    assert np.array_equal(kept, want_kept) and np.array_equal(wout, want_w) and np.array_equal(got, want)
