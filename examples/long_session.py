@@ -2,9 +2,9 @@
 
 The layer's queries, keys and values are drawn at random; everything between them and the layer's output runs
 through the library: a prompt of text and image patches is turned by its time, height and width positions, appended
-to the paged cache and attended in chunks; then tokens are generated one at a time, their attention weights are added
-up, and whenever the cache has grown past its budget the positions that drew the least weight are evicted and their
-pages given back.
+to the paged cache and attended in chunks, and the attention weights that its last queries draw are added up; then
+tokens are generated one at a time, their weights are added too, and whenever the cache has grown past its budget the
+positions that drew the least weight are evicted and their pages given back.
 
     python examples/long_session.py --prompt 8192 --tokens 512 --budget 4096
 """
@@ -84,6 +84,20 @@ class Session:
         jf.jf_prefill_chunk_attn(self.pool, self.table[0], q, self.length - n, 1 / math.sqrt(self.d), True, out, ws)
         return out
 
+    def observe(self, q):
+        """Adds up the weights that the last n positions' queries draw, q [n, Hq, D] as `prompt` has turned them: a
+        batch of n single-token calls over one request's pages, each up to its own position."""
+        n = q.shape[0]
+        ctx = torch.arange(self.length - n + 1, self.length + 1, dtype=torch.int32, device=self.device)
+        table = self.table.repeat(n, 1)
+        weights = torch.zeros(n, self.hkv, self.length, device=self.device)
+        splits = jf.default_num_splits(n, self.hkv, format=jf.JF_FMT_E4M3_B32)
+        ws = jf.decode_weights_workspace(n, self.hq, self.hkv, self.d, splits, self.length, device=self.device)
+        jf.jf_paged_decode_weights_attn(self.pool, table, ctx, q, 1 / math.sqrt(self.d), torch.empty_like(q), None, weights,
+                                        ws, splits)
+        self.weights[0, :, :self.length] += weights.sum(0)
+        self.err |= ws[:4].view(torch.int32)
+
     def step(self, q, k, v, pos):
         """One generated token: its attention output [1, Hq, D]; its weights are added up."""
         self.extend(q, k, v, pos)
@@ -115,7 +129,7 @@ class Session:
         return int(self.err.item()) | jf.workspace_status(self.ws)
 
 
-def run(prompt=8192, tokens=512, budget=4096, chunk=2048, hq=24, hkv=4, d=256, page=256, seed=0, verbose=True):
+def run(prompt=8192, tokens=512, budget=4096, chunk=2048, hq=24, hkv=4, d=256, page=256, seed=0, verbose=True, window=64):
     g = torch.Generator(device="cuda").manual_seed(seed)
     draw = lambda n, h: torch.randn(n, h, d, generator=g, device="cuda").bfloat16()  # noqa: E731
     slack = 256     # the cache grows this far past its budget before it is cut
@@ -125,7 +139,10 @@ def run(prompt=8192, tokens=512, budget=4096, chunk=2048, hq=24, hkv=4, d=256, p
     t = time.perf_counter()
     for at in range(0, prompt, chunk):
         n = min(chunk, prompt - at)
-        s.prompt(draw(n, hq), draw(n, hkv), draw(n, hkv), pos[:, at:at + n])
+        q = draw(n, hq)
+        s.prompt(q, draw(n, hkv), draw(n, hkv), pos[:, at:at + n])
+    if prompt:
+        s.observe(q[-window:])
     torch.cuda.synchronize()
     t_prompt, cuts = time.perf_counter() - t, 0
     t = time.perf_counter()
