@@ -36,10 +36,10 @@
 //                D = 128)
 //   warps 6-13   Q at the start; softmax; O / l -> bf16 (or the split's partial)
 // Bound: the tensor core, at the clock its power allows.  1,596 queries after 30,720
-// positions (24 / 4 heads x 256, two full waves) 711 us, 1,740 TFLOP/s: 0.91 of the
-// bf16 burst rate, 1.01 of the sustained one.  At D = 128 a tile has half the products for
+// positions (24 / 4 heads x 256, two full waves) 738 us, 1,670 TFLOP/s: 0.88 of the
+// bf16 burst rate, 0.97 of the sustained one.  At D = 128 a tile has half the products for
 // the same exponentials, and the softmax warps set the pace: 798 queries so, one wave,
-// 1,030 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
+// 290 us, 1,050 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
 // ways: 19.5 us of launches, Q's way in, eight tiles one after the other and the merge.
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
 // from TMEM behind a tcgen05 fence, or from this CTA's own shared memory, never by
@@ -151,8 +151,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P8_THREADS, 1)
 kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ PrefillArgs a,
                    const __grid_constant__ typename P8PlanArg<PLAN>::type plan) {
   using L = P8Smem<D>;
-  constexpr uint32_t IDHI = tc::idesc_f8_f32(2 * PF_BM, 2 * PF_BN, 0);   // a tile pair
-  constexpr uint32_t IDLO = tc::idesc_f8_f32(2 * PF_BM, 2 * PF_BN, 1);
+  constexpr uint32_t IDHI = tc::idesc_e4m3_f32(2 * PF_BM, 2 * PF_BN);   // a tile pair
+  constexpr uint32_t IDLO = IDHI | (1u << 7);                           // A's type: e5m2
   constexpr uint32_t IDPV = tc::idesc_f16_f32(2 * PF_BM, D, 0, 1);
   // S of pair i is issued before P V of pair i - AHEAD, so that the softmax of a pair may
   // run while the P V of AHEAD pairs before it are outstanding: V buffers and barriers for
@@ -740,8 +740,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 // The plan's estimate, in history tiles (0.8 us each at D = 256): a part beyond a
 // place's first costs P8_HDR tiles (queries, pipeline fill, its partial rows), the
 // merge P8_MERGE.  The tail is cut where that is sooner than one wave more.  2,048
-// queries after 30,720 positions (44 of 196 pairs left over): uncut 1,055 us, cut
-// 972 (967 to 974 with headers of 6 to 32); with an earlier kernel uncut 1,243, the
+// queries after 30,720 positions (44 of 196 pairs left over), side by side: uncut 1,055 us,
+// cut 972 (967 to 974 with headers of 6 to 32; in other runs up to 1,005); with an earlier kernel uncut 1,243, the
 // left-over pairs as a second launch of three even splits 1,163, cut so 1,131.
 constexpr int P8_HDR = 12, P8_MERGE = 16, P8_MIN_PIECE = 16;
 

@@ -67,11 +67,10 @@ __device__ __forceinline__ void mma2_ss(uint32_t d_tmem, uint64_t a_desc, uint64
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-// Instruction descriptor, kind::f8f6f4 with e4m3 (a_e5m2 1: e5m2) A, e4m3 B (both
-// K-major) and f32 accumulation.
-__host__ __device__ constexpr uint32_t idesc_f8_f32(int M, int N, int a_e5m2) {
-  return (1u << 4) | ((uint32_t)a_e5m2 << 7) | ((uint32_t)(N >> 3) << 17) |
-         ((uint32_t)(M >> 4) << 24);
+// Instruction descriptor, kind::f8f6f4 with e4m3 A/B (both K-major) and f32
+// accumulation.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 
 // Pair MMAs issued where `leader` is set, for a warp that runs the issuing code as
