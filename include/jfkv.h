@@ -77,8 +77,8 @@ extern "C" {
 
 /*
  * 8-bit block format (no paper counterpart: a cache with twice the bytes of
- * the 4-bit formats and a relative error of at most 2^-4 per element).  The
- * codes are e4m3 values (1 sign, 4 exponent, 3 mantissa bits; bias 7; largest
+ * the 4-bit formats; an element is off by at most 2^-4 of itself, or, below
+ * 2^-6 of its block's scale, by 2^-10 of the scale).  The codes are e4m3 values (1 sign, 4 exponent, 3 mantissa bits; bias 7; largest
  * 448); positions 32 j .. 32 j + 31 of a KV head share a scale 2^e for K and
  * one for V:  x_hat = code * 2^e.  e is the smallest exponent with
  * max|x| <= 448 * 2^e over the block's finite values, limited to [-40, 40]
@@ -317,7 +317,12 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * num_splits > 1); over an E4M3 pool the two are one launch, the rest's
  * histories cut into one piece of equal work per pair of SMs.  With a smaller
  * workspace it runs undivided.  Both forms compute the same attention; the
- * summation order, and so the last bits, differ.
+ * summation order, and so the last bits, differ.  A chunk whose pairs fit one
+ * wave is not divided: a short chunk over a long prefix fills the GPU through
+ * jf_prefill_batch_attn with a batch of one and num_splits > 1.
+ * A page outside the pool sets JF_DEV_ERR_PAGE_ID; its positions then enter as
+ * zero keys and values, which draw weight (a decode leaves them out), so that
+ * the outputs which attend them are not reliable.
  * Numerics (affine pools): each 64-position K/V tile is rebuilt in shared
  * memory as fp16 code * scale + bias (one rounding) for the tensor cores, and
  * q * softmax_scale * log2(e) enters as fp16; accumulation and the softmax
