@@ -341,8 +341,8 @@ int jf_paged_decode_append_attn(const jf_kv_pool* pool, const int32_t* page_tabl
  * row (bf16's 8 bits exactly for elements within 2^13 of the row's largest,
  * at most 2^-21 of the largest off below); V's codes enter as fp16 (exact) and
  * the block scales are applied as in the decode; no scale is out of range.
- * A position a query does not see has the weight zero: a NaN among its values
- * (not its key) still reaches the queries of the chunk before it, as 0 * NaN.
+ * A NaN among a position's values reaches that channel of the queries that see
+ * the position, and no other.
  * A query row that holds an infinity or a NaN gives NaN.
  */
 int jf_prefill_chunk_attn(const jf_kv_pool* pool, const int32_t* page_table_row,

@@ -39,7 +39,7 @@
 // positions (24 / 4 heads x 256, two full waves) 738 us, 1,670 TFLOP/s: 0.88 of the
 // bf16 burst rate, 0.97 of the sustained one.  At D = 128 a tile has half the products for
 // the same exponentials, and the softmax warps set the pace: 798 queries so, one wave,
-// 290 us, 1,050 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
+// 294 us, 1,040 TFLOP/s.  77 queries after 4,001 positions (8 / 2 heads x 128), history split 8
 // ways: 19.5 us of launches, Q's way in, eight tiles one after the other and the merge.
 // Waits acquire at CTA scope: what a barrier publishes is read by the tensor core,
 // from TMEM behind a tcgen05 fence, or from this CTA's own shared memory, never by
@@ -94,7 +94,9 @@ struct P8Smem {
   static constexpr int OFF_X = OFF_L + 2 * PF_BM * 8;    // [128] largest magnitude of a Q row
   static constexpr int OFF_R = OFF_X + PF_BM * 4;        // [128] output row, -1: none
   static constexpr int OFF_OUT = OFF_R + PF_BM * 8;      // P8Out
-  static constexpr int TOTAL = 1024 + OFF_OUT + 16;
+  static constexpr int OFF_NAN = OFF_OUT + 16;           // [D + 1] first positions of NaN (below)
+  static constexpr int OFF_LIM = OFF_NAN + (D + 4) * 4;  // [128] last position a row sees
+  static constexpr int TOTAL = 1024 + OFF_LIM + PF_BM * 4;
   // at the end O's rows pass through what held Q, K and V on their way out
   static_assert(PF_BM * D * 4 <= OFF_BAR, "O rows");
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
@@ -141,6 +143,30 @@ __device__ __forceinline__ uint32_t row_max(uint32_t x) {
   }
 }
 
+// A value that is NaN and that some query of the pair does not see would reach that query as
+// 0 * NaN.  It enters the product as zero instead, and the first such position of its channel
+// is kept in both CTAs (`first`, shared; element D is the first of all channels), so that the
+// outputs of the queries that do see it can be made NaN at the end.  (798 queries at
+// D = 128 290 -> 294 us; at D = 256 no difference.)
+template <int D>
+__device__ __noinline__ void note_nan(uint32_t mask, int d, int pos, uint32_t first) {
+  for (uint32_t rank = 0; rank < 2; ++rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(first), "r"(rank));
+    for (int i = 0; i < 5; ++i)
+      if (i == 4 || ((mask >> (8 * i)) & 1u))
+        asm volatile("red.relaxed.cluster.shared::cluster.min.s32 [%0], %1;\n"
+                     ::"r"(at + 4 * (i == 4 ? D : d + i)), "r"(pos) : "memory");
+  }
+}
+// the codes of channels d .. d + 3 with NaN replaced by zero
+template <int D>
+__device__ __forceinline__ uint32_t without_nan(uint32_t w, int d, int pos, uint32_t first) {
+  const uint32_t mask = __vcmpeq4(w & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+  if (mask) note_nan<D>(mask, d, pos, first);
+  return w & ~mask;
+}
+
 struct P8NoPlan {};
 template <bool PLAN> struct P8PlanArg { using type = P8Plan; };
 template <> struct P8PlanArg<false> { using type = P8NoPlan; };
@@ -173,6 +199,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   int64_t* const s_row = reinterpret_cast<int64_t*>(sm + L::OFF_R);
   P8Out* const s_out = reinterpret_cast<P8Out*>(sm + L::OFF_OUT);
   uint32_t* const s_x = reinterpret_cast<uint32_t*>(sm + L::OFF_X);
+  int32_t* const s_nan = reinterpret_cast<int32_t*>(sm + L::OFF_NAN);
+  int32_t* const s_lim = reinterpret_cast<int32_t*>(sm + L::OFF_LIM);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // On CTA 0, where the pair's MMAs are issued:
   uint64_t* const k_full = bars + 0;     // [3] both CTAs' K halves of a pair have landed
@@ -247,11 +275,13 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   if (warp >= P8_SM_WARP0 && group == 0) {
     const int64_t at = (int64_t)(q0 + qi) * a.Hq + kvh * a.G + r % a.G;
     s_row[r] = !row_ok ? -1 : split ? ((int64_t)rq.row0 * a.Hq + at) * a.num_splits + z : at;
+    s_lim[r] = q_start + q0 + qi;
   }
   if (threadIdx.x == 0)
     *s_out = P8Out{split ? reinterpret_cast<uint8_t*>(a.part_o) : reinterpret_cast<uint8_t*>(rq.out),
                    split ? 1 : 0, last ? a.num_splits - 1 - z : 0};
   const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+  for (int i = threadIdx.x; i <= D; i += P8_THREADS) s_nan[i] = 0x7FFFFFFF;
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
     mbar_init(q_ready, 2 * 2 * PF_SM_WARPS);
@@ -478,6 +508,8 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
     // its 16-byte pieces (8 fp16) in the tile [D/128][64 rows][128 B]
     uint8_t* const dst = sV + (D == 256 ? part : 0) * (PF_BN * 128) + t * 128;
     const int piece0 = D == 256 ? 0 : 4 * part;
+    const int seen = a.causal ? q_start + min(qt, qt_partner) * a.QPC : 0x7FFFFFFF;   // by every row
+    const int d0 = (D == 256 ? 128 * (int)rank : 0) + 16 * code0;                     // first channel
     for (int j = 0; j < ntiles; ++j) {
       const int sb = j % P8_SBUF, vb = j % PVR;
       if (!mbar_wait_bounded(&s_land[sb], (j / P8_SBUF) & 1)) { ok = false; break; }
@@ -485,9 +517,19 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
 #pragma unroll
       for (int u = 0; u < NLD; ++u)
         c[u] = ld_shared_v4(src + sb * L::VS_BYTES + (((code0 + u) ^ (t & 7)) << 4));
-      if ((jb + j) * PF_BN + t >= kmax_pair) {   // a slot no query sees: whatever it holds
+      const int pos = (jb + j) * PF_BN + t;
+      if (pos >= kmax_pair) {   // a slot no query sees: whatever it holds
 #pragma unroll
         for (int u = 0; u < NLD; ++u) c[u] = make_uint4(0u, 0u, 0u, 0u);
+      } else if (pos > seen) {
+#pragma unroll
+        for (int u = 0; u < NLD; ++u) {
+          const uint32_t first = smem_u32(s_nan);
+          c[u].x = without_nan<D>(c[u].x, d0 + 16 * u, pos, first);
+          c[u].y = without_nan<D>(c[u].y, d0 + 16 * u + 4, pos, first);
+          c[u].z = without_nan<D>(c[u].z, d0 + 16 * u + 8, pos, first);
+          c[u].w = without_nan<D>(c[u].w, d0 + 16 * u + 12, pos, first);
+        }
       }
       uint32_t f[NLD][8];
 #pragma unroll
@@ -734,6 +776,18 @@ kv8_prefill_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_consta
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
+  }
+  if (warp >= P8_SM_WARP0 && all_ok && s_nan[D] != 0x7FFFFFFF) {   // NaN that some rows see
+    const P8Out out = *s_out;
+    const int64_t row_at = s_row[r];
+    const int limit = s_lim[r];
+    for (int d = group * (D / 2); d < (group + 1) * (D / 2) && row_at >= 0; ++d)
+      if (s_nan[d] <= limit) {
+        if (out.split)
+          reinterpret_cast<float*>(out.to)[row_at * D + d] = __uint_as_float(0x7FC00000u);
+        else
+          reinterpret_cast<uint16_t*>(out.to)[row_at * D + d] = 0x7FC0u;
+      }
   }
 }
 

@@ -249,3 +249,59 @@ def test_prefill_of_scaled_queries(qscale, hq, hkv, d):
         bound = (C.out_bound(ref[:, h], mass[:, h], n, top) + mass[:, h] * 2 * e.max(-1)[:, None] +
                  n * top * 448 * 2.0 ** -25)
         assert (np.abs(got[:, h] - ref[:, h]) <= bound).all(), float((np.abs(got[:, h] - ref[:, h]) / bound).max())
+
+
+@pytest.mark.parametrize("hq,hkv,d,p,start,c,splits", [(4, 2, 128, 64, 250, 150, 1), (6, 1, 256, 128, 0, 130, 1),
+                                                       (12, 2, 256, 64, 500, 90, 3), (1, 1, 128, 64, 63, 300, 1),
+                                                       (8, 1, 128, 256, 700, 40, 4)])
+def test_prefill_of_values_that_are_no_numbers(hq, hkv, d, p, start, c, splits):
+    """NaN among the values of a position reaches the channel it lies in, of the queries that see the position, and
+    nothing else: not the chunk's queries before it."""
+    rng = np.random.default_rng(c)
+    n = start + c
+    L, table, pool = C.filled(rng, hkv, p, d, [n])
+    q = queries(rng, c, hq, d)
+    want = prefill(L, table, pool, start, q, 0.1, splits)
+    assert np.isfinite(want).all()
+    hit = np.zeros((c, hkv, d), dtype=bool)
+    places = [(start + c - 1, 0, 5), (start + c // 2, 0, d - 1), (start + c // 2, hkv - 1, d // 2),
+              (start + 1, hkv - 1, 17), (start + 33, 0, d // 2 - 1), (start + 33, 0, 0), (start, 0, 64)]
+    if start > 64:
+        places.append((start - 40, hkv - 1, 3))           # seen by all of the chunk
+    for t, h, j in places:
+        pool[table[0, t // p], ((hkv + h) * p + t % p) * d + j] = (0x7F, 0xFF)[t % 2]
+        hit[max(t - start, 0):, h, j] = True
+    hit = np.repeat(hit, hq // hkv, 1)
+    got = prefill(L, table, pool, start, q, 0.1, splits)
+    assert np.isnan(got[hit]).all() and np.array_equal(got[~hit], want[~hit])
+
+
+def test_prefill_of_values_that_are_no_numbers_in_a_divided_wave():
+    """The same where the chunk's first rows have their histories in parts, and without a mask."""
+    rng = np.random.default_rng(9)
+    hq, hkv, d, p, start, c = 24, 4, 256, 256, 3400, 840
+    pages = -(-(start + c) // p)
+    g = jf.KVPool.allocate(pages, p, hkv, d, format=jf.JF_FMT_E4M3_B32)
+    order = rng.permutation(pages)
+    table = C.ints(order[None])
+    torch.manual_seed(2)
+    x = [torch.randn(start + c, hkv, d, device=DEV).bfloat16() for _ in range(2)]
+    jf.jf_kv8_append(g, table, C.ints([0]), C.ints([0, start + c]), *x)
+    q = torch.randn(c, hq, d, device=DEV).bfloat16()
+    ws = jf.prefill_chunk_workspace(g, start, c, hq)
+    outs = {}
+    for poison in (False, True):
+        if poison:
+            hit = torch.zeros(c, hkv, d, dtype=torch.bool, device=DEV)
+            for t, h, j in ((start + 1, 0, 7), (start + 20, 3, 200), (start + 839, 1, 0), (start + 400, 2, 127)):
+                g.data[int(order[t // p]), ((hkv + h) * p + t % p) * d + j] = 0x7F
+                hit[t - start:, h, j] = True
+        for causal in (True, False):
+            out = torch.full_like(q, 7.0)
+            jf.jf_prefill_chunk_attn(g, table[0], q, start, 1 / 16, causal, out, ws)
+            assert jf.workspace_status(ws) == 0
+            outs[poison, causal] = out
+    for causal in (True, False):
+        bad = (hit if causal else hit.any(0, keepdim=True).expand_as(hit)).repeat_interleave(hq // hkv, 1)
+        assert torch.isnan(outs[True, causal][bad]).all()
+        assert torch.equal(outs[True, causal][~bad], outs[False, causal][~bad])
