@@ -74,6 +74,8 @@ extern "C" {
 #define JF_FMT_TQ4         1      /* TQ4 (Sec. 3.1 Eq. 4), see below         */
 #define JF_FMT_E4M3_B32    8      /* 8-bit e4m3, one scale per 32 positions
                                      and KV head, see below                 */
+#define JF_FMT_LATENT16   16      /* one bf16 latent and rotated key a
+                                     position, for all heads, see below      */
 
 /*
  * 8-bit block format (no paper counterpart: a cache with twice the bytes of
@@ -88,6 +90,15 @@ extern "C" {
  * page_bytes = 2*Hkv*(P*D + P/8), 2,049 bytes per position and layer at
  * Hkv 4, D 256.  A reader takes a scale word's exponent bits alone and limits
  * them to [-40, 40].
+ */
+
+/*
+ * Latent format (no paper counterpart): a position is one row of bf16 values,
+ * the latent vector c of R channels that every head's key and value come from
+ * and the 64 rotated key channels r that all heads share.
+ *   page record = [P rows x (R + 64) bf16]
+ * A pool has num_kv_heads 1 and head_dim R + 64, R 256 or 512 (group_size is
+ * not used); page_bytes = 2*P*(R + 64).
  */
 
 /*
@@ -623,6 +634,129 @@ int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_s
                  int64_t weight_stride, int32_t budget, int32_t sinks, int32_t recent,
                  const int32_t* dst_page_table, int32_t dst_stride, int32_t* dst_context_lens,
                  float* dst_weights, int32_t* kept, int32_t* err_flag, void* stream);
+
+/* ======================================================================
+ * The latent cache (pools of format JF_FMT_LATENT16) and the attention that
+ * reads it.  jf_kv_checkpoint and jf_kv_restore copy its pages; the other
+ * entry points return JF_ERR_UNSUPPORTED for it.
+ * ====================================================================== */
+#define JF_LATENT_ROT        64    /* rotated key channels of a position      */
+#define JF_LATENT_MAX_GROUPS 64    /* groups of a jf_latent_prefix_decode_attn */
+
+/*
+ * Append runs of rows: rows row_offsets[b] .. row_offsets[b + 1] - 1 go to
+ * positions start_pos[b], start_pos[b] + 1, ... of request b.
+ *   page_table   int32 [num_requests, pt_stride]
+ *   start_pos    int32 [num_requests] on the device
+ *   row_offsets  int32 [num_requests + 1] on the device, from 0 up, <= n_rows
+ *   latent       bf16, row i at latent + i * latent_stride elements, its R
+ *                channels adjoining; k_rot the same, 64 channels.  16-byte
+ *                aligned, strides multiples of 8, latent_stride >= R,
+ *                rot_stride >= 64: the slices of one projection's output will do
+ *   n_rows       rows of both, >= row_offsets[num_requests]; 0: a no-op
+ *   err_flag     device int32 or NULL: JF_DEV_ERR_POSITION for a request whose
+ *                offsets or positions do not fit (it is skipped),
+ *                JF_DEV_ERR_PAGE_ID for a page outside the pool (its rows are)
+ */
+int jf_latent_append(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                     int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                     const void* latent, int64_t latent_stride, const void* k_rot,
+                     int64_t rot_stride, int32_t n_rows, int32_t* err_flag, void* stream);
+
+/* The inverse: runs of positions into latent and k_rot.  Rows of no request, and
+ * those that err_flag reports, are left as they are. */
+int jf_latent_read(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                   int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                   void* latent, int64_t latent_stride, void* k_rot, int64_t rot_stride,
+                   int32_t n_rows, int32_t* err_flag, void* stream);
+
+/* Workspace bytes of a latent decode (num_groups 0) or prefix decode call on a
+ * GPU with num_sms SMs (0: the current device's); independent of every length.
+ * 0 for invalid arguments. */
+size_t jf_latent_workspace_bytes(int32_t batch, int32_t num_heads, int32_t latent_dim,
+                                 int32_t num_groups, int32_t num_sms);
+
+/*
+ * Decode attention in the absorbed form: a head's query is (q_lat, q_rot), its
+ * R latent channels already multiplied by the head's key projection;
+ *   s_t = softmax_scale (q_lat . c_t + q_rot . r_t),   out = sum_t softmax(s)_t c_t
+ * over the positions t < context_lens[b] (zeros where there are none); the
+ * caller applies the head's value projection to out.
+ *   page_table    int32 [batch, pt_stride]
+ *   context_lens  int32 [batch] on the device
+ *   q             bf16 [batch, num_heads, R + 64], out bf16 [batch, num_heads, R],
+ *                 16-byte aligned; batch <= 65535, num_heads <= 1024
+ *   workspace     >= jf_latent_workspace_bytes(batch, num_heads, R, 0, 0) bytes,
+ *                 256-byte aligned, its first 256 bytes zero before the first
+ *                 call; its first int32 is the device status word
+ * A context length outside [0, pt_stride * P] sets JF_DEV_ERR_POSITION and counts
+ * as 0; positions of a page outside the pool draw no weight
+ * (JF_DEV_ERR_PAGE_ID).  Several tokens of one request (a draft's, say) go in as
+ * requests with the same page-table row and a context length each.
+ * Numerics: products of the bf16 values in fp32; maxima, sums and outputs in
+ * fp32.  The weights enter their product with c as bf16 (2^-8 of each), and the
+ * sum they are divided by is that of the rounded ones.
+ */
+int jf_latent_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                          const int32_t* context_lens, int32_t batch, const void* q,
+                          int32_t num_heads, float softmax_scale, void* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * The same where groups of requests begin with one shared run of positions (many
+ * continuations of one prompt): request b of group g, group_offsets[g] <= b <
+ * group_offsets[g + 1], attends the prefix_lens[g] positions of the group's pages
+ * and then the context_lens[b] positions of its own.  The prefix is read once for
+ * all queries of its group, whose rows are multiplied together.
+ *   prefix_table   int32 [num_groups, prefix_stride]
+ *   prefix_lens    int32 [num_groups] on the device
+ *   group_offsets  int32 [num_groups + 1] on the HOST, from 0 to batch, none
+ *                  below the one before; 1 <= num_groups <= JF_LATENT_MAX_GROUPS
+ *   page_table, context_lens  each request's own pages and positions
+ *   workspace      jf_latent_workspace_bytes(batch, num_heads, R, num_groups, 0)
+ * Other arguments, errors and numerics as above (a prefix length outside its
+ * table counts as 0).  To branch off inside a page, copy the prompt's last,
+ * partly filled page into each request's own: the prefix may end anywhere.
+ */
+int jf_latent_prefix_decode_attn(const jf_kv_pool* pool, const int32_t* prefix_table,
+                                 int32_t prefix_stride, const int32_t* prefix_lens,
+                                 const int32_t* group_offsets, int32_t num_groups,
+                                 const int32_t* page_table, int32_t pt_stride,
+                                 const int32_t* context_lens, int32_t batch, const void* q,
+                                 int32_t num_heads, float softmax_scale, void* out,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/* Workspace bytes of jf_latent_prefill_attn: the heads' expanded keys and values
+ * (512 bytes a position and head, as many heads at a time as fill the GPU) and the
+ * parts of a divided history.  num_sms as above.  0 for invalid arguments. */
+size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int32_t num_heads,
+                                         int32_t num_sms);
+
+/*
+ * Prefill-chunk attention in the expanded form: position t has the key
+ * (w_k[h] c_t, r_t) of 128 + 64 channels and the value w_v[h] c_t of 128 for head
+ * h; query i, at position q_start + i, attends positions [0, q_start + i]
+ * (causal != 0) or [0, q_start + chunk_len) of the request's cache, which must
+ * already hold the chunk's own rows (append, then attend).
+ *   page_table_row  int32 [>= ceil((q_start + chunk_len) / P)]
+ *   q               bf16 [chunk_len, num_heads, 192]: 128 channels, then the 64
+ *                   rotated ones
+ *   w_k, w_v        bf16 [num_heads, 128, R]
+ *   out             bf16 [chunk_len, num_heads, 128]
+ *   workspace       >= jf_latent_prefill_workspace_bytes(q_start, chunk_len,
+ *                   num_heads, 0) bytes, 256-byte aligned; its first int32 is the
+ *                   device status word, zero before the first call
+ * All 16-byte aligned; num_heads <= 1024; q_start + chunk_len < 2^31.
+ * A page outside the pool sets JF_DEV_ERR_PAGE_ID; the outputs that attend its
+ * positions are not reliable.  A value that is not finite reaches the queries that
+ * see its position, and no other.
+ * Numerics: products of bf16 values in fp32; the expanded keys and values and the
+ * weights are rounded to bf16 (2^-8 of each).
+ */
+int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row, const void* q,
+                           int32_t q_start, int32_t chunk_len, int32_t num_heads,
+                           const void* w_k, const void* w_v, float softmax_scale, int32_t causal,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Human-readable name of a JF_* status code. */
 const char* jf_status_string(int status);

@@ -1,5 +1,6 @@
-"""GB300-native paged 4-bit KV attention (the KVExec hot path of JustFit), and an
-8-bit cache with rotary axes and eviction for long image-and-text sessions.
+"""GB300-native paged 4-bit KV attention (the KVExec hot path of JustFit), an
+8-bit cache with rotary axes and eviction for long image-and-text sessions, and a
+latent cache with its attention.
 
 The compute lives in libjfkv.so (hand-written sm_103a CUDA behind a C ABI,
 include/jfkv.h); ``binding`` marshals torch tensors into those calls.
@@ -15,4 +16,7 @@ from .binding import (  # noqa: F401
     jf_prefill_chunk_workspace_bytes, prefill_chunk_workspace,
     JF_FMT_E4M3_B32, JF_KV8_BLOCK, Rope, jf_rope_axes, jf_kv8_append, jf_kv8_read,
     jf_paged_decode_weights_attn, decode_weights_workspace, jf_kv8_evict,
+    JF_FMT_LATENT16, JF_LATENT_ROT, jf_latent_append, jf_latent_read, jf_latent_decode_attn,
+    jf_latent_prefix_decode_attn, jf_latent_prefill_attn, jf_latent_workspace_bytes,
+    jf_latent_prefill_workspace_bytes, latent_decode_workspace, latent_prefill_workspace,
 )

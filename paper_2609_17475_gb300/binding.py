@@ -29,10 +29,13 @@ JF_DEV_ERR_RANGE = 16
 JF_FMT_AFFINE4_G64 = 0
 JF_FMT_TQ4 = 1
 JF_FMT_E4M3_B32 = 8
+JF_FMT_LATENT16 = 16
 JF_KV8_BLOCK = 32           # positions that share a scale in an E4M3 pool
 JF_ROPE_PAIR_HALF = 0
 JF_ROPE_PAIR_ADJACENT = 1
 JF_ROPE_MAX_AXES = 3
+JF_LATENT_ROT = 64          # rotated key channels of a latent pool's row
+JF_LATENT_MAX_GROUPS = 64
 
 EXPORTS = [
     "jf_kv_page_bytes", "jf_attn_workspace_bytes", "jf_prefill_workspace_bytes",
@@ -43,6 +46,8 @@ EXPORTS = [
     "jf_prefill_batch_workspace_bytes", "jf_prefill_chunk_workspace_bytes",
     "jf_selftest_bounded_wait", "jf_rope_axes", "jf_kv8_append", "jf_kv8_read",
     "jf_decode_weights_workspace_bytes", "jf_paged_decode_weights_attn", "jf_kv8_evict",
+    "jf_latent_append", "jf_latent_read", "jf_latent_workspace_bytes", "jf_latent_decode_attn",
+    "jf_latent_prefix_decode_attn", "jf_latent_prefill_workspace_bytes", "jf_latent_prefill_attn",
 ]
 JF_STATIC_WORKSPACE_BYTES = 8 << 20
 
@@ -126,6 +131,15 @@ def lib() -> ctypes.CDLL:
                                                             P, I64, P, SZ, I32, P]),
             "jf_kv8_evict": (ctypes.c_int, [PP, P, I32, P, I32, P, I64, I32, I32, I32, P, I32, P,
                                             P, P, P, P]),
+            "jf_latent_append": (ctypes.c_int, [PP, P, I32, I32, P, P, P, I64, P, I64, I32, P, P]),
+            "jf_latent_read": (ctypes.c_int, [PP, P, I32, I32, P, P, P, I64, P, I64, I32, P, P]),
+            "jf_latent_workspace_bytes": (SZ, [I32, I32, I32, I32, I32]),
+            "jf_latent_decode_attn": (ctypes.c_int, [PP, P, I32, P, I32, P, I32, F32, P, P, SZ, P]),
+            "jf_latent_prefix_decode_attn": (ctypes.c_int, [PP, P, I32, P, P, I32, P, I32, P, I32, P,
+                                                            I32, F32, P, P, SZ, P]),
+            "jf_latent_prefill_workspace_bytes": (SZ, [I32, I32, I32, I32]),
+            "jf_latent_prefill_attn": (ctypes.c_int, [PP, P, P, I32, I32, I32, P, P, F32, I32, P, P,
+                                                      SZ, P]),
             "jf_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "jf_version": (ctypes.c_char_p, []),
         }
@@ -264,7 +278,8 @@ class Tq4Codec:
 
 @dataclasses.dataclass
 class KVPool:
-    """A paged KV pool (4-bit, or 8-bit with JF_FMT_E4M3_B32): ``data`` is a CUDA uint8
+    """A paged KV pool (4-bit, 8-bit with JF_FMT_E4M3_B32, or one latent row a position with
+    JF_FMT_LATENT16: num_kv_heads 1, head_dim latent channels + 64): ``data`` is a CUDA uint8
     tensor [num_pages, page_bytes].  ``codec`` is required for the TQ4 format."""
     data: torch.Tensor
     page_size: int
@@ -814,3 +829,159 @@ def jf_kv8_evict(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Ten
                                        dst_page_table, dst_context_lens, dst_weights, kept, err_flag, stream)
     if st:
         raise JfError("jf_kv8_evict", st)
+
+
+# ---------------------------------------------------------------------------
+# the latent cache
+# ---------------------------------------------------------------------------
+def _latent_rows(fn, pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag, stream):
+    _need(page_table, torch.int32, "page_table")
+    _need(start_pos, torch.int32, "start_pos")
+    _need(row_offsets, torch.int32, "row_offsets")
+    if err_flag is not None:
+        _need(err_flag, torch.int32, "err_flag")
+    R = pool.head_dim - JF_LATENT_ROT
+    strides = []
+    for t, width, name in ((latent, R, "latent"), (k_rot, JF_LATENT_ROT, "k_rot")):
+        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
+        if t.dim() != 2 or t.shape[1] != width:
+            raise ValueError(f"{name} must be [rows, {width}]")
+        if t.shape[0] and t.stride(1) != 1:
+            raise ValueError(f"{name}: the channels of a row must adjoin")
+        # the row stride of a single row is whatever a slicing left: it is not used
+        strides.append(t.stride(0) if t.shape[0] > 1 else width)
+    n = latent.shape[0]
+    pt = page_table if page_table.dim() == 2 else page_table.view(1, -1)
+    if k_rot.shape[0] != n:
+        raise ValueError("latent and k_rot must have the same rows")
+    if start_pos.numel() != pt.shape[0] or row_offsets.numel() != pt.shape[0] + 1:
+        raise ValueError("one start_pos per page-table row, and one row offset more")
+    _check(fn, getattr(lib(), fn)(ctypes.byref(pool.c_struct()), _ptr(pt), pt.shape[1], pt.shape[0],
+                                  _ptr(start_pos), _ptr(row_offsets), _ptr(latent), strides[0],
+                                  _ptr(k_rot), strides[1], n, _ptr(err_flag), _stream(stream)))
+
+
+@_traced
+def jf_latent_append(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
+                     row_offsets: torch.Tensor, latent: torch.Tensor, k_rot: torch.Tensor,
+                     err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Append rows row_offsets[b] .. row_offsets[b + 1] - 1 of latent (bf16 [rows, R]) and
+    k_rot ([rows, 64], rows any stride apart) at positions start_pos[b] .. of request b."""
+    _latent_rows("jf_latent_append", pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag,
+                 stream)
+
+
+@_traced
+def jf_latent_read(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
+                   row_offsets: torch.Tensor, latent: torch.Tensor, k_rot: torch.Tensor,
+                   err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Read runs of positions back into latent and k_rot."""
+    _latent_rows("jf_latent_read", pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag,
+                 stream)
+
+
+def jf_latent_workspace_bytes(batch: int, num_heads: int, latent_dim: int, num_groups: int = 0,
+                              num_sms: int = 0) -> int:
+    return int(lib().jf_latent_workspace_bytes(batch, num_heads, latent_dim, num_groups, num_sms))
+
+
+def latent_decode_workspace(batch: int, num_heads: int, latent_dim: int, num_groups: int = 0,
+                            device="cuda") -> torch.Tensor:
+    """A workspace for jf_latent_decode_attn, or, with num_groups, jf_latent_prefix_decode_attn."""
+    n = jf_latent_workspace_bytes(batch, num_heads, latent_dim, num_groups)
+    if n == 0:
+        raise ValueError("invalid workspace geometry")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def _latent_decode_args(pool, page_table, context_lens, q, out, workspace):
+    _need(page_table, torch.int32, "page_table")
+    _need(context_lens, torch.int32, "context_lens")
+    _need(q, torch.bfloat16, "q")
+    _need(out, torch.bfloat16, "out")
+    _need(workspace, torch.uint8, "workspace")
+    if (q.dim() != 3 or q.shape[2] != pool.head_dim or page_table.dim() != 2
+            or tuple(out.shape) != (q.shape[0], q.shape[1], pool.head_dim - JF_LATENT_ROT)
+            or page_table.shape[0] != q.shape[0] or context_lens.numel() != q.shape[0]):
+        raise ValueError("shape mismatch")
+
+
+@_traced
+def jf_latent_decode_attn(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Tensor,
+                          q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
+                          workspace: torch.Tensor, stream=None) -> None:
+    """Decode attention over a latent pool, absorbed form: q is [batch, heads, R + 64], out
+    [batch, heads, R]: the weighted sum of the latents, before the heads' value projections."""
+    _latent_decode_args(pool, page_table, context_lens, q, out, workspace)
+    st = lib().jf_latent_decode_attn(ctypes.byref(pool.c_struct()), _ptr(page_table), page_table.shape[1],
+                                     _ptr(context_lens), q.shape[0], _ptr(q), q.shape[1],
+                                     float(softmax_scale), _ptr(out), _ptr(workspace), workspace.numel(),
+                                     _stream(stream))
+    _check("jf_latent_decode_attn", st)
+
+
+@_traced
+def jf_latent_prefix_decode_attn(pool: KVPool, prefix_table: torch.Tensor, prefix_lens: torch.Tensor,
+                                 group_offsets, page_table: torch.Tensor, context_lens: torch.Tensor,
+                                 q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
+                                 workspace: torch.Tensor, stream=None) -> None:
+    """jf_latent_decode_attn for groups of requests that begin with one shared run of positions:
+    request b of group g (group_offsets[g] <= b < group_offsets[g + 1], a host sequence) attends
+    prefix_lens[g] positions of prefix_table[g]'s pages, then context_lens[b] of its own."""
+    _latent_decode_args(pool, page_table, context_lens, q, out, workspace)
+    _need(prefix_table, torch.int32, "prefix_table")
+    _need(prefix_lens, torch.int32, "prefix_lens")
+    G = prefix_lens.numel()
+    if prefix_table.dim() != 2 or prefix_table.shape[0] != G or len(group_offsets) != G + 1:
+        raise ValueError("one prefix_table row and prefix length per group, and one group offset more")
+    off = (ctypes.c_int32 * (G + 1))(*[int(x) for x in group_offsets])
+    st = lib().jf_latent_prefix_decode_attn(ctypes.byref(pool.c_struct()), _ptr(prefix_table),
+                                            prefix_table.shape[1], _ptr(prefix_lens), off, G,
+                                            _ptr(page_table), page_table.shape[1], _ptr(context_lens),
+                                            q.shape[0], _ptr(q), q.shape[1], float(softmax_scale),
+                                            _ptr(out), _ptr(workspace), workspace.numel(),
+                                            _stream(stream))
+    _check("jf_latent_prefix_decode_attn", st)
+
+
+def jf_latent_prefill_workspace_bytes(q_start: int, chunk_len: int, num_heads: int,
+                                      num_sms: int = 0) -> int:
+    return int(lib().jf_latent_prefill_workspace_bytes(int(q_start), int(chunk_len), num_heads, num_sms))
+
+
+def latent_prefill_workspace(q_start: int, chunk_len: int, num_heads: int, device="cuda") -> torch.Tensor:
+    """A workspace for jf_latent_prefill_attn."""
+    n = jf_latent_prefill_workspace_bytes(q_start, chunk_len, num_heads)
+    if n == 0:
+        raise ValueError("invalid workspace geometry")
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+@_traced
+def jf_latent_prefill_attn(pool: KVPool, page_table_row: torch.Tensor, q: torch.Tensor, q_start: int,
+                           w_k: torch.Tensor, w_v: torch.Tensor, softmax_scale: float, causal: bool,
+                           out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    """Prefill-chunk attention over a latent pool, expanded form: q is [chunk, heads, 192] (128
+    channels and the 64 rotated ones), w_k and w_v [heads, 128, R], out [chunk, heads, 128]."""
+    _need(page_table_row, torch.int32, "page_table_row")
+    _need(q, torch.bfloat16, "q")
+    _need(w_k, torch.bfloat16, "w_k")
+    _need(w_v, torch.bfloat16, "w_v")
+    _need(out, torch.bfloat16, "out")
+    _need(workspace, torch.uint8, "workspace")
+    R = pool.head_dim - JF_LATENT_ROT
+    if (q.dim() != 3 or q.shape[2] != 128 + JF_LATENT_ROT or tuple(out.shape) != (q.shape[0], q.shape[1], 128)
+            or tuple(w_k.shape) != (q.shape[1], 128, R) or w_v.shape != w_k.shape):
+        raise ValueError("shape mismatch")
+    if page_table_row.numel() * pool.page_size < int(q_start) + q.shape[0]:
+        raise ValueError("the page-table row does not hold the chunk")
+    st = lib().jf_latent_prefill_attn(ctypes.byref(pool.c_struct()), _ptr(page_table_row), _ptr(q),
+                                      int(q_start), q.shape[0], q.shape[1], _ptr(w_k), _ptr(w_v),
+                                      float(softmax_scale), int(bool(causal)), _ptr(out), _ptr(workspace),
+                                      workspace.numel(), _stream(stream))
+    _check("jf_latent_prefill_attn", st)

@@ -5,6 +5,7 @@
 #include <mutex>
 
 #include "common.cuh"
+#include "latent.cuh"
 #include "prefill.cuh"
 #include "tq4.cuh"
 
@@ -102,9 +103,39 @@ int check_pool8(const jf_kv_pool* pool) {
 }
 
 // Pools of any format, for the entry points that read or copy all of them
-// (single-query decode, prefill, checkpoint, restore).
+// (single-query decode, prefill; page copies take latent pools as well).
 int check_pool_read(const jf_kv_pool* pool) {
   return pool && pool->format == JF_FMT_E4M3_B32 ? check_pool8(pool) : check_pool_any(pool);
+}
+
+// Latent pools.
+int check_pool_latent(const jf_kv_pool* pool) {
+  if (!pool || !pool->base || !aligned(pool->base, 16)) return JF_ERR_INVALID_ARG;
+  if (pool->num_pages < 1 || pool->num_kv_heads < 1) return JF_ERR_INVALID_ARG;
+  if (pool->format != JF_FMT_LATENT16) return JF_ERR_UNSUPPORTED;
+  if (pool->num_kv_heads != 1) return JF_ERR_UNSUPPORTED;
+  if (pool->head_dim != 256 + JF_LATENT_ROT && pool->head_dim != 512 + JF_LATENT_ROT)
+    return JF_ERR_UNSUPPORTED;
+  if (pool->page_size != 64 && pool->page_size != 128 && pool->page_size != 256)
+    return JF_ERR_UNSUPPORTED;
+  // a row's index is a 32-bit coordinate
+  if (pool->num_pages > 0x7FFFFFFFLL / pool->page_size) return JF_ERR_UNSUPPORTED;
+  return JF_OK;
+}
+
+// What page copies need to know of a pool: its pages' size.
+int copy_geom(const jf_kv_pool* pool, Geom* g) {
+  const bool latent = pool && pool->format == JF_FMT_LATENT16;
+  const int st = latent ? check_pool_latent(pool) : check_pool_read(pool);
+  if (st) return st;
+  if (latent) {
+    *g = Geom{};
+    g->num_pages = pool->num_pages;
+    g->page_bytes = (int64_t)pool->page_size * pool->head_dim * 2;
+  } else {
+    *g = make_geom(*pool);
+  }
+  return JF_OK;
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
@@ -181,6 +212,11 @@ size_t jf_kv_page_bytes(int32_t num_kv_heads, int32_t page_size, int32_t head_di
 
 size_t jf_kv_page_bytes_fmt(int32_t format, int32_t num_kv_heads, int32_t page_size,
                             int32_t head_dim) {
+  if (format == JF_FMT_LATENT16) {
+    if (num_kv_heads != 1 || page_size < 1) return 0;
+    if (head_dim != 256 + JF_LATENT_ROT && head_dim != 512 + JF_LATENT_ROT) return 0;
+    return (size_t)page_size * head_dim * 2;
+  }
   if (format != JF_FMT_AFFINE4_G64 && format != JF_FMT_TQ4 && format != JF_FMT_E4M3_B32) return 0;
   if (format == JF_FMT_E4M3_B32 && page_size % 32) return 0;
   if (num_kv_heads < 1 || page_size < 1 || (head_dim != 128 && head_dim != 256)) return 0;
@@ -531,12 +567,12 @@ int64_t jf_reservation_pages(int64_t prompt_len, int64_t output_len, int64_t g_o
 
 int jf_kv_checkpoint(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t num_pages,
                      void* dst, size_t dst_bytes, int32_t* err_flag, void* stream) {
-  int st = check_pool_read(pool);
+  Geom g;
+  const int st = copy_geom(pool, &g);
   if (st) return st;
   if (num_pages < 0) return JF_ERR_INVALID_ARG;
   if (num_pages == 0) return JF_OK;
   if (!page_table_row || !dst || !aligned(dst, 16)) return JF_ERR_INVALID_ARG;
-  const Geom g = make_geom(*pool);
   if (dst_bytes < (size_t)num_pages * (size_t)g.page_bytes) return JF_ERR_INVALID_ARG;
   return launch_page_copy(g, *pool, page_table_row, num_pages, dst, err_flag, true,
                           static_cast<cudaStream_t>(stream));
@@ -544,12 +580,12 @@ int jf_kv_checkpoint(const jf_kv_pool* pool, const int32_t* page_table_row, int3
 
 int jf_kv_restore(const jf_kv_pool* pool, const int32_t* page_table_row, int32_t num_pages,
                   const void* src, size_t src_bytes, int32_t* err_flag, void* stream) {
-  int st = check_pool_read(pool);
+  Geom g;
+  const int st = copy_geom(pool, &g);
   if (st) return st;
   if (num_pages < 0) return JF_ERR_INVALID_ARG;
   if (num_pages == 0) return JF_OK;
   if (!page_table_row || !src || !aligned(src, 16)) return JF_ERR_INVALID_ARG;
-  const Geom g = make_geom(*pool);
   if (src_bytes < (size_t)num_pages * (size_t)g.page_bytes) return JF_ERR_INVALID_ARG;
   return launch_page_copy(g, *pool, page_table_row, num_pages, const_cast<void*>(src), err_flag,
                           false, static_cast<cudaStream_t>(stream));
@@ -696,6 +732,159 @@ int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_s
                           weight_stride, budget, sinks, recent, dst_page_table, dst_stride,
                           dst_context_lens, dst_weights, kept, err_flag,
                           static_cast<cudaStream_t>(stream));
+}
+
+// ---------------------------------------------------------------------------
+// The latent cache
+// ---------------------------------------------------------------------------
+static int latent_rows(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                       int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                       void* latent, int64_t latent_stride, void* k_rot, int64_t rot_stride,
+                       int32_t n_rows, int32_t* err_flag, bool read, void* stream) {
+  const int st = check_pool_latent(pool);
+  if (st) return st;
+  if (n_rows < 0 || pt_stride < 1 || num_requests < 1) return JF_ERR_INVALID_ARG;
+  if (n_rows == 0) return JF_OK;
+  if (!page_table || !start_pos || !row_offsets || !latent || !k_rot) return JF_ERR_INVALID_ARG;
+  if (!aligned(latent, 16) || !aligned(k_rot, 16)) return JF_ERR_INVALID_ARG;
+  if (latent_stride % 8 || rot_stride % 8 || latent_stride < pool->head_dim - JF_LATENT_ROT ||
+      rot_stride < JF_LATENT_ROT)
+    return JF_ERR_INVALID_ARG;
+  return launch_latent_rows(latent_pool(*pool), page_table, pt_stride, num_requests, start_pos,
+                            row_offsets, latent, latent_stride, k_rot, rot_stride, n_rows,
+                            err_flag, read, static_cast<cudaStream_t>(stream));
+}
+
+int jf_latent_append(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                     int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                     const void* latent, int64_t latent_stride, const void* k_rot,
+                     int64_t rot_stride, int32_t n_rows, int32_t* err_flag, void* stream) {
+  return latent_rows(pool, page_table, pt_stride, num_requests, start_pos, row_offsets,
+                     const_cast<void*>(latent), latent_stride, const_cast<void*>(k_rot),
+                     rot_stride, n_rows, err_flag, false, stream);
+}
+
+int jf_latent_read(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                   int32_t num_requests, const int32_t* start_pos, const int32_t* row_offsets,
+                   void* latent, int64_t latent_stride, void* k_rot, int64_t rot_stride,
+                   int32_t n_rows, int32_t* err_flag, void* stream) {
+  return latent_rows(pool, page_table, pt_stride, num_requests, start_pos, row_offsets, latent,
+                     latent_stride, k_rot, rot_stride, n_rows, err_flag, true, stream);
+}
+
+size_t jf_latent_workspace_bytes(int32_t batch, int32_t num_heads, int32_t latent_dim,
+                                 int32_t num_groups, int32_t num_sms) {
+  if (batch < 1 || batch > 65535 || num_heads < 1 || num_heads > 1024) return 0;
+  if (latent_dim != 256 && latent_dim != 512) return 0;
+  if (num_groups < 0 || num_groups > JF_LATENT_MAX_GROUPS || num_sms < 0) return 0;
+  return latent_decode_workspace_bytes(batch, num_heads, latent_dim, num_groups,
+                                       num_sms ? num_sms : sm_count());
+}
+
+static int latent_decode(const jf_kv_pool* pool, const int32_t* prefix_table,
+                         int32_t prefix_stride, const int32_t* prefix_lens,
+                         const int32_t* group_offsets, int32_t num_groups,
+                         const int32_t* page_table, int32_t pt_stride,
+                         const int32_t* context_lens, int32_t batch, const void* q,
+                         int32_t num_heads, float softmax_scale, void* out, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  const int st = check_pool_latent(pool);
+  if (st) return st;
+  if (!page_table || !context_lens || !q || !out || !workspace) return JF_ERR_INVALID_ARG;
+  if (batch < 1 || batch > 65535 || pt_stride < 1 || num_heads < 1) return JF_ERR_INVALID_ARG;
+  if (num_heads > 1024) return JF_ERR_UNSUPPORTED;
+  if (!(softmax_scale == softmax_scale)) return JF_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 256)) return JF_ERR_INVALID_ARG;
+  LatentDecode a{};
+  if (num_groups) {
+    if (!prefix_table || !prefix_lens || !group_offsets || prefix_stride < 1 || num_groups < 1)
+      return JF_ERR_INVALID_ARG;
+    if (num_groups > JF_LATENT_MAX_GROUPS) return JF_ERR_UNSUPPORTED;
+    if (group_offsets[0] != 0 || group_offsets[num_groups] != batch) return JF_ERR_INVALID_ARG;
+    for (int g = 0; g < num_groups; ++g)
+      if (group_offsets[g + 1] < group_offsets[g]) return JF_ERR_INVALID_ARG;
+    for (int g = 0; g <= num_groups; ++g) a.first[g] = group_offsets[g];
+  }
+  if (workspace_bytes < jf_latent_workspace_bytes(batch, num_heads, pool->head_dim - JF_LATENT_ROT,
+                                                  num_groups, 0))
+    return JF_ERR_WORKSPACE_TOO_SMALL;
+  a.pool = latent_pool(*pool);
+  a.prefix_table = prefix_table;
+  a.prefix_lens = prefix_lens;
+  a.prefix_stride = prefix_stride;
+  a.num_groups = num_groups;
+  a.page_table = page_table;
+  a.context_lens = context_lens;
+  a.pt_stride = pt_stride;
+  a.batch = batch;
+  a.H = num_heads;
+  a.q = static_cast<const uint16_t*>(q);
+  a.out = static_cast<uint16_t*>(out);
+  a.scale_log2 = softmax_scale * 1.4426950408889634f;
+  a.status = static_cast<int32_t*>(workspace);
+  return launch_latent_decode(a, workspace, static_cast<cudaStream_t>(stream));
+}
+
+int jf_latent_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,
+                          const int32_t* context_lens, int32_t batch, const void* q,
+                          int32_t num_heads, float softmax_scale, void* out, void* workspace,
+                          size_t workspace_bytes, void* stream) {
+  return latent_decode(pool, nullptr, 0, nullptr, nullptr, 0, page_table, pt_stride, context_lens,
+                       batch, q, num_heads, softmax_scale, out, workspace, workspace_bytes, stream);
+}
+
+int jf_latent_prefix_decode_attn(const jf_kv_pool* pool, const int32_t* prefix_table,
+                                 int32_t prefix_stride, const int32_t* prefix_lens,
+                                 const int32_t* group_offsets, int32_t num_groups,
+                                 const int32_t* page_table, int32_t pt_stride,
+                                 const int32_t* context_lens, int32_t batch, const void* q,
+                                 int32_t num_heads, float softmax_scale, void* out,
+                                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (num_groups < 1) return JF_ERR_INVALID_ARG;
+  return latent_decode(pool, prefix_table, prefix_stride, prefix_lens, group_offsets, num_groups,
+                       page_table, pt_stride, context_lens, batch, q, num_heads, softmax_scale,
+                       out, workspace, workspace_bytes, stream);
+}
+
+size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int32_t num_heads,
+                                         int32_t num_sms) {
+  if (q_start < 0 || chunk_len < 0 || num_heads < 1 || num_heads > 1024 || num_sms < 0) return 0;
+  if ((int64_t)q_start + chunk_len > 0x7FFFFFFF) return 0;
+  return latent_prefill_workspace_bytes(q_start, chunk_len, num_heads,
+                                        num_sms ? num_sms : sm_count());
+}
+
+int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row, const void* q,
+                           int32_t q_start, int32_t chunk_len, int32_t num_heads,
+                           const void* w_k, const void* w_v, float softmax_scale, int32_t causal,
+                           void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  const int st = check_pool_latent(pool);
+  if (st) return st;
+  if (q_start < 0 || chunk_len < 0 || num_heads < 1) return JF_ERR_INVALID_ARG;
+  if (num_heads > 1024) return JF_ERR_UNSUPPORTED;
+  if ((int64_t)q_start + chunk_len > 0x7FFFFFFF) return JF_ERR_INVALID_ARG;
+  if (!(softmax_scale == softmax_scale)) return JF_ERR_INVALID_ARG;
+  if (chunk_len == 0) return JF_OK;
+  if (!page_table_row || !q || !w_k || !w_v || !out || !workspace) return JF_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(w_k, 16) || !aligned(w_v, 16) || !aligned(out, 16) ||
+      !aligned(workspace, 256))
+    return JF_ERR_INVALID_ARG;
+  if (workspace_bytes < jf_latent_prefill_workspace_bytes(q_start, chunk_len, num_heads, 0))
+    return JF_ERR_WORKSPACE_TOO_SMALL;
+  LatentPrefill a;
+  a.pool = latent_pool(*pool);
+  a.pt = page_table_row;
+  a.q = static_cast<const uint16_t*>(q);
+  a.w_k = static_cast<const uint16_t*>(w_k);
+  a.w_v = static_cast<const uint16_t*>(w_v);
+  a.out = static_cast<uint16_t*>(out);
+  a.q_start = q_start;
+  a.C = chunk_len;
+  a.H = num_heads;
+  a.causal = causal;
+  a.scale_log2 = softmax_scale * 1.4426950408889634f;
+  a.status = static_cast<int32_t*>(workspace);
+  return launch_latent_prefill(a, workspace, static_cast<cudaStream_t>(stream));
 }
 
 // ---------------------------------------------------------------------------
