@@ -189,36 +189,6 @@ __device__ void row_join(RowSmem<R>& s, RowState<R>& st) {
   __syncthreads();
 }
 
-__device__ __forceinline__ int checked_len(int n, int stride, int P, int32_t* status) {
-  if (n >= 0 && n <= (int64_t)stride * P) return n;
-  if (threadIdx.x == 0) flag_error(status, JF_DEV_ERR_POSITION);
-  return 0;
-}
-
-template <int R>
-__global__ void __launch_bounds__(32 * LS_WARPS)
-latent_decode_rows_kernel(const __grid_constant__ LatentDecode a) {
-  __shared__ RowSmem<R> s;
-  const int h = blockIdx.x, b = blockIdx.y;
-  const int64_t row = (int64_t)b * a.H + h;
-  for (int i = threadIdx.x; i < R + LAT_ROT; i += blockDim.x)
-    s.q[i] = __uint_as_float((uint32_t)a.q[row * (R + LAT_ROT) + i] << 16) * a.scale_log2;
-  __syncthreads();
-  RowState<R> st;
-  for (int i = 0; i < R / 32; ++i) st.o[i] = 0.f;
-  if (a.num_groups) {
-    int g = 0;
-    while (g + 1 < a.num_groups && a.first[g + 1] <= b) ++g;
-    const int n = checked_len(a.prefix_lens[g], a.prefix_stride, a.pool.P, a.status);
-    row_run<R>(a.pool, a.prefix_table + (int64_t)g * a.prefix_stride, n, s, st, a.status);
-  }
-  const int n = checked_len(a.context_lens[b], a.pt_stride, a.pool.P, a.status);
-  row_run<R>(a.pool, a.page_table + (int64_t)b * a.pt_stride, n, s, st, a.status);
-  row_join<R>(s, st);
-  for (int c = threadIdx.x * 2; c < R; c += blockDim.x * 2)
-    *reinterpret_cast<uint32_t*>(a.out + row * R + c) = pack_bf16x2(s.o[0][c], s.o[0][c + 1]);
-}
-
 template <int R>
 __global__ void __launch_bounds__(32 * LS_WARPS)
 latent_prefill_rows_kernel(const __grid_constant__ LatentPrefill a) {
@@ -247,17 +217,7 @@ latent_prefill_rows_kernel(const __grid_constant__ LatentPrefill a) {
   }
 }
 
-size_t latent_decode_workspace_bytes(int64_t, int64_t, int64_t, int64_t, int64_t) { return 256; }
 size_t latent_prefill_workspace_bytes(int64_t, int64_t, int64_t, int64_t) { return 256; }
-
-int launch_latent_decode(const LatentDecode& a, void*, cudaStream_t stream) {
-  const dim3 grid((unsigned)a.H, (unsigned)a.batch);
-  if (a.pool.R == 512)
-    latent_decode_rows_kernel<512><<<grid, 32 * LS_WARPS, 0, stream>>>(a);
-  else
-    latent_decode_rows_kernel<256><<<grid, 32 * LS_WARPS, 0, stream>>>(a);
-  return cudaGetLastError() == cudaSuccess ? JF_OK : JF_ERR_CUDA;
-}
 
 int launch_latent_prefill(const LatentPrefill& a, void*, cudaStream_t stream) {
   const dim3 grid((unsigned)a.C, (unsigned)a.H);

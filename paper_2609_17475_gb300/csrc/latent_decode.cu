@@ -1,0 +1,846 @@
+// Decode attention over the latent cache on the 5th-generation tensor cores: one
+// query a request, or groups of requests over a shared prefix.
+//
+// All heads read the same position rows, so up to 128 (request, head) rows form one
+// M = 128 tile of a CTA pair: S = Q K^T with K = (c, r) of R + 64 channels, O += P V
+// with V = c.  Each CTA of the pair holds 64 query rows and gets their S and O; of
+// the products' other operand it supplies half: of a tile of 128 positions its own
+// 64 rows of K, and its own R / 2 channels of V.  In tensor memory an M = 128 pair
+// product keeps columns 0 .. N/2 - 1 in lanes 0 - 63 and the others in lanes 64 - 127,
+// so O takes R / 2 columns and each thread of the four softmax warps has half a row.
+//
+// Work: the calls' items (a group's rows over its prefix, a request's heads over its
+// own positions), in tiles and a header each, are laid end to end and cut into one
+// run of equal length per CTA pair, whatever the lengths.  An item that one pair
+// takes whole is written out directly (decode) or as one partial (prefixes); of one
+// that is cut each pair writes an unnormalized partial (m, l, O), and a second kernel
+// joins them.  A pair has at most two cut items, so the workspace does not depend on
+// any length.
+//
+// Warp roles (each CTA):
+//   warp 0     TMEM; CTA 0: one thread issues the pair's MMAs; CTA 1: passes its K
+//              arrivals on
+//   warp 1     K by TMA
+//   warp 2     passes V's arrivals on; where a tile's last positions hold nothing yet it
+//              first clears them (a weight of zero does not undo a NaN)
+//   warp 3     V by TMA
+//   warps 4-7  Q into shared memory, softmax, O out
+#include <type_traits>
+
+#include "latent.cuh"
+#include "tc.cuh"
+
+namespace jfkv {
+
+int latent_tensor_map(const LatentPool& p, CUtensorMap* map);
+int sm_count();
+
+constexpr int LD_T = 128;           // positions a tile
+constexpr int LD_ROWS = 128;        // rows a pair, 64 each CTA
+constexpr int LD_HDR = 2;           // an item's fixed cost, in tiles
+constexpr int LD_THREADS = 256;
+constexpr float LD_TOP = 16.f;      // the reference maximum moves when a score exceeds it by this (log2)
+
+struct LatentPlan {
+  int32_t pairs;                    // CTA pairs of the launch
+  int32_t items, prefix_items, blocks;   // items; those of prefixes; row blocks of a request
+  int32_t slot_rows;                // rows of a cut item's partial
+  int32_t item0[LAT_MAX_GROUPS + 1];     // first items of the groups
+  int64_t* starts;                  // [items + 1], in units of tiles
+  float* ml;                        // [rows][2]
+  float* o;                         // [rows][R]
+};
+
+template <int R>
+struct LdSmem {
+  static constexpr int KC = R == 512 ? 3 : 5;          // 64-channel chunks of K a stage
+  static constexpr int KPT = (R / 64 + 1) / KC;        // stages a tile
+  static constexpr int KS = R == 512 ? 3 : 2;          // K stages
+  static constexpr int U = R / 256;                    // V stages a tile (256 channels of the pair)
+  static constexpr int VS = 2;                         // V stages
+  static constexpr int CHUNK = 64 * 128;               // 64 rows of 128 bytes
+  static constexpr int Q_BYTES = (R / 64 + 1) * CHUNK;
+  static constexpr int K_BYTES = KC * CHUNK;
+  static constexpr int V_BYTES = 2 * 2 * CHUNK;        // [2 x 64 channels][128 positions][128 B]
+  static constexpr int OFF_K = Q_BYTES;
+  static constexpr int OFF_V = OFF_K + KS * K_BYTES;
+  static constexpr int OFF_P = OFF_V + VS * V_BYTES;   // [2 x 64 positions][64 rows][128 B]
+  static constexpr int OFF_BAR = OFF_P + 2 * CHUNK;
+  static constexpr int OFF_X = OFF_BAR + 256;          // [2][128] exchange between a row's halves
+  static constexpr int OFF_PLAN = OFF_X + 2 * 128 * 4;     // [32] of the plan's scan
+  static constexpr int TOTAL = 1024 + OFF_PLAN + 32 * 8;
+  static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
+};
+
+__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn) {
+  return tc::idesc_f16_f32(M, N, 0, b_mn) | (1u << 7) | (1u << 10);
+}
+
+// Pair MMA, both operands in shared memory, issued by the one thread that runs this code.
+__device__ __forceinline__ void mma2_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
+                                          uint32_t accumulate) {
+  tc::mma2_ss(d, a, b, idesc, accumulate);
+}
+
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+               : "=r"(p));
+  return p != 0;
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];\n"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n"
+               ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// ---- items ------------------------------------------------------------------------
+struct LatentItem {
+  const int32_t* pt;
+  int32_t len, row0, nrows;
+};
+
+__device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan& pl, int i, int& g) {
+  int n, stride;
+  if (i < pl.prefix_items) {
+    g = 0;
+    while (pl.item0[g + 1] <= i) ++g;
+    n = a.prefix_lens[g];
+    stride = a.prefix_stride;
+  } else {
+    g = -1;
+    n = a.context_lens[(i - pl.prefix_items) / pl.blocks];
+    stride = a.pt_stride;
+  }
+  return n < 0 || n > (int64_t)stride * a.pool.P ? -1 : n;
+}
+
+__device__ __forceinline__ int tiles_of(int len) { return len <= 0 ? 0 : (len + LD_T - 1) / LD_T; }
+__device__ __forceinline__ int64_t units_of(int len) {
+  const int n = tiles_of(len);
+  return n ? n + LD_HDR : 0;
+}
+
+__device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const LatentPlan& pl, int i,
+                                              int g, int len) {
+  LatentItem it;
+  it.len = len;
+  if (g >= 0) {
+    it.row0 = a.first[g] * a.H + (i - pl.item0[g]) * LD_ROWS;
+    it.nrows = min(LD_ROWS, a.first[g + 1] * a.H - it.row0);
+    it.pt = a.prefix_table + (int64_t)g * a.prefix_stride;
+  } else {
+    const int k = i - pl.prefix_items, b = k / pl.blocks, hb = k - b * pl.blocks;
+    it.row0 = b * a.H + hb * LD_ROWS;
+    it.nrows = min(LD_ROWS, a.H - hb * LD_ROWS);
+    it.pt = a.page_table + (int64_t)b * a.pt_stride;
+  }
+  return it;
+}
+
+// The segments of a pair's run of units [u0, u1), in order.
+struct SegIter {
+  int64_t start, u0, u1;
+  int item;
+};
+struct Seg {
+  LatentItem it;
+  int item, j0, j1, n;   // tiles j0 .. j1 - 1 of the item's n
+};
+
+__device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan& pl, SegIter& s,
+                                         Seg& seg) {
+  while (s.item < pl.items && s.start < s.u1) {
+    int g;
+    const int len = item_len(a, pl, s.item, g);
+    const int n = tiles_of(len);
+    const int64_t first = s.start + LD_HDR;   // unit of tile 0
+    const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
+    const int i = s.item++;
+    if (n) s.start += n + LD_HDR;
+    if (lo < hi) {
+      seg.it = item_of(a, pl, i, g, len);
+      seg.item = i;
+      seg.j0 = (int)lo;
+      seg.j1 = (int)hi;
+      seg.n = n;
+      return true;
+    }
+  }
+  return false;
+}
+
+// first unit of pair p's run
+__device__ __forceinline__ int64_t unit_of_pair(int64_t units, int p, int pairs) {
+  return (int64_t)(((unsigned long long)units * (unsigned)p) / (unsigned)pairs);
+}
+
+// the page of the 64 positions from pos, as a row of the pool; past the map's end (the copy then
+// brings zeros) where there is none
+__device__ __forceinline__ int half_row(const LatentPool& p, const int32_t* pt, int pos, int len,
+                                        int32_t* status) {
+  const int end = (int)(p.num_pages << p.log2P);
+  if (pos >= len) return end;
+  const int32_t page = __ldg(pt + (pos >> p.log2P));
+  if (page < 0 || page >= p.num_pages) {
+    if (status) flag_error(status, JF_DEV_ERR_PAGE_ID);
+    return end;
+  }
+  return (page << p.log2P) + (pos & (p.P - 1));
+}
+
+template <int R>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LD_THREADS, 1)
+latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ LatentDecode a,
+                     const __grid_constant__ LatentPlan pl) {
+  using L = LdSmem<R>;
+  constexpr uint32_t IDQK = idesc_bf16(LD_ROWS, LD_T, 0);
+  constexpr uint32_t IDPV = idesc_bf16(LD_ROWS, 256, 1);
+  extern __shared__ uint8_t smraw[];
+  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) &
+                                           ~static_cast<uintptr_t>(1023));
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
+  // on CTA 0, where the pair's MMAs are issued:
+  uint64_t* const k_full = bars + 0;     // [3] both CTAs' K of a stage
+  uint64_t* const v_full = bars + 3;     // [2] both CTAs' V of a stage
+  uint64_t* const p_ready = bars + 5;    // both CTAs' P of a tile
+  uint64_t* const q_ready = bars + 6;    // both CTAs' Q of a segment
+  // on each CTA:
+  uint64_t* const k_land = bars + 7;     // [3] CTA 1: its K
+  uint64_t* const v_land = bars + 10;    // [2] its V
+  uint64_t* const k_free = bars + 12;    // [3] stage read by its products
+  uint64_t* const v_free = bars + 15;    // [2]
+  uint64_t* const s_full = bars + 17;    // [2] S of tile t % 2
+  uint64_t* const pv_done = bars + 19;   // P V of a tile
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 20);
+  float* const s_x = reinterpret_cast<float*>(sm + L::OFF_X);
+  int64_t* const s_plan = reinterpret_cast<int64_t*>(sm + L::OFF_PLAN);
+
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  const int pair = (int)(blockIdx.x >> 1);
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
+
+  // ---- the plan: units before each thread's items, and this pair's first item ----------
+  SegIter run;
+  {
+    const int per = (pl.items + LD_THREADS - 1) / LD_THREADS;
+    const int i0 = min(pl.items, (int)threadIdx.x * per), i1 = min(pl.items, i0 + per);
+    int64_t sum = 0;
+    for (int i = i0; i < i1; ++i) {
+      int g;
+      const int len = item_len(a, pl, i, g);
+      if (len < 0 && blockIdx.x == 0) flag_error(a.status, JF_DEV_ERR_POSITION);
+      sum += units_of(len);
+    }
+    int64_t incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    if (lane == 31) s_plan[warp] = incl;
+    __syncthreads();
+    int64_t before = 0, units = 0;
+    for (int w = 0; w < LD_THREADS / 32; ++w) {
+      if (w < warp) before += s_plan[w];
+      units += s_plan[w];
+    }
+    int64_t at = before + incl - sum;   // units before this thread's items
+    run.u0 = unit_of_pair(units, pair, pl.pairs);
+    run.u1 = unit_of_pair(units, pair + 1, pl.pairs);
+    const bool mine = run.u0 < run.u1 && at <= run.u0 && run.u0 < at + sum;
+    if (mine || blockIdx.x == 0)
+      for (int i = i0; i < i1; ++i) {
+        int g;
+        const int64_t n = units_of(item_len(a, pl, i, g));
+        if (blockIdx.x == 0) pl.starts[i] = at;
+        if (mine && at <= run.u0 && run.u0 < at + n) {
+          s_plan[8] = i;
+          s_plan[9] = at;
+        }
+        at += n;
+      }
+    if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
+    __syncthreads();
+    run.item = (int)s_plan[8];
+    run.start = s_plan[9];
+  }
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (run.u0 >= run.u1) return;   // both CTAs of the pair
+
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&k_full[i], 2);
+      mbar_init(&k_land[i], 1);
+      mbar_init(&k_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&v_full[i], 2);
+      mbar_init(&v_land[i], 1);
+      mbar_init(&v_free[i], 1);
+      mbar_init(&s_full[i], 1);
+    }
+    mbar_init(p_ready, 8);
+    mbar_init(q_ready, 8);
+    mbar_init(pv_done, 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) tc::alloc2(tmem_slot, 512);
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+  tc::fence_after();
+  // all 512 columns are this CTA's: O from 0, the S buffers behind it
+  constexpr uint32_t tO = 0, tS = R / 2;
+
+  bool ok = true;
+  Seg sg;
+  if (warp == 0) {
+    if (rank == 0) {
+      // ================= MMA issuer =================
+      if (elect_one()) {
+        const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
+        const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
+        const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 128 * 128, 1024);
+        const uint64_t pd = tc::sdesc_sw128(smem_u32(sm + L::OFF_P), 16, 1024);
+        int t = 0, nseg = 0;          // tiles and segments of all segments so far
+        // stages are constants of the code below: for R = 512 a tile takes all K and V stages once,
+        // for 256 the tile's parity names them
+        auto qk = [&](auto par, int tt) {
+          constexpr int PAR = decltype(par)::value;
+#pragma unroll
+          for (int c = 0; c < L::KPT; ++c) {
+            const int st = R == 512 ? c : PAR;
+            const int use = R == 512 ? tt : tt >> 1;      // how often the stage was filled before
+            if (!mbar_wait_bounded(&k_full[st], use & 1)) return false;
+            tc::fence_after();
+#pragma unroll
+            for (int k = 0; k < 4 * L::KC; ++k) {
+              const int ch = c * L::KC + (k >> 2);
+              mma2_bf16(tS + PAR * 64, qd + ((ch * L::CHUNK + (k & 3) * 32) >> 4),
+                        kd + ((st * L::K_BYTES + (k >> 2) * L::CHUNK + (k & 3) * 32) >> 4), IDQK,
+                        (c > 0 || k > 0) ? 1u : 0u);
+            }
+            tc::commit2_both(&k_free[st]);
+          }
+          tc::commit2_both(&s_full[PAR]);
+          return true;
+        };
+        auto pv = [&](auto par, int tt, bool first) {
+          constexpr int PAR = decltype(par)::value;
+          if (!mbar_wait_bounded(p_ready, tt & 1)) return false;
+#pragma unroll
+          for (int u = 0; u < L::U; ++u) {
+            const int st = R == 512 ? u : PAR;
+            const int use = R == 512 ? tt : tt >> 1;
+            if (!mbar_wait_bounded(&v_full[st], use & 1)) return false;
+            tc::fence_after();
+#pragma unroll
+            for (int k = 0; k < LD_T / 16; ++k)
+              mma2_bf16(tO + u * 128, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
+                        vd + ((st * L::V_BYTES + k * 2048) >> 4), IDPV, (!first || k > 0) ? 1u : 0u);
+            tc::commit2_both(&v_free[st]);
+          }
+          tc::commit2_both(pv_done);
+          return true;
+        };
+        while (ok && next_seg(a, pl, run, sg)) {
+          ok = mbar_wait_bounded(q_ready, nseg & 1);
+          ++nseg;
+          const int nt = sg.j1 - sg.j0;
+          for (int i = 0; i <= nt && ok; ++i) {   // S of tile i before P V of tile i - 1
+            if (i < nt)
+              ok = ((t + i) & 1) ? qk(std::integral_constant<int, 1>{}, t + i)
+                                 : qk(std::integral_constant<int, 0>{}, t + i);
+            if (i > 0 && ok)
+              ok = ((t + i - 1) & 1) ? pv(std::integral_constant<int, 1>{}, t + i - 1, i == 1)
+                                     : pv(std::integral_constant<int, 0>{}, t + i - 1, i == 1);
+          }
+          t += nt;
+        }
+        if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+      }
+      __syncwarp();
+    } else {
+      // ================= CTA 1's K arrivals =================
+      if (lane == 0) {
+        int ks = 0;
+        while (ok && next_seg(a, pl, run, sg))
+          for (int i = (sg.j1 - sg.j0) * L::KPT; i > 0 && ok; --i, ++ks) {
+            ok = mbar_wait_bounded(&k_land[ks % L::KS], (ks / L::KS) & 1);
+            if (ok) tc::arrive_cluster(&k_full[ks % L::KS], 0);
+          }
+        if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+      }
+      __syncwarp();
+    }
+  } else if (warp == 1) {
+    // ================= K: this CTA's 64 positions of each tile =================
+    if (lane == 0) {
+      int ks = 0;
+      while (ok && next_seg(a, pl, run, sg)) {
+        int y = half_row(a.pool, sg.it.pt, sg.j0 * LD_T + 64 * (int)rank, sg.it.len, a.status);
+        for (int j = sg.j0; j < sg.j1 && ok; ++j) {
+          const int row = y;
+          if (j + 1 < sg.j1)
+            y = half_row(a.pool, sg.it.pt, (j + 1) * LD_T + 64 * (int)rank, sg.it.len, a.status);
+          for (int c = 0; c < L::KPT; ++c, ++ks) {
+            const int st = ks % L::KS;
+            if (ks >= L::KS && !mbar_wait_bounded(&k_free[st], (ks / L::KS - 1) & 1)) {
+              ok = false;
+              break;
+            }
+            uint64_t* const land = rank == 0 ? &k_full[st] : &k_land[st];
+            mbar_arrive_expect_tx(land, L::K_BYTES);
+            const uint32_t dst = smem_u32(sm + L::OFF_K + st * L::K_BYTES);
+#pragma unroll
+            for (int k = 0; k < L::KC; ++k)
+              tma_load_2d(dst + k * L::CHUNK, &map, (c * L::KC + k) * 64, row, land);
+          }
+        }
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ================= V's arrivals; positions past the last one cleared =================
+    int vs = 0;
+    while (ok && next_seg(a, pl, run, sg))
+      for (int j = sg.j0; j < sg.j1 && ok; ++j) {
+        const int live = sg.it.len - j * LD_T;   // positions of this tile that there are
+        for (int u = 0; u < L::U; ++u, ++vs) {
+          const int st = vs % L::VS;
+          if (!mbar_wait_bounded(&v_land[st], (vs / L::VS) & 1)) {
+            ok = false;
+            break;
+          }
+          if (live < LD_T && (live & 63)) {   // past the half's end the copy brought zeros
+            const uint32_t at = smem_u32(sm + L::OFF_V + st * L::V_BYTES);
+            const int end = (live + 63) & ~63;
+            for (int p = live * 8 + lane; p < end * 8; p += 32)
+              for (int ch = 0; ch < 2; ++ch) sts128(at + ch * 2 * L::CHUNK + p * 16, 0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
+          }
+          __syncwarp();
+          if (lane == 0) tc::arrive_cluster(&v_full[st], 0);
+        }
+      }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+  } else if (warp == 3) {
+    // ================= V: this CTA's channels of all 128 positions =================
+    if (lane == 0) {
+      int vs = 0;
+      while (ok && next_seg(a, pl, run, sg))
+        for (int j = sg.j0; j < sg.j1 && ok; ++j) {
+          int row[2];
+          for (int h = 0; h < 2; ++h)
+            row[h] = half_row(a.pool, sg.it.pt, j * LD_T + 64 * h, sg.it.len, nullptr);
+          for (int u = 0; u < L::U; ++u, ++vs) {
+            const int st = vs % L::VS;
+            if (vs >= L::VS && !mbar_wait_bounded(&v_free[st], (vs / L::VS - 1) & 1)) {
+              ok = false;
+              break;
+            }
+            mbar_arrive_expect_tx(&v_land[st], L::V_BYTES);
+            const uint32_t dst = smem_u32(sm + L::OFF_V + st * L::V_BYTES);
+#pragma unroll
+            for (int ch = 0; ch < 2; ++ch)
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+                tma_load_2d(dst + (2 * ch + h) * L::CHUNK, &map,
+                            u * 256 + (int)rank * 128 + ch * 64, row[h], &v_land[st]);
+          }
+        }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else {
+    // ================= Q, softmax, O: thread 32 quarter + lane has row r's half =================
+    const int quarter = warp & 3, half = quarter >> 1;
+    const int r = (quarter & 1) * 32 + lane;
+    const int tid = quarter * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const uint32_t sp = smem_u32(sm + L::OFF_P);
+    auto pair_sync2 = [&] {   // the two warps that hold the same rows
+      asm volatile("bar.sync %0, 64;\n" ::"r"(1 + (quarter & 1)) : "memory");
+    };
+    auto load_q = [&](const LatentItem& it) {
+      constexpr int PIECES = (R + LAT_ROT) / 8;
+      const int rows = min(64, it.nrows - 64 * (int)rank);   // 0 or less: none
+      const uint16_t* const src = a.q + ((int64_t)it.row0 + 64 * rank) * (R + LAT_ROT);
+#pragma unroll 9
+      for (int i = tid; i < 64 * PIECES; i += 128) {
+        const int row = i / PIECES, piece = i - row * PIECES;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(src + (int64_t)row * (R + LAT_ROT) + piece * 8);
+        sts128(smem_u32(sm) + (piece >> 3) * L::CHUNK + row * 128 + (((piece & 7) ^ (row & 7)) << 4),
+               v.x, v.y, v.z, v.w);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::arrive_cluster(q_ready, 0);
+    };
+    int t = 0;
+    Seg nx;
+    bool more = next_seg(a, pl, run, sg);
+    if (more) load_q(sg.it);
+    while (more && ok) {
+      float m = -INFINITY, l = 0.f;
+      for (int j = sg.j0; j < sg.j1; ++j, ++t) {
+        const int pos = j * LD_T + half * 64;
+        const int end = (int)(a.pool.num_pages << a.pool.log2P);
+        const int live = half_row(a.pool, sg.it.pt, pos, sg.it.len, nullptr) == end
+                             ? 0 : min(64, sg.it.len - pos);
+        if (!mbar_wait_bounded(&s_full[t & 1], (t >> 1) & 1)) { ok = false; break; }
+        tc::fence_after();
+        uint32_t s[2][32];
+        tc::ld32(tS + (t & 1) * 64 + lane_off, s[0]);
+        tc::ld32(tS + (t & 1) * 64 + 32 + lane_off, s[1]);
+        tc::wait_ld();
+#pragma unroll
+        for (int c = 0; c < 64; ++c)
+          s[c >> 5][c & 31] = __float_as_uint(__uint_as_float(s[c >> 5][c & 31]) * a.scale_log2);
+        if (live < 64) {
+#pragma unroll
+          for (int c = 0; c < 64; ++c)
+            if (c >= live) s[c >> 5][c & 31] = 0xFF800000u;
+        }
+        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 64; ++c) x[c & 3] = fmaxf(x[c & 3], __uint_as_float(s[c >> 5][c & 31]));
+        // two buffers: a warp may be at the next tile before the other has read this one's
+        float* const sx = s_x + (t & 1) * 128;
+        sx[tid] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+        pair_sync2();
+        const float mt = fmaxf(sx[tid], sx[tid ^ 64]);
+        const bool up = mt > m + LD_TOP || (m == -INFINITY && mt > m);
+        const float m_new = up ? mt : m;
+        const float mm = m_new == -INFINITY ? 0.f : m_new;
+        float sum[2] = {0.f, 0.f};
+        uint32_t p[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) {
+          const float p0 = fast_exp2(__uint_as_float(s[c >> 4][(2 * c) & 31]) - mm);
+          const float p1 = fast_exp2(__uint_as_float(s[c >> 4][(2 * c + 1) & 31]) - mm);
+          p[c] = pack_bf16x2(p0, p1);
+          sum[0] += bf16lo_to_f32(p[c]);   // of the rounded weights, so that they add up to one
+          sum[1] += bf16hi_to_f32(p[c]);
+        }
+        if (j > sg.j0) {   // P is free, and O complete up to the last tile
+          if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
+          if (__any_sync(0xffffffffu, up)) {
+            tc::fence_after();
+            const float f = up && m != -INFINITY ? fast_exp2(m - m_new) : 1.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < R / 2; c0 += 32) {
+              uint32_t o[32];
+              tc::ld32(tO + c0 + lane_off, o);
+              tc::wait_ld();
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+              tc::st32(tO + c0 + lane_off, o);
+            }
+            tc::wait_st();
+            l *= f;
+          }
+        }
+        m = m_new;
+        l += sum[0] + sum[1];
+        const uint32_t to = sp + half * L::CHUNK + r * 128;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          sts128(to + ((k ^ (r & 7)) << 4), p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
+        fence_proxy_async_smem();
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) tc::arrive_cluster(p_ready, 0);
+      }
+      if (!ok) break;
+      // all products with Q are done (the last S has been seen): the next segment's queries
+      more = next_seg(a, pl, run, nx);
+      if (more) load_q(nx.it);
+      if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
+      tc::fence_after();
+      s_x[(t & 1) * 128 + tid] = l;
+      pair_sync2();
+      l += s_x[(t & 1) * 128 + (tid ^ 64)];
+      const bool whole = sg.j1 - sg.j0 == sg.n;
+      const bool direct = whole && a.num_groups == 0;
+      const int64_t prow =
+          whole ? (int64_t)2 * pl.pairs * pl.slot_rows +
+                      (sg.item < pl.prefix_items ? 0 : (int64_t)a.batch * a.H) + sg.it.row0
+                : (int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * pl.slot_rows;
+      const int64_t crow = (direct ? (int64_t)sg.it.row0 : prow) + 64 * rank;   // this CTA's first row
+      const int rows = sg.it.nrows - 64 * (int)rank;
+      if (!direct && half == 0 && r < rows)
+        *reinterpret_cast<float2*>(pl.ml + (crow + r) * 2) = make_float2(m, l);
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      // 128-byte pieces of the warp's 32 rows go through its part of P, so that whole lines are written
+      const uint32_t tr = sp + quarter * 4096;
+      const int row_base = (quarter & 1) * 32;
+      if (row_base < rows) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < R / 2; c0 += direct ? 64 : 32) {
+          uint32_t o[32];
+          tc::ld32(tO + c0 + lane_off, o);
+          tc::wait_ld();
+          if (direct) {
+            uint32_t o2[32];
+            tc::ld32(tO + c0 + 32 + lane_off, o2);
+            tc::wait_ld();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+              uint32_t w[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int c = 8 * k + 2 * i;
+                w[i] = pack_bf16x2(__uint_as_float(c < 32 ? o[c & 31] : o2[c & 31]) * inv,
+                                   __uint_as_float(c < 32 ? o[(c + 1) & 31] : o2[(c + 1) & 31]) * inv);
+              }
+              sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), o[4 * k], o[4 * k + 1], o[4 * k + 2],
+                     o[4 * k + 3]);
+          }
+          __syncwarp();
+          const int d0 = (c0 >> 7) * 256 + half * 128 + (c0 & 127);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int row = i * 4 + (lane >> 3), piece = lane & 7;
+            const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
+            if (row_base + row < rows) {
+              const int64_t at = (crow + row_base + row) * R + d0;
+              if (direct)
+                *reinterpret_cast<uint4*>(a.out + at + piece * 8) = v;
+              else
+                *reinterpret_cast<uint4*>(pl.o + at + piece * 4) = v;
+            }
+          }
+          __syncwarp();
+        }
+      }
+      tc::fence_before();
+      sg = nx;
+      pair_sync2();   // s_x read, and P's parts, before either warp goes on to write them
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+  }
+
+  // neither CTA may release TMEM or exit while its partner can still reach it
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  if (warp == 0) {
+    tc::fence_after();
+    tc::dealloc2(*tmem_slot, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Join the partials of each row that has any.  A CTA takes a row at a time: a thread
+// a partial for the weights, then 4 channels a thread, the partials in turn over
+// groups of R / 4 threads.
+// ---------------------------------------------------------------------------
+constexpr int LM_THREADS = 256;
+
+template <int R>
+__global__ void __launch_bounds__(LM_THREADS)
+latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
+  constexpr int LANES = R / 4, GROUPS = LM_THREADS / LANES;
+  __shared__ float s_w[LM_THREADS];
+  __shared__ int32_t s_row[LM_THREADS];
+  __shared__ float s_red[2][LM_THREADS / 32];
+  __shared__ float4 s_o[LM_THREADS];
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int64_t units = pl.starts[pl.items];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t total = (int64_t)a.batch * a.H;
+  for (int64_t row = blockIdx.x; row < total; row += gridDim.x) {
+    const int b = (int)(row / a.H), h = (int)(row - (int64_t)b * a.H);
+    // the row's partials: those of the prefix's item, then its own's
+    int count = 0;
+    bool direct = false;
+    __syncthreads();
+    for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
+      int item, inside;
+      if (part == 0) {
+        int g = 0;
+        while (a.first[g + 1] <= b) ++g;
+        inside = (int)(row - (int64_t)a.first[g] * a.H);
+        item = pl.item0[g] + inside / LD_ROWS;
+        inside %= LD_ROWS;
+      } else {
+        item = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
+        inside = h % LD_ROWS;
+      }
+      const int64_t s0 = pl.starts[item] + LD_HDR, s1 = pl.starts[item + 1];
+      if (s1 <= s0) continue;   // nothing there
+      const int p0 = (int)(((s0 + 1) * pl.pairs + units - 1) / units) - 1;
+      const int p1 = (int)((s1 * pl.pairs + units - 1) / units) - 1;
+      if (p0 == p1) {
+        if (a.num_groups == 0) direct = true;
+        if (threadIdx.x == 0)
+          s_row[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
+        ++count;
+        continue;
+      }
+      // pairs between the first and the last that have units at all
+      const int p = p0 + (int)threadIdx.x;
+      const bool has = p <= p1 && unit_of_pair(units, p, pl.pairs) < unit_of_pair(units, p + 1, pl.pairs);
+      const unsigned m = __ballot_sync(0xffffffffu, has);
+      if (lane == 0) s_red[0][warp] = __uint_as_float(__popc(m));
+      __syncthreads();
+      int at = count, all = 0;
+      for (int w = 0; w < LM_THREADS / 32; ++w) {
+        const int c = (int)__float_as_uint(s_red[0][w]);
+        if (w < warp) at += c;
+        all += c;
+      }
+      if (has) s_row[at + __popc(m & ((1u << lane) - 1))] = (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside;
+      count += all;
+      __syncthreads();
+    }
+    if (direct) continue;   // uniform over the CTA
+    __syncthreads();
+    // weights
+    float m = -INFINITY, l = 0.f;
+    if ((int)threadIdx.x < count) {
+      const float2 v = *reinterpret_cast<const float2*>(pl.ml + (int64_t)s_row[threadIdx.x] * 2);
+      m = v.x;
+      l = v.y;
+    }
+    float M = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    if (lane == 0) s_red[0][warp] = M;
+    __syncthreads();
+    M = s_red[0][0];
+    for (int w = 1; w < LM_THREADS / 32; ++w) M = fmaxf(M, s_red[0][w]);
+    // no maximum at all: sums of zero, or NaN where every score was
+    const float f = M == -INFINITY ? 1.f : fast_exp2(m - M);
+    float S = f * l;
+    s_w[threadIdx.x] = f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+    if (lane == 0) s_red[1][warp] = S;
+    __syncthreads();
+    S = 0.f;
+    for (int w = 0; w < LM_THREADS / 32; ++w) S += s_red[1][w];
+    const int c = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int i = grp; i < count; i += GROUPS) {
+      const float4 v = *reinterpret_cast<const float4*>(pl.o + (int64_t)s_row[i] * R + c * 4);
+      const float w = s_w[i];
+      acc.x = fmaf(v.x, w, acc.x);
+      acc.y = fmaf(v.y, w, acc.y);
+      acc.z = fmaf(v.z, w, acc.z);
+      acc.w = fmaf(v.w, w, acc.w);
+    }
+    s_o[threadIdx.x] = acc;
+    __syncthreads();
+    if (grp == 0) {
+      for (int g = 1; g < GROUPS; ++g) {
+        const float4 v = s_o[g * LANES + c];
+        acc.x += v.x;
+        acc.y += v.y;
+        acc.z += v.z;
+        acc.w += v.w;
+      }
+      const float inv = S != 0.f ? 1.f / S : 0.f;
+      *reinterpret_cast<uint2*>(a.out + row * R + c * 4) =
+          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+static int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+
+// items, and the partials' rows
+static void plan_sizes(int64_t batch, int64_t H, int64_t groups, int64_t sms, int64_t* items,
+                       int64_t* slot_rows, int64_t* rows) {
+  const int64_t pairs = sms / 2;
+  // a group's rows fill ceil(rows / 128) items; at most one of them is partly filled
+  *items = batch * ((H + LD_ROWS - 1) / LD_ROWS) + (groups ? groups + batch * H / LD_ROWS : 0);
+  *slot_rows = groups || H > LD_ROWS ? LD_ROWS : H;
+  *rows = 2 * pairs * *slot_rows + (groups ? 2 * batch * H : 0);
+}
+
+size_t latent_decode_workspace_bytes(int64_t batch, int64_t H, int64_t R, int64_t groups, int64_t sms) {
+  int64_t items, slot_rows, rows;
+  plan_sizes(batch, H, groups, sms, &items, &slot_rows, &rows);
+  return (size_t)(256 + round256((items + 1) * 8) + round256(rows * 8) + rows * R * 4);
+}
+
+template <int R>
+static int launch_t(const CUtensorMap& map, const LatentDecode& a, const LatentPlan& pl,
+                    cudaStream_t stream) {
+  if (smem_optin((const void*)latent_decode_kernel<R>, LdSmem<R>::TOTAL) != JF_OK) return JF_ERR_CUDA;
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * (unsigned)pl.pairs);
+  cfg.blockDim = dim3(LD_THREADS);
+  cfg.dynamicSmemBytes = LdSmem<R>::TOTAL;
+  cfg.stream = stream;
+  cfg.attrs = pdl;
+  cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, a, pl) != cudaSuccess) return JF_ERR_CUDA;
+  const int64_t rows = (int64_t)a.batch * a.H;
+  cfg.gridDim = dim3((unsigned)(rows < 16 * pl.pairs ? rows : 16 * pl.pairs));
+  cfg.blockDim = dim3(LM_THREADS);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, latent_merge_kernel<R>, a, pl) == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+}
+
+int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t stream) {
+  CUtensorMap map;
+  const int st = latent_tensor_map(a.pool, &map);
+  if (st) return st;
+  LatentPlan pl;
+  int64_t items, slot_rows, rows;
+  const int sms = sm_count();
+  plan_sizes(a.batch, a.H, a.num_groups, sms, &items, &slot_rows, &rows);
+  uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
+  pl.pairs = sms / 2;
+  pl.slot_rows = (int32_t)slot_rows;
+  pl.blocks = (a.H + LD_ROWS - 1) / LD_ROWS;
+  pl.item0[0] = 0;
+  for (int g = 0; g < a.num_groups; ++g)
+    pl.item0[g + 1] = pl.item0[g] + ((a.first[g + 1] - a.first[g]) * a.H + LD_ROWS - 1) / LD_ROWS;
+  pl.prefix_items = a.num_groups ? pl.item0[a.num_groups] : 0;
+  pl.items = pl.prefix_items + a.batch * pl.blocks;
+  pl.starts = reinterpret_cast<int64_t*>(ws);
+  ws += round256((items + 1) * 8);
+  pl.ml = reinterpret_cast<float*>(ws);
+  ws += round256(rows * 8);
+  pl.o = reinterpret_cast<float*>(ws);
+  return a.pool.R == 512 ? launch_t<512>(map, a, pl, stream) : launch_t<256>(map, a, pl, stream);
+}
+
+}  // namespace jfkv
