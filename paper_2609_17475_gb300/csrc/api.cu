@@ -196,16 +196,16 @@ int kv8_tensor_map(const Geom& g, void* base, int halves, int rows, int kv, CUte
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
-// 2-D map over a latent pool's rows, box = 64 channels of 64 rows, 128B swizzle.
-int latent_tensor_map(const LatentPool& p, CUtensorMap* map) {
+// 2-D map over rows of bf16 channels that adjoin, box = 64 channels of box_rows rows, 128B swizzle.
+int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows, CUtensorMap* map) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return JF_ERR_CUDA;
-  cuuint64_t dims[2] = {(cuuint64_t)p.row, (cuuint64_t)p.num_pages * p.P};
-  cuuint64_t strides[1] = {(cuuint64_t)p.row * 2};
-  cuuint32_t box[2] = {64, 64};
+  cuuint64_t dims[2] = {(cuuint64_t)channels, (cuuint64_t)rows};
+  cuuint64_t strides[1] = {(cuuint64_t)channels * 2};
+  cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
-  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<uint16_t*>(p.base), dims,
-                   strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides,
+                   box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }

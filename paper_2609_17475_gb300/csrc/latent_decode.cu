@@ -24,21 +24,25 @@
 //   warp 2     passes V's arrivals on; where a tile's last positions hold nothing yet it
 //              first clears them (a weight of zero does not undo a NaN)
 //   warp 3     V by TMA
-//   warps 4-7  Q into shared memory, softmax, O out
-#include <type_traits>
+//   warps 4-11 softmax (four threads a row), O out
+//   warp 12    Q by TMA, as soon as the last products with the segment's before are done
+#include <cmath>
 
 #include "latent.cuh"
-#include "tc.cuh"
+#include "prefill.cuh"
 
 namespace jfkv {
 
-int latent_tensor_map(const LatentPool& p, CUtensorMap* map);
+int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows, CUtensorMap* map);
 int sm_count();
 
 constexpr int LD_T = 128;           // positions a tile
 constexpr int LD_ROWS = 128;        // rows a pair, 64 each CTA
 constexpr int LD_HDR = 2;           // an item's fixed cost, in tiles
-constexpr int LD_THREADS = 256;
+constexpr int LD_THREADS = 32 * 13;
+constexpr int LD_SOFT = 8;           // softmax warps
+constexpr int LD_SBUF = 4;          // S buffers
+constexpr int LD_AHEAD = 2;         // S of a tile is issued before P V of the tile this many before it
 constexpr float LD_TOP = 16.f;      // the reference maximum moves when a score exceeds it by this (log2)
 
 struct LatentPlan {
@@ -66,9 +70,9 @@ struct LdSmem {
   static constexpr int OFF_V = OFF_K + KS * K_BYTES;
   static constexpr int OFF_P = OFF_V + VS * V_BYTES;   // [2 x 64 positions][64 rows][128 B]
   static constexpr int OFF_BAR = OFF_P + 2 * CHUNK;
-  static constexpr int OFF_X = OFF_BAR + 256;          // [2][128] exchange between a row's halves
-  static constexpr int OFF_PLAN = OFF_X + 2 * 128 * 4;     // [32] of the plan's scan
-  static constexpr int TOTAL = 1024 + OFF_PLAN + 32 * 8;
+  static constexpr int OFF_X = OFF_BAR + 256;          // [2][256] exchange between a row's threads
+  static constexpr int OFF_PLAN = OFF_X + 2 * 256 * 4; // [32] of the plan's scan
+  static constexpr int TOTAL = OFF_PLAN + 32 * 8;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -76,17 +80,29 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn) {
   return tc::idesc_f16_f32(M, N, 0, b_mn) | (1u << 7) | (1u << 10);
 }
 
-// Pair MMA, both operands in shared memory, issued by the one thread that runs this code.
-__device__ __forceinline__ void mma2_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                          uint32_t accumulate) {
-  tc::mma2_ss(d, a, b, idesc, accumulate);
+// Pair MMA, both operands in shared memory, issued where `leader` is set by a warp that runs the
+// issuing code as a whole: control flow and operands are then uniform values.  (Run by one thread
+// alone, each descriptor was moved to uniform registers first: 72 to 100 cycles an instruction for
+// the 32 to 64 that the product takes.)
+__device__ __forceinline__ void mma2_ss_if(uint32_t leader, uint32_t d, uint64_t a, uint64_t b,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
 
-__device__ __forceinline__ bool elect_one() {
+__device__ __forceinline__ uint32_t elect_one() {
   uint32_t p;
   asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
                : "=r"(p));
-  return p != 0;
+  return p;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y,
@@ -114,18 +130,17 @@ struct LatentItem {
   int32_t len, row0, nrows;
 };
 
-__device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan& pl, int i, int& g) {
-  int n, stride;
-  if (i < pl.prefix_items) {
-    g = 0;
-    while (pl.item0[g + 1] <= i) ++g;
-    n = a.prefix_lens[g];
-    stride = a.prefix_stride;
-  } else {
-    g = -1;
-    n = a.context_lens[(i - pl.prefix_items) / pl.blocks];
-    stride = a.pt_stride;
-  }
+// the group of item i, -1 for a request's own positions
+__device__ __forceinline__ int item_group(const LatentPlan& pl, int i) {
+  if (i >= pl.prefix_items) return -1;
+  int g = 0;
+  while (pl.item0[g + 1] <= i) ++g;
+  return g;
+}
+// its positions, -1 where their number does not fit the table
+__device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan& pl, int i, int g) {
+  const int n = g >= 0 ? a.prefix_lens[g] : a.context_lens[(i - pl.prefix_items) / pl.blocks];
+  const int stride = g >= 0 ? a.prefix_stride : a.pt_stride;
   return n < 0 || n > (int64_t)stride * a.pool.P ? -1 : n;
 }
 
@@ -156,6 +171,7 @@ __device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const Laten
 struct SegIter {
   int64_t start, u0, u1;
   int item;
+  int known;    // the first item's length, read already
 };
 struct Seg {
   LatentItem it;
@@ -165,8 +181,9 @@ struct Seg {
 __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan& pl, SegIter& s,
                                          Seg& seg) {
   while (s.item < pl.items && s.start < s.u1) {
-    int g;
-    const int len = item_len(a, pl, s.item, g);
+    const int g = item_group(pl, s.item);
+    const int len = s.known >= 0 ? s.known : item_len(a, pl, s.item, g);
+    s.known = -1;
     const int n = tiles_of(len);
     const int64_t first = s.start + LD_HDR;   // unit of tile 0
     const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
@@ -185,9 +202,24 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
 }
 
 // first unit of pair p's run
-__device__ __forceinline__ int64_t unit_of_pair(int64_t units, int p, int pairs) {
-  return (int64_t)(((unsigned long long)units * (unsigned)p) / (unsigned)pairs);
+__device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
+  return (x | y) >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y);
 }
+struct PairRuns {   // floor(units * p / pairs), by one division
+  int64_t units, each;
+  uint32_t rest, pairs;
+  __device__ __forceinline__ PairRuns(int64_t u, int n) : units(u), pairs((uint32_t)n) {
+    each = (int64_t)divide((uint64_t)u, pairs);
+    rest = (uint32_t)(u - each * n);
+  }
+  __device__ __forceinline__ int64_t first(int p) const {
+    return each * p + (uint32_t)p * rest / pairs;
+  }
+  // the pair that has unit u: the last p with first(p) <= u
+  __device__ __forceinline__ int of(int64_t u) const {
+    return (int)divide((uint64_t)(u + 1) * pairs + (uint64_t)units - 1, (uint64_t)units) - 1;
+  }
+};
 
 // the page of the 64 positions from pos, as a row of the pool; past the map's end (the copy then
 // brings zeros) where there is none
@@ -205,28 +237,29 @@ __device__ __forceinline__ int half_row(const LatentPool& p, const int32_t* pt, 
 
 template <int R>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LD_THREADS, 1)
-latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ LatentDecode a,
+latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap qmap,
+                     const __grid_constant__ LatentDecode a,
                      const __grid_constant__ LatentPlan pl) {
   using L = LdSmem<R>;
   constexpr uint32_t IDQK = idesc_bf16(LD_ROWS, LD_T, 0);
   constexpr uint32_t IDPV = idesc_bf16(LD_ROWS, 256, 1);
-  extern __shared__ uint8_t smraw[];
-  uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smraw) + 1023) &
-                                           ~static_cast<uintptr_t>(1023));
+  extern __shared__ __align__(1024) uint8_t sm[];
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // on CTA 0, where the pair's MMAs are issued:
   uint64_t* const k_full = bars + 0;     // [3] both CTAs' K of a stage
   uint64_t* const v_full = bars + 3;     // [2] both CTAs' V of a stage
   uint64_t* const p_ready = bars + 5;    // both CTAs' P of a tile
-  uint64_t* const q_ready = bars + 6;    // both CTAs' Q of a segment
+  uint64_t* const q_full = bars + 6;     // both CTAs' Q of a segment
   // on each CTA:
   uint64_t* const k_land = bars + 7;     // [3] CTA 1: its K
   uint64_t* const v_land = bars + 10;    // [2] its V
   uint64_t* const k_free = bars + 12;    // [3] stage read by its products
   uint64_t* const v_free = bars + 15;    // [2]
-  uint64_t* const s_full = bars + 17;    // [2] S of tile t % 2
-  uint64_t* const pv_done = bars + 19;   // P V of a tile
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 20);
+  uint64_t* const s_full = bars + 17;    // [4] S of tile t % 4
+  uint64_t* const pv_done = bars + 21;   // P V of a tile
+  uint64_t* const q_land = bars + 22;    // CTA 1: its Q
+  uint64_t* const q_free = bars + 23;    // products with a segment's Q done
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 24);
   float* const s_x = reinterpret_cast<float*>(sm + L::OFF_X);
   int64_t* const s_plan = reinterpret_cast<int64_t*>(sm + L::OFF_PLAN);
 
@@ -234,6 +267,32 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
   const int pair = (int)(blockIdx.x >> 1);
+  if (smem_u32(sm) & 1023u) {   // the swizzled layouts need it; the same in every CTA
+    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&map);
+    prefetch_tensormap(&qmap);
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(&k_full[i], 2);
+      mbar_init(&k_land[i], 1);
+      mbar_init(&k_free[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&v_full[i], 2);
+      mbar_init(&v_land[i], 1);
+      mbar_init(&v_free[i], 1);
+    }
+    for (int i = 0; i < LD_SBUF; ++i) mbar_init(&s_full[i], 1);
+    mbar_init(p_ready, 2 * LD_SOFT);
+    mbar_init(q_full, 2);
+    mbar_init(q_land, 1);
+    mbar_init(q_free, 1);
+    mbar_init(pv_done, 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) tc::alloc2(tmem_slot, 512);
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
 
   // ---- the plan: units before each thread's items, and this pair's first item ----------
@@ -242,10 +301,11 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     const int per = (pl.items + LD_THREADS - 1) / LD_THREADS;
     const int i0 = min(pl.items, (int)threadIdx.x * per), i1 = min(pl.items, i0 + per);
     int64_t sum = 0;
+    int len0 = -1;   // of this thread's first item
     for (int i = i0; i < i1; ++i) {
-      int g;
-      const int len = item_len(a, pl, i, g);
+      const int len = item_len(a, pl, i, item_group(pl, i));
       if (len < 0 && blockIdx.x == 0) flag_error(a.status, JF_DEV_ERR_POSITION);
+      if (i == i0) len0 = len;
       sum += units_of(len);
     }
     int64_t incl = sum;
@@ -262,51 +322,32 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       units += s_plan[w];
     }
     int64_t at = before + incl - sum;   // units before this thread's items
-    run.u0 = unit_of_pair(units, pair, pl.pairs);
-    run.u1 = unit_of_pair(units, pair + 1, pl.pairs);
+    const PairRuns runs(units, pl.pairs);
+    run.u0 = runs.first(pair);
+    run.u1 = runs.first(pair + 1);
     const bool mine = run.u0 < run.u1 && at <= run.u0 && run.u0 < at + sum;
     if (mine || blockIdx.x == 0)
       for (int i = i0; i < i1; ++i) {
-        int g;
-        const int64_t n = units_of(item_len(a, pl, i, g));
+        const int len = i == i0 ? len0 : item_len(a, pl, i, item_group(pl, i));
+        const int64_t n = units_of(len);
         if (blockIdx.x == 0) pl.starts[i] = at;
         if (mine && at <= run.u0 && run.u0 < at + n) {
-          s_plan[8] = i;
-          s_plan[9] = at;
+          s_plan[16] = i;
+          s_plan[17] = at;
+          s_plan[18] = len;
         }
         at += n;
       }
     if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
+    tc::fence_before();
     __syncthreads();
-    run.item = (int)s_plan[8];
-    run.start = s_plan[9];
+    tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+    tc::fence_after();
+    run.item = run.u0 < run.u1 ? (int)s_plan[16] : pl.items;
+    run.start = s_plan[17];
+    run.known = run.u0 < run.u1 ? (int)s_plan[18] : -1;
   }
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-  if (run.u0 >= run.u1) return;   // both CTAs of the pair
-
-  if (threadIdx.x == 0) {
-    prefetch_tensormap(&map);
-    for (int i = 0; i < 3; ++i) {
-      mbar_init(&k_full[i], 2);
-      mbar_init(&k_land[i], 1);
-      mbar_init(&k_free[i], 1);
-    }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&v_full[i], 2);
-      mbar_init(&v_land[i], 1);
-      mbar_init(&v_free[i], 1);
-      mbar_init(&s_full[i], 1);
-    }
-    mbar_init(p_ready, 8);
-    mbar_init(q_ready, 8);
-    mbar_init(pv_done, 1);
-    fence_barrier_init();
-  }
-  if (warp == 0) tc::alloc2(tmem_slot, 512);
-  tc::fence_before();
-  __syncthreads();
-  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
-  tc::fence_after();
   // all 512 columns are this CTA's: O from 0, the S buffers behind it
   constexpr uint32_t tO = 0, tS = R / 2;
 
@@ -315,78 +356,78 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   if (warp == 0) {
     if (rank == 0) {
       // ================= MMA issuer =================
-      if (elect_one()) {
-        const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
-        const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
-        const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 128 * 128, 1024);
-        const uint64_t pd = tc::sdesc_sw128(smem_u32(sm + L::OFF_P), 16, 1024);
-        int t = 0, nseg = 0;          // tiles and segments of all segments so far
-        // stages are constants of the code below: for R = 512 a tile takes all K and V stages once,
-        // for 256 the tile's parity names them
-        auto qk = [&](auto par, int tt) {
-          constexpr int PAR = decltype(par)::value;
+      const uint32_t leader = elect_one();
+      const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
+      const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
+      const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 128 * 128, 1024);
+      const uint64_t pd = tc::sdesc_sw128(smem_u32(sm + L::OFF_P), 16, 1024);
+      auto wait = [&](uint64_t* bar, int phase) {
+        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
+      };
+      int ks = 0, vs = 0, t = 0, nseg = 0;   // stages, tiles and segments of all segments so far
+      while (__all_sync(0xffffffffu, ok && next_seg(a, pl, run, sg))) {
+        ok = wait(q_full, nseg);
+        ++nseg;
+        const int nt = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
+        for (int i = 0; i < nt + LD_AHEAD && ok; ++i) {
+          if (i < nt) {
+            const uint32_t d = tS + ((t + i) % LD_SBUF) * 64;
+            uint64_t q = qd;
+#pragma unroll 1
+            for (int c = 0; c < L::KPT && ok; ++c, ++ks, q += (L::K_BYTES >> 4)) {
+              const int st = ks % L::KS;
+              ok = wait(&k_full[st], ks / L::KS);
+              tc::fence_after();
+              const uint64_t k0 = kd + (uint64_t)(st * (L::K_BYTES >> 4));
+              if (ok) {
 #pragma unroll
-          for (int c = 0; c < L::KPT; ++c) {
-            const int st = R == 512 ? c : PAR;
-            const int use = R == 512 ? tt : tt >> 1;      // how often the stage was filled before
-            if (!mbar_wait_bounded(&k_full[st], use & 1)) return false;
-            tc::fence_after();
-#pragma unroll
-            for (int k = 0; k < 4 * L::KC; ++k) {
-              const int ch = c * L::KC + (k >> 2);
-              mma2_bf16(tS + PAR * 64, qd + ((ch * L::CHUNK + (k & 3) * 32) >> 4),
-                        kd + ((st * L::K_BYTES + (k >> 2) * L::CHUNK + (k & 3) * 32) >> 4), IDQK,
-                        (c > 0 || k > 0) ? 1u : 0u);
+                for (int k = 0; k < 4 * L::KC; ++k) {
+                  const uint32_t at = ((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4;
+                  mma2_ss_if(leader, d, q + at, k0 + at, IDQK, (c > 0 || k > 0) ? 1u : 0u);
+                }
+                tc::commit2_both_if(leader, &k_free[st]);
+              }
             }
-            tc::commit2_both(&k_free[st]);
+            if (ok) tc::commit2_both_if(leader, &s_full[(t + i) % LD_SBUF]);
+            if (ok && i == nt - 1) tc::commit2_both_if(leader, q_free);
           }
-          tc::commit2_both(&s_full[PAR]);
-          return true;
-        };
-        auto pv = [&](auto par, int tt, bool first) {
-          constexpr int PAR = decltype(par)::value;
-          if (!mbar_wait_bounded(p_ready, tt & 1)) return false;
+          const int j = i - LD_AHEAD;   // the segment's tile whose P V is due
+          if (j >= 0 && ok) {
+            ok = wait(p_ready, t + j);
+#pragma unroll 1
+            for (int u = 0; u < L::U && ok; ++u, ++vs) {
+              const int st = vs % L::VS;
+              ok = wait(&v_full[st], vs / L::VS);
+              tc::fence_after();
+              const uint64_t v0 = vd + (uint64_t)(st * (L::V_BYTES >> 4));
+              if (ok) {
 #pragma unroll
-          for (int u = 0; u < L::U; ++u) {
-            const int st = R == 512 ? u : PAR;
-            const int use = R == 512 ? tt : tt >> 1;
-            if (!mbar_wait_bounded(&v_full[st], use & 1)) return false;
-            tc::fence_after();
-#pragma unroll
-            for (int k = 0; k < LD_T / 16; ++k)
-              mma2_bf16(tO + u * 128, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
-                        vd + ((st * L::V_BYTES + k * 2048) >> 4), IDPV, (!first || k > 0) ? 1u : 0u);
-            tc::commit2_both(&v_free[st]);
+                for (int k = 0; k < LD_T / 16; ++k)
+                  mma2_ss_if(leader, tO + u * 128, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
+                             v0 + ((k * 2048) >> 4), IDPV, (j > 0 || k > 0) ? 1u : 0u);
+                tc::commit2_both_if(leader, &v_free[st]);
+              }
+            }
+            if (ok) tc::commit2_both_if(leader, pv_done);
           }
-          tc::commit2_both(pv_done);
-          return true;
-        };
-        while (ok && next_seg(a, pl, run, sg)) {
-          ok = mbar_wait_bounded(q_ready, nseg & 1);
-          ++nseg;
-          const int nt = sg.j1 - sg.j0;
-          for (int i = 0; i <= nt && ok; ++i) {   // S of tile i before P V of tile i - 1
-            if (i < nt)
-              ok = ((t + i) & 1) ? qk(std::integral_constant<int, 1>{}, t + i)
-                                 : qk(std::integral_constant<int, 0>{}, t + i);
-            if (i > 0 && ok)
-              ok = ((t + i - 1) & 1) ? pv(std::integral_constant<int, 1>{}, t + i - 1, i == 1)
-                                     : pv(std::integral_constant<int, 0>{}, t + i - 1, i == 1);
-          }
-          t += nt;
         }
-        if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+        t += nt;
       }
+      if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
       __syncwarp();
     } else {
-      // ================= CTA 1's K arrivals =================
+      // ================= CTA 1's Q and K arrivals =================
       if (lane == 0) {
-        int ks = 0;
-        while (ok && next_seg(a, pl, run, sg))
+        int ks = 0, nseg = 0;
+        while (ok && next_seg(a, pl, run, sg)) {
+          ok = mbar_wait_bounded(q_land, nseg & 1);
+          if (ok) tc::arrive_cluster(q_full, 0);
+          ++nseg;
           for (int i = (sg.j1 - sg.j0) * L::KPT; i > 0 && ok; --i, ++ks) {
             ok = mbar_wait_bounded(&k_land[ks % L::KS], (ks / L::KS) & 1);
             if (ok) tc::arrive_cluster(&k_full[ks % L::KS], 0);
           }
+        }
         if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
       }
       __syncwarp();
@@ -471,77 +512,93 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     }
     __syncwarp();
+  } else if (warp == 4 + LD_SOFT) {
+    // ================= Q: 64 rows from the item's first; rows past its last are computed and not
+    // stored =================
+    if (lane == 0) {
+      // (a barrier of its own: one that other tiles complete as well could be a phase behind, and its
+      // parity then says yes too early)
+      int nseg = 0;
+      while (ok && next_seg(a, pl, run, sg)) {
+        if (nseg > 0 && !mbar_wait_bounded(q_free, (nseg - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        ++nseg;
+        uint64_t* const land = rank == 0 ? q_full : q_land;
+        mbar_arrive_expect_tx(land, L::Q_BYTES);
+        for (int c = 0; c < L::Q_BYTES / L::CHUNK; ++c)
+          tma_load_2d(smem_u32(sm) + c * L::CHUNK, &qmap, c * 64, sg.it.row0 + 64 * (int)rank, land);
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
   } else {
-    // ================= Q, softmax, O: thread 32 quarter + lane has row r's half =================
-    const int quarter = warp & 3, half = quarter >> 1;
+    // ================= softmax, O =================
+    // Four threads have a row: of its lane with the tile's first 64 positions and the one with the
+    // others, each half of the 64 (and half of O's columns of that lane).
+    const int quarter = warp & 3, half = quarter >> 1, side = warp >= 4 + LD_SOFT / 2 ? 1 : 0;
     const int r = (quarter & 1) * 32 + lane;
-    const int tid = quarter * 32 + lane;
+    const int tid = (int)threadIdx.x - 4 * 32;
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t sp = smem_u32(sm + L::OFF_P);
-    auto pair_sync2 = [&] {   // the two warps that hold the same rows
-      asm volatile("bar.sync %0, 64;\n" ::"r"(1 + (quarter & 1)) : "memory");
-    };
-    auto load_q = [&](const LatentItem& it) {
-      constexpr int PIECES = (R + LAT_ROT) / 8;
-      const int rows = min(64, it.nrows - 64 * (int)rank);   // 0 or less: none
-      const uint16_t* const src = a.q + ((int64_t)it.row0 + 64 * rank) * (R + LAT_ROT);
-#pragma unroll 9
-      for (int i = tid; i < 64 * PIECES; i += 128) {
-        const int row = i / PIECES, piece = i - row * PIECES;
-        uint4 v = make_uint4(0u, 0u, 0u, 0u);
-        if (row < rows) v = *reinterpret_cast<const uint4*>(src + (int64_t)row * (R + LAT_ROT) + piece * 8);
-        sts128(smem_u32(sm) + (piece >> 3) * L::CHUNK + row * 128 + (((piece & 7) ^ (row & 7)) << 4),
-               v.x, v.y, v.z, v.w);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) tc::arrive_cluster(q_ready, 0);
+    // the four warps that hold the same rows
+    auto row_sync = [&] { asm volatile("bar.sync %0, 128;\n" ::"r"(1 + (quarter & 1)) : "memory"); };
+    // weights are 2^(sc S - m), sc above zero: a scale below it negates S first, one of zero makes it
+    // zero (or NaN)
+    const float sc = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+    const int end = (int)(a.pool.num_pages << a.pool.log2P);
+    // positions of this thread's 32 in tile j that there are
+    auto live_of = [&](const Seg& g, int j) {
+      const int pos = j * LD_T + half * 64;
+      return half_row(a.pool, g.it.pt, pos, g.it.len, nullptr) == end ? 0 : g.it.len - pos - side * 32;
     };
     int t = 0;
     Seg nx;
     bool more = next_seg(a, pl, run, sg);
-    if (more) load_q(sg.it);
     while (more && ok) {
       float m = -INFINITY, l = 0.f;
+      int live = live_of(sg, sg.j0);
       for (int j = sg.j0; j < sg.j1; ++j, ++t) {
-        const int pos = j * LD_T + half * 64;
-        const int end = (int)(a.pool.num_pages << a.pool.log2P);
-        const int live = half_row(a.pool, sg.it.pt, pos, sg.it.len, nullptr) == end
-                             ? 0 : min(64, sg.it.len - pos);
-        if (!mbar_wait_bounded(&s_full[t & 1], (t >> 1) & 1)) { ok = false; break; }
+        if (!mbar_wait_bounded(&s_full[t % LD_SBUF], (t / LD_SBUF) & 1)) { ok = false; break; }
         tc::fence_after();
-        uint32_t s[2][32];
-        tc::ld32(tS + (t & 1) * 64 + lane_off, s[0]);
-        tc::ld32(tS + (t & 1) * 64 + 32 + lane_off, s[1]);
+        uint32_t s[32];
+        tc::ld32(tS + (t % LD_SBUF) * 64 + side * 32 + lane_off, s);
         tc::wait_ld();
+        if (!(a.scale_log2 > 0.f)) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c)
-          s[c >> 5][c & 31] = __float_as_uint(__uint_as_float(s[c >> 5][c & 31]) * a.scale_log2);
-        if (live < 64) {
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (c >= live) s[c >> 5][c & 31] = 0xFF800000u;
+          for (int c = 0; c < 32; ++c)
+            s[c] = a.scale_log2 < 0.f ? s[c] ^ 0x80000000u : __float_as_uint(__uint_as_float(s[c]) * 0.f);
         }
-        float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        if (live < 32) {
 #pragma unroll
-        for (int c = 0; c < 64; ++c) x[c & 3] = fmaxf(x[c & 3], __uint_as_float(s[c >> 5][c & 31]));
-        // two buffers: a warp may be at the next tile before the other has read this one's
-        float* const sx = s_x + (t & 1) * 128;
-        sx[tid] = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-        pair_sync2();
-        const float mt = fmaxf(sx[tid], sx[tid ^ 64]);
+          for (int c = 0; c < 32; ++c)
+            if (c >= live) s[c] = 0xFF800000u;
+        }
+        if (j + 1 < sg.j1) live = live_of(sg, j + 1);
+        float x[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          x[c & 1] = max3(x[c & 1], __uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+        // two buffers: a warp may be at the next tile before the others have read this one's
+        float* const sx = s_x + (t & 1) * 256;
+        sx[tid] = fmaxf(x[0], x[1]);
+        row_sync();
+        const float mt = sc * fmaxf(fmaxf(sx[tid], sx[tid ^ 64]), fmaxf(sx[tid ^ 128], sx[tid ^ 192]));
         const bool up = mt > m + LD_TOP || (m == -INFINITY && mt > m);
         const float m_new = up ? mt : m;
         const float mm = m_new == -INFINITY ? 0.f : m_new;
-        float sum[2] = {0.f, 0.f};
-        uint32_t p[32];
+        const uint64_t kk = f32x2(sc, sc), cc = f32x2(-mm, -mm);
+        uint64_t sum = f32x2(0.f, 0.f);
+        uint32_t p[16];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          const float p0 = fast_exp2(__uint_as_float(s[c >> 4][(2 * c) & 31]) - mm);
-          const float p1 = fast_exp2(__uint_as_float(s[c >> 4][(2 * c + 1) & 31]) - mm);
-          p[c] = pack_bf16x2(p0, p1);
-          sum[0] += bf16lo_to_f32(p[c]);   // of the rounded weights, so that they add up to one
-          sum[1] += bf16hi_to_f32(p[c]);
+        for (int c = 0; c < 16; ++c) {
+          float d0, d1;
+          unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1])), kk, cc),
+                       d0, d1);
+          p[c] = pack_bf16x2(fast_exp2(d0), fast_exp2(d1));
+          // of the rounded weights, so that they add up to one
+          sum = add_f32x2(sum, f32x2(bf16lo_to_f32(p[c]), bf16hi_to_f32(p[c])));
         }
         if (j > sg.j0) {   // P is free, and O complete up to the last tile
           if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
@@ -549,7 +606,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             tc::fence_after();
             const float f = up && m != -INFINITY ? fast_exp2(m - m_new) : 1.f;
 #pragma unroll 1
-            for (int c0 = 0; c0 < R / 2; c0 += 32) {
+            for (int c0 = side * (R / 4); c0 < (side + 1) * (R / 4); c0 += 32) {
               uint32_t o[32];
               tc::ld32(tO + c0 + lane_off, o);
               tc::wait_ld();
@@ -561,26 +618,27 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             l *= f;
           }
         }
-        m = m_new;
-        l += sum[0] + sum[1];
         const uint32_t to = sp + half * L::CHUNK + r * 128;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          sts128(to + ((k ^ (r & 7)) << 4), p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
+        for (int k = 0; k < 4; ++k)
+          sts128(to + (((4 * side + k) ^ (r & 7)) << 4), p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]);
         fence_proxy_async_smem();
         tc::fence_before();
         __syncwarp();
         if (lane == 0) tc::arrive_cluster(p_ready, 0);
+        m = m_new;
+        float u, v;
+        unpack_f32x2(sum, u, v);
+        l += u + v;
       }
       if (!ok) break;
-      // all products with Q are done (the last S has been seen): the next segment's queries
       more = next_seg(a, pl, run, nx);
-      if (more) load_q(nx.it);
       if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
       tc::fence_after();
-      s_x[(t & 1) * 128 + tid] = l;
-      pair_sync2();
-      l += s_x[(t & 1) * 128 + (tid ^ 64)];
+      float* const sx = s_x + (t & 1) * 256;
+      sx[tid] = l;
+      row_sync();
+      l = (sx[tid] + sx[tid ^ 64]) + (sx[tid ^ 128] + sx[tid ^ 192]);
       const bool whole = sg.j1 - sg.j0 == sg.n;
       const bool direct = whole && a.num_groups == 0;
       const int64_t prow =
@@ -589,59 +647,54 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 : (int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * pl.slot_rows;
       const int64_t crow = (direct ? (int64_t)sg.it.row0 : prow) + 64 * rank;   // this CTA's first row
       const int rows = sg.it.nrows - 64 * (int)rank;
-      if (!direct && half == 0 && r < rows)
+      if (!direct && half == 0 && side == 0 && r < rows)
         *reinterpret_cast<float2*>(pl.ml + (crow + r) * 2) = make_float2(m, l);
       const float inv = l != 0.f ? 1.f / l : 0.f;
-      // 128-byte pieces of the warp's 32 rows go through its part of P, so that whole lines are written
-      const uint32_t tr = sp + quarter * 4096;
+      // 64-byte pieces of the warp's 32 rows go through its part of P, so that whole sectors are
+      // written: piece p of row i at p ^ ((i >> 1) & 3).  The part is one of the same four warps' rows:
+      // the other four may be at their next tile's P already.
       const int row_base = (quarter & 1) * 32;
+      const uint32_t tr = sp + half * L::CHUNK + row_base * 128 + side * 2048;
       if (row_base < rows) {
 #pragma unroll 1
-        for (int c0 = 0; c0 < R / 2; c0 += direct ? 64 : 32) {
+        for (int c0 = side * (R / 4); c0 < (side + 1) * (R / 4); c0 += 32) {
           uint32_t o[32];
           tc::ld32(tO + c0 + lane_off, o);
           tc::wait_ld();
-          if (direct) {
-            uint32_t o2[32];
-            tc::ld32(tO + c0 + 32 + lane_off, o2);
-            tc::wait_ld();
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-              uint32_t w[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const int c = 8 * k + 2 * i;
-                w[i] = pack_bf16x2(__uint_as_float(c < 32 ? o[c & 31] : o2[c & 31]) * inv,
-                                   __uint_as_float(c < 32 ? o[(c + 1) & 31] : o2[(c + 1) & 31]) * inv);
-              }
-              sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), o[4 * k], o[4 * k + 1], o[4 * k + 2],
-                     o[4 * k + 3]);
-          }
-          __syncwarp();
           const int d0 = (c0 >> 7) * 256 + half * 128 + (c0 & 127);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int row = i * 4 + (lane >> 3), piece = lane & 7;
-            const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
-            if (row_base + row < rows) {
-              const int64_t at = (crow + row_base + row) * R + d0;
-              if (direct)
-                *reinterpret_cast<uint4*>(a.out + at + piece * 8) = v;
-              else
-                *reinterpret_cast<uint4*>(pl.o + at + piece * 4) = v;
+          for (int h = 0; h < 2; ++h) {
+            if (direct && h == 1) break;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              uint32_t w[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                w[i] = direct ? pack_bf16x2(__uint_as_float(o[8 * k + 2 * i]) * inv,
+                                            __uint_as_float(o[8 * k + 2 * i + 1]) * inv)
+                              : o[16 * h + 4 * k + i];
+              sts128(tr + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
             }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int row = i * 8 + (lane >> 2), piece = lane & 3;
+              const uint4 v = lds128(tr + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
+              if (row_base + row < rows) {
+                const int64_t at = (crow + row_base + row) * R + d0;
+                if (direct)
+                  *reinterpret_cast<uint4*>(a.out + at + piece * 8) = v;
+                else
+                  *reinterpret_cast<uint4*>(pl.o + at + 16 * h + piece * 4) = v;
+              }
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
       }
       tc::fence_before();
       sg = nx;
-      pair_sync2();   // s_x read, and P's parts, before either warp goes on to write them
+      row_sync();   // s_x read, and P's parts, before a warp goes on to write them
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   }
@@ -672,7 +725,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
   __shared__ float s_red[2][LM_THREADS / 32];
   __shared__ float4 s_o[LM_THREADS];
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const int64_t units = pl.starts[pl.items];
+  const PairRuns runs(pl.starts[pl.items], pl.pairs);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t total = (int64_t)a.batch * a.H;
   for (int64_t row = blockIdx.x; row < total; row += gridDim.x) {
@@ -695,8 +748,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
       }
       const int64_t s0 = pl.starts[item] + LD_HDR, s1 = pl.starts[item + 1];
       if (s1 <= s0) continue;   // nothing there
-      const int p0 = (int)(((s0 + 1) * pl.pairs + units - 1) / units) - 1;
-      const int p1 = (int)((s1 * pl.pairs + units - 1) / units) - 1;
+      const int p0 = runs.of(s0), p1 = runs.of(s1 - 1);
       if (p0 == p1) {
         if (a.num_groups == 0) direct = true;
         if (threadIdx.x == 0)
@@ -706,7 +758,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
       }
       // pairs between the first and the last that have units at all
       const int p = p0 + (int)threadIdx.x;
-      const bool has = p <= p1 && unit_of_pair(units, p, pl.pairs) < unit_of_pair(units, p + 1, pl.pairs);
+      const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
       const unsigned m = __ballot_sync(0xffffffffu, has);
       if (lane == 0) s_red[0][warp] = __uint_as_float(__popc(m));
       __syncthreads();
@@ -797,8 +849,8 @@ size_t latent_decode_workspace_bytes(int64_t batch, int64_t H, int64_t R, int64_
 }
 
 template <int R>
-static int launch_t(const CUtensorMap& map, const LatentDecode& a, const LatentPlan& pl,
-                    cudaStream_t stream) {
+static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const LatentDecode& a,
+                    const LatentPlan& pl, cudaStream_t stream) {
   if (smem_optin((const void*)latent_decode_kernel<R>, LdSmem<R>::TOTAL) != JF_OK) return JF_ERR_CUDA;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -810,7 +862,7 @@ static int launch_t(const CUtensorMap& map, const LatentDecode& a, const LatentP
   cfg.stream = stream;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, a, pl) != cudaSuccess) return JF_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
   const int64_t rows = (int64_t)a.batch * a.H;
   cfg.gridDim = dim3((unsigned)(rows < 16 * pl.pairs ? rows : 16 * pl.pairs));
   cfg.blockDim = dim3(LM_THREADS);
@@ -819,8 +871,9 @@ static int launch_t(const CUtensorMap& map, const LatentDecode& a, const LatentP
 }
 
 int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t stream) {
-  CUtensorMap map;
-  const int st = latent_tensor_map(a.pool, &map);
+  CUtensorMap map, qmap;
+  int st = bf16_rows_map(a.pool.base, a.pool.row, a.pool.num_pages * a.pool.P, 64, &map);
+  if (!st) st = bf16_rows_map(a.q, a.pool.row, (int64_t)a.batch * a.H, 64, &qmap);
   if (st) return st;
   LatentPlan pl;
   int64_t items, slot_rows, rows;
@@ -840,7 +893,8 @@ int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t st
   pl.ml = reinterpret_cast<float*>(ws);
   ws += round256(rows * 8);
   pl.o = reinterpret_cast<float*>(ws);
-  return a.pool.R == 512 ? launch_t<512>(map, a, pl, stream) : launch_t<256>(map, a, pl, stream);
+  return a.pool.R == 512 ? launch_t<512>(map, qmap, a, pl, stream)
+                         : launch_t<256>(map, qmap, a, pl, stream);
 }
 
 }  // namespace jfkv

@@ -137,6 +137,19 @@ def test_decode_of_many_requests():
         check(out[b], q[b], O.gather(pool, table[b], n), T.SCALE)
 
 
+@pytest.mark.parametrize("R", [256, 512])
+def test_decode_of_long_and_short_requests_in_turn(R):
+    """A pair of CTAs that takes the end of one request, others whole and a long run of the next."""
+    rng = np.random.default_rng(19)
+    ctx = [9000, 100, 0, 4097, 64, 7000, 1, 200, 6400, 8191, 130, 5000, 12, 3000, 9999, 128]
+    table, pool = T.filled(rng, R, 256, ctx)
+    q = T.queries(rng, len(ctx), 16, R)
+    out, st = run_decode(table, pool, ctx, q, T.SCALE)
+    assert st == 0
+    for b, n in enumerate(ctx):
+        check(out[b], q[b], O.gather(pool, table[b], n), T.SCALE)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.05, 1.0, 30.0])
 def test_decode_scales(scale):
     """Equal weights, a negative scale, and scores so large that one position takes all."""
@@ -253,6 +266,7 @@ def run_prefix(pool, ptable, plens, off, table, ctx, q, scale, ws=None):
     (512, 5, 256, [40], [700], list(range(40))),
     (256, 64, 64, [3, 1], [65, 4000], [64, 128, 0, 1]),
     (512, 20, 64, [7, 9], [3000, 129], [0] * 16),
+    (512, 16, 128, [30, 2, 9], [9000, 4000, 6001], [700 * (i % 3) + i for i in range(41)]),
 ], ids=str)
 def test_prefix_decode(R, H, P, sizes, plens, ctx):
     rng = np.random.default_rng(R + H + sum(plens) + sum(ctx))
