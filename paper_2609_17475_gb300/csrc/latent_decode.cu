@@ -710,30 +710,33 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 }
 
 // ---------------------------------------------------------------------------
-// Join the partials of each row that has any.  A CTA takes a row at a time: a thread
-// a partial for the weights, then 4 channels a thread, the partials in turn over
-// groups of R / 4 threads.
+// Join the partials of each row that has any.  A CTA takes CH channels of a row: first
+// its partials' places and, a thread each, their weights; then a thread 4 channels, the
+// partials in turn over the groups of CH / 4 threads, eight loads in flight.
 // ---------------------------------------------------------------------------
-constexpr int LM_THREADS = 256;
+constexpr int LM_THREADS = 256, LM_BATCH = 8;
 
-template <int R>
+template <int R, int CH>
 __global__ void __launch_bounds__(LM_THREADS)
 latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
-  constexpr int LANES = R / 4, GROUPS = LM_THREADS / LANES;
+  constexpr int LANES = CH / 4, GROUPS = LM_THREADS / LANES, WARPS = LM_THREADS / 32;
   __shared__ float s_w[LM_THREADS];
   __shared__ int32_t s_row[LM_THREADS];
-  __shared__ float s_red[2][LM_THREADS / 32];
+  __shared__ float s_red[2][WARPS];
+  __shared__ int32_t s_cnt[WARPS];
   __shared__ float4 s_o[LM_THREADS];
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
-  const PairRuns runs(pl.starts[pl.items], pl.pairs);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = (int)threadIdx.x % LANES, grp = (int)threadIdx.x / LANES;
   const int64_t total = (int64_t)a.batch * a.H;
-  for (int64_t row = blockIdx.x; row < total; row += gridDim.x) {
+  const PairRuns runs(pl.starts[pl.items], pl.pairs);
+  for (int64_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
+    const int64_t row = slice / (R / CH);
+    const int ch = (int)(slice % (R / CH)) * CH + c * 4;
     const int b = (int)(row / a.H), h = (int)(row - (int64_t)b * a.H);
     // the row's partials: those of the prefix's item, then its own's
     int count = 0;
     bool direct = false;
-    __syncthreads();
     for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
       int item, inside;
       if (part == 0) {
@@ -760,26 +763,31 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
       const int p = p0 + (int)threadIdx.x;
       const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
       const unsigned m = __ballot_sync(0xffffffffu, has);
-      if (lane == 0) s_red[0][warp] = __uint_as_float(__popc(m));
+      if (lane == 0) s_cnt[warp] = __popc(m);
       __syncthreads();
-      int at = count, all = 0;
-      for (int w = 0; w < LM_THREADS / 32; ++w) {
-        const int c = (int)__float_as_uint(s_red[0][w]);
-        if (w < warp) at += c;
-        all += c;
+      int at = count;
+      for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) at += s_cnt[w];
+        count += s_cnt[w];
       }
-      if (has) s_row[at + __popc(m & ((1u << lane) - 1))] = (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside;
-      count += all;
+      if (has)
+        s_row[at + __popc(m & ((1u << lane) - 1))] = (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside;
       __syncthreads();
     }
     if (direct) continue;   // uniform over the CTA
     __syncthreads();
-    // weights
+    // the first loads, under way while the weights are worked out
+    const float* const src = pl.o + ch;
+    float4 v[LM_BATCH];
+#pragma unroll
+    for (int k = 0; k < LM_BATCH; ++k)
+      if (grp + k * GROUPS < count)
+        v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[grp + k * GROUPS] * R);
     float m = -INFINITY, l = 0.f;
     if ((int)threadIdx.x < count) {
-      const float2 v = *reinterpret_cast<const float2*>(pl.ml + (int64_t)s_row[threadIdx.x] * 2);
-      m = v.x;
-      l = v.y;
+      const float2 x = *reinterpret_cast<const float2*>(pl.ml + (int64_t)s_row[threadIdx.x] * 2);
+      m = x.x;
+      l = x.y;
     }
     float M = m;
 #pragma unroll
@@ -787,7 +795,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     if (lane == 0) s_red[0][warp] = M;
     __syncthreads();
     M = s_red[0][0];
-    for (int w = 1; w < LM_THREADS / 32; ++w) M = fmaxf(M, s_red[0][w]);
+    for (int w = 1; w < WARPS; ++w) M = fmaxf(M, s_red[0][w]);
     // no maximum at all: sums of zero, or NaN where every score was
     const float f = M == -INFINITY ? 1.f : fast_exp2(m - M);
     float S = f * l;
@@ -797,30 +805,36 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     if (lane == 0) s_red[1][warp] = S;
     __syncthreads();
     S = 0.f;
-    for (int w = 0; w < LM_THREADS / 32; ++w) S += s_red[1][w];
-    const int c = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+    for (int w = 0; w < WARPS; ++w) S += s_red[1][w];
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int i = grp; i < count; i += GROUPS) {
-      const float4 v = *reinterpret_cast<const float4*>(pl.o + (int64_t)s_row[i] * R + c * 4);
-      const float w = s_w[i];
-      acc.x = fmaf(v.x, w, acc.x);
-      acc.y = fmaf(v.y, w, acc.y);
-      acc.z = fmaf(v.z, w, acc.z);
-      acc.w = fmaf(v.w, w, acc.w);
+    for (int i = grp; i < count; i += LM_BATCH * GROUPS) {
+#pragma unroll
+      for (int k = 0; k < LM_BATCH; ++k)
+        if (i + k * GROUPS < count) {
+          const float w = s_w[i + k * GROUPS];
+          acc.x = fmaf(v[k].x, w, acc.x);
+          acc.y = fmaf(v[k].y, w, acc.y);
+          acc.z = fmaf(v[k].z, w, acc.z);
+          acc.w = fmaf(v[k].w, w, acc.w);
+        }
+      const int next = i + LM_BATCH * GROUPS;
+#pragma unroll
+      for (int k = 0; k < LM_BATCH; ++k)
+        if (next + k * GROUPS < count)
+          v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[next + k * GROUPS] * R);
     }
     s_o[threadIdx.x] = acc;
     __syncthreads();
     if (grp == 0) {
       for (int g = 1; g < GROUPS; ++g) {
-        const float4 v = s_o[g * LANES + c];
-        acc.x += v.x;
-        acc.y += v.y;
-        acc.z += v.z;
-        acc.w += v.w;
+        const float4 x = s_o[g * LANES + c];
+        acc.x += x.x;
+        acc.y += x.y;
+        acc.z += x.z;
+        acc.w += x.w;
       }
       const float inv = S != 0.f ? 1.f / S : 0.f;
-      *reinterpret_cast<uint2*>(a.out + row * R + c * 4) =
+      *reinterpret_cast<uint2*>(a.out + row * R + ch) =
           make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
     __syncthreads();
@@ -863,11 +877,16 @@ static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const Laten
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
-  const int64_t rows = (int64_t)a.batch * a.H;
-  cfg.gridDim = dim3((unsigned)(rows < 16 * pl.pairs ? rows : 16 * pl.pairs));
+  // few rows: 128 channels a CTA, so that more of the GPU takes part
+  const int64_t rows = (int64_t)a.batch * a.H, most = 16 * pl.pairs;
+  const bool wide = rows >= 4 * pl.pairs;
+  const int64_t slices = wide ? rows : rows * (R / 128);
+  cfg.gridDim = dim3((unsigned)(slices < most ? slices : most));
   cfg.blockDim = dim3(LM_THREADS);
   cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, latent_merge_kernel<R>, a, pl) == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+  const cudaError_t e = wide ? cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R>, a, pl)
+                             : cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, 128>, a, pl);
+  return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 
 int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t stream) {
