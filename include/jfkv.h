@@ -642,6 +642,7 @@ int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_s
  * ====================================================================== */
 #define JF_LATENT_ROT        64    /* rotated key channels of a position      */
 #define JF_LATENT_MAX_GROUPS 64    /* groups of a jf_latent_prefix_decode_attn */
+#define JF_LATENT_MAX_POSITIONS 0x7FFFFF00   /* of a request: a tile's end fits 32 bits */
 
 /*
  * Append runs of rows: rows row_offsets[b] .. row_offsets[b + 1] - 1 go to
@@ -689,7 +690,8 @@ size_t jf_latent_workspace_bytes(int32_t batch, int32_t num_heads, int32_t laten
  *   workspace     >= jf_latent_workspace_bytes(batch, num_heads, R, 0, 0) bytes,
  *                 256-byte aligned, its first 256 bytes zero before the first
  *                 call; its first int32 is the device status word
- * A context length outside [0, pt_stride * P] sets JF_DEV_ERR_POSITION and counts
+ * A context length outside [0, pt_stride * P], or past JF_LATENT_MAX_POSITIONS, sets
+ * JF_DEV_ERR_POSITION and counts
  * as 0; positions of a page outside the pool draw no weight
  * (JF_DEV_ERR_PAGE_ID).  Several tokens of one request (a draft's, say) go in as
  * requests with the same page-table row and a context length each.
@@ -746,7 +748,8 @@ size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int
  *   workspace       >= jf_latent_prefill_workspace_bytes(q_start, chunk_len,
  *                   num_heads, 0) bytes, 256-byte aligned; its first int32 is the
  *                   device status word, zero before the first call
- * All 16-byte aligned; num_heads <= 1024; q_start + chunk_len < 2^31.
+ * All 16-byte aligned; num_heads <= 1024; q_start + chunk_len <=
+ * JF_LATENT_MAX_POSITIONS.
  * A page outside the pool sets JF_DEV_ERR_PAGE_ID; the outputs that attend its
  * positions are not reliable.  A value that is not finite reaches the queries that
  * see its position, and no other.

@@ -23,7 +23,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libjfkv.so")
 CALL = os.path.join(HERE, "_jfcall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 SOURCES = ["api.cu", "append.cu", "checkpoint.cu", "decode.cu", "kv8.cu", "kv8_decode.cu",
-           "kv8_evict.cu", "kv8_prefill.cu", "latent.cu", "latent_decode.cu", "prefill.cu", "rope.cu", "selftest.cu", "tq4.cu",
+           "kv8_evict.cu", "kv8_prefill.cu", "latent.cu", "latent_decode.cu", "latent_prefill.cu",
+           "prefill.cu", "rope.cu", "selftest.cu", "tq4.cu",
            "tq4_verify.cu", "verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

@@ -210,6 +210,21 @@ int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
+// 3-D map over queries [C, H, 192], box = 64 channels of 128 queries of a head, 128B swizzle.
+int latent_query_map(const void* q, int64_t H, int64_t C, CUtensorMap* map) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return JF_ERR_CUDA;
+  const cuuint64_t row = 128 + JF_LATENT_ROT;
+  cuuint64_t dims[3] = {row, (cuuint64_t)H, (cuuint64_t)C};
+  cuuint64_t strides[2] = {row * 2, row * 2 * (cuuint64_t)H};
+  cuuint32_t box[3] = {64, 1, 128};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box,
+                   estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
+}
+
 }  // namespace jfkv
 
 extern "C" {
@@ -863,7 +878,7 @@ int jf_latent_prefix_decode_attn(const jf_kv_pool* pool, const int32_t* prefix_t
 size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int32_t num_heads,
                                          int32_t num_sms) {
   if (q_start < 0 || chunk_len < 0 || num_heads < 1 || num_heads > 1024 || num_sms < 0) return 0;
-  if ((int64_t)q_start + chunk_len > 0x7FFFFFFF) return 0;
+  if ((int64_t)q_start + chunk_len > JF_LATENT_MAX_POSITIONS) return 0;
   return latent_prefill_workspace_bytes(q_start, chunk_len, num_heads,
                                         num_sms ? num_sms : sm_count());
 }
@@ -876,7 +891,7 @@ int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row
   if (st) return st;
   if (q_start < 0 || chunk_len < 0 || num_heads < 1) return JF_ERR_INVALID_ARG;
   if (num_heads > 1024) return JF_ERR_UNSUPPORTED;
-  if ((int64_t)q_start + chunk_len > 0x7FFFFFFF) return JF_ERR_INVALID_ARG;
+  if ((int64_t)q_start + chunk_len > JF_LATENT_MAX_POSITIONS) return JF_ERR_INVALID_ARG;
   if (!(softmax_scale == softmax_scale)) return JF_ERR_INVALID_ARG;
   if (chunk_len == 0) return JF_OK;
   if (!page_table_row || !q || !w_k || !w_v || !out || !workspace) return JF_ERR_INVALID_ARG;

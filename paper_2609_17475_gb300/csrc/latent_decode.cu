@@ -28,13 +28,9 @@
 //   warp 12    Q by TMA, as soon as the last products with the segment's before are done
 #include <cmath>
 
-#include "latent.cuh"
-#include "prefill.cuh"
+#include "latent_tc.cuh"
 
 namespace jfkv {
-
-int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows, CUtensorMap* map);
-int sm_count();
 
 constexpr int LD_T = 128;           // positions a tile
 constexpr int LD_ROWS = 128;        // rows a pair, 64 each CTA
@@ -76,54 +72,6 @@ struct LdSmem {
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
-__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn) {
-  return tc::idesc_f16_f32(M, N, 0, b_mn) | (1u << 7) | (1u << 10);
-}
-
-// Pair MMA, both operands in shared memory, issued where `leader` is set by a warp that runs the
-// issuing code as a whole: control flow and operands are then uniform values.  (Run by one thread
-// alone, each descriptor was moved to uniform registers first: 72 to 100 cycles an instruction for
-// the 32 to 64 that the product takes.)
-__device__ __forceinline__ void mma2_ss_if(uint32_t leader, uint32_t d, uint64_t a, uint64_t b,
-                                           uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
-      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
-      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
-
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t p;
-  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
-               : "=r"(p));
-  return p;
-}
-
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y,
-                                            uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3}], [%4];\n"
-      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
-  return v;
-}
-__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n"
-               ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-
 // ---- items ------------------------------------------------------------------------
 struct LatentItem {
   const int32_t* pt;
@@ -141,7 +89,7 @@ __device__ __forceinline__ int item_group(const LatentPlan& pl, int i) {
 __device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan& pl, int i, int g) {
   const int n = g >= 0 ? a.prefix_lens[g] : a.context_lens[(i - pl.prefix_items) / pl.blocks];
   const int stride = g >= 0 ? a.prefix_stride : a.pt_stride;
-  return n < 0 || n > (int64_t)stride * a.pool.P ? -1 : n;
+  return n < 0 || n > (int64_t)stride * a.pool.P || n > JF_LATENT_MAX_POSITIONS ? -1 : n;
 }
 
 __device__ __forceinline__ int tiles_of(int len) { return len <= 0 ? 0 : (len + LD_T - 1) / LD_T; }
@@ -199,40 +147,6 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
     }
   }
   return false;
-}
-
-// first unit of pair p's run
-__device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
-  return (x | y) >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y);
-}
-struct PairRuns {   // floor(units * p / pairs), by one division
-  int64_t units, each;
-  uint32_t rest, pairs;
-  __device__ __forceinline__ PairRuns(int64_t u, int n) : units(u), pairs((uint32_t)n) {
-    each = (int64_t)divide((uint64_t)u, pairs);
-    rest = (uint32_t)(u - each * n);
-  }
-  __device__ __forceinline__ int64_t first(int p) const {
-    return each * p + (uint32_t)p * rest / pairs;
-  }
-  // the pair that has unit u: the last p with first(p) <= u
-  __device__ __forceinline__ int of(int64_t u) const {
-    return (int)divide((uint64_t)(u + 1) * pairs + (uint64_t)units - 1, (uint64_t)units) - 1;
-  }
-};
-
-// the page of the 64 positions from pos, as a row of the pool; past the map's end (the copy then
-// brings zeros) where there is none
-__device__ __forceinline__ int half_row(const LatentPool& p, const int32_t* pt, int pos, int len,
-                                        int32_t* status) {
-  const int end = (int)(p.num_pages << p.log2P);
-  if (pos >= len) return end;
-  const int32_t page = __ldg(pt + (pos >> p.log2P));
-  if (page < 0 || page >= p.num_pages) {
-    if (status) flag_error(status, JF_DEV_ERR_PAGE_ID);
-    return end;
-  }
-  return (page << p.log2P) + (pos & (p.P - 1));
 }
 
 template <int R>
@@ -556,11 +470,13 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     int t = 0;
     Seg nx;
     bool more = next_seg(a, pl, run, sg);
-    while (more && ok) {
+    // A wait that gave up ends the work but not the meetings: the warps of a row would wait for one
+    // another for ever.
+    while (more) {
       float m = -INFINITY, l = 0.f;
       int live = live_of(sg, sg.j0);
       for (int j = sg.j0; j < sg.j1; ++j, ++t) {
-        if (!mbar_wait_bounded(&s_full[t % LD_SBUF], (t / LD_SBUF) & 1)) { ok = false; break; }
+        if (ok) ok = mbar_wait_bounded(&s_full[t % LD_SBUF], (t / LD_SBUF) & 1);
         tc::fence_after();
         uint32_t s[32];
         tc::ld32(tS + (t % LD_SBUF) * 64 + side * 32 + lane_off, s);
@@ -601,7 +517,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
           sum = add_f32x2(sum, f32x2(bf16lo_to_f32(p[c]), bf16hi_to_f32(p[c])));
         }
         if (j > sg.j0) {   // P is free, and O complete up to the last tile
-          if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
+          if (ok) ok = mbar_wait_bounded(pv_done, (t - 1) & 1);
           if (__any_sync(0xffffffffu, up)) {
             tc::fence_after();
             const float f = up && m != -INFINITY ? fast_exp2(m - m_new) : 1.f;
@@ -625,15 +541,14 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         fence_proxy_async_smem();
         tc::fence_before();
         __syncwarp();
-        if (lane == 0) tc::arrive_cluster(p_ready, 0);
+        if (lane == 0 && ok) tc::arrive_cluster(p_ready, 0);
         m = m_new;
         float u, v;
         unpack_f32x2(sum, u, v);
         l += u + v;
       }
-      if (!ok) break;
       more = next_seg(a, pl, run, nx);
-      if (!mbar_wait_bounded(pv_done, (t - 1) & 1)) { ok = false; break; }
+      if (ok) ok = mbar_wait_bounded(pv_done, (t - 1) & 1);
       tc::fence_after();
       float* const sx = s_x + (t & 1) * 256;
       sx[tid] = l;
@@ -646,7 +561,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                       (sg.item < pl.prefix_items ? 0 : (int64_t)a.batch * a.H) + sg.it.row0
                 : (int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * pl.slot_rows;
       const int64_t crow = (direct ? (int64_t)sg.it.row0 : prow) + 64 * rank;   // this CTA's first row
-      const int rows = sg.it.nrows - 64 * (int)rank;
+      const int rows = __all_sync(0xffffffffu, ok) ? sg.it.nrows - 64 * (int)rank : 0;
       if (!direct && half == 0 && side == 0 && r < rows)
         *reinterpret_cast<float2*>(pl.ml + (crow + r) * 2) = make_float2(m, l);
       const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -844,8 +759,6 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
 // ---------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------
-static int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
-
 // items, and the partials' rows
 static void plan_sizes(int64_t batch, int64_t H, int64_t groups, int64_t sms, int64_t* items,
                        int64_t* slot_rows, int64_t* rows) {

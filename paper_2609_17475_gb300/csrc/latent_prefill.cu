@@ -1,0 +1,921 @@
+// Prefill-chunk attention over the latent cache in the expanded form, on the
+// 5th-generation tensor cores: the heads' keys and values are worked out from the
+// latents once (latent_expand_kernel), then attention runs over them
+// (latent_prefill_kernel), as many heads at a time as the workspace holds.
+//
+// Expansion: [positions, R] times [R, 128 + 128] of a head, M = 256 positions and N =
+// 256 channels a CTA pair, CTA 0 supplying the key's weights and CTA 1 the value's;
+// the products of a tile run while the tile before goes out.  Positions past the last
+// are written as zeros, so that a weight of zero finds no NaN there.  A value of the
+// chunk's own positions that is not finite would reach queries before it the same way
+// (0 * NaN): it is written as zero and its position noted for its channel, and the
+// queries that see it get NaN at the end.
+//
+// Attention: 256 queries of a head a CTA pair (M = 256, 128 rows each), tiles of 128
+// positions of which each CTA supplies 64 keys (128 expanded channels, and the 64
+// rotated ones straight from the pool) and 64 of the values' channels.  S is taken
+// into three buffers of tensor memory, two tiles ahead of P V; P (bf16) replaces S; O
+// stays in tensor memory.  Two groups of four softmax warps take the even and the odd
+// tiles, a row a thread.  Weights are 2^(s - m) with a reference m that is 0 unless
+// scores leave [-60, 60] (in powers of two): bf16 and fp32 hold such weights as well as
+// any.  Where a row's reference moves, the tile's weights are worked out again and O is
+// scaled.
+//
+// Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
+// cut into one run of equal length per pair; a cut item's parts are joined by
+// latent_prefill_merge_kernel.
+#include <cmath>
+
+#include "latent_tc.cuh"
+
+namespace jfkv {
+
+constexpr int LP_T = 128;            // positions a tile
+constexpr int LP_Q = 256;            // queries a pair
+constexpr int LP_HDR = 2;            // an item's fixed cost, in tiles
+constexpr float LP_TOP = 60.f;       // how far scores may be from the reference (log2)
+constexpr int LP_BAD = 132;          // first positions of values that are not finite: [128], their least
+
+struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
+  LatentPool pool;
+  const int32_t* pt;
+  uint16_t* k;                       // [heads][n_pad][128]
+  uint16_t* v;
+  uint16_t* out;                     // [C][H][128]
+  int32_t* bad;                      // [heads][LP_BAD]
+  int32_t* status;
+  float* ml;                         // [2 * pairs * 256][2]
+  float* o;                          // [2 * pairs * 256][128]
+  int64_t units, units_head;         // of the pass, of a head
+  int32_t n, n_pad, q_start, C, H, h0, heads, causal;
+  int32_t q_tiles, pairs;
+  float scale_log2;
+};
+
+// ===========================================================================
+// Expansion
+// ===========================================================================
+constexpr int LE_STAGES = 5;
+constexpr int LE_THREADS = 32 * 12;
+struct LeSmem {
+  static constexpr int A_BYTES = 128 * 128, B_BYTES = 128 * 128;   // 64 channels of 128 rows
+  static constexpr int STAGE = A_BYTES + B_BYTES;
+  static constexpr int OFF_OUT = LE_STAGES * STAGE;                // 8 warps x [32 rows][128 B]
+  static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
+  static constexpr int TOTAL = OFF_BAR + 256;
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LE_THREADS, 1)
+latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap kmap,
+                     const __grid_constant__ CUtensorMap vmap, const __grid_constant__ LatentChunk a) {
+  using L = LeSmem;
+  constexpr uint32_t ID = idesc_bf16(256, 256, 0);
+  extern __shared__ __align__(1024) uint8_t sm[];
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
+  uint64_t* const full = bars + 0;      // [5] on CTA 0: both CTAs' operands
+  uint64_t* const land = bars + 5;      // [5] CTA 1's
+  uint64_t* const free_ = bars + 10;    // [5] stage read
+  uint64_t* const d_full = bars + 15;   // [2] a tile's products done
+  uint64_t* const d_free = bars + 17;   // [2] on CTA 0: and gone out, in both CTAs
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  const int pair = (int)(blockIdx.x >> 1);
+  if (smem_u32(sm) & 1023u) {   // the same in both CTAs
+    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&pmap);
+    prefetch_tensormap(rank ? &vmap : &kmap);
+    for (int i = 0; i < LE_STAGES; ++i) {
+      mbar_init(&full[i], 2);
+      mbar_init(&land[i], 1);
+      mbar_init(&free_[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&d_full[i], 1);
+      mbar_init(&d_free[i], 16);
+    }
+    fence_barrier_init();
+  }
+  if (warp == 0) tc::alloc2(tmem_slot, 512);
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+  tc::fence_after();
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+
+  const int tiles = (a.n_pad / 256) * a.heads;   // heads within 256 positions
+  const int steps = a.pool.R / 64;
+  bool ok = true;
+  if (warp == 0) {
+    int st = 0, ph = 0;   // stage and how often the ring went round
+    if (rank == 0) {
+      const uint32_t leader = elect_one();
+      const uint64_t ad = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
+      auto wait = [&](uint64_t* bar, int phase) {
+        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
+      };
+      int t = 0;
+      for (int i = pair; i < tiles && ok; i += a.pairs, ++t) {
+        if (t >= 2) ok = wait(&d_free[t & 1], (t >> 1) - 1);
+        tc::fence_after();
+        const uint32_t d = (t & 1) * 256;
+        for (int s = 0; s < steps && ok; ++s) {
+          ok = wait(&full[st], ph);
+          tc::fence_after();
+          const uint64_t at = ad + (uint64_t)(st * (L::STAGE >> 4));
+          if (ok) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              mma2_ss_if(leader, d, at + ((k * 32) >> 4), at + ((L::A_BYTES + k * 32) >> 4), ID,
+                         (s > 0 || k > 0) ? 1u : 0u);
+            tc::commit2_both_if(leader, &free_[st]);
+          }
+          if (++st == LE_STAGES) {
+            st = 0;
+            ++ph;
+          }
+        }
+        if (ok) tc::commit2_both_if(leader, &d_full[t & 1]);
+      }
+    } else if (lane == 0) {
+      for (int i = pair; i < tiles && ok; i += a.pairs)
+        for (int s = 0; s < steps && ok; ++s) {
+          ok = mbar_wait_bounded(&land[st], ph & 1);
+          if (ok) tc::arrive_cluster(&full[st], 0);
+          if (++st == LE_STAGES) {
+            st = 0;
+            ++ph;
+          }
+        }
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int st = 0, ph = 0;
+      for (int i = pair; i < tiles && ok; i += a.pairs) {
+        const int pos = (i / a.heads) * 256 + 128 * (int)rank, h = a.h0 + i % a.heads;
+        const int row0 = half_row(a.pool, a.pt, pos, a.n, a.status);
+        const int row1 = half_row(a.pool, a.pt, pos + 64, a.n, a.status);
+        for (int s = 0; s < steps; ++s) {
+          if (ph > 0 && !mbar_wait_bounded(&free_[st], (ph - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          uint64_t* const bar = rank == 0 ? &full[st] : &land[st];
+          mbar_arrive_expect_tx(bar, L::STAGE);
+          const uint32_t dst = smem_u32(sm) + st * L::STAGE;
+          tma_load_2d(dst, &pmap, s * 64, row0, bar);
+          tma_load_2d(dst + 8192, &pmap, s * 64, row1, bar);
+          tma_load_2d(dst + L::A_BYTES, rank ? &vmap : &kmap, s * 64, h * 128, bar);
+          if (++st == LE_STAGES) {
+            st = 0;
+            ++ph;
+          }
+        }
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ---- out: warps 4-7 the keys' 128 columns, 8-11 the values' -----------------------
+    const int quarter = warp & 3, kind = warp >= 8 ? 1 : 0;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
+    uint16_t* const dst = kind ? a.v : a.k;
+    // values of positions that not every query of the chunk sees
+    const int apart = kind && a.causal ? a.q_start + 1 : 0x7FFFFFFF;
+    int t = 0;
+    for (int i = pair; i < tiles; i += a.pairs, ++t) {
+      const int hl = i % a.heads;
+      const int pos0 = (i / a.heads) * 256 + 128 * (int)rank + quarter * 32;
+      const int pos = pos0 + lane;
+      if (!mbar_wait_bounded(&d_full[t & 1], (t >> 1) & 1)) {
+        ok = false;
+        break;
+      }
+      tc::fence_after();
+#pragma unroll 1
+      for (int c0 = 0; c0 < 128; c0 += 64) {
+        uint32_t x[2][32];
+        tc::ld32((t & 1) * 256 + kind * 128 + c0 + lane_off, x[0]);
+        tc::ld32((t & 1) * 256 + kind * 128 + c0 + 32 + lane_off, x[1]);
+        tc::wait_ld();
+        if (c0 == 64) {   // the tile's columns have been read
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) tc::arrive_cluster(&d_free[t & 1], 0);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int c = 8 * k + 2 * u;
+            w[u] = pack_bf16x2(__uint_as_float(x[c >> 5][c & 31]), __uint_as_float(x[c >> 5][(c + 1) & 31]));
+            if (pos >= a.n) w[u] = 0u;
+            if (pos >= apart) {
+              const bool lo = (w[u] & 0x7F80u) == 0x7F80u, hi = (w[u] & 0x7F800000u) == 0x7F800000u;
+              if (lo || hi) {
+                int32_t* const bad = a.bad + hl * LP_BAD;
+                if (lo) atomicMin(bad + c0 + c, pos);
+                if (hi) atomicMin(bad + c0 + c + 1, pos);
+                atomicMin(bad + 128, pos);
+                w[u] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0xFFFFu : 0xFFFFFFFFu);
+              }
+            }
+          }
+          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+        uint16_t* const to = dst + ((int64_t)hl * a.n_pad + pos0) * 128 + c0;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int row = u * 4 + (lane >> 3), piece = lane & 7;
+          *reinterpret_cast<uint4*>(to + row * 128 + piece * 8) =
+              lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
+        }
+        __syncwarp();
+      }
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+  }
+  // neither CTA may release TMEM or exit while its partner can still reach it
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  if (warp == 0) {
+    tc::fence_after();
+    tc::dealloc2(*tmem_slot, 512);
+  }
+}
+
+// ===========================================================================
+// Attention
+// ===========================================================================
+constexpr int LA_THREADS = 32 * 12;
+constexpr int LA_KS = 3, LA_VS = 4, LA_SB = 3, LA_AHEAD = 2;
+struct LaSmem {
+  static constexpr int Q_BYTES = 3 * 128 * 128;         // [64-channel chunk][128 rows][128 B]
+  static constexpr int K_BYTES = 3 * 64 * 128;          // [64-channel chunk][64 positions][128 B]
+  static constexpr int V_BYTES = 128 * 128;             // 64 channels of 128 positions
+  static constexpr int OFF_K = Q_BYTES;
+  static constexpr int OFF_V = OFF_K + LA_KS * K_BYTES;
+  static constexpr int OFF_OUT = OFF_V + LA_VS * V_BYTES;   // 8 warps x [32 rows][128 B]
+  static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
+  static constexpr int OFF_M = OFF_BAR + 512;           // [128] references
+  static constexpr int OFF_L = OFF_M + 128 * 4;         // [2 groups][128] (m, l)
+  static constexpr int TOTAL = OFF_L + 2 * 128 * 8;
+  static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
+};
+
+// tiles and first unit (of its head) of query tile qt
+__device__ __forceinline__ int chunk_tiles(const LatentChunk& a, int qt) {
+  if (!a.causal) return (a.n + LP_T - 1) / LP_T;
+  const int64_t seen = (int64_t)a.q_start + (int64_t)(qt + 1) * LP_Q;
+  return (int)(((seen < a.n ? seen : a.n) + LP_T - 1) / LP_T);
+}
+__device__ __forceinline__ int64_t chunk_start(const LatentChunk& a, int qt) {
+  const int64_t q = qt;
+  if (!a.causal) return q * ((a.n + LP_T - 1) / LP_T + LP_HDR);
+  // tiles before the last query tile: 2 (qt + 1) + ceil(q_start / 128)
+  return q * (q - 1) + q * (2 + (a.q_start + LP_T - 1) / LP_T + LP_HDR);
+}
+
+struct ChunkSeg {
+  int hl, qt, j0, j1, n;
+};
+struct ChunkIter {
+  int64_t start, u0, u1;   // first unit of item (hl, qt); the pair's run
+  int hl, qt;
+};
+
+__device__ __forceinline__ ChunkIter chunk_run(const LatentChunk& a, int pair) {
+  const PairRuns runs(a.units, a.pairs);
+  ChunkIter s;
+  s.u0 = runs.first(pair);
+  s.u1 = runs.first(pair + 1);
+  s.hl = (int)divide((uint64_t)s.u0, (uint64_t)a.units_head);
+  const int64_t in = s.u0 - s.hl * a.units_head;
+  int lo = 0, hi = a.q_tiles - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (chunk_start(a, mid) <= in) lo = mid; else hi = mid - 1;
+  }
+  s.qt = lo;
+  s.start = s.hl * a.units_head + chunk_start(a, lo);
+  return s;
+}
+__device__ __forceinline__ bool next_chunk_seg(const LatentChunk& a, ChunkIter& s, ChunkSeg& g) {
+  while (s.start < s.u1 && s.hl < a.heads) {
+    const int n = chunk_tiles(a, s.qt);
+    const int64_t first = s.start + LP_HDR;
+    const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
+    g.hl = s.hl;
+    g.qt = s.qt;
+    g.n = n;
+    s.start += n + LP_HDR;
+    if (++s.qt == a.q_tiles) {
+      s.qt = 0;
+      ++s.hl;
+    }
+    if (lo < hi) {
+      g.j0 = (int)lo;
+      g.j1 = (int)hi;
+      return true;
+    }
+  }
+  return false;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];\n"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LA_THREADS, 1)
+latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap pmap,
+                      const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                      const __grid_constant__ LatentChunk a) {
+  using L = LaSmem;
+  constexpr uint32_t IDQK = idesc_bf16(256, LP_T, 0);
+  constexpr uint32_t IDPV = idesc_bf16(256, 128, 1);
+  extern __shared__ __align__(1024) uint8_t sm[];
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
+  // on CTA 0, where the pair's MMAs are issued:
+  uint64_t* const k_full = bars + 0;     // [3] both CTAs' K of a tile
+  uint64_t* const v_full = bars + 3;     // [4] both CTAs' V
+  uint64_t* const q_full = bars + 7;     // both CTAs' Q of a segment
+  uint64_t* const p_ready = bars + 8;    // [4] both CTAs' P of tile t % 4
+  // on each CTA:
+  uint64_t* const k_land = bars + 12;    // [3] CTA 1: its operands have landed
+  uint64_t* const v_land = bars + 15;    // [4]
+  uint64_t* const q_land = bars + 19;
+  uint64_t* const k_free = bars + 20;    // [3] stage read
+  uint64_t* const v_free = bars + 23;    // [4]
+  uint64_t* const q_free = bars + 27;    // products with a segment's Q done
+  uint64_t* const s_full = bars + 28;    // [3] S of tile t % 3
+  uint64_t* const pv_done = bars + 31;   // [4] P V of tile t % 4
+  uint64_t* const m_bar = bars + 35;     // [2 groups][4 quarters] the group's reference is set
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 43);
+  float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
+  float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = tc::cluster_rank();
+  const int pair = (int)(blockIdx.x >> 1);
+  if (smem_u32(sm) & 1023u) {   // the same in both CTAs
+    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    prefetch_tensormap(&qmap);
+    prefetch_tensormap(&pmap);
+    prefetch_tensormap(&kmap);
+    prefetch_tensormap(&vmap);
+    for (int i = 0; i < LA_KS; ++i) {
+      mbar_init(&k_full[i], 2);
+      mbar_init(&k_land[i], 1);
+      mbar_init(&k_free[i], 1);
+    }
+    for (int i = 0; i < LA_VS; ++i) {
+      mbar_init(&v_full[i], 2);
+      mbar_init(&v_land[i], 1);
+      mbar_init(&v_free[i], 1);
+    }
+    for (int i = 0; i < LA_SB; ++i) mbar_init(&s_full[i], 1);
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&p_ready[i], 8);
+      mbar_init(&pv_done[i], 1);
+      mbar_init(&m_bar[i], 1);
+      mbar_init(&m_bar[4 + i], 1);
+    }
+    mbar_init(q_full, 2);
+    mbar_init(q_land, 1);
+    mbar_init(q_free, 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) tc::alloc2(tmem_slot, 512);
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+  tc::fence_after();
+  ChunkIter run = chunk_run(a, pair);
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the keys and values have been written
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  // all 512 columns are this CTA's: O from 0, the S buffers behind it
+  constexpr uint32_t tO = 0, tS = 128;
+
+  bool ok = true;
+  ChunkSeg sg;
+  if (warp == 0) {
+    if (rank == 0) {
+      // ================= MMA issuer (the whole warp: control flow stays uniform) ==========
+      const uint32_t leader = elect_one();
+      const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
+      const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
+      const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 16, 1024);
+      auto wait = [&](uint64_t* bar, int phase) {
+        return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
+      };
+      int t = 0, nseg = 0;   // tiles and segments so far
+      while (__all_sync(0xffffffffu, ok && next_chunk_seg(a, run, sg))) {
+        ok = wait(q_full, nseg);
+        ++nseg;
+        const int nt = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
+        for (int i = 0; i < nt + LA_AHEAD && ok; ++i) {
+          if (i < nt) {
+            const int T = t + i, st = T % LA_KS;
+            ok = wait(&k_full[st], T / LA_KS);
+            tc::fence_after();
+            const uint64_t k0 = kd + (uint64_t)(st * (L::K_BYTES >> 4));
+            const uint32_t d = tS + (T % LA_SB) * 128;
+            if (ok) {
+#pragma unroll
+              for (int k = 0; k < 12; ++k)
+                mma2_ss_if(leader, d, qd + (((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4),
+                           k0 + (((k >> 2) * 64 * 128 + (k & 3) * 32) >> 4), IDQK, k > 0 ? 1u : 0u);
+              tc::commit2_both_if(leader, &k_free[st]);
+              tc::commit2_both_if(leader, &s_full[T % LA_SB]);
+              if (i == nt - 1) tc::commit2_both_if(leader, q_free);
+            }
+          }
+          const int j = i - LA_AHEAD;   // the segment's tile whose P V is due
+          if (j >= 0 && ok) {
+            const int T = t + j, st = T % LA_VS;
+            ok = wait(&p_ready[T & 3], T >> 2) && wait(&v_full[st], T / LA_VS);
+            tc::fence_after();
+            const uint64_t v0 = vd + (uint64_t)(st * (L::V_BYTES >> 4));
+            const uint32_t p = tS + (T % LA_SB) * 128;
+            if (ok) {
+#pragma unroll
+              for (int k = 0; k < LP_T / 16; ++k)
+                tc::mma2_ts_if(leader, tO, p + 8 * k, v0 + ((k * 2048) >> 4), IDPV,
+                               (j > 0 || k > 0) ? 1u : 0u);
+              tc::commit2_both_if(leader, &v_free[st]);
+              tc::commit2_both_if(leader, &pv_done[T & 3]);
+            }
+          }
+        }
+        t += nt;
+      }
+    } else if (lane == 0) {
+      // ================= CTA 1's arrivals, in the order the issuer takes them =================
+      int t = 0, nseg = 0;
+      while (ok && next_chunk_seg(a, run, sg)) {
+        ok = mbar_wait_bounded(q_land, nseg & 1);
+        if (ok) tc::arrive_cluster(q_full, 0);
+        ++nseg;
+        const int nt = sg.j1 - sg.j0;
+        for (int i = 0; i < nt + LA_AHEAD && ok; ++i) {
+          if (i < nt) {
+            const int T = t + i;
+            ok = mbar_wait_bounded(&k_land[T % LA_KS], (T / LA_KS) & 1);
+            if (ok) tc::arrive_cluster(&k_full[T % LA_KS], 0);
+          }
+          if (i >= LA_AHEAD && ok) {
+            const int T = t + i - LA_AHEAD;
+            ok = mbar_wait_bounded(&v_land[T % LA_VS], (T / LA_VS) & 1);
+            if (ok) tc::arrive_cluster(&v_full[T % LA_VS], 0);
+          }
+        }
+        t += nt;
+      }
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    __syncwarp();
+  } else if (warp == 1) {
+    // ================= K: this CTA's 64 positions of each tile =================
+    if (lane == 0) {
+      int t = 0;
+      while (ok && next_chunk_seg(a, run, sg)) {
+        int y = half_row(a.pool, a.pt, sg.j0 * LP_T + 64 * (int)rank, a.n, a.status);
+        for (int j = sg.j0; j < sg.j1; ++j, ++t) {
+          const int row = y, st = t % LA_KS, pos = j * LP_T + 64 * (int)rank;
+          if (j + 1 < sg.j1) y = half_row(a.pool, a.pt, pos + LP_T, a.n, a.status);
+          if (t >= LA_KS && !mbar_wait_bounded(&k_free[st], (t / LA_KS - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          uint64_t* const land = rank == 0 ? &k_full[st] : &k_land[st];
+          mbar_arrive_expect_tx(land, L::K_BYTES);
+          const uint32_t dst = smem_u32(sm + L::OFF_K + st * L::K_BYTES);
+          const int at = sg.hl * a.n_pad + pos;
+          tma_load_2d(dst, &kmap, 0, at, land);
+          tma_load_2d(dst + 8192, &kmap, 64, at, land);
+          tma_load_2d(dst + 16384, &pmap, a.pool.R, row, land);
+        }
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ================= V: this CTA's 64 channels of all 128 positions =================
+    if (lane == 0) {
+      int t = 0;
+      while (ok && next_chunk_seg(a, run, sg))
+        for (int j = sg.j0; j < sg.j1; ++j, ++t) {
+          const int st = t % LA_VS;
+          if (t >= LA_VS && !mbar_wait_bounded(&v_free[st], (t / LA_VS - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          uint64_t* const land = rank == 0 ? &v_full[st] : &v_land[st];
+          mbar_arrive_expect_tx(land, L::V_BYTES);
+          tma_load_2d(smem_u32(sm + L::OFF_V + st * L::V_BYTES), &vmap, 64 * (int)rank,
+                      sg.hl * a.n_pad + j * LP_T, land);
+        }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp == 3) {
+    // ================= Q: 128 rows; zeros past the chunk's end =================
+    if (lane == 0) {
+      int nseg = 0;
+      while (ok && next_chunk_seg(a, run, sg)) {
+        if (nseg > 0 && !mbar_wait_bounded(q_free, (nseg - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        ++nseg;
+        uint64_t* const land = rank == 0 ? q_full : q_land;
+        mbar_arrive_expect_tx(land, L::Q_BYTES);
+        for (int c = 0; c < 3; ++c)
+          tma_load_3d(smem_u32(sm) + c * 128 * 128, &qmap, c * 64, a.h0 + sg.hl,
+                      sg.qt * LP_Q + 128 * (int)rank, land);
+      }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else {
+    // ================= softmax: group 0 the even tiles, group 1 the odd; O out =================
+    const int quarter = warp & 3, group = warp >= 8 ? 1 : 0;
+    const int r = quarter * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+    const float sc = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
+    const uint64_t kk = f32x2(sc, sc);
+    auto all_sync = [] { asm volatile("bar.sync 1, 256;\n" ::: "memory"); };
+    int t0 = 0;   // tiles of the segments before
+    // a wait that gave up ends the work but not the meetings: the others would wait for ever
+    while (next_chunk_seg(a, run, sg)) {
+      const int q = sg.qt * LP_Q + 128 * (int)rank + r;
+      const int limit = a.causal ? min(a.q_start + q, a.n - 1) : a.n - 1;   // last position seen
+      const int nt = sg.j1 - sg.j0;
+      float m_own = -INFINITY, l = 0.f;   // the reference at this group's last tile
+      for (int i = (t0 + group) & 1; i < nt && ok; i += 2) {
+        const int T = t0 + i, key0 = (sg.j0 + i) * LP_T;
+        const uint32_t tb = tS + (T % LA_SB) * 128 + lane_off;
+        ok = __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[T % LA_SB], (T / LA_SB) & 1)) != 0;
+        if (!ok) break;
+        tc::fence_after();
+        uint32_t p[64];
+        float m_use = m_own, m_new = m_own, l_new = 0.f;
+        bool agreed = false;
+#pragma unroll 1
+        for (;;) {
+          const float mm = m_use == -INFINITY ? 0.f : m_use;   // -inf: nothing seen so far
+          const uint64_t cc = f32x2(-mm, -mm);
+          float x[2] = {-INFINITY, -INFINITY};
+          uint64_t sum = f32x2(0.f, 0.f);
+#pragma unroll
+          for (int h = 0; h < 4; ++h) {
+            uint32_t s[32];
+            tc::ld32(tb + 32 * h, s);
+            tc::wait_ld();
+            if (!(a.scale_log2 > 0.f)) {   // a scale below zero negates S, one of zero makes it zero or NaN
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                s[c] = a.scale_log2 < 0.f ? s[c] ^ 0x80000000u : __float_as_uint(__uint_as_float(s[c]) * 0.f);
+            }
+            if (key0 + 32 * h + 31 > limit) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (key0 + 32 * h + c > limit) s[c] = 0xFF800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const float a0 = __uint_as_float(s[2 * c]), a1 = __uint_as_float(s[2 * c + 1]);
+              x[c & 1] = max3(x[c & 1], a0, a1);
+              float d0, d1;
+              unpack_f32x2(fma_f32x2(f32x2(a0, a1), kk, cc), d0, d1);
+              const uint32_t w = pack_bf16x2(fast_exp2(d0), fast_exp2(d1));
+              p[16 * h + c] = w;
+              // of the rounded weights, so that they add up to one
+              sum = add_f32x2(sum, f32x2(bf16lo_to_f32(w), bf16hi_to_f32(w)));
+            }
+          }
+          float u, v;
+          unpack_f32x2(sum, u, v);
+          l_new = u + v;
+          if (agreed) break;
+          const float mt = sc * fmaxf(x[0], x[1]);
+          // the reference after the tile before, the other group's
+          float m_ref = -INFINITY;
+          if (i > 0) {
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&m_bar[((T - 1) & 1) * 4 + quarter],
+                                                           ((T - 1) >> 1) & 1)) != 0;
+            if (!ok) break;
+            m_ref = s_m[r];
+          }
+          if (m_ref == -INFINITY)
+            m_new = mt == -INFINITY ? mt : fabsf(mt) <= LP_TOP ? 0.f : mt;
+          else
+            m_new = mt > m_ref + LP_TOP ? mt : m_ref;
+          if (!__any_sync(0xffffffffu, (m_new == -INFINITY ? 0.f : m_new) != mm)) break;
+          const bool moves = m_ref != -INFINITY && m_new != m_ref;
+          if (__any_sync(0xffffffffu, moves)) {   // O's rows with it
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(T - 1) & 3], ((T - 1) >> 2) & 1)) != 0;
+            if (!ok) break;
+            tc::fence_after();
+            const float f = moves ? fast_exp2(m_ref - m_new) : 1.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < 128; c0 += 32) {
+              uint32_t o[32];
+              tc::ld32(tO + c0 + lane_off, o);
+              tc::wait_ld();
+#pragma unroll
+              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+              tc::st32(tO + c0 + lane_off, o);
+            }
+            tc::wait_st();
+          }
+          m_use = m_new;
+          agreed = true;
+        }
+        if (!ok) break;
+        s_m[r] = m_new;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&m_bar[group * 4 + quarter]);
+        if (m_new != m_own) {
+          if (m_own != -INFINITY) l *= fast_exp2(m_own - m_new);
+          m_own = m_new;
+        }
+        l += l_new;
+        tc::st32(tb, *reinterpret_cast<const uint32_t(*)[32]>(p));
+        tc::st32(tb + 32, *reinterpret_cast<const uint32_t(*)[32]>(p + 32));
+        tc::wait_st();
+        tc::fence_before();
+        __syncwarp();
+        if (lane == 0) tc::arrive_cluster(&p_ready[T & 3], 0);
+      }
+      t0 += nt;
+      s_ml[group * 128 + r] = make_float2(m_own, l);
+      const int last = t0 - 1;
+      if (ok) ok = mbar_wait_bounded(&pv_done[last & 3], (last >> 2) & 1);
+      const bool done = __all_sync(0xffffffffu, ok) != 0;
+      all_sync();   // every softmax thread's (m, l)
+      tc::fence_after();
+      const float m = s_m[r];   // after the last tile
+      float lsum = 0.f;
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const float2 x = s_ml[g * 128 + r];
+        // no reference: a sum of zero, or NaN where every score was
+        lsum = x.x == -INFINITY ? lsum + x.y : fmaf(x.y, fast_exp2(x.x - m), lsum);
+      }
+      const bool whole = nt == sg.n;
+      const int64_t prow = ((int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * LP_Q) + 128 * rank;
+      if (!whole && group == 0 && done) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m, lsum);
+      const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
+      const int32_t* const bad = a.bad + sg.hl * LP_BAD;
+      const bool any_bad = a.causal && bad[128] <= limit;
+      // each group half of the columns; 128-byte pieces of a warp's 32 rows go through shared memory,
+      // so that whole lines are written
+      const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
+#pragma unroll 1
+      for (int part = 0; part < (whole ? 1 : 2); ++part) {
+        uint32_t o[2][32];
+        tc::ld32(tO + group * 64 + part * 32 + lane_off, o[0]);
+        if (whole) tc::ld32(tO + group * 64 + 32 + lane_off, o[1]);
+        tc::wait_ld();
+        if (any_bad) {
+          for (int c = 0; c < (whole ? 64 : 32); ++c)
+            if (bad[group * 64 + part * 32 + c] <= limit) {
+#pragma unroll
+              for (int e = 0; e < 64; ++e)
+                if (e == c) o[e >> 5][e & 31] = 0x7FC00000u;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          uint32_t w[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int c = 8 * k + 2 * u;
+            w[u] = whole ? pack_bf16x2(__uint_as_float(o[c >> 5][c & 31]) * inv,
+                                       __uint_as_float(o[c >> 5][(c + 1) & 31]) * inv)
+                         : o[0][4 * k + u];
+          }
+          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int row = u * 4 + (lane >> 3), piece = lane & 7;
+          const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
+          const int rr = quarter * 32 + row, qq = sg.qt * LP_Q + 128 * (int)rank + rr;
+          if (qq < a.C && done) {
+            if (whole)
+              *reinterpret_cast<uint4*>(a.out + ((int64_t)qq * a.H + a.h0 + sg.hl) * 128 + group * 64 +
+                                        piece * 8) = v;
+            else
+              *reinterpret_cast<uint4*>(a.o + (prow + rr) * 128 + group * 64 + part * 32 + piece * 4) = v;
+          }
+        }
+        __syncwarp();
+      }
+      tc::fence_before();
+      all_sync();   // s_m and s_ml read, before a warp goes on to write them
+    }
+    if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+  }
+  // neither CTA may release TMEM or exit while its partner can still reach it
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();
+  if (warp == 0) {
+    tc::fence_after();
+    tc::dealloc2(*tmem_slot, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Join the parts of the item that ends in pair p, if it began in one before: a warp a row,
+// a lane 4 channels.
+// ---------------------------------------------------------------------------
+constexpr int LJ_WARPS = 16, LJ_BATCH = 4, LJ_MAX = 128;   // LJ_MAX: pairs at most
+
+__global__ void __launch_bounds__(32 * LJ_WARPS)
+latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
+  __shared__ float s_w[LJ_WARPS][LJ_MAX];
+  __shared__ int s_slot[LJ_MAX], s_n;
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int pair = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  ChunkIter run = chunk_run(a, pair);
+  const int64_t item = run.start;
+  ChunkSeg sg;
+  if (run.u0 >= run.u1 || !next_chunk_seg(a, run, sg) || sg.j0 == 0 || sg.j1 != sg.n) return;
+  const PairRuns runs(a.units, a.pairs);
+  const int p0 = runs.of(item + LP_HDR);
+  if (threadIdx.x == 0) {   // pairs from the first to this one that have units at all
+    int k = 0;
+    for (int p = p0; p <= pair; ++p)
+      if (runs.first(p) < runs.first(p + 1)) s_slot[k++] = 2 * p + (p == p0 ? 1 : 0);
+    s_n = k;
+  }
+  __syncthreads();
+  const int n = s_n, row = blockIdx.y * LJ_WARPS + warp;
+  const int q = sg.qt * LP_Q + row;
+  if (q >= a.C) return;
+  float M = -INFINITY;
+  for (int i = lane; i < n; i += 32) M = fmaxf(M, a.ml[((int64_t)s_slot[i] * LP_Q + row) * 2]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  float S = 0.f;
+  for (int i = lane; i < n; i += 32) {
+    const float2 x = *reinterpret_cast<const float2*>(a.ml + ((int64_t)s_slot[i] * LP_Q + row) * 2);
+    const float f = M == -INFINITY ? 1.f : fast_exp2(x.x - M);
+    s_w[warp][i] = f;
+    S = fmaf(f, x.y, S);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+  __syncwarp();
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < n; i += LJ_BATCH) {
+    float4 v[LJ_BATCH];
+#pragma unroll
+    for (int k = 0; k < LJ_BATCH; ++k)
+      if (i + k < n)
+        v[k] = *reinterpret_cast<const float4*>(a.o + ((int64_t)s_slot[i + k] * LP_Q + row) * 128 + lane * 4);
+#pragma unroll
+    for (int k = 0; k < LJ_BATCH; ++k)
+      if (i + k < n) {
+        const float w = s_w[warp][i + k];
+        acc.x = fmaf(v[k].x, w, acc.x);
+        acc.y = fmaf(v[k].y, w, acc.y);
+        acc.z = fmaf(v[k].z, w, acc.z);
+        acc.w = fmaf(v[k].w, w, acc.w);
+      }
+  }
+  const float inv = S != 0.f ? 1.f / S : 0.f;
+  *reinterpret_cast<uint2*>(a.out + ((int64_t)q * a.H + a.h0 + sg.hl) * 128 + lane * 4) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+int latent_query_map(const void* q, int64_t H, int64_t C, CUtensorMap* map);
+
+// Heads a pass: enough for eight items a pair, and at least what the L2 cache holds of their keys
+// and values, but no more than 1 GB of them (one head, whatever it takes).
+static int64_t heads_per_pass(int64_t n_pad, int64_t C, int64_t H, int64_t pairs) {
+  const int64_t bytes = n_pad * 512, q_tiles = (C + LP_Q - 1) / LP_Q;
+  const int64_t cached = (int64_t)96 * 1024 * 1024 / bytes, most = (int64_t)1024 * 1024 * 1024 / bytes;
+  int64_t h = (8 * pairs + q_tiles - 1) / q_tiles;
+  if (h > most) h = most;
+  if (h < cached) h = cached;
+  if (h < 1) h = 1;
+  if (h >= H) return H;
+  const int64_t passes = (H + h - 1) / h;   // passes of about equal size
+  return (H + passes - 1) / passes;
+}
+
+static int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
+
+size_t latent_prefill_workspace_bytes(int64_t q_start, int64_t C, int64_t H, int64_t sms) {
+  const int64_t pairs = sms / 2, n_pad = padded(q_start + C);
+  if (C == 0) return 256;
+  const int64_t heads = heads_per_pass(n_pad, C, H, pairs);
+  return (size_t)(256 + round256(H * LP_BAD * 4) + 2 * pairs * LP_Q * (8 + 512) + heads * n_pad * 512);
+}
+
+template <typename... P, typename... A>
+static int launch(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaStream_t stream, const A&... args) {
+  if (smem && smem_optin((const void*)kernel, smem) != JF_OK) return JF_ERR_CUDA;
+  cudaLaunchAttribute pdl[1];
+  pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  pdl[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cfg.attrs = pdl;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? JF_OK : JF_ERR_CUDA;
+}
+
+int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t stream) {
+  const int pairs = sm_count() / 2;
+  if (pairs > LJ_MAX) return JF_ERR_UNSUPPORTED;
+  LatentChunk a{};
+  a.pool = p.pool;
+  a.pt = p.pt;
+  a.out = p.out;
+  a.status = p.status;
+  a.n = p.q_start + p.C;
+  const int64_t n_pad = padded(a.n);
+  a.n_pad = (int32_t)n_pad;
+  a.q_start = p.q_start;
+  a.C = p.C;
+  a.H = p.H;
+  a.causal = p.causal != 0;
+  a.pairs = pairs;
+  a.scale_log2 = p.scale_log2;
+  const int64_t q_tiles = ((int64_t)p.C + LP_Q - 1) / LP_Q;
+  a.q_tiles = (int32_t)q_tiles;
+  const int64_t tiles = ((int64_t)a.n + LP_T - 1) / LP_T, before = ((int64_t)p.q_start + LP_T - 1) / LP_T;
+  // as chunk_start() has it, and the last query tile's
+  a.units_head = (a.causal ? (q_tiles - 1) * (q_tiles - 2) + (q_tiles - 1) * (2 + before + LP_HDR)
+                           : (q_tiles - 1) * (tiles + LP_HDR)) + tiles + LP_HDR;
+  const int64_t per = heads_per_pass(n_pad, p.C, p.H, pairs);
+  uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
+  int32_t* const bad = reinterpret_cast<int32_t*>(ws);
+  const int64_t bad_bytes = round256((int64_t)p.H * LP_BAD * 4);
+  ws += bad_bytes;
+  a.ml = reinterpret_cast<float*>(ws);
+  ws += (int64_t)2 * pairs * LP_Q * 8;
+  a.o = reinterpret_cast<float*>(ws);
+  ws += (int64_t)2 * pairs * LP_Q * 512;
+  a.k = reinterpret_cast<uint16_t*>(ws);
+  a.v = a.k + per * n_pad * 128;
+  CUtensorMap pmap, wkmap, wvmap, qmap, kmap, vmap;
+  int st = bf16_rows_map(p.pool.base, p.pool.row, p.pool.num_pages * p.pool.P, 64, &pmap);
+  if (!st) st = bf16_rows_map(p.w_k, p.pool.R, (int64_t)p.H * 128, 128, &wkmap);
+  if (!st) st = bf16_rows_map(p.w_v, p.pool.R, (int64_t)p.H * 128, 128, &wvmap);
+  if (!st) st = latent_query_map(p.q, p.H, p.C, &qmap);
+  if (!st) st = bf16_rows_map(a.k, 128, per * n_pad, 64, &kmap);
+  if (!st) st = bf16_rows_map(a.v, 128, per * n_pad, 128, &vmap);
+  if (st) return st;
+  if (a.causal && cudaMemsetAsync(bad, 0x7F, bad_bytes, stream) != cudaSuccess) return JF_ERR_CUDA;
+  for (int64_t h0 = 0; h0 < p.H; h0 += per) {
+    a.h0 = (int32_t)h0;
+    a.heads = (int32_t)(p.H - h0 < per ? p.H - h0 : per);
+    a.units = a.units_head * a.heads;
+    a.bad = bad + h0 * LP_BAD;
+    const int64_t e_tiles = n_pad / 256 * a.heads;
+    const unsigned e_pairs = (unsigned)(e_tiles < pairs ? e_tiles : pairs);
+    st = launch(latent_expand_kernel, dim3(2 * e_pairs), LE_THREADS, LeSmem::TOTAL, stream, pmap, wkmap,
+                wvmap, a);
+    if (!st)
+      st = launch(latent_prefill_kernel, dim3(2 * (unsigned)pairs), LA_THREADS, LaSmem::TOTAL, stream, qmap,
+                  pmap, kmap, vmap, a);
+    if (!st)
+      st = launch(latent_prefill_merge_kernel, dim3((unsigned)pairs, LP_Q / LJ_WARPS), 32 * LJ_WARPS, 0,
+                  stream, a);
+    if (st) return st;
+  }
+  return JF_OK;
+}
+
+}  // namespace jfkv

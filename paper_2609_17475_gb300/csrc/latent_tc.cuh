@@ -1,0 +1,96 @@
+// Helpers of the latent cache's tensor-core kernels: pair MMAs on bf16, tiled copies, and
+// the division of a launch's work into one run of equal length per CTA pair.
+#pragma once
+#include "latent.cuh"
+#include "prefill.cuh"
+
+namespace jfkv {
+
+int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows, CUtensorMap* map);
+int sm_count();
+
+inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
+
+__host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int b_mn) {
+  return tc::idesc_f16_f32(M, N, 0, b_mn) | (1u << 7) | (1u << 10);
+}
+
+// Pair MMA, both operands in shared memory, issued where `leader` is set by a warp that runs the
+// issuing code as a whole: control flow and operands are then uniform values.  (Run by one thread
+// alone, each descriptor was moved to uniform registers first: 72 to 100 cycles an instruction for
+// the 32 to 64 that the product takes.)
+__device__ __forceinline__ void mma2_ss_if(uint32_t leader, uint32_t d, uint64_t a, uint64_t b,
+                                           uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, e;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 e, %5, 0;\n\t"
+      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+      ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+
+__device__ __forceinline__ uint32_t elect_one() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xffffffff;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+               : "=r"(p));
+  return p;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;\n" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3}], [%4];\n"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n"
+               ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+// x / y, in 32 bits where both have no more
+__device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
+  return (x | y) >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y);
+}
+struct PairRuns {   // floor(units * p / pairs), by one division
+  int64_t units, each;
+  uint32_t rest, pairs;
+  __device__ __forceinline__ PairRuns(int64_t u, int n) : units(u), pairs((uint32_t)n) {
+    each = (int64_t)divide((uint64_t)u, pairs);
+    rest = (uint32_t)(u - each * n);
+  }
+  __device__ __forceinline__ int64_t first(int p) const {
+    return each * p + (uint32_t)p * rest / pairs;
+  }
+  // the pair that has unit u: the last p with first(p) <= u
+  __device__ __forceinline__ int of(int64_t u) const {
+    return (int)divide((uint64_t)(u + 1) * pairs + (uint64_t)units - 1, (uint64_t)units) - 1;
+  }
+};
+
+// the page of the 64 positions from pos, as a row of the pool; past the map's end (the copy then
+// brings zeros) where there is none
+__device__ __forceinline__ int half_row(const LatentPool& p, const int32_t* pt, int pos, int len,
+                                        int32_t* status) {
+  const int end = (int)(p.num_pages << p.log2P);
+  if (pos >= len) return end;
+  const int32_t page = __ldg(pt + (pos >> p.log2P));
+  if (page < 0 || page >= p.num_pages) {
+    if (status) flag_error(status, JF_DEV_ERR_PAGE_ID);
+    return end;
+  }
+  return (page << p.log2P) + (pos & (p.P - 1));
+}
+
+}  // namespace jfkv
