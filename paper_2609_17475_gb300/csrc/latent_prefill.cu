@@ -18,8 +18,7 @@
 // stays in tensor memory.  Two groups of four softmax warps take the even and the odd
 // tiles, a row a thread.  Weights are 2^(s - m) with a reference m that is 0 unless
 // scores leave [-60, 60] (in powers of two): bf16 and fp32 hold such weights as well as
-// any.  Where a row's reference moves, the tile's weights are worked out again and O is
-// scaled.
+// any.  Where a row's reference moves, O is scaled.
 //
 // Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
 // cut into one run of equal length per pair; a cut item's parts are joined by
@@ -576,81 +575,64 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         ok = __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[T % LA_SB], (T / LA_SB) & 1)) != 0;
         if (!ok) break;
         tc::fence_after();
-        uint32_t p[64];
-        float m_use = m_own, m_new = m_own, l_new = 0.f;
-        bool agreed = false;
+        // S of 64 positions from column c0 in, those not seen at -inf; a scale below zero negates S, one
+        // of zero makes it zero or NaN
+        uint32_t s[2][32];
+        auto scores = [&](int c0) {
+          tc::ld32(tb + c0, s[0]);
+          tc::ld32(tb + c0 + 32, s[1]);
+          tc::wait_ld();
+          if (!(a.scale_log2 > 0.f)) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+              s[c >> 5][c & 31] = a.scale_log2 < 0.f ? s[c >> 5][c & 31] ^ 0x80000000u
+                                                     : __float_as_uint(__uint_as_float(s[c >> 5][c & 31]) * 0.f);
+          }
+          if (key0 + c0 + 63 > limit) {
+#pragma unroll
+            for (int c = 0; c < 64; ++c)
+              if (key0 + c0 + c > limit) s[c >> 5][c & 31] = 0xFF800000u;
+          }
+        };
+        // the row's largest score, then the weights: two short loops, each one copy of its code (written
+        // out over the 128 positions, the code came from beyond the instruction caches at every tile)
+        float x[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-        for (;;) {
-          const float mm = m_use == -INFINITY ? 0.f : m_use;   // -inf: nothing seen so far
-          const uint64_t cc = f32x2(-mm, -mm);
-          float x[2] = {-INFINITY, -INFINITY};
-          uint64_t sum = f32x2(0.f, 0.f);
+        for (int c0 = 0; c0 < LP_T; c0 += 64) {
+          scores(c0);
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            uint32_t s[32];
-            tc::ld32(tb + 32 * h, s);
-            tc::wait_ld();
-            if (!(a.scale_log2 > 0.f)) {   // a scale below zero negates S, one of zero makes it zero or NaN
-#pragma unroll
-              for (int c = 0; c < 32; ++c)
-                s[c] = a.scale_log2 < 0.f ? s[c] ^ 0x80000000u : __float_as_uint(__uint_as_float(s[c]) * 0.f);
-            }
-            if (key0 + 32 * h + 31 > limit) {
-#pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (key0 + 32 * h + c > limit) s[c] = 0xFF800000u;
-            }
-#pragma unroll
-            for (int c = 0; c < 16; ++c) {
-              const float a0 = __uint_as_float(s[2 * c]), a1 = __uint_as_float(s[2 * c + 1]);
-              x[c & 1] = max3(x[c & 1], a0, a1);
-              float d0, d1;
-              unpack_f32x2(fma_f32x2(f32x2(a0, a1), kk, cc), d0, d1);
-              const uint32_t w = pack_bf16x2(fast_exp2(d0), fast_exp2(d1));
-              p[16 * h + c] = w;
-              // of the rounded weights, so that they add up to one
-              sum = add_f32x2(sum, f32x2(bf16lo_to_f32(w), bf16hi_to_f32(w)));
-            }
-          }
-          float u, v;
-          unpack_f32x2(sum, u, v);
-          l_new = u + v;
-          if (agreed) break;
-          const float mt = sc * fmaxf(x[0], x[1]);
-          // the reference after the tile before, the other group's
-          float m_ref = -INFINITY;
-          if (i > 0) {
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&m_bar[((T - 1) & 1) * 4 + quarter],
-                                                           ((T - 1) >> 1) & 1)) != 0;
-            if (!ok) break;
-            m_ref = s_m[r];
-          }
-          if (m_ref == -INFINITY)
-            m_new = mt == -INFINITY ? mt : fabsf(mt) <= LP_TOP ? 0.f : mt;
-          else
-            m_new = mt > m_ref + LP_TOP ? mt : m_ref;
-          if (!__any_sync(0xffffffffu, (m_new == -INFINITY ? 0.f : m_new) != mm)) break;
-          const bool moves = m_ref != -INFINITY && m_new != m_ref;
-          if (__any_sync(0xffffffffu, moves)) {   // O's rows with it
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(T - 1) & 3], ((T - 1) >> 2) & 1)) != 0;
-            if (!ok) break;
-            tc::fence_after();
-            const float f = moves ? fast_exp2(m_ref - m_new) : 1.f;
-#pragma unroll 1
-            for (int c0 = 0; c0 < 128; c0 += 32) {
-              uint32_t o[32];
-              tc::ld32(tO + c0 + lane_off, o);
-              tc::wait_ld();
-#pragma unroll
-              for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-              tc::st32(tO + c0 + lane_off, o);
-            }
-            tc::wait_st();
-          }
-          m_use = m_new;
-          agreed = true;
+          for (int c = 0; c < 32; ++c)
+            x[c & 1] = max3(x[c & 1], __uint_as_float(s[c >> 4][(2 * c) & 31]),
+                            __uint_as_float(s[c >> 4][(2 * c + 1) & 31]));
         }
-        if (!ok) break;
+        const float mt = sc * fmaxf(x[0], x[1]);
+        // the reference after the tile before, the other group's
+        float m_ref = -INFINITY;   // nothing seen so far
+        if (i > 0) {
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&m_bar[((T - 1) & 1) * 4 + quarter],
+                                                         ((T - 1) >> 1) & 1)) != 0;
+          if (!ok) break;
+          m_ref = s_m[r];
+        }
+        const float m_new = m_ref == -INFINITY ? (mt == -INFINITY ? mt : fabsf(mt) <= LP_TOP ? 0.f : mt)
+                                               : (mt > m_ref + LP_TOP ? mt : m_ref);
+        const bool moves = m_ref != -INFINITY && m_new != m_ref;
+        if (__any_sync(0xffffffffu, moves)) {   // O's rows with it
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(T - 1) & 3], ((T - 1) >> 2) & 1)) != 0;
+          if (!ok) break;
+          tc::fence_after();
+          const float f = moves ? fast_exp2(m_ref - m_new) : 1.f;
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t o[32];
+            tc::ld32(tO + c0 + lane_off, o);
+            tc::wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+            tc::st32(tO + c0 + lane_off, o);
+          }
+          tc::wait_st();
+        }
         s_m[r] = m_new;
         __syncwarp();
         if (lane == 0) mbar_arrive(&m_bar[group * 4 + quarter]);
@@ -658,9 +640,30 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           if (m_own != -INFINITY) l *= fast_exp2(m_own - m_new);
           m_own = m_new;
         }
-        l += l_new;
-        tc::st32(tb, *reinterpret_cast<const uint32_t(*)[32]>(p));
-        tc::st32(tb + 32, *reinterpret_cast<const uint32_t(*)[32]>(p + 32));
+        const float mm = m_new == -INFINITY ? 0.f : m_new;
+        const uint64_t cc = f32x2(-mm, -mm);
+        uint64_t sum = f32x2(0.f, 0.f);
+#pragma unroll 1
+        for (int c0 = 0; c0 < LP_T; c0 += 64) {
+          scores(c0);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t p[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              float d0, d1;
+              unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s[h][2 * c]), __uint_as_float(s[h][2 * c + 1])),
+                                     kk, cc), d0, d1);
+              p[c] = pack_bf16x2(fast_exp2(d0), fast_exp2(d1));
+              // of the rounded weights, so that they add up to one
+              sum = add_f32x2(sum, f32x2(bf16lo_to_f32(p[c]), bf16hi_to_f32(p[c])));
+            }
+            st16(tb + c0 / 2 + 16 * h, p);   // over scores already read
+          }
+        }
+        float u, v;
+        unpack_f32x2(sum, u, v);
+        l += u + v;
         tc::wait_st();
         tc::fence_before();
         __syncwarp();
