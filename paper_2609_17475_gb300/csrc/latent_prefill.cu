@@ -54,14 +54,19 @@ struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
 // ===========================================================================
 // Expansion
 // ===========================================================================
-constexpr int LE_STAGES = 5;
+// A pair takes a run of (256 positions, head) tiles, heads within positions, and keeps the
+// positions' latents in shared memory while the heads' weights stream past: with both
+// streamed a CTA read 64 bytes a cycle, more than the L2 cache gives all of them.
+constexpr int LE_STAGES = 4;
+constexpr int LE_CHUNKS = 8;           // 64-channel chunks of R at most
 constexpr int LE_THREADS = 32 * 12;
 struct LeSmem {
-  static constexpr int A_BYTES = 128 * 128, B_BYTES = 128 * 128;   // 64 channels of 128 rows
-  static constexpr int STAGE = A_BYTES + B_BYTES;
-  static constexpr int OFF_OUT = LE_STAGES * STAGE;                // 8 warps x [32 rows][128 B]
+  static constexpr int CHUNK = 128 * 128;                          // 64 channels of 128 rows
+  static constexpr int OFF_B = LE_CHUNKS * CHUNK;
+  static constexpr int OFF_OUT = OFF_B + LE_STAGES * CHUNK;        // 8 warps x [32 rows][128 B]
   static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
-  static constexpr int TOTAL = OFF_BAR + 256;
+  static constexpr int TOTAL = OFF_BAR + 512;
+  static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LE_THREADS, 1)
@@ -71,16 +76,19 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   constexpr uint32_t ID = idesc_bf16(256, 256, 0);
   extern __shared__ __align__(1024) uint8_t sm[];
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
-  uint64_t* const full = bars + 0;      // [5] on CTA 0: both CTAs' operands
-  uint64_t* const land = bars + 5;      // [5] CTA 1's
-  uint64_t* const free_ = bars + 10;    // [5] stage read
-  uint64_t* const d_full = bars + 15;   // [2] a tile's products done
-  uint64_t* const d_free = bars + 17;   // [2] on CTA 0: and gone out, in both CTAs
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 19);
+  uint64_t* const b_full = bars + 0;    // [4] on CTA 0: both CTAs' weights of a stage
+  uint64_t* const a_full = bars + 4;    // [8] on CTA 0: both CTAs' latents, 64 channels
+  uint64_t* const b_land = bars + 12;   // [4] CTA 1's
+  uint64_t* const a_land = bars + 16;   // [8]
+  uint64_t* const b_free = bars + 24;   // [4] stage read
+  uint64_t* const a_free = bars + 28;   // all products with these latents done
+  uint64_t* const d_full = bars + 29;   // [2] a tile's products done
+  uint64_t* const d_free = bars + 31;   // [2] on CTA 0: and gone out, in both CTAs
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 33);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
-  const int pair = (int)(blockIdx.x >> 1);
+  const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
   if (smem_u32(sm) & 1023u) {   // the same in both CTAs
     if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
     return;
@@ -89,10 +97,15 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
     prefetch_tensormap(&pmap);
     prefetch_tensormap(rank ? &vmap : &kmap);
     for (int i = 0; i < LE_STAGES; ++i) {
-      mbar_init(&full[i], 2);
-      mbar_init(&land[i], 1);
-      mbar_init(&free_[i], 1);
+      mbar_init(&b_full[i], 2);
+      mbar_init(&b_land[i], 1);
+      mbar_init(&b_free[i], 1);
     }
+    for (int i = 0; i < LE_CHUNKS; ++i) {
+      mbar_init(&a_full[i], 2);
+      mbar_init(&a_land[i], 1);
+    }
+    mbar_init(a_free, 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&d_full[i], 1);
       mbar_init(&d_free[i], 16);
@@ -104,78 +117,119 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
   tc::fence_after();
+  const int64_t tiles = (int64_t)(a.n_pad / 256) * a.heads;
+  const int64_t i0 = tiles * pair / pairs, i1 = tiles * (pair + 1) / pairs;
+  int pt = (int)(i0 / a.heads), hl = (int)(i0 - (int64_t)pt * a.heads);   // of the current tile
+  const int count = (int)(i1 - i0), steps = a.pool.R / 64;
+  auto advance = [&] {
+    if (++hl == a.heads) {
+      hl = 0;
+      ++pt;
+    }
+  };
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
-  const int tiles = (a.n_pad / 256) * a.heads;   // heads within 256 positions
-  const int steps = a.pool.R / 64;
   bool ok = true;
   if (warp == 0) {
-    int st = 0, ph = 0;   // stage and how often the ring went round
+    int st = 0, ph = 0, na = 0;   // stage, how often the ring went round, latents taken so far
     if (rank == 0) {
       const uint32_t leader = elect_one();
       const uint64_t ad = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
+      const uint64_t bd = tc::sdesc_sw128(smem_u32(sm + L::OFF_B), 16, 1024);
       auto wait = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
-      int t = 0;
-      for (int i = pair; i < tiles && ok; i += a.pairs, ++t) {
+      for (int t = 0; t < count && ok; ++t) {
+        const bool fresh = t == 0 || hl == 0;
         if (t >= 2) ok = wait(&d_free[t & 1], (t >> 1) - 1);
         tc::fence_after();
         const uint32_t d = (t & 1) * 256;
         for (int s = 0; s < steps && ok; ++s) {
-          ok = wait(&full[st], ph);
+          if (fresh) ok = wait(&a_full[s], na);
+          ok = ok && wait(&b_full[st], ph);
           tc::fence_after();
-          const uint64_t at = ad + (uint64_t)(st * (L::STAGE >> 4));
+          const uint64_t at = ad + (uint64_t)(s * (L::CHUNK >> 4)), bt = bd + (uint64_t)(st * (L::CHUNK >> 4));
           if (ok) {
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              mma2_ss_if(leader, d, at + ((k * 32) >> 4), at + ((L::A_BYTES + k * 32) >> 4), ID,
+              mma2_ss_if(leader, d, at + ((k * 32) >> 4), bt + ((k * 32) >> 4), ID,
                          (s > 0 || k > 0) ? 1u : 0u);
-            tc::commit2_both_if(leader, &free_[st]);
+            tc::commit2_both_if(leader, &b_free[st]);
           }
           if (++st == LE_STAGES) {
             st = 0;
             ++ph;
           }
         }
+        if (fresh) ++na;
+        advance();
+        if (ok && hl == 0) tc::commit2_both_if(leader, a_free);
         if (ok) tc::commit2_both_if(leader, &d_full[t & 1]);
       }
     } else if (lane == 0) {
-      for (int i = pair; i < tiles && ok; i += a.pairs)
+      for (int t = 0; t < count && ok; ++t) {
+        const bool fresh = t == 0 || hl == 0;
         for (int s = 0; s < steps && ok; ++s) {
-          ok = mbar_wait_bounded(&land[st], ph & 1);
-          if (ok) tc::arrive_cluster(&full[st], 0);
+          if (fresh) {
+            ok = mbar_wait_bounded(&a_land[s], na & 1);
+            if (ok) tc::arrive_cluster(&a_full[s], 0);
+          }
+          if (ok) ok = mbar_wait_bounded(&b_land[st], ph & 1);
+          if (ok) tc::arrive_cluster(&b_full[st], 0);
           if (++st == LE_STAGES) {
             st = 0;
             ++ph;
           }
         }
+        if (fresh) ++na;
+        advance();
+      }
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     __syncwarp();
   } else if (warp == 1) {
+    // ---- weights: the keys' 128 rows of the head (CTA 0), the values' (CTA 1) ----------------
     if (lane == 0) {
       int st = 0, ph = 0;
-      for (int i = pair; i < tiles && ok; i += a.pairs) {
-        const int pos = (i / a.heads) * 256 + 128 * (int)rank, h = a.h0 + i % a.heads;
-        const int row0 = half_row(a.pool, a.pt, pos, a.n, a.status);
-        const int row1 = half_row(a.pool, a.pt, pos + 64, a.n, a.status);
+      for (int t = 0; t < count && ok; ++t, advance())
         for (int s = 0; s < steps; ++s) {
-          if (ph > 0 && !mbar_wait_bounded(&free_[st], (ph - 1) & 1)) {
+          if (ph > 0 && !mbar_wait_bounded(&b_free[st], (ph - 1) & 1)) {
             ok = false;
             break;
           }
-          uint64_t* const bar = rank == 0 ? &full[st] : &land[st];
-          mbar_arrive_expect_tx(bar, L::STAGE);
-          const uint32_t dst = smem_u32(sm) + st * L::STAGE;
-          tma_load_2d(dst, &pmap, s * 64, row0, bar);
-          tma_load_2d(dst + 8192, &pmap, s * 64, row1, bar);
-          tma_load_2d(dst + L::A_BYTES, rank ? &vmap : &kmap, s * 64, h * 128, bar);
+          uint64_t* const bar = rank == 0 ? &b_full[st] : &b_land[st];
+          mbar_arrive_expect_tx(bar, L::CHUNK);
+          tma_load_2d(smem_u32(sm + L::OFF_B + st * L::CHUNK), rank ? &vmap : &kmap, s * 64,
+                      (a.h0 + hl) * 128, bar);
           if (++st == LE_STAGES) {
             st = 0;
             ++ph;
           }
+        }
+      if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
+    }
+    __syncwarp();
+  } else if (warp == 2) {
+    // ---- latents: this CTA's 128 of the 256 positions -----------------------------------
+    if (lane == 0) {
+      int na = 0;
+      for (int t = 0; t < count && ok; ++t, advance()) {
+        if (t > 0 && hl > 0) continue;
+        if (na > 0 && !mbar_wait_bounded(a_free, (na - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        ++na;
+        const int pos = pt * 256 + 128 * (int)rank;
+        const int row0 = half_row(a.pool, a.pt, pos, a.n, a.status);
+        const int row1 = half_row(a.pool, a.pt, pos + 64, a.n, a.status);
+        for (int s = 0; s < steps; ++s) {
+          uint64_t* const bar = rank == 0 ? &a_full[s] : &a_land[s];
+          mbar_arrive_expect_tx(bar, L::CHUNK);
+          const uint32_t dst = smem_u32(sm) + s * L::CHUNK;
+          tma_load_2d(dst, &pmap, s * 64, row0, bar);
+          tma_load_2d(dst + 8192, &pmap, s * 64, row1, bar);
         }
       }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -189,10 +243,8 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
     uint16_t* const dst = kind ? a.v : a.k;
     // values of positions that not every query of the chunk sees
     const int apart = kind && a.causal ? a.q_start + 1 : 0x7FFFFFFF;
-    int t = 0;
-    for (int i = pair; i < tiles; i += a.pairs, ++t) {
-      const int hl = i % a.heads;
-      const int pos0 = (i / a.heads) * 256 + 128 * (int)rank + quarter * 32;
+    for (int t = 0; t < count; ++t, advance()) {
+      const int pos0 = pt * 256 + 128 * (int)rank + quarter * 32;
       const int pos = pos0 + lane;
       if (!mbar_wait_bounded(&d_full[t & 1], (t >> 1) & 1)) {
         ok = false;
@@ -751,67 +803,85 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
 }
 
 // ---------------------------------------------------------------------------
-// Join the parts of the item that ends in pair p, if it began in one before: a warp a row,
-// a lane 4 channels.
+// Join the parts of the item that ends in pair p, if it began in one before: four rows a
+// warp, a lane 4 channels.
 // ---------------------------------------------------------------------------
-constexpr int LJ_WARPS = 16, LJ_BATCH = 4, LJ_MAX = 128;   // LJ_MAX: pairs at most
+constexpr int LJ_WARPS = 8, LJ_ROWS = 4, LJ_MAX = 128;   // LJ_MAX: pairs at most
 
 __global__ void __launch_bounds__(32 * LJ_WARPS)
 latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
-  __shared__ float s_w[LJ_WARPS][LJ_MAX];
+  __shared__ float s_w[LJ_WARPS][LJ_ROWS][LJ_MAX];
   __shared__ int s_slot[LJ_MAX], s_n;
-  asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int pair = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ChunkIter run = chunk_run(a, pair);
   const int64_t item = run.start;
   ChunkSeg sg;
   if (run.u0 >= run.u1 || !next_chunk_seg(a, run, sg) || sg.j0 == 0 || sg.j1 != sg.n) return;
-  const PairRuns runs(a.units, a.pairs);
-  const int p0 = runs.of(item + LP_HDR);
-  if (threadIdx.x == 0) {   // pairs from the first to this one that have units at all
-    int k = 0;
-    for (int p = p0; p <= pair; ++p)
-      if (runs.first(p) < runs.first(p + 1)) s_slot[k++] = 2 * p + (p == p0 ? 1 : 0);
-    s_n = k;
+  const int row0 = ((int)blockIdx.y * LJ_WARPS + warp) * LJ_ROWS;
+  if (warp == 0) {   // pairs from the first to this one that have units at all
+    const PairRuns runs(a.units, a.pairs);
+    const int p0 = runs.of(item + LP_HDR);
+    int n = 0;
+    for (int p = p0 + lane; p - lane <= pair; p += 32) {
+      const bool has = p <= pair && runs.first(p) < runs.first(p + 1);
+      const unsigned m = __ballot_sync(0xffffffffu, has);
+      if (has) s_slot[n + __popc(m & ((1u << lane) - 1))] = 2 * p + (p == p0 ? 1 : 0);
+      n += __popc(m);
+    }
+    if (lane == 0) s_n = n;
   }
   __syncthreads();
-  const int n = s_n, row = blockIdx.y * LJ_WARPS + warp;
-  const int q = sg.qt * LP_Q + row;
-  if (q >= a.C) return;
-  float M = -INFINITY;
-  for (int i = lane; i < n; i += 32) M = fmaxf(M, a.ml[((int64_t)s_slot[i] * LP_Q + row) * 2]);
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int n = s_n, q0 = sg.qt * LP_Q + row0;
+  if (q0 >= a.C) return;
+  // weights: eight lanes a row
+  const int sub = lane & 7, mine = lane >> 3;
+  const float* const ml = a.ml + (int64_t)(row0 + mine) * 2;
+  float M = -INFINITY, S = 0.f;
+  for (int i = sub; i < n; i += 8) M = fmaxf(M, ml[(int64_t)s_slot[i] * (LP_Q * 2)]);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  float S = 0.f;
-  for (int i = lane; i < n; i += 32) {
-    const float2 x = *reinterpret_cast<const float2*>(a.ml + ((int64_t)s_slot[i] * LP_Q + row) * 2);
+  for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  for (int i = sub; i < n; i += 8) {
+    const float2 x = *reinterpret_cast<const float2*>(ml + (int64_t)s_slot[i] * (LP_Q * 2));
     const float f = M == -INFINITY ? 1.f : fast_exp2(x.x - M);
-    s_w[warp][i] = f;
+    s_w[warp][mine][i] = f;
     S = fmaf(f, x.y, S);
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+  for (int o = 4; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
   __syncwarp();
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < n; i += LJ_BATCH) {
-    float4 v[LJ_BATCH];
+  float4 acc[LJ_ROWS];
 #pragma unroll
-    for (int k = 0; k < LJ_BATCH; ++k)
-      if (i + k < n)
-        v[k] = *reinterpret_cast<const float4*>(a.o + ((int64_t)s_slot[i + k] * LP_Q + row) * 128 + lane * 4);
+  for (int k = 0; k < LJ_ROWS; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* const o = a.o + (int64_t)row0 * 128 + lane * 4;
+  for (int i = 0; i < n; i += 2) {
+    float4 v[2][LJ_ROWS];
 #pragma unroll
-    for (int k = 0; k < LJ_BATCH; ++k)
-      if (i + k < n) {
-        const float w = s_w[warp][i + k];
-        acc.x = fmaf(v[k].x, w, acc.x);
-        acc.y = fmaf(v[k].y, w, acc.y);
-        acc.z = fmaf(v[k].z, w, acc.z);
-        acc.w = fmaf(v[k].w, w, acc.w);
-      }
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int k = 0; k < LJ_ROWS; ++k)   // rows past the chunk's end: whatever is there
+        if (i + u < n)
+          v[u][k] = *reinterpret_cast<const float4*>(o + ((int64_t)s_slot[i + u] * LP_Q + k) * 128);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int k = 0; k < LJ_ROWS; ++k)
+        if (i + u < n) {
+          const float w = s_w[warp][k][i + u];
+          acc[k].x = fmaf(v[u][k].x, w, acc[k].x);
+          acc[k].y = fmaf(v[u][k].y, w, acc[k].y);
+          acc[k].z = fmaf(v[u][k].z, w, acc[k].z);
+          acc[k].w = fmaf(v[u][k].w, w, acc[k].w);
+        }
   }
-  const float inv = S != 0.f ? 1.f / S : 0.f;
-  *reinterpret_cast<uint2*>(a.out + ((int64_t)q * a.H + a.h0 + sg.hl) * 128 + lane * 4) =
-      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+#pragma unroll
+  for (int k = 0; k < LJ_ROWS; ++k) {
+    const float s = __shfl_sync(0xffffffffu, S, 8 * k);
+    const float inv = s != 0.f ? 1.f / s : 0.f;
+    if (q0 + k < a.C)
+      *reinterpret_cast<uint2*>(a.out + ((int64_t)(q0 + k) * a.H + a.h0 + sg.hl) * 128 + lane * 4) =
+          make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -914,7 +984,7 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
       st = launch(latent_prefill_kernel, dim3(2 * (unsigned)pairs), LA_THREADS, LaSmem::TOTAL, stream, qmap,
                   pmap, kmap, vmap, a);
     if (!st)
-      st = launch(latent_prefill_merge_kernel, dim3((unsigned)pairs, LP_Q / LJ_WARPS), 32 * LJ_WARPS, 0,
+      st = launch(latent_prefill_merge_kernel, dim3((unsigned)pairs, LP_Q / (LJ_WARPS * LJ_ROWS)), 32 * LJ_WARPS, 0,
                   stream, a);
     if (st) return st;
   }
