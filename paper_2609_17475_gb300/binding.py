@@ -166,7 +166,9 @@ def _calls():
         at = lambda f: ctypes.cast(f, ctypes.c_void_p).value  # noqa: E731
         _jfcall.setup((at(L.jf_kv8_append), at(L.jf_kv8_read), at(L.jf_rope_axes),
                        at(L.jf_paged_decode_attn), at(L.jf_paged_decode_weights_attn),
-                       at(L.jf_kv8_evict)),
+                       at(L.jf_kv8_evict), at(L.jf_latent_append), at(L.jf_latent_read),
+                       at(L.jf_latent_decode_attn), at(L.jf_latent_prefix_decode_attn),
+                       at(L.jf_latent_prefill_attn)),
                       (torch.int32, torch.uint8, torch.float32, torch.bfloat16, torch.float16),
                       _raw_stream, _get_device, torch.cuda.current_stream, torch.is_grad_enabled,
                       torch.autograd.graph.increment_version)
@@ -834,42 +836,15 @@ def jf_kv8_evict(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Ten
 # ---------------------------------------------------------------------------
 # the latent cache
 # ---------------------------------------------------------------------------
-def _latent_rows(fn, pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag, stream):
-    _need(page_table, torch.int32, "page_table")
-    _need(start_pos, torch.int32, "start_pos")
-    _need(row_offsets, torch.int32, "row_offsets")
-    if err_flag is not None:
-        _need(err_flag, torch.int32, "err_flag")
-    R = pool.head_dim - JF_LATENT_ROT
-    strides = []
-    for t, width, name in ((latent, R, "latent"), (k_rot, JF_LATENT_ROT, "k_rot")):
-        if not isinstance(t, torch.Tensor) or t.dtype is not torch.bfloat16 or not t.is_cuda:
-            raise TypeError(f"{name} must be a CUDA tensor of dtype torch.bfloat16")
-        if t.dim() != 2 or t.shape[1] != width:
-            raise ValueError(f"{name} must be [rows, {width}]")
-        if t.shape[0] and t.stride(1) != 1:
-            raise ValueError(f"{name}: the channels of a row must adjoin")
-        # the row stride of a single row is whatever a slicing left: it is not used
-        strides.append(t.stride(0) if t.shape[0] > 1 else width)
-    n = latent.shape[0]
-    pt = page_table if page_table.dim() == 2 else page_table.view(1, -1)
-    if k_rot.shape[0] != n:
-        raise ValueError("latent and k_rot must have the same rows")
-    if start_pos.numel() != pt.shape[0] or row_offsets.numel() != pt.shape[0] + 1:
-        raise ValueError("one start_pos per page-table row, and one row offset more")
-    _check(fn, getattr(lib(), fn)(ctypes.byref(pool.c_struct()), _ptr(pt), pt.shape[1], pt.shape[0],
-                                  _ptr(start_pos), _ptr(row_offsets), _ptr(latent), strides[0],
-                                  _ptr(k_rot), strides[1], n, _ptr(err_flag), _stream(stream)))
-
-
 @_traced
 def jf_latent_append(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tensor,
                      row_offsets: torch.Tensor, latent: torch.Tensor, k_rot: torch.Tensor,
                      err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Append rows row_offsets[b] .. row_offsets[b + 1] - 1 of latent (bf16 [rows, R]) and
     k_rot ([rows, 64], rows any stride apart) at positions start_pos[b] .. of request b."""
-    _latent_rows("jf_latent_append", pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag,
-                 stream)
+    st = (_fast or _calls()).latent_append(pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag, stream)
+    if st:
+        raise JfError("jf_latent_append", st)
 
 
 @_traced
@@ -877,8 +852,9 @@ def jf_latent_read(pool: KVPool, page_table: torch.Tensor, start_pos: torch.Tens
                    row_offsets: torch.Tensor, latent: torch.Tensor, k_rot: torch.Tensor,
                    err_flag: Optional[torch.Tensor] = None, stream=None) -> None:
     """Read runs of positions back into latent and k_rot."""
-    _latent_rows("jf_latent_read", pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag,
-                 stream)
+    st = (_fast or _calls()).latent_read(pool, page_table, start_pos, row_offsets, latent, k_rot, err_flag, stream)
+    if st:
+        raise JfError("jf_latent_read", st)
 
 
 def jf_latent_workspace_bytes(batch: int, num_heads: int, latent_dim: int, num_groups: int = 0,
@@ -897,30 +873,15 @@ def latent_decode_workspace(batch: int, num_heads: int, latent_dim: int, num_gro
     return ws
 
 
-def _latent_decode_args(pool, page_table, context_lens, q, out, workspace):
-    _need(page_table, torch.int32, "page_table")
-    _need(context_lens, torch.int32, "context_lens")
-    _need(q, torch.bfloat16, "q")
-    _need(out, torch.bfloat16, "out")
-    _need(workspace, torch.uint8, "workspace")
-    if (q.dim() != 3 or q.shape[2] != pool.head_dim or page_table.dim() != 2
-            or tuple(out.shape) != (q.shape[0], q.shape[1], pool.head_dim - JF_LATENT_ROT)
-            or page_table.shape[0] != q.shape[0] or context_lens.numel() != q.shape[0]):
-        raise ValueError("shape mismatch")
-
-
 @_traced
 def jf_latent_decode_attn(pool: KVPool, page_table: torch.Tensor, context_lens: torch.Tensor,
                           q: torch.Tensor, softmax_scale: float, out: torch.Tensor,
                           workspace: torch.Tensor, stream=None) -> None:
     """Decode attention over a latent pool, absorbed form: q is [batch, heads, R + 64], out
     [batch, heads, R]: the weighted sum of the latents, before the heads' value projections."""
-    _latent_decode_args(pool, page_table, context_lens, q, out, workspace)
-    st = lib().jf_latent_decode_attn(ctypes.byref(pool.c_struct()), _ptr(page_table), page_table.shape[1],
-                                     _ptr(context_lens), q.shape[0], _ptr(q), q.shape[1],
-                                     float(softmax_scale), _ptr(out), _ptr(workspace), workspace.numel(),
-                                     _stream(stream))
-    _check("jf_latent_decode_attn", st)
+    st = (_fast or _calls()).latent_decode(pool, page_table, context_lens, q, softmax_scale, out, workspace, stream)
+    if st:
+        raise JfError("jf_latent_decode_attn", st)
 
 
 @_traced
@@ -931,20 +892,10 @@ def jf_latent_prefix_decode_attn(pool: KVPool, prefix_table: torch.Tensor, prefi
     """jf_latent_decode_attn for groups of requests that begin with one shared run of positions:
     request b of group g (group_offsets[g] <= b < group_offsets[g + 1], a host sequence) attends
     prefix_lens[g] positions of prefix_table[g]'s pages, then context_lens[b] of its own."""
-    _latent_decode_args(pool, page_table, context_lens, q, out, workspace)
-    _need(prefix_table, torch.int32, "prefix_table")
-    _need(prefix_lens, torch.int32, "prefix_lens")
-    G = prefix_lens.numel()
-    if prefix_table.dim() != 2 or prefix_table.shape[0] != G or len(group_offsets) != G + 1:
-        raise ValueError("one prefix_table row and prefix length per group, and one group offset more")
-    off = (ctypes.c_int32 * (G + 1))(*[int(x) for x in group_offsets])
-    st = lib().jf_latent_prefix_decode_attn(ctypes.byref(pool.c_struct()), _ptr(prefix_table),
-                                            prefix_table.shape[1], _ptr(prefix_lens), off, G,
-                                            _ptr(page_table), page_table.shape[1], _ptr(context_lens),
-                                            q.shape[0], _ptr(q), q.shape[1], float(softmax_scale),
-                                            _ptr(out), _ptr(workspace), workspace.numel(),
-                                            _stream(stream))
-    _check("jf_latent_prefix_decode_attn", st)
+    st = (_fast or _calls()).latent_prefix(pool, prefix_table, prefix_lens, group_offsets, page_table, context_lens, q,
+                                           softmax_scale, out, workspace, stream)
+    if st:
+        raise JfError("jf_latent_prefix_decode_attn", st)
 
 
 def jf_latent_prefill_workspace_bytes(q_start: int, chunk_len: int, num_heads: int,
@@ -968,20 +919,7 @@ def jf_latent_prefill_attn(pool: KVPool, page_table_row: torch.Tensor, q: torch.
                            out: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
     """Prefill-chunk attention over a latent pool, expanded form: q is [chunk, heads, 192] (128
     channels and the 64 rotated ones), w_k and w_v [heads, 128, R], out [chunk, heads, 128]."""
-    _need(page_table_row, torch.int32, "page_table_row")
-    _need(q, torch.bfloat16, "q")
-    _need(w_k, torch.bfloat16, "w_k")
-    _need(w_v, torch.bfloat16, "w_v")
-    _need(out, torch.bfloat16, "out")
-    _need(workspace, torch.uint8, "workspace")
-    R = pool.head_dim - JF_LATENT_ROT
-    if (q.dim() != 3 or q.shape[2] != 128 + JF_LATENT_ROT or tuple(out.shape) != (q.shape[0], q.shape[1], 128)
-            or tuple(w_k.shape) != (q.shape[1], 128, R) or w_v.shape != w_k.shape):
-        raise ValueError("shape mismatch")
-    if page_table_row.numel() * pool.page_size < int(q_start) + q.shape[0]:
-        raise ValueError("the page-table row does not hold the chunk")
-    st = lib().jf_latent_prefill_attn(ctypes.byref(pool.c_struct()), _ptr(page_table_row), _ptr(q),
-                                      int(q_start), q.shape[0], q.shape[1], _ptr(w_k), _ptr(w_v),
-                                      float(softmax_scale), int(bool(causal)), _ptr(out), _ptr(workspace),
-                                      workspace.numel(), _stream(stream))
-    _check("jf_latent_prefill_attn", st)
+    st = (_fast or _calls()).latent_prefill(pool, page_table_row, q, q_start, w_k, w_v, softmax_scale, causal, out,
+                                            workspace, stream)
+    if st:
+        raise JfError("jf_latent_prefill_attn", st)

@@ -67,8 +67,9 @@ struct LdSmem {
   static constexpr int OFF_P = OFF_V + VS * V_BYTES;   // [2 x 64 positions][64 rows][128 B]
   static constexpr int OFF_BAR = OFF_P + 2 * CHUNK;
   static constexpr int OFF_X = OFF_BAR + 256;          // [2][256] exchange between a row's threads
-  static constexpr int OFF_PLAN = OFF_X + 2 * 256 * 4; // [32] of the plan's scan
-  static constexpr int TOTAL = OFF_PLAN + 32 * 8;
+  static constexpr int OFF_PLAN = OFF_X + 2 * 256 * 4; // [16] of the plan's scan
+  static constexpr int OFF_FIRST = OFF_PLAN + 16 * 8;  // LdFirst
+  static constexpr int TOTAL = OFF_FIRST + 128;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -116,22 +117,26 @@ __device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const Laten
 }
 
 // The segments of a pair's run of units [u0, u1), in order.
-struct SegIter {
-  int64_t start, u0, u1;
-  int item;
-  int known;    // the first item's length, read already
-};
 struct Seg {
   LatentItem it;
   int item, j0, j1, n;   // tiles j0 .. j1 - 1 of the item's n
 };
+struct SegIter {
+  int64_t start, u0, u1;   // first unit of the item
+  int item;
+  const Seg* first;        // the first segment, worked out already
+};
 
 __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan& pl, SegIter& s,
                                          Seg& seg) {
+  if (s.first) {
+    seg = *s.first;
+    s.first = nullptr;
+    return true;
+  }
   while (s.item < pl.items && s.start < s.u1) {
     const int g = item_group(pl, s.item);
-    const int len = s.known >= 0 ? s.known : item_len(a, pl, s.item, g);
-    s.known = -1;
+    const int len = item_len(a, pl, s.item, g);
     const int n = tiles_of(len);
     const int64_t first = s.start + LD_HDR;   // unit of tile 0
     const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
@@ -148,6 +153,12 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
   }
   return false;
 }
+
+struct LdFirst {   // a pair's first segment and what comes after it
+  SegIter next;
+  Seg seg;
+  int has;
+};
 
 template <int R>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LD_THREADS, 1)
@@ -176,6 +187,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 24);
   float* const s_x = reinterpret_cast<float*>(sm + L::OFF_X);
   int64_t* const s_plan = reinterpret_cast<int64_t*>(sm + L::OFF_PLAN);
+  LdFirst* const s_first = reinterpret_cast<LdFirst*>(sm + L::OFF_FIRST);
+  static_assert(sizeof(LdFirst) <= 128 && LD_THREADS / 32 <= 16, "shared memory of the plan");
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
@@ -207,6 +220,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     fence_barrier_init();
   }
   if (warp == 0) tc::alloc2(tmem_slot, 512);
+  tc::fence_before();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // waited for after the plan
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
 
   // ---- the plan: units before each thread's items, and this pair's first item ----------
@@ -240,26 +255,46 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     run.u0 = runs.first(pair);
     run.u1 = runs.first(pair + 1);
     const bool mine = run.u0 < run.u1 && at <= run.u0 && run.u0 < at + sum;
+    if (threadIdx.x == 0) s_first->has = 0;
+    __syncthreads();
     if (mine || blockIdx.x == 0)
       for (int i = i0; i < i1; ++i) {
-        const int len = i == i0 ? len0 : item_len(a, pl, i, item_group(pl, i));
-        const int64_t n = units_of(len);
+        const int g = item_group(pl, i);
+        const int len = i == i0 ? len0 : item_len(a, pl, i, g);
+        const int n = tiles_of(len);
+        const int64_t next = at + units_of(len);
         if (blockIdx.x == 0) pl.starts[i] = at;
-        if (mine && at <= run.u0 && run.u0 < at + n) {
-          s_plan[16] = i;
-          s_plan[17] = at;
-          s_plan[18] = len;
+        if (mine && at <= run.u0 && run.u0 < next) {
+          // this thread has the pair's first item: its first segment, unless that is the header alone
+          SegIter it{next, run.u0, run.u1, i + 1, nullptr};
+          Seg seg;
+          const int64_t lo = max((int64_t)0, run.u0 - at - LD_HDR), hi = min((int64_t)n, run.u1 - at - LD_HDR);
+          bool has = lo < hi;
+          if (has) {
+            seg.it = item_of(a, pl, i, g, len);
+            seg.item = i;
+            seg.j0 = (int)lo;
+            seg.j1 = (int)hi;
+            seg.n = n;
+          } else {
+            has = next_seg(a, pl, it, seg);
+          }
+          s_first->next = it;
+          s_first->seg = seg;
+          s_first->has = has;
         }
-        at += n;
+        at = next;
       }
     if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
-    tc::fence_before();
     __syncthreads();
-    tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // both CTAs: barriers, TMEM
     tc::fence_after();
-    run.item = run.u0 < run.u1 ? (int)s_plan[16] : pl.items;
-    run.start = s_plan[17];
-    run.known = run.u0 < run.u1 ? (int)s_plan[18] : -1;
+    if (s_first->has) {
+      run = s_first->next;
+      run.first = &s_first->seg;
+    } else {
+      run = SegIter{0, 0, 0, pl.items, nullptr};
+    }
   }
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   // all 512 columns are this CTA's: O from 0, the S buffers behind it

@@ -29,13 +29,21 @@ static struct {
   int (*evict)(const jf_kv_pool*, const int32_t*, int32_t, const int32_t*, int32_t, const float*,
                int64_t, int32_t, int32_t, int32_t, const int32_t*, int32_t, int32_t*, float*,
                int32_t*, int32_t*, void*);
+  rows_fn latent_append, latent_read;
+  int (*latent_decode)(const jf_kv_pool*, const int32_t*, int32_t, const int32_t*, int32_t,
+                       const void*, int32_t, float, void*, void*, size_t, void*);
+  int (*latent_prefix)(const jf_kv_pool*, const int32_t*, int32_t, const int32_t*, const int32_t*,
+                       int32_t, const int32_t*, int32_t, const int32_t*, int32_t, const void*,
+                       int32_t, float, void*, void*, size_t, void*);
+  int (*latent_prefill)(const jf_kv_pool*, const int32_t*, const void*, int32_t, int32_t, int32_t,
+                        const void*, const void*, float, int32_t, void*, void*, size_t, void*);
   PyObject *i32, *u8, *f32, *bf16, *f16;      /* torch dtypes */
   PyObject *raw_stream, *get_device;          /* or raw_stream NULL: current_stream */
   PyObject* current_stream;
   PyObject *grad_enabled, *written;           /* torch.is_grad_enabled, autograd's increment_version */
 } G;
 
-static PyObject *s_dtype, *s_is_cuda, *s_contig, *s_ptr, *s_shape, *s_stride, *s_numel, *s_stream, *s_grad;
+static PyObject *s_dtype, *s_is_cuda, *s_contig, *s_ptr, *s_shape, *s_stride, *s_numel, *s_stream, *s_grad, *s_device;
 static PyObject *s_data, *s_page, *s_hkv, *s_dim, *s_group, *s_format;
 
 /* ---- tensors ------------------------------------------------------------- */
@@ -454,13 +462,193 @@ static PyObject* kv8_evict(PyObject* m, PyObject* const* a, Py_ssize_t na) {
                (int32_t)ds[1], dctx, dw, kept, err, stream));
 }
 
+/* ---- the latent cache ---- */
+static int latent_pool(PyObject* p, jf_kv_pool* out) {
+  if (pool_of(p, out)) return -1;
+  /* kernels run on the current device, whatever device the memory is on (a pool on the host is
+   * refused by the other tensors' checks) */
+  PyObject* data = PyObject_GetAttr(p, s_data);
+  if (!data) return -1;
+  PyObject* has = PyObject_CallMethodNoArgs(data, s_device);
+  Py_DECREF(data);
+  if (!has) return -1;
+  const long at = PyLong_AsLong(has);
+  Py_DECREF(has);
+  if (at < 0) return PyErr_Occurred() ? -1 : 0;
+  PyObject* dev = PyObject_CallNoArgs(G.get_device);
+  if (!dev) return -1;
+  const long cur = PyLong_AsLong(dev);
+  Py_DECREF(dev);
+  if (PyErr_Occurred()) return -1;
+  return at != cur ? bad("the pool is on another device than the current one") : 0;
+}
+
+/* pool, page_table, start_pos, row_offsets, latent, k_rot, err, stream */
+static int latent_arg(PyObject* x, const char* name, int64_t width, void** ptr, int64_t* n,
+                      int64_t* stride) {
+  int64_t sh[4], st[4];
+  if (tensor(x, G.bf16, name, 0, "CUDA tensor of dtype torch.bfloat16", ptr)) return -1;
+  const int d = ints_of(x, 0, sh);
+  if (d < 0) return -1;
+  if (d != 2 || sh[1] != width) {
+    PyErr_Format(PyExc_ValueError, "%s must be [rows, %lld]", name, (long long)width);
+    return -1;
+  }
+  if (ints_of(x, 1, st) != 2) return -1;
+  if (sh[0] && st[1] != 1) {
+    PyErr_Format(PyExc_ValueError, "%s: the channels of a row must adjoin", name);
+    return -1;
+  }
+  *n = sh[0];
+  /* the row stride of a single row is whatever a slicing left: it is not used */
+  *stride = sh[0] > 1 ? st[0] : width;
+  return 0;
+}
+
+static PyObject* latent_rows_call(rows_fn fn, PyObject* const* a, Py_ssize_t na) {
+  jf_kv_pool p;
+  void *pt, *start, *off, *lat, *rot, *err = NULL, *stream;
+  int64_t n, nr, ls, rs, sh[4];
+  if (want(8, na) || latent_pool(a[0], &p) || tensor(a[1], G.i32, "page_table", 1, I32_T, &pt) ||
+      tensor(a[2], G.i32, "start_pos", 1, I32_T, &start) ||
+      tensor(a[3], G.i32, "row_offsets", 1, I32_T, &off) ||
+      latent_arg(a[4], "latent", p.head_dim - JF_LATENT_ROT, &lat, &n, &ls) ||
+      latent_arg(a[5], "k_rot", JF_LATENT_ROT, &rot, &nr, &rs) ||
+      (a[6] != Py_None && tensor(a[6], G.i32, "err_flag", 1, I32_T, &err)))
+    return NULL;
+  const int d = ints_of(a[1], 0, sh);
+  if (d < 0 || (d == 0 && bad("page_table must be [requests, pages]"))) return NULL;
+  const int64_t B = d == 2 ? sh[0] : 1, cols = d == 2 ? sh[1] : numel(a[1]);
+  if (n != nr && bad("latent and k_rot must have the same rows")) return NULL;
+  if ((numel(a[2]) != B || numel(a[3]) != B + 1) &&
+      bad("one start_pos per page-table row, and one row offset more"))
+    return NULL;
+  if (stream_of(a[7], &stream)) return NULL;
+  if (fit(cols) || fit(B) || fit(n)) return NULL;
+  CALL(fn(&p, pt, (int32_t)cols, (int32_t)B, start, off, lat, ls, rot, rs, (int32_t)n, err, stream));
+}
+static PyObject* latent_append(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  (void)m;
+  return latent_rows_call(G.latent_append, a, n);
+}
+static PyObject* latent_read(PyObject* m, PyObject* const* a, Py_ssize_t n) {
+  (void)m;
+  return latent_rows_call(G.latent_read, a, n);
+}
+
+/* page_table, context_lens, q, scale, out, workspace, stream: what both decodes end in */
+struct latent_decode_args {
+  void *pt, *ctx, *q, *out, *ws, *stream;
+  int64_t cols, batch, heads, bytes;
+  float scale;
+};
+static int latent_decode_tail(PyObject* const* a, const jf_kv_pool* p, struct latent_decode_args* d) {
+  int64_t sh[4], qs[4], os[4];
+  if (tensor(a[0], G.i32, "page_table", 1, I32_T, &d->pt) ||
+      tensor(a[1], G.i32, "context_lens", 1, I32_T, &d->ctx) ||
+      tensor(a[2], G.bf16, "q", 1, BF16_T, &d->q) || tensor(a[4], G.bf16, "out", 1, BF16_T, &d->out) ||
+      tensor(a[5], G.u8, "workspace", 1, U8_T, &d->ws))
+    return -1;
+  const int nt = ints_of(a[0], 0, sh), nq = ints_of(a[2], 0, qs), no = ints_of(a[4], 0, os);
+  if (nt < 0 || nq < 0 || no < 0) return -1;
+  if ((nt != 2 || nq != 3 || no != 3 || qs[0] != os[0] || qs[1] != os[1] || qs[2] != p->head_dim ||
+       os[2] != p->head_dim - JF_LATENT_ROT || sh[0] != qs[0] || numel(a[1]) != qs[0]) &&
+      bad("shape mismatch"))
+    return -1;
+  d->cols = sh[1];
+  d->batch = qs[0];
+  d->heads = qs[1];
+  d->bytes = numel(a[5]);
+  d->scale = (float)PyFloat_AsDouble(a[3]);
+  if (PyErr_Occurred() || stream_of(a[6], &d->stream)) return -1;
+  return fit(d->cols) || fit(d->batch) || fit(d->heads) ? -1 : 0;
+}
+
+/* pool, page_table, context_lens, q, scale, out, workspace, stream */
+static PyObject* latent_decode(PyObject* m, PyObject* const* a, Py_ssize_t na) {
+  (void)m;
+  jf_kv_pool p;
+  struct latent_decode_args d;
+  if (want(8, na) || latent_pool(a[0], &p) || latent_decode_tail(a + 1, &p, &d)) return NULL;
+  CALL(G.latent_decode(&p, d.pt, (int32_t)d.cols, d.ctx, (int32_t)d.batch, d.q, (int32_t)d.heads,
+                       d.scale, d.out, d.ws, (size_t)d.bytes, d.stream));
+}
+
+/* pool, prefix_table, prefix_lens, group_offsets, then as above */
+static PyObject* latent_prefix(PyObject* m, PyObject* const* a, Py_ssize_t na) {
+  (void)m;
+  jf_kv_pool p;
+  struct latent_decode_args d;
+  void *ppt, *plen;
+  int64_t ps[4];
+  int32_t off[JF_LATENT_MAX_GROUPS + 1];
+  if (want(11, na) || latent_pool(a[0], &p) ||
+      tensor(a[1], G.i32, "prefix_table", 1, I32_T, &ppt) ||
+      tensor(a[2], G.i32, "prefix_lens", 1, I32_T, &plen) || latent_decode_tail(a + 4, &p, &d))
+    return NULL;
+  const int nt = ints_of(a[1], 0, ps);
+  const int64_t groups = numel(a[2]);
+  if (nt < 0 || groups < 0) return NULL;
+  PyObject* seq = PySequence_Fast(a[3], "group_offsets must be a sequence of integers");
+  if (!seq) return NULL;
+  int ok = 1;
+  if (nt != 2 || ps[0] != groups || PySequence_Fast_GET_SIZE(seq) != groups + 1) {
+    bad("one prefix_table row and prefix length per group, and one group offset more");
+    ok = 0;
+  }
+  for (int64_t i = 0; ok && i <= groups && i <= JF_LATENT_MAX_GROUPS; ++i) {
+    PyObject* v = PyNumber_Index(PySequence_Fast_GET_ITEM(seq, i));
+    ok = v && !int_of(v, &off[i]);
+    Py_XDECREF(v);
+  }
+  Py_DECREF(seq);
+  if (!ok || fit(ps[1])) return NULL;
+  CALL(G.latent_prefix(&p, ppt, (int32_t)ps[1], plen, off,
+                       (int32_t)(groups > INT32_MAX ? INT32_MAX : groups), d.pt, (int32_t)d.cols,
+                       d.ctx, (int32_t)d.batch, d.q, (int32_t)d.heads, d.scale, d.out, d.ws,
+                       (size_t)d.bytes, d.stream));
+}
+
+/* pool, page_table_row, q, q_start, w_k, w_v, scale, causal, out, workspace, stream */
+static PyObject* latent_prefill(PyObject* m, PyObject* const* a, Py_ssize_t na) {
+  (void)m;
+  jf_kv_pool p;
+  void *pt, *q, *wk, *wv, *out, *ws, *stream;
+  int64_t qs[4], ks[4], vs[4], os[4];
+  int32_t start;
+  if (want(11, na) || latent_pool(a[0], &p) ||
+      tensor(a[1], G.i32, "page_table_row", 1, I32_T, &pt) ||
+      tensor(a[2], G.bf16, "q", 1, BF16_T, &q) || int_of(a[3], &start) ||
+      tensor(a[4], G.bf16, "w_k", 1, BF16_T, &wk) || tensor(a[5], G.bf16, "w_v", 1, BF16_T, &wv) ||
+      tensor(a[8], G.bf16, "out", 1, BF16_T, &out) || tensor(a[9], G.u8, "workspace", 1, U8_T, &ws))
+    return NULL;
+  const int nq = ints_of(a[2], 0, qs), nk = ints_of(a[4], 0, ks), nv = ints_of(a[5], 0, vs),
+            no = ints_of(a[8], 0, os);
+  if (nq < 0 || nk < 0 || nv < 0 || no < 0) return NULL;
+  if ((nq != 3 || nk != 3 || nv != 3 || no != 3 || qs[2] != 128 + JF_LATENT_ROT || os[0] != qs[0] ||
+       os[1] != qs[1] || os[2] != 128 || ks[0] != qs[1] || ks[1] != 128 ||
+       ks[2] != p.head_dim - JF_LATENT_ROT || vs[0] != ks[0] || vs[1] != ks[1] || vs[2] != ks[2]) &&
+      bad("shape mismatch"))
+    return NULL;
+  if (numel(a[1]) * p.page_size < (int64_t)start + qs[0] &&
+      bad("the page-table row does not hold the chunk"))
+    return NULL;
+  const double scale = PyFloat_AsDouble(a[6]);
+  if (PyErr_Occurred()) return NULL;
+  const int causal = PyObject_IsTrue(a[7]);
+  const int64_t bytes = numel(a[9]);
+  if (causal < 0 || stream_of(a[10], &stream) || fit(qs[0]) || fit(qs[1])) return NULL;
+  CALL(G.latent_prefill(&p, pt, q, start, (int32_t)qs[0], (int32_t)qs[1], wk, wv, (float)scale, causal,
+                        out, ws, (size_t)bytes, stream));
+}
+
 /* ---- set-up: the entry points' addresses, torch's dtypes, stream and autograd functions ---- */
 static PyObject* setup(PyObject* m, PyObject* args) {
   (void)m;
-  unsigned long long f[6];
+  unsigned long long f[11];
   PyObject *dt[5], *raw, *dev, *cur, *grad, *written;
-  if (!PyArg_ParseTuple(args, "(KKKKKK)(OOOOO)OOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5, dt,
-                        dt + 1, dt + 2, dt + 3, dt + 4, &raw, &dev, &cur, &grad, &written))
+  if (!PyArg_ParseTuple(args, "(KKKKKKKKKKK)(OOOOO)OOOOO", f, f + 1, f + 2, f + 3, f + 4, f + 5,
+                        f + 6, f + 7, f + 8, f + 9, f + 10, dt, dt + 1, dt + 2, dt + 3, dt + 4, &raw, &dev, &cur, &grad, &written))
     return NULL;
   G.append = (rows_fn)(uintptr_t)f[0];
   G.read = (rows_fn)(uintptr_t)f[1];
@@ -468,6 +656,11 @@ static PyObject* setup(PyObject* m, PyObject* args) {
   G.decode = (void*)(uintptr_t)f[3];
   G.weights = (void*)(uintptr_t)f[4];
   G.evict = (void*)(uintptr_t)f[5];
+  G.latent_append = (rows_fn)(uintptr_t)f[6];
+  G.latent_read = (rows_fn)(uintptr_t)f[7];
+  G.latent_decode = (void*)(uintptr_t)f[8];
+  G.latent_prefix = (void*)(uintptr_t)f[9];
+  G.latent_prefill = (void*)(uintptr_t)f[10];
   G.i32 = Py_NewRef(dt[0]);
   G.u8 = Py_NewRef(dt[1]);
   G.f32 = Py_NewRef(dt[2]);
@@ -484,6 +677,8 @@ static PyObject* setup(PyObject* m, PyObject* args) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
 static PyMethodDef methods[] = {FAST(kv8_append), FAST(kv8_read), FAST(rope_axes), FAST(decode),
                                 FAST(decode_weights), FAST(kv8_evict),
+                                FAST(latent_append), FAST(latent_read), FAST(latent_decode),
+                                FAST(latent_prefix), FAST(latent_prefill),
                                 {"setup", setup, METH_VARARGS, NULL},
                                 {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_jfcall", NULL, -1, methods,
@@ -496,7 +691,7 @@ PyMODINIT_FUNC PyInit__jfcall(void) {
   } names[] = {{&s_dtype, "dtype"}, {&s_is_cuda, "is_cuda"}, {&s_contig, "is_contiguous"},
                {&s_ptr, "data_ptr"}, {&s_shape, "shape"}, {&s_stride, "stride"},
                {&s_numel, "numel"}, {&s_stream, "cuda_stream"},
-               {&s_grad, "requires_grad"}, {&s_data, "data"},
+               {&s_grad, "requires_grad"}, {&s_device, "get_device"}, {&s_data, "data"},
                {&s_page, "page_size"}, {&s_hkv, "num_kv_heads"}, {&s_dim, "head_dim"},
                {&s_group, "group_size"}, {&s_format, "format"}};
   for (size_t i = 0; i < sizeof names / sizeof names[0]; ++i) {
