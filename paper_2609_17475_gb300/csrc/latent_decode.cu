@@ -37,8 +37,7 @@ constexpr int LD_ROWS = 128;        // rows a pair, 64 each CTA
 constexpr int LD_HDR = 2;           // an item's fixed cost, in tiles
 constexpr int LD_THREADS = 32 * 13;
 constexpr int LD_SOFT = 8;           // softmax warps
-constexpr int LD_SBUF = 4;          // S buffers
-constexpr int LD_AHEAD = 2;         // S of a tile is issued before P V of the tile this many before it
+constexpr int LD_SBUF = 4;          // S buffers: S may be this many tiles ahead of P V
 constexpr float LD_TOP = 16.f;      // the reference maximum moves when a score exceeds it by this (log2)
 
 struct LatentPlan {
@@ -93,6 +92,10 @@ __device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan&
   return n < 0 || n > (int64_t)stride * a.pool.P || n > JF_LATENT_MAX_POSITIONS ? -1 : n;
 }
 
+__device__ __forceinline__ int item_alone(const LatentPlan& pl, int g) {
+  return g >= 0 ? pl.item0[g + 1] - pl.item0[g] == 1 : pl.blocks == 1;
+}
+
 __device__ __forceinline__ int tiles_of(int len) { return len <= 0 ? 0 : (len + LD_T - 1) / LD_T; }
 __device__ __forceinline__ int64_t units_of(int len) {
   const int n = tiles_of(len);
@@ -120,6 +123,7 @@ __device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const Laten
 struct Seg {
   LatentItem it;
   int item, j0, j1, n;   // tiles j0 .. j1 - 1 of the item's n
+  int alone;             // no other item reads these positions
 };
 struct SegIter {
   int64_t start, u0, u1;   // first unit of the item
@@ -148,6 +152,7 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
       seg.j0 = (int)lo;
       seg.j1 = (int)hi;
       seg.n = n;
+      seg.alone = item_alone(pl, g);
       return true;
     }
   }
@@ -276,6 +281,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             seg.j0 = (int)lo;
             seg.j1 = (int)hi;
             seg.n = n;
+            seg.alone = item_alone(pl, g);
           } else {
             has = next_seg(a, pl, it, seg);
           }
@@ -313,52 +319,67 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       auto wait = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
-      int ks = 0, vs = 0, t = 0, nseg = 0;   // stages, tiles and segments of all segments so far
+      // Whichever product has its operands goes next: taken in a fixed order, S behind K that is on its
+      // way from memory held up P V whose V stage is wanted for the next tile.  S buffers bound how
+      // far S may be ahead.
+      int ks = 0, kp = 0, vs = 0, vp = 0;   // next stage of K and of V, and how often their rings went round
+      int t = 0, nseg = 0;                 // tiles and segments of all segments so far
+      auto ready = [&](uint64_t* bar, int phase) {
+        return __all_sync(0xffffffffu, mbar_test(bar, phase)) != 0;
+      };
       while (__all_sync(0xffffffffu, ok && next_seg(a, pl, run, sg))) {
         ok = wait(q_full, nseg);
         ++nseg;
         const int nt = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
-        for (int i = 0; i < nt + LD_AHEAD && ok; ++i) {
-          if (i < nt) {
-            const uint32_t d = tS + ((t + i) % LD_SBUF) * 64;
-            uint64_t q = qd;
-#pragma unroll 1
-            for (int c = 0; c < L::KPT && ok; ++c, ++ks, q += (L::K_BYTES >> 4)) {
-              const int st = ks % L::KS;
-              ok = wait(&k_full[st], ks / L::KS);
-              tc::fence_after();
-              const uint64_t k0 = kd + (uint64_t)(st * (L::K_BYTES >> 4));
-              if (ok) {
+        int qi = 0, qc = 0, pi = 0, pu = 0;   // next S (tile, stage) and P V (tile, stage)
+        uint32_t idle = 0;
+        while (ok && pi < nt) {
+          bool did = false;
+          if (qi < nt && qi - pi < LD_SBUF && ready(&k_full[ks], kp)) {
+            tc::fence_after();
+            const uint64_t q0 = qd + (uint64_t)(qc * (L::K_BYTES >> 4));
+            const uint64_t k0 = kd + (uint64_t)(ks * (L::K_BYTES >> 4));
+            const uint32_t d = tS + ((t + qi) % LD_SBUF) * 64;
 #pragma unroll
-                for (int k = 0; k < 4 * L::KC; ++k) {
-                  const uint32_t at = ((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4;
-                  mma2_ss_if(leader, d, q + at, k0 + at, IDQK, (c > 0 || k > 0) ? 1u : 0u);
-                }
-                tc::commit2_both_if(leader, &k_free[st]);
-              }
+            for (int k = 0; k < 4 * L::KC; ++k) {
+              const uint32_t at = ((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4;
+              mma2_ss_if(leader, d, q0 + at, k0 + at, IDQK, (qc > 0 || k > 0) ? 1u : 0u);
             }
-            if (ok) tc::commit2_both_if(leader, &s_full[(t + i) % LD_SBUF]);
-            if (ok && i == nt - 1) tc::commit2_both_if(leader, q_free);
+            tc::commit2_both_if(leader, &k_free[ks]);
+            if (++ks == L::KS) {
+              ks = 0;
+              ++kp;
+            }
+            if (++qc == L::KPT) {
+              tc::commit2_both_if(leader, &s_full[(t + qi) % LD_SBUF]);
+              if (qi == nt - 1) tc::commit2_both_if(leader, q_free);
+              qc = 0;
+              ++qi;
+            }
+            did = true;
           }
-          const int j = i - LD_AHEAD;   // the segment's tile whose P V is due
-          if (j >= 0 && ok) {
-            ok = wait(p_ready, t + j);
-#pragma unroll 1
-            for (int u = 0; u < L::U && ok; ++u, ++vs) {
-              const int st = vs % L::VS;
-              ok = wait(&v_full[st], vs / L::VS);
-              tc::fence_after();
-              const uint64_t v0 = vd + (uint64_t)(st * (L::V_BYTES >> 4));
-              if (ok) {
+          if (pi < qi && (pu > 0 || ready(p_ready, t + pi)) && ready(&v_full[vs], vp)) {
+            tc::fence_after();
+            const uint64_t v0 = vd + (uint64_t)(vs * (L::V_BYTES >> 4));
+            const uint32_t d = tO + pu * 128;
 #pragma unroll
-                for (int k = 0; k < LD_T / 16; ++k)
-                  mma2_ss_if(leader, tO + u * 128, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
-                             v0 + ((k * 2048) >> 4), IDPV, (j > 0 || k > 0) ? 1u : 0u);
-                tc::commit2_both_if(leader, &v_free[st]);
-              }
+            for (int k = 0; k < LD_T / 16; ++k)
+              mma2_ss_if(leader, d, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
+                         v0 + ((k * 2048) >> 4), IDPV, (pi > 0 || k > 0) ? 1u : 0u);
+            tc::commit2_both_if(leader, &v_free[vs]);
+            if (++vs == L::VS) {
+              vs = 0;
+              ++vp;
             }
-            if (ok) tc::commit2_both_if(leader, pv_done);
+            if (++pu == L::U) {
+              tc::commit2_both_if(leader, pv_done);
+              pu = 0;
+              ++pi;
+            }
+            did = true;
           }
+          idle = did ? 0 : idle + 1;
+          if (idle > (1u << 24)) ok = false;
         }
         t += nt;
       }
@@ -385,12 +406,15 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     // ================= K: this CTA's 64 positions of each tile =================
     if (lane == 0) {
       int ks = 0;
+      const int last = (int)(a.pool.num_pages << a.pool.log2P);   // no row
       while (ok && next_seg(a, pl, run, sg)) {
         int y = half_row(a.pool, sg.it.pt, sg.j0 * LD_T + 64 * (int)rank, sg.it.len, a.status);
         for (int j = sg.j0; j < sg.j1 && ok; ++j) {
           const int row = y;
           if (j + 1 < sg.j1)
             y = half_row(a.pool, sg.it.pt, (j + 1) * LD_T + 64 * (int)rank, sg.it.len, a.status);
+          const int apos = (j + 1) * LD_T + 64 * (int)rank, ahead_rows = sg.it.len - apos;
+          const int ahead = j + 1 < sg.j1 && sg.alone ? y : last;
           for (int c = 0; c < L::KPT; ++c, ++ks) {
             const int st = ks % L::KS;
             if (ks >= L::KS && !mbar_wait_bounded(&k_free[st], (ks / L::KS - 1) & 1)) {
@@ -403,6 +427,13 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 #pragma unroll
             for (int k = 0; k < L::KC; ++k)
               tma_load_2d(dst + k * L::CHUNK, &map, (c * L::KC + k) * 64, row, land);
+            // The ring holds one tile, less than memory's latency calls for: what comes after it is brought
+            // into the L2 cache meanwhile (from where V is read as well), a part with every stage.
+            if (ahead < last) {
+              const int r0 = c * (64 / L::KPT), rows = min(c + 1 == L::KPT ? 64 - r0 : 64 / L::KPT, ahead_rows - r0);
+              if (rows > 0)
+                prefetch_l2(a.pool.base + (int64_t)(ahead + r0) * (R + LAT_ROT), (uint32_t)rows * (R + LAT_ROT) * 2);
+            }
           }
         }
       }

@@ -14,9 +14,10 @@
 // Attention: 256 queries of a head a CTA pair (M = 256, 128 rows each), tiles of 128
 // positions of which each CTA supplies 64 keys (128 expanded channels, and the 64
 // rotated ones straight from the pool) and 64 of the values' channels.  S is taken
-// into three buffers of tensor memory, two tiles ahead of P V; P (bf16) replaces S; O
+// into three buffers of tensor memory, up to two tiles ahead of P V; P (bf16) replaces S; O
 // stays in tensor memory.  Two groups of four softmax warps take the even and the odd
-// tiles, a row a thread.  Weights are 2^(s - m) with a reference m that is 0 unless
+// tiles, a row a thread; the group with an item's last tile takes O out, while the other
+// is at the next item's first.  Weights are 2^(s - m) with a reference m that is 0 unless
 // scores leave [-60, 60] (in powers of two): bf16 and fp32 hold such weights as well as
 // any.  Where a row's reference moves, O is scaled.
 //
@@ -310,7 +311,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
 // Attention
 // ===========================================================================
 constexpr int LA_THREADS = 32 * 12;
-constexpr int LA_KS = 3, LA_VS = 4, LA_SB = 3, LA_AHEAD = 2;
+constexpr int LA_KS = 3, LA_VS = 4, LA_SB = 3;
 struct LaSmem {
   static constexpr int Q_BYTES = 3 * 128 * 128;         // [64-channel chunk][128 rows][128 B]
   static constexpr int K_BYTES = 3 * 64 * 128;          // [64-channel chunk][64 positions][128 B]
@@ -319,9 +320,9 @@ struct LaSmem {
   static constexpr int OFF_V = OFF_K + LA_KS * K_BYTES;
   static constexpr int OFF_OUT = OFF_V + LA_VS * V_BYTES;   // 8 warps x [32 rows][128 B]
   static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
-  static constexpr int OFF_M = OFF_BAR + 512;           // [128] references
-  static constexpr int OFF_L = OFF_M + 128 * 4;         // [2 groups][128] (m, l)
-  static constexpr int TOTAL = OFF_L + 2 * 128 * 8;
+  static constexpr int OFF_M = OFF_BAR + 512;           // [4][128] references after tile t % 4
+  static constexpr int OFF_L = OFF_M + 4 * 128 * 4;     // [4][128] (m, l) of segment s % 4, from one group to the other
+  static constexpr int TOTAL = OFF_L + 4 * 128 * 8;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -415,8 +416,11 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   uint64_t* const q_free = bars + 27;    // products with a segment's Q done
   uint64_t* const s_full = bars + 28;    // [3] S of tile t % 3
   uint64_t* const pv_done = bars + 31;   // [4] P V of tile t % 4
-  uint64_t* const m_bar = bars + 35;     // [2 groups][4 quarters] the group's reference is set
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 43);
+  // [4][4 quarters] the reference after tile t % 4 is set.  (One barrier a group would do but for a
+  // group that takes O out: the other may be two of its tiles on, and a parity then says no for ever.)
+  uint64_t* const m_bar = bars + 35;
+  uint64_t* const o_free = bars + 51;    // on CTA 0: both CTAs have read a segment's O
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 52);
   float* const s_m = reinterpret_cast<float*>(sm + L::OFF_M);
   float2* const s_ml = reinterpret_cast<float2*>(sm + L::OFF_L);
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
@@ -446,12 +450,12 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     for (int i = 0; i < 4; ++i) {
       mbar_init(&p_ready[i], 8);
       mbar_init(&pv_done[i], 1);
-      mbar_init(&m_bar[i], 1);
-      mbar_init(&m_bar[4 + i], 1);
     }
+    for (int i = 0; i < 16; ++i) mbar_init(&m_bar[i], 1);
     mbar_init(q_full, 2);
     mbar_init(q_land, 1);
     mbar_init(q_free, 1);
+    mbar_init(o_free, 8);
     fence_barrier_init();
   }
   if (warp == 0) tc::alloc2(tmem_slot, 512);
@@ -474,72 +478,82 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
       const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
       const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 16, 1024);
+      // S of tile qi (of qleft more of its segment) up to two tiles before P V of tile pi, across the
+      // segments' ends; where a segment's queries are not there yet, P V goes first.
       auto wait = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
-      int t = 0, nseg = 0;   // tiles and segments so far
-      while (__all_sync(0xffffffffu, ok && next_chunk_seg(a, run, sg))) {
-        ok = wait(q_full, nseg);
-        ++nseg;
-        const int nt = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
-        for (int i = 0; i < nt + LA_AHEAD && ok; ++i) {
-          if (i < nt) {
-            const int T = t + i, st = T % LA_KS;
-            ok = wait(&k_full[st], T / LA_KS);
-            tc::fence_after();
-            const uint64_t k0 = kd + (uint64_t)(st * (L::K_BYTES >> 4));
-            const uint32_t d = tS + (T % LA_SB) * 128;
-            if (ok) {
-#pragma unroll
-              for (int k = 0; k < 12; ++k)
-                mma2_ss_if(leader, d, qd + (((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4),
-                           k0 + (((k >> 2) * 64 * 128 + (k & 3) * 32) >> 4), IDQK, k > 0 ? 1u : 0u);
-              tc::commit2_both_if(leader, &k_free[st]);
-              tc::commit2_both_if(leader, &s_full[T % LA_SB]);
-              if (i == nt - 1) tc::commit2_both_if(leader, q_free);
-            }
-          }
-          const int j = i - LA_AHEAD;   // the segment's tile whose P V is due
-          if (j >= 0 && ok) {
-            const int T = t + j, st = T % LA_VS;
-            ok = wait(&p_ready[T & 3], T >> 2) && wait(&v_full[st], T / LA_VS);
-            tc::fence_after();
-            const uint64_t v0 = vd + (uint64_t)(st * (L::V_BYTES >> 4));
-            const uint32_t p = tS + (T % LA_SB) * 128;
-            if (ok) {
-#pragma unroll
-              for (int k = 0; k < LP_T / 16; ++k)
-                tc::mma2_ts_if(leader, tO, p + 8 * k, v0 + ((k * 2048) >> 4), IDPV,
-                               (j > 0 || k > 0) ? 1u : 0u);
-              tc::commit2_both_if(leader, &v_free[st]);
-              tc::commit2_both_if(leader, &pv_done[T & 3]);
-            }
-          }
+      ChunkIter prun = run;
+      int qi = 0, qleft = 0, qseg = 0, pi = 0, pleft = 0, pseg = 0;
+      bool fresh_q = false, fresh_o = false, more = true;   // the segment's first S, its first P V
+      while (ok) {
+        if (qleft == 0 && more) {
+          more = __all_sync(0xffffffffu, next_chunk_seg(a, run, sg)) != 0;
+          qleft = more ? __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0) : 0;
+          fresh_q = true;
         }
-        t += nt;
+        if (qleft > 0 && qi - pi < LA_SB &&
+            (!fresh_q || pi == qi || __all_sync(0xffffffffu, mbar_test(q_full, qseg)))) {
+          const int st = qi % LA_KS;
+          if (fresh_q) ok = wait(q_full, qseg++);
+          ok = ok && wait(&k_full[st], qi / LA_KS);
+          tc::fence_after();
+          const uint64_t k0 = kd + (uint64_t)(st * (L::K_BYTES >> 4));
+          const uint32_t d = tS + (qi % LA_SB) * 128;
+          fresh_q = false;
+          ++qi;
+          --qleft;
+          if (ok) {
+#pragma unroll
+            for (int k = 0; k < 12; ++k)
+              mma2_ss_if(leader, d, qd + (((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4),
+                         k0 + (((k >> 2) * 64 * 128 + (k & 3) * 32) >> 4), IDQK, k > 0 ? 1u : 0u);
+            tc::commit2_both_if(leader, &k_free[st]);
+            tc::commit2_both_if(leader, &s_full[(qi - 1) % LA_SB]);
+            if (qleft == 0) tc::commit2_both_if(leader, q_free);
+          }
+        } else if (pi < qi) {
+          if (pleft == 0) {
+            next_chunk_seg(a, prun, sg);
+            pleft = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
+            fresh_o = true;
+            if (pseg > 0) ok = wait(o_free, pseg - 1);
+            ++pseg;
+          }
+          const int st = pi % LA_VS;
+          ok = ok && wait(&p_ready[pi & 3], pi >> 2) && wait(&v_full[st], pi / LA_VS);
+          tc::fence_after();
+          const uint64_t v0 = vd + (uint64_t)(st * (L::V_BYTES >> 4));
+          const uint32_t p = tS + (pi % LA_SB) * 128;
+          if (ok) {
+#pragma unroll
+            for (int k = 0; k < LP_T / 16; ++k)
+              tc::mma2_ts_if(leader, tO, p + 8 * k, v0 + ((k * 2048) >> 4), IDPV,
+                             (!fresh_o || k > 0) ? 1u : 0u);
+            tc::commit2_both_if(leader, &v_free[st]);
+            tc::commit2_both_if(leader, &pv_done[pi & 3]);
+          }
+          fresh_o = false;
+          ++pi;
+          --pleft;
+        } else {
+          break;   // nothing left
+        }
       }
     } else if (lane == 0) {
-      // ================= CTA 1's arrivals, in the order the issuer takes them =================
-      int t = 0, nseg = 0;
-      while (ok && next_chunk_seg(a, run, sg)) {
-        ok = mbar_wait_bounded(q_land, nseg & 1);
-        if (ok) tc::arrive_cluster(q_full, 0);
-        ++nseg;
-        const int nt = sg.j1 - sg.j0;
-        for (int i = 0; i < nt + LA_AHEAD && ok; ++i) {
-          if (i < nt) {
-            const int T = t + i;
-            ok = mbar_wait_bounded(&k_land[T % LA_KS], (T / LA_KS) & 1);
-            if (ok) tc::arrive_cluster(&k_full[T % LA_KS], 0);
-          }
-          if (i >= LA_AHEAD && ok) {
-            const int T = t + i - LA_AHEAD;
-            ok = mbar_wait_bounded(&v_land[T % LA_VS], (T / LA_VS) & 1);
-            if (ok) tc::arrive_cluster(&v_full[T % LA_VS], 0);
-          }
+      // ================= CTA 1's arrivals =================
+      int t = 0;
+      auto pass_v = [&](int T) {
+        ok = mbar_wait_bounded(&v_land[T % LA_VS], (T / LA_VS) & 1);
+        if (ok) tc::arrive_cluster(&v_full[T % LA_VS], 0);
+      };
+      while (ok && next_chunk_seg(a, run, sg))
+        for (int j = sg.j0; j < sg.j1 && ok; ++j, ++t) {
+          ok = mbar_wait_bounded(&k_land[t % LA_KS], (t / LA_KS) & 1);
+          if (ok) tc::arrive_cluster(&k_full[t % LA_KS], 0);
+          if (ok && t >= 2) pass_v(t - 2);
         }
-        t += nt;
-      }
+      for (int T = max(0, t - 2); T < t && ok; ++T) pass_v(T);
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     __syncwarp();
@@ -602,6 +616,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         for (int c = 0; c < 3; ++c)
           tma_load_3d(smem_u32(sm) + c * 128 * 128, &qmap, c * 64, a.h0 + sg.hl,
                       sg.qt * LP_Q + 128 * (int)rank, land);
+        if (rank == 1) {   // passed on to CTA 0
+          ok = mbar_wait_bounded(q_land, (nseg - 1) & 1);
+          if (ok) tc::arrive_cluster(q_full, 0);
+        }
       }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     }
@@ -613,13 +631,16 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const float sc = a.scale_log2 == 0.f ? 1.f : fabsf(a.scale_log2);
     const uint64_t kk = f32x2(sc, sc);
-    auto all_sync = [] { asm volatile("bar.sync 1, 256;\n" ::: "memory"); };
-    int t0 = 0;   // tiles of the segments before
-    // a wait that gave up ends the work but not the meetings: the others would wait for ever
-    while (next_chunk_seg(a, run, sg)) {
-      const int q = sg.qt * LP_Q + 128 * (int)rank + r;
-      const int limit = a.causal ? min(a.q_start + q, a.n - 1) : a.n - 1;   // last position seen
+    int t0 = 0, seg = 0;   // tiles and number of the segments before
+    // A wait that gave up ends the work but not the meetings: the other group would wait for ever.
+    for (; next_chunk_seg(a, run, sg); ++seg) {
+      const int row0 = sg.qt * LP_Q + 128 * (int)rank + quarter * 32;   // the warp's first query
+      auto limit_of = [&](int q) { return a.causal ? min(a.q_start + q, a.n - 1) : a.n - 1; };
+      const int limit = limit_of(row0 + lane);         // last position seen
+      const int first_limit = limit_of(row0);          // by every query of the warp
       const int nt = sg.j1 - sg.j0;
+      const int32_t* const bad = a.bad + sg.hl * LP_BAD;
+      const int first_bad = a.causal ? bad[128] : 0x7FFFFFFF;
       float m_own = -INFINITY, l = 0.f;   // the reference at this group's last tile
       for (int i = (t0 + group) & 1; i < nt && ok; i += 2) {
         const int T = t0 + i, key0 = (sg.j0 + i) * LP_T;
@@ -627,31 +648,31 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         ok = __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[T % LA_SB], (T / LA_SB) & 1)) != 0;
         if (!ok) break;
         tc::fence_after();
-        // S of 64 positions from column c0 in, those not seen at -inf; a scale below zero negates S, one
-        // of zero makes it zero or NaN
+        // The row's largest score, then the weights: two short loops, each one copy of its code (written
+        // out over the 128 positions, the code came from beyond the instruction caches at every tile).
+        // What the first changes of S -- the sign of a scale below zero, a scale of zero, positions not
+        // seen -- it writes back.
         uint32_t s[2][32];
-        auto scores = [&](int c0) {
+        float x[2] = {-INFINITY, -INFINITY};
+        const bool plain = a.scale_log2 > 0.f && key0 + LP_T - 1 <= first_limit;   // of the whole warp
+#pragma unroll 1
+        for (int c0 = 0; c0 < LP_T; c0 += 64) {
           tc::ld32(tb + c0, s[0]);
           tc::ld32(tb + c0 + 32, s[1]);
           tc::wait_ld();
-          if (!(a.scale_log2 > 0.f)) {
+          if (!plain) {
+            const int seen = limit - key0 - c0;
 #pragma unroll
-            for (int c = 0; c < 64; ++c)
-              s[c >> 5][c & 31] = a.scale_log2 < 0.f ? s[c >> 5][c & 31] ^ 0x80000000u
-                                                     : __float_as_uint(__uint_as_float(s[c >> 5][c & 31]) * 0.f);
+            for (int c = 0; c < 64; ++c) {
+              uint32_t w = s[c >> 5][c & 31];
+              if (a.scale_log2 < 0.f) w ^= 0x80000000u;
+              if (a.scale_log2 == 0.f) w = __float_as_uint(__uint_as_float(w) * 0.f);
+              s[c >> 5][c & 31] = c > seen ? 0xFF800000u : w;
+            }
+            tc::st32(tb + c0, s[0]);
+            tc::st32(tb + c0 + 32, s[1]);
+            tc::wait_st();
           }
-          if (key0 + c0 + 63 > limit) {
-#pragma unroll
-            for (int c = 0; c < 64; ++c)
-              if (key0 + c0 + c > limit) s[c >> 5][c & 31] = 0xFF800000u;
-          }
-        };
-        // the row's largest score, then the weights: two short loops, each one copy of its code (written
-        // out over the 128 positions, the code came from beyond the instruction caches at every tile)
-        float x[2] = {-INFINITY, -INFINITY};
-#pragma unroll 1
-        for (int c0 = 0; c0 < LP_T; c0 += 64) {
-          scores(c0);
 #pragma unroll
           for (int c = 0; c < 32; ++c)
             x[c & 1] = max3(x[c & 1], __uint_as_float(s[c >> 4][(2 * c) & 31]),
@@ -661,10 +682,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         // the reference after the tile before, the other group's
         float m_ref = -INFINITY;   // nothing seen so far
         if (i > 0) {
-          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&m_bar[((T - 1) & 1) * 4 + quarter],
-                                                         ((T - 1) >> 1) & 1)) != 0;
+          ok = __all_sync(0xffffffffu, mbar_wait_bounded(&m_bar[((T - 1) & 3) * 4 + quarter],
+                                                         ((T - 1) >> 2) & 1)) != 0;
           if (!ok) break;
-          m_ref = s_m[r];
+          m_ref = s_m[((T - 1) & 3) * 128 + r];
         }
         const float m_new = m_ref == -INFINITY ? (mt == -INFINITY ? mt : fabsf(mt) <= LP_TOP ? 0.f : mt)
                                                : (mt > m_ref + LP_TOP ? mt : m_ref);
@@ -685,9 +706,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           }
           tc::wait_st();
         }
-        s_m[r] = m_new;
+        s_m[(T & 3) * 128 + r] = m_new;
         __syncwarp();
-        if (lane == 0) mbar_arrive(&m_bar[group * 4 + quarter]);
+        if (lane == 0) mbar_arrive(&m_bar[(T & 3) * 4 + quarter]);
         if (m_new != m_own) {
           if (m_own != -INFINITY) l *= fast_exp2(m_own - m_new);
           m_own = m_new;
@@ -697,7 +718,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         uint64_t sum = f32x2(0.f, 0.f);
 #pragma unroll 1
         for (int c0 = 0; c0 < LP_T; c0 += 64) {
-          scores(c0);
+          tc::ld32(tb + c0, s[0]);
+          tc::ld32(tb + c0 + 32, s[1]);
+          tc::wait_ld();
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t p[16];
@@ -722,73 +745,72 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         if (lane == 0) tc::arrive_cluster(&p_ready[T & 3], 0);
       }
       t0 += nt;
-      s_ml[group * 128 + r] = make_float2(m_own, l);
       const int last = t0 - 1;
-      if (ok) ok = mbar_wait_bounded(&pv_done[last & 3], (last >> 2) & 1);
-      const bool done = __all_sync(0xffffffffu, ok) != 0;
-      all_sync();   // every softmax thread's (m, l)
-      tc::fence_after();
-      const float m = s_m[r];   // after the last tile
-      float lsum = 0.f;
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const float2 x = s_ml[g * 128 + r];
-        // no reference: a sum of zero, or NaN where every score was
-        lsum = x.x == -INFINITY ? lsum + x.y : fmaf(x.y, fast_exp2(x.x - m), lsum);
+      // The group with the last tile, whose reference is the row's, goes on to O; the other leaves it its
+      // sum.  (Barriers and places of four segments in turn: neither group gets that far ahead.)
+      float2* const ml = s_ml + (seg & 3) * 128 + r;
+      if (group != (last & 1)) {
+        *ml = make_float2(m_own, l);
+        asm volatile("bar.arrive %0, 256;\n" ::"r"(1 + (seg & 3)) : "memory");
+        continue;
       }
+      asm volatile("bar.sync %0, 256;\n" ::"r"(1 + (seg & 3)) : "memory");
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[last & 3], (last >> 2) & 1)) != 0;
+      if (!ok) continue;
+      tc::fence_after();
+      const float2 other = *ml;
+      // no reference: a sum of zero, or NaN where every score was
+      const float lsum = other.x == -INFINITY ? l + other.y : fmaf(other.y, fast_exp2(other.x - m_own), l);
       const bool whole = nt == sg.n;
       const int64_t prow = ((int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * LP_Q) + 128 * rank;
-      if (!whole && group == 0 && done) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m, lsum);
-      const float inv = lsum != 0.f ? 1.f / lsum : 0.f;
-      const int32_t* const bad = a.bad + sg.hl * LP_BAD;
-      const bool any_bad = a.causal && bad[128] <= limit;
-      // each group half of the columns; 128-byte pieces of a warp's 32 rows go through shared memory,
-      // so that whole lines are written
+      if (!whole) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m_own, lsum);
+      const float inv = whole ? (lsum != 0.f ? 1.f / lsum : 0.f) : 1.f;
+      // 128-byte pieces of a warp's 32 rows go through shared memory, so that whole lines are written
       const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
+      uint8_t* const to = whole ? reinterpret_cast<uint8_t*>(a.out + ((int64_t)row0 * a.H + a.h0 + sg.hl) * 128)
+                                : reinterpret_cast<uint8_t*>(a.o + (prow + quarter * 32) * 128);
+      const int64_t pitch = whole ? (int64_t)a.H * 256 : 512;
 #pragma unroll 1
-      for (int part = 0; part < (whole ? 1 : 2); ++part) {
+      for (int half = 0; half < 2; ++half) {
         uint32_t o[2][32];
-        tc::ld32(tO + group * 64 + part * 32 + lane_off, o[0]);
-        if (whole) tc::ld32(tO + group * 64 + 32 + lane_off, o[1]);
+        tc::ld32(tO + 64 * half + lane_off, o[0]);
+        tc::ld32(tO + 64 * half + 32 + lane_off, o[1]);
         tc::wait_ld();
-        if (any_bad) {
-          for (int c = 0; c < (whole ? 64 : 32); ++c)
-            if (bad[group * 64 + part * 32 + c] <= limit) {
+        if (half == 1) {   // the next segment's products may begin
+          tc::fence_before();
+          __syncwarp();
+          if (lane == 0) tc::arrive_cluster(o_free, 0);
+        }
+        if (first_bad <= limit) {   // a value that is not finite among those seen
 #pragma unroll
-              for (int e = 0; e < 64; ++e)
-                if (e == c) o[e >> 5][e & 31] = 0x7FC00000u;
+          for (int c = 0; c < 64; ++c)
+            if (bad[64 * half + c] <= limit) o[c >> 5][c & 31] = 0x7FC00000u;
+        }
+#pragma unroll 1
+        for (int part = 0; part < (whole ? 1 : 2); ++part) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            uint32_t w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const int c = 8 * k + 2 * u;
+              w[u] = whole ? pack_bf16x2(__uint_as_float(o[c >> 5][c & 31]) * inv,
+                                         __uint_as_float(o[c >> 5][(c + 1) & 31]) * inv)
+                           : (part == 0 ? o[0][4 * k + u] : o[1][4 * k + u]);
             }
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          uint32_t w[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int c = 8 * k + 2 * u;
-            w[u] = whole ? pack_bf16x2(__uint_as_float(o[c >> 5][c & 31]) * inv,
-                                       __uint_as_float(o[c >> 5][(c + 1) & 31]) * inv)
-                         : o[0][4 * k + u];
+            sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
           }
-          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
-        }
-        __syncwarp();
+          __syncwarp();
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int row = u * 4 + (lane >> 3), piece = lane & 7;
-          const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
-          const int rr = quarter * 32 + row, qq = sg.qt * LP_Q + 128 * (int)rank + rr;
-          if (qq < a.C && done) {
-            if (whole)
-              *reinterpret_cast<uint4*>(a.out + ((int64_t)qq * a.H + a.h0 + sg.hl) * 128 + group * 64 +
-                                        piece * 8) = v;
-            else
-              *reinterpret_cast<uint4*>(a.o + (prow + rr) * 128 + group * 64 + part * 32 + piece * 4) = v;
+          for (int u = 0; u < 8; ++u) {
+            const int row = u * 4 + (lane >> 3), piece = lane & 7;
+            const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
+            if (row0 + row < a.C)
+              *reinterpret_cast<uint4*>(to + row * pitch + (whole ? half : 2 * half + part) * 128 + piece * 16) = v;
           }
+          __syncwarp();
         }
-        __syncwarp();
       }
-      tc::fence_before();
-      all_sync();   // s_m and s_ml read, before a warp goes on to write them
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   }

@@ -358,6 +358,21 @@ def test_prefill(R, H, P, q_start, C, causal):
     check_prefill(out, q, O.gather(pool, table[0], n), q_start, w, T.SCALE, causal)
 
 
+@pytest.mark.parametrize("R,H,q_start,C,causal", [(256, 128, 0, 1, True), (256, 128, 0, 130, True), (512, 128, 300, 100, True),
+                                                  (256, 64, 0, 1100, True), (256, 100, 120, 400, False)])
+def test_prefill_of_many_heads(R, H, q_start, C, causal):
+    """Several items for every pair of CTAs, one after the other, of one tile and of more."""
+    rng = np.random.default_rng(R + H + C)
+    n = q_start + C
+    table, pool = T.filled(rng, R, 64, [n])
+    q, w = T.bf16(rng.standard_normal((C, H, 192))), weights(rng, H, R)
+    out, st = run_prefill(table[0], pool, q, q_start, w, T.SCALE, causal)
+    assert st == 0
+    kv = O.gather(pool, table[0], n)
+    for h in range(0, H, 3):
+        check_prefill(out[:, h:h + 1], q[:, h:h + 1], kv, q_start, w[:, h:h + 1], T.SCALE, causal)
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
 def test_prefill_scales(scale):
     rng = np.random.default_rng(31)
