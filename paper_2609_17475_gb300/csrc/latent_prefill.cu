@@ -479,7 +479,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
       const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 16, 1024);
       // S of tile qi (of qleft more of its segment) up to two tiles before P V of tile pi, across the
-      // segments' ends; where a segment's queries are not there yet, P V goes first.
+      // segments' ends; but a segment's last P V go first as soon as they can, since O's way out waits
+      // for them.
       auto wait = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
@@ -492,8 +493,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           qleft = more ? __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0) : 0;
           fresh_q = true;
         }
+        const bool last_pv = pi < qi && (fresh_q || qseg > pseg) && pleft > 0;   // S is a segment ahead
         if (qleft > 0 && qi - pi < LA_SB &&
-            (!fresh_q || pi == qi || __all_sync(0xffffffffu, mbar_test(q_full, qseg)))) {
+            (!last_pv || (!__all_sync(0xffffffffu, mbar_test(&p_ready[pi & 3], pi >> 2)) &&
+                          (!fresh_q || __all_sync(0xffffffffu, mbar_test(q_full, qseg)))))) {
           const int st = qi % LA_KS;
           if (fresh_q) ok = wait(q_full, qseg++);
           ok = ok && wait(&k_full[st], qi / LA_KS);
@@ -770,9 +773,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       uint8_t* const to = whole ? reinterpret_cast<uint8_t*>(a.out + ((int64_t)row0 * a.H + a.h0 + sg.hl) * 128)
                                 : reinterpret_cast<uint8_t*>(a.o + (prow + quarter * 32) * 128);
       const int64_t pitch = whole ? (int64_t)a.H * 256 : 512;
-#pragma unroll 1
-      for (int half = 0; half < 2; ++half) {
-        uint32_t o[2][32];
+      uint32_t o[2][32], w[2][32];
+      auto read = [&](int half) {   // 64 columns
         tc::ld32(tO + 64 * half + lane_off, o[0]);
         tc::ld32(tO + 64 * half + 32 + lane_off, o[1]);
         tc::wait_ld();
@@ -786,29 +788,37 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           for (int c = 0; c < 64; ++c)
             if (bad[64 * half + c] <= limit) o[c >> 5][c & 31] = 0x7FC00000u;
         }
+      };
+      auto out = [&](const uint32_t (&x)[32], int part) {   // 32 words a row
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int row = u * 4 + (lane >> 3), piece = lane & 7;
+          const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
+          if (row0 + row < a.C) *reinterpret_cast<uint4*>(to + row * pitch + part * 128 + piece * 16) = v;
+        }
+        __syncwarp();
+      };
+      if (whole) {   // all of O into registers first
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          read(half);
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            w[half][c] = pack_bf16x2(__uint_as_float(o[c >> 4][(2 * c) & 31]) * inv,
+                                     __uint_as_float(o[c >> 4][(2 * c + 1) & 31]) * inv);
+        }
+        out(w[0], 0);
+        out(w[1], 1);
+      } else {
 #pragma unroll 1
-        for (int part = 0; part < (whole ? 1 : 2); ++part) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            uint32_t w[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const int c = 8 * k + 2 * u;
-              w[u] = whole ? pack_bf16x2(__uint_as_float(o[c >> 5][c & 31]) * inv,
-                                         __uint_as_float(o[c >> 5][(c + 1) & 31]) * inv)
-                           : (part == 0 ? o[0][4 * k + u] : o[1][4 * k + u]);
-            }
-            sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
-          }
-          __syncwarp();
-#pragma unroll
-          for (int u = 0; u < 8; ++u) {
-            const int row = u * 4 + (lane >> 3), piece = lane & 7;
-            const uint4 v = lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
-            if (row0 + row < a.C)
-              *reinterpret_cast<uint4*>(to + row * pitch + (whole ? half : 2 * half + part) * 128 + piece * 16) = v;
-          }
-          __syncwarp();
+        for (int half = 0; half < 2; ++half) {
+          read(half);
+          out(o[0], 2 * half);
+          out(o[1], 2 * half + 1);
         }
       }
     }
