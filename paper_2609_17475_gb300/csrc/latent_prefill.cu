@@ -263,27 +263,36 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
           __syncwarp();
           if (lane == 0) tc::arrive_cluster(&d_free[t & 1], 0);
         }
+        uint32_t w[32], top = 0u;   // the values, and the largest magnitudes' bits of both halves
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          uint32_t w[4];
+        for (int c = 0; c < 32; ++c) {
+          w[c] = pack_bf16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]), __uint_as_float(x[c >> 4][(2 * c + 1) & 31]));
+          top = __vmaxu2(top, w[c] & 0x7FFF7FFFu);
+        }
+        if (pos0 + 31 >= a.n) {   // positions past the last
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int c = 8 * k + 2 * u;
-            w[u] = pack_bf16x2(__uint_as_float(x[c >> 5][c & 31]), __uint_as_float(x[c >> 5][(c + 1) & 31]));
-            if (pos >= a.n) w[u] = 0u;
-            if (pos >= apart) {
-              const bool lo = (w[u] & 0x7F80u) == 0x7F80u, hi = (w[u] & 0x7F800000u) == 0x7F800000u;
-              if (lo || hi) {
-                int32_t* const bad = a.bad + hl * LP_BAD;
-                if (lo) atomicMin(bad + c0 + c, pos);
-                if (hi) atomicMin(bad + c0 + c + 1, pos);
-                atomicMin(bad + 128, pos);
-                w[u] &= (lo ? 0xFFFF0000u : 0xFFFFFFFFu) & (hi ? 0xFFFFu : 0xFFFFFFFFu);
-              }
+          for (int c = 0; c < 32; ++c)
+            if (pos >= a.n) w[c] = 0u;
+          if (pos >= a.n) top = 0u;
+        }
+        if (pos >= apart && max(top & 0xFFFFu, top >> 16) >= 0x7F80u) {
+          int32_t* const bad = a.bad + hl * LP_BAD;
+          atomicMin(bad + 128, pos);
+#pragma unroll
+          for (int c = 0; c < 32; ++c) {
+            if ((w[c] & 0x7F80u) == 0x7F80u) {
+              atomicMin(bad + c0 + 2 * c, pos);
+              w[c] &= 0xFFFF0000u;
+            }
+            if ((w[c] & 0x7F800000u) == 0x7F800000u) {
+              atomicMin(bad + c0 + 2 * c + 1, pos);
+              w[c] &= 0xFFFFu;
             }
           }
-          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[0], w[1], w[2], w[3]);
         }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          sts128(tr + lane * 128 + ((k ^ (lane & 7)) << 4), w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
         __syncwarp();
         uint16_t* const to = dst + ((int64_t)hl * a.n_pad + pos0) * 128 + c0;
 #pragma unroll
