@@ -782,7 +782,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       uint8_t* const to = whole ? reinterpret_cast<uint8_t*>(a.out + ((int64_t)row0 * a.H + a.h0 + sg.hl) * 128)
                                 : reinterpret_cast<uint8_t*>(a.o + (prow + quarter * 32) * 128);
       const int64_t pitch = whole ? (int64_t)a.H * 256 : 512;
-      uint32_t o[2][32], w[2][32];
+      uint32_t o[2][32], w[1][32];
       auto read = [&](int half) {   // 64 columns
         tc::ld32(tO + 64 * half + lane_off, o[0]);
         tc::ld32(tO + 64 * half + 32 + lane_off, o[1]);
@@ -811,17 +811,16 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         }
         __syncwarp();
       };
-      if (whole) {   // all of O into registers first
-#pragma unroll
+      if (whole) {
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
           read(half);
 #pragma unroll
           for (int c = 0; c < 32; ++c)
-            w[half][c] = pack_bf16x2(__uint_as_float(o[c >> 4][(2 * c) & 31]) * inv,
-                                     __uint_as_float(o[c >> 4][(2 * c + 1) & 31]) * inv);
+            w[0][c] = pack_bf16x2(__uint_as_float(o[c >> 4][(2 * c) & 31]) * inv,
+                                  __uint_as_float(o[c >> 4][(2 * c + 1) & 31]) * inv);
+          out(w[0], half);
         }
-        out(w[0], 0);
-        out(w[1], 1);
       } else {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
