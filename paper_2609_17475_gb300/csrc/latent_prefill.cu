@@ -14,12 +14,14 @@
 // Attention: 256 queries of a head a CTA pair (M = 256, 128 rows each), tiles of 128
 // positions of which each CTA supplies 64 keys (128 expanded channels, and the 64
 // rotated ones straight from the pool) and 64 of the values' channels.  S is taken
-// into three buffers of tensor memory, up to two tiles ahead of P V; P (bf16) replaces S; O
+// into three buffers of tensor memory, up to two tiles ahead of P V; P replaces S; O
 // stays in tensor memory.  Two groups of four softmax warps take the even and the odd
 // tiles, a row a thread; the group with an item's last tile takes O out, while the other
-// is at the next item's first.  Weights are 2^(s - m) with a reference m that is 0 unless
-// scores leave [-60, 60] (in powers of two): bf16 and fp32 hold such weights as well as
-// any.  Where a row's reference moves, O is scaled.
+// is at the next item's first.  Keys and queries multiply as bf16; values and weights as
+// fp16, whose three more bits they need: in bf16 the two roundings weighed as much as the
+// output's own (a whole prompt of 4,095 off by 0.0026 of its norm for the 0.0017 of
+// rounding exact values).  Weights are 2^(s - m); a row's reference m is set so that its
+// largest weight is 2^10 and moves, O's row with it, when a weight passes 2^15.
 //
 // Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
 // cut into one run of equal length per pair; a cut item's parts are joined by
@@ -33,14 +35,15 @@ namespace jfkv {
 constexpr int LP_T = 128;            // positions a tile
 constexpr int LP_Q = 256;            // queries a pair
 constexpr int LP_HDR = 2;            // an item's fixed cost, in tiles
-constexpr float LP_TOP = 60.f;       // how far scores may be from the reference (log2)
+constexpr float LP_SET = 10.f;       // a reference puts the largest weight at 2^10;
+constexpr float LP_TOP = 15.f;       // it moves when one passes 2^15 (fp16 ends below 2^16)
 constexpr int LP_BAD = 132;          // first positions of values that are not finite: [128], their least
 
 struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
   LatentPool pool;
   const int32_t* pt;
-  uint16_t* k;                       // [heads][n_pad][128]
-  uint16_t* v;
+  uint16_t* k;                       // [heads][n_pad][128] bf16
+  uint16_t* v;                       // the same, fp16
   uint16_t* out;                     // [C][H][128]
   int32_t* bad;                      // [heads][LP_BAD]
   int32_t* status;
@@ -264,10 +267,16 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
           if (lane == 0) tc::arrive_cluster(&d_free[t & 1], 0);
         }
         uint32_t w[32], top = 0u;   // the values, and the largest magnitudes' bits of both halves
+        if (kind) {
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          w[c] = pack_bf16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]), __uint_as_float(x[c >> 4][(2 * c + 1) & 31]));
-          top = __vmaxu2(top, w[c] & 0x7FFF7FFFu);
+          for (int c = 0; c < 32; ++c) {
+            w[c] = pack_f16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]), __uint_as_float(x[c >> 4][(2 * c + 1) & 31]));
+            top = __vmaxu2(top, w[c] & 0x7FFF7FFFu);
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; ++c)
+            w[c] = pack_bf16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]), __uint_as_float(x[c >> 4][(2 * c + 1) & 31]));
         }
         if (pos0 + 31 >= a.n) {   // positions past the last
 #pragma unroll
@@ -275,18 +284,17 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
             if (pos >= a.n) w[c] = 0u;
           if (pos >= a.n) top = 0u;
         }
-        if (pos >= apart && max(top & 0xFFFFu, top >> 16) >= 0x7F80u) {
+        if (max(top & 0xFFFFu, top >> 16) >= 0x7C00u) {   // a value that is not finite, or past fp16
           int32_t* const bad = a.bad + hl * LP_BAD;
-          atomicMin(bad + 128, pos);
+          if (pos >= apart) atomicMin(bad + 128, pos);
 #pragma unroll
-          for (int c = 0; c < 32; ++c) {
-            if ((w[c] & 0x7F80u) == 0x7F80u) {
-              atomicMin(bad + c0 + 2 * c, pos);
-              w[c] &= 0xFFFF0000u;
-            }
-            if ((w[c] & 0x7F800000u) == 0x7F800000u) {
-              atomicMin(bad + c0 + 2 * c + 1, pos);
-              w[c] &= 0xFFFFu;
+          for (int c = 0; c < 64; ++c) {
+            const uint32_t half = c & 1 ? w[c >> 1] >> 16 : w[c >> 1];
+            if ((half & 0x7C00u) != 0x7C00u) continue;
+            if (fabsf(__uint_as_float(x[c >> 5][c & 31])) < INFINITY) flag_error(a.status, JF_DEV_ERR_RANGE);
+            if (pos >= apart) {
+              atomicMin(bad + c0 + c, pos);
+              w[c >> 1] &= c & 1 ? 0xFFFFu : 0xFFFF0000u;
             }
           }
         }
@@ -408,7 +416,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
                       const __grid_constant__ LatentChunk a) {
   using L = LaSmem;
   constexpr uint32_t IDQK = idesc_bf16(256, LP_T, 0);
-  constexpr uint32_t IDPV = idesc_bf16(256, 128, 1);
+  constexpr uint32_t IDPV = tc::idesc_f16_f32(256, 128, 0, 1);
   extern __shared__ __align__(1024) uint8_t sm[];
   uint64_t* const bars = reinterpret_cast<uint64_t*>(sm + L::OFF_BAR);
   // on CTA 0, where the pair's MMAs are issued:
@@ -699,8 +707,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           if (!ok) break;
           m_ref = s_m[((T - 1) & 3) * 128 + r];
         }
-        const float m_new = m_ref == -INFINITY ? (mt == -INFINITY ? mt : fabsf(mt) <= LP_TOP ? 0.f : mt)
-                                               : (mt > m_ref + LP_TOP ? mt : m_ref);
+        const float m_new = mt > m_ref + LP_TOP || m_ref == -INFINITY ? mt - LP_SET : m_ref;
         const bool moves = m_ref != -INFINITY && m_new != m_ref;
         if (__any_sync(0xffffffffu, moves)) {   // O's rows with it
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(T - 1) & 3], ((T - 1) >> 2) & 1)) != 0;
@@ -741,9 +748,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
               float d0, d1;
               unpack_f32x2(fma_f32x2(f32x2(__uint_as_float(s[h][2 * c]), __uint_as_float(s[h][2 * c + 1])),
                                      kk, cc), d0, d1);
-              p[c] = pack_bf16x2(fast_exp2(d0), fast_exp2(d1));
-              // of the rounded weights, so that they add up to one
-              sum = add_f32x2(sum, f32x2(bf16lo_to_f32(p[c]), bf16hi_to_f32(p[c])));
+              const float p0 = fast_exp2(d0), p1 = fast_exp2(d1);
+              p[c] = pack_f16x2(p0, p1);
+              sum = add_f32x2(sum, f32x2(p0, p1));
             }
             st16(tb + c0 / 2 + 16 * h, p);   // over scores already read
           }

@@ -331,17 +331,20 @@ def run_prefill(table_row, pool, q, q_start, w, scale, causal, ws=None):
 
 def check_prefill(out, q, kv, q_start, w, scale, causal, rows=None):
     ref, mass, reach = O.prefill(q, kv, q_start, w[0], w[1], scale, causal)
-    # scores: keys off by 2^-8 of each channel and sums of 192 and R products in fp32; values by 2^-8 of each, weights by
-    # 2^-8 each over a sum as much off
+    # scores: keys off by 2^-8 of each channel and sums of 192 and R products in fp32 (a sum that cuts off:
+    # 2^-23 an addition); values and weights by 2^-11 of each, or, below 2^-14 of a value and 2^-24 of the
+    # largest weight, by 2^-25 and 2^-34 of it
     width = 192 + kv.shape[1]
     err = abs(scale) * reach[..., None] * (2.0 ** -8 + width * 2.0 ** -23)
-    bound = np.abs(ref) * 2.0 ** -8 + mass * (3 * 2.0 ** -8 + 2.0 ** -19 + np.expm1(2 * err)) + 2.0 ** -130
+    top = max(np.abs(O.expand(kv, w[0][h], w[1][h])[1]).max() for h in range(q.shape[1]))
+    bound = (np.abs(ref) * 2.0 ** -8 + mass * (2.0 ** -10 + 2.0 ** -19 + np.expm1(2 * err)) + 2.0 ** -25
+             + len(kv) * top * 2.0 ** -34)
     got = f64(out)
     pick = slice(None) if rows is None else rows
     bad = ~(np.abs(got - ref) <= bound)[pick]
     assert not bad.any(), (bad.sum(), np.abs(got - ref)[pick].max(), np.argwhere(bad)[:3])
     # roundings of either sign average out: the mean error stays below half a step of a typical term
-    assert np.abs(got - ref)[pick].mean() <= 2.0 ** -8 * mass[pick].mean()
+    assert np.abs(got - ref)[pick].mean() <= 2.0 ** -8 * mass[pick].mean() + 2.0 ** -25
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -410,6 +413,29 @@ def test_a_value_that_is_not_finite_reaches_the_queries_that_see_it_alone(what):
     out, st = run_prefill(table[0], pool, q, q_start, w, T.SCALE, True)
     assert st == 0 and torch.isnan(out[at - q_start:]).all()
     check_prefill(out, q, kv, q_start, w, T.SCALE, True, rows=slice(0, at - q_start))
+
+
+def test_a_value_past_fp16_is_flagged():
+    rng = np.random.default_rng(36)
+    table, pool = T.filled(rng, 256, 64, [200])
+    q, w = T.bf16(rng.standard_normal((150, 3, 192))), weights(rng, 3, 256)
+    w[1, 1] *= 2.0 ** 20
+    out, st = run_prefill(table[0], pool, q, 50, w, T.SCALE, True)
+    assert st == 16                                     # JF_DEV_ERR_RANGE
+    keep = [0, 2]
+    check_prefill(out[:, keep], q[:, keep], O.gather(pool, table[0], 200), 50, w[:, keep], T.SCALE, True)
+
+
+@pytest.mark.parametrize("power", [-30, 13])
+def test_small_and_large_values(power):
+    """Values near either end of fp16: products of 2^-30 lose all but what 2^-25 leaves of them."""
+    rng = np.random.default_rng(37)
+    table, pool = T.filled(rng, 256, 64, [200])
+    q, w = T.bf16(rng.standard_normal((150, 2, 192))), weights(rng, 2, 256)
+    w[1] *= 2.0 ** power
+    out, st = run_prefill(table[0], pool, q, 50, w, T.SCALE, True)
+    assert st == 0
+    check_prefill(out, q, O.gather(pool, table[0], 200), 50, w, T.SCALE, True)
 
 
 def test_a_query_of_nan_stays_alone():
