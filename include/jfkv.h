@@ -752,7 +752,7 @@ size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int
  * JF_LATENT_MAX_POSITIONS.
  * A page outside the pool sets JF_DEV_ERR_PAGE_ID; the outputs that attend its
  * positions are not reliable.  A value among the chunk's own positions that is not
- * finite makes that channel NaN for the queries that see it, and for no other.
+ * finite makes the head's output NaN for the queries that see it, and for no other.
  * Numerics: products and sums in fp32.  The expanded keys are rounded to bf16 (2^-8
  * of each), the expanded values and the weights to fp16 (2^-11); a value past
  * 65504 sets JF_DEV_ERR_RANGE and counts as infinite.

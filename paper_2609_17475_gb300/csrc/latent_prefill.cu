@@ -8,7 +8,7 @@
 // the products of a tile run while the tile before goes out.  Positions past the last
 // are written as zeros, so that a weight of zero finds no NaN there.  A value of the
 // chunk's own positions that is not finite would reach queries before it the same way
-// (0 * NaN): it is written as zero and its position noted for its channel, and the
+// (0 * NaN): it is written as zero and the first such position of each 32 noted, and the
 // queries that see it get NaN at the end.
 //
 // Attention: 256 queries of a head a CTA pair (M = 256, 128 rows each), tiles of 128
@@ -37,7 +37,7 @@ constexpr int LP_Q = 256;            // queries a pair
 constexpr int LP_HDR = 2;            // an item's fixed cost, in tiles
 constexpr float LP_SET = 10.f;       // a reference puts the largest weight at 2^10;
 constexpr float LP_TOP = 15.f;       // it moves when one passes 2^15 (fp16 ends below 2^16)
-constexpr int LP_BAD = 132;          // first positions of values that are not finite: [128], their least
+constexpr int LP_NONE = 0x7FFFFFFF;  // no position
 
 struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
   LatentPool pool;
@@ -45,7 +45,7 @@ struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
   uint16_t* k;                       // [heads][n_pad][128] bf16
   uint16_t* v;                       // the same, fp16
   uint16_t* out;                     // [C][H][128]
-  int32_t* bad;                      // [heads][LP_BAD]
+  int32_t* bad;                      // [heads][n_pad / 32]: first position of a value that is not finite
   int32_t* status;
   float* ml;                         // [2 * pairs * 256][2]
   float* o;                          // [2 * pairs * 256][128]
@@ -246,7 +246,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
     const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
     uint16_t* const dst = kind ? a.v : a.k;
     // values of positions that not every query of the chunk sees
-    const int apart = kind && a.causal ? a.q_start + 1 : 0x7FFFFFFF;
+    const int apart = kind && a.causal ? a.q_start + 1 : LP_NONE;
     for (int t = 0; t < count; ++t, advance()) {
       const int pos0 = pt * 256 + 128 * (int)rank + quarter * 32;
       const int pos = pos0 + lane;
@@ -255,6 +255,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
         break;
       }
       tc::fence_after();
+      int first = LP_NONE;
 #pragma unroll 1
       for (int c0 = 0; c0 < 128; c0 += 64) {
         uint32_t x[2][32];
@@ -285,17 +286,13 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
           if (pos >= a.n) top = 0u;
         }
         if (max(top & 0xFFFFu, top >> 16) >= 0x7C00u) {   // a value that is not finite, or past fp16
-          int32_t* const bad = a.bad + hl * LP_BAD;
-          if (pos >= apart) atomicMin(bad + 128, pos);
+          if (pos >= apart) first = pos;
 #pragma unroll
           for (int c = 0; c < 64; ++c) {
             const uint32_t half = c & 1 ? w[c >> 1] >> 16 : w[c >> 1];
             if ((half & 0x7C00u) != 0x7C00u) continue;
             if (fabsf(__uint_as_float(x[c >> 5][c & 31])) < INFINITY) flag_error(a.status, JF_DEV_ERR_RANGE);
-            if (pos >= apart) {
-              atomicMin(bad + c0 + c, pos);
-              w[c >> 1] &= c & 1 ? 0xFFFFu : 0xFFFF0000u;
-            }
+            if (pos >= apart) w[c >> 1] &= c & 1 ? 0xFFFFu : 0xFFFF0000u;
           }
         }
 #pragma unroll
@@ -310,6 +307,10 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
               lds128(tr + row * 128 + ((piece ^ (row & 7)) << 4));
         }
         __syncwarp();
+      }
+      if (kind) {
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (lane == 0) a.bad[((int64_t)hl * a.n_pad + pos0) >> 5] = first;
       }
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -659,8 +660,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       const int limit = limit_of(row0 + lane);         // last position seen
       const int first_limit = limit_of(row0);          // by every query of the warp
       const int nt = sg.j1 - sg.j0;
-      const int32_t* const bad = a.bad + sg.hl * LP_BAD;
-      const int first_bad = a.causal ? bad[128] : 0x7FFFFFFF;
+      int first_bad = LP_NONE;   // of the values that the warp's queries see and not all of the chunk's
+      if (a.causal)
+        for (int b = ((a.q_start + 1) >> 5) + lane; b <= (limit_of(row0 + 31) >> 5); b += 32)
+          first_bad = min(first_bad, a.bad[(((int64_t)sg.hl * a.n_pad) >> 5) + b]);
       float m_own = -INFINITY, l = 0.f;   // the reference at this group's last tile
       for (int i = (t0 + group) & 1; i < nt && ok; i += 2) {
         const int T = t0 + i, key0 = (sg.j0 + i) * LP_T;
@@ -782,8 +785,10 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       const float lsum = other.x == -INFINITY ? l + other.y : fmaf(other.y, fast_exp2(other.x - m_own), l);
       const bool whole = nt == sg.n;
       const int64_t prow = ((int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * LP_Q) + 128 * rank;
-      if (!whole) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m_own, lsum);
-      const float inv = whole ? (lsum != 0.f ? 1.f / lsum : 0.f) : 1.f;
+      float inv = whole ? (lsum != 0.f ? 1.f / lsum : 0.f) : 1.f;
+      // a value that is not finite among those seen
+      if (__reduce_min_sync(0xffffffffu, first_bad) <= limit) inv = __uint_as_float(0x7FC00000u);
+      if (!whole) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m_own, lsum * inv);
       // 128-byte pieces of a warp's 32 rows go through shared memory, so that whole lines are written
       const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
       uint8_t* const to = whole ? reinterpret_cast<uint8_t*>(a.out + ((int64_t)row0 * a.H + a.h0 + sg.hl) * 128)
@@ -798,11 +803,6 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           tc::fence_before();
           __syncwarp();
           if (lane == 0) tc::arrive_cluster(o_free, 0);
-        }
-        if (first_bad <= limit) {   // a value that is not finite among those seen
-#pragma unroll
-          for (int c = 0; c < 64; ++c)
-            if (bad[64 * half + c] <= limit) o[c >> 5][c & 31] = 0x7FC00000u;
         }
       };
       auto out = [&](const uint32_t (&x)[32], int part) {   // 32 words a row
@@ -956,7 +956,7 @@ size_t latent_prefill_workspace_bytes(int64_t q_start, int64_t C, int64_t H, int
   const int64_t pairs = sms / 2, n_pad = padded(q_start + C);
   if (C == 0) return 256;
   const int64_t heads = heads_per_pass(n_pad, C, H, pairs);
-  return (size_t)(256 + round256(H * LP_BAD * 4) + 2 * pairs * LP_Q * (8 + 512) + heads * n_pad * 512);
+  return (size_t)(256 + round256(heads * n_pad / 8) + 2 * pairs * LP_Q * (8 + 512) + heads * n_pad * 512);
 }
 
 template <typename... P, typename... A>
@@ -1000,9 +1000,8 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
                            : (q_tiles - 1) * (tiles + LP_HDR)) + tiles + LP_HDR;
   const int64_t per = heads_per_pass(n_pad, p.C, p.H, pairs);
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
-  int32_t* const bad = reinterpret_cast<int32_t*>(ws);
-  const int64_t bad_bytes = round256((int64_t)p.H * LP_BAD * 4);
-  ws += bad_bytes;
+  a.bad = reinterpret_cast<int32_t*>(ws);
+  ws += round256(per * n_pad / 8);
   a.ml = reinterpret_cast<float*>(ws);
   ws += (int64_t)2 * pairs * LP_Q * 8;
   a.o = reinterpret_cast<float*>(ws);
@@ -1017,12 +1016,10 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
   if (!st) st = bf16_rows_map(a.k, 128, per * n_pad, 64, &kmap);
   if (!st) st = bf16_rows_map(a.v, 128, per * n_pad, 128, &vmap);
   if (st) return st;
-  if (a.causal && cudaMemsetAsync(bad, 0x7F, bad_bytes, stream) != cudaSuccess) return JF_ERR_CUDA;
   for (int64_t h0 = 0; h0 < p.H; h0 += per) {
     a.h0 = (int32_t)h0;
     a.heads = (int32_t)(p.H - h0 < per ? p.H - h0 : per);
     a.units = a.units_head * a.heads;
-    a.bad = bad + h0 * LP_BAD;
     const int64_t e_tiles = n_pad / 256 * a.heads;
     const unsigned e_pairs = (unsigned)(e_tiles < pairs ? e_tiles : pairs);
     st = launch(latent_expand_kernel, dim3(2 * e_pairs), LE_THREADS, LeSmem::TOTAL, stream, pmap, wkmap,
