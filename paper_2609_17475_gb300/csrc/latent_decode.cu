@@ -693,12 +693,12 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 // ---------------------------------------------------------------------------
 // Join the partials of each row that has any.  A CTA takes CH channels of a row: first
 // its partials' places and, a thread each, their weights; then a thread 4 channels, the
-// partials in turn over the groups of CH / 4 threads, eight loads in flight.
+// partials in turn over the groups of CH / 4 threads, BATCH loads in flight.
 // ---------------------------------------------------------------------------
-constexpr int LM_THREADS = 256, LM_BATCH = 8;
+constexpr int LM_THREADS = 256;
 
-template <int R, int CH>
-__global__ void __launch_bounds__(LM_THREADS)
+template <int R, int CH, int BATCH>
+__global__ void __launch_bounds__(LM_THREADS, BATCH > 4 ? 4 : 6)
 latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
   constexpr int LANES = CH / 4, GROUPS = LM_THREADS / LANES, WARPS = LM_THREADS / 32;
   __shared__ float s_w[LM_THREADS];
@@ -706,15 +706,16 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
   __shared__ float s_red[2][WARPS];
   __shared__ int32_t s_cnt[WARPS];
   __shared__ float4 s_o[LM_THREADS];
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (int)threadIdx.x % LANES, grp = (int)threadIdx.x / LANES;
-  const int64_t total = (int64_t)a.batch * a.H;
+  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
   const PairRuns runs(pl.starts[pl.items], pl.pairs);
-  for (int64_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
-    const int64_t row = slice / (R / CH);
+  for (uint32_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
+    const uint32_t row = slice / (R / CH);
     const int ch = (int)(slice % (R / CH)) * CH + c * 4;
-    const int b = (int)(row / a.H), h = (int)(row - (int64_t)b * a.H);
+    const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
     // the row's partials: those of the prefix's item, then its own's
     int count = 0;
     bool direct = false;
@@ -723,7 +724,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
       if (part == 0) {
         int g = 0;
         while (a.first[g + 1] <= b) ++g;
-        inside = (int)(row - (int64_t)a.first[g] * a.H);
+        inside = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
         item = pl.item0[g] + inside / LD_ROWS;
         inside %= LD_ROWS;
       } else {
@@ -759,9 +760,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     __syncthreads();
     // the first loads, under way while the weights are worked out
     const float* const src = pl.o + ch;
-    float4 v[LM_BATCH];
+    float4 v[BATCH];
 #pragma unroll
-    for (int k = 0; k < LM_BATCH; ++k)
+    for (int k = 0; k < BATCH; ++k)
       if (grp + k * GROUPS < count)
         v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[grp + k * GROUPS] * R);
     float m = -INFINITY, l = 0.f;
@@ -788,9 +789,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     S = 0.f;
     for (int w = 0; w < WARPS; ++w) S += s_red[1][w];
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = grp; i < count; i += LM_BATCH * GROUPS) {
+    for (int i = grp; i < count; i += BATCH * GROUPS) {
 #pragma unroll
-      for (int k = 0; k < LM_BATCH; ++k)
+      for (int k = 0; k < BATCH; ++k)
         if (i + k * GROUPS < count) {
           const float w = s_w[i + k * GROUPS];
           acc.x = fmaf(v[k].x, w, acc.x);
@@ -798,9 +799,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
           acc.z = fmaf(v[k].z, w, acc.z);
           acc.w = fmaf(v[k].w, w, acc.w);
         }
-      const int next = i + LM_BATCH * GROUPS;
+      const int next = i + BATCH * GROUPS;
 #pragma unroll
-      for (int k = 0; k < LM_BATCH; ++k)
+      for (int k = 0; k < BATCH; ++k)
         if (next + k * GROUPS < count)
           v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[next + k * GROUPS] * R);
     }
@@ -815,7 +816,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
         acc.w += x.w;
       }
       const float inv = S != 0.f ? 1.f / S : 0.f;
-      *reinterpret_cast<uint2*>(a.out + row * R + ch) =
+      *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) =
           make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
     }
     __syncthreads();
@@ -863,8 +864,8 @@ static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const Laten
   cfg.gridDim = dim3((unsigned)(slices < most ? slices : most));
   cfg.blockDim = dim3(LM_THREADS);
   cfg.dynamicSmemBytes = 0;
-  const cudaError_t e = wide ? cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R>, a, pl)
-                             : cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, 128>, a, pl);
+  const cudaError_t e = wide ? cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R, 4>, a, pl)
+                             : cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, 128, 8>, a, pl);
   return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 

@@ -859,6 +859,7 @@ __global__ void __launch_bounds__(32 * LJ_WARPS)
 latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   __shared__ float s_w[LJ_WARPS][LJ_ROWS][LJ_MAX];
   __shared__ int s_slot[LJ_MAX], s_n;
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   const int pair = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   ChunkIter run = chunk_run(a, pair);
   const int64_t item = run.start;
