@@ -693,12 +693,12 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 // ---------------------------------------------------------------------------
 // Join the partials of each row that has any.  A CTA takes CH channels of a row: first
 // its partials' places and, a thread each, their weights; then a thread 4 channels, the
-// partials in turn over the groups of CH / 4 threads, BATCH loads in flight.
+// partials in turn over the groups of CH / 4 threads, eight loads in flight.
 // ---------------------------------------------------------------------------
-constexpr int LM_THREADS = 256;
+constexpr int LM_THREADS = 256, LM_BATCH = 8;
 
-template <int R, int CH, int BATCH>
-__global__ void __launch_bounds__(LM_THREADS, BATCH > 4 ? 4 : 6)
+template <int R, int CH>
+__global__ void __launch_bounds__(LM_THREADS)
 latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
   constexpr int LANES = CH / 4, GROUPS = LM_THREADS / LANES, WARPS = LM_THREADS / 32;
   __shared__ float s_w[LM_THREADS];
@@ -760,9 +760,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     __syncthreads();
     // the first loads, under way while the weights are worked out
     const float* const src = pl.o + ch;
-    float4 v[BATCH];
+    float4 v[LM_BATCH];
 #pragma unroll
-    for (int k = 0; k < BATCH; ++k)
+    for (int k = 0; k < LM_BATCH; ++k)
       if (grp + k * GROUPS < count)
         v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[grp + k * GROUPS] * R);
     float m = -INFINITY, l = 0.f;
@@ -789,9 +789,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     S = 0.f;
     for (int w = 0; w < WARPS; ++w) S += s_red[1][w];
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = grp; i < count; i += BATCH * GROUPS) {
+    for (int i = grp; i < count; i += LM_BATCH * GROUPS) {
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k)
+      for (int k = 0; k < LM_BATCH; ++k)
         if (i + k * GROUPS < count) {
           const float w = s_w[i + k * GROUPS];
           acc.x = fmaf(v[k].x, w, acc.x);
@@ -799,9 +799,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
           acc.z = fmaf(v[k].z, w, acc.z);
           acc.w = fmaf(v[k].w, w, acc.w);
         }
-      const int next = i + BATCH * GROUPS;
+      const int next = i + LM_BATCH * GROUPS;
 #pragma unroll
-      for (int k = 0; k < BATCH; ++k)
+      for (int k = 0; k < LM_BATCH; ++k)
         if (next + k * GROUPS < count)
           v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[next + k * GROUPS] * R);
     }
@@ -821,6 +821,105 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
     }
     __syncthreads();
   }
+}
+
+// The same for many rows over prefixes, each with a pair's part or more to join: a warp 128 channels
+// of a row, on its own, its places and weights worked out without the other warps.
+constexpr int LW_MAX = 256;   // partials of a row: at most 2 (pairs + 1)
+
+template <int R>
+__global__ void __launch_bounds__(LM_THREADS)
+latent_merge_rows_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
+  __shared__ int32_t s_row[LM_THREADS / 32][LW_MAX];
+  __shared__ float2 s_w[LM_THREADS / 32][LW_MAX];   // (m, l), then the weight
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
+  const uint32_t slice = blockIdx.x * (LM_THREADS / 32) + warp, row = slice / (R / 128);
+  const int ch = (int)(slice % (R / 128)) * 128 + lane * 4;
+  if (row >= total) return;
+  const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
+  int32_t* const rows = s_row[warp];
+  float2* const w = s_w[warp];
+  // the row's partials: those of the prefix's item, then its own's
+  int item[2], inside[2];
+  int64_t s0[2] = {0, 0}, s1[2] = {0, 0};
+  item[1] = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
+  inside[1] = h % LD_ROWS;
+  if (a.num_groups) {
+    int g = 0;
+    while (a.first[g + 1] <= b) ++g;
+    const int at = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
+    item[0] = pl.item0[g] + at / LD_ROWS;
+    inside[0] = at % LD_ROWS;
+    s0[0] = pl.starts[item[0]] + LD_HDR;
+    s1[0] = pl.starts[item[0] + 1];
+  }
+  s0[1] = pl.starts[item[1]] + LD_HDR;
+  s1[1] = pl.starts[item[1] + 1];
+  const PairRuns runs(pl.starts[pl.items], pl.pairs);
+  int count = 0;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    if (s1[part] <= s0[part]) continue;   // nothing there
+    const int p0 = runs.of(s0[part]), p1 = runs.of(s1[part] - 1);
+    if (p0 == p1) {
+      if (a.num_groups == 0) return;      // written out already
+      if (lane == 0)
+        rows[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
+      ++count;
+      continue;
+    }
+    for (int p = p0 + lane; p - lane <= p1; p += 32) {   // those that have units at all
+      const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
+      const unsigned m = __ballot_sync(0xffffffffu, has);
+      if (has)
+        rows[count + __popc(m & ((1u << lane) - 1))] =
+            (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside[part];
+      count += __popc(m);
+    }
+  }
+  __syncwarp();
+  const float* const src = pl.o + ch;
+  float4 v[LM_BATCH];
+  auto load = [&](int i) {
+#pragma unroll
+    for (int k = 0; k < LM_BATCH; ++k)
+      if (i + k < count) v[k] = *reinterpret_cast<const float4*>(src + (int64_t)rows[i + k] * R);
+  };
+  load(0);   // under way while the weights are worked out
+  float M = -INFINITY, S = 0.f;
+  for (int i = lane; i < count; i += 32) {
+    w[i] = *reinterpret_cast<const float2*>(pl.ml + (int64_t)rows[i] * 2);
+    M = fmaxf(M, w[i].x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  for (int i = lane; i < count; i += 32) {
+    const float f = M == -INFINITY ? 1.f : fast_exp2(w[i].x - M);
+    S = fmaf(f, w[i].y, S);
+    w[i].x = f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+  __syncwarp();
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < count; i += LM_BATCH) {
+#pragma unroll
+    for (int k = 0; k < LM_BATCH; ++k)
+      if (i + k < count) {
+        const float f = w[i + k].x;
+        acc.x = fmaf(v[k].x, f, acc.x);
+        acc.y = fmaf(v[k].y, f, acc.y);
+        acc.z = fmaf(v[k].z, f, acc.z);
+        acc.w = fmaf(v[k].w, f, acc.w);
+      }
+    load(i + LM_BATCH);
+  }
+  const float inv = S != 0.f ? 1.f / S : 0.f;
+  *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
 }
 
 // ---------------------------------------------------------------------------
@@ -857,15 +956,26 @@ static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const Laten
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
   if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
-  // few rows: 128 channels a CTA, so that more of the GPU takes part
-  const int64_t rows = (int64_t)a.batch * a.H, most = 16 * pl.pairs;
-  const bool wide = rows >= 4 * pl.pairs;
-  const int64_t slices = wide ? rows : rows * (R / 128);
-  cfg.gridDim = dim3((unsigned)(slices < most ? slices : most));
+  // Few rows: 128 channels a CTA, so that more of the GPU takes part (one request of 131,072 positions
+  // x 128 heads 43 us, a warp a piece 90).  Many: a CTA a row, since most of a decode's rows have a few
+  // parts or none (32 mixed requests 102.9 us, a warp a piece 104.3, 128 channels a CTA 110); over
+  // prefixes a warp a piece (64 continuations 61.0 us, a CTA a row 62.8; 2 x 4 continuations x 128
+  // heads 27.1 and 29.2).
+  const int64_t rows = (int64_t)a.batch * a.H, slices = rows * (R / 128);
+  const bool many = rows >= 4 * pl.pairs;
   cfg.blockDim = dim3(LM_THREADS);
   cfg.dynamicSmemBytes = 0;
-  const cudaError_t e = wide ? cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R, 4>, a, pl)
-                             : cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, 128, 8>, a, pl);
+  cudaError_t e;
+  if (!many) {
+    cfg.gridDim = dim3((unsigned)slices);
+    e = cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, 128>, a, pl);
+  } else if (!a.num_groups) {
+    cfg.gridDim = dim3((unsigned)(rows < 16 * pl.pairs ? rows : 16 * pl.pairs));
+    e = cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R>, a, pl);
+  } else {
+    cfg.gridDim = dim3((unsigned)((slices + LM_THREADS / 32 - 1) / (LM_THREADS / 32)));
+    e = cudaLaunchKernelEx(&cfg, latent_merge_rows_kernel<R>, a, pl);
+  }
   return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 
@@ -877,6 +987,7 @@ int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t st
   LatentPlan pl;
   int64_t items, slot_rows, rows;
   const int sms = sm_count();
+  if (sms / 2 > LW_MAX / 2 - 2) return JF_ERR_UNSUPPORTED;
   plan_sizes(a.batch, a.H, a.num_groups, sms, &items, &slot_rows, &rows);
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
   pl.pairs = sms / 2;
