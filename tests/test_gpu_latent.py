@@ -236,6 +236,49 @@ def test_decode_repeats_bit_for_bit_and_any_batch_order():
         check(three[i], q[b], O.gather(pool, table[b], ctx[b]), T.SCALE)
 
 
+def test_a_batch_that_holds_nothing_yet():
+    rng = np.random.default_rng(20)
+    table, pool = T.filled(rng, 512, 64, [0, 0, 0])
+    q = T.queries(rng, 3, 16, 512)
+    out, st = run_decode(table, pool, [0, 0, 0], q, T.SCALE)
+    assert st == 0 and (out == 0).all()
+    out, st = run_prefix(pool, table[:1], [0], [0, 2], table[1:], [0, 0], q[:2], T.SCALE)
+    assert st == 0 and (out == 0).all()
+
+
+def test_three_row_blocks_a_request():
+    rng = np.random.default_rng(23)
+    table, pool = T.filled(rng, 256, 128, [3000, 1, 700])
+    q = T.queries(rng, 3, 300, 256)
+    out, st = run_decode(table, pool, [3000, 1, 700], q, T.SCALE)
+    assert st == 0
+    for b, n in enumerate([3000, 1, 700]):
+        check(out[b], q[b], O.gather(pool, table[b], n), T.SCALE)
+
+
+def test_memory_at_any_16_byte_address():
+    """A pool, queries, weights and outputs that begin 16 bytes past a line."""
+    rng = np.random.default_rng(24)
+    table, pool = T.filled(rng, 512, 64, [500])
+    raw = torch.empty(pool.size * 2 + 16, dtype=torch.uint8, device="cuda")
+    data = raw[16:].view(len(pool), -1)
+    data.copy_(T.gpu_pool(pool).data)
+    g = jf.KVPool(data, 64, 1, 576, format=jf.JF_FMT_LATENT16)
+
+    def moved(t):
+        buf = torch.zeros(t.numel() + 8, dtype=t.dtype, device="cuda")
+        buf[8:].copy_(t.flatten())
+        return buf[8:].view(t.shape)
+
+    q, w, q3 = T.queries(rng, 1, 16, 512), weights(rng, 2, 512), T.bf16(rng.standard_normal((100, 2, 192)))
+    out, out3 = moved(torch.zeros(1, 16, 512).bfloat16().cuda()), moved(torch.zeros(100, 2, 128).bfloat16().cuda())
+    jf.jf_latent_decode_attn(g, ints(table), ints([500]), moved(gpu(q)), T.SCALE, out, jf.latent_decode_workspace(1, 16, 512))
+    check(out[0], q[0], O.gather(pool, table[0], 500), T.SCALE)
+    jf.jf_latent_prefill_attn(g, ints(table[0]), moved(gpu(q3)), 400, moved(gpu(w[0])), moved(gpu(w[1])), T.SCALE, True, out3,
+                              jf.latent_prefill_workspace(400, 100, 2))
+    check_prefill(out3, q3, O.gather(pool, table[0], 500), 400, w, T.SCALE, True)
+
+
 def test_draft_tokens_as_requests():
     """Four tokens of one request: the same page-table row, a context length each."""
     rng = np.random.default_rng(18)
@@ -374,6 +417,20 @@ def test_prefill_of_many_heads(R, H, q_start, C, causal):
     kv = O.gather(pool, table[0], n)
     for h in range(0, H, 3):
         check_prefill(out[:, h:h + 1], q[:, h:h + 1], kv, q_start, w[:, h:h + 1], T.SCALE, causal)
+
+
+def test_prefill_in_several_passes():
+    """More heads than the workspace holds keys and values of."""
+    rng = np.random.default_rng(38)
+    C, H, R = 4000, 60, 256
+    table, pool = T.filled(rng, R, 256, [C])
+    q, w = T.bf16(rng.standard_normal((C, H, 192))), weights(rng, H, R)
+    assert jf.jf_latent_prefill_workspace_bytes(0, C, H) < H * 4096 * 512
+    out, st = run_prefill(table[0], pool, q, 0, w, T.SCALE, True)
+    assert st == 0
+    kv = O.gather(pool, table[0], C)
+    for h in (0, 29, 30, 59):
+        check_prefill(out[:, h:h + 1], q[:, h:h + 1], kv, 0, w[:, h:h + 1], T.SCALE, True)
 
 
 @pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
