@@ -1,7 +1,8 @@
 /*
- * jfkv.h -- C ABI of the GB300 paged KV library (libjfkv.so): 4-bit pages, and
- * for long image-and-text sessions 8-bit pages, rotary positions with several
- * axes and eviction by attention weight.
+ * jfkv.h -- C ABI of the GB300 paged KV library (libjfkv.so): 4-bit pages; for
+ * long image-and-text sessions 8-bit pages, rotary positions with several axes
+ * and eviction by attention weight; and a latent cache of one bf16 row a position
+ * for all heads.
  *
  * The library implements the data-parallel hot path of KVExec (Sec. 3.1 and
  * Sec. 3.4 of "JustFit: Just-in-Time State Management for Local LLM Serving"):
@@ -690,11 +691,10 @@ size_t jf_latent_workspace_bytes(int32_t batch, int32_t num_heads, int32_t laten
  *   workspace     >= jf_latent_workspace_bytes(batch, num_heads, R, 0, 0) bytes,
  *                 256-byte aligned, its first 256 bytes zero before the first
  *                 call; its first int32 is the device status word
- * A context length outside [0, pt_stride * P], or past JF_LATENT_MAX_POSITIONS, sets
- * JF_DEV_ERR_POSITION and counts
- * as 0; positions of a page outside the pool draw no weight
- * (JF_DEV_ERR_PAGE_ID).  Several tokens of one request (a draft's, say) go in as
- * requests with the same page-table row and a context length each.
+ * A context length outside [0, pt_stride * P], or past JF_LATENT_MAX_POSITIONS,
+ * sets JF_DEV_ERR_POSITION and counts as 0; positions of a page outside the pool
+ * draw no weight (JF_DEV_ERR_PAGE_ID).  Several tokens of one request (a draft's,
+ * say) go in as requests with the same page-table row and a context length each.
  * Numerics: products of the bf16 values in fp32; maxima, sums and outputs in
  * fp32.  The weights enter their product with c as bf16 (2^-8 of each), and the
  * sum they are divided by is that of the rounded ones.
@@ -709,7 +709,7 @@ int jf_latent_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int
  * continuations of one prompt): request b of group g, group_offsets[g] <= b <
  * group_offsets[g + 1], attends the prefix_lens[g] positions of the group's pages
  * and then the context_lens[b] positions of its own.  The prefix is read once for
- * all queries of its group, whose rows are multiplied together.
+ * every 128 (request, head) rows of its group, which are multiplied together.
  *   prefix_table   int32 [num_groups, prefix_stride]
  *   prefix_lens    int32 [num_groups] on the device
  *   group_offsets  int32 [num_groups + 1] on the HOST, from 0 to batch, none

@@ -682,7 +682,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
-  __syncthreads();
+  settle(ok);
   tc::cluster_sync();
   if (warp == 0) {
     tc::fence_after();

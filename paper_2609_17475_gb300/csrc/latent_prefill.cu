@@ -317,7 +317,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   }
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
-  __syncthreads();
+  settle(ok);
   tc::cluster_sync();
   if (warp == 0) {
     tc::fence_after();
@@ -841,7 +841,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   }
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
-  __syncthreads();
+  settle(ok);
   tc::cluster_sync();
   if (warp == 0) {
     tc::fence_after();
@@ -864,9 +864,9 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   ChunkIter run = chunk_run(a, pair);
   const int64_t item = run.start;
   ChunkSeg sg;
-  if (run.u0 >= run.u1 || !next_chunk_seg(a, run, sg) || sg.j0 == 0 || sg.j1 != sg.n) return;
+  const bool joins = run.u0 < run.u1 && next_chunk_seg(a, run, sg) && sg.j0 > 0 && sg.j1 == sg.n;
   const int row0 = ((int)blockIdx.y * LJ_WARPS + warp) * LJ_ROWS;
-  if (warp == 0) {   // pairs from the first to this one that have units at all
+  if (joins && warp == 0) {   // pairs from the first to this one that have units at all
     const PairRuns runs(a.units, a.pairs);
     const int p0 = runs.of(item + LP_HDR);
     int n = 0;
@@ -878,8 +878,11 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
     }
     if (lane == 0) s_n = n;
   }
-  __syncthreads();
+  // Blocks with nothing to join wait too: the kernel after this one takes this one's end for the end of
+  // all before it.
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
+  if (!joins) return;
+  __syncthreads();
   const int n = s_n, q0 = sg.qt * LP_Q + row0;
   if (q0 >= a.C) return;
   // weights: eight lanes a row

@@ -81,6 +81,13 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
                ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
+// The block's end, all threads together.  Where a wait gave up, copies and products may still be under
+// way: they get a millisecond, a thousand times what they take, before the memory is released.
+__device__ __forceinline__ void settle(bool ok) {
+  if (__syncthreads_or(!ok))
+    for (int i = 0; i < 100; ++i) __nanosleep(10000);
+}
+
 // brings memory into the L2 cache, 16-byte aligned
 __device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(p), "r"(bytes) : "memory");

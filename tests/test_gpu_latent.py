@@ -419,6 +419,29 @@ def test_prefill_of_many_heads(R, H, q_start, C, causal):
         check_prefill(out[:, h:h + 1], q[:, h:h + 1], kv, q_start, w[:, h:h + 1], T.SCALE, causal)
 
 
+def test_short_prefills_back_to_back():
+    """Chunks too short to be divided, one after the other through one workspace: each call's expansion
+    writes over the keys and values that the attention before it reads."""
+    rng = np.random.default_rng(39)
+    R, H, C = 512, 8, 40
+    table, pool = T.filled(rng, R, 64, [C] * 12)
+    g, w = T.gpu_pool(pool), weights(rng, H, R)
+    wk, wv, ws = gpu(w[0]), gpu(w[1]), jf.latent_prefill_workspace(0, C, H)
+    qs = [T.bf16(rng.standard_normal((C, H, 192))) for _ in range(12)]
+    gq, rows = [gpu(q) for q in qs], [ints(table[b]) for b in range(12)]
+    outs = [torch.zeros(C, H, 128, dtype=torch.bfloat16, device="cuda") for _ in range(12)]
+    after = []
+    torch.cuda.synchronize()
+    for b in range(12):
+        jf.jf_latent_prefill_attn(g, rows[b], gq[b], 0, wk, wv, T.SCALE, True, outs[b], ws)
+        after.append(outs[b].clone())
+    torch.cuda.synchronize()
+    assert jf.workspace_status(ws) == 0
+    for b in range(12):
+        assert torch.equal(after[b], outs[b])
+        check_prefill(outs[b], qs[b], O.gather(pool, table[b], C), 0, w, T.SCALE, True)
+
+
 def test_prefill_in_several_passes():
     """More heads than the workspace holds keys and values of."""
     rng = np.random.default_rng(38)

@@ -28,6 +28,13 @@ def test_kernels_wait_for_what_came_before_them(name):
     assert len(re.findall(r"__global__", text)) == len(re.findall(r"griddepcontrol\.wait", text))
 
 
+def test_no_block_ends_before_the_join_has_waited():
+    """The next kernel takes the join's end for the end of the attention before it."""
+    with open(os.path.join(CSRC, "latent_prefill.cu")) as f:
+        body = f.read().split("latent_prefill_merge_kernel(const")[1]
+    assert "return" not in body[:body.index("griddepcontrol.wait")]
+
+
 @pytest.mark.parametrize("name", FILES)
 def test_waits_are_bounded(name):
     """Barriers in memory are waited for with a limit (a poll that is its own loop counts its turns)."""
