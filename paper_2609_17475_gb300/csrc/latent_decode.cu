@@ -631,51 +631,48 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       if (!direct && half == 0 && side == 0 && r < rows)
         *reinterpret_cast<float2*>(pl.ml + (crow + r) * 2) = make_float2(m, l);
       const float inv = l != 0.f ? 1.f / l : 0.f;
-      // 64-byte pieces of the warp's 32 rows go through its part of P, so that whole sectors are
-      // written: piece p of row i at p ^ ((i >> 1) & 3).  The part is one of the same four warps' rows:
-      // the other four may be at their next tile's P already.
-      const int row_base = (quarter & 1) * 32;
-      const uint32_t tr = sp + half * L::CHUNK + row_base * 128 + side * 2048;
-      if (row_base < rows) {
+      // O is read in pieces of 16 rows x 8 columns, of which four threads have 32 bytes of a row: whole
+      // sectors are written from the registers.  (Through shared memory, a row a thread, this took
+      // 1.4 us for 16 rows and 3 us for 64.)  A short loop, one copy of its code: it runs once a segment.
+      const int row_base = (quarter & 1) * 32, sub = lane >> 2, col = lane & 3;
+#pragma unroll 1
+      for (int r0 = row_base; r0 < min(row_base + 32, rows); r0 += 16) {
+        const bool lo = r0 + sub < rows, hi = r0 + sub + 8 < rows;
+        const uint32_t from = tO + lane_off + ((uint32_t)(r0 - row_base) << 16);
+        const float f0 = __shfl_sync(0xffffffffu, inv, r0 - row_base + sub);
+        const float f1 = __shfl_sync(0xffffffffu, inv, r0 - row_base + sub + 8);
 #pragma unroll 1
         for (int c0 = side * (R / 4); c0 < (side + 1) * (R / 4); c0 += 32) {
-          uint32_t o[32];
-          tc::ld32(tO + c0 + lane_off, o);
+          const int64_t at = (crow + r0 + sub) * R + (c0 >> 7) * 256 + half * 128 + (c0 & 127);
+          uint32_t o[16];
+          ld16_32(from + c0, o);
           tc::wait_ld();
-          const int d0 = (c0 >> 7) * 256 + half * 128 + (c0 & 127);
+          if (direct) {   // neighbours exchange a piece: eight bytes each
+            uint16_t* const to = a.out + at + 8 * (col & 1) + 4 * (col >> 1);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            if (direct && h == 1) break;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              uint32_t w[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                w[i] = direct ? pack_bf16x2(__uint_as_float(o[8 * k + 2 * i]) * inv,
-                                            __uint_as_float(o[8 * k + 2 * i + 1]) * inv)
-                              : o[16 * h + 4 * k + i];
-              sts128(tr + lane * 64 + ((k ^ ((lane >> 1) & 3)) << 4), w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < 4; ++i) {   // pieces 0 and 1, then 2 and 3, of both rows
+              const uint32_t* const x = o + 8 * (i >> 1) + 2 * (i & 1);
+              const float f = i & 1 ? f1 : f0;
+              const uint32_t u = pack_bf16x2(__uint_as_float(x[0]) * f, __uint_as_float(x[1]) * f);
+              const uint32_t v = pack_bf16x2(__uint_as_float(x[4]) * f, __uint_as_float(x[5]) * f);
+              const uint32_t w = __shfl_xor_sync(0xffffffffu, col & 1 ? u : v, 1);
+              if (i & 1 ? hi : lo)
+                *reinterpret_cast<uint2*>(to + 8 * R * (i & 1) + 16 * (i >> 1)) =
+                    col & 1 ? make_uint2(w, v) : make_uint2(u, w);
             }
-            __syncwarp();
+          } else {
+            float* const to = pl.o + at + 2 * col;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int row = i * 8 + (lane >> 2), piece = lane & 3;
-              const uint4 v = lds128(tr + row * 64 + ((piece ^ ((row >> 1) & 3)) << 4));
-              if (row_base + row < rows) {
-                const int64_t at = (crow + row_base + row) * R + d0;
-                if (direct)
-                  *reinterpret_cast<uint4*>(a.out + at + piece * 8) = v;
-                else
-                  *reinterpret_cast<uint4*>(pl.o + at + 16 * h + piece * 4) = v;
-              }
+              if (lo) *reinterpret_cast<uint2*>(to + 8 * i) = make_uint2(o[4 * i], o[4 * i + 1]);
+              if (hi) *reinterpret_cast<uint2*>(to + 8 * R + 8 * i) = make_uint2(o[4 * i + 2], o[4 * i + 3]);
             }
-            __syncwarp();
           }
         }
       }
       tc::fence_before();
       sg = nx;
-      row_sync();   // s_x read, and P's parts, before a warp goes on to write them
+      row_sync();   // s_x read before a warp goes on to write it
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   }
