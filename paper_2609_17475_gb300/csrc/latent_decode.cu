@@ -44,6 +44,7 @@ struct LatentPlan {
   int32_t pairs;                    // CTA pairs of the launch
   int32_t items, prefix_items, blocks;   // items; those of prefixes; row blocks of a request
   int32_t slot_rows;                // rows of a cut item's partial
+  uint32_t inv;                     // of the pairs, for PairRuns
   int32_t item0[LAT_MAX_GROUPS + 1];     // first items of the groups
   int64_t* starts;                  // [items + 1], in units of tiles
   float* ml;                        // [rows][2]
@@ -68,7 +69,7 @@ struct LdSmem {
   static constexpr int OFF_X = OFF_BAR + 256;          // [2][256] exchange between a row's threads
   static constexpr int OFF_PLAN = OFF_X + 2 * 256 * 4; // [16] of the plan's scan
   static constexpr int OFF_FIRST = OFF_PLAN + 16 * 8;  // LdFirst
-  static constexpr int TOTAL = OFF_FIRST + 128;
+  static constexpr int TOTAL = OFF_FIRST + 16;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -78,6 +79,9 @@ struct LatentItem {
   int32_t len, row0, nrows;
 };
 
+__device__ __forceinline__ int request_of(const LatentPlan& pl, int k) {
+  return pl.blocks == 1 ? k : k / pl.blocks;
+}
 // the group of item i, -1 for a request's own positions
 __device__ __forceinline__ int item_group(const LatentPlan& pl, int i) {
   if (i >= pl.prefix_items) return -1;
@@ -87,7 +91,7 @@ __device__ __forceinline__ int item_group(const LatentPlan& pl, int i) {
 }
 // its positions, -1 where their number does not fit the table
 __device__ __forceinline__ int item_len(const LatentDecode& a, const LatentPlan& pl, int i, int g) {
-  const int n = g >= 0 ? a.prefix_lens[g] : a.context_lens[(i - pl.prefix_items) / pl.blocks];
+  const int n = g >= 0 ? a.prefix_lens[g] : a.context_lens[request_of(pl, i - pl.prefix_items)];
   const int stride = g >= 0 ? a.prefix_stride : a.pt_stride;
   return n < 0 || n > (int64_t)stride * a.pool.P || n > JF_LATENT_MAX_POSITIONS ? -1 : n;
 }
@@ -111,7 +115,7 @@ __device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const Laten
     it.nrows = min(LD_ROWS, a.first[g + 1] * a.H - it.row0);
     it.pt = a.prefix_table + (int64_t)g * a.prefix_stride;
   } else {
-    const int k = i - pl.prefix_items, b = k / pl.blocks, hb = k - b * pl.blocks;
+    const int k = i - pl.prefix_items, b = request_of(pl, k), hb = k - b * pl.blocks;
     it.row0 = b * a.H + hb * LD_ROWS;
     it.nrows = min(LD_ROWS, a.H - hb * LD_ROWS);
     it.pt = a.page_table + (int64_t)b * a.pt_stride;
@@ -128,19 +132,16 @@ struct Seg {
 struct SegIter {
   int64_t start, u0, u1;   // first unit of the item
   int item;
-  const Seg* first;        // the first segment, worked out already
+  int len;                 // of the item, where it is known already (else LD_ASK)
 };
+constexpr int LD_ASK = -2;
 
 __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan& pl, SegIter& s,
                                          Seg& seg) {
-  if (s.first) {
-    seg = *s.first;
-    s.first = nullptr;
-    return true;
-  }
   while (s.item < pl.items && s.start < s.u1) {
     const int g = item_group(pl, s.item);
-    const int len = item_len(a, pl, s.item, g);
+    const int len = s.len != LD_ASK ? s.len : item_len(a, pl, s.item, g);
+    s.len = LD_ASK;
     const int n = tiles_of(len);
     const int64_t first = s.start + LD_HDR;   // unit of tile 0
     const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
@@ -159,11 +160,79 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
   return false;
 }
 
-struct LdFirst {   // a pair's first segment and what comes after it
-  SegIter next;
-  Seg seg;
-  int has;
+struct LdFirst {   // a pair's first item
+  int64_t start;
+  int item, len;
 };
+
+// This pair's run of the items, which the last thread with items' units before it works out; every
+// thread takes part.  Block 0 writes the items' first units for the kernel that joins the partials.
+__device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentPlan& pl, int pair, int warp,
+                                            int lane, int64_t* s_plan, LdFirst* s_first) {
+  SegIter run{0, 0, 0, pl.items, LD_ASK};
+  if (pl.items <= 32) {   // an item a lane, each warp by itself
+    const int len = lane < pl.items ? item_len(a, pl, lane, item_group(pl, lane)) : 0;
+    const int n = (int)units_of(len);
+    int incl = n;   // below 2^30
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += y;
+    }
+    const int at = incl - n;
+    const PairRuns runs(__shfl_sync(0xffffffffu, incl, 31), pl.pairs, pl.inv);
+    const int64_t u0 = runs.first(pair), u1 = runs.first(pair + 1);
+    const unsigned mine = __ballot_sync(0xffffffffu, u0 < u1 && at <= u0 && u0 < incl);
+    const int src = mine ? __ffs(mine) - 1 : 0;
+    const int start = __shfl_sync(0xffffffffu, at, src), first_len = __shfl_sync(0xffffffffu, len, src);
+    if (mine) run = SegIter{start, u0, u1, src, first_len};
+    if (blockIdx.x == 0 && warp == 0) {
+      if (len < 0) flag_error(a.status, JF_DEV_ERR_POSITION);
+      if (lane < pl.items) pl.starts[lane] = at;
+      if (lane == 31) pl.starts[pl.items] = incl;
+    }
+    return run;
+  }
+  const int per = (pl.items + LD_THREADS - 1) / LD_THREADS;
+  const int i0 = min(pl.items, (int)threadIdx.x * per), i1 = min(pl.items, i0 + per);
+  int64_t sum = 0;
+  for (int i = i0; i < i1; ++i) {
+    const int len = item_len(a, pl, i, item_group(pl, i));
+    if (len < 0 && blockIdx.x == 0) flag_error(a.status, JF_DEV_ERR_POSITION);
+    sum += units_of(len);
+  }
+  int64_t incl = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) s_plan[warp] = incl;
+  if (threadIdx.x == 0) s_first->item = -1;
+  __syncthreads();
+  int64_t before = 0, units = 0;
+#pragma unroll 1
+  for (int w = 0; w < LD_THREADS / 32; ++w) {
+    if (w < warp) before += s_plan[w];
+    units += s_plan[w];
+  }
+  int64_t at = before + incl - sum;   // units before this thread's items
+  const PairRuns runs(units, pl.pairs, pl.inv);
+  const int64_t u0 = runs.first(pair), u1 = runs.first(pair + 1);
+  const bool mine = u0 < u1 && at <= u0 && u0 < at + sum;
+  if (mine || blockIdx.x == 0)
+    for (int i = i0; i < i1; ++i) {
+      const int len = item_len(a, pl, i, item_group(pl, i));
+      const int64_t next = at + units_of(len);
+      if (blockIdx.x == 0) pl.starts[i] = at;
+      if (mine && at <= u0 && u0 < next) *s_first = LdFirst{at, i, len};
+      at = next;
+    }
+  if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
+  __syncthreads();
+  if (s_first->item >= 0) run = SegIter{s_first->start, u0, u1, s_first->item, s_first->len};
+  return run;
+}
 
 template <int R>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LD_THREADS, 1)
@@ -193,7 +262,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   float* const s_x = reinterpret_cast<float*>(sm + L::OFF_X);
   int64_t* const s_plan = reinterpret_cast<int64_t*>(sm + L::OFF_PLAN);
   LdFirst* const s_first = reinterpret_cast<LdFirst*>(sm + L::OFF_FIRST);
-  static_assert(sizeof(LdFirst) <= 128 && LD_THREADS / 32 <= 16, "shared memory of the plan");
+  static_assert(sizeof(LdFirst) <= 16 && LD_THREADS / 32 <= 16, "shared memory of the plan");
 
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
@@ -229,79 +298,9 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // waited for after the plan
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
 
-  // ---- the plan: units before each thread's items, and this pair's first item ----------
-  SegIter run;
-  {
-    const int per = (pl.items + LD_THREADS - 1) / LD_THREADS;
-    const int i0 = min(pl.items, (int)threadIdx.x * per), i1 = min(pl.items, i0 + per);
-    int64_t sum = 0;
-    int len0 = -1;   // of this thread's first item
-    for (int i = i0; i < i1; ++i) {
-      const int len = item_len(a, pl, i, item_group(pl, i));
-      if (len < 0 && blockIdx.x == 0) flag_error(a.status, JF_DEV_ERR_POSITION);
-      if (i == i0) len0 = len;
-      sum += units_of(len);
-    }
-    int64_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += y;
-    }
-    if (lane == 31) s_plan[warp] = incl;
-    __syncthreads();
-    int64_t before = 0, units = 0;
-    for (int w = 0; w < LD_THREADS / 32; ++w) {
-      if (w < warp) before += s_plan[w];
-      units += s_plan[w];
-    }
-    int64_t at = before + incl - sum;   // units before this thread's items
-    const PairRuns runs(units, pl.pairs);
-    run.u0 = runs.first(pair);
-    run.u1 = runs.first(pair + 1);
-    const bool mine = run.u0 < run.u1 && at <= run.u0 && run.u0 < at + sum;
-    if (threadIdx.x == 0) s_first->has = 0;
-    __syncthreads();
-    if (mine || blockIdx.x == 0)
-      for (int i = i0; i < i1; ++i) {
-        const int g = item_group(pl, i);
-        const int len = i == i0 ? len0 : item_len(a, pl, i, g);
-        const int n = tiles_of(len);
-        const int64_t next = at + units_of(len);
-        if (blockIdx.x == 0) pl.starts[i] = at;
-        if (mine && at <= run.u0 && run.u0 < next) {
-          // this thread has the pair's first item: its first segment, unless that is the header alone
-          SegIter it{next, run.u0, run.u1, i + 1, nullptr};
-          Seg seg;
-          const int64_t lo = max((int64_t)0, run.u0 - at - LD_HDR), hi = min((int64_t)n, run.u1 - at - LD_HDR);
-          bool has = lo < hi;
-          if (has) {
-            seg.it = item_of(a, pl, i, g, len);
-            seg.item = i;
-            seg.j0 = (int)lo;
-            seg.j1 = (int)hi;
-            seg.n = n;
-            seg.alone = item_alone(pl, g);
-          } else {
-            has = next_seg(a, pl, it, seg);
-          }
-          s_first->next = it;
-          s_first->seg = seg;
-          s_first->has = has;
-        }
-        at = next;
-      }
-    if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
-    __syncthreads();
-    asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // both CTAs: barriers, TMEM
-    tc::fence_after();
-    if (s_first->has) {
-      run = s_first->next;
-      run.first = &s_first->seg;
-    } else {
-      run = SegIter{0, 0, 0, pl.items, nullptr};
-    }
-  }
+  SegIter run = plan_run(a, pl, pair, warp, lane, s_plan, s_first);
+  asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // both CTAs: barriers, TMEM
+  tc::fence_after();
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   // all 512 columns are this CTA's: O from 0, the S buffers behind it
   constexpr uint32_t tO = 0, tS = R / 2;
@@ -633,41 +632,45 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       const float inv = l != 0.f ? 1.f / l : 0.f;
       // O is read in pieces of 16 rows x 8 columns, of which four threads have 32 bytes of a row: whole
       // sectors are written from the registers.  (Through shared memory, a row a thread, this took
-      // 1.4 us for 16 rows and 3 us for 64.)  A short loop, one copy of its code: it runs once a segment.
+      // 1.4 us for 16 rows and 3 us for 64.)
       const int row_base = (quarter & 1) * 32, sub = lane >> 2, col = lane & 3;
 #pragma unroll 1
       for (int r0 = row_base; r0 < min(row_base + 32, rows); r0 += 16) {
         const bool lo = r0 + sub < rows, hi = r0 + sub + 8 < rows;
-        const uint32_t from = tO + lane_off + ((uint32_t)(r0 - row_base) << 16);
+        const uint32_t from = tO + lane_off + ((uint32_t)(r0 - row_base) << 16) + side * (R / 4);
         const float f0 = __shfl_sync(0xffffffffu, inv, r0 - row_base + sub);
         const float f1 = __shfl_sync(0xffffffffu, inv, r0 - row_base + sub + 8);
-#pragma unroll 1
-        for (int c0 = side * (R / 4); c0 < (side + 1) * (R / 4); c0 += 32) {
-          const int64_t at = (crow + r0 + sub) * R + (c0 >> 7) * 256 + half * 128 + (c0 & 127);
-          uint32_t o[16];
-          ld16_32(from + c0, o);
-          tc::wait_ld();
-          if (direct) {   // neighbours exchange a piece: eight bytes each
-            uint16_t* const to = a.out + at + 8 * (col & 1) + 4 * (col >> 1);
+        // this thread's R / 4 columns adjoin in a row of O
+        const int64_t at = (crow + r0 + sub) * R + half * 128 + (R == 512 ? side * 256 : side * 64);
+        uint32_t o[R / 128][16];
+#pragma unroll
+        for (int c = 0; c < R / 128; ++c) ld16_32(from + 32 * c, o[c]);
+        tc::wait_ld();
+        if (direct) {   // neighbours exchange a piece: eight bytes each
+          uint16_t* const to = a.out + at + 8 * (col & 1) + 4 * (col >> 1);
+#pragma unroll
+          for (int c = 0; c < R / 128; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {   // pieces 0 and 1, then 2 and 3, of both rows
-              const uint32_t* const x = o + 8 * (i >> 1) + 2 * (i & 1);
+              const uint32_t* const x = o[c] + 8 * (i >> 1) + 2 * (i & 1);
               const float f = i & 1 ? f1 : f0;
               const uint32_t u = pack_bf16x2(__uint_as_float(x[0]) * f, __uint_as_float(x[1]) * f);
               const uint32_t v = pack_bf16x2(__uint_as_float(x[4]) * f, __uint_as_float(x[5]) * f);
               const uint32_t w = __shfl_xor_sync(0xffffffffu, col & 1 ? u : v, 1);
               if (i & 1 ? hi : lo)
-                *reinterpret_cast<uint2*>(to + 8 * R * (i & 1) + 16 * (i >> 1)) =
+                *reinterpret_cast<uint2*>(to + 8 * R * (i & 1) + 32 * c + 16 * (i >> 1)) =
                     col & 1 ? make_uint2(w, v) : make_uint2(u, w);
             }
-          } else {
-            float* const to = pl.o + at + 2 * col;
+        } else {
+          float* const to = pl.o + at + 2 * col;
+#pragma unroll
+          for (int c = 0; c < R / 128; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              if (lo) *reinterpret_cast<uint2*>(to + 8 * i) = make_uint2(o[4 * i], o[4 * i + 1]);
-              if (hi) *reinterpret_cast<uint2*>(to + 8 * R + 8 * i) = make_uint2(o[4 * i + 2], o[4 * i + 3]);
+              if (lo) *reinterpret_cast<uint2*>(to + 32 * c + 8 * i) = make_uint2(o[c][4 * i], o[c][4 * i + 1]);
+              if (hi)
+                *reinterpret_cast<uint2*>(to + 8 * R + 32 * c + 8 * i) = make_uint2(o[c][4 * i + 2], o[c][4 * i + 3]);
             }
-          }
         }
       }
       tc::fence_before();
@@ -680,7 +683,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  tc::cluster_sync();
+  cluster_meet();
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
@@ -708,7 +711,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (int)threadIdx.x % LANES, grp = (int)threadIdx.x / LANES;
   const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
-  const PairRuns runs(pl.starts[pl.items], pl.pairs);
+  const PairRuns runs(pl.starts[pl.items], pl.pairs, pl.inv);
   for (uint32_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
     const uint32_t row = slice / (R / CH);
     const int ch = (int)(slice % (R / CH)) * CH + c * 4;
@@ -855,7 +858,7 @@ latent_merge_rows_kernel(const __grid_constant__ LatentDecode a, const __grid_co
   }
   s0[1] = pl.starts[item[1]] + LD_HDR;
   s1[1] = pl.starts[item[1] + 1];
-  const PairRuns runs(pl.starts[pl.items], pl.pairs);
+  const PairRuns runs(pl.starts[pl.items], pl.pairs, pl.inv);
   int count = 0;
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
@@ -988,6 +991,7 @@ int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t st
   plan_sizes(a.batch, a.H, a.num_groups, sms, &items, &slot_rows, &rows);
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
   pl.pairs = sms / 2;
+  pl.inv = pairs_inverse(pl.pairs);
   pl.slot_rows = (int32_t)slot_rows;
   pl.blocks = (a.H + LD_ROWS - 1) / LD_ROWS;
   pl.item0[0] = 0;

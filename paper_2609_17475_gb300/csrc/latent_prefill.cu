@@ -52,6 +52,7 @@ struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
   int64_t units, units_head;         // of the pass, of a head
   int32_t n, n_pad, q_start, C, H, h0, heads, causal;
   int32_t q_tiles, pairs;
+  uint32_t inv;                      // of the pairs, for PairRuns
   float scale_log2;
 };
 
@@ -318,7 +319,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  tc::cluster_sync();
+  cluster_meet();
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
@@ -366,7 +367,7 @@ struct ChunkIter {
 };
 
 __device__ __forceinline__ ChunkIter chunk_run(const LatentChunk& a, int pair) {
-  const PairRuns runs(a.units, a.pairs);
+  const PairRuns runs(a.units, a.pairs, a.inv);
   ChunkIter s;
   s.u0 = runs.first(pair);
   s.u1 = runs.first(pair + 1);
@@ -842,7 +843,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  tc::cluster_sync();
+  cluster_meet();
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
@@ -867,7 +868,7 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   const bool joins = run.u0 < run.u1 && next_chunk_seg(a, run, sg) && sg.j0 > 0 && sg.j1 == sg.n;
   const int row0 = ((int)blockIdx.y * LJ_WARPS + warp) * LJ_ROWS;
   if (joins && warp == 0) {   // pairs from the first to this one that have units at all
-    const PairRuns runs(a.units, a.pairs);
+    const PairRuns runs(a.units, a.pairs, a.inv);
     const int p0 = runs.of(item + LP_HDR);
     int n = 0;
     for (int p = p0 + lane; p - lane <= pair; p += 32) {
@@ -995,6 +996,7 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
   a.H = p.H;
   a.causal = p.causal != 0;
   a.pairs = pairs;
+  a.inv = pairs_inverse(pairs);
   a.scale_log2 = p.scale_log2;
   const int64_t q_tiles = ((int64_t)p.C + LP_Q - 1) / LP_Q;
   a.q_tiles = (int32_t)q_tiles;

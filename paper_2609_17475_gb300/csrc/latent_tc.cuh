@@ -100,6 +100,12 @@ __device__ __forceinline__ void settle(bool ok) {
     for (int i = 0; i < 100; ++i) __nanosleep(10000);
 }
 
+// Both CTAs of the pair are here.  Relaxed: nothing is handed over, and a release would first wait for
+// this CTA's stores to reach memory, which the kernel's end does anyway.
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
+}
+
 // brings memory into the L2 cache, 16-byte aligned
 __device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(p), "r"(bytes) : "memory");
@@ -109,15 +115,35 @@ __device__ __forceinline__ void prefetch_l2(const void* p, uint32_t bytes) {
 __device__ __forceinline__ uint64_t divide(uint64_t x, uint64_t y) {
   return (x | y) >> 32 ? x / y : (uint64_t)((uint32_t)x / (uint32_t)y);
 }
-struct PairRuns {   // floor(units * p / pairs), by one division
+// 2^32 / pairs, rounded up
+inline uint32_t pairs_inverse(int64_t pairs) {
+  const uint64_t x = (((uint64_t)1 << 32) + pairs - 1) / pairs;
+  return x >> 32 ? 0xFFFFFFFFu : (uint32_t)x;
+}
+struct PairRuns {   // floor(units * p / pairs); inv is pairs_inverse(pairs)
   int64_t units, each;
-  uint32_t rest, pairs;
-  __device__ __forceinline__ PairRuns(int64_t u, int n) : units(u), pairs((uint32_t)n) {
-    each = (int64_t)divide((uint64_t)u, pairs);
-    rest = (uint32_t)(u - each * n);
+  uint32_t rest, pairs, inv;
+  __device__ __forceinline__ PairRuns(int64_t u, int n, uint32_t v) : units(u), pairs((uint32_t)n), inv(v) {
+    int64_t left;
+    if ((uint64_t)u >> 32) {
+      each = (int64_t)((uint64_t)u / pairs);
+      left = u - each * n;
+    } else {   // the product with the inverse is off by one at most
+      each = __umulhi((uint32_t)u, inv);
+      left = u - each * n;
+      if (left < 0) {
+        --each;
+        left += n;
+      }
+      if (left >= n) {
+        ++each;
+        left -= n;
+      }
+    }
+    rest = (uint32_t)left;
   }
   __device__ __forceinline__ int64_t first(int p) const {
-    return each * p + (uint32_t)p * rest / pairs;
+    return each * p + __umulhi((uint32_t)p * rest, inv);   // p * rest below 2^14: exact
   }
   // the pair that has unit u: the last p with first(p) <= u
   __device__ __forceinline__ int of(int64_t u) const {
