@@ -298,7 +298,11 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   asm volatile("barrier.cluster.arrive.release.aligned;\n" ::: "memory");   // waited for after the plan
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
 
+  // The first segment is worked out here, in one copy of that code for all roles: it is fetched when it
+  // first runs (the roles' own copies took 2,000 to 2,500 cycles for it, 1 us).
   SegIter run = plan_run(a, pl, pair, warp, lane, s_plan, s_first);
+  Seg sg;
+  bool more = next_seg(a, pl, run, sg);
   asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // both CTAs: barriers, TMEM
   tc::fence_after();
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -306,7 +310,6 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   constexpr uint32_t tO = 0, tS = R / 2;
 
   bool ok = true;
-  Seg sg;
   if (warp == 0) {
     if (rank == 0) {
       // ================= MMA issuer =================
@@ -326,7 +329,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       auto ready = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_test(bar, phase)) != 0;
       };
-      while (__all_sync(0xffffffffu, ok && next_seg(a, pl, run, sg))) {
+      for (; __all_sync(0xffffffffu, ok && more); more = next_seg(a, pl, run, sg)) {
         ok = wait(q_full, nseg);
         ++nseg;
         const int nt = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
@@ -388,7 +391,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       // ================= CTA 1's Q and K arrivals =================
       if (lane == 0) {
         int ks = 0, nseg = 0;
-        while (ok && next_seg(a, pl, run, sg)) {
+        for (; ok && more; more = next_seg(a, pl, run, sg)) {
           ok = mbar_wait_bounded(q_land, nseg & 1);
           if (ok) tc::arrive_cluster(q_full, 0);
           ++nseg;
@@ -406,7 +409,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     if (lane == 0) {
       int ks = 0;
       const int last = (int)(a.pool.num_pages << a.pool.log2P);   // no row
-      while (ok && next_seg(a, pl, run, sg)) {
+      for (; ok && more; more = next_seg(a, pl, run, sg)) {
         int y = half_row(a.pool, sg.it.pt, sg.j0 * LD_T + 64 * (int)rank, sg.it.len, a.status);
         for (int j = sg.j0; j < sg.j1 && ok; ++j) {
           const int row = y;
@@ -442,7 +445,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
   } else if (warp == 2) {
     // ================= V's arrivals; positions past the last one cleared =================
     int vs = 0;
-    while (ok && next_seg(a, pl, run, sg))
+    for (; ok && more; more = next_seg(a, pl, run, sg))
       for (int j = sg.j0; j < sg.j1 && ok; ++j) {
         const int live = sg.it.len - j * LD_T;   // positions of this tile that there are
         for (int u = 0; u < L::U; ++u, ++vs) {
@@ -467,7 +470,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     // ================= V: this CTA's channels of all 128 positions =================
     if (lane == 0) {
       int vs = 0;
-      while (ok && next_seg(a, pl, run, sg))
+      for (; ok && more; more = next_seg(a, pl, run, sg))
         for (int j = sg.j0; j < sg.j1 && ok; ++j) {
           int row[2];
           for (int h = 0; h < 2; ++h)
@@ -498,7 +501,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       // (a barrier of its own: one that other tiles complete as well could be a phase behind, and its
       // parity then says yes too early)
       int nseg = 0;
-      while (ok && next_seg(a, pl, run, sg)) {
+      for (; ok && more; more = next_seg(a, pl, run, sg)) {
         if (nseg > 0 && !mbar_wait_bounded(q_free, (nseg - 1) & 1)) {
           ok = false;
           break;
@@ -534,7 +537,6 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     };
     int t = 0;
     Seg nx;
-    bool more = next_seg(a, pl, run, sg);
     // A wait that gave up ends the work but not the meetings: the warps of a row would wait for one
     // another for ever.
     while (more) {
