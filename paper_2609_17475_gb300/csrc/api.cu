@@ -210,6 +210,21 @@ int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows
   return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
 }
 
+// 3-D map over the same rows: (channel of a 64-channel chunk, row, chunk), box = 64 rows of box_chunks
+// chunks, which come to lie chunk after chunk.
+int bf16_chunks_map(const void* base, int64_t channels, int64_t rows, int box_chunks, CUtensorMap* map) {
+  EncodeTiledFn enc = encode_fn();
+  if (!enc) return JF_ERR_CUDA;
+  cuuint64_t dims[3] = {64, (cuuint64_t)rows, (cuuint64_t)channels / 64};
+  cuuint64_t strides[2] = {(cuuint64_t)channels * 2, 128};
+  cuuint32_t box[3] = {64, 64, (cuuint32_t)box_chunks};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides,
+                   box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? JF_OK : JF_ERR_CUDA;
+}
+
 // 3-D map over queries [C, H, 192], box = 64 channels of 128 queries of a head, 128B swizzle.
 int latent_query_map(const void* q, int64_t H, int64_t C, CUtensorMap* map) {
   EncodeTiledFn enc = encode_fn();

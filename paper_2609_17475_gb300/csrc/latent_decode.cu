@@ -46,7 +46,8 @@ struct LatentPlan {
   int32_t slot_rows;                // rows of a cut item's partial
   uint32_t inv;                     // of the pairs, for PairRuns
   int32_t item0[LAT_MAX_GROUPS + 1];     // first items of the groups
-  int64_t* starts;                  // [items + 1], in units of tiles
+  int64_t* units;                   // of the call, for the joins
+  int2* spans;                      // [items] first and last pair of its tiles, (0, -1) where it has none
   float* ml;                        // [rows][2]
   float* o;                         // [rows][R]
 };
@@ -61,7 +62,7 @@ struct LdSmem {
   static constexpr int CHUNK = 64 * 128;               // 64 rows of 128 bytes
   static constexpr int Q_BYTES = (R / 64 + 1) * CHUNK;
   static constexpr int K_BYTES = KC * CHUNK;
-  static constexpr int V_BYTES = 2 * 2 * CHUNK;        // [2 x 64 channels][128 positions][128 B]
+  static constexpr int V_BYTES = 2 * 2 * CHUNK;        // [2 x 64 positions][2 x 64 channels][64][128 B]
   static constexpr int OFF_K = Q_BYTES;
   static constexpr int OFF_V = OFF_K + KS * K_BYTES;
   static constexpr int OFF_P = OFF_V + VS * V_BYTES;   // [2 x 64 positions][64 rows][128 B]
@@ -165,8 +166,12 @@ struct LdFirst {   // a pair's first item
   int item, len;
 };
 
+__device__ __forceinline__ int2 span_of(const PairRuns& runs, int64_t at, int64_t n) {
+  return n ? make_int2(runs.of(at + LD_HDR), runs.of(at + n - 1)) : make_int2(0, -1);
+}
+
 // This pair's run of the items, which the last thread with items' units before it works out; every
-// thread takes part.  Block 0 writes the items' first units for the kernel that joins the partials.
+// thread takes part.  Block 0 writes down the items' pairs for the kernel that joins the partials.
 __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentPlan& pl, int pair, int warp,
                                             int lane, int64_t* s_plan, LdFirst* s_first) {
   SegIter run{0, 0, 0, pl.items, LD_ASK};
@@ -186,10 +191,10 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
     const int src = mine ? __ffs(mine) - 1 : 0;
     const int start = __shfl_sync(0xffffffffu, at, src), first_len = __shfl_sync(0xffffffffu, len, src);
     if (mine) run = SegIter{start, u0, u1, src, first_len};
-    if (blockIdx.x == 0 && warp == 0) {
+    if (blockIdx.x == 0 && warp == 2) {   // which is the last to have anything else to do
       if (len < 0) flag_error(a.status, JF_DEV_ERR_POSITION);
-      if (lane < pl.items) pl.starts[lane] = at;
-      if (lane == 31) pl.starts[pl.items] = incl;
+      if (lane < pl.items) pl.spans[lane] = span_of(runs, at, n);
+      if (lane == 31) *pl.units = incl;
     }
     return run;
   }
@@ -224,11 +229,11 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
     for (int i = i0; i < i1; ++i) {
       const int len = item_len(a, pl, i, item_group(pl, i));
       const int64_t next = at + units_of(len);
-      if (blockIdx.x == 0) pl.starts[i] = at;
+      if (blockIdx.x == 0) pl.spans[i] = span_of(runs, at, next - at);
       if (mine && at <= u0 && u0 < next) *s_first = LdFirst{at, i, len};
       at = next;
     }
-  if (blockIdx.x == 0 && threadIdx.x == 0) pl.starts[pl.items] = units;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *pl.units = units;
   __syncthreads();
   if (s_first->item >= 0) run = SegIter{s_first->start, u0, u1, s_first->item, s_first->len};
   return run;
@@ -236,8 +241,8 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
 
 template <int R>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LD_THREADS, 1)
-latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ CUtensorMap qmap,
-                     const __grid_constant__ LatentDecode a,
+latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+                     const __grid_constant__ CUtensorMap qmap, const __grid_constant__ LatentDecode a,
                      const __grid_constant__ LatentPlan pl) {
   using L = LdSmem<R>;
   constexpr uint32_t IDQK = idesc_bf16(LD_ROWS, LD_T, 0);
@@ -273,7 +278,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     return;
   }
   if (threadIdx.x == 0) {
-    prefetch_tensormap(&map);
+    prefetch_tensormap(&kmap);
+    prefetch_tensormap(&vmap);
     prefetch_tensormap(&qmap);
     for (int i = 0; i < 3; ++i) {
       mbar_init(&k_full[i], 2);
@@ -316,7 +322,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
       const uint32_t leader = elect_one();
       const uint64_t qd = tc::sdesc_sw128(smem_u32(sm), 16, 1024);
       const uint64_t kd = tc::sdesc_sw128(smem_u32(sm + L::OFF_K), 16, 1024);
-      const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), 128 * 128, 1024);
+      const uint64_t vd = tc::sdesc_sw128(smem_u32(sm + L::OFF_V), L::CHUNK, 1024);
       const uint64_t pd = tc::sdesc_sw128(smem_u32(sm + L::OFF_P), 16, 1024);
       auto wait = [&](uint64_t* bar, int phase) {
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
@@ -367,7 +373,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 #pragma unroll
             for (int k = 0; k < LD_T / 16; ++k)
               mma2_ss_if(leader, d, pd + (((k >> 2) * L::CHUNK + (k & 3) * 32) >> 4),
-                         v0 + ((k * 2048) >> 4), IDPV, (pi > 0 || k > 0) ? 1u : 0u);
+                         v0 + (((k >> 2) * 2 * L::CHUNK + (k & 3) * 2048) >> 4), IDPV, (pi > 0 || k > 0) ? 1u : 0u);
             tc::commit2_both_if(leader, &v_free[vs]);
             if (++vs == L::VS) {
               vs = 0;
@@ -425,10 +431,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             }
             uint64_t* const land = rank == 0 ? &k_full[st] : &k_land[st];
             mbar_arrive_expect_tx(land, L::K_BYTES);
-            const uint32_t dst = smem_u32(sm + L::OFF_K + st * L::K_BYTES);
-#pragma unroll
-            for (int k = 0; k < L::KC; ++k)
-              tma_load_2d(dst + k * L::CHUNK, &map, (c * L::KC + k) * 64, row, land);
+            tma_load_3d(smem_u32(sm + L::OFF_K + st * L::K_BYTES), &kmap, 0, row, c * L::KC, land);
             // The ring holds one tile, less than memory's latency calls for: what comes after it is brought
             // into the L2 cache meanwhile (from where V is read as well), a part with every stage.
             if (ahead < last) {
@@ -455,10 +458,9 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             break;
           }
           if (live < LD_T && (live & 63)) {   // past the half's end the copy brought zeros
-            const uint32_t at = smem_u32(sm + L::OFF_V + st * L::V_BYTES);
-            const int end = (live + 63) & ~63;
-            for (int p = live * 8 + lane; p < end * 8; p += 32)
-              for (int ch = 0; ch < 2; ++ch) sts128(at + ch * 2 * L::CHUNK + p * 16, 0u, 0u, 0u, 0u);
+            const uint32_t at = smem_u32(sm + L::OFF_V + st * L::V_BYTES + (live >> 6) * 2 * L::CHUNK);
+            for (int p = (live & 63) * 8 + lane; p < 64 * 8; p += 32)
+              for (int ch = 0; ch < 2; ++ch) sts128(at + ch * L::CHUNK + p * 16, 0u, 0u, 0u, 0u);
             fence_proxy_async_smem();
           }
           __syncwarp();
@@ -482,13 +484,9 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
               break;
             }
             mbar_arrive_expect_tx(&v_land[st], L::V_BYTES);
-            const uint32_t dst = smem_u32(sm + L::OFF_V + st * L::V_BYTES);
-#pragma unroll
-            for (int ch = 0; ch < 2; ++ch)
-#pragma unroll
-              for (int h = 0; h < 2; ++h)
-                tma_load_2d(dst + (2 * ch + h) * L::CHUNK, &map,
-                            u * 256 + (int)rank * 128 + ch * 64, row[h], &v_land[st]);
+            for (int h = 0; h < 2; ++h)
+              tma_load_3d(smem_u32(sm + L::OFF_V + st * L::V_BYTES + h * 2 * L::CHUNK), &vmap, 0, row[h],
+                          u * 4 + (int)rank * 2, &v_land[st]);
           }
         }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -509,8 +507,8 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         ++nseg;
         uint64_t* const land = rank == 0 ? q_full : q_land;
         mbar_arrive_expect_tx(land, L::Q_BYTES);
-        for (int c = 0; c < L::Q_BYTES / L::CHUNK; ++c)
-          tma_load_2d(smem_u32(sm) + c * L::CHUNK, &qmap, c * 64, sg.it.row0 + 64 * (int)rank, land);
+        for (int c = 0; c < L::KPT; ++c)
+          tma_load_3d(smem_u32(sm) + c * L::K_BYTES, &qmap, 0, sg.it.row0 + 64 * (int)rank, c * L::KC, land);
       }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     }
@@ -693,16 +691,82 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
 }
 
 // ---------------------------------------------------------------------------
-// Join the partials of each row that has any.  A CTA takes CH channels of a row: first
-// its partials' places and, a thread each, their weights; then a thread 4 channels, the
-// partials in turn over the groups of CH / 4 threads, eight loads in flight.
+// Join the partials of each row that has any.
 // ---------------------------------------------------------------------------
-constexpr int LM_THREADS = 256, LM_BATCH = 8;
+constexpr int LM_THREADS = 256, LM_BATCH = 8, LM_WARPS = LM_THREADS / 32;
+constexpr int LM_MAX = 256;   // partials of a row: at most 2 (pairs + 1)
 
+// The rows of a row's partials over prefixes: those of the prefix's item, then its own's.
+__device__ __forceinline__ int places_of(const LatentDecode& a, const LatentPlan& pl, uint32_t row, int lane,
+                                         int32_t* rows) {
+  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
+  const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
+  const int64_t units = *pl.units;
+  int g = 0;
+  while (a.first[g + 1] <= b) ++g;
+  const int at = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
+  const int2 span[2] = {pl.spans[pl.item0[g] + at / LD_ROWS],
+                        pl.spans[pl.prefix_items + b * pl.blocks + h / LD_ROWS]};
+  const int inside[2] = {at % LD_ROWS, h % LD_ROWS};
+  const PairRuns runs(units, pl.pairs, pl.inv);
+  int count = 0;
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    const int p0 = span[part].x, p1 = span[part].y;
+    if (p1 < p0) continue;   // nothing there
+    if (p0 == p1) {
+      if (lane == 0)
+        rows[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
+      ++count;
+      continue;
+    }
+    for (int p = p0 + lane; p - lane <= p1; p += 32) {   // those that have units at all
+      const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
+      const unsigned m = __ballot_sync(0xffffffffu, has);
+      if (has)
+        rows[count + __popc(m & ((1u << lane) - 1))] =
+            (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside[part];
+      count += __popc(m);
+    }
+  }
+  __syncwarp();
+  return count;
+}
+
+// Their weights, and one over the sum of all.
+__device__ __forceinline__ float weights_of(const LatentPlan& pl, int count, int lane, const int32_t* rows,
+                                            float2* w) {
+  float M = -INFINITY, S = 0.f;
+  for (int i = lane; i < count; i += 32) {
+    w[i] = *reinterpret_cast<const float2*>(pl.ml + (int64_t)rows[i] * 2);
+    M = fmaxf(M, w[i].x);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  for (int i = lane; i < count; i += 32) {
+    // no maximum at all: sums of zero, or NaN where every score was
+    const float f = M == -INFINITY ? 1.f : fast_exp2(w[i].x - M);
+    S = fmaf(f, w[i].y, S);
+    w[i].x = f;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+  __syncwarp();
+  return S != 0.f ? 1.f / S : 0.f;
+}
+
+__device__ __forceinline__ uint2 to_bf16(const float4& x, float f) {
+  return make_uint2(pack_bf16x2(x.x * f, x.y * f), pack_bf16x2(x.z * f, x.w * f));
+}
+
+// A CTA takes CH channels of a row: first its partials' places and, a thread each, their weights; then a
+// thread 4 channels, the partials in turn over the groups of CH / 4 threads, eight loads in flight.  (Places
+// and weights by each warp on its own, as below, took one request of 131,072 positions x 128 heads 41.7 us
+// for 40.6.)
 template <int R, int CH>
 __global__ void __launch_bounds__(LM_THREADS)
 latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
-  constexpr int LANES = CH / 4, GROUPS = LM_THREADS / LANES, WARPS = LM_THREADS / 32;
+  constexpr int LANES = CH / 4, GROUPS = LM_THREADS / LANES, WARPS = LM_WARPS;
   __shared__ float s_w[LM_THREADS];
   __shared__ int32_t s_row[LM_THREADS];
   __shared__ float s_red[2][WARPS];
@@ -713,12 +777,12 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (int)threadIdx.x % LANES, grp = (int)threadIdx.x / LANES;
   const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
-  const PairRuns runs(pl.starts[pl.items], pl.pairs, pl.inv);
   for (uint32_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
     const uint32_t row = slice / (R / CH);
     const int ch = (int)(slice % (R / CH)) * CH + c * 4;
     const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
     // the row's partials: those of the prefix's item, then its own's
+    const int64_t units = *pl.units;
     int count = 0;
     bool direct = false;
     for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
@@ -733,9 +797,9 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
         item = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
         inside = h % LD_ROWS;
       }
-      const int64_t s0 = pl.starts[item] + LD_HDR, s1 = pl.starts[item + 1];
-      if (s1 <= s0) continue;   // nothing there
-      const int p0 = runs.of(s0), p1 = runs.of(s1 - 1);
+      const int2 span = pl.spans[item];
+      const int p0 = span.x, p1 = span.y;
+      if (p1 < p0) continue;   // nothing there
       if (p0 == p1) {
         if (a.num_groups == 0) direct = true;
         if (threadIdx.x == 0)
@@ -744,6 +808,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
         continue;
       }
       // pairs between the first and the last that have units at all
+      const PairRuns runs(units, pl.pairs, pl.inv);
       const int p = p0 + (int)threadIdx.x;
       const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
       const unsigned m = __ballot_sync(0xffffffffu, has);
@@ -818,71 +883,28 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
         acc.w += x.w;
       }
       const float inv = S != 0.f ? 1.f / S : 0.f;
-      *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) =
-          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+      *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) = to_bf16(acc, inv);
     }
     __syncthreads();
   }
 }
 
 // The same for many rows over prefixes, each with a pair's part or more to join: a warp 128 channels
-// of a row, on its own, its places and weights worked out without the other warps.
-constexpr int LW_MAX = 256;   // partials of a row: at most 2 (pairs + 1)
-
+// of a row, its places and weights worked out on its own.
 template <int R>
 __global__ void __launch_bounds__(LM_THREADS)
 latent_merge_rows_kernel(const __grid_constant__ LatentDecode a, const __grid_constant__ LatentPlan pl) {
-  __shared__ int32_t s_row[LM_THREADS / 32][LW_MAX];
-  __shared__ float2 s_w[LM_THREADS / 32][LW_MAX];   // (m, l), then the weight
+  __shared__ int32_t s_row[LM_WARPS][LM_MAX];
+  __shared__ float2 s_w[LM_WARPS][LM_MAX];   // (m, l), then the weight
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
-  const uint32_t slice = blockIdx.x * (LM_THREADS / 32) + warp, row = slice / (R / 128);
+  const uint32_t slice = blockIdx.x * LM_WARPS + warp, row = slice / (R / 128);
   const int ch = (int)(slice % (R / 128)) * 128 + lane * 4;
-  if (row >= total) return;
-  const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
+  if (row >= (uint32_t)a.batch * (uint32_t)a.H) return;
   int32_t* const rows = s_row[warp];
   float2* const w = s_w[warp];
-  // the row's partials: those of the prefix's item, then its own's
-  int item[2], inside[2];
-  int64_t s0[2] = {0, 0}, s1[2] = {0, 0};
-  item[1] = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
-  inside[1] = h % LD_ROWS;
-  if (a.num_groups) {
-    int g = 0;
-    while (a.first[g + 1] <= b) ++g;
-    const int at = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
-    item[0] = pl.item0[g] + at / LD_ROWS;
-    inside[0] = at % LD_ROWS;
-    s0[0] = pl.starts[item[0]] + LD_HDR;
-    s1[0] = pl.starts[item[0] + 1];
-  }
-  s0[1] = pl.starts[item[1]] + LD_HDR;
-  s1[1] = pl.starts[item[1] + 1];
-  const PairRuns runs(pl.starts[pl.items], pl.pairs, pl.inv);
-  int count = 0;
-#pragma unroll
-  for (int part = 0; part < 2; ++part) {
-    if (s1[part] <= s0[part]) continue;   // nothing there
-    const int p0 = runs.of(s0[part]), p1 = runs.of(s1[part] - 1);
-    if (p0 == p1) {
-      if (a.num_groups == 0) return;      // written out already
-      if (lane == 0)
-        rows[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
-      ++count;
-      continue;
-    }
-    for (int p = p0 + lane; p - lane <= p1; p += 32) {   // those that have units at all
-      const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
-      const unsigned m = __ballot_sync(0xffffffffu, has);
-      if (has)
-        rows[count + __popc(m & ((1u << lane) - 1))] =
-            (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside[part];
-      count += __popc(m);
-    }
-  }
-  __syncwarp();
+  const int count = places_of(a, pl, row, lane, rows);
   const float* const src = pl.o + ch;
   float4 v[LM_BATCH];
   auto load = [&](int i) {
@@ -891,21 +913,7 @@ latent_merge_rows_kernel(const __grid_constant__ LatentDecode a, const __grid_co
       if (i + k < count) v[k] = *reinterpret_cast<const float4*>(src + (int64_t)rows[i + k] * R);
   };
   load(0);   // under way while the weights are worked out
-  float M = -INFINITY, S = 0.f;
-  for (int i = lane; i < count; i += 32) {
-    w[i] = *reinterpret_cast<const float2*>(pl.ml + (int64_t)rows[i] * 2);
-    M = fmaxf(M, w[i].x);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-  for (int i = lane; i < count; i += 32) {
-    const float f = M == -INFINITY ? 1.f : fast_exp2(w[i].x - M);
-    S = fmaf(f, w[i].y, S);
-    w[i].x = f;
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
-  __syncwarp();
+  const float inv = weights_of(pl, count, lane, rows, w);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i = 0; i < count; i += LM_BATCH) {
 #pragma unroll
@@ -919,9 +927,7 @@ latent_merge_rows_kernel(const __grid_constant__ LatentDecode a, const __grid_co
       }
     load(i + LM_BATCH);
   }
-  const float inv = S != 0.f ? 1.f / S : 0.f;
-  *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) =
-      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) = to_bf16(acc, inv);
 }
 
 // ---------------------------------------------------------------------------
@@ -944,8 +950,14 @@ size_t latent_decode_workspace_bytes(int64_t batch, int64_t H, int64_t R, int64_
 }
 
 template <int R>
-static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const LatentDecode& a,
-                    const LatentPlan& pl, cudaStream_t stream) {
+static int launch_t(const LatentDecode& a, const LatentPlan& pl, cudaStream_t stream) {
+  // a copy brings 64 rows of several 64-channel chunks: issued one chunk a copy, a tile's K alone kept its
+  // thread for 0.6 us
+  CUtensorMap kmap, vmap, qmap;
+  int st = bf16_chunks_map(a.pool.base, a.pool.row, a.pool.num_pages * a.pool.P, LdSmem<R>::KC, &kmap);
+  if (!st) st = bf16_chunks_map(a.pool.base, a.pool.row, a.pool.num_pages * a.pool.P, 2, &vmap);
+  if (!st) st = bf16_chunks_map(a.q, a.pool.row, (int64_t)a.batch * a.H, LdSmem<R>::KC, &qmap);
+  if (st) return st;
   if (smem_optin((const void*)latent_decode_kernel<R>, LdSmem<R>::TOTAL) != JF_OK) return JF_ERR_CUDA;
   cudaLaunchAttribute pdl[1];
   pdl[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -957,7 +969,7 @@ static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const Laten
   cfg.stream = stream;
   cfg.attrs = pdl;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, map, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
+  if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, kmap, vmap, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
   // Few rows: 128 channels a CTA, so that more of the GPU takes part (one request of 131,072 positions
   // x 128 heads 43 us, a warp a piece 90).  Many: a CTA a row, since most of a decode's rows have a few
   // parts or none (32 mixed requests 102.9 us, a warp a piece 104.3, 128 channels a CTA 110); over
@@ -975,21 +987,17 @@ static int launch_t(const CUtensorMap& map, const CUtensorMap& qmap, const Laten
     cfg.gridDim = dim3((unsigned)(rows < 16 * pl.pairs ? rows : 16 * pl.pairs));
     e = cudaLaunchKernelEx(&cfg, latent_merge_kernel<R, R>, a, pl);
   } else {
-    cfg.gridDim = dim3((unsigned)((slices + LM_THREADS / 32 - 1) / (LM_THREADS / 32)));
+    cfg.gridDim = dim3((unsigned)((slices + LM_WARPS - 1) / LM_WARPS));
     e = cudaLaunchKernelEx(&cfg, latent_merge_rows_kernel<R>, a, pl);
   }
   return e == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 
 int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t stream) {
-  CUtensorMap map, qmap;
-  int st = bf16_rows_map(a.pool.base, a.pool.row, a.pool.num_pages * a.pool.P, 64, &map);
-  if (!st) st = bf16_rows_map(a.q, a.pool.row, (int64_t)a.batch * a.H, 64, &qmap);
-  if (st) return st;
   LatentPlan pl;
   int64_t items, slot_rows, rows;
   const int sms = sm_count();
-  if (sms / 2 > LW_MAX / 2 - 2) return JF_ERR_UNSUPPORTED;
+  if (sms / 2 > LM_MAX / 2 - 2) return JF_ERR_UNSUPPORTED;
   plan_sizes(a.batch, a.H, a.num_groups, sms, &items, &slot_rows, &rows);
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
   pl.pairs = sms / 2;
@@ -1001,13 +1009,13 @@ int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t st
     pl.item0[g + 1] = pl.item0[g] + ((a.first[g + 1] - a.first[g]) * a.H + LD_ROWS - 1) / LD_ROWS;
   pl.prefix_items = a.num_groups ? pl.item0[a.num_groups] : 0;
   pl.items = pl.prefix_items + a.batch * pl.blocks;
-  pl.starts = reinterpret_cast<int64_t*>(ws);
+  pl.units = reinterpret_cast<int64_t*>(ws);
+  pl.spans = reinterpret_cast<int2*>(ws) + 1;
   ws += round256((items + 1) * 8);
   pl.ml = reinterpret_cast<float*>(ws);
   ws += round256(rows * 8);
   pl.o = reinterpret_cast<float*>(ws);
-  return a.pool.R == 512 ? launch_t<512>(map, qmap, a, pl, stream)
-                         : launch_t<256>(map, qmap, a, pl, stream);
+  return a.pool.R == 512 ? launch_t<512>(a, pl, stream) : launch_t<256>(a, pl, stream);
 }
 
 }  // namespace jfkv

@@ -7,6 +7,7 @@
 namespace jfkv {
 
 int bf16_rows_map(const void* base, int64_t channels, int64_t rows, int box_rows, CUtensorMap* map);
+int bf16_chunks_map(const void* base, int64_t channels, int64_t rows, int box_chunks, CUtensorMap* map);
 int sm_count();
 
 inline int64_t round256(int64_t n) { return (n + 255) / 256 * 256; }
@@ -57,6 +58,14 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map
       "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
       " [%0], [%1, {%2, %3}], [%4];\n"
       ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z,
+                                            uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];\n"
+      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
 }
 
 // 32 lanes x 16 columns of 32-bit words
