@@ -34,7 +34,10 @@ namespace jfkv {
 
 constexpr int LD_T = 128;           // positions a tile
 constexpr int LD_ROWS = 128;        // rows a pair, 64 each CTA
-constexpr int LD_HDR = 2;           // an item's fixed cost, in tiles
+// An item's fixed cost in tiles, its queries' way in and its partials' way out: more where both CTAs have
+// rows.  (2 x 4 continuations x 128 heads 21.8 us with 4 there, 23.9 with 2; 64 continuations x 16 heads
+// 56.4 and 57.0.)
+constexpr int LD_HDR = 2, LD_HDR_FULL = 4;
 constexpr int LD_THREADS = 32 * 13;
 constexpr int LD_SOFT = 8;           // softmax warps
 constexpr int LD_SBUF = 4;          // S buffers: S may be this many tiles ahead of P V
@@ -102,9 +105,12 @@ __device__ __forceinline__ int item_alone(const LatentPlan& pl, int g) {
 }
 
 __device__ __forceinline__ int tiles_of(int len) { return len <= 0 ? 0 : (len + LD_T - 1) / LD_T; }
-__device__ __forceinline__ int64_t units_of(int len) {
+__device__ __forceinline__ int header_of(const LatentDecode& a, int g) {
+  return g >= 0 || a.H > LD_ROWS / 2 ? LD_HDR_FULL : LD_HDR;
+}
+__device__ __forceinline__ int64_t units_of(const LatentDecode& a, int g, int len) {
   const int n = tiles_of(len);
-  return n ? n + LD_HDR : 0;
+  return n ? n + header_of(a, g) : 0;
 }
 
 __device__ __forceinline__ LatentItem item_of(const LatentDecode& a, const LatentPlan& pl, int i,
@@ -144,10 +150,10 @@ __device__ __forceinline__ bool next_seg(const LatentDecode& a, const LatentPlan
     const int len = s.len != LD_ASK ? s.len : item_len(a, pl, s.item, g);
     s.len = LD_ASK;
     const int n = tiles_of(len);
-    const int64_t first = s.start + LD_HDR;   // unit of tile 0
+    const int64_t first = s.start + header_of(a, g);   // unit of tile 0
     const int64_t lo = max((int64_t)0, s.u0 - first), hi = min((int64_t)n, s.u1 - first);
     const int i = s.item++;
-    if (n) s.start += n + LD_HDR;
+    if (n) s.start += n + header_of(a, g);
     if (lo < hi) {
       seg.it = item_of(a, pl, i, g, len);
       seg.item = i;
@@ -166,8 +172,8 @@ struct LdFirst {   // a pair's first item
   int item, len;
 };
 
-__device__ __forceinline__ int2 span_of(const PairRuns& runs, int64_t at, int64_t n) {
-  return n ? make_int2(runs.of(at + LD_HDR), runs.of(at + n - 1)) : make_int2(0, -1);
+__device__ __forceinline__ int2 span_of(const PairRuns& runs, int64_t at, int header, int64_t n) {
+  return n ? make_int2(runs.of(at + header), runs.of(at + n - 1)) : make_int2(0, -1);
 }
 
 // This pair's run of the items, which the last thread with items' units before it works out; every
@@ -176,8 +182,9 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
                                             int lane, int64_t* s_plan, LdFirst* s_first) {
   SegIter run{0, 0, 0, pl.items, LD_ASK};
   if (pl.items <= 32) {   // an item a lane, each warp by itself
-    const int len = lane < pl.items ? item_len(a, pl, lane, item_group(pl, lane)) : 0;
-    const int n = (int)units_of(len);
+    const int g = item_group(pl, lane);
+    const int len = lane < pl.items ? item_len(a, pl, lane, g) : 0;
+    const int n = (int)units_of(a, g, len);
     int incl = n;   // below 2^30
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -193,7 +200,7 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
     if (mine) run = SegIter{start, u0, u1, src, first_len};
     if (blockIdx.x == 0 && warp == 2) {   // which is the last to have anything else to do
       if (len < 0) flag_error(a.status, JF_DEV_ERR_POSITION);
-      if (lane < pl.items) pl.spans[lane] = span_of(runs, at, n);
+      if (lane < pl.items) pl.spans[lane] = span_of(runs, at, header_of(a, g), n);
       if (lane == 31) *pl.units = incl;
     }
     return run;
@@ -202,9 +209,9 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
   const int i0 = min(pl.items, (int)threadIdx.x * per), i1 = min(pl.items, i0 + per);
   int64_t sum = 0;
   for (int i = i0; i < i1; ++i) {
-    const int len = item_len(a, pl, i, item_group(pl, i));
+    const int g = item_group(pl, i), len = item_len(a, pl, i, g);
     if (len < 0 && blockIdx.x == 0) flag_error(a.status, JF_DEV_ERR_POSITION);
-    sum += units_of(len);
+    sum += units_of(a, g, len);
   }
   int64_t incl = sum;
 #pragma unroll
@@ -227,9 +234,9 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
   const bool mine = u0 < u1 && at <= u0 && u0 < at + sum;
   if (mine || blockIdx.x == 0)
     for (int i = i0; i < i1; ++i) {
-      const int len = item_len(a, pl, i, item_group(pl, i));
-      const int64_t next = at + units_of(len);
-      if (blockIdx.x == 0) pl.spans[i] = span_of(runs, at, next - at);
+      const int g = item_group(pl, i), len = item_len(a, pl, i, g);
+      const int64_t next = at + units_of(a, g, len);
+      if (blockIdx.x == 0) pl.spans[i] = span_of(runs, at, header_of(a, g), next - at);
       if (mine && at <= u0 && u0 < next) *s_first = LdFirst{at, i, len};
       at = next;
     }

@@ -474,14 +474,16 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
   tc::fence_after();
+  // the first segment, in one copy of that code for all roles: it is fetched when it first runs
   ChunkIter run = chunk_run(a, pair);
+  ChunkSeg sg;
+  bool more = next_chunk_seg(a, run, sg);
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the keys and values have been written
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   // all 512 columns are this CTA's: O from 0, the S buffers behind it
   constexpr uint32_t tO = 0, tS = 128;
 
   bool ok = true;
-  ChunkSeg sg;
   if (warp == 0) {
     if (rank == 0) {
       // ================= MMA issuer (the whole warp: control flow stays uniform) ==========
@@ -496,8 +498,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         return __all_sync(0xffffffffu, mbar_wait_bounded(bar, phase & 1)) != 0;
       };
       ChunkIter prun = run;
-      int qi = 0, qleft = 0, qseg = 0, pi = 0, pleft = 0, pseg = 0;
-      bool fresh_q = false, fresh_o = false, more = true;   // the segment's first S, its first P V
+      const int first = __shfl_sync(0xffffffffu, more ? sg.j1 - sg.j0 : 0, 0);
+      int qi = 0, qleft = first, qseg = 0, pi = 0, pleft = 0, pseg = 0;
+      bool fresh_q = true, fresh_o = false;   // the segment's first S, its first P V
       while (ok) {
         if (qleft == 0 && more) {
           more = __all_sync(0xffffffffu, next_chunk_seg(a, run, sg)) != 0;
@@ -528,10 +531,13 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           }
         } else if (pi < qi) {
           if (pleft == 0) {
-            next_chunk_seg(a, prun, sg);
-            pleft = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
+            pleft = first;
+            if (pseg > 0) {
+              next_chunk_seg(a, prun, sg);
+              pleft = __shfl_sync(0xffffffffu, sg.j1 - sg.j0, 0);
+              ok = wait(o_free, pseg - 1);
+            }
             fresh_o = true;
-            if (pseg > 0) ok = wait(o_free, pseg - 1);
             ++pseg;
           }
           const int st = pi % LA_VS;
@@ -561,7 +567,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         ok = mbar_wait_bounded(&v_land[T % LA_VS], (T / LA_VS) & 1);
         if (ok) tc::arrive_cluster(&v_full[T % LA_VS], 0);
       };
-      while (ok && next_chunk_seg(a, run, sg))
+      for (; ok && more; more = next_chunk_seg(a, run, sg))
         for (int j = sg.j0; j < sg.j1 && ok; ++j, ++t) {
           ok = mbar_wait_bounded(&k_land[t % LA_KS], (t / LA_KS) & 1);
           if (ok) tc::arrive_cluster(&k_full[t % LA_KS], 0);
@@ -575,7 +581,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= K: this CTA's 64 positions of each tile =================
     if (lane == 0) {
       int t = 0;
-      while (ok && next_chunk_seg(a, run, sg)) {
+      for (; ok && more; more = next_chunk_seg(a, run, sg)) {
         int y = half_row(a.pool, a.pt, sg.j0 * LP_T + 64 * (int)rank, a.n, a.status);
         for (int j = sg.j0; j < sg.j1; ++j, ++t) {
           const int row = y, st = t % LA_KS, pos = j * LP_T + 64 * (int)rank;
@@ -600,7 +606,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= V: this CTA's 64 channels of all 128 positions =================
     if (lane == 0) {
       int t = 0;
-      while (ok && next_chunk_seg(a, run, sg))
+      for (; ok && more; more = next_chunk_seg(a, run, sg))
         for (int j = sg.j0; j < sg.j1; ++j, ++t) {
           const int st = t % LA_VS;
           if (t >= LA_VS && !mbar_wait_bounded(&v_free[st], (t / LA_VS - 1) & 1)) {
@@ -619,7 +625,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= Q: 128 rows; zeros past the chunk's end =================
     if (lane == 0) {
       int nseg = 0;
-      while (ok && next_chunk_seg(a, run, sg)) {
+      for (; ok && more; more = next_chunk_seg(a, run, sg)) {
         if (nseg > 0 && !mbar_wait_bounded(q_free, (nseg - 1) & 1)) {
           ok = false;
           break;
@@ -647,7 +653,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     const uint64_t kk = f32x2(sc, sc);
     int t0 = 0, seg = 0;   // tiles and number of the segments before
     // A wait that gave up ends the work but not the meetings: the other group would wait for ever.
-    for (; next_chunk_seg(a, run, sg); ++seg) {
+    for (; more; more = next_chunk_seg(a, run, sg), ++seg) {
       const int row0 = sg.qt * LP_Q + 128 * (int)rank + quarter * 32;   // the warp's first query
       auto limit_of = [&](int q) { return a.causal ? min(a.q_start + q, a.n - 1) : a.n - 1; };
       const int limit = limit_of(row0 + lane);         // last position seen
