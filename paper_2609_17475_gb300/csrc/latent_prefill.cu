@@ -93,39 +93,30 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0);   // uniform
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
-  const int pair = (int)(blockIdx.x >> 1), pairs = (int)(gridDim.x >> 1);
+  const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   if (smem_u32(sm) & 1023u) {   // the same in both CTAs
     if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
     return;
   }
-  if (threadIdx.x == 0) {
-    prefetch_tensormap(&pmap);
-    prefetch_tensormap(rank ? &vmap : &kmap);
-    for (int i = 0; i < LE_STAGES; ++i) {
-      mbar_init(&b_full[i], 2);
-      mbar_init(&b_land[i], 1);
-      mbar_init(&b_free[i], 1);
-    }
-    for (int i = 0; i < LE_CHUNKS; ++i) {
-      mbar_init(&a_full[i], 2);
-      mbar_init(&a_land[i], 1);
-    }
-    mbar_init(a_free, 1);
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(&d_full[i], 1);
-      mbar_init(&d_free[i], 16);
-    }
+  if (warp == 0) {
+    tc::alloc2(tmem_slot, 512);
+  } else if (warp == 1) {   // a barrier a thread
+    if (lane == 0) prefetch_tensormap(&pmap);
+    if (lane == 1) prefetch_tensormap(rank ? &vmap : &kmap);
+    // b_full, a_full: both CTAs; d_free: their 16 warps; the others one arrival
+    mbar_init(&bars[lane], lane < 12 ? 2 : lane >= 31 ? 16 : 1);
+    if (lane == 0) mbar_init(&bars[32], 16);
     fence_barrier_init();
   }
-  if (warp == 0) tc::alloc2(tmem_slot, 512);
+  // tiles of a pass: below 2^24, and their product with the pairs below 2^31
+  const uint32_t tiles = (uint32_t)(a.n_pad / 256) * (uint32_t)a.heads;
+  const uint32_t i0 = tiles * pair / pairs, i1 = tiles * (pair + 1) / pairs;
+  int pt = (int)(i0 / a.heads), hl = (int)(i0 - pt * a.heads);   // of the current tile
+  const int count = (int)(i1 - i0), steps = a.pool.R / 64;
   tc::fence_before();
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
   tc::fence_after();
-  const int64_t tiles = (int64_t)(a.n_pad / 256) * a.heads;
-  const int64_t i0 = tiles * pair / pairs, i1 = tiles * (pair + 1) / pairs;
-  int pt = (int)(i0 / a.heads), hl = (int)(i0 - (int64_t)pt * a.heads);   // of the current tile
-  const int count = (int)(i1 - i0), steps = a.pool.R / 64;
   auto advance = [&] {
     if (++hl == a.heads) {
       hl = 0;
@@ -442,42 +433,26 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
     return;
   }
-  if (threadIdx.x == 0) {
-    prefetch_tensormap(&qmap);
-    prefetch_tensormap(&pmap);
-    prefetch_tensormap(&kmap);
-    prefetch_tensormap(&vmap);
-    for (int i = 0; i < LA_KS; ++i) {
-      mbar_init(&k_full[i], 2);
-      mbar_init(&k_land[i], 1);
-      mbar_init(&k_free[i], 1);
-    }
-    for (int i = 0; i < LA_VS; ++i) {
-      mbar_init(&v_full[i], 2);
-      mbar_init(&v_land[i], 1);
-      mbar_init(&v_free[i], 1);
-    }
-    for (int i = 0; i < LA_SB; ++i) mbar_init(&s_full[i], 1);
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&p_ready[i], 8);
-      mbar_init(&pv_done[i], 1);
-    }
-    for (int i = 0; i < 16; ++i) mbar_init(&m_bar[i], 1);
-    mbar_init(q_full, 2);
-    mbar_init(q_land, 1);
-    mbar_init(q_free, 1);
-    mbar_init(o_free, 8);
+  if (warp == 0) {
+    tc::alloc2(tmem_slot, 512);
+  } else if (warp == 1) {   // a barrier a thread
+    if (lane == 0) prefetch_tensormap(&qmap);
+    if (lane == 1) prefetch_tensormap(&pmap);
+    if (lane == 2) prefetch_tensormap(&kmap);
+    if (lane == 3) prefetch_tensormap(&vmap);
+    // k_full, v_full, q_full: both CTAs; p_ready, o_free: their eight warps; the others one arrival
+    mbar_init(&bars[lane], lane < 8 ? 2 : lane < 12 ? 8 : 1);
+    if (lane < 20) mbar_init(&bars[32 + lane], lane == 19 ? 8 : 1);
     fence_barrier_init();
   }
-  if (warp == 0) tc::alloc2(tmem_slot, 512);
-  tc::fence_before();
-  __syncthreads();
-  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
-  tc::fence_after();
   // the first segment, in one copy of that code for all roles: it is fetched when it first runs
   ChunkIter run = chunk_run(a, pair);
   ChunkSeg sg;
   bool more = next_chunk_seg(a, run, sg);
+  tc::fence_before();
+  __syncthreads();
+  tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
+  tc::fence_after();
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the keys and values have been written
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   // all 512 columns are this CTA's: O from 0, the S buffers behind it
@@ -884,6 +859,18 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   __syncthreads();
   const int n = s_n, q0 = sg.qt * LP_Q + row0;
   if (q0 >= a.C) return;
+  // the first parts, under way while the weights are worked out
+  const float* const o = a.o + (int64_t)row0 * 128 + lane * 4;
+  float4 v[2][LJ_ROWS];
+  auto load = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int k = 0; k < LJ_ROWS; ++k)   // rows past the chunk's end: whatever is there
+        if (i + u < n)
+          v[u][k] = *reinterpret_cast<const float4*>(o + ((int64_t)s_slot[i + u] * LP_Q + k) * 128);
+  };
+  load(0);
   // weights: eight lanes a row
   const int sub = lane & 7, mine = lane >> 3;
   const float* const ml = a.ml + (int64_t)(row0 + mine) * 2;
@@ -903,15 +890,7 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   float4 acc[LJ_ROWS];
 #pragma unroll
   for (int k = 0; k < LJ_ROWS; ++k) acc[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float* const o = a.o + (int64_t)row0 * 128 + lane * 4;
   for (int i = 0; i < n; i += 2) {
-    float4 v[2][LJ_ROWS];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int k = 0; k < LJ_ROWS; ++k)   // rows past the chunk's end: whatever is there
-        if (i + u < n)
-          v[u][k] = *reinterpret_cast<const float4*>(o + ((int64_t)s_slot[i + u] * LP_Q + k) * 128);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -923,6 +902,7 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
           acc[k].z = fmaf(v[u][k].z, w, acc[k].z);
           acc[k].w = fmaf(v[u][k].w, w, acc[k].w);
         }
+    load(i + 2);
   }
 #pragma unroll
   for (int k = 0; k < LJ_ROWS; ++k) {
