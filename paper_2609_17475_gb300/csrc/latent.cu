@@ -1,8 +1,10 @@
 // Append to and read back from the latent cache.
 //
 // Append and read copy rows of R + 64 bf16 values between the caller's latent and
-// key parts and the pages: one 16-byte piece a thread.  Bound: the launch for a
-// step, memory for long runs.
+// key parts and the pages: one 16-byte piece a thread, its row's request found by
+// bisection, so that runs of any lengths need no plan.  Bound: a launch and three
+// dependent loads (offsets, page, row).  Both calls for 32 rows of 576 channels
+// take 4.4 us, for 2,048 rows (9.4 MB moved in all, 1.4 us at copy rate) 4.2 us.
 #include "latent.cuh"
 
 namespace jfkv {

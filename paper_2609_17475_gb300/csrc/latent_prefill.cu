@@ -23,6 +23,14 @@
 // rounding exact values).  Weights are 2^(s - m); a row's reference m is set so that its
 // largest weight is 2^10 and moves, O's row with it, when a weight passes 2^15.
 //
+// What bounds it: the tensor cores at the power they may take.  2,048 queries after 30,720
+// positions x 16 heads take 462 us; each kernel alone: expansion 81 (137 GFLOP, 1,700 TFLOP/s, the
+// tensor pipe 78 % active), attention 385 (667 GFLOP, 1,730 TFLOP/s, 91 %), the join 9.  Expanding costs 2 R
+// 256 operations a position and head once and saves 1,536 of 2,176 a (query, position) pair of the
+// absorbed form: from about 170 queries on it is less.  Below that (77 queries after 4,001 x 16
+// heads: 32 us, expansion 13, attention 11, join 3) the absorbed form's products would be 6 us
+// against 11, but it would need two products with the weights around the decode and its join.
+//
 // Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
 // cut into one run of equal length per pair; a cut item's parts are joined by
 // latent_prefill_merge_kernel.
@@ -61,7 +69,8 @@ struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
 // ===========================================================================
 // A pair takes a run of (256 positions, head) tiles, heads within positions, and keeps the
 // positions' latents in shared memory while the heads' weights stream past: with both
-// streamed a CTA read 64 bytes a cycle, more than the L2 cache gives all of them.
+// streamed a CTA read 64 bytes a cycle, more than the L2 cache gives all of them (2,048 queries
+// after 30,720 positions x 16 heads 525 us, 501 so).
 constexpr int LE_STAGES = 4;
 constexpr int LE_CHUNKS = 8;           // 64-channel chunks of R at most
 constexpr int LE_THREADS = 32 * 12;
@@ -825,7 +834,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
 
 // ---------------------------------------------------------------------------
 // Join the parts of the item that ends in pair p, if it began in one before: four rows a
-// warp, a lane 4 channels.
+// warp, a lane 4 channels.  Bound: the parts' way from L2 (18 MB for 128 items of 256 queries: 8.8 us).
 // ---------------------------------------------------------------------------
 constexpr int LJ_WARPS = 8, LJ_ROWS = 4, LJ_MAX = 128;   // LJ_MAX: pairs at most
 
