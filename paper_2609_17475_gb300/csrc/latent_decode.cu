@@ -183,10 +183,6 @@ struct LdFirst {   // a pair's first item
   int item, len;
 };
 
-__device__ __forceinline__ int2 span_of(const PairRuns& runs, int64_t at, int header, int64_t n) {
-  return n ? make_int2(runs.of(at + header), runs.of(at + n - 1)) : make_int2(0, -1);
-}
-
 // This pair's run of the items, which the last thread with items' units before it works out; every
 // thread takes part.  Block 0 writes down the items' pairs for the kernel that joins the partials.
 __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentPlan& pl, int pair, int warp,
@@ -211,7 +207,11 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
     if (mine) run = SegIter{start, u0, u1, src, first_len};
     if (blockIdx.x == 0 && warp == 2) {   // which is the last to have anything else to do
       if (len < 0) flag_error(a.status, JF_DEV_ERR_POSITION);
-      if (lane < pl.items) pl.spans[lane] = span_of(runs, at, header_of(a, g), n);
+      if (lane < pl.items) {
+        int2 span = make_int2(0, -1);
+        if (n) span = make_int2(runs.of(at + header_of(a, g)), runs.of(incl - 1));
+        pl.spans[lane] = span;
+      }
       if (lane == 31) *pl.units = incl;
     }
     return run;
@@ -243,11 +243,23 @@ __device__ __forceinline__ SegIter plan_run(const LatentDecode& a, const LatentP
   const PairRuns runs(units, pl.pairs, pl.inv);
   const int64_t u0 = runs.first(pair), u1 = runs.first(pair + 1);
   const bool mine = u0 < u1 && at <= u0 && u0 < at + sum;
+  int p = blockIdx.x == 0 && sum ? runs.of(at) : 0;   // the pair that has the unit looked at
+  auto pair_of = [&](int64_t u) {
+    while (runs.first(p + 1) <= u) ++p;
+    return p;
+  };
   if (mine || blockIdx.x == 0)
     for (int i = i0; i < i1; ++i) {
       const int g = item_group(pl, i), len = item_len(a, pl, i, g);
       const int64_t next = at + units_of(a, g, len);
-      if (blockIdx.x == 0) pl.spans[i] = span_of(runs, at, header_of(a, g), next - at);
+      if (blockIdx.x == 0) {
+        int2 span = make_int2(0, -1);
+        if (next > at) {
+          span.x = pair_of(at + header_of(a, g));
+          span.y = pair_of(next - 1);
+        }
+        pl.spans[i] = span;
+      }
       if (mine && at <= u0 && u0 < next) *s_first = LdFirst{at, i, len};
       at = next;
     }

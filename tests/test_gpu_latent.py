@@ -137,6 +137,26 @@ def test_decode_of_many_requests():
         check(out[b], q[b], O.gather(pool, table[b], n), T.SCALE)
 
 
+def test_more_requests_than_threads():
+    rng = np.random.default_rng(12)
+    ctx = [int(n) for n in rng.integers(0, 130, 1500)]
+    ctx[700], ctx[1499] = 20000, 3000
+    table, pool = T.filled(rng, 256, 64, ctx)
+    q = T.queries(rng, 1500, 4, 256)
+    out, st = run_decode(table, pool, ctx, q, T.SCALE)
+    assert st == 0
+    for b, n in enumerate(ctx):
+        check(out[b], q[b], O.gather(pool, table[b], n), T.SCALE)
+    off, plens = [0, 1, 300, 300, 1100, 1500], [1, 200, 64, 5000, 0]
+    both, pool = T.filled(rng, 256, 64, plens + ctx)
+    out, st = run_prefix(pool, both[:5], plens, off, both[5:], ctx, q, T.SCALE)
+    assert st == 0
+    for g in range(5):
+        for b in range(off[g], off[g + 1]):
+            kv = np.concatenate([O.gather(pool, both[g], plens[g]), O.gather(pool, both[5 + b], ctx[b])])
+            check(out[b], q[b], kv, T.SCALE)
+
+
 @pytest.mark.parametrize("R", [256, 512])
 def test_decode_of_long_and_short_requests_in_turn(R):
     """A pair of CTAs that takes the end of one request, others whole and a long run of the next."""
