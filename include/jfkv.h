@@ -639,7 +639,9 @@ int jf_kv8_evict(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_s
 /* ======================================================================
  * The latent cache (pools of format JF_FMT_LATENT16) and the attention that
  * reads it.  jf_kv_checkpoint and jf_kv_restore copy its pages; the other
- * entry points return JF_ERR_UNSUPPORTED for it.
+ * entry points return JF_ERR_UNSUPPORTED for it.  Calls that may run at the
+ * same time need workspaces of their own; calls in one stream, or graphs that
+ * are replayed one after the other, may share one.
  * ====================================================================== */
 #define JF_LATENT_ROT        64    /* rotated key channels of a position      */
 #define JF_LATENT_MAX_GROUPS 64    /* groups of a jf_latent_prefix_decode_attn */

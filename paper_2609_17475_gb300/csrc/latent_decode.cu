@@ -18,7 +18,7 @@
 // any length.
 //
 // What bounds it: memory, the products and what of one the other cannot hide.  32 requests to
-// 65,535 positions x 16 heads take 102 us: their 593 MB 87 at copy rate, the same launch without
+// 65,535 positions x 16 heads take 101 us: their 593 MB 87 at copy rate, the same launch without
 // its loads 80 (2,500 cycles a tile of R = 512 where its products are 2,176).  All of K's and V's
 // shared memory holds one tile each, the next one's K is on its way into the L2 cache, and every
 // position crosses from there twice, as K and as V: 137 KB a tile and CTA, 12 TB/s in all.  One

@@ -28,7 +28,7 @@
 // tensor pipe 78 % active), attention 385 (667 GFLOP, 1,730 TFLOP/s, 91 %), the join 9.  Expanding costs 2 R
 // 256 operations a position and head once and saves 1,536 of 2,176 a (query, position) pair of the
 // absorbed form: from about 170 queries on it is less.  Below that (77 queries after 4,001 x 16
-// heads: 32 us, expansion 13, attention 11, join 3) the absorbed form's products would be 6 us
+// heads: 31.6 us, expansion 13, attention 11, join 3) the absorbed form's products would be 6 us
 // against 11, but it would need two products with the weights around the decode and its join.
 //
 // Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
