@@ -822,120 +822,148 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
   __shared__ float s_red[2][WARPS];
   __shared__ int32_t s_cnt[WARPS];
   __shared__ float4 s_o[LM_THREADS];
+  __shared__ uint32_t s_list[LM_THREADS];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (int)threadIdx.x % LANES, grp = (int)threadIdx.x / LANES;
-  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H;   // below 2^26
-  for (uint32_t slice = blockIdx.x; slice < total * (R / CH); slice += gridDim.x) {
-    const uint32_t row = slice / (R / CH);
-    const int ch = (int)(slice % (R / CH)) * CH + c * 4;
-    const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
-    // the row's partials: those of the prefix's item, then its own's
-    const int64_t units = *pl.units;
-    int count = 0;
-    bool direct = false;
-    for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
-      int item, inside;
-      if (part == 0) {
-        int g = 0;
-        while (a.first[g + 1] <= b) ++g;
-        inside = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
-        item = pl.item0[g] + inside / LD_ROWS;
-        inside %= LD_ROWS;
-      } else {
-        item = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
-        inside = h % LD_ROWS;
+  const uint32_t total = (uint32_t)a.batch * (uint32_t)a.H, slices = total * (R / CH);   // below 2^28
+  // More rows than blocks (of a decode, CH = R): a thread looks a row over, and the block takes those that are
+  // not written out already.  (A block a row in turn, 4,096 requests of 64 positions x 16 heads took 266 us, 203 so.)
+  const bool list = CH == R && gridDim.x < slices;
+  for (uint32_t base = blockIdx.x; base < slices; base += gridDim.x * LM_THREADS) {
+    int todo = 1;
+    if (list) {
+      const uint32_t mine = base + threadIdx.x * gridDim.x;
+      bool need = false;
+      if (mine < slices) {
+        const uint32_t b = mine / (uint32_t)a.H, h = mine - b * (uint32_t)a.H;
+        const int2 span = pl.spans[(int)b * pl.blocks + (int)h / LD_ROWS];
+        need = span.x != span.y;
       }
-      const int2 span = pl.spans[item];
-      const int p0 = span.x, p1 = span.y;
-      if (p1 < p0) continue;   // nothing there
-      if (p0 == p1) {
-        if (a.num_groups == 0) direct = true;
-        if (threadIdx.x == 0)
-          s_row[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
-        ++count;
-        continue;
-      }
-      // pairs between the first and the last that have units at all
-      const PairRuns runs(units, pl.pairs, pl.inv);
-      const int p = p0 + (int)threadIdx.x;
-      const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
-      const unsigned m = __ballot_sync(0xffffffffu, has);
+      const unsigned m = __ballot_sync(0xffffffffu, need);
       if (lane == 0) s_cnt[warp] = __popc(m);
       __syncthreads();
-      int at = count;
+      int at = 0;
+      todo = 0;
       for (int w = 0; w < WARPS; ++w) {
         if (w < warp) at += s_cnt[w];
-        count += s_cnt[w];
+        todo += s_cnt[w];
       }
-      if (has)
-        s_row[at + __popc(m & ((1u << lane) - 1))] = (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside;
+      if (need) s_list[at + __popc(m & ((1u << lane) - 1))] = mine;
       __syncthreads();
     }
-    if (direct) continue;   // uniform over the CTA
-    __syncthreads();
-    // the first loads, under way while the weights are worked out
-    const float* const src = pl.o + ch;
-    float4 v[LM_BATCH];
-#pragma unroll
-    for (int k = 0; k < LM_BATCH; ++k)
-      if (grp + k * GROUPS < count)
-        v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[grp + k * GROUPS] * R);
-    float m = -INFINITY, l = 0.f;
-    if ((int)threadIdx.x < count) {
-      const float2 x = *reinterpret_cast<const float2*>(pl.ml + (int64_t)s_row[threadIdx.x] * 2);
-      m = x.x;
-      l = x.y;
-    }
-    float M = m;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    if (lane == 0) s_red[0][warp] = M;
-    __syncthreads();
-    M = s_red[0][0];
-    for (int w = 1; w < WARPS; ++w) M = fmaxf(M, s_red[0][w]);
-    // no maximum at all: sums of zero, or NaN where every score was
-    const float f = M == -INFINITY ? 1.f : fast_exp2(m - M);
-    float S = f * l;
-    s_w[threadIdx.x] = f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
-    if (lane == 0) s_red[1][warp] = S;
-    __syncthreads();
-    S = 0.f;
-    for (int w = 0; w < WARPS; ++w) S += s_red[1][w];
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = grp; i < count; i += LM_BATCH * GROUPS) {
-#pragma unroll
-      for (int k = 0; k < LM_BATCH; ++k)
-        if (i + k * GROUPS < count) {
-          const float w = s_w[i + k * GROUPS];
-          acc.x = fmaf(v[k].x, w, acc.x);
-          acc.y = fmaf(v[k].y, w, acc.y);
-          acc.z = fmaf(v[k].z, w, acc.z);
-          acc.w = fmaf(v[k].w, w, acc.w);
+    for (int t = 0; t < todo; ++t) {
+      const uint32_t slice = list ? s_list[t] : base;
+      const uint32_t row = slice / (R / CH);
+      const int ch = (int)(slice % (R / CH)) * CH + c * 4;
+      const int b = (int)(row / (uint32_t)a.H), h = (int)(row - (uint32_t)b * (uint32_t)a.H);
+      // the row's partials: those of the prefix's item, then its own's
+      const int64_t units = *pl.units;
+      int count = 0;
+      bool direct = false;
+      for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
+        int item, inside;
+        if (part == 0) {
+          int g = 0;
+          while (a.first[g + 1] <= b) ++g;
+          inside = (int)(row - (uint32_t)a.first[g] * (uint32_t)a.H);
+          item = pl.item0[g] + inside / LD_ROWS;
+          inside %= LD_ROWS;
+        } else {
+          item = pl.prefix_items + b * pl.blocks + h / LD_ROWS;
+          inside = h % LD_ROWS;
         }
-      const int next = i + LM_BATCH * GROUPS;
+        const int2 span = pl.spans[item];
+        const int p0 = span.x, p1 = span.y;
+        if (p1 < p0) continue;   // nothing there
+        if (p0 == p1) {
+          if (a.num_groups == 0) direct = true;
+          if (threadIdx.x == 0)
+            s_row[count] = (int32_t)(2 * pl.pairs * pl.slot_rows + (part == 0 ? 0 : total) + row);
+          ++count;
+          continue;
+        }
+        // pairs between the first and the last that have units at all
+        const PairRuns runs(units, pl.pairs, pl.inv);
+        const int p = p0 + (int)threadIdx.x;
+        const bool has = p <= p1 && runs.first(p) < runs.first(p + 1);
+        const unsigned m = __ballot_sync(0xffffffffu, has);
+        if (lane == 0) s_cnt[warp] = __popc(m);
+        __syncthreads();
+        int at = count;
+        for (int w = 0; w < WARPS; ++w) {
+          if (w < warp) at += s_cnt[w];
+          count += s_cnt[w];
+        }
+        if (has)
+          s_row[at + __popc(m & ((1u << lane) - 1))] = (2 * p + (p == p0 ? 1 : 0)) * pl.slot_rows + inside;
+        __syncthreads();
+      }
+      if (direct) continue;   // uniform over the CTA
+      __syncthreads();
+      // the first loads, under way while the weights are worked out
+      const float* const src = pl.o + ch;
+      float4 v[LM_BATCH];
 #pragma unroll
       for (int k = 0; k < LM_BATCH; ++k)
-        if (next + k * GROUPS < count)
-          v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[next + k * GROUPS] * R);
-    }
-    s_o[threadIdx.x] = acc;
-    __syncthreads();
-    if (grp == 0) {
-      for (int g = 1; g < GROUPS; ++g) {
-        const float4 x = s_o[g * LANES + c];
-        acc.x += x.x;
-        acc.y += x.y;
-        acc.z += x.z;
-        acc.w += x.w;
+        if (grp + k * GROUPS < count)
+          v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[grp + k * GROUPS] * R);
+      float m = -INFINITY, l = 0.f;
+      if ((int)threadIdx.x < count) {
+        const float2 x = *reinterpret_cast<const float2*>(pl.ml + (int64_t)s_row[threadIdx.x] * 2);
+        m = x.x;
+        l = x.y;
       }
-      const float inv = S != 0.f ? 1.f / S : 0.f;
-      *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) = to_bf16(acc, inv);
+      float M = m;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+      if (lane == 0) s_red[0][warp] = M;
+      __syncthreads();
+      M = s_red[0][0];
+      for (int w = 1; w < WARPS; ++w) M = fmaxf(M, s_red[0][w]);
+      // no maximum at all: sums of zero, or NaN where every score was
+      const float f = M == -INFINITY ? 1.f : fast_exp2(m - M);
+      float S = f * l;
+      s_w[threadIdx.x] = f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
+      if (lane == 0) s_red[1][warp] = S;
+      __syncthreads();
+      S = 0.f;
+      for (int w = 0; w < WARPS; ++w) S += s_red[1][w];
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = grp; i < count; i += LM_BATCH * GROUPS) {
+#pragma unroll
+        for (int k = 0; k < LM_BATCH; ++k)
+          if (i + k * GROUPS < count) {
+            const float w = s_w[i + k * GROUPS];
+            acc.x = fmaf(v[k].x, w, acc.x);
+            acc.y = fmaf(v[k].y, w, acc.y);
+            acc.z = fmaf(v[k].z, w, acc.z);
+            acc.w = fmaf(v[k].w, w, acc.w);
+          }
+        const int next = i + LM_BATCH * GROUPS;
+#pragma unroll
+        for (int k = 0; k < LM_BATCH; ++k)
+          if (next + k * GROUPS < count)
+            v[k] = *reinterpret_cast<const float4*>(src + (int64_t)s_row[next + k * GROUPS] * R);
+      }
+      s_o[threadIdx.x] = acc;
+      __syncthreads();
+      if (grp == 0) {
+        for (int g = 1; g < GROUPS; ++g) {
+          const float4 x = s_o[g * LANES + c];
+          acc.x += x.x;
+          acc.y += x.y;
+          acc.z += x.z;
+          acc.w += x.w;
+        }
+        const float inv = S != 0.f ? 1.f / S : 0.f;
+        *reinterpret_cast<uint2*>(a.out + (int64_t)row * R + ch) = to_bf16(acc, inv);
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -1021,10 +1049,9 @@ static int launch_t(const LatentDecode& a, const LatentPlan& pl, cudaStream_t st
   cfg.numAttrs = 1;
   if (cudaLaunchKernelEx(&cfg, latent_decode_kernel<R>, kmap, vmap, qmap, a, pl) != cudaSuccess) return JF_ERR_CUDA;
   // Few rows: 128 channels a CTA, so that more of the GPU takes part (one request of 131,072 positions
-  // x 128 heads 43 us, a warp a piece 90).  Many: a CTA a row, since most of a decode's rows have a few
-  // parts or none (32 mixed requests 102.9 us, a warp a piece 104.3, 128 channels a CTA 110); over
-  // prefixes a warp a piece (64 continuations 61.0 us, a CTA a row 62.8; 2 x 4 continuations x 128
-  // heads 27.1 and 29.2).
+  // x 128 heads 39.7 us, a CTA a row 43.7).  Many: a CTA a row, since most of a decode's rows have a few
+  // parts or none (32 mixed requests 101.5 us, 128 channels a CTA 105.5); over prefixes a warp 128
+  // channels (64 continuations 55.6 us, a CTA a row 57.3; 2 x 4 continuations x 128 heads 21.5 and 23.0).
   const int64_t rows = (int64_t)a.batch * a.H, slices = rows * (R / 128);
   const bool many = rows >= 4 * pl.pairs;
   cfg.blockDim = dim3(LM_THREADS);
