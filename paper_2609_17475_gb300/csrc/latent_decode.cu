@@ -733,7 +733,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  cluster_meet();
+  cluster_meet();   // CTA 1's arrivals (K, V, Q, P) were all waited for by the products they belong to
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);

@@ -172,6 +172,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
         if (ok && hl == 0) tc::commit2_both_if(leader, a_free);
         if (ok) tc::commit2_both_if(leader, &d_full[t & 1]);
       }
+      for (int t = max(0, count - 2); t < count && ok; ++t) ok = wait(&d_free[t & 1], t >> 1);
     } else if (lane == 0) {
       for (int t = 0; t < count && ok; ++t) {
         const bool fresh = t == 0 || hl == 0;
@@ -319,7 +320,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  cluster_meet();
+  cluster_meet();   // CTA 1's arrivals were all waited for, the last ones at the issuer's end
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
@@ -544,6 +545,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           break;   // nothing left
         }
       }
+      if (ok && pseg > 0) ok = wait(o_free, pseg - 1);
     } else if (lane == 0) {
       // ================= CTA 1's arrivals =================
       int t = 0;
@@ -825,7 +827,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   // neither CTA may release TMEM or exit while its partner can still reach it
   tc::fence_before();
   settle(ok);
-  cluster_meet();
+  cluster_meet();   // CTA 1's arrivals were all waited for, the last ones at the issuer's end
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);

@@ -110,7 +110,8 @@ __device__ __forceinline__ void settle(bool ok) {
 }
 
 // Both CTAs of the pair are here.  Relaxed: nothing is handed over, and a release would first wait for
-// this CTA's stores to reach memory, which the kernel's end does anyway.
+// this CTA's stores to reach memory, which the kernel's end does anyway.  Only where every arrival at the
+// partner's barriers has been waited for there: nothing orders one still on its way.
 __device__ __forceinline__ void cluster_meet() {
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
 }
