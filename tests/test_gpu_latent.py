@@ -330,6 +330,8 @@ def run_prefix(pool, ptable, plens, off, table, ctx, q, scale, ws=None):
     (256, 64, 64, [3, 1], [65, 4000], [64, 128, 0, 1]),
     (512, 20, 64, [7, 9], [3000, 129], [0] * 16),
     (512, 16, 128, [30, 2, 9], [9000, 4000, 6001], [700 * (i % 3) + i for i in range(41)]),
+    (256, 200, 64, [2, 1], [300, 64], [10, 0, 130]),
+    (512, 1024, 128, [1, 2], [1500, 129], [1, 700, 0]),
 ], ids=str)
 def test_prefix_decode(R, H, P, sizes, plens, ctx):
     rng = np.random.default_rng(R + H + sum(plens) + sum(ctx))
