@@ -756,8 +756,12 @@ size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int
  * positions are not reliable.  A value among the chunk's own positions that is not
  * finite makes the head's output NaN for the queries that see it, and for no other.
  * Numerics: products and sums in fp32.  The expanded keys are rounded to bf16 (2^-8
- * of each), the expanded values and the weights to fp16 (2^-11); a value past
- * 65504 sets JF_DEV_ERR_RANGE and counts as infinite.
+ * of each), the expanded values and the weights to fp16 beside powers of two: a
+ * value by 2^-11 of it or 2^-39 of the largest of its head's 128 positions, a
+ * weight by 2^-11 or what counts 2^-33 of the row's largest weight times value.
+ * Values may have any magnitude that fp32 holds; one past 65504 sets
+ * JF_DEV_ERR_RANGE, as a notice: the outputs are no less exact.  Scores (times
+ * log2 e) are to stay below 2^24, where fp32 tells neighbours apart.
  */
 int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row, const void* q,
                            int32_t q_start, int32_t chunk_len, int32_t num_heads,

@@ -20,8 +20,15 @@
 // is at the next item's first.  Keys and queries multiply as bf16; values and weights as
 // fp16, whose three more bits they need: in bf16 the two roundings weighed as much as the
 // output's own (a whole prompt of 4,095 off by 0.0026 of its norm for the 0.0017 of
-// rounding exact values).  Weights are 2^(s - m); a row's reference m is set so that its
-// largest weight is 2^10 and moves, O's row with it, when a weight passes 2^15.
+// rounding exact values).  fp16's range is not bf16's, so a tile's 128 values of a head are
+// held as v 2^-e, e a whole number that puts the largest between 2^14 and 2^15, and a
+// position counts by s + e: its weight is 2^(s + e - m), and O = sum of weight times held
+// value is in units of 2^m whatever e.  A row's reference m is a whole number too (powers of
+// two change no other bits), set so that the largest weight is about 2^10; it moves, O's row
+// with it, when a weight passes 2^15.9.  The sum of 2^s has a reference of its own: each tile's weights
+// add 2^(m - e) times theirs, and what is stored as nothing beside far larger values still counts.
+// A value's error is 2^-11 of it, or 2^-39 of its tile's largest.  (In fp16 as they are, values of
+// 2^-20 gave outputs off by 0.017 of their norm, of 2^-30 zeros.)
 //
 // What bounds it: the tensor cores at the power they may take.  2,048 queries after 30,720
 // positions x 16 heads take 462 us; each kernel alone: expansion 81 (137 GFLOP, 1,700 TFLOP/s, the
@@ -43,8 +50,11 @@ namespace jfkv {
 constexpr int LP_T = 128;            // positions a tile
 constexpr int LP_Q = 256;            // queries a pair
 constexpr int LP_HDR = 2;            // an item's fixed cost, in tiles
-constexpr float LP_SET = 10.f;       // a reference puts the largest weight at 2^10;
-constexpr float LP_TOP = 15.f;       // it moves when one passes 2^15 (fp16 ends below 2^16)
+constexpr float LP_SET = 10.f;       // a reference puts the largest weight at 2^9.5 to 2^10.5;
+// it moves when one passes 2^15.9 (fp16 ends below 2^16).  With floor() and 15, powers that differ by one
+// between tiles made it move more often: 2,048 queries after 30,720 positions 486 us for 475.
+constexpr float LP_TOP = 15.9f;
+constexpr float LP_FAR = 100.f;      // weights this far below 2^s (log2) are not summed as stored
 constexpr int LP_NONE = 0x7FFFFFFF;  // no position
 
 struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
@@ -54,8 +64,9 @@ struct LatentChunk {                 // one pass: heads h0 .. h0 + heads - 1
   uint16_t* v;                       // the same, fp16
   uint16_t* out;                     // [C][H][128]
   int32_t* bad;                      // [heads][n_pad / 32]: first position of a value that is not finite
+  float* power;                      // [heads][n_pad / 128]: e of a tile, -infinity where all its values are zero
   int32_t* status;
-  float* ml;                         // [2 * pairs * 256][2]
+  float4* ml;                        // [2 * pairs * 256]: O's reference, the sum's, the sum, -
   float* o;                          // [2 * pairs * 256][128]
   int64_t units, units_head;         // of the pass, of a head
   int32_t n, n_pad, q_start, C, H, h0, heads, causal;
@@ -79,7 +90,8 @@ struct LeSmem {
   static constexpr int OFF_B = LE_CHUNKS * CHUNK;
   static constexpr int OFF_OUT = OFF_B + LE_STAGES * CHUNK;        // 8 warps x [32 rows][128 B]
   static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
-  static constexpr int TOTAL = OFF_BAR + 512;
+  static constexpr int OFF_TOP = OFF_BAR + 512;                    // [2][4] largest magnitudes, tile t % 2
+  static constexpr int TOTAL = OFF_TOP + 32;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -247,17 +259,47 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
     const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
     const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
     uint16_t* const dst = kind ? a.v : a.k;
+    uint32_t* const s_top = reinterpret_cast<uint32_t*>(sm + L::OFF_TOP);
     // values of positions that not every query of the chunk sees
     const int apart = kind && a.causal ? a.q_start + 1 : LP_NONE;
     for (int t = 0; t < count; ++t, advance()) {
       const int pos0 = pt * 256 + 128 * (int)rank + quarter * 32;
       const int pos = pos0 + lane;
-      if (!mbar_wait_bounded(&d_full[t & 1], (t >> 1) & 1)) {
-        ok = false;
-        break;
-      }
+      // A wait that gave up ends the work but not the meetings: the four warps of a tile's values would wait
+      // for one another for ever.
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&d_full[t & 1], (t >> 1) & 1)) != 0;
       tc::fence_after();
       int first = LP_NONE;
+      float power = -INFINITY, scale = 1.f;
+      if (kind) {
+        // The largest finite magnitude of the tile, as twice its bits and 2^24: those of infinities and NaN
+        // pass 2^32 and come out below 2^24.
+        uint32_t top = 0u;
+        if (ok) {
+#pragma unroll 1
+          for (int c0 = 0; c0 < 128; c0 += 32) {
+            uint32_t x[32];
+            tc::ld32((t & 1) * 256 + 128 + c0 + lane_off, x);
+            tc::wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) top = max(top, 2u * x[c] + (1u << 24));
+          }
+        }
+        top = __reduce_max_sync(0xffffffffu, pos < a.n ? top : 0u);
+        if (lane == 0) s_top[4 * (t & 1) + quarter] = top;
+        // two buffers: a warp may be at the next tile before the others have read this one's
+        asm volatile("bar.sync 1, 128;\n" ::: "memory");
+        const uint4 of = lds128(smem_u32(s_top + 4 * (t & 1)));
+        top = max(max(of.x, of.y), max(of.z, of.w));
+        if (top > 1u << 24) {   // to between 2^14 and 2^15; by 2^126 at most, from 2^-112 down
+          const int expo = max((int)(top >> 24) - 1, 15);
+          power = (float)(expo - 141);
+          scale = __uint_as_float((uint32_t)(268 - expo) << 23);
+          if (top >= 2u * 0x477FF000u + (1u << 24) && lane == 0)   // 65,520: past fp16 as it is
+            flag_error(a.status, JF_DEV_ERR_RANGE);
+        }
+      }
+      if (!ok) continue;
 #pragma unroll 1
       for (int c0 = 0; c0 < 128; c0 += 64) {
         uint32_t x[2][32];
@@ -273,7 +315,8 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
         if (kind) {
 #pragma unroll
           for (int c = 0; c < 32; ++c) {
-            w[c] = pack_f16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]), __uint_as_float(x[c >> 4][(2 * c + 1) & 31]));
+            w[c] = pack_f16x2(__uint_as_float(x[c >> 4][(2 * c) & 31]) * scale,
+                              __uint_as_float(x[c >> 4][(2 * c + 1) & 31]) * scale);
             top = __vmaxu2(top, w[c] & 0x7FFF7FFFu);
           }
         } else {
@@ -287,14 +330,12 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
             if (pos >= a.n) w[c] = 0u;
           if (pos >= a.n) top = 0u;
         }
-        if (max(top & 0xFFFFu, top >> 16) >= 0x7C00u) {   // a value that is not finite, or past fp16
-          if (pos >= apart) first = pos;
+        if (pos >= apart && max(top & 0xFFFFu, top >> 16) >= 0x7C00u) {   // a value that is not finite
+          first = pos;
 #pragma unroll
-          for (int c = 0; c < 64; ++c) {
-            const uint32_t half = c & 1 ? w[c >> 1] >> 16 : w[c >> 1];
-            if ((half & 0x7C00u) != 0x7C00u) continue;
-            if (fabsf(__uint_as_float(x[c >> 5][c & 31])) < INFINITY) flag_error(a.status, JF_DEV_ERR_RANGE);
-            if (pos >= apart) w[c >> 1] &= c & 1 ? 0xFFFFu : 0xFFFF0000u;
+          for (int c = 0; c < 32; ++c) {
+            if ((w[c] & 0x7C00u) == 0x7C00u) w[c] &= 0xFFFF0000u;
+            if ((w[c] & 0x7C000000u) == 0x7C000000u) w[c] &= 0xFFFFu;
           }
         }
 #pragma unroll
@@ -312,7 +353,11 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
       }
       if (kind) {
         first = __reduce_min_sync(0xffffffffu, first);
-        if (lane == 0) a.bad[((int64_t)hl * a.n_pad + pos0) >> 5] = first;
+        if (lane == 0) {
+          const int64_t at = (int64_t)hl * a.n_pad + pos0;
+          a.bad[at >> 5] = first;
+          if (quarter == 0) a.power[at >> 7] = power;
+        }
       }
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
@@ -340,11 +385,19 @@ struct LaSmem {
   static constexpr int OFF_V = OFF_K + LA_KS * K_BYTES;
   static constexpr int OFF_OUT = OFF_V + LA_VS * V_BYTES;   // 8 warps x [32 rows][128 B]
   static constexpr int OFF_BAR = OFF_OUT + 8 * 4096;
-  static constexpr int OFF_M = OFF_BAR + 512;           // [4][128] references after tile t % 4
-  static constexpr int OFF_L = OFF_M + 4 * 128 * 4;     // [4][128] (m, l) of segment s % 4, from one group to the other
+  static constexpr int OFF_M = OFF_BAR + 512;           // [4][128] O's references after tile t % 4
+  static constexpr int OFF_L = OFF_M + 4 * 128 * 4;     // [4][128] (reference, sum) of segment s % 4, from one group to the other
   static constexpr int TOTAL = OFF_L + 4 * 128 * 8;
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
+
+// 2^(m - ms), the unit of O over that of the sum, in two factors: one alone could leave fp32's range where the
+// output does not
+__device__ __forceinline__ float half_power(float m, float ms, float* rest) {
+  const float k = m == -INFINITY || ms == -INFINITY ? 0.f : m - ms, half = floorf(0.5f * k);
+  *rest = fast_exp2(k - half);
+  return fast_exp2(half);
+}
 
 // tiles and first unit (of its head) of query tile qt
 __device__ __forceinline__ int chunk_tiles(const LatentChunk& a, int qt) {
@@ -645,11 +698,15 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       const int limit = limit_of(row0 + lane);         // last position seen
       const int first_limit = limit_of(row0);          // by every query of the warp
       const int nt = sg.j1 - sg.j0;
+      const float* const powers = a.power + (((int64_t)sg.hl * a.n_pad) >> 7) + sg.j0;
+      float e_next = 0.f;
+      if (((t0 + group) & 1) < nt) e_next = powers[(t0 + group) & 1];
       int first_bad = LP_NONE;   // of the values that the warp's queries see and not all of the chunk's
       if (a.causal)
         for (int b = ((a.q_start + 1) >> 5) + lane; b <= (limit_of(row0 + 31) >> 5); b += 32)
           first_bad = min(first_bad, a.bad[(((int64_t)sg.hl * a.n_pad) >> 5) + b]);
-      float m_own = -INFINITY, l = 0.f;   // the reference at this group's last tile
+      float m_own = -INFINITY;              // O's reference at this group's last tile
+      float m_sum = -INFINITY, l = 0.f;     // the group's sum of weights, and its reference
       for (int i = (t0 + group) & 1; i < nt && ok; i += 2) {
         const int T = t0 + i, key0 = (sg.j0 + i) * LP_T;
         const uint32_t tb = tS + (T % LA_SB) * 128 + lane_off;
@@ -661,6 +718,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         // What the first changes of S -- the sign of a scale below zero, a scale of zero, positions not
         // seen -- it writes back.
         uint32_t s[2][32];
+        const float e = e_next;   // the power that the tile's values are held by
         float x[2] = {-INFINITY, -INFINITY};
         const bool plain = a.scale_log2 > 0.f && key0 + LP_T - 1 <= first_limit;   // of the whole warp
 #pragma unroll 1
@@ -686,7 +744,13 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
             x[c & 1] = max3(x[c & 1], __uint_as_float(s[c >> 4][(2 * c) & 31]),
                             __uint_as_float(s[c >> 4][(2 * c + 1) & 31]));
         }
-        const float mt = sc * fmaxf(x[0], x[1]);
+        const float top = fmaxf(x[0], x[1]), top_e = fmaf(sc, top, e);
+        const float mt = sc * top;
+        if (mt > m_sum + LP_TOP || m_sum == -INFINITY) {
+          const float to = floorf(mt);
+          if (m_sum != -INFINITY) l *= fast_exp2(m_sum - to);
+          m_sum = to;
+        }
         // the reference after the tile before, the other group's
         float m_ref = -INFINITY;   // nothing seen so far
         if (i > 0) {
@@ -695,7 +759,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           if (!ok) break;
           m_ref = s_m[((T - 1) & 3) * 128 + r];
         }
-        const float m_new = mt > m_ref + LP_TOP || m_ref == -INFINITY ? mt - LP_SET : m_ref;
+        const float m_new = top_e > m_ref + LP_TOP || m_ref == -INFINITY ? rintf(top_e) - LP_SET : m_ref;
         const bool moves = m_ref != -INFINITY && m_new != m_ref;
         if (__any_sync(0xffffffffu, moves)) {   // O's rows with it
           ok = __all_sync(0xffffffffu, mbar_wait_bounded(&pv_done[(T - 1) & 3], ((T - 1) >> 2) & 1)) != 0;
@@ -716,12 +780,24 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         s_m[(T & 3) * 128 + r] = m_new;
         __syncwarp();
         if (lane == 0) mbar_arrive(&m_bar[(T & 3) * 4 + quarter]);
-        if (m_new != m_own) {
-          if (m_own != -INFINITY) l *= fast_exp2(m_own - m_new);
-          m_own = m_new;
+        m_own = m_new;
+        const float mm = m_new == -INFINITY ? 0.f : m_new, ms = m_sum == -INFINITY ? 0.f : m_sum;
+        // Beside far larger values a tile's weights may be stored as nothing: their part of the sum is worked
+        // out by itself.  (Without this branch the code about it came out slower: a whole prompt of 4,095 621 us.)
+        const bool apart = __any_sync(0xffffffffu, mm - ms - e > LP_FAR && top != -INFINITY);
+        if (apart) {
+#pragma unroll 1
+          for (int c0 = 0; c0 < LP_T; c0 += 32) {
+            tc::ld32(tb + c0, s[0]);
+            tc::wait_ld();
+            float sum = 0.f;
+#pragma unroll
+            for (int c = 0; c < 32; ++c) sum += fast_exp2(fmaf(__uint_as_float(s[0][c]), sc, -ms));
+            l += sum;
+          }
         }
-        const float mm = m_new == -INFINITY ? 0.f : m_new;
-        const uint64_t cc = f32x2(-mm, -mm);
+        const float shift = e - mm;
+        const uint64_t cc = f32x2(shift, shift);
         uint64_t sum = f32x2(0.f, 0.f);
 #pragma unroll 1
         for (int c0 = 0; c0 < LP_T; c0 += 64) {
@@ -745,7 +821,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
         }
         float u, v;
         unpack_f32x2(sum, u, v);
-        l += u + v;
+        if (i + 2 < nt) e_next = powers[i + 2];
+        if (!apart) l = fmaf(u + v, fast_exp2(fminf(-ms - shift, 126.f)), l);
         tc::wait_st();
         tc::fence_before();
         __syncwarp();
@@ -757,7 +834,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       // sum.  (Barriers and places of four segments in turn: neither group gets that far ahead.)
       float2* const ml = s_ml + (seg & 3) * 128 + r;
       if (group != (last & 1)) {
-        *ml = make_float2(m_own, l);
+        *ml = make_float2(m_sum, l);
         asm volatile("bar.arrive %0, 256;\n" ::"r"(1 + (seg & 3)) : "memory");
         continue;
       }
@@ -767,13 +844,16 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
       tc::fence_after();
       const float2 other = *ml;
       // no reference: a sum of zero, or NaN where every score was
-      const float lsum = other.x == -INFINITY ? l + other.y : fmaf(other.y, fast_exp2(other.x - m_own), l);
+      const float ms = fmaxf(m_sum, other.x);
+      const float lsum = ms == -INFINITY ? l + other.y : l * fast_exp2(m_sum - ms) + other.y * fast_exp2(other.x - ms);
       const bool whole = nt == sg.n;
       const int64_t prow = ((int64_t)(2 * pair + (sg.j0 == 0 ? 1 : 0)) * LP_Q) + 128 * rank;
-      float inv = whole ? (lsum != 0.f ? 1.f / lsum : 0.f) : 1.f;
+      float inv = whole ? (lsum != 0.f ? 1.f / lsum : 0.f) : 1.f, rest;
+      const float half = half_power(m_own, ms, &rest);
       // a value that is not finite among those seen
       if (__reduce_min_sync(0xffffffffu, first_bad) <= limit) inv = __uint_as_float(0x7FC00000u);
-      if (!whole) *reinterpret_cast<float2*>(a.ml + (prow + r) * 2) = make_float2(m_own, lsum * inv);
+      if (!whole) a.ml[prow + r] = make_float4(m_own, ms, lsum * inv, 0.f);
+      inv *= half;
       // 128-byte pieces of a warp's 32 rows go through shared memory, so that whole lines are written
       const uint32_t tr = smem_u32(sm + L::OFF_OUT) + (warp - 4) * 4096;
       uint8_t* const to = whole ? reinterpret_cast<uint8_t*>(a.out + ((int64_t)row0 * a.H + a.h0 + sg.hl) * 128)
@@ -809,8 +889,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           read(half);
 #pragma unroll
           for (int c = 0; c < 32; ++c)
-            w[0][c] = pack_bf16x2(__uint_as_float(o[c >> 4][(2 * c) & 31]) * inv,
-                                  __uint_as_float(o[c >> 4][(2 * c + 1) & 31]) * inv);
+            w[0][c] = pack_bf16x2(__uint_as_float(o[c >> 4][(2 * c) & 31]) * inv * rest,
+                                  __uint_as_float(o[c >> 4][(2 * c + 1) & 31]) * inv * rest);
           out(w[0], half);
         }
       } else {
@@ -884,16 +964,22 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
   load(0);
   // weights: eight lanes a row
   const int sub = lane & 7, mine = lane >> 3;
-  const float* const ml = a.ml + (int64_t)(row0 + mine) * 2;
-  float M = -INFINITY, S = 0.f;
-  for (int i = sub; i < n; i += 8) M = fmaxf(M, ml[(int64_t)s_slot[i] * (LP_Q * 2)]);
-#pragma unroll
-  for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+  const float4* const ml = a.ml + row0 + mine;
+  float M = -INFINITY, MS = -INFINITY, S = 0.f;
   for (int i = sub; i < n; i += 8) {
-    const float2 x = *reinterpret_cast<const float2*>(ml + (int64_t)s_slot[i] * (LP_Q * 2));
-    const float f = M == -INFINITY ? 1.f : fast_exp2(x.x - M);
-    s_w[warp][mine][i] = f;
-    S = fmaf(f, x.y, S);
+    const float4 x = ml[(int64_t)s_slot[i] * LP_Q];
+    M = fmaxf(M, x.x);
+    MS = fmaxf(MS, x.y);
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) {
+    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    MS = fmaxf(MS, __shfl_xor_sync(0xffffffffu, MS, o));
+  }
+  for (int i = sub; i < n; i += 8) {
+    const float4 x = ml[(int64_t)s_slot[i] * LP_Q];
+    s_w[warp][mine][i] = M == -INFINITY ? 1.f : fast_exp2(x.x - M);
+    S = fmaf(MS == -INFINITY ? 1.f : fast_exp2(x.y - MS), x.z, S);
   }
 #pragma unroll
   for (int o = 4; o > 0; o >>= 1) S += __shfl_xor_sync(0xffffffffu, S, o);
@@ -918,10 +1004,13 @@ latent_prefill_merge_kernel(const __grid_constant__ LatentChunk a) {
 #pragma unroll
   for (int k = 0; k < LJ_ROWS; ++k) {
     const float s = __shfl_sync(0xffffffffu, S, 8 * k);
-    const float inv = s != 0.f ? 1.f / s : 0.f;
+    float rest;
+    const float half = half_power(__shfl_sync(0xffffffffu, M, 8 * k), __shfl_sync(0xffffffffu, MS, 8 * k), &rest);
+    const float inv = (s != 0.f ? 1.f / s : 0.f) * half;
     if (q0 + k < a.C)
       *reinterpret_cast<uint2*>(a.out + ((int64_t)(q0 + k) * a.H + a.h0 + sg.hl) * 128 + lane * 4) =
-          make_uint2(pack_bf16x2(acc[k].x * inv, acc[k].y * inv), pack_bf16x2(acc[k].z * inv, acc[k].w * inv));
+          make_uint2(pack_bf16x2(acc[k].x * inv * rest, acc[k].y * inv * rest),
+                     pack_bf16x2(acc[k].z * inv * rest, acc[k].w * inv * rest));
   }
 }
 
@@ -950,7 +1039,8 @@ size_t latent_prefill_workspace_bytes(int64_t q_start, int64_t C, int64_t H, int
   const int64_t pairs = sms / 2, n_pad = padded(q_start + C);
   if (C == 0) return 256;
   const int64_t heads = heads_per_pass(n_pad, C, H, pairs);
-  return (size_t)(256 + round256(heads * n_pad / 8) + 2 * pairs * LP_Q * (8 + 512) + heads * n_pad * 512);
+  return (size_t)(256 + round256(heads * n_pad / 8) + round256(heads * n_pad / 32) + 2 * pairs * LP_Q * (16 + 512) +
+                  heads * n_pad * 512);
 }
 
 template <typename... P, typename... A>
@@ -997,8 +1087,10 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
   a.bad = reinterpret_cast<int32_t*>(ws);
   ws += round256(per * n_pad / 8);
-  a.ml = reinterpret_cast<float*>(ws);
-  ws += (int64_t)2 * pairs * LP_Q * 8;
+  a.power = reinterpret_cast<float*>(ws);
+  ws += round256(per * n_pad / 32);
+  a.ml = reinterpret_cast<float4*>(ws);
+  ws += (int64_t)2 * pairs * LP_Q * 16;
   a.o = reinterpret_cast<float*>(ws);
   ws += (int64_t)2 * pairs * LP_Q * 512;
   a.k = reinterpret_cast<uint16_t*>(ws);
