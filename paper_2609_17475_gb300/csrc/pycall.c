@@ -166,21 +166,19 @@ static int pool_of(PyObject* p, jf_kv_pool* out) {
   PyObject* data = PyObject_GetAttr(p, s_data);
   if (!data) return -1;
   int64_t shape[4] = {0, 0, 0, 0};
-  PyObject* at = PyObject_CallMethodNoArgs(data, s_ptr);
-  const int n = at ? ints_of(data, 0, shape) : -1;
+  const int n = tensor(data, G.u8, "a pool's data", 1, U8_T, &out->base) ? -1 : ints_of(data, 0, shape);
   Py_DECREF(data);
-  if (at) {
-    out->base = PyLong_AsVoidPtr(at);
-    Py_DECREF(at);
-  }
   if (n < 1) return n ? -1 : bad("a pool's data must be [pages, bytes]");
   out->num_pages = shape[0];
   out->tq4 = NULL;
-  return int_attr(p, s_page, &out->page_size) || int_attr(p, s_hkv, &out->num_kv_heads) ||
-                 int_attr(p, s_dim, &out->head_dim) || int_attr(p, s_group, &out->group_size) ||
-                 int_attr(p, s_format, &out->format)
-             ? -1
-             : 0;
+  if (int_attr(p, s_page, &out->page_size) || int_attr(p, s_hkv, &out->num_kv_heads) ||
+      int_attr(p, s_dim, &out->head_dim) || int_attr(p, s_group, &out->group_size) ||
+      int_attr(p, s_format, &out->format))
+    return -1;
+  if (out->format == JF_FMT_LATENT16 &&
+      (n != 2 || shape[1] != (int64_t)out->page_size * out->head_dim * 2))
+    return bad("a latent pool's data must be [pages, page_size * head_dim * 2]");
+  return 0;
 }
 
 static int fit(int64_t n) { return n > INT32_MAX ? bad("a size is past 32 bits") : 0; }
@@ -465,8 +463,7 @@ static PyObject* kv8_evict(PyObject* m, PyObject* const* a, Py_ssize_t na) {
 /* ---- the latent cache ---- */
 static int latent_pool(PyObject* p, jf_kv_pool* out) {
   if (pool_of(p, out)) return -1;
-  /* kernels run on the current device, whatever device the memory is on (a pool on the host is
-   * refused by the other tensors' checks) */
+  /* kernels run on the current device, whatever device the memory is on */
   PyObject* data = PyObject_GetAttr(p, s_data);
   if (!data) return -1;
   PyObject* has = PyObject_CallMethodNoArgs(data, s_device);
@@ -474,7 +471,7 @@ static int latent_pool(PyObject* p, jf_kv_pool* out) {
   if (!has) return -1;
   const long at = PyLong_AsLong(has);
   Py_DECREF(has);
-  if (at < 0) return PyErr_Occurred() ? -1 : 0;
+  if (PyErr_Occurred()) return -1;
   PyObject* dev = PyObject_CallNoArgs(G.get_device);
   if (!dev) return -1;
   const long cur = PyLong_AsLong(dev);
