@@ -62,14 +62,34 @@ static int is_true_attr(PyObject* t, PyObject* name) {
   return r;
 }
 
-/* a CUDA tensor of one dtype (checked by identity), contiguous or not -> its pointer */
-static int tensor(PyObject* t, PyObject* dtype, const char* name, int contiguous,
-                  const char* what, void** ptr) {
+/* the device of a CUDA tensor, -1 for others */
+static long device_of(PyObject* t) {
+  PyObject* v = PyObject_CallMethodNoArgs(t, s_device);
+  if (!v) return -1;
+  const long at = PyLong_AsLong(v);
+  Py_DECREF(v);
+  return at;
+}
+
+/* a CUDA tensor of one dtype (checked by identity), on the device `dev` (any: -1), contiguous or not
+ * -> its pointer */
+static int tensor_on(PyObject* t, PyObject* dtype, const char* name, int contiguous,
+                     const char* what, void** ptr, long dev) {
   PyObject* d = PyObject_GetAttr(t, s_dtype);
   if (!d) return wrong_type(name, what);
   const int same = d == dtype;
   Py_DECREF(d);
-  if (!same || is_true_attr(t, s_is_cuda) != 1) return wrong_type(name, what);
+  if (!same) return wrong_type(name, what);
+  if (dev < 0) {
+    if (is_true_attr(t, s_is_cuda) != 1) return wrong_type(name, what);
+  } else {
+    const long at = device_of(t);
+    if (at < 0) return wrong_type(name, what);
+    if (at != dev) {
+      PyErr_Format(PyExc_ValueError, "%s is on another device than the current one", name);
+      return -1;
+    }
+  }
   if (contiguous) {
     PyObject* c = PyObject_CallMethodNoArgs(t, s_contig);
     if (!c) return wrong_type(name, what);
@@ -82,6 +102,11 @@ static int tensor(PyObject* t, PyObject* dtype, const char* name, int contiguous
   *ptr = PyLong_AsVoidPtr(p);
   Py_DECREF(p);
   return PyErr_Occurred() ? -1 : 0;
+}
+
+static int tensor(PyObject* t, PyObject* dtype, const char* name, int contiguous,
+                  const char* what, void** ptr) {
+  return tensor_on(t, dtype, name, contiguous, what, ptr, -1);
 }
 
 #define I32_T "contiguous CUDA tensor of dtype torch.int32"
@@ -461,30 +486,27 @@ static PyObject* kv8_evict(PyObject* m, PyObject* const* a, Py_ssize_t na) {
 }
 
 /* ---- the latent cache ---- */
-static int latent_pool(PyObject* p, jf_kv_pool* out) {
+/* kernels run on the current device, whatever device the memory is on: *dev, where every tensor has to be */
+static int latent_pool(PyObject* p, jf_kv_pool* out, long* dev) {
   if (pool_of(p, out)) return -1;
-  /* kernels run on the current device, whatever device the memory is on */
   PyObject* data = PyObject_GetAttr(p, s_data);
   if (!data) return -1;
-  PyObject* has = PyObject_CallMethodNoArgs(data, s_device);
+  const long at = device_of(data);
   Py_DECREF(data);
-  if (!has) return -1;
-  const long at = PyLong_AsLong(has);
-  Py_DECREF(has);
   if (PyErr_Occurred()) return -1;
-  PyObject* dev = PyObject_CallNoArgs(G.get_device);
-  if (!dev) return -1;
-  const long cur = PyLong_AsLong(dev);
-  Py_DECREF(dev);
+  PyObject* cur = PyObject_CallNoArgs(G.get_device);
+  if (!cur) return -1;
+  *dev = PyLong_AsLong(cur);
+  Py_DECREF(cur);
   if (PyErr_Occurred()) return -1;
-  return at != cur ? bad("the pool is on another device than the current one") : 0;
+  return at != *dev ? bad("the pool is on another device than the current one") : 0;
 }
 
 /* pool, page_table, start_pos, row_offsets, latent, k_rot, err, stream */
 static int latent_arg(PyObject* x, const char* name, int64_t width, void** ptr, int64_t* n,
-                      int64_t* stride) {
+                      int64_t* stride, long dev) {
   int64_t sh[4], st[4];
-  if (tensor(x, G.bf16, name, 0, "CUDA tensor of dtype torch.bfloat16", ptr)) return -1;
+  if (tensor_on(x, G.bf16, name, 0, "CUDA tensor of dtype torch.bfloat16", ptr, dev)) return -1;
   const int d = ints_of(x, 0, sh);
   if (d < 0) return -1;
   if (d != 2 || sh[1] != width) {
@@ -504,14 +526,15 @@ static int latent_arg(PyObject* x, const char* name, int64_t width, void** ptr, 
 
 static PyObject* latent_rows_call(rows_fn fn, PyObject* const* a, Py_ssize_t na) {
   jf_kv_pool p;
+  long dev;
   void *pt, *start, *off, *lat, *rot, *err = NULL, *stream;
   int64_t n, nr, ls, rs, sh[4];
-  if (want(8, na) || latent_pool(a[0], &p) || tensor(a[1], G.i32, "page_table", 1, I32_T, &pt) ||
-      tensor(a[2], G.i32, "start_pos", 1, I32_T, &start) ||
-      tensor(a[3], G.i32, "row_offsets", 1, I32_T, &off) ||
-      latent_arg(a[4], "latent", p.head_dim - JF_LATENT_ROT, &lat, &n, &ls) ||
-      latent_arg(a[5], "k_rot", JF_LATENT_ROT, &rot, &nr, &rs) ||
-      (a[6] != Py_None && tensor(a[6], G.i32, "err_flag", 1, I32_T, &err)))
+  if (want(8, na) || latent_pool(a[0], &p, &dev) || tensor_on(a[1], G.i32, "page_table", 1, I32_T, &pt, dev) ||
+      tensor_on(a[2], G.i32, "start_pos", 1, I32_T, &start, dev) ||
+      tensor_on(a[3], G.i32, "row_offsets", 1, I32_T, &off, dev) ||
+      latent_arg(a[4], "latent", p.head_dim - JF_LATENT_ROT, &lat, &n, &ls, dev) ||
+      latent_arg(a[5], "k_rot", JF_LATENT_ROT, &rot, &nr, &rs, dev) ||
+      (a[6] != Py_None && tensor_on(a[6], G.i32, "err_flag", 1, I32_T, &err, dev)))
     return NULL;
   const int d = ints_of(a[1], 0, sh);
   if (d < 0 || (d == 0 && bad("page_table must be [requests, pages]"))) return NULL;
@@ -539,12 +562,14 @@ struct latent_decode_args {
   int64_t cols, batch, heads, bytes;
   float scale;
 };
-static int latent_decode_tail(PyObject* const* a, const jf_kv_pool* p, struct latent_decode_args* d) {
+static int latent_decode_tail(PyObject* const* a, const jf_kv_pool* p, struct latent_decode_args* d,
+                              long dev) {
   int64_t sh[4], qs[4], os[4];
-  if (tensor(a[0], G.i32, "page_table", 1, I32_T, &d->pt) ||
-      tensor(a[1], G.i32, "context_lens", 1, I32_T, &d->ctx) ||
-      tensor(a[2], G.bf16, "q", 1, BF16_T, &d->q) || tensor(a[4], G.bf16, "out", 1, BF16_T, &d->out) ||
-      tensor(a[5], G.u8, "workspace", 1, U8_T, &d->ws))
+  if (tensor_on(a[0], G.i32, "page_table", 1, I32_T, &d->pt, dev) ||
+      tensor_on(a[1], G.i32, "context_lens", 1, I32_T, &d->ctx, dev) ||
+      tensor_on(a[2], G.bf16, "q", 1, BF16_T, &d->q, dev) ||
+      tensor_on(a[4], G.bf16, "out", 1, BF16_T, &d->out, dev) ||
+      tensor_on(a[5], G.u8, "workspace", 1, U8_T, &d->ws, dev))
     return -1;
   const int nt = ints_of(a[0], 0, sh), nq = ints_of(a[2], 0, qs), no = ints_of(a[4], 0, os);
   if (nt < 0 || nq < 0 || no < 0) return -1;
@@ -565,8 +590,9 @@ static int latent_decode_tail(PyObject* const* a, const jf_kv_pool* p, struct la
 static PyObject* latent_decode(PyObject* m, PyObject* const* a, Py_ssize_t na) {
   (void)m;
   jf_kv_pool p;
+  long dev;
   struct latent_decode_args d;
-  if (want(8, na) || latent_pool(a[0], &p) || latent_decode_tail(a + 1, &p, &d)) return NULL;
+  if (want(8, na) || latent_pool(a[0], &p, &dev) || latent_decode_tail(a + 1, &p, &d, dev)) return NULL;
   CALL(G.latent_decode(&p, d.pt, (int32_t)d.cols, d.ctx, (int32_t)d.batch, d.q, (int32_t)d.heads,
                        d.scale, d.out, d.ws, (size_t)d.bytes, d.stream));
 }
@@ -575,13 +601,14 @@ static PyObject* latent_decode(PyObject* m, PyObject* const* a, Py_ssize_t na) {
 static PyObject* latent_prefix(PyObject* m, PyObject* const* a, Py_ssize_t na) {
   (void)m;
   jf_kv_pool p;
+  long dev;
   struct latent_decode_args d;
   void *ppt, *plen;
   int64_t ps[4];
   int32_t off[JF_LATENT_MAX_GROUPS + 1];
-  if (want(11, na) || latent_pool(a[0], &p) ||
-      tensor(a[1], G.i32, "prefix_table", 1, I32_T, &ppt) ||
-      tensor(a[2], G.i32, "prefix_lens", 1, I32_T, &plen) || latent_decode_tail(a + 4, &p, &d))
+  if (want(11, na) || latent_pool(a[0], &p, &dev) ||
+      tensor_on(a[1], G.i32, "prefix_table", 1, I32_T, &ppt, dev) ||
+      tensor_on(a[2], G.i32, "prefix_lens", 1, I32_T, &plen, dev) || latent_decode_tail(a + 4, &p, &d, dev))
     return NULL;
   const int nt = ints_of(a[1], 0, ps);
   const int64_t groups = numel(a[2]);
@@ -610,14 +637,17 @@ static PyObject* latent_prefix(PyObject* m, PyObject* const* a, Py_ssize_t na) {
 static PyObject* latent_prefill(PyObject* m, PyObject* const* a, Py_ssize_t na) {
   (void)m;
   jf_kv_pool p;
+  long dev;
   void *pt, *q, *wk, *wv, *out, *ws, *stream;
   int64_t qs[4], ks[4], vs[4], os[4];
   int32_t start;
-  if (want(11, na) || latent_pool(a[0], &p) ||
-      tensor(a[1], G.i32, "page_table_row", 1, I32_T, &pt) ||
-      tensor(a[2], G.bf16, "q", 1, BF16_T, &q) || int_of(a[3], &start) ||
-      tensor(a[4], G.bf16, "w_k", 1, BF16_T, &wk) || tensor(a[5], G.bf16, "w_v", 1, BF16_T, &wv) ||
-      tensor(a[8], G.bf16, "out", 1, BF16_T, &out) || tensor(a[9], G.u8, "workspace", 1, U8_T, &ws))
+  if (want(11, na) || latent_pool(a[0], &p, &dev) ||
+      tensor_on(a[1], G.i32, "page_table_row", 1, I32_T, &pt, dev) ||
+      tensor_on(a[2], G.bf16, "q", 1, BF16_T, &q, dev) || int_of(a[3], &start) ||
+      tensor_on(a[4], G.bf16, "w_k", 1, BF16_T, &wk, dev) ||
+      tensor_on(a[5], G.bf16, "w_v", 1, BF16_T, &wv, dev) ||
+      tensor_on(a[8], G.bf16, "out", 1, BF16_T, &out, dev) ||
+      tensor_on(a[9], G.u8, "workspace", 1, U8_T, &ws, dev))
     return NULL;
   const int nq = ints_of(a[2], 0, qs), nk = ints_of(a[4], 0, ks), nv = ints_of(a[5], 0, vs),
             no = ints_of(a[8], 0, os);

@@ -1,5 +1,5 @@
-"""Pools that the latent cache's calls refuse before anything is launched: memory on the host, of another type or
-shape than the pool's fields say.  No GPU: tensors are stand-ins whose memory is never touched."""
+"""Memory that the latent cache's calls refuse before anything is launched: a pool on the host, of another type or
+shape than its fields say, tensors on another device.  No GPU: tensors are stand-ins whose memory is never touched."""
 import pytest
 import torch
 
@@ -53,21 +53,25 @@ def pool(data, P=64, d=576, fmt=jf.JF_FMT_LATENT16):
     return jf.KVPool(data, P, 1, d, format=fmt)
 
 
-def calls(p, d=576):
+def arguments(p, d=576):
     """Every entry point with everything on the GPU but what the pool says; workspaces of 64 bytes are too small, so
     that a call whose arguments pass is refused by the library instead."""
-    R, one, ws = d - 64, Tensor(I32, 1), Tensor(U8, 64)
-    table, q, out = Tensor(I32, 1, 4), Tensor(BF, 1, 4, d), Tensor(BF, 1, 4, R)
-    rows = (Tensor(BF, 3, R), Tensor(BF, 3, 64))
-    w = Tensor(BF, 4, 128, R)
+    R, table, one = d - 64, lambda: Tensor(I32, 1, 4), lambda: Tensor(I32, 1)
+    rows = lambda: [p, table(), one(), Tensor(I32, 2), Tensor(BF, 3, R), Tensor(BF, 3, 64), Tensor(I32, 1), 0]  # noqa: E731
+    tail = lambda: [table(), one(), Tensor(BF, 1, 4, d), 0.1, Tensor(BF, 1, 4, R), Tensor(U8, 64), 0]  # noqa: E731
+    w = lambda: Tensor(BF, 4, 128, R)  # noqa: E731
     return {
-        "append": lambda: jf.jf_latent_append(p, table, one, Tensor(I32, 2), *rows, None, 0),
-        "read": lambda: jf.jf_latent_read(p, table, one, Tensor(I32, 2), *rows, None, 0),
-        "decode": lambda: jf.jf_latent_decode_attn(p, table, one, q, 0.1, out, ws, 0),
-        "prefix": lambda: jf.jf_latent_prefix_decode_attn(p, table, one, [0, 1], table, one, q, 0.1, out, ws, 0),
-        "prefill": lambda: jf.jf_latent_prefill_attn(p, Tensor(I32, 4), Tensor(BF, 16, 4, 192), 0, w, w, 0.1, True,
-                                                     Tensor(BF, 16, 4, 128), ws, 0),
+        "append": (jf.jf_latent_append, rows()),
+        "read": (jf.jf_latent_read, rows()),
+        "decode": (jf.jf_latent_decode_attn, [p] + tail()),
+        "prefix": (jf.jf_latent_prefix_decode_attn, [p, table(), one(), [0, 1]] + tail()),
+        "prefill": (jf.jf_latent_prefill_attn, [p, Tensor(I32, 4), Tensor(BF, 16, 4, 192), 0, w(), w(), 0.1, True,
+                                                Tensor(BF, 16, 4, 128), Tensor(U8, 64), 0]),
     }
+
+
+def calls(p):
+    return {name: lambda f=f, a=a: f(*a) for name, (f, a) in arguments(p).items()}
 
 
 ATTEND = ["decode", "prefix", "prefill"]
@@ -107,6 +111,35 @@ def test_a_pool_on_the_host_is_refused(name):
 def test_a_pool_whose_memory_is_not_what_it_says(name, data, kw, error):
     with pytest.raises(error):
         calls(pool(data, **kw))[name]()
+
+
+@pytest.mark.parametrize("name", ALL)
+def test_tensors_on_another_device_are_refused(name):
+    """Each of a call's tensors in turn on a second device, or on the host, the others on the current one."""
+    whole = pool(Tensor(U8, 8, 64 * 576 * 2))
+    f, a = arguments(whole)[name]
+    for t in [whole.data] + [x for x in a if isinstance(x, Tensor)]:
+        t.device = 1
+        with pytest.raises(ValueError, match="another device"):
+            f(*a)
+        t.device, t.is_cuda = -1, False
+        with pytest.raises(TypeError):
+            f(*a)
+        t.device, t.is_cuda = 0, True
+
+
+def test_the_current_device_may_be_any(monkeypatch):
+    monkeypatch.setattr(B, "_get_device", lambda: 1)
+    p = pool(Tensor(U8, 8, 64 * 576 * 2, device=1))
+    f, a = arguments(p)["decode"]
+    with pytest.raises(ValueError, match="another device"):
+        f(*a)
+    for x in a:
+        if isinstance(x, Tensor):
+            x.device = 1
+    with pytest.raises(jf.JfError) as e:
+        f(*a)
+    assert e.value.status == B.JF_ERR_WORKSPACE_TOO_SMALL
 
 
 @pytest.mark.parametrize("call", [jf.jf_kv8_append, jf.jf_kv8_read])
