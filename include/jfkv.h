@@ -732,7 +732,12 @@ int jf_latent_prefix_decode_attn(const jf_kv_pool* pool, const int32_t* prefix_t
 
 /* Workspace bytes of jf_latent_prefill_attn: the heads' expanded keys and values
  * (512 bytes a position and head, as many heads at a time as fill the GPU) and the
- * parts of a divided history.  num_sms as above.  0 for invalid arguments. */
+ * parts of a divided history.  A short chunk fills the GPU with more heads than a
+ * long one, so the size does not grow with every argument; but a call takes any
+ * workspace that holds one head, (q_start, chunk_len, 1), which depends on q_start +
+ * chunk_len alone and grows with it, and goes over the heads in more passes.  So one
+ * workspace, made for a prompt's last chunk or for any as far into it, serves all of
+ * the prompt's chunks.  num_sms as above.  0 for invalid arguments. */
 size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int32_t num_heads,
                                          int32_t num_sms);
 
@@ -747,9 +752,10 @@ size_t jf_latent_prefill_workspace_bytes(int32_t q_start, int32_t chunk_len, int
  *                   rotated ones
  *   w_k, w_v        bf16 [num_heads, 128, R]
  *   out             bf16 [chunk_len, num_heads, 128]
- *   workspace       >= jf_latent_prefill_workspace_bytes(q_start, chunk_len,
- *                   num_heads, 0) bytes, 256-byte aligned; its first int32 is the
- *                   device status word, zero before the first call
+ *   workspace       jf_latent_prefill_workspace_bytes(q_start, chunk_len,
+ *                   num_heads, 0) bytes, or fewer as said there, 256-byte aligned;
+ *                   its first int32 is the device status word, zero before the
+ *                   first call
  * All 16-byte aligned; num_heads <= 1024; q_start + chunk_len <=
  * JF_LATENT_MAX_POSITIONS.
  * A page outside the pool sets JF_DEV_ERR_PAGE_ID; the outputs that attend its

@@ -904,7 +904,8 @@ def jf_latent_prefill_workspace_bytes(q_start: int, chunk_len: int, num_heads: i
 
 
 def latent_prefill_workspace(q_start: int, chunk_len: int, num_heads: int, device="cuda") -> torch.Tensor:
-    """A workspace for jf_latent_prefill_attn."""
+    """A workspace for jf_latent_prefill_attn: for this chunk and, with more passes over the heads if need be, any
+    other that ends no further into the cache."""
     n = jf_latent_prefill_workspace_bytes(q_start, chunk_len, num_heads)
     if n == 0:
         raise ValueError("invalid workspace geometry")

@@ -913,7 +913,8 @@ int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row
   if (!aligned(q, 16) || !aligned(w_k, 16) || !aligned(w_v, 16) || !aligned(out, 16) ||
       !aligned(workspace, 256))
     return JF_ERR_INVALID_ARG;
-  if (workspace_bytes < jf_latent_prefill_workspace_bytes(q_start, chunk_len, num_heads, 0))
+  // a head at a time at least
+  if (workspace_bytes < jf_latent_prefill_workspace_bytes(q_start, chunk_len, 1, 0))
     return JF_ERR_WORKSPACE_TOO_SMALL;
   LatentPrefill a;
   a.pool = latent_pool(*pool);
@@ -928,7 +929,7 @@ int jf_latent_prefill_attn(const jf_kv_pool* pool, const int32_t* page_table_row
   a.causal = causal;
   a.scale_log2 = softmax_scale * 1.4426950408889634f;
   a.status = static_cast<int32_t*>(workspace);
-  return launch_latent_prefill(a, workspace, static_cast<cudaStream_t>(stream));
+  return launch_latent_prefill(a, workspace, workspace_bytes, static_cast<cudaStream_t>(stream));
 }
 
 // ---------------------------------------------------------------------------

@@ -61,7 +61,7 @@ int launch_latent_rows(const LatentPool& pool, const int32_t* page_table, int32_
                        void* latent, int64_t latent_stride, void* k_rot, int64_t rot_stride,
                        int32_t n_rows, int32_t* err, bool read, cudaStream_t stream);
 int launch_latent_decode(const LatentDecode& a, void* workspace, cudaStream_t stream);
-int launch_latent_prefill(const LatentPrefill& a, void* workspace, cudaStream_t stream);
+int launch_latent_prefill(const LatentPrefill& a, void* workspace, size_t workspace_bytes, cudaStream_t stream);
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   uint32_t r;

@@ -1035,12 +1035,15 @@ static int64_t heads_per_pass(int64_t n_pad, int64_t C, int64_t H, int64_t pairs
 
 static int64_t padded(int64_t n) { return (n + 255) / 256 * 256; }
 
-size_t latent_prefill_workspace_bytes(int64_t q_start, int64_t C, int64_t H, int64_t sms) {
-  const int64_t pairs = sms / 2, n_pad = padded(q_start + C);
-  if (C == 0) return 256;
-  const int64_t heads = heads_per_pass(n_pad, C, H, pairs);
+// what a pass of so many heads takes
+static size_t pass_bytes(int64_t n_pad, int64_t heads, int64_t pairs) {
   return (size_t)(256 + round256(heads * n_pad / 8) + round256(heads * n_pad / 32) + 2 * pairs * LP_Q * (16 + 512) +
                   heads * n_pad * 512);
+}
+
+size_t latent_prefill_workspace_bytes(int64_t q_start, int64_t C, int64_t H, int64_t sms) {
+  const int64_t pairs = sms / 2, n_pad = padded(q_start + C);
+  return C == 0 ? 256 : pass_bytes(n_pad, heads_per_pass(n_pad, C, H, pairs), pairs);
 }
 
 template <typename... P, typename... A>
@@ -1059,7 +1062,7 @@ static int launch(void (*kernel)(P...), dim3 grid, int threads, int smem, cudaSt
   return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? JF_OK : JF_ERR_CUDA;
 }
 
-int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t stream) {
+int launch_latent_prefill(const LatentPrefill& p, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
   const int pairs = sm_count() / 2;
   if (pairs > LJ_MAX) return JF_ERR_UNSUPPORTED;
   LatentChunk a{};
@@ -1083,7 +1086,10 @@ int launch_latent_prefill(const LatentPrefill& p, void* workspace, cudaStream_t 
   // as chunk_start() has it, and the last query tile's
   a.units_head = (a.causal ? (q_tiles - 1) * (q_tiles - 2) + (q_tiles - 1) * (2 + before + LP_HDR)
                            : (q_tiles - 1) * (tiles + LP_HDR)) + tiles + LP_HDR;
-  const int64_t per = heads_per_pass(n_pad, p.C, p.H, pairs);
+  // The caller's workspace may be one for another chunk of the same prompt, and that a smaller one: a short chunk
+  // takes more heads at a time than a long one.
+  int64_t per = heads_per_pass(n_pad, p.C, p.H, pairs);
+  while (per > 1 && pass_bytes(n_pad, per, pairs) > workspace_bytes) --per;
   uint8_t* ws = static_cast<uint8_t*>(workspace) + 256;
   a.bad = reinterpret_cast<int32_t*>(ws);
   ws += round256(per * n_pad / 8);
