@@ -172,7 +172,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
             for (int k = 0; k < 4; ++k)
               mma2_ss_if(leader, d, at + ((k * 32) >> 4), bt + ((k * 32) >> 4), ID,
                          (s > 0 || k > 0) ? 1u : 0u);
-            tc::commit2_both_if(leader, &b_free[st]);
+            if (t * steps + s < count * steps - LE_STAGES) tc::commit2_both_if(leader, &b_free[st]);   // waited for
           }
           if (++st == LE_STAGES) {
             st = 0;
@@ -181,7 +181,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
         }
         if (fresh) ++na;
         advance();
-        if (ok && hl == 0) tc::commit2_both_if(leader, a_free);
+        if (ok && hl == 0 && t + 1 < count) tc::commit2_both_if(leader, a_free);   // waited for
         if (ok) tc::commit2_both_if(leader, &d_full[t & 1]);
       }
       for (int t = max(0, count - 2); t < count && ok; ++t) ok = wait(&d_free[t & 1], t >> 1);
@@ -362,10 +362,12 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   }
-  // neither CTA may release TMEM or exit while its partner can still reach it
+  // Neither CTA may release TMEM or exit while its partner can still reach it.  CTA 1's arrivals were all waited
+  // for, the last ones at the issuer's end, the products' at d_full on the way out, at b_free and a_free by the
+  // next copies: where none is to come, no arrival is asked for.
   tc::fence_before();
   settle(ok);
-  cluster_meet();   // CTA 1's arrivals were all waited for, the last ones at the issuer's end
+  cluster_meet();
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);
@@ -376,7 +378,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
 // Attention
 // ===========================================================================
 constexpr int LA_THREADS = 32 * 12;
-constexpr int LA_KS = 3, LA_VS = 4, LA_SB = 3;
+constexpr int LA_KS = 3, LA_VS = 4, LA_SB = 3;   // LA_VS: also of pv_done
 struct LaSmem {
   static constexpr int Q_BYTES = 3 * 128 * 128;         // [64-channel chunk][128 rows][128 B]
   static constexpr int K_BYTES = 3 * 64 * 128;          // [64-channel chunk][64 positions][128 B]
@@ -477,10 +479,9 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   uint64_t* const v_land = bars + 15;    // [4]
   uint64_t* const q_land = bars + 19;
   uint64_t* const k_free = bars + 20;    // [3] stage read
-  uint64_t* const v_free = bars + 23;    // [4]
+  uint64_t* const pv_done = bars + 23;   // [4] P V of tile t % 4, and so V's stage read
   uint64_t* const q_free = bars + 27;    // products with a segment's Q done
   uint64_t* const s_full = bars + 28;    // [3] S of tile t % 3
-  uint64_t* const pv_done = bars + 31;   // [4] P V of tile t % 4
   // [4][4 quarters] the reference after tile t % 4 is set.  (One barrier a group would do but for a
   // group that takes O out: the other may be two of its tiles on, and a parity then says no for ever.)
   uint64_t* const m_bar = bars + 35;
@@ -588,7 +589,6 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
             for (int k = 0; k < LP_T / 16; ++k)
               tc::mma2_ts_if(leader, tO, p + 8 * k, v0 + ((k * 2048) >> 4), IDPV,
                              (!fresh_o || k > 0) ? 1u : 0u);
-            tc::commit2_both_if(leader, &v_free[st]);
             tc::commit2_both_if(leader, &pv_done[pi & 3]);
           }
           fresh_o = false;
@@ -620,15 +620,19 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= K: this CTA's 64 positions of each tile =================
     if (lane == 0) {
       int t = 0;
-      for (; ok && more; more = next_chunk_seg(a, run, sg)) {
-        int y = half_row(a.pool, a.pt, sg.j0 * LP_T + 64 * (int)rank, a.n, a.status);
-        for (int j = sg.j0; j < sg.j1; ++j, ++t) {
+      for (;; more = next_chunk_seg(a, run, sg)) {
+        // after the last segment a turn over the ring that waits and brings nothing: each stage's last products
+        // have told both CTAs before either ends
+        const int j0 = more ? sg.j0 : 0, j1 = more ? sg.j1 : LA_KS;
+        int y = more ? half_row(a.pool, a.pt, j0 * LP_T + 64 * (int)rank, a.n, a.status) : 0;
+        for (int j = j0; j < j1; ++j, ++t) {
           const int row = y, st = t % LA_KS, pos = j * LP_T + 64 * (int)rank;
-          if (j + 1 < sg.j1) y = half_row(a.pool, a.pt, pos + LP_T, a.n, a.status);
+          if (more && j + 1 < j1) y = half_row(a.pool, a.pt, pos + LP_T, a.n, a.status);
           if (t >= LA_KS && !mbar_wait_bounded(&k_free[st], (t / LA_KS - 1) & 1)) {
             ok = false;
             break;
           }
+          if (!more) continue;
           uint64_t* const land = rank == 0 ? &k_full[st] : &k_land[st];
           mbar_arrive_expect_tx(land, L::K_BYTES);
           const uint32_t dst = smem_u32(sm + L::OFF_K + st * L::K_BYTES);
@@ -637,6 +641,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           tma_load_2d(dst + 8192, &kmap, 64, at, land);
           tma_load_2d(dst + 16384, &pmap, a.pool.R, row, land);
         }
+        if (!more || !ok) break;
       }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     }
@@ -645,18 +650,22 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= V: this CTA's 64 channels of all 128 positions =================
     if (lane == 0) {
       int t = 0;
-      for (; ok && more; more = next_chunk_seg(a, run, sg))
-        for (int j = sg.j0; j < sg.j1; ++j, ++t) {
+      for (;; more = next_chunk_seg(a, run, sg)) {
+        const int j0 = more ? sg.j0 : 0, j1 = more ? sg.j1 : LA_VS;   // a last turn, as K's
+        for (int j = j0; j < j1; ++j, ++t) {
           const int st = t % LA_VS;
-          if (t >= LA_VS && !mbar_wait_bounded(&v_free[st], (t / LA_VS - 1) & 1)) {
+          if (t >= LA_VS && !mbar_wait_bounded(&pv_done[st], (t / LA_VS - 1) & 1)) {
             ok = false;
             break;
           }
+          if (!more) continue;
           uint64_t* const land = rank == 0 ? &v_full[st] : &v_land[st];
           mbar_arrive_expect_tx(land, L::V_BYTES);
           tma_load_2d(smem_u32(sm + L::OFF_V + st * L::V_BYTES), &vmap, 64 * (int)rank,
                       sg.hl * a.n_pad + j * LP_T, land);
         }
+        if (!more || !ok) break;
+      }
       if (!ok) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
     }
     __syncwarp();
@@ -664,11 +673,12 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     // ================= Q: 128 rows; zeros past the chunk's end =================
     if (lane == 0) {
       int nseg = 0;
-      for (; ok && more; more = next_chunk_seg(a, run, sg)) {
+      for (; ok; more = next_chunk_seg(a, run, sg)) {
         if (nseg > 0 && !mbar_wait_bounded(q_free, (nseg - 1) & 1)) {
           ok = false;
           break;
         }
+        if (!more) break;
         ++nseg;
         uint64_t* const land = rank == 0 ? q_full : q_land;
         mbar_arrive_expect_tx(land, L::Q_BYTES);
@@ -904,10 +914,12 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
     }
     if (!ok && lane == 0) flag_error(a.status, JF_DEV_ERR_TIMEOUT);
   }
-  // neither CTA may release TMEM or exit while its partner can still reach it
+  // Neither CTA may release TMEM or exit while its partner can still reach it.  CTA 1's arrivals were all waited
+  // for, the last ones at the issuer's end, the products' at k_free, pv_done and q_free by the copies' last turns,
+  // at s_full by the softmax.
   tc::fence_before();
   settle(ok);
-  cluster_meet();   // CTA 1's arrivals were all waited for, the last ones at the issuer's end
+  cluster_meet();
   if (warp == 0) {
     tc::fence_after();
     tc::dealloc2(*tmem_slot, 512);

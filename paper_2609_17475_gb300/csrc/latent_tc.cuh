@@ -102,16 +102,18 @@ __device__ __forceinline__ void sts128(uint32_t addr, uint32_t x, uint32_t y, ui
                ::"r"(addr), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
-// The block's end, all threads together.  Where a wait gave up, copies and products may still be under
-// way: they get a millisecond, a thousand times what they take, before the memory is released.
-__device__ __forceinline__ void settle(bool ok) {
-  if (__syncthreads_or(!ok))
-    for (int i = 0; i < 100; ++i) __nanosleep(10000);
+// The block's end, all threads together; whether no wait gave up.  Where one did, copies and products may still
+// be under way: they get a millisecond, a thousand times what they take, before the memory is released.
+__device__ __forceinline__ bool settle(bool ok) {
+  if (!__syncthreads_or(!ok)) return true;
+  for (int i = 0; i < 100; ++i) __nanosleep(10000);
+  return false;
 }
 
 // Both CTAs of the pair are here.  Relaxed: nothing is handed over, and a release would first wait for
-// this CTA's stores to reach memory, which the kernel's end does anyway.  Only where every arrival at the
-// partner's barriers has been waited for there: nothing orders one still on its way.
+// this CTA's stores to reach memory, which the kernel's end does anyway.  Only where every arrival at either
+// CTA's barriers has been waited for there, those of the products' commits among them: nothing orders one
+// still on its way, not the one of a later commit.
 __device__ __forceinline__ void cluster_meet() {
   asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;\n" ::: "memory");
 }

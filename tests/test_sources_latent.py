@@ -35,6 +35,41 @@ def test_no_block_ends_before_the_join_has_waited():
     assert "return" not in body[:body.index("griddepcontrol.wait")]
 
 
+def kernels(name):
+    """The bodies of a file's kernels that run on CTA pairs."""
+    with open(os.path.join(CSRC, name)) as f:
+        text = f.read()
+    return [t for t in re.split(r"__global__", text)[1:] if "__cluster_dims__" in t[:80] and "commit2_both_if" in t]
+
+
+def commits(body):
+    """(the condition before a commit to both CTAs, its first argument, the barrier's name)"""
+    out = []
+    for m in re.finditer(r"(?:if \(([^;{}]*)\) )?tc::commit2_both_if\((.+?), &?(\w+)[^,;]*\);", body):
+        out.append((m.group(1) or "", m.group(2), m.group(3)))
+    assert len(out) == len(arguments(body, "commit2_both_if"))
+    return out
+
+
+def test_no_arrival_is_on_its_way_when_a_pair_parts():
+    """The products' commits arrive in both CTAs, no two of them in order: a CTA whose barriers one may still be on
+    its way to must not end.  Each barrier's every phase is waited for: of scores and outputs by the softmax (or the
+    way out); of the stages by the copies that fill them again, and where none will, either no arrival is asked for,
+    or the copies go round once more and wait."""
+    (decode,), (expand, attend) = kernels("latent_decode.cu"), kernels("latent_prefill.cu")
+    want = {"k_free": "qi < again ? leader : 0u", "v_free": "pi < again ? leader : 0u", "q_free": "next > 0 ? leader : 0u"}
+    for _, leader, name in commits(decode):
+        assert leader == want.get(name, "leader") and (name in want or name in ("s_full", "pv_done")), (leader, name)
+    want = {"b_free": "t * steps + s < count * steps - LE_STAGES", "a_free": "ok && hl == 0 && t + 1 < count", "d_full": "ok"}
+    for cond, _, name in commits(expand):
+        assert cond == want[name]
+    assert {name for _, _, name in commits(attend)} == {"s_full", "k_free", "q_free", "pv_done"}
+    for ring in ("k_free", "pv_done"):   # waited for, and after the last segment nothing else
+        assert re.search(r"!mbar_wait_bounded\(&%s\[st\][^;]*\{\s*ok = false;\s*break;\s*\}\s*if \(!more\) continue;" % ring, attend)
+    assert re.search(r"!mbar_wait_bounded\(q_free[^;]*\{\s*ok = false;\s*break;\s*\}\s*if \(!more\) break;", attend)
+    assert attend.count("if (!more || !ok) break;") == 2
+
+
 @pytest.mark.parametrize("name", FILES)
 def test_waits_are_bounded(name):
     """Barriers in memory are waited for with a limit (a poll that is its own loop counts its turns)."""
