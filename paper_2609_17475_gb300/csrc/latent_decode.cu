@@ -325,10 +325,6 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
   const int pair = (int)(blockIdx.x >> 1);
-  if (smem_u32(sm) & 1023u) {   // the swizzled layouts need it; the same in every CTA
-    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
-    return;
-  }
   if (threadIdx.x == 0) {
     prefetch_tensormap(&kmap);
     prefetch_tensormap(&vmap);
@@ -359,6 +355,10 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
   // The first segment is worked out here, in one copy of that code for all roles: it is fetched when it
   // first runs (the roles' own copies took 2,000 to 2,500 cycles for it, 1 us).
   SegIter run = plan_run(a, pl, pair, warp, lane, s_plan, s_first);
+  if (smem_u32(sm) & 1023u) {   // the swizzled layouts need it: no work, but the plan stands, which the joins read
+    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
+    run.item = pl.items;
+  }
   Seg sg;
   bool more = next_seg(a, pl, run, sg);
   asm volatile("barrier.cluster.wait.acquire.aligned;\n" ::: "memory");   // both CTAs: barriers, TMEM

@@ -115,10 +115,6 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
   const uint32_t pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-  if (smem_u32(sm) & 1023u) {   // the same in both CTAs
-    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
-    return;
-  }
   if (warp == 0) {
     tc::alloc2(tmem_slot, 512);
   } else if (warp == 1) {   // a barrier a thread
@@ -133,7 +129,8 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   const uint32_t tiles = (uint32_t)(a.n_pad / 256) * (uint32_t)a.heads;
   const uint32_t i0 = tiles * pair / pairs, i1 = tiles * (pair + 1) / pairs;
   int pt = (int)(i0 / a.heads), hl = (int)(i0 - pt * a.heads);   // of the current tile
-  const int count = (int)(i1 - i0), steps = a.pool.R / 64;
+  const bool placed = !(smem_u32(sm) & 1023u);   // the swizzled layouts need it; the same in both CTAs
+  const int count = placed ? (int)(i1 - i0) : 0, steps = a.pool.R / 64;
   tc::fence_before();
   __syncthreads();
   tc::cluster_sync();   // both CTAs: barriers initialized, TMEM allocated
@@ -146,6 +143,7 @@ latent_expand_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_cons
   };
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // what came before has been written
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (!placed && threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
 
   bool ok = true;
   if (warp == 0) {
@@ -493,10 +491,6 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   const int lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_rank();
   const int pair = (int)(blockIdx.x >> 1);
-  if (smem_u32(sm) & 1023u) {   // the same in both CTAs
-    if (threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
-    return;
-  }
   if (warp == 0) {
     tc::alloc2(tmem_slot, 512);
   } else if (warp == 1) {   // a barrier a thread
@@ -512,6 +506,8 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   // the first segment, in one copy of that code for all roles: it is fetched when it first runs
   ChunkIter run = chunk_run(a, pair);
   ChunkSeg sg;
+  const bool placed = !(smem_u32(sm) & 1023u);   // the swizzled layouts need it; the same in both CTAs
+  if (!placed) run.hl = a.heads;                 // no work
   bool more = next_chunk_seg(a, run, sg);
   tc::fence_before();
   __syncthreads();
@@ -519,6 +515,7 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
   tc::fence_after();
   asm volatile("griddepcontrol.wait;\n" ::: "memory");   // the keys and values have been written
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (!placed && threadIdx.x == 0) flag_error(a.status, JF_DEV_ERR_LAYOUT);
   // all 512 columns are this CTA's: O from 0, the S buffers behind it
   constexpr uint32_t tO = 0, tS = 128;
 

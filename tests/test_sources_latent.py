@@ -28,6 +28,17 @@ def test_kernels_wait_for_what_came_before_them(name):
     assert len(re.findall(r"__global__", text)) == len(re.findall(r"griddepcontrol\.wait", text))
 
 
+@pytest.mark.parametrize("name", FILES)
+def test_no_block_ends_before_it_has_waited(name):
+    """Nor does one leave out what the next kernel reads: a block that gives up early still waits for its predecessor,
+    and the decode's first one writes the plan by which the join finds its way."""
+    with open(os.path.join(CSRC, name)) as f:
+        for body in re.split(r"__global__", f.read())[1:]:
+            assert not re.search(r"\breturn;", body[:body.index("griddepcontrol.wait")])
+            if "plan_run(" in body:
+                assert not re.search(r"\breturn;", body[:body.index("plan_run(")])
+
+
 def test_no_block_ends_before_the_join_has_waited():
     """The next kernel takes the join's end for the end of the attention before it."""
     with open(os.path.join(CSRC, "latent_prefill.cu")) as f:
