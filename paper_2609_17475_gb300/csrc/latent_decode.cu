@@ -598,7 +598,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
       float m = -INFINITY, l = 0.f;
       int live = live_of(sg, sg.j0);
       for (int j = sg.j0; j < sg.j1; ++j, ++t) {
-        if (ok) ok = mbar_wait_bounded(&s_full[t % LD_SBUF], (t / LD_SBUF) & 1);
+        ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(&s_full[t % LD_SBUF], (t / LD_SBUF) & 1)) != 0;
         tc::fence_after();
         uint32_t s[32];
         tc::ld32(tS + (t % LD_SBUF) * 64 + side * 32 + lane_off, s);
@@ -639,7 +639,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
           sum = add_f32x2(sum, f32x2(bf16lo_to_f32(p[c]), bf16hi_to_f32(p[c])));
         }
         if (j > sg.j0) {   // P is free, and O complete up to the last tile
-          if (ok) ok = mbar_wait_bounded(pv_done, (t - 1) & 1);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(pv_done, (t - 1) & 1)) != 0;
           if (__any_sync(0xffffffffu, up)) {
             tc::fence_after();
             const float f = up && m != -INFINITY ? fast_exp2(m - m_new) : 1.f;
@@ -670,7 +670,7 @@ latent_decode_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_cons
         l += u + v;
       }
       more = later_seg(a, pl, run, nx);
-      if (ok) ok = mbar_wait_bounded(pv_done, (t - 1) & 1);
+      ok = ok && __all_sync(0xffffffffu, mbar_wait_bounded(pv_done, (t - 1) & 1)) != 0;
       tc::fence_after();
       float* const sx = s_x + (t & 1) * 256;
       sx[tid] = l;

@@ -62,6 +62,16 @@ def commits(body):
     return out
 
 
+def test_warps_are_whole_where_tensor_memory_is_read():
+    """Reads and writes of tensor memory are a whole warp's: a wait before them that lanes may leave one by one brings
+    them together again."""
+    (decode,), (expand, attend) = kernels("latent_decode.cu"), kernels("latent_prefill.cu")
+    for body, role in ((decode, "softmax, O"), (expand, "out: warps 4-7"), (attend, "softmax: group 0")):
+        body = body[body.index(role):]
+        waits = arguments(body[:body.index("cluster_meet")], "mbar_wait_bounded")
+        assert waits and len(waits) == len([a for a in arguments(body, "__all_sync") if "mbar_wait_bounded" in a])
+
+
 def test_no_arrival_is_on_its_way_when_a_pair_parts():
     """The products' commits arrive in both CTAs, no two of them in order: a CTA whose barriers one may still be on
     its way to must not end.  Each barrier's every phase is waited for: of scores and outputs by the softmax (or the
