@@ -867,7 +867,7 @@ latent_merge_kernel(const __grid_constant__ LatentDecode a, const __grid_constan
       const int64_t units = *pl.units;
       int count = 0;
       bool direct = false;
-      for (int part = a.num_groups ? 0 : 1; part < 2; ++part) {
+      for (int part = CH < R && a.num_groups ? 0 : 1; part < 2; ++part) {   // CH = R: no prefixes
         int item, inside;
         if (part == 0) {
           int g = 0;
