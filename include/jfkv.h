@@ -698,7 +698,8 @@ size_t jf_latent_workspace_bytes(int32_t batch, int32_t num_heads, int32_t laten
  * draw no weight (JF_DEV_ERR_PAGE_ID).  Several tokens of one request (a draft's,
  * say) go in as requests with the same page-table row and a context length each.
  * Numerics: products of the bf16 values in fp32; maxima, sums and outputs in
- * fp32.  The weights enter their product with c as bf16 (2^-8 of each), and the
+ * fp32 (scores times log2 e are to stay below 2^24, where fp32 tells neighbours
+ * apart).  The weights enter their product with c as bf16 (2^-8 of each), and the
  * sum they are divided by is that of the rounded ones.
  */
 int jf_latent_decode_attn(const jf_kv_pool* pool, const int32_t* page_table, int32_t pt_stride,

@@ -18,15 +18,15 @@
 // any length.
 //
 // What bounds it: memory, the products and what of one the other cannot hide.  32 requests to
-// 65,535 positions x 16 heads take 101 us: their 593 MB 87 at copy rate, the same launch without
+// 65,535 positions x 16 heads take 99 to 104 us: their 593 MB 87 at copy rate, the same launch without
 // its loads 80 (2,500 cycles a tile of R = 512 where its products are 2,176).  All of K's and V's
 // shared memory holds one tile each, the next one's K is on its way into the L2 cache, and every
 // position crosses from there twice, as K and as V: 137 KB a tile and CTA, 12 TB/s in all.  One
 // request of 131,072 positions x 128 heads takes 41 us: a tile passes at memory's rate (1.68 us;
 // 22.2 for all), before it the plan and the first copies, after it 128 rows x R of every pair
-// go out (2.6) and are joined (6).  Short calls are latency: 10.3 us for one request of 4,096 positions
+// go out (2.6) and are joined (6).  Short calls are latency: 10.0 us for one request of 4,096 positions
 // are the plan (1.0 us), a page's look-up, the copies and S (1.9), softmax and P V (1.3), O out
-// (1.0), and set-up, two launches and the join (5.1).
+// (1.0), and set-up, two launches and the join (4.8).
 //
 // Warp roles (each CTA):
 //   warp 0     TMEM; CTA 0: issues the pair's MMAs; CTA 1: passes its K and Q arrivals on

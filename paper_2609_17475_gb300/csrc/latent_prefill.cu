@@ -20,8 +20,8 @@
 // is at the next item's first.  Keys and queries multiply as bf16; values and weights as
 // fp16, whose three more bits they need: in bf16 the two roundings weighed as much as the
 // output's own (a whole prompt of 4,095 off by 0.0026 of its norm for the 0.0017 of
-// rounding exact values).  fp16's range is not bf16's, so a tile's 128 values of a head are
-// held as v 2^-e, e a whole number that puts the largest between 2^14 and 2^15, and a
+// rounding exact values).  fp16's range is not bf16's, so a head's values of a tile of 128
+// positions are held as v 2^-e, e a whole number that puts the largest between 2^14 and 2^15, and a
 // position counts by s + e: its weight is 2^(s + e - m), and O = sum of weight times held
 // value is in units of 2^m whatever e.  A row's reference m is a whole number too (powers of
 // two change no other bits), set so that the largest weight is about 2^10; it moves, O's row
@@ -31,11 +31,11 @@
 // 2^-20 gave outputs off by 0.017 of their norm, of 2^-30 zeros.)
 //
 // What bounds it: the tensor cores at the power they may take.  2,048 queries after 30,720
-// positions x 16 heads take 462 us; each kernel alone: expansion 81 (137 GFLOP, 1,700 TFLOP/s, the
-// tensor pipe 78 % active), attention 385 (667 GFLOP, 1,730 TFLOP/s, 91 %), the join 9.  Expanding costs 2 R
+// positions x 16 heads take 467 to 487 us; each kernel alone: expansion 81 (137 GFLOP, 1,690 TFLOP/s, the
+// tensor pipe 73 % active), attention 392 (667 GFLOP, 1,700 TFLOP/s, 91 %), the join 9.  Expanding costs 2 R
 // 256 operations a position and head once and saves 1,536 of 2,176 a (query, position) pair of the
 // absorbed form: from about 170 queries on it is less.  Below that (77 queries after 4,001 x 16
-// heads: 31.6 us, expansion 13, attention 11, join 3) the absorbed form's products would be 6 us
+// heads: 32.7 us, with their launches expansion 15, attention 13, join 5) the absorbed form's products would be 6 us
 // against 11, but it would need two products with the weights around the decode and its join.
 //
 // Work: the (head, 256 queries) items' tiles, and a header each, are laid end to end and
