@@ -734,14 +734,17 @@ latent_prefill_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_con
           tc::ld32(tb + c0 + 32, s[1]);
           tc::wait_ld();
           if (!plain) {
+            if (!(a.scale_log2 > 0.f)) {   // of a scale below zero the sign, of one of zero nothing (or NaN)
+#pragma unroll
+              for (int c = 0; c < 64; ++c) {
+                const uint32_t w = s[c >> 5][c & 31];
+                s[c >> 5][c & 31] = a.scale_log2 < 0.f ? w ^ 0x80000000u : __float_as_uint(__uint_as_float(w) * 0.f);
+              }
+            }
             const int seen = limit - key0 - c0;
 #pragma unroll
-            for (int c = 0; c < 64; ++c) {
-              uint32_t w = s[c >> 5][c & 31];
-              if (a.scale_log2 < 0.f) w ^= 0x80000000u;
-              if (a.scale_log2 == 0.f) w = __float_as_uint(__uint_as_float(w) * 0.f);
-              s[c >> 5][c & 31] = c > seen ? 0xFF800000u : w;
-            }
+            for (int c = 0; c < 64; ++c)
+              if (c > seen) s[c >> 5][c & 31] = 0xFF800000u;
             tc::st32(tb + c0, s[0]);
             tc::st32(tb + c0 + 32, s[1]);
             tc::wait_st();
