@@ -64,7 +64,8 @@ extern "C" {
                                      fp16 reconstruction can overflow
                                      (|bias| + 15 scale >= 65504, or a
                                      non-finite scale/bias word): outputs
-                                     reading it are not reliable           */
+                                     reading it are not reliable; of a
+                                     latent prefill a notice alone         */
 #define JF_DEV_ERR_LAYOUT     8   /* the kernel's dynamic shared-memory
                                      window was not 1024-byte aligned (the
                                      swizzled copies need it); the CTA did
